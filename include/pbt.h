@@ -483,6 +483,71 @@ int pbt_selftest_bounded_wait(void* status_device, int polls, void* stream);
 int pbt_energy_fitness_static(const float* x_device, int n, int n_members, float* fitness_out_device,
                               void* stream);
 
+/*
+ * Global gradient norm over many tensors, and clipping, per group (one group per population member, or one for all):
+ *   norm_g = sqrt(sum of e^2 over all elements of the tensors of group g),  dst = src * min(1, limit_g / norm_g).
+ * The tensors of a handle are described once (they are where the gradients live, like the slabs of a population) and
+ * read anew by every pbt_clip_run.  A tensor may be clipped in place (dst == src) or into another buffer of its type;
+ * a destination that overlaps anything else of the call is refused.  Any element alignment and any size, zero included.
+ * A NaN in a group makes its norm and every clipped element NaN (a diverged member stays visible: NaN ranks last at the
+ * next ready point); an infinite element gives an infinite norm (finite elements become 0, infinite ones NaN); an
+ * infinite limit leaves the gradients as they are.  Sums are reproducible bit for bit.
+ */
+typedef struct pbt_clip_tensor {
+  const void* src; void* dst;   /* device */
+  int64_t numel;
+  int32_t dtype;                /* 0 float, 1 bfloat16 */
+  int32_t group;                /* 0 .. n_groups - 1 */
+} pbt_clip_tensor;
+typedef struct pbt_clip pbt_clip_t;
+/* Bytes of device workspace (256-byte aligned base) that pbt_clip_create needs.  tensors_host: host array. */
+int pbt_clip_query_workspace(const pbt_clip_tensor* tensors_host, int32_t n_tensors, int32_t n_groups, size_t* bytes);
+/* Uploads the table of the tensors into the workspace (which the caller keeps until pbt_clip_destroy); synchronises. */
+int pbt_clip_create(pbt_clip_t** out, const pbt_clip_tensor* tensors_host, int32_t n_tensors, int32_t n_groups,
+                    void* workspace, size_t workspace_bytes, void* stream);
+int pbt_clip_destroy(pbt_clip_t* p);
+/*
+ * One pass: norms_out_device [n_groups] floats (before clipping).  The limit is limits_device[g] (device floats, e.g. a
+ * hyperparameter of every member), or `limit` for all groups if limits_device is NULL.  Only enqueues.  The handle's
+ * workspace serves one run at a time: runs on several streams have to be ordered.
+ */
+int pbt_clip_run(pbt_clip_t* p, float limit, const float* limits_device, float* norms_out_device, void* stream);
+
+/*
+ * Norms before and after a residual block, fused with the block's gate and residual scale.  Per member m and row i:
+ *   v = b rsqrt(mean b^2 + eps),  y = x + scale_m sigmoid(gate) (v post_weight_m),
+ *   u = y rsqrt(mean y^2 + eps) next_weight_m
+ * b: the output of the block, x / y: the residual stream before / after it, u: the input of the next block.
+ * block == NULL: only the norm before a block (u from x; y is x and is not written).  u == NULL: only the norm after it.
+ * gate: one logit per element, or (gate_vector) one per member and column, or NULL (sigmoid replaced by 1); scale NULL: 1.
+ * Inputs may have any member and row stride (in elements); columns are contiguous; results are contiguous.  Weights are
+ * float [members][width], scale float [members]; width <= 8192.  Sums are fp32; each result is rounded once.
+ *
+ * Backward, given dy (gradient that reaches y through the residual stream; NULL: zero) and du (NULL: no next norm), with
+ * x holding y and the two reciprocal roots that the forward pass wrote: dx, dblock, dgate (type and shape of gate: summed
+ * over the rows for gate_vector), dpost_weight, dnext_weight (float [members][width]), dscale (float [members] or NULL).
+ */
+typedef struct pbt_block_norm_desc {
+  int32_t members, rows, width;
+  int32_t dtype;                 /* of x, block, gate, y, u and their gradients: 0 float, 1 bfloat16 */
+  int32_t gate_vector;
+  float eps;
+  const void* x; int64_t x_member, x_row;
+  const void* block; int64_t block_member, block_row;
+  const void* gate; int64_t gate_member, gate_row;
+  const float* post_weight; const float* next_weight; const float* scale;
+  void* y; void* u;
+  float* rstd_block; float* rstd_next;   /* [members][rows]; the forward pass writes those that are not NULL */
+  const void* dy; int64_t dy_member, dy_row;
+  const void* du; int64_t du_member, du_row;
+  void* dx; void* dblock; void* dgate;
+  float* dpost_weight; float* dnext_weight; float* dscale;
+} pbt_block_norm_desc;
+int pbt_block_norm_forward(const pbt_block_norm_desc* desc, void* stream);
+/* Bytes of device workspace (256-byte aligned base) of the backward pass of this description. */
+int pbt_block_norm_query_workspace(const pbt_block_norm_desc* desc, size_t* bytes);
+int pbt_block_norm_backward(const pbt_block_norm_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
+
 const char* pbt_last_error(const pbt_t* p); /* p may be NULL: error of the last failed create/query */
 
 #ifdef __cplusplus

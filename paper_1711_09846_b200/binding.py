@@ -75,6 +75,25 @@ class PbtGemmDesc(C.Structure):
                 ("status_device", C.c_void_p)]
 
 
+class PbtClipTensor(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("numel", C.c_int64), ("dtype", C.c_int32),
+                ("group", C.c_int32)]
+
+
+class PbtBlockNormDesc(C.Structure):
+    _fields_ = [("members", C.c_int32), ("rows", C.c_int32), ("width", C.c_int32), ("dtype", C.c_int32),
+                ("gate_vector", C.c_int32), ("eps", C.c_float),
+                ("x", C.c_void_p), ("x_member", C.c_int64), ("x_row", C.c_int64),
+                ("block", C.c_void_p), ("block_member", C.c_int64), ("block_row", C.c_int64),
+                ("gate", C.c_void_p), ("gate_member", C.c_int64), ("gate_row", C.c_int64),
+                ("post_weight", C.c_void_p), ("next_weight", C.c_void_p), ("scale", C.c_void_p),
+                ("y", C.c_void_p), ("u", C.c_void_p), ("rstd_block", C.c_void_p), ("rstd_next", C.c_void_p),
+                ("dy", C.c_void_p), ("dy_member", C.c_int64), ("dy_row", C.c_int64),
+                ("du", C.c_void_p), ("du_member", C.c_int64), ("du_row", C.c_int64),
+                ("dx", C.c_void_p), ("dblock", C.c_void_p), ("dgate", C.c_void_p),
+                ("dpost_weight", C.c_void_p), ("dnext_weight", C.c_void_p), ("dscale", C.c_void_p)]
+
+
 EXPORTS = [
     "pbt_query_workspace", "pbt_param_count", "pbt_create", "pbt_destroy", "pbt_step", "pbt_step_subset", "pbt_eval",
     "pbt_exploit_explore", "pbt_exploit_explore_ready", "pbt_exploit_explore_global", "pbt_set_global_history",
@@ -84,6 +103,8 @@ EXPORTS = [
     "pbt_get_hparams", "pbt_set_hparams", "pbt_get_copy_map", "pbt_get_best", "pbt_get_last_loss",
     "pbt_set_batch", "pbt_step_host", "pbt_prefetch_host_batch", "pbt_step_prefetched", "pbt_get_launch_count", "pbt_profile_begin", "pbt_profile_end", "pbt_profile_get",
     "pbt_grouped_gemm", "pbt_selftest_bounded_wait", "pbt_energy_fitness_static", "pbt_last_error",
+    "pbt_clip_query_workspace", "pbt_clip_create", "pbt_clip_destroy", "pbt_clip_run",
+    "pbt_block_norm_forward", "pbt_block_norm_query_workspace", "pbt_block_norm_backward",
 ]
 
 _LIB = None
@@ -139,6 +160,13 @@ def load_library() -> C.CDLL:
     lib.pbt_grouped_gemm.argtypes = [C.POINTER(PbtGemmDesc), vp]
     lib.pbt_energy_fitness_static.argtypes = [vp, C.c_int, C.c_int, vp, vp]
     lib.pbt_selftest_bounded_wait.argtypes = [vp, C.c_int, vp]
+    lib.pbt_clip_query_workspace.argtypes = [vp, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
+    lib.pbt_clip_create.argtypes = [C.POINTER(vp), vp, C.c_int32, C.c_int32, vp, C.c_size_t, vp]
+    lib.pbt_clip_destroy.argtypes = [vp]
+    lib.pbt_clip_run.argtypes = [vp, C.c_float, vp, vp, vp]
+    lib.pbt_block_norm_forward.argtypes = [C.POINTER(PbtBlockNormDesc), vp]
+    lib.pbt_block_norm_query_workspace.argtypes = [C.POINTER(PbtBlockNormDesc), C.POINTER(C.c_size_t)]
+    lib.pbt_block_norm_backward.argtypes = [C.POINTER(PbtBlockNormDesc), vp, C.c_size_t, vp]
     lib.pbt_last_error.argtypes = [vp]
     lib.pbt_last_error.restype = C.c_char_p
     for name in EXPORTS:
