@@ -548,6 +548,41 @@ int pbt_block_norm_forward(const pbt_block_norm_desc* desc, void* stream);
 int pbt_block_norm_query_workspace(const pbt_block_norm_desc* desc, size_t* bytes);
 int pbt_block_norm_backward(const pbt_block_norm_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Low-rank adapters of many requests, or of many population members, at once beside one shared frozen projection.  Rows
+ * come in segments (a request's tokens, a member's batch): segment j holds rows [row_offsets[j], row_offsets[j + 1]) and
+ * uses adapter a = adapter_ids[j]; an id outside [0, n_adapters) means no adapter.  Offsets ascend (equal ones: an empty
+ * segment), the same adapter may serve many segments, rows in no segment have no adapter; both arrays are device memory
+ * and are read when the kernels run.
+ *   forward   S = x A_a^T (fp32),  y = x W^T + bias + scale_a S B_a^T
+ *   backward  dS = scale_a dy B_a,  dx = dy W + dS A_a,  dA_a = sum dS^T x,  dB_a = scale_a sum dy^T S
+ * W [outputs][inputs] with row stride ld_weight, A [n_adapters][rank][inputs] and B [n_adapters][outputs][rank]
+ * contiguous, x / y / dy / dx with any row stride; all of one type (0 float, 1 bfloat16).  bias float [outputs] or NULL,
+ * scale float [n_adapters].  s float [rows][rank]: written by the forward pass unless NULL (rows without an adapter are
+ * left alone), read by the backward pass.  dA, dB are float in the shapes of A and B, written for every adapter (zero for
+ * one without rows).  Sums are fp32.  rank <= 64.  Elements have to be aligned to their size only.
+ * A row depends on its own segment's adapter alone: NaN or infinite weights of one adapter reach no row of another.
+ */
+typedef struct pbt_adapter_desc {
+  int32_t rows, inputs, outputs, rank, n_adapters, n_segments;
+  int32_t dtype;
+  const void* weight; int64_t ld_weight;
+  const void* A; const void* B;
+  const float* scale; const float* bias;
+  const int32_t* row_offsets;   /* device [n_segments + 1] */
+  const int32_t* adapter_ids;   /* device [n_segments] */
+  const void* x; int64_t ld_x;
+  void* y; int64_t ld_y;
+  float* s;
+  const void* dy; int64_t ld_dy;
+  void* dx; int64_t ld_dx;
+  float* dA; float* dB;
+} pbt_adapter_desc;
+/* Bytes of device workspace (256-byte aligned base) of one forward (backward == 0) or backward call. */
+int pbt_adapter_query_workspace(const pbt_adapter_desc* desc, int backward, size_t* bytes);
+int pbt_adapter_forward(const pbt_adapter_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
+int pbt_adapter_backward(const pbt_adapter_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
+
 const char* pbt_last_error(const pbt_t* p); /* p may be NULL: error of the last failed create/query */
 
 #ifdef __cplusplus

@@ -94,6 +94,16 @@ class PbtBlockNormDesc(C.Structure):
                 ("dpost_weight", C.c_void_p), ("dnext_weight", C.c_void_p), ("dscale", C.c_void_p)]
 
 
+class PbtAdapterDesc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("inputs", C.c_int32), ("outputs", C.c_int32), ("rank", C.c_int32),
+                ("n_adapters", C.c_int32), ("n_segments", C.c_int32), ("dtype", C.c_int32),
+                ("weight", C.c_void_p), ("ld_weight", C.c_int64), ("A", C.c_void_p), ("B", C.c_void_p),
+                ("scale", C.c_void_p), ("bias", C.c_void_p), ("row_offsets", C.c_void_p), ("adapter_ids", C.c_void_p),
+                ("x", C.c_void_p), ("ld_x", C.c_int64), ("y", C.c_void_p), ("ld_y", C.c_int64), ("s", C.c_void_p),
+                ("dy", C.c_void_p), ("ld_dy", C.c_int64), ("dx", C.c_void_p), ("ld_dx", C.c_int64),
+                ("dA", C.c_void_p), ("dB", C.c_void_p)]
+
+
 EXPORTS = [
     "pbt_query_workspace", "pbt_param_count", "pbt_create", "pbt_destroy", "pbt_step", "pbt_step_subset", "pbt_eval",
     "pbt_exploit_explore", "pbt_exploit_explore_ready", "pbt_exploit_explore_global", "pbt_set_global_history",
@@ -105,6 +115,7 @@ EXPORTS = [
     "pbt_grouped_gemm", "pbt_selftest_bounded_wait", "pbt_energy_fitness_static", "pbt_last_error",
     "pbt_clip_query_workspace", "pbt_clip_create", "pbt_clip_destroy", "pbt_clip_run",
     "pbt_block_norm_forward", "pbt_block_norm_query_workspace", "pbt_block_norm_backward",
+    "pbt_adapter_query_workspace", "pbt_adapter_forward", "pbt_adapter_backward",
 ]
 
 _LIB = None
@@ -167,6 +178,9 @@ def load_library() -> C.CDLL:
     lib.pbt_block_norm_forward.argtypes = [C.POINTER(PbtBlockNormDesc), vp]
     lib.pbt_block_norm_query_workspace.argtypes = [C.POINTER(PbtBlockNormDesc), C.POINTER(C.c_size_t)]
     lib.pbt_block_norm_backward.argtypes = [C.POINTER(PbtBlockNormDesc), vp, C.c_size_t, vp]
+    lib.pbt_adapter_query_workspace.argtypes = [C.POINTER(PbtAdapterDesc), C.c_int, C.POINTER(C.c_size_t)]
+    lib.pbt_adapter_forward.argtypes = [C.POINTER(PbtAdapterDesc), vp, C.c_size_t, vp]
+    lib.pbt_adapter_backward.argtypes = [C.POINTER(PbtAdapterDesc), vp, C.c_size_t, vp]
     lib.pbt_last_error.argtypes = [vp]
     lib.pbt_last_error.restype = C.c_char_p
     for name in EXPORTS:

@@ -1,0 +1,253 @@
+// Low-rank adapters of many requests (or members) at once beside one shared, frozen projection:
+//   S = x A_a^T,  y = x W^T + bias + c_a S B_a^T        (a: the adapter of the row's segment)
+//   dS = c_a dy B_a,  dx = dy W + dS A_a,  dA_a = sum dS^T x,  dB_a = c_a sum dy^T S
+// The entry points and the fp32 kernels.
+//
+// fp32: the shared product is the library's fp32-ALU GEMM; the low-rank parts are small beside it (r / K of its work)
+// and each runs as one pass over the rows.
+#include <algorithm>
+
+#include "adapters.cuh"
+
+namespace pbt {
+void set_last_error(const char* msg);
+
+namespace adapters {
+namespace {
+
+template <typename T> __device__ __forceinline__ float to_float(T v) { return (float)v; }
+template <> __device__ __forceinline__ float to_float<bf16>(bf16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T from_float(float v) { return (T)v; }
+template <> __device__ __forceinline__ bf16 from_float<bf16>(float v) { return __float2bfloat16_rn(v); }
+
+// s[row][j] = f sum_k x[row][k] m_a(j, k), one warp per row; m_a is A_a [rank][K] or, TRANS, B_a [K][rank].
+// f: the adapter's scale or 1.
+template <typename T, bool TRANS>
+__global__ void __launch_bounds__(256) k_adapter_shrink_simple(const T* __restrict__ x, long long ldx, int K, const T* __restrict__ mats,
+                                                               int rank, const float* __restrict__ scale, Segments segs,
+                                                               float* __restrict__ s) {
+  pdl_prologue();
+  const int row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (row >= segs.rows) return;
+  const int j = segment_of_row(segs, row);
+  if (j < 0 || row >= segment_begin(segs, j + 1)) return;
+  const int a = segment_adapter(segs, j);
+  if (a < 0) return;
+  const T* xr = x + row * ldx;
+  const T* m = mats + (long long)a * rank * K;
+  const float f = scale ? scale[a] : 1.f;
+  for (int r0 = 0; r0 < rank; r0 += 8) {
+    float acc[8] = {};
+    for (int k = lane; k < K; k += 32) {
+      const float v = to_float(xr[k]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (r0 + i < rank) acc[i] = __fmaf_rn(v, to_float(TRANS ? m[(long long)k * rank + r0 + i] : m[(long long)(r0 + i) * K + k]), acc[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) acc[i] += __shfl_xor_sync(0xFFFFFFFFu, acc[i], o);
+      if (lane == 0 && r0 + i < rank) s[(long long)row * rank + r0 + i] = f * acc[i];
+    }
+  }
+}
+
+// out[row][n] = base[row][n] + f sum_j s[row][j] m_a(n, j); m_a is B_a [N][rank] or, TRANS, A_a [rank][N].  `base` may be
+// `out` itself.
+template <typename T, bool TRANS>
+__global__ void __launch_bounds__(256) k_adapter_expand_simple(const float* base, long long ld_base, T* out, long long ld_out, int N,
+                                                               const T* __restrict__ mats, int rank,
+                                                               const float* __restrict__ scale, Segments segs,
+                                                               const float* __restrict__ s) {
+  pdl_prologue();
+  const int row = blockIdx.x, n = blockIdx.y * 256 + threadIdx.x;
+  __shared__ float sr[kMaxRank];
+  const int j = segment_of_row(segs, row);
+  const int a = j >= 0 && row < segment_begin(segs, j + 1) ? segment_adapter(segs, j) : -1;
+  if (a >= 0 && threadIdx.x < rank) sr[threadIdx.x] = s[(long long)row * rank + threadIdx.x];
+  __syncthreads();
+  if (n >= N) return;
+  float acc = 0.f;
+  if (a >= 0) {
+    const T* m = mats + (long long)a * rank * N;
+    for (int i = 0; i < rank; ++i) acc = __fmaf_rn(sr[i], to_float(TRANS ? m[(long long)i * N + n] : m[(long long)n * rank + i]), acc);
+    if (scale) acc *= scale[a];
+  }
+  out[row * ld_out + n] = from_float<T>(base[row * ld_base + n] + acc);
+}
+
+// g_a(j, n) = f_a sum over the rows of adapter a of s[row][j] v[row][n], written as [rank][N] or, TRANS, [N][rank].
+// A block owns 64 columns of one adapter; its 256 threads take every fourth row and add up in shared memory.
+template <typename T, bool TRANS, int RANK>
+__global__ void __launch_bounds__(256) k_adapter_grad_simple(const T* __restrict__ v, long long ldv, int N, const float* __restrict__ s,
+                                                             int rank, const float* __restrict__ scale, Segments segs,
+                                                             float* __restrict__ g) {
+  pdl_prologue();
+  __shared__ float sum[3][RANK][64];
+  const int col = threadIdx.x & 63, part = threadIdx.x >> 6, n = blockIdx.x * 64 + col, a = blockIdx.y;
+  float acc[RANK] = {};
+  for (int j = 0; j < segs.n; ++j) {
+    if (segment_adapter(segs, j) != a) continue;
+    const int end = segment_begin(segs, j + 1);
+    for (int row = segment_begin(segs, j) + part; row < end; row += 4) {
+      const float x = n < N ? to_float(v[row * ldv + n]) : 0.f;
+      const float* sr = s + (long long)row * rank;
+#pragma unroll
+      for (int i = 0; i < RANK; ++i) if (i < rank) acc[i] = __fmaf_rn(__ldg(sr + i), x, acc[i]);
+    }
+  }
+  if (part > 0)
+#pragma unroll
+    for (int i = 0; i < RANK; ++i) sum[part - 1][i][col] = acc[i];
+  __syncthreads();
+  if (part > 0 || n >= N) return;
+  const float f = scale ? scale[a] : 1.f;
+  float* out = g + (long long)a * rank * N;
+#pragma unroll
+  for (int i = 0; i < RANK; ++i)
+    if (i < rank) out[TRANS ? (long long)n * rank + i : (long long)i * N + n] = f * (acc[i] + sum[0][i][col] + sum[1][i][col] + sum[2][i][col]);
+}
+
+template <typename T, bool TRANS>
+cudaError_t launch_grad_simple(const T* v, long long ldv, int N, const float* s, int rank, const float* scale, const Segments& segs,
+                               float* g, cudaStream_t st) {
+  auto l = launch_with(dim3((N + 63) / 64, segs.n_adapters), 256, 0, st);
+  if (rank <= 8) return l(k_adapter_grad_simple<T, TRANS, 8>, v, ldv, N, s, rank, scale, segs, g);
+  if (rank <= 16) return l(k_adapter_grad_simple<T, TRANS, 16>, v, ldv, N, s, rank, scale, segs, g);
+  if (rank <= 32) return l(k_adapter_grad_simple<T, TRANS, 32>, v, ldv, N, s, rank, scale, segs, g);
+  return l(k_adapter_grad_simple<T, TRANS, 64>, v, ldv, N, s, rank, scale, segs, g);
+}
+
+int fail(int code, const char* msg) {
+  set_last_error(msg);
+  return code;
+}
+
+int check(const pbt_adapter_desc* d) {
+  if (!d) return fail(PBT_ERR_INVALID_ARG, "desc is NULL");
+  if (d->rows < 0 || d->inputs < 1 || d->outputs < 1 || d->n_adapters < 1 || d->n_segments < 0)
+    return fail(PBT_ERR_INVALID_ARG, "inputs, outputs and n_adapters must be positive, rows and n_segments >= 0");
+  if (d->rank < 1 || d->rank > kMaxRank) return fail(PBT_ERR_UNSUPPORTED, "rank must be in [1, 64]");
+  if (d->n_adapters > 65535) return fail(PBT_ERR_UNSUPPORTED, "more than 65535 adapters");
+  if (d->dtype != 0 && d->dtype != 1) return fail(PBT_ERR_UNSUPPORTED, "operands are float or bfloat16");
+  if (!d->weight || !d->A || !d->B || !d->scale || !d->row_offsets || (d->n_segments && !d->adapter_ids))
+    return fail(PBT_ERR_INVALID_ARG, "weight, A, B, scale, row_offsets or adapter_ids is NULL");
+  if (d->ld_weight < d->inputs) return fail(PBT_ERR_INVALID_ARG, "ld_weight is smaller than inputs");
+  return PBT_OK;
+}
+
+size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+struct Layout {
+  size_t s, base, total;
+};
+Layout layout(const pbt_adapter_desc* d, bool backward) {
+  Layout l;
+  const size_t rows = (size_t)d->rows;
+  l.s = 0;                                                   // S of a forward pass that does not keep it, dS
+  l.base = align256(rows * d->rank * sizeof(float));
+  l.total = l.base + (d->dtype ? align256(rows * (backward ? d->inputs : d->outputs) * sizeof(float)) : 0);
+  if (!l.total) l.total = 256;
+  return l;
+}
+
+template <typename T>
+cudaError_t forward_simple(const pbt_adapter_desc* d, const Segments& segs, char* ws, const Layout& l, cudaStream_t st) {
+  float* s = d->s ? d->s : (float*)(ws + l.s);
+  const T *x = (const T*)d->x, *A = (const T*)d->A, *B = (const T*)d->B;
+  cudaError_t e = launch_with((d->rows + 7) / 8, 256, 0, st)(k_adapter_shrink_simple<T, false>, x, d->ld_x, d->inputs, A, d->rank, nullptr, segs, s);
+  if (e != cudaSuccess) return e;
+  float* base = d->dtype ? (float*)(ws + l.base) : (float*)d->y;
+  const long long ld_base = d->dtype ? d->outputs : d->ld_y;
+  GemmArgs g;
+  memset(&g, 0, sizeof(g));
+  g.M = d->rows; g.N = d->outputs; g.K = d->inputs; g.batch = 1;
+  g.in_dtype = d->dtype ? kBF16 : kF32; g.out_dtype = kF32;
+  g.A = d->x; g.lda = d->ld_x;
+  g.B = d->weight; g.ldb = d->ld_weight;
+  g.C = base; g.ldc = ld_base;
+  g.bias = d->bias;
+  e = launch_gemm_simt(g, st);
+  if (e != cudaSuccess) return e;
+  return launch_with(dim3(d->rows, (d->outputs + 255) / 256), 256, 0, st)(k_adapter_expand_simple<T, false>, base, ld_base, (T*)d->y, d->ld_y,
+                                                                     d->outputs, B, d->rank, d->scale, segs, s);
+}
+
+template <typename T>
+cudaError_t backward_simple(const pbt_adapter_desc* d, const Segments& segs, char* ws, const Layout& l, cudaStream_t st) {
+  float* ds = (float*)(ws + l.s);
+  const T *x = (const T*)d->x, *dy = (const T*)d->dy, *A = (const T*)d->A, *B = (const T*)d->B;
+  cudaError_t e = launch_with((d->rows + 7) / 8, 256, 0, st)(k_adapter_shrink_simple<T, true>, dy, d->ld_dy, d->outputs, B, d->rank, d->scale, segs, ds);
+  if (e != cudaSuccess) return e;
+  float* base = d->dtype ? (float*)(ws + l.base) : (float*)d->dx;
+  const long long ld_base = d->dtype ? d->inputs : d->ld_dx;
+  GemmArgs g;
+  memset(&g, 0, sizeof(g));
+  g.M = d->rows; g.N = d->inputs; g.K = d->outputs; g.batch = 1;
+  g.in_dtype = d->dtype ? kBF16 : kF32; g.out_dtype = kF32;
+  g.A = d->dy; g.lda = d->ld_dy;
+  g.B = d->weight; g.ldb = d->ld_weight; g.b_mn = 1;
+  g.C = base; g.ldc = ld_base;
+  e = launch_gemm_simt(g, st);
+  if (e != cudaSuccess) return e;
+  e = launch_with(dim3(d->rows, (d->inputs + 255) / 256), 256, 0, st)(k_adapter_expand_simple<T, true>, base, ld_base, (T*)d->dx, d->ld_dx,
+                                                                 d->inputs, A, d->rank, nullptr, segs, ds);
+  if (e != cudaSuccess) return e;
+  e = launch_grad_simple<T, false>(x, d->ld_x, d->inputs, ds, d->rank, nullptr, segs, d->dA, st);
+  if (e != cudaSuccess) return e;
+  return launch_grad_simple<T, true>(dy, d->ld_dy, d->outputs, d->s, d->rank, d->scale, segs, d->dB, st);
+}
+
+}  // namespace
+}  // namespace adapters
+}  // namespace pbt
+
+extern "C" int pbt_adapter_query_workspace(const pbt_adapter_desc* d, int backward, size_t* bytes) {
+  using namespace pbt::adapters;
+  if (!bytes) return fail(PBT_ERR_INVALID_ARG, "bytes is NULL");
+  const int rc = check(d);
+  if (rc) return rc;
+  *bytes = layout(d, backward != 0).total;
+  return PBT_OK;
+}
+
+extern "C" int pbt_adapter_forward(const pbt_adapter_desc* d, void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace pbt;
+  using namespace pbt::adapters;
+  const int rc = check(d);
+  if (rc) return rc;
+  if (!d->rows) return PBT_OK;
+  if (!d->x || !d->y || d->ld_x < d->inputs || d->ld_y < d->outputs)
+    return fail(PBT_ERR_INVALID_ARG, "x or y is NULL, or its row stride is smaller than a row");
+  const Layout l = layout(d, false);
+  if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < l.total)
+    return fail(PBT_ERR_WORKSPACE, "workspace missing, not 256-byte aligned or smaller than pbt_adapter_query_workspace says");
+  const Segments segs = {d->row_offsets, d->adapter_ids, d->n_segments, d->rows, d->n_adapters};
+  const cudaError_t e = d->dtype ? forward_simple<bf16>(d, segs, (char*)workspace, l, (cudaStream_t)stream)
+                                 : forward_simple<float>(d, segs, (char*)workspace, l, (cudaStream_t)stream);
+  return e == cudaSuccess ? PBT_OK : fail(PBT_ERR_CUDA, cudaGetErrorString(e));
+}
+
+extern "C" int pbt_adapter_backward(const pbt_adapter_desc* d, void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace pbt;
+  using namespace pbt::adapters;
+  const int rc = check(d);
+  if (rc) return rc;
+  if (!d->dA || !d->dB) return fail(PBT_ERR_INVALID_ARG, "dA or dB is NULL");
+  if (d->rows && (!d->x || !d->dy || !d->dx || !d->s || d->ld_x < d->inputs || d->ld_dy < d->outputs || d->ld_dx < d->inputs))
+    return fail(PBT_ERR_INVALID_ARG, "x, s, dy or dx is NULL, or a row stride is smaller than a row");
+  const Layout l = layout(d, true);
+  if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < l.total)
+    return fail(PBT_ERR_WORKSPACE, "workspace missing, not 256-byte aligned or smaller than pbt_adapter_query_workspace says");
+  cudaStream_t st = (cudaStream_t)stream;
+  cudaError_t e;
+  if (!d->rows) {
+    e = cudaMemsetAsync(d->dA, 0, (size_t)d->n_adapters * d->rank * d->inputs * sizeof(float), st);
+    if (e == cudaSuccess) e = cudaMemsetAsync(d->dB, 0, (size_t)d->n_adapters * d->rank * d->outputs * sizeof(float), st);
+  } else {
+    const Segments segs = {d->row_offsets, d->adapter_ids, d->n_segments, d->rows, d->n_adapters};
+    e = d->dtype ? backward_simple<bf16>(d, segs, (char*)workspace, l, st) : backward_simple<float>(d, segs, (char*)workspace, l, st);
+  }
+  return e == cudaSuccess ? PBT_OK : fail(PBT_ERR_CUDA, cudaGetErrorString(e));
+}

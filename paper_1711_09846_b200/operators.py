@@ -1,6 +1,7 @@
-"""Operators of a population that fine-tunes adapters on shared blocks: gradient clipping and block norms.
+"""Operators of a population that fine-tunes adapters on shared blocks: low-rank adapters beside a shared projection,
+block norms, gradient clipping.
 
-Thin wrappers over the pbt_clip_* and pbt_block_norm_* calls of the C ABI: argument checks, result allocation and
+Thin wrappers over the pbt_adapter_*, pbt_block_norm_* and pbt_clip_* calls of the C ABI: argument checks, result allocation and
 marshalling; every computation runs in the library's CUDA kernels.  Each call only enqueues work, on `stream` (a torch
 stream) or the current stream of the tensors' device; results are allocated for that stream.
 """
@@ -11,7 +12,7 @@ from typing import NamedTuple, Optional, Sequence
 
 import torch
 
-from .binding import PbtBlockNormDesc, PbtClipTensor, PbtError, load_library
+from .binding import PbtAdapterDesc, PbtBlockNormDesc, PbtClipTensor, PbtError, load_library
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1}
 
@@ -241,3 +242,91 @@ def block_norm_backward(dy, du, y, block=None, *, post_weight=None, gate=None, s
                 if t is not None:
                     t.zero_()
     return BlockNormGrads(dx, dblock, dgate, dpost, dnext, dscale if scale is not None else None)
+
+
+# --- adapters --------------------------------------------------------------------------------------------------------------
+
+
+class AdapterProjection:
+    """One shared frozen projection with a low-rank adapter per request or member (pbt_adapter_*).
+
+    weight [outputs, inputs] (contiguous columns), A [adapters, rank, inputs], B [adapters, outputs, rank] (contiguous),
+    all float32 or all bfloat16; scale float32 [adapters] (say alpha / rank, a hyperparameter of every member); bias
+    float32 [outputs] or None.  The tensors are used where they lie: update A, B and scale in place between calls.
+
+    Rows come in segments: segment j holds rows [row_offsets[j], row_offsets[j + 1]) and uses adapter adapter_ids[j]
+    (outside [0, adapters): none); both int32 on the device.  One token per request is a batch of segments of length 1."""
+
+    def __init__(self, weight, A, B, scale, bias=None):
+        _require(weight.is_cuda and weight.dim() == 2 and weight.dtype in _TYPES and weight.stride(1) == 1,
+                 "weight is a CUDA tensor [outputs, inputs], float32 or bfloat16, with contiguous columns")
+        n, k = weight.shape
+        _require(A.dim() == 3 and A.shape[2] == k and A.dtype == weight.dtype and A.device == weight.device and A.is_contiguous(),
+                 "A is a contiguous [adapters, rank, inputs] of the weight's type and device")
+        count, rank = A.shape[0], A.shape[1]
+        _require(B.shape == (count, n, rank) and B.dtype == weight.dtype and B.device == weight.device and B.is_contiguous(),
+                 "B is a contiguous [adapters, outputs, rank] of the weight's type and device")
+        for t, shape, name in ((scale, (count,), "scale"), (bias, (n,), "bias")):
+            _require(t is None or (t.dtype == torch.float32 and t.shape == shape and t.device == weight.device and t.is_contiguous()),
+                     f"{name} is a contiguous float32 tensor {list(shape)} on the weight's device")
+        self.weight, self.A, self.B, self.scale, self.bias = weight, A, B, scale, bias
+        self.lib = load_library()
+        d = self._desc = PbtAdapterDesc()
+        d.inputs, d.outputs, d.rank, d.n_adapters, d.dtype = k, n, rank, count, _TYPES[weight.dtype]
+        d.weight, d.ld_weight, d.A, d.B, d.scale = weight.data_ptr(), weight.stride(0), A.data_ptr(), B.data_ptr(), scale.data_ptr()
+        d.bias = bias.data_ptr() if bias is not None else None
+        d.row_offsets = d.adapter_ids = weight.data_ptr()
+        _check(self.lib.pbt_adapter_query_workspace(C.byref(d), 0, C.byref(C.c_size_t(0))))
+
+    def _call(self, x, row_offsets, adapter_ids):
+        """The description of a call on these rows (a copy: calls from several threads do not share it)."""
+        w = self.weight
+        _require(x.dim() == 2 and x.shape[1] == w.shape[1] and x.dtype == w.dtype and x.device == w.device and (x.stride(1) == 1 or x.shape[1] == 1),
+                 "x is [rows, inputs] of the weight's type and device, with contiguous columns")
+        n = adapter_ids.numel()
+        _require(row_offsets.dtype == torch.int32 and adapter_ids.dtype == torch.int32 and row_offsets.numel() == n + 1
+                 and row_offsets.device == w.device and adapter_ids.device == w.device and row_offsets.is_contiguous() and adapter_ids.is_contiguous(),
+                 "row_offsets [segments + 1] and adapter_ids [segments] are contiguous int32 tensors on the weight's device")
+        d = PbtAdapterDesc.from_buffer_copy(self._desc)
+        d.rows, d.n_segments = x.shape[0], n
+        d.row_offsets, d.adapter_ids = row_offsets.data_ptr(), adapter_ids.data_ptr()
+        d.x, d.ld_x = x.data_ptr(), max(x.stride(0), x.shape[1])
+        return d
+
+    def forward(self, x, row_offsets, adapter_ids, keep: bool = False, stream=None):
+        """y = x W^T + bias + scale_a (x A_a^T) B_a^T; with keep, also S = x A_a^T (float32 [rows, rank], defined for the
+        rows that have an adapter), which the backward pass takes."""
+        d, w = self._call(x, row_offsets, adapter_ids), self.weight
+        with _On(w.device, stream, (x, row_offsets, adapter_ids, w, self.A, self.B, self.scale, self.bias)) as s:
+            y = torch.empty((x.shape[0], w.shape[0]), dtype=w.dtype, device=w.device)
+            d.y, d.ld_y = y.data_ptr(), w.shape[0]
+            kept = None
+            if keep:
+                kept = torch.empty((x.shape[0], d.rank), dtype=torch.float32, device=w.device)
+                d.s = kept.data_ptr()
+            if x.shape[0]:
+                self._run(d, 0, self.lib.pbt_adapter_forward, s)
+        return (y, kept) if keep else y
+
+    def backward(self, dy, x, kept, row_offsets, adapter_ids, stream=None):
+        """(dx, dA, dB) from dy [rows, outputs], the forward pass's x and what it kept; dA and dB are float32."""
+        d, w = self._call(x, row_offsets, adapter_ids), self.weight
+        rows = x.shape[0]
+        _require(dy.shape == (rows, w.shape[0]) and dy.dtype == w.dtype and dy.device == w.device and (dy.stride(1) == 1 or dy.shape[1] == 1),
+                 "dy is [rows, outputs] of the weight's type and device, with contiguous columns")
+        _require(kept.shape == (rows, d.rank) and kept.dtype == torch.float32 and kept.device == w.device and kept.is_contiguous(),
+                 "kept is what forward(keep=True) returned")
+        d.dy, d.ld_dy, d.s = dy.data_ptr(), max(dy.stride(0), dy.shape[1]), kept.data_ptr()
+        with _On(w.device, stream, (x, dy, kept, row_offsets, adapter_ids, w, self.A, self.B, self.scale)) as s:
+            dx = torch.empty((rows, w.shape[1]), dtype=w.dtype, device=w.device)
+            d_a = torch.empty(self.A.shape, dtype=torch.float32, device=w.device)
+            d_b = torch.empty(self.B.shape, dtype=torch.float32, device=w.device)
+            d.dx, d.ld_dx, d.dA, d.dB = dx.data_ptr(), w.shape[1], d_a.data_ptr(), d_b.data_ptr()
+            self._run(d, 1, self.lib.pbt_adapter_backward, s)
+        return dx, d_a, d_b
+
+    def _run(self, d, backward, call, s):
+        nbytes = C.c_size_t(0)
+        _check(self.lib.pbt_adapter_query_workspace(C.byref(d), backward, C.byref(nbytes)))
+        ws = _workspace(nbytes.value, self.weight.device)
+        _check(call(C.byref(d), ws.data_ptr(), nbytes.value, s))

@@ -1,0 +1,323 @@
+"""Low-rank adapters beside a shared projection (AdapterProjection / pbt_adapter_*) against the formulas in 64 bits.
+
+Tolerances, from the magnitudes that the reference returns beside the values (the same sums over absolute values).
+eps = 2^-24.  fp32 sums, whatever their order, of n terms are within n eps of the sum of magnitudes; the longest
+sequential chain of any of the kernels is taken as (inputs + outputs) / 16 + rows / 4 + 64 terms.  A bf16 result is rounded
+once (2^-8 of its value); its low-rank part may also hold S or dS rounded to bf16 before the second product (2^-8 of that
+part's magnitude).  dA and dB are fp32 and are allowed the chain twice (dS or S, then the sum over rows)."""
+import ctypes as C
+
+import pytest
+
+EPS32 = 2.0 ** -24
+
+
+def _case(dtype, lengths, ids, inputs, outputs, rank, adapters, seed=0, pad=0, lead=0):
+    """Inputs; `pad` gives rows a stride of their own, `lead` rows in front of the first segment have none."""
+    import torch
+    gen = torch.Generator().manual_seed(seed)
+    dt = getattr(torch, dtype)
+    rows = lead + sum(lengths)
+
+    def draw(*shape, scale=1.0, wide=0):
+        t = torch.randn(*shape[:-1], shape[-1] + wide, generator=gen).mul_(scale).to(dt).cuda()
+        return t[..., :shape[-1]]
+    at = [lead]
+    for n in lengths:
+        at.append(at[-1] + n)
+    return dict(x=draw(rows, inputs, wide=pad), dy=draw(rows, outputs, scale=0.1, wide=pad),
+                weight=draw(outputs, inputs, scale=inputs ** -0.5, wide=pad), A=draw(adapters, rank, inputs, scale=inputs ** -0.5),
+                B=draw(adapters, outputs, rank, scale=rank ** -0.5), scale=(torch.rand(adapters, generator=gen) * 2 - 0.5).cuda(),
+                bias=torch.randn(outputs, generator=gen).cuda(), row_offsets=torch.tensor(at, dtype=torch.int32).cuda(),
+                adapter_ids=torch.tensor(ids, dtype=torch.int32).cuda(), segments=list(zip(at[:-1], at[1:], ids)))
+
+
+def _reference(c, backward=True):
+    """{name: (value, magnitude)} in 64 bits on the CPU; low: the magnitude of the low-rank part alone."""
+    import torch
+    f = {k: v.cpu().double() for k, v in c.items() if k != "segments"}
+    x, w, a, b, s, dy = (f[k] for k in ("x", "weight", "A", "B", "scale", "dy"))
+    y, ym = x @ w.T + f["bias"], x.abs() @ w.abs().T + f["bias"].abs()
+    dx, dxm = dy @ w, dy.abs() @ w.abs()
+    ylow, dxlow = torch.zeros_like(y), torch.zeros_like(dx)
+    S, Sm = torch.zeros(x.shape[0], a.shape[1]).double(), torch.zeros(x.shape[0], a.shape[1]).double()
+    dA, dAm, dB, dBm = (torch.zeros_like(t) for t in (a, a, b, b))
+    for lo, hi, i in c["segments"]:
+        if not 0 <= i < a.shape[0]:
+            continue
+        r, k = slice(lo, hi), s[i].abs()
+        S[r], Sm[r] = x[r] @ a[i].T, x[r].abs() @ a[i].abs().T
+        y[r] += s[i] * S[r] @ b[i].T
+        ylow[r] = k * Sm[r] @ b[i].abs().T
+        ds, dsm = s[i] * dy[r] @ b[i], k * dy[r].abs() @ b[i].abs()
+        dx[r] += ds @ a[i]
+        dxlow[r] = dsm @ a[i].abs()
+        dA[i] += ds.T @ x[r]
+        dAm[i] += dsm.T @ x[r].abs()
+        dB[i] += s[i] * dy[r].T @ S[r]
+        dBm[i] += k * dy[r].abs().T @ Sm[r]
+    return dict(y=(y, ym + ylow, ylow), s=(S, Sm, None), dx=(dx, dxm + dxlow, dxlow), dA=(dA, dAm, None), dB=(dB, dBm, None))
+
+
+def _close(name, got, ref, c, rows=None):
+    import torch
+    value, mag, low = ref[name]
+    t, k = c["x"].shape
+    chain = ((k + c["weight"].shape[0]) / 16 + t / 4 + 64) * EPS32
+    tol = chain * (2 if name in ("dA", "dB") else 1) * mag
+    if got.dtype == torch.bfloat16:
+        tol = tol + 2.0 ** -8 * (value.abs() + low) + 1e-38
+    g = got.cpu().double()
+    assert g.shape == value.shape
+    if rows is not None:
+        g, value, tol = g[rows], value[rows], tol[rows]
+    bad = ~((g - value).abs() <= tol)
+    assert not bad.any(), (name, ((g - value).abs() / tol.clamp_min(1e-300)).max().item(), int(bad.sum()))
+
+
+def _owned(c):
+    """Rows that have an adapter."""
+    import torch
+    m = torch.zeros(c["x"].shape[0], dtype=torch.bool)
+    for lo, hi, i in c["segments"]:
+        if 0 <= i < c["A"].shape[0]:
+            m[lo:hi] = True
+    return m
+
+
+def _run(c, stream=None):
+    import paper_1711_09846_b200 as pbt
+    layer = pbt.AdapterProjection(c["weight"], c["A"], c["B"], c["scale"], bias=c["bias"])
+    where = (c["row_offsets"], c["adapter_ids"])
+    y, kept = layer.forward(c["x"], *where, keep=True, stream=stream)
+    dx, d_a, d_b = layer.backward(c["dy"], c["x"], kept, *where, stream=stream)
+    return layer, dict(y=y, s=kept, dx=dx, dA=d_a, dB=d_b)
+
+
+def _verify(c):
+    import torch
+    layer, out = _run(c)
+    ref = _reference(c)
+    for name in ("y", "dx", "dA", "dB"):
+        _close(name, out[name], ref, c)
+    _close("s", out["s"], ref, c, _owned(c))
+    only = layer.forward(c["x"], c["row_offsets"], c["adapter_ids"])
+    assert torch.equal(only, out["y"])         # keeping S changes nothing
+    return out
+
+
+# (segment lengths, adapter ids, inputs, outputs, rank, adapters)
+CASES = {
+    "one row": ([1], [0], 64, 64, 8, 1),
+    "one column": ([3, 2], [1, 0], 1, 1, 1, 2),
+    "tiny odd": ([2, 3, 1], [0, 1, 0], 7, 5, 3, 2),
+    "no adapter at all": ([40, 30], [-1, -1], 64, 72, 8, 2),
+    "single tokens": ([1] * 9, [2, -1, 0, 1, 2, 2, 0, 1, -1], 128, 136, 16, 3),
+    "single tokens, many": ([1] * 70, [(7 * k) % 13 - 1 for k in range(70)], 264, 392, 8, 12),
+    "empty segments": ([0, 5, 0, 0, 130, 0, 1, 0], [0, 1, 2, 0, 2, 1, 0, 2], 96, 160, 16, 3),
+    "shared adapters": ([33, 64, 1, 127, 65], [1, 0, 1, 1, 0], 200, 256, 16, 4),
+    "an id out of range": ([20, 20], [5, 1], 64, 64, 8, 2),
+    "equal members": ([128] * 5, [0, 1, 2, 3, 4], 256, 384, 16, 5),
+    "rank 64": ([300, 41], [1, 0], 320, 264, 64, 2),
+    "rank 24": ([70, 200], [1, 0], 136, 520, 24, 2),
+    "rank 4": ([257, 3], [0, 1], 784, 512, 4, 2),
+    "odd widths": ([150, 77], [0, 1], 333, 259, 12, 2),
+    "one odd width": ([150, 77], [1, 0], 512, 259, 16, 2),
+    "long": ([1100, 300, 13], [0, 1, 0], 512, 640, 8, 2),
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("name", list(CASES))
+def test_forward_and_backward_match_the_formulas(name, dtype):
+    _verify(_case(dtype, *CASES[name], seed=len(name)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("pad", [1, 8])
+def test_row_strides_and_rows_outside_every_segment(pad, dtype):
+    lengths, ids, *rest = CASES["shared adapters"]
+    _verify(_case(dtype, lengths, ids, *rest, seed=pad, pad=pad, lead=5))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("lengths", [[1] * 12, [130, 60, 3, 200]], ids=["tokens", "ragged"])
+def test_a_diverged_adapter_reaches_no_other_row(lengths, dtype):
+    import torch
+    ids = [k % 3 for k in range(len(lengths))]
+    c = _case(dtype, lengths, ids, 192, 256, 16, 3, seed=3)
+    _, clean = _run(c)
+    c["A"][1, 3, 7] = float("nan")
+    c["B"][1, 5, 2] = float("inf")
+    mine = torch.zeros(c["x"].shape[0], dtype=torch.bool)
+    for lo, hi, i in c["segments"]:
+        if i == 1:
+            mine[lo:hi] = True
+    _, out = _run(c)
+    for name in ("y", "dx", "s"):
+        assert torch.equal(out[name][~mine.cuda()], clean[name][~mine.cuda()]), name
+    assert torch.isnan(out["y"][mine.cuda()]).any(1).all() and torch.isnan(out["dx"][mine.cuda()]).any(1).all()
+    for name in ("dA", "dB"):
+        assert torch.equal(out[name][[0, 2]], clean[name][[0, 2]]), name
+    # and a row that holds NaN stays alone, in the gradients of the other adapters too
+    c = _case(dtype, lengths, ids, 192, 256, 16, 3, seed=3)
+    lo, hi, _ = c["segments"][1]
+    c["x"][lo, 0] = float("nan")
+    c["dy"][hi - 1, 3] = float("inf")
+    _, out = _run(c)
+    others = torch.ones(c["x"].shape[0], dtype=torch.bool)
+    others[lo:hi] = False
+    for name in ("y", "dx", "s"):
+        assert torch.equal(out[name][others.cuda()], clean[name][others.cuda()]), name
+    for name in ("dA", "dB"):
+        assert torch.equal(out[name][[0, 2]], clean[name][[0, 2]]), name
+        assert not torch.isfinite(out[name][1]).all(), name
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_no_rows(dtype):
+    c = _case(dtype, [0, 0], [0, 1], 64, 64, 8, 2)
+    _, out = _run(c)
+    assert out["y"].shape == (0, 64) and out["dx"].shape == (0, 64)
+    assert (out["dA"] == 0).all() and (out["dB"] == 0).all()
+
+
+@pytest.mark.gpu
+def test_segment_tables_that_make_no_sense_stay_inside_the_buffers():
+    """Offsets beyond the rows and ids beyond the adapters are clamped (what the rows hold then is unspecified): the
+    results' neighbours in memory stay as they were."""
+    import torch
+    import paper_1711_09846_b200 as pbt
+    for dtype in ("float32", "bfloat16"):
+        c = _case(dtype, [90, 60], [0, 1], 128, 128, 8, 2)
+        for offsets, ids in (([0, 5000, 9000], [0, 1]), ([-7, 60, 150], [1, 99]), ([150, 20, 0], [0, 1])):
+            layer = pbt.AdapterProjection(c["weight"], c["A"], c["B"], c["scale"])
+            where = [torch.tensor(v, dtype=torch.int32, device="cuda") for v in (offsets, ids)]
+            y, kept = layer.forward(c["x"], *where, keep=True)
+            layer.backward(c["dy"], c["x"], torch.zeros_like(kept), *where)
+        torch.cuda.synchronize()
+        _verify(c)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_runs_are_reproducible_and_another_stream_gives_the_same_bits(dtype):
+    import torch
+    c = _case(dtype, [200, 1, 90, 300], [0, 1, 1, 0], 256, 320, 16, 2, seed=8)
+    _, first = _run(c)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for stream in (None, side):
+        _, out = _run(c, stream)
+        torch.cuda.synchronize()
+        for name in first:
+            assert torch.equal(first[name], out[name]), name
+
+
+@pytest.mark.gpu
+def test_gradients_agree_with_differences_of_the_forward_pass():
+    """Loss sum(y dy) in fp32: it is bilinear in (A, B) and linear in x, so a central difference along one tensor is exact
+    up to the forward pass's rounding, about 1e-6 of a loss of order 100 over a step of 2: 2e-4 of the largest."""
+    import torch
+    import paper_1711_09846_b200 as pbt
+    c = _case("float32", [30, 50, 20], [0, 1, 0], 48, 56, 8, 2, seed=2)
+    _, out = _run(c)
+
+    def loss(**kw):
+        e = {**c, **kw}
+        y = pbt.AdapterProjection(e["weight"], e["A"], e["B"], e["scale"], bias=e["bias"]).forward(e["x"], e["row_offsets"], e["adapter_ids"])
+        return (y.double() * c["dy"].double()).sum().item()
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    pairs = []
+    for key, grad in (("x", "dx"), ("A", "dA"), ("B", "dB")):
+        v = torch.randn(c[key].shape, generator=gen, device="cuda")
+        diff = (loss(**{key: c[key] + v}) - loss(**{key: c[key] - v})) / 2
+        pairs.append((key, diff, (out[grad].double() * v.double()).sum().item()))
+    largest = max(abs(p[2]) for p in pairs)
+    for key, diff, exact in pairs:
+        assert abs(diff - exact) <= 2e-4 * max(largest, 100.0), pairs
+
+
+def test_the_written_out_gradients_are_those_of_autograd(monkeypatch):
+    """Pins the reference above (CPU, 64 bits) to automatic differentiation of the forward formula."""
+    import torch
+    monkeypatch.setattr(torch.Tensor, "cuda", lambda self, *a, **k: self)
+    c = _case("float32", [3, 0, 4], [1, 0, 1], 6, 5, 2, 2)
+    f = {k: c[k].double().requires_grad_() for k in ("x", "A", "B")}
+    y = f["x"] @ c["weight"].double().T + c["bias"].double()
+    low = torch.zeros_like(y)
+    for lo, hi, i in c["segments"]:
+        low = low + torch.nn.functional.pad(c["scale"][i].double() * f["x"][lo:hi] @ f["A"][i].T @ f["B"][i].T, (0, 0, lo, y.shape[0] - hi))
+    y = y + low
+    (y * c["dy"].double()).sum().backward()
+    ref = _reference(c)
+    assert torch.allclose(ref["y"][0], y.detach())
+    for name, key in (("dx", "x"), ("dA", "A"), ("dB", "B")):
+        assert torch.allclose(ref[name][0], f[key].grad)
+
+
+@pytest.mark.gpu
+def test_adapter_refusals():
+    import torch
+    import paper_1711_09846_b200 as pbt
+    c = _case("bfloat16", [4, 5], [0, 1], 32, 48, 8, 2)
+    good = dict(weight=c["weight"], A=c["A"], B=c["B"], scale=c["scale"], bias=c["bias"])
+    pbt.AdapterProjection(**good)
+    for kw in (dict(weight=c["weight"].float()), dict(weight=c["weight"].cpu()), dict(weight=c["weight"].half()), dict(weight=c["weight"].T),
+               dict(A=c["A"][:, :, :16]), dict(A=c["A"].transpose(0, 1)), dict(B=c["B"][:1]), dict(B=c["B"].float()),
+               dict(scale=c["scale"].double()), dict(scale=c["scale"][:1]), dict(bias=c["bias"][:5])):
+        with pytest.raises(ValueError):
+            pbt.AdapterProjection(**{**good, **kw})
+    wide = _case("bfloat16", [4], [0], 128, 128, 65, 1)
+    with pytest.raises(pbt.PbtError):
+        pbt.AdapterProjection(wide["weight"], wide["A"], wide["B"], wide["scale"])
+    layer = pbt.AdapterProjection(**good)
+    o, i = c["row_offsets"], c["adapter_ids"]
+    for args in ((c["x"][:, :16], o, i), (c["x"].float(), o, i), (c["x"], o.long(), i), (c["x"], o[:-1], i), (c["x"], o, i.cpu()),
+                 (c["x"][0], o, i), (torch.zeros(9, 64, device="cuda", dtype=torch.bfloat16)[:, ::2], o, i)):
+        with pytest.raises(ValueError):
+            layer.forward(*args)
+    y, kept = layer.forward(c["x"], o, i, keep=True)
+    for args in ((c["dy"][:3], c["x"], kept, o, i), (c["dy"].float(), c["x"], kept, o, i), (c["dy"], c["x"], kept[:, :4], o, i),
+                 (c["dy"], c["x"], kept.bfloat16(), o, i)):
+        with pytest.raises(ValueError):
+            layer.backward(*args)
+
+
+def test_adapter_arguments_are_checked_before_the_device_is_touched():
+    import paper_1711_09846_b200 as pbt
+    from paper_1711_09846_b200.binding import PbtAdapterDesc
+    lib = pbt.load_library()
+    n = C.c_size_t(0)
+
+    def desc(**kw):
+        d = PbtAdapterDesc()
+        d.rows, d.inputs, d.outputs, d.rank, d.n_adapters, d.n_segments = 10, 32, 64, 8, 3, 2
+        for name in ("weight", "A", "B", "scale", "row_offsets", "adapter_ids", "x", "y", "s", "dy", "dx", "dA", "dB"):
+            setattr(d, name, 4096)
+        d.ld_weight = d.ld_x = d.ld_dx = 32
+        d.ld_y = d.ld_dy = 64
+        for k, v in kw.items():
+            setattr(d, k, v)
+        return d
+    for backward in (0, 1):
+        assert lib.pbt_adapter_query_workspace(C.byref(desc()), backward, C.byref(n)) == 0 and n.value > 0 and n.value % 256 == 0
+    assert lib.pbt_adapter_query_workspace(C.byref(desc()), 0, None) == 1
+    for kw, code in ((dict(rows=-1), 1), (dict(inputs=0), 1), (dict(outputs=0), 1), (dict(rank=0), 2), (dict(rank=65), 2), (dict(dtype=2), 2),
+                     (dict(n_adapters=0), 1), (dict(n_segments=-1), 1), (dict(weight=None), 1), (dict(A=None), 1), (dict(B=None), 1),
+                     (dict(scale=None), 1), (dict(row_offsets=None), 1), (dict(adapter_ids=None), 1), (dict(ld_weight=31), 1)):
+        assert lib.pbt_adapter_forward(C.byref(desc(**kw)), None, 0, None) == code, kw
+        assert lib.pbt_adapter_backward(C.byref(desc(**kw)), None, 0, None) == code, kw
+        assert lib.pbt_last_error(None)
+    for kw in (dict(x=None), dict(y=None), dict(ld_x=31), dict(ld_y=63)):
+        assert lib.pbt_adapter_forward(C.byref(desc(**kw)), None, 0, None) == 1, kw
+    for kw in (dict(x=None), dict(s=None), dict(dy=None), dict(dx=None), dict(dA=None), dict(dB=None), dict(ld_dy=63), dict(ld_dx=31)):
+        assert lib.pbt_adapter_backward(C.byref(desc(**kw)), None, 0, None) == 1, kw
+    assert lib.pbt_adapter_forward(C.byref(desc()), None, 0, None) == 3
+    assert lib.pbt_adapter_backward(C.byref(desc()), None, 0, None) == 3
+    assert lib.pbt_adapter_forward(None, None, 0, None) == 1
+    assert lib.pbt_adapter_forward(C.byref(desc(rows=0)), None, 0, None) == 0
