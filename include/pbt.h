@@ -560,7 +560,8 @@ int pbt_block_norm_backward(const pbt_block_norm_desc* desc, void* workspace, si
  * contiguous, x / y / dy / dx with any row stride; all of one type (0 float, 1 bfloat16).  bias float [outputs] or NULL,
  * scale float [n_adapters].  s float [rows][rank]: written by the forward pass unless NULL (rows without an adapter are
  * left alone), read by the backward pass.  dA, dB are float in the shapes of A and B, written for every adapter (zero for
- * one without rows).  Sums are fp32.  rank <= 64.  Elements have to be aligned to their size only.
+ * one without rows).  Sums are fp32; a bfloat16 pass rounds S (dS) to bfloat16 for the second product of y (dx), but not
+ * for dB (dA).  rank <= 64.  Elements have to be aligned to their size only.
  * A row depends on its own segment's adapter alone: NaN or infinite weights of one adapter reach no row of another.
  */
 typedef struct pbt_adapter_desc {
@@ -577,8 +578,10 @@ typedef struct pbt_adapter_desc {
   const void* dy; int64_t ld_dy;
   void* dx; int64_t ld_dx;
   float* dA; float* dB;
+  void* status_device;          /* bfloat16: 32 zeroed bytes of device memory, as for pbt_grouped_gemm */
 } pbt_adapter_desc;
-/* Bytes of device workspace (256-byte aligned base) of one forward (backward == 0) or backward call. */
+/* Bytes of device workspace (256-byte aligned base) of one forward (backward == 0) or backward call of this description
+ * (its pointers and strides included: rows that are not multiples of 16 bytes are laid out anew in the workspace). */
 int pbt_adapter_query_workspace(const pbt_adapter_desc* desc, int backward, size_t* bytes);
 int pbt_adapter_forward(const pbt_adapter_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
 int pbt_adapter_backward(const pbt_adapter_desc* desc, void* workspace, size_t workspace_bytes, void* stream);

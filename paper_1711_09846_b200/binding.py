@@ -101,7 +101,7 @@ class PbtAdapterDesc(C.Structure):
                 ("scale", C.c_void_p), ("bias", C.c_void_p), ("row_offsets", C.c_void_p), ("adapter_ids", C.c_void_p),
                 ("x", C.c_void_p), ("ld_x", C.c_int64), ("y", C.c_void_p), ("ld_y", C.c_int64), ("s", C.c_void_p),
                 ("dy", C.c_void_p), ("ld_dy", C.c_int64), ("dx", C.c_void_p), ("ld_dx", C.c_int64),
-                ("dA", C.c_void_p), ("dB", C.c_void_p)]
+                ("dA", C.c_void_p), ("dB", C.c_void_p), ("status_device", C.c_void_p)]
 
 
 EXPORTS = [

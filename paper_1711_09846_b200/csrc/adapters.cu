@@ -15,15 +15,10 @@ void set_last_error(const char* msg);
 namespace adapters {
 namespace {
 
-template <typename T> __device__ __forceinline__ float to_float(T v) { return (float)v; }
-template <> __device__ __forceinline__ float to_float<bf16>(bf16 v) { return __bfloat162float(v); }
-template <typename T> __device__ __forceinline__ T from_float(float v) { return (T)v; }
-template <> __device__ __forceinline__ bf16 from_float<bf16>(float v) { return __float2bfloat16_rn(v); }
-
 // s[row][j] = f sum_k x[row][k] m_a(j, k), one warp per row; m_a is A_a [rank][K] or, TRANS, B_a [K][rank].
 // f: the adapter's scale or 1.
-template <typename T, bool TRANS>
-__global__ void __launch_bounds__(256) k_adapter_shrink_simple(const T* __restrict__ x, long long ldx, int K, const T* __restrict__ mats,
+template <bool TRANS>
+__global__ void __launch_bounds__(256) k_adapter_shrink_f32(const float* __restrict__ x, long long ldx, int K, const float* __restrict__ mats,
                                                                int rank, const float* __restrict__ scale, Segments segs,
                                                                float* __restrict__ s) {
   pdl_prologue();
@@ -33,16 +28,16 @@ __global__ void __launch_bounds__(256) k_adapter_shrink_simple(const T* __restri
   if (j < 0 || row >= segment_begin(segs, j + 1)) return;
   const int a = segment_adapter(segs, j);
   if (a < 0) return;
-  const T* xr = x + row * ldx;
-  const T* m = mats + (long long)a * rank * K;
+  const float* xr = x + row * ldx;
+  const float* m = mats + (long long)a * rank * K;
   const float f = scale ? scale[a] : 1.f;
   for (int r0 = 0; r0 < rank; r0 += 8) {
     float acc[8] = {};
     for (int k = lane; k < K; k += 32) {
-      const float v = to_float(xr[k]);
+      const float v = xr[k];
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (r0 + i < rank) acc[i] = __fmaf_rn(v, to_float(TRANS ? m[(long long)k * rank + r0 + i] : m[(long long)(r0 + i) * K + k]), acc[i]);
+        if (r0 + i < rank) acc[i] = __fmaf_rn(v, TRANS ? m[(long long)k * rank + r0 + i] : m[(long long)(r0 + i) * K + k], acc[i]);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -53,11 +48,10 @@ __global__ void __launch_bounds__(256) k_adapter_shrink_simple(const T* __restri
   }
 }
 
-// out[row][n] = base[row][n] + f sum_j s[row][j] m_a(n, j); m_a is B_a [N][rank] or, TRANS, A_a [rank][N].  `base` may be
-// `out` itself.
-template <typename T, bool TRANS>
-__global__ void __launch_bounds__(256) k_adapter_expand_simple(const float* base, long long ld_base, T* out, long long ld_out, int N,
-                                                               const T* __restrict__ mats, int rank,
+// out[row][n] += f sum_j s[row][j] m_a(n, j); m_a is B_a [N][rank] or, TRANS, A_a [rank][N].
+template <bool TRANS>
+__global__ void __launch_bounds__(256) k_adapter_expand_f32(float* out, long long ld_out, int N,
+                                                               const float* __restrict__ mats, int rank,
                                                                const float* __restrict__ scale, Segments segs,
                                                                const float* __restrict__ s) {
   pdl_prologue();
@@ -65,22 +59,20 @@ __global__ void __launch_bounds__(256) k_adapter_expand_simple(const float* base
   __shared__ float sr[kMaxRank];
   const int j = segment_of_row(segs, row);
   const int a = j >= 0 && row < segment_begin(segs, j + 1) ? segment_adapter(segs, j) : -1;
-  if (a >= 0 && threadIdx.x < rank) sr[threadIdx.x] = s[(long long)row * rank + threadIdx.x];
+  if (a < 0) return;
+  if (threadIdx.x < rank) sr[threadIdx.x] = s[(long long)row * rank + threadIdx.x];
   __syncthreads();
   if (n >= N) return;
+  const float* m = mats + (long long)a * rank * N;
   float acc = 0.f;
-  if (a >= 0) {
-    const T* m = mats + (long long)a * rank * N;
-    for (int i = 0; i < rank; ++i) acc = __fmaf_rn(sr[i], to_float(TRANS ? m[(long long)i * N + n] : m[(long long)n * rank + i]), acc);
-    if (scale) acc *= scale[a];
-  }
-  out[row * ld_out + n] = from_float<T>(base[row * ld_base + n] + acc);
+  for (int i = 0; i < rank; ++i) acc = __fmaf_rn(sr[i], TRANS ? m[(long long)i * N + n] : m[(long long)n * rank + i], acc);
+  out[row * ld_out + n] += scale ? scale[a] * acc : acc;
 }
 
 // g_a(j, n) = f_a sum over the rows of adapter a of s[row][j] v[row][n], written as [rank][N] or, TRANS, [N][rank].
 // A block owns 64 columns of one adapter; its 256 threads take every fourth row and add up in shared memory.
-template <typename T, bool TRANS, int RANK>
-__global__ void __launch_bounds__(256) k_adapter_grad_simple(const T* __restrict__ v, long long ldv, int N, const float* __restrict__ s,
+template <bool TRANS, int RANK>
+__global__ void __launch_bounds__(256) k_adapter_grad_f32(const float* __restrict__ v, long long ldv, int N, const float* __restrict__ s,
                                                              int rank, const float* __restrict__ scale, Segments segs,
                                                              float* __restrict__ g) {
   pdl_prologue();
@@ -91,7 +83,7 @@ __global__ void __launch_bounds__(256) k_adapter_grad_simple(const T* __restrict
     if (segment_adapter(segs, j) != a) continue;
     const int end = segment_begin(segs, j + 1);
     for (int row = segment_begin(segs, j) + part; row < end; row += 4) {
-      const float x = n < N ? to_float(v[row * ldv + n]) : 0.f;
+      const float x = n < N ? v[row * ldv + n] : 0.f;
       const float* sr = s + (long long)row * rank;
 #pragma unroll
       for (int i = 0; i < RANK; ++i) if (i < rank) acc[i] = __fmaf_rn(__ldg(sr + i), x, acc[i]);
@@ -109,14 +101,14 @@ __global__ void __launch_bounds__(256) k_adapter_grad_simple(const T* __restrict
     if (i < rank) out[TRANS ? (long long)n * rank + i : (long long)i * N + n] = f * (acc[i] + sum[0][i][col] + sum[1][i][col] + sum[2][i][col]);
 }
 
-template <typename T, bool TRANS>
-cudaError_t launch_grad_simple(const T* v, long long ldv, int N, const float* s, int rank, const float* scale, const Segments& segs,
+template <bool TRANS>
+cudaError_t launch_grad_f32(const float* v, long long ldv, int N, const float* s, int rank, const float* scale, const Segments& segs,
                                float* g, cudaStream_t st) {
   auto l = launch_with(dim3((N + 63) / 64, segs.n_adapters), 256, 0, st);
-  if (rank <= 8) return l(k_adapter_grad_simple<T, TRANS, 8>, v, ldv, N, s, rank, scale, segs, g);
-  if (rank <= 16) return l(k_adapter_grad_simple<T, TRANS, 16>, v, ldv, N, s, rank, scale, segs, g);
-  if (rank <= 32) return l(k_adapter_grad_simple<T, TRANS, 32>, v, ldv, N, s, rank, scale, segs, g);
-  return l(k_adapter_grad_simple<T, TRANS, 64>, v, ldv, N, s, rank, scale, segs, g);
+  if (rank <= 8) return l(k_adapter_grad_f32<TRANS, 8>, v, ldv, N, s, rank, scale, segs, g);
+  if (rank <= 16) return l(k_adapter_grad_f32<TRANS, 16>, v, ldv, N, s, rank, scale, segs, g);
+  if (rank <= 32) return l(k_adapter_grad_f32<TRANS, 32>, v, ldv, N, s, rank, scale, segs, g);
+  return l(k_adapter_grad_f32<TRANS, 64>, v, ldv, N, s, rank, scale, segs, g);
 }
 
 int fail(int code, const char* msg) {
@@ -133,70 +125,61 @@ int check(const pbt_adapter_desc* d) {
   if (d->dtype != 0 && d->dtype != 1) return fail(PBT_ERR_UNSUPPORTED, "operands are float or bfloat16");
   if (!d->weight || !d->A || !d->B || !d->scale || !d->row_offsets || (d->n_segments && !d->adapter_ids))
     return fail(PBT_ERR_INVALID_ARG, "weight, A, B, scale, row_offsets or adapter_ids is NULL");
+  if (d->dtype == 1 && !d->status_device) return fail(PBT_ERR_INVALID_ARG, "status_device is required by the tensor-core kernels");
   if (d->ld_weight < d->inputs) return fail(PBT_ERR_INVALID_ARG, "ld_weight is smaller than inputs");
   return PBT_OK;
 }
 
-size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
-
-struct Layout {
-  size_t s, base, total;
-};
-Layout layout(const pbt_adapter_desc* d, bool backward) {
-  Layout l;
-  const size_t rows = (size_t)d->rows;
-  l.s = 0;                                                   // S of a forward pass that does not keep it, dS
-  l.base = align256(rows * d->rank * sizeof(float));
-  l.total = l.base + (d->dtype ? align256(rows * (backward ? d->inputs : d->outputs) * sizeof(float)) : 0);
-  if (!l.total) l.total = 256;
-  return l;
-}
-
-template <typename T>
-cudaError_t forward_simple(const pbt_adapter_desc* d, const Segments& segs, char* ws, const Layout& l, cudaStream_t st) {
-  float* s = d->s ? d->s : (float*)(ws + l.s);
-  const T *x = (const T*)d->x, *A = (const T*)d->A, *B = (const T*)d->B;
-  cudaError_t e = launch_with((d->rows + 7) / 8, 256, 0, st)(k_adapter_shrink_simple<T, false>, x, d->ld_x, d->inputs, A, d->rank, nullptr, segs, s);
+cudaError_t forward_f32(const pbt_adapter_desc* d, const Segments& segs, float* ws, cudaStream_t st) {
+  float *s = d->s ? d->s : ws, *y = (float*)d->y;
+  cudaError_t e = launch_with((d->rows + 7) / 8, 256, 0, st)(k_adapter_shrink_f32<false>, (const float*)d->x, d->ld_x, d->inputs, (const float*)d->A,
+                                                         d->rank, nullptr, segs, s);
   if (e != cudaSuccess) return e;
-  float* base = d->dtype ? (float*)(ws + l.base) : (float*)d->y;
-  const long long ld_base = d->dtype ? d->outputs : d->ld_y;
   GemmArgs g;
   memset(&g, 0, sizeof(g));
   g.M = d->rows; g.N = d->outputs; g.K = d->inputs; g.batch = 1;
-  g.in_dtype = d->dtype ? kBF16 : kF32; g.out_dtype = kF32;
+  g.in_dtype = g.out_dtype = kF32;
   g.A = d->x; g.lda = d->ld_x;
   g.B = d->weight; g.ldb = d->ld_weight;
-  g.C = base; g.ldc = ld_base;
+  g.C = y; g.ldc = d->ld_y;
   g.bias = d->bias;
   e = launch_gemm_simt(g, st);
   if (e != cudaSuccess) return e;
-  return launch_with(dim3(d->rows, (d->outputs + 255) / 256), 256, 0, st)(k_adapter_expand_simple<T, false>, base, ld_base, (T*)d->y, d->ld_y,
-                                                                     d->outputs, B, d->rank, d->scale, segs, s);
+  return launch_with(dim3(d->rows, (d->outputs + 255) / 256), 256, 0, st)(k_adapter_expand_f32<false>, y, d->ld_y, d->outputs, (const float*)d->B, d->rank,
+                                                                     d->scale, segs, s);
 }
 
-template <typename T>
-cudaError_t backward_simple(const pbt_adapter_desc* d, const Segments& segs, char* ws, const Layout& l, cudaStream_t st) {
-  float* ds = (float*)(ws + l.s);
-  const T *x = (const T*)d->x, *dy = (const T*)d->dy, *A = (const T*)d->A, *B = (const T*)d->B;
-  cudaError_t e = launch_with((d->rows + 7) / 8, 256, 0, st)(k_adapter_shrink_simple<T, true>, dy, d->ld_dy, d->outputs, B, d->rank, d->scale, segs, ds);
+cudaError_t backward_f32(const pbt_adapter_desc* d, const Segments& segs, float* ds, cudaStream_t st) {
+  const float *x = (const float*)d->x, *dy = (const float*)d->dy;
+  float* dx = (float*)d->dx;
+  cudaError_t e = launch_with((d->rows + 7) / 8, 256, 0, st)(k_adapter_shrink_f32<true>, dy, d->ld_dy, d->outputs, (const float*)d->B, d->rank, d->scale, segs, ds);
   if (e != cudaSuccess) return e;
-  float* base = d->dtype ? (float*)(ws + l.base) : (float*)d->dx;
-  const long long ld_base = d->dtype ? d->inputs : d->ld_dx;
   GemmArgs g;
   memset(&g, 0, sizeof(g));
   g.M = d->rows; g.N = d->inputs; g.K = d->outputs; g.batch = 1;
-  g.in_dtype = d->dtype ? kBF16 : kF32; g.out_dtype = kF32;
-  g.A = d->dy; g.lda = d->ld_dy;
+  g.in_dtype = g.out_dtype = kF32;
+  g.A = dy; g.lda = d->ld_dy;
   g.B = d->weight; g.ldb = d->ld_weight; g.b_mn = 1;
-  g.C = base; g.ldc = ld_base;
+  g.C = dx; g.ldc = d->ld_dx;
   e = launch_gemm_simt(g, st);
   if (e != cudaSuccess) return e;
-  e = launch_with(dim3(d->rows, (d->inputs + 255) / 256), 256, 0, st)(k_adapter_expand_simple<T, true>, base, ld_base, (T*)d->dx, d->ld_dx,
-                                                                 d->inputs, A, d->rank, nullptr, segs, ds);
+  e = launch_with(dim3(d->rows, (d->inputs + 255) / 256), 256, 0, st)(k_adapter_expand_f32<true>, dx, d->ld_dx, d->inputs, (const float*)d->A, d->rank, nullptr,
+                                                                 segs, ds);
   if (e != cudaSuccess) return e;
-  e = launch_grad_simple<T, false>(x, d->ld_x, d->inputs, ds, d->rank, nullptr, segs, d->dA, st);
+  e = launch_grad_f32<false>(x, d->ld_x, d->inputs, ds, d->rank, nullptr, segs, d->dA, st);
   if (e != cudaSuccess) return e;
-  return launch_grad_simple<T, true>(dy, d->ld_dy, d->outputs, d->s, d->rank, d->scale, segs, d->dB, st);
+  return launch_grad_f32<true>(dy, d->ld_dy, d->outputs, d->s, d->rank, d->scale, segs, d->dB, st);
+}
+
+// fp32: S of a forward pass that does not keep it, dS of a backward pass
+size_t workspace_bytes(const pbt_adapter_desc* d, bool backward) {
+  if (d->dtype) return tc_workspace(d, backward);
+  return std::max<size_t>(256, ((size_t)d->rows * d->rank * sizeof(float) + 255) & ~(size_t)255);
+}
+
+int check_workspace(const pbt_adapter_desc* d, bool backward, const void* workspace, size_t bytes) {
+  if (workspace && ((uintptr_t)workspace & 255) == 0 && bytes >= workspace_bytes(d, backward)) return PBT_OK;
+  return fail(PBT_ERR_WORKSPACE, "workspace missing, not 256-byte aligned or smaller than pbt_adapter_query_workspace says");
 }
 
 }  // namespace
@@ -208,7 +191,7 @@ extern "C" int pbt_adapter_query_workspace(const pbt_adapter_desc* d, int backwa
   if (!bytes) return fail(PBT_ERR_INVALID_ARG, "bytes is NULL");
   const int rc = check(d);
   if (rc) return rc;
-  *bytes = layout(d, backward != 0).total;
+  *bytes = workspace_bytes(d, backward != 0);
   return PBT_OK;
 }
 
@@ -220,12 +203,10 @@ extern "C" int pbt_adapter_forward(const pbt_adapter_desc* d, void* workspace, s
   if (!d->rows) return PBT_OK;
   if (!d->x || !d->y || d->ld_x < d->inputs || d->ld_y < d->outputs)
     return fail(PBT_ERR_INVALID_ARG, "x or y is NULL, or its row stride is smaller than a row");
-  const Layout l = layout(d, false);
-  if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < l.total)
-    return fail(PBT_ERR_WORKSPACE, "workspace missing, not 256-byte aligned or smaller than pbt_adapter_query_workspace says");
+  const int ws = check_workspace(d, false, workspace, workspace_bytes);
+  if (ws) return ws;
   const Segments segs = {d->row_offsets, d->adapter_ids, d->n_segments, d->rows, d->n_adapters};
-  const cudaError_t e = d->dtype ? forward_simple<bf16>(d, segs, (char*)workspace, l, (cudaStream_t)stream)
-                                 : forward_simple<float>(d, segs, (char*)workspace, l, (cudaStream_t)stream);
+  const cudaError_t e = d->dtype ? tc_forward(d, segs, (char*)workspace, (cudaStream_t)stream) : forward_f32(d, segs, (float*)workspace, (cudaStream_t)stream);
   return e == cudaSuccess ? PBT_OK : fail(PBT_ERR_CUDA, cudaGetErrorString(e));
 }
 
@@ -237,9 +218,8 @@ extern "C" int pbt_adapter_backward(const pbt_adapter_desc* d, void* workspace, 
   if (!d->dA || !d->dB) return fail(PBT_ERR_INVALID_ARG, "dA or dB is NULL");
   if (d->rows && (!d->x || !d->dy || !d->dx || !d->s || d->ld_x < d->inputs || d->ld_dy < d->outputs || d->ld_dx < d->inputs))
     return fail(PBT_ERR_INVALID_ARG, "x, s, dy or dx is NULL, or a row stride is smaller than a row");
-  const Layout l = layout(d, true);
-  if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < l.total)
-    return fail(PBT_ERR_WORKSPACE, "workspace missing, not 256-byte aligned or smaller than pbt_adapter_query_workspace says");
+  const int ws = check_workspace(d, true, workspace, workspace_bytes);
+  if (ws) return ws;
   cudaStream_t st = (cudaStream_t)stream;
   cudaError_t e;
   if (!d->rows) {
@@ -247,7 +227,7 @@ extern "C" int pbt_adapter_backward(const pbt_adapter_desc* d, void* workspace, 
     if (e == cudaSuccess) e = cudaMemsetAsync(d->dB, 0, (size_t)d->n_adapters * d->rank * d->outputs * sizeof(float), st);
   } else {
     const Segments segs = {d->row_offsets, d->adapter_ids, d->n_segments, d->rows, d->n_adapters};
-    e = d->dtype ? backward_simple<bf16>(d, segs, (char*)workspace, l, st) : backward_simple<float>(d, segs, (char*)workspace, l, st);
+    e = d->dtype ? tc_backward(d, segs, (char*)workspace, st) : backward_f32(d, segs, (float*)workspace, st);
   }
   return e == cudaSuccess ? PBT_OK : fail(PBT_ERR_CUDA, cudaGetErrorString(e));
 }

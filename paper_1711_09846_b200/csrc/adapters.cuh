@@ -17,6 +17,11 @@ struct Segments {
   int n, rows, n_adapters;
 };
 
+// bf16, on the tensor cores (adapters_tc.cu)
+size_t tc_workspace(const pbt_adapter_desc* d, bool backward);
+cudaError_t tc_forward(const pbt_adapter_desc* d, const Segments& segs, char* workspace, cudaStream_t s);
+cudaError_t tc_backward(const pbt_adapter_desc* d, const Segments& segs, char* workspace, cudaStream_t s);
+
 #ifdef __CUDACC__
 __device__ __forceinline__ int segment_begin(const Segments& s, int j) { return min(max(__ldg(s.offsets + j), 0), s.rows); }
 __device__ __forceinline__ int segment_adapter(const Segments& s, int j) {

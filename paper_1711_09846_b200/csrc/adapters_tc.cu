@@ -1,0 +1,834 @@
+// bf16 adapters on the tensor cores.  Three kernels carry both directions:
+//
+//   k_adapter_shrink   S = x A_a^T (or dS = c dy B_a): a product with r <= 64 columns, bound by reading x once; rows of
+//                      one (64-row tile, segment) pair per CTA, mma.sync fed by 16-byte loads straight from global memory
+//   k_adapter_gemm     y = x W^T + bias + c S B_a^T (or dx = dy W + dS A_a): the shared product on tcgen05, with the
+//                      low-rank product as one more block of the same contraction in the same TMEM accumulator
+//   k_adapter_grad     dA_a = dS^T x, dB_a = dy^T (c S): contractions over an adapter's rows on tcgen05, r columns wide
+//
+// Segments and tiles.  Output tiles are 128 consecutive rows whatever the segments; for every segment that reaches into
+// a tile the low-rank block is issued once with that adapter's matrix and with the other segments' rows switched off in
+// the instruction (the disable-output-lane mask: a TMEM lane is a row).  Rows are therefore independent of one another's
+// adapters exactly, not up to a multiplication with zero: an adapter that has diverged to NaN reaches only its own rows.
+//
+// Precision.  The low-rank operand of a bf16 result is S (dS) rounded once to bf16, like every GEMM operand of a bf16
+// population; the result is rounded to bf16 anyway.  dA and dB are fp32 results, so their operand is S (dS) as the sum of
+// three bf16 numbers (24 bits), whose three products land in separate accumulator columns and are added in fp32.  The tensor
+// cores' accumulation truncates (about 2^-24 of the accumulator per instruction), so chains are kept short: the shrink
+// folds its accumulators into fp32 registers every 64 columns, the gradients every 128 rows.
+#include <algorithm>
+
+#include "adapters.cuh"
+#include "tc_epilogue.cuh"
+
+namespace pbt {
+namespace adapters {
+namespace {
+
+using namespace tc;
+
+// ------------------------------------------------------------------------------------------------------------------
+// Operands whose rows are not multiples of 16 bytes are copied once into rows that are.
+// ------------------------------------------------------------------------------------------------------------------
+__global__ void __launch_bounds__(256) k_pack_rows(const bf16* __restrict__ src, long long ld, long long rows, int cols, bf16* __restrict__ dst,
+                                                   int ld_dst) {
+  pdl_prologue();
+  const long long n = rows * ld_dst;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+    const long long r = i / ld_dst;
+    const int c = (int)(i % ld_dst);
+    dst[i] = c < cols ? src[r * ld + c] : __float2bfloat16_rn(0.f);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// Shrink
+// ------------------------------------------------------------------------------------------------------------------
+constexpr int kShrinkRows = 64;
+
+struct ShrinkArgs {
+  const bf16* x; long long ldx; int K;
+  const bf16* mats; int pitch;        // A_a [rank][pitch] (K of them used), or B_a [K][pitch] (rank of them used)
+  int rank, rp;                       // rp: columns of a plane, the rank rounded up to 16
+  const float* scale;
+  Segments segs;
+  int n_tiles;
+  float* s;                           // fp32 result, not scaled (may be null)
+  bf16* planes; int terms;            // scaled result as `terms` bf16 summands side by side, [rows][terms * rp]
+  const float* kept; bf16* kept_planes;   // a second fp32 matrix [rows][rank], split into three summands the same way
+  int* tile_seg; int tile_rows, n_table;  // first segment of every output tile of the product that follows
+};
+
+__device__ __forceinline__ uint4 ld16(const bf16* p) {
+  uint4 r;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+  return r;
+}
+__device__ __forceinline__ void mma16816(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t* r, uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+
+__device__ __forceinline__ void store_terms(bf16* row, int rp, int col, float v, int terms) {
+  for (int t = 0; t < terms; ++t) {
+    const bf16 h = __float2bfloat16_rn(v);
+    row[t * rp + col] = h;
+    v -= __bfloat162float(h);
+  }
+}
+
+// A warp multiplies 32 rows by the adapter's matrix over every `parts`-th block of 64 columns.  The columns of a block are
+// dealt to the fragments in the order in which 16-byte loads deliver them (lane t of a quad holds columns 8t .. 8t+7 of
+// each half block); the sum over k does not mind, as long as both operands use the same order.  B_a lies with its ranks
+// contiguous, so its fragments are transposed on the way: 64 rows of it go through shared memory, stored so that the
+// eight rows one ldmatrix takes are 128 consecutive bytes.
+template <bool TRANS, int NT>
+__global__ void __launch_bounds__(256) k_adapter_shrink(const ShrinkArgs a) {
+  pdl_prologue();
+  extern __shared__ __align__(16) uint8_t shrink_smem[];
+  const int q = blockIdx.x, tid = threadIdx.x;
+  const Segments& g = a.segs;
+  if (q >= a.n_tiles + g.n) {
+    const int i = (q - a.n_tiles - g.n) * 256 + tid;
+    if (i < a.n_table) a.tile_seg[i] = max(segment_of_row(g, i * a.tile_rows), 0);
+    return;
+  }
+  // The pairs (tile t, segment j) that meet ascend in t + j by at least one, so q = t + j names at most one of them: j is
+  // the last segment whose first pair is not behind q.
+  int j = -1;
+  for (int base = 0; base < g.n; base += 256) {
+    const int i = base + tid;
+    j += __syncthreads_count(i < g.n && segment_begin(g, i) / kShrinkRows + i <= q);
+  }
+  if (j < 0) return;
+  const int t = q - j;
+  const int adapter = segment_adapter(g, j);
+  const int lo = max(segment_begin(g, j), t * kShrinkRows), hi = min(segment_begin(g, j + 1), (t + 1) * kShrinkRows);
+  if (lo >= hi || adapter < 0) return;
+
+  const int warp = tid >> 5, lane = tid & 31, gr = lane >> 2, tq = lane & 3;
+  const int groups = hi - lo > 32 ? 2 : 1, parts = 8 / groups;     // few rows: more warps share the columns
+  const int group = warp / parts, part = warp % parts;
+  const int nt8 = TRANS ? a.pitch / 8 : (a.rank + 7) / 8;
+  const bf16* mat = a.mats + (long long)adapter * (TRANS ? (long long)a.K : (long long)a.rank) * a.pitch;
+  const bf16* xrow[4];
+  bool in[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = lo + group * 32 + gr + 8 * i;
+    in[i] = row < hi;
+    xrow[i] = a.x + (long long)row * a.ldx;
+  }
+  uint8_t* stage = shrink_smem + warp * (NT * 1024);
+  const uint32_t stage_addr = smem_u32(stage);
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  float acc[2][NT][4] = {};
+  for (int k0 = part * 64; k0 < a.K; k0 += parts * 64) {
+    uint4 xv[4][2], bv[TRANS ? 1 : NT][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int k = k0 + h * 32 + tq * 8;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) xv[i][h] = in[i] && k < a.K ? ld16(xrow[i] + k) : zero;
+      if constexpr (!TRANS) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const int r = n * 8 + gr;
+          bv[n][h] = r < a.rank && k < a.K ? __ldg(reinterpret_cast<const uint4*>(mat + (long long)r * a.pitch + k)) : zero;
+        }
+      }
+    }
+    if constexpr (TRANS) {
+      __syncwarp();   // the previous block's fragments have been read
+      for (int p = lane; p < 64 * nt8; p += 32) {
+        const int k = p / nt8, n = p % nt8;
+        const uint4 v = k0 + k < a.K ? __ldg(reinterpret_cast<const uint4*>(mat + (long long)(k0 + k) * a.pitch) + n) : zero;
+        *reinterpret_cast<uint4*>(stage + n * 1024 + ((k & 32) + (k & 7) * 4 + ((k & 31) >> 3)) * 16) = v;
+      }
+      __syncwarp();
+    }
+    float sum[2][NT][4] = {};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        if (n >= nt8) continue;
+        uint32_t b[4];   // two steps of 16 columns, two registers each
+        if constexpr (TRANS) {
+          // matrix m = lane / 8 holds, for step m / 2 and half m % 2, row 2t + e: column 8t + 4 (m / 2) + 2 (m % 2) + e of the block
+          const int m = lane >> 3, c = lane & 7;
+          ldmatrix4_trans(b, stage_addr + n * 1024 + (h * 32 + (4 * (m >> 1) + 2 * (m & 1) + (c & 1)) * 4 + (c >> 1)) * 16);
+        } else {
+          b[0] = bv[n][h].x; b[1] = bv[n][h].y; b[2] = bv[n][h].z; b[3] = bv[n][h].w;
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+            mma16816(sum[m][n], word(xv[2 * m][h], 2 * s), word(xv[2 * m + 1][h], 2 * s), word(xv[2 * m][h], 2 * s + 1),
+                     word(xv[2 * m + 1][h], 2 * s + 1), b[2 * s], b[2 * s + 1]);
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[m][n][e] += sum[m][n][e];
+  }
+  __syncthreads();   // the staging memory becomes the parts' sums: [warp][32 rows][8 NT]
+  float* red = reinterpret_cast<float*>(shrink_smem);
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        *reinterpret_cast<float2*>(&red[(warp * 32 + m * 16 + gr + 8 * e) * (NT * 8) + n * 8 + tq * 2]) = make_float2(acc[m][n][2 * e], acc[m][n][2 * e + 1]);
+  __syncthreads();
+  const float f = a.scale[adapter];
+  const int width = a.terms * a.rp;
+  for (int i = tid; i < (hi - lo) * a.rp; i += 256) {
+    const int r = i / a.rp, c = i % a.rp;
+    const long long row = lo + r;
+    float v = 0.f;
+    if (c < a.rank) {
+      for (int p = 0; p < parts; ++p) v += red[(((r >> 5) * parts + p) * 32 + (r & 31)) * (NT * 8) + c];
+      if (a.s) a.s[row * a.rank + c] = v;
+    }
+    store_terms(a.planes + row * width, a.rp, c, f * v, a.terms);
+    if (a.kept) store_terms(a.kept_planes + row * 3 * a.rp, a.rp, c, c < a.rank ? f * a.kept[row * a.rank + c] : 0.f, 3);
+  }
+}
+
+template <bool TRANS, int NT>
+cudaError_t launch_shrink(const ShrinkArgs& a, unsigned grid, cudaStream_t s) {
+  static DeviceSetup setup;
+  int sms = 0;
+  const cudaError_t e = device_setup(&setup, k_adapter_shrink<TRANS, NT>, NT * 8192, &sms);
+  if (e != cudaSuccess) return e;
+  return launch_with(grid, 256, NT * 8192, s)(k_adapter_shrink<TRANS, NT>, a);
+}
+template <bool TRANS>
+cudaError_t launch_shrink(ShrinkArgs a, cudaStream_t s) {
+  a.n_tiles = (a.segs.rows + kShrinkRows - 1) / kShrinkRows;
+  const unsigned grid = (unsigned)(a.n_tiles + a.segs.n + (a.n_table + 255) / 256);
+  if (a.rank <= 8) return launch_shrink<TRANS, 1>(a, grid, s);
+  if (a.rank <= 16) return launch_shrink<TRANS, 2>(a, grid, s);
+  if (a.rank <= 32) return launch_shrink<TRANS, 4>(a, grid, s);
+  return launch_shrink<TRANS, 8>(a, grid, s);
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// Shared product with the low-rank block
+// ------------------------------------------------------------------------------------------------------------------
+constexpr int kGemmStages128 = 4, kGemmStages256 = 3, kGemmEpiWarps = 8;
+
+struct LowRank {
+  Segments segs;
+  const int* tile_seg;
+  int steps;        // MMA steps of 16 ranks
+};
+
+// The segments that reach into rows [m0, m0 + tile_rows): walked in the same order by the roles of a CTA.
+struct SegmentWalk {
+  const Segments& g;
+  int j, m0, m1;
+  __device__ SegmentWalk(const Segments& segs, int first, int row0, int tile_rows) : g(segs), j(first), m0(row0), m1(min(row0 + tile_rows, segs.rows)) {}
+  // next segment with an adapter and rows in the tile; false at the end
+  __device__ bool next(int& adapter, int& lo, int& hi) {
+    while (j < g.n) {
+      const int b = segment_begin(g, j), e = segment_begin(g, j + 1);
+      if (b >= m1) return false;
+      adapter = segment_adapter(g, j);
+      ++j;
+      lo = max(b, m0);
+      hi = min(e, m1);
+      if (adapter >= 0 && lo < hi) return true;
+    }
+    return false;
+  }
+};
+
+// bits of the rows of a 32-row group that starts at `base` and are NOT in [lo, hi)
+__device__ __forceinline__ uint32_t rows_off(int base, int lo, int hi) {
+  const int b = min(max(lo - base, 0), 32), e = min(max(hi - base, 0), 32);
+  const uint32_t below_e = e >= 32 ? 0xFFFFFFFFu : (1u << e) - 1u, below_b = b >= 32 ? 0xFFFFFFFFu : (1u << b) - 1u;
+  return ~(below_e & ~below_b);
+}
+
+// the lanes whose bit is set keep their accumulator
+__device__ __forceinline__ void umma_bf16_rows(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, const uint32_t* off) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.eq.b32 p, 1, 1;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%4, %5, %6, %7}, p;\n\t}"
+      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(off[0]), "r"(off[1]), "r"(off[2]), "r"(off[3])
+      : "memory");
+}
+
+template <int BN, int STAGES>
+struct GemmSmem {
+  static constexpr int kABytes = kBM * kBK * 2;
+  static constexpr int kBBytes = BN * kBK * 2;
+  static constexpr int kStageBytes = kABytes + kBBytes;
+  static constexpr int kEpiOffset = STAGES * kStageBytes;
+  static constexpr int kEpiBytesPerWarp = 32 * kEpiPitch * 4;
+  static constexpr int kBarOffset = kEpiOffset + kGemmEpiWarps * kEpiBytesPerWarp;
+  static constexpr int kTotal = kBarOffset + 256 + 1024;
+  static_assert(kTotal <= 232448, "shared memory budget of one CTA");
+};
+
+// Roles as in the member-batched GEMM: warp 0 TMA producer, warp 1 MMA issuer, 8 epilogue warps, double-buffered
+// accumulator.  After a tile's k-blocks both walk its segments: one more stage each, 128 rows of the low-rank operand and
+// the adapter's matrix (columns past the rank are out of the tensor map and arrive as zeros).
+template <int BN, int STAGES, bool B_MN>
+__global__ void __launch_bounds__(64 + 32 * kGemmEpiWarps, 1)
+k_adapter_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmP,
+               const __grid_constant__ CUtensorMap tmL, const TcParams p, const LowRank low) {
+  pdl_prologue();
+  using L = GemmSmem<BN, STAGES>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBarOffset);
+  uint64_t* empty = full + STAGES;
+  uint64_t* tfull = empty + STAGES;
+  uint64_t* tempty = tfull + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty + 2);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  constexpr uint32_t kTmemCols = 2 * BN;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+    for (int a = 0; a < 2; ++a) { mbar_init(&tfull[a], 1); mbar_init(&tempty[a], kGemmEpiWarps); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) tmem_alloc(tmem_slot, kTmemCols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t stage = 0, phase = 0;
+      bool ok = true;
+      for (int tile = blockIdx.x; tile < p.num_tiles && ok; tile += gridDim.x) {
+        const int tm = tile / p.tiles_n, m0 = tm * kBM, n0 = (tile % p.tiles_n) * BN;
+        const int first = __ldg(low.tile_seg + tm);
+        for (int kb = 0; kb < p.k_blocks; ++kb) {
+          if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) { ok = false; break; }
+          uint8_t* sa = smem + stage * L::kStageBytes;
+          uint8_t* sb = sa + L::kABytes;
+          mbar_expect_tx(&full[stage], L::kStageBytes);
+          const int k0 = kb * kBK;
+          tma_load_3d(sa, &tmA, &full[stage], k0, m0, 0);
+          if constexpr (!B_MN) {
+            tma_load_3d(sb, &tmB, &full[stage], k0, n0, 0);
+          } else {
+#pragma unroll
+            for (int j = 0; j < BN / 64; ++j) tma_load_3d(sb + j * 8192, &tmB, &full[stage], n0 + j * 64, k0, 0);
+          }
+          if (++stage == STAGES) { stage = 0; phase ^= 1; }
+        }
+        SegmentWalk walk(low.segs, first, m0, kBM);
+        int adapter, lo, hi;
+        while (ok && walk.next(adapter, lo, hi)) {
+          if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) { ok = false; break; }
+          uint8_t* sa = smem + stage * L::kStageBytes;
+          uint8_t* sb = sa + L::kABytes;
+          mbar_expect_tx(&full[stage], L::kStageBytes);
+          tma_load_3d(sa, &tmP, &full[stage], 0, m0, 0);
+          if constexpr (!B_MN) {
+            tma_load_3d(sb, &tmL, &full[stage], 0, n0, adapter);
+          } else {
+#pragma unroll
+            for (int j = 0; j < BN / 64; ++j) tma_load_3d(sb + j * 8192, &tmL, &full[stage], n0 + j * 64, 0, adapter);
+          }
+          if (++stage == STAGES) { stage = 0; phase ^= 1; }
+        }
+      }
+      if (!ok) {
+        *abort_flag = 1;
+        atomicCAS(&p.counters->status, 0, PBT_ERR_TIMEOUT);
+        p.counters->status_info = 31;
+      }
+      // every stage this thread armed has landed and been read before the CTA exits
+      for (int s = 0; s < STAGES && ok; ++s) {
+        if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) break;
+        if (++stage == STAGES) { stage = 0; phase ^= 1; }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)B_MN << 16) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(kBM >> 4) << 24);
+      uint32_t stage = 0, phase = 0;
+      int it = 0;
+      bool ok = true;
+      for (int tile = blockIdx.x; tile < p.num_tiles && ok; tile += gridDim.x, ++it) {
+        const int tm = tile / p.tiles_n, m0 = tm * kBM;
+        const int first = __ldg(low.tile_seg + tm);
+        const int acc = it & 1;
+        if (!mbar_wait(&tempty[acc], ((it >> 1) & 1) ^ 1, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t tmem_d = tmem_base + acc * BN;
+        for (int kb = 0; kb < p.k_blocks; ++kb) {
+          if (!mbar_wait(&full[stage], phase, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t sa = smem_u32(smem + stage * L::kStageBytes), sb = sa + L::kABytes;
+#pragma unroll
+          for (int k = 0; k < kBK / 16; ++k)
+            umma_bf16(tmem_d, smem_desc(sa + k * 32, 16, 1024), B_MN ? smem_desc(sb + k * 2048, 8192, 1024) : smem_desc(sb + k * 32, 16, 1024), idesc,
+                      (kb | k) != 0 ? 1u : 0u);
+          umma_commit(&empty[stage]);
+          if (++stage == STAGES) { stage = 0; phase ^= 1; }
+        }
+        SegmentWalk walk(low.segs, first, m0, kBM);
+        int adapter, lo, hi;
+        while (ok && walk.next(adapter, lo, hi)) {
+          if (!mbar_wait(&full[stage], phase, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t sa = smem_u32(smem + stage * L::kStageBytes), sb = sa + L::kABytes;
+          uint32_t off[4];
+#pragma unroll
+          for (int w = 0; w < 4; ++w) off[w] = rows_off(m0 + 32 * w, lo, hi);
+          for (int k = 0; k < low.steps; ++k)
+            umma_bf16_rows(tmem_d, smem_desc(sa + k * 32, 16, 1024), B_MN ? smem_desc(sb + k * 2048, 8192, 1024) : smem_desc(sb + k * 32, 16, 1024), idesc, off);
+          umma_commit(&empty[stage]);
+          if (++stage == STAGES) { stage = 0; phase ^= 1; }
+        }
+        if (ok) umma_commit(&tfull[acc]);
+      }
+      if (!ok) {
+        *abort_flag = 1;
+        atomicCAS(&p.counters->status, 0, PBT_ERR_TIMEOUT);
+        p.counters->status_info = 32;
+      }
+    }
+  } else {
+    const int q = warp & 3, e = warp - 2, half = e >> 2;
+    float* buf = reinterpret_cast<float*>(smem + L::kEpiOffset + e * L::kEpiBytesPerWarp);
+    int it = 0;
+    bool ok = true;
+    const bool vec_ok = (((uintptr_t)p.C & 15) == 0) && ((p.ldc * 2) % 16 == 0) && (!p.bias || (((uintptr_t)p.bias & 15) == 0));
+    for (int tile = blockIdx.x; tile < p.num_tiles && ok; tile += gridDim.x, ++it) {
+      const int m0 = (tile / p.tiles_n) * kBM, n0 = (tile % p.tiles_n) * BN;
+      const int acc = it & 1;
+      if (!mbar_wait(&tfull[acc], (it >> 1) & 1, abort_flag)) { ok = false; break; }
+      tc_fence_after();
+      epilogue_tile<BN, kGemmEpiWarps>(p, buf, tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN), 0, m0, n0, q, half, lane, vec_ok);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&tempty[acc]);
+    }
+    if (!ok && lane == 0) {
+      *abort_flag = 1;
+      atomicCAS(&p.counters->status, 0, PBT_ERR_TIMEOUT);
+      p.counters->status_info = 33;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) tmem_dealloc(tmem_base, kTmemCols);
+}
+
+template <int BN, int STAGES, bool B_MN>
+cudaError_t launch_gemm(const CUtensorMap* maps, TcParams& p, const LowRank& low, cudaStream_t s) {
+  using L = GemmSmem<BN, STAGES>;
+  static DeviceSetup setup;
+  int sms = 0;
+  const cudaError_t e = device_setup(&setup, k_adapter_gemm<BN, STAGES, B_MN>, L::kTotal, &sms);
+  if (e != cudaSuccess) return e;
+  p.tiles_n = (p.N + BN - 1) / BN;
+  p.num_tiles = p.tiles_m * p.tiles_n;
+  return launch_with(p.num_tiles < sms ? p.num_tiles : sms, 64 + 32 * kGemmEpiWarps, L::kTotal, s)(k_adapter_gemm<BN, STAGES, B_MN>, maps[0], maps[1], maps[2],
+                                                                                                maps[3], p, low);
+}
+
+// C[rows][N] = X[rows][K] B^T + bias + low-rank; B is [N][K], or [K][N] when b_mn; the low-rank matrices alike over ranks.
+struct GemmCall {
+  const bf16* x; long long ldx;
+  const bf16* b; long long ldb; int b_mn;
+  const bf16* planes; long long ld_planes; int rp;
+  const bf16* mats; int mat_pitch, rank;
+  void* c; long long ldc;
+  const float* bias;
+  int N, K;
+};
+cudaError_t launch_gemm(const GemmCall& c, const Segments& segs, const int* tile_seg, Counters* counters, cudaStream_t s) {
+  TcParams p;
+  memset(&p, 0, sizeof(p));
+  p.M = segs.rows; p.N = c.N; p.K = c.K; p.batch = 1;
+  p.tiles_m = (segs.rows + kBM - 1) / kBM;
+  p.k_blocks = (c.K + kBK - 1) / kBK;
+  p.C = c.c; p.ldc = c.ldc; p.out_dtype = kBF16;
+  p.bias = c.bias;
+  p.counters = counters;
+  const LowRank low = {segs, tile_seg, c.rp / 16};
+  // 256-wide tiles once they go round the SMs; below that, twice as many tiles of half the width
+  const bool wide = (long long)p.tiles_m * ((c.N + 255) / 256) >= 148;
+  CUtensorMap maps[4];
+  bool ok = make_map(&maps[0], c.x, c.K, segs.rows, c.ldx, 1, 0, kBM) && make_map(&maps[2], c.planes, c.rp, segs.rows, c.ld_planes, 1, 0, kBM);
+  if (!c.b_mn) {
+    ok = ok && make_map(&maps[1], c.b, c.K, c.N, c.ldb, 1, 0, wide ? 256 : 128);
+    ok = ok && make_map(&maps[3], c.mats, c.mat_pitch, c.N, c.mat_pitch, segs.n_adapters, (long long)c.N * c.mat_pitch, wide ? 256 : 128);
+  } else {
+    ok = ok && make_map(&maps[1], c.b, c.N, c.K, c.ldb, 1, 0, kBK);
+    ok = ok && make_map(&maps[3], c.mats, c.N, c.rank, c.mat_pitch, segs.n_adapters, (long long)c.rank * c.mat_pitch, kBK);
+  }
+  if (!ok) return cudaErrorInvalidValue;
+  if (c.b_mn) return wide ? launch_gemm<256, kGemmStages256, true>(maps, p, low, s) : launch_gemm<128, kGemmStages128, true>(maps, p, low, s);
+  return wide ? launch_gemm<256, kGemmStages256, false>(maps, p, low, s) : launch_gemm<128, kGemmStages128, false>(maps, p, low, s);
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// Gradients of the adapters
+// ------------------------------------------------------------------------------------------------------------------
+constexpr int kGradStages = 4, kGradChunk = 512, kGradList = 1024;
+
+struct GradArgs {
+  Segments segs;
+  int rank, rp, boxes, term_cols;      // boxes of 64 columns of the planes; term_cols = 3 rp
+  int K, N, blocks_k;                  // column blocks of dA come first, those of dB after them
+  int splits;
+  float *dA, *dB;                      // [splits][adapters][...]: the results themselves when splits == 1
+  long long stride_a, stride_b;        // elements of one split
+  uint32_t tmem_cols;
+  Counters* counters;
+};
+
+// a bounded wait of a whole warp: every lane gives up if one does
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag));
+}
+
+// One CTA: 128 columns of v (x for dA, dy for dB) of one adapter, over every splits-th chunk of 512 rows of it.  The 128
+// columns are the accumulator's lanes, its columns the three summands of the r ranks.  Both operands are read as they lie
+// (rows = contraction index: MN-major).  Where a block of 64 rows ends inside a segment's last box, the rows behind the
+// end (another member's) are cleared in shared memory in both operands before the MMA reads them.
+__global__ void __launch_bounds__(192) k_adapter_grad(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmDS,
+                                                      const __grid_constant__ CUtensorMap tmDY, const __grid_constant__ CUtensorMap tmS, const GradArgs a) {
+  pdl_prologue();
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  const int stage_bytes = 16384 + a.boxes * 8192;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + kGradStages * stage_bytes);
+  uint64_t* empty = full + kGradStages;
+  uint64_t* tfull = empty + kGradStages;
+  uint64_t* tempty = tfull + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty + 2);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int2* list = reinterpret_cast<int2*>(tempty + 4);
+  __shared__ int list_n;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int adapter = blockIdx.y, z = blockIdx.z;
+  const bool is_b = (int)blockIdx.x >= a.blocks_k;
+  const int c0 = ((int)blockIdx.x - (is_b ? a.blocks_k : 0)) * 128;
+  const CUtensorMap* tmV = is_b ? &tmDY : &tmX;
+  const CUtensorMap* tmT = is_b ? &tmS : &tmDS;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kGradStages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 4); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) tmem_alloc(tmem_slot, a.tmem_cols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+
+  uint32_t stage = 0, phase = 0;   // producer, MMA warp
+  int folds = 0;                   // MMA warp, epilogue: accumulators handed over so far
+  bool ok = true;
+  float acc[kMaxRank];
+#pragma unroll
+  for (int i = 0; i < kMaxRank; ++i) acc[i] = 0.f;
+
+  // The adapter's segments, kGradList table entries at a time, as a list of row ranges in shared memory.
+  for (int base = 0; base < a.segs.n; base += kGradList) {
+    __syncthreads();
+    if (warp == 0) {
+      int n = 0;
+      for (int i0 = base; i0 < min(a.segs.n, base + kGradList); i0 += 32) {   // (kGradList is a multiple of 32)
+        const int i = i0 + lane;
+        const bool have = i < a.segs.n && segment_adapter(a.segs, i) == adapter;
+        const int2 r = have ? make_int2(segment_begin(a.segs, i), segment_begin(a.segs, i + 1)) : make_int2(0, 0);
+        const bool keep = have && r.x < r.y;
+        const uint32_t votes = __ballot_sync(0xFFFFFFFFu, keep);
+        if (keep) list[n + __popc(votes & ((1u << lane) - 1u))] = r;
+        n += __popc(votes);
+      }
+      if (lane == 0) list_n = n;
+    }
+    __syncthreads();
+    const int n = list_n;
+    int blocks = 0;   // blocks of 64 rows in this list that belong to this split
+    for (int i = 0; i < n; ++i)
+      for (int t = list[i].x / kGradChunk; t * kGradChunk < list[i].y; ++t)
+        if (t % a.splits == z) blocks += (min(list[i].y, (t + 1) * kGradChunk) - max(list[i].x, t * kGradChunk) + 63) / 64;
+
+    if (warp == 0) {
+      if (lane == 0 && ok) {
+        for (int i = 0; i < n && ok; ++i)
+          for (int t = list[i].x / kGradChunk; t * kGradChunk < list[i].y && ok; ++t) {
+            if (t % a.splits != z) continue;
+            const int end = min(list[i].y, (t + 1) * kGradChunk);
+            for (int row = max(list[i].x, t * kGradChunk); row < end; row += 64) {
+              if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) { ok = false; break; }
+              uint8_t* sv = smem + stage * stage_bytes;
+              mbar_expect_tx(&full[stage], stage_bytes);
+              tma_load_3d(sv, tmV, &full[stage], c0, row, 0);
+              tma_load_3d(sv + 8192, tmV, &full[stage], c0 + 64, row, 0);
+              for (int b = 0; b < a.boxes; ++b) tma_load_3d(sv + 16384 + b * 8192, tmT, &full[stage], b * 64, row, 0);
+              if (++stage == kGradStages) { stage = 0; phase ^= 1; }
+            }
+          }
+      }
+    } else if (warp == 1) {
+      const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(a.term_cols >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+      int done = 0;
+      for (int i = 0; i < n && ok; ++i)
+        for (int t = list[i].x / kGradChunk; t * kGradChunk < list[i].y && ok; ++t) {
+          if (t % a.splits != z) continue;
+          const int end = min(list[i].y, (t + 1) * kGradChunk);
+          for (int row = max(list[i].x, t * kGradChunk); row < end; row += 64, ++done) {
+            const int acc_buf = folds & 1;
+            if ((done & 1) == 0) {
+              if (!warp_wait(&tempty[acc_buf], ((folds >> 1) & 1) ^ 1, abort_flag)) { ok = false; break; }
+            }
+            if (!warp_wait(&full[stage], phase, abort_flag)) { ok = false; break; }
+            uint8_t* sv = smem + stage * stage_bytes;
+            const int valid = end - row;
+            if (valid < 64) {   // rows are 128-byte lines of each box
+              for (int b = 0; b < 2 + a.boxes; ++b)
+                for (int o = valid * 8 + lane; o < 64 * 8; o += 32) reinterpret_cast<uint4*>(sv + b * 8192)[o] = make_uint4(0u, 0u, 0u, 0u);
+              fence_async_smem();
+              __syncwarp();
+            }
+            if (lane == 0) {
+              tc_fence_after();
+              const uint32_t sa = smem_u32(sv), sb = sa + 16384;
+              const uint32_t tmem_d = tmem_base + (uint32_t)(acc_buf * a.term_cols);
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                umma_bf16(tmem_d, smem_desc(sa + k * 2048, 8192, 1024), smem_desc(sb + k * 2048, 8192, 1024), idesc, ((done & 1) | k) != 0 ? 1u : 0u);
+              umma_commit(&empty[stage]);
+              if ((done & 1) == 1 || done + 1 == blocks) umma_commit(&tfull[acc_buf]);
+            }
+            __syncwarp();
+            if ((done & 1) == 1 || done + 1 == blocks) ++folds;
+            if (++stage == kGradStages) { stage = 0; phase ^= 1; }
+          }
+        }
+    } else {
+      const int q = warp & 3;
+      for (int f = 0; f < (blocks + 1) / 2 && ok; ++f, ++folds) {
+        const int acc_buf = folds & 1;
+        if (!warp_wait(&tfull[acc_buf], (folds >> 1) & 1, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t t0 = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc_buf * a.term_cols);
+#pragma unroll
+        for (int c = 0; c < kMaxRank; c += 16) {
+          if (c >= a.rp) continue;
+          uint32_t h[16], m[16], l[16];
+          tmem_ld16(t0 + c, h);
+          tmem_ld16(t0 + a.rp + c, m);
+          tmem_ld16(t0 + 2 * a.rp + c, l);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[c + i] += __uint_as_float(h[i]) + (__uint_as_float(m[i]) + __uint_as_float(l[i]));
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&tempty[acc_buf]);
+      }
+    }
+  }
+  if (!ok && lane == 0) {
+    *abort_flag = 1;
+    atomicCAS(&a.counters->status, 0, PBT_ERR_TIMEOUT);
+    a.counters->status_info = 40 + min(warp, 2);
+  }
+  // the last commits into `empty` have landed before the CTA exits
+  if (warp == 0 && lane == 0 && ok)
+    for (int s = 0; s < kGradStages; ++s) {
+      if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) break;
+      if (++stage == kGradStages) { stage = 0; phase ^= 1; }
+    }
+  if (warp >= 2) {
+    const int col = c0 + (warp & 3) * 32 + lane;
+    if (!is_b && col < a.K) {
+      float* o = a.dA + z * a.stride_a + (long long)adapter * a.rank * a.K + col;
+#pragma unroll
+      for (int i = 0; i < kMaxRank; ++i)
+        if (i < a.rank) o[(long long)i * a.K] = acc[i];
+    } else if (is_b && col < a.N) {
+      float* o = a.dB + z * a.stride_b + ((long long)adapter * a.N + col) * a.rank;
+#pragma unroll
+      for (int i = 0; i < kMaxRank; ++i)
+        if (i < a.rank) o[i] = acc[i];
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) tmem_dealloc(tmem_base, a.tmem_cols);
+}
+
+// out = the splits' partial results, added in order
+__global__ void __launch_bounds__(256) k_adapter_grad_join(const float* __restrict__ pa, const float* __restrict__ pb, long long na, long long nb, int splits,
+                                                           float* __restrict__ dA, float* __restrict__ dB) {
+  pdl_prologue();
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < na + nb; i += (long long)gridDim.x * 256) {
+    const bool is_b = i >= na;
+    const float* p = is_b ? pb + (i - na) : pa + i;
+    const long long stride = is_b ? nb : na;
+    float t = 0.f;
+    for (int z = 0; z < splits; ++z) t += p[z * stride];
+    (is_b ? dB[i - na] : dA[i]) = t;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// Host side
+// ------------------------------------------------------------------------------------------------------------------
+size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+int round_up(int n, int m) { return (n + m - 1) / m * m; }
+bool aligned(const void* p, long long ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
+
+struct Plan {
+  int rp, splits;
+  bool pack_x, pack_w, pack_a, pack_b, pack_dy;
+  size_t x, w, a, b, dy, planes, kept, table, parts, total;
+};
+Plan plan(const pbt_adapter_desc* d, bool backward) {
+  Plan p;
+  memset(&p, 0, sizeof(p));
+  const size_t rows = (size_t)d->rows;
+  p.rp = round_up(d->rank, 16);
+  p.pack_x = !aligned(d->x, d->ld_x) || d->inputs % 8;     // (vector loads end with the row)
+  p.pack_w = !aligned(d->weight, d->ld_weight);
+  p.pack_a = !aligned(d->A, d->inputs);
+  p.pack_b = !aligned(d->B, d->rank);
+  p.pack_dy = backward && (!aligned(d->dy, d->ld_dy) || d->outputs % 8);
+  // enough CTAs for two per SM, at most one split per chunk of rows
+  const int blocks = (d->inputs + 127) / 128 + (d->outputs + 127) / 128;
+  p.splits = std::max(1, std::min((2 * 148 + blocks * d->n_adapters - 1) / (blocks * d->n_adapters), (d->rows + kGradChunk - 1) / kGradChunk));
+  size_t at = 0;
+  auto take = [&](bool want, size_t bytes) {
+    const size_t here = at;
+    if (want) at += align256(bytes);
+    return here;
+  };
+  p.x = take(p.pack_x, rows * round_up(d->inputs, 8) * 2);
+  p.w = take(p.pack_w, (size_t)d->outputs * round_up(d->inputs, 8) * 2);
+  p.a = take(p.pack_a, (size_t)d->n_adapters * d->rank * round_up(d->inputs, 8) * 2);
+  p.b = take(p.pack_b, (size_t)d->n_adapters * d->outputs * round_up(d->rank, 8) * 2);
+  p.dy = take(p.pack_dy, rows * round_up(d->outputs, 8) * 2);
+  p.planes = take(true, rows * p.rp * 2 * (backward ? 3 : 1));
+  p.kept = take(backward, rows * p.rp * 2 * 3);
+  p.table = take(true, ((rows + kBM - 1) / kBM) * sizeof(int));
+  p.parts = take(backward && p.splits > 1, (size_t)p.splits * d->n_adapters * d->rank * ((size_t)d->inputs + d->outputs) * sizeof(float));
+  p.total = std::max<size_t>(at, 256);
+  return p;
+}
+
+cudaError_t pack(const void*& src, long long& ld, long long rows, int cols, char* dst, cudaStream_t s) {
+  const int to = round_up(cols, 8);
+  const long long n = rows * to;
+  const unsigned grid = (unsigned)std::max<long long>(1, std::min<long long>((n + 1023) / 1024, 148 * 16));
+  const cudaError_t e = launch_with(grid, 256, 0, s)(k_pack_rows, (const bf16*)src, ld, rows, cols, (bf16*)dst, to);
+  src = dst;
+  ld = to;
+  return e;
+}
+
+}  // namespace
+
+size_t tc_workspace(const pbt_adapter_desc* d, bool backward) { return plan(d, backward).total; }
+
+#define STEP(call) do { const cudaError_t e_ = (call); if (e_ != cudaSuccess) return e_; } while (0)
+
+cudaError_t tc_forward(const pbt_adapter_desc* d, const Segments& segs, char* ws, cudaStream_t st) {
+  const Plan p = plan(d, false);
+  const void *x = d->x, *w = d->weight, *A = d->A, *B = d->B;
+  long long ldx = d->ld_x, ldw = d->ld_weight, lda = d->inputs, ldb = d->rank;
+  if (p.pack_x) STEP(pack(x, ldx, d->rows, d->inputs, ws + p.x, st));
+  if (p.pack_w) STEP(pack(w, ldw, d->outputs, d->inputs, ws + p.w, st));
+  if (p.pack_a) STEP(pack(A, lda, (long long)d->n_adapters * d->rank, d->inputs, ws + p.a, st));
+  if (p.pack_b) STEP(pack(B, ldb, (long long)d->n_adapters * d->outputs, d->rank, ws + p.b, st));
+  ShrinkArgs a;
+  memset(&a, 0, sizeof(a));
+  a.x = (const bf16*)x; a.ldx = ldx; a.K = d->inputs;
+  a.mats = (const bf16*)A; a.pitch = (int)lda; a.rank = d->rank; a.rp = p.rp;
+  a.scale = d->scale; a.segs = segs;
+  a.s = d->s; a.planes = (bf16*)(ws + p.planes); a.terms = 1;
+  a.tile_seg = (int*)(ws + p.table); a.tile_rows = kBM; a.n_table = (d->rows + kBM - 1) / kBM;
+  STEP(launch_shrink<false>(a, st));
+  const GemmCall c = {(const bf16*)x, ldx, (const bf16*)w, ldw, 0, a.planes, p.rp, p.rp, (const bf16*)B, (int)ldb, d->rank, d->y, d->ld_y, d->bias, d->outputs, d->inputs};
+  return launch_gemm(c, segs, a.tile_seg, (Counters*)d->status_device, st);
+}
+
+cudaError_t tc_backward(const pbt_adapter_desc* d, const Segments& segs, char* ws, cudaStream_t st) {
+  const Plan p = plan(d, true);
+  const void *x = d->x, *w = d->weight, *A = d->A, *B = d->B, *dy = d->dy;
+  long long ldx = d->ld_x, ldw = d->ld_weight, lda = d->inputs, ldb = d->rank, lddy = d->ld_dy;
+  if (p.pack_x) STEP(pack(x, ldx, d->rows, d->inputs, ws + p.x, st));
+  if (p.pack_w) STEP(pack(w, ldw, d->outputs, d->inputs, ws + p.w, st));
+  if (p.pack_a) STEP(pack(A, lda, (long long)d->n_adapters * d->rank, d->inputs, ws + p.a, st));
+  if (p.pack_b) STEP(pack(B, ldb, (long long)d->n_adapters * d->outputs, d->rank, ws + p.b, st));
+  if (p.pack_dy) STEP(pack(dy, lddy, d->rows, d->outputs, ws + p.dy, st));
+  const int width = 3 * p.rp;
+  ShrinkArgs a;
+  memset(&a, 0, sizeof(a));
+  a.x = (const bf16*)dy; a.ldx = lddy; a.K = d->outputs;
+  a.mats = (const bf16*)B; a.pitch = (int)ldb; a.rank = d->rank; a.rp = p.rp;
+  a.scale = d->scale; a.segs = segs;
+  a.planes = (bf16*)(ws + p.planes); a.terms = 3;
+  a.kept = d->s; a.kept_planes = (bf16*)(ws + p.kept);
+  a.tile_seg = (int*)(ws + p.table); a.tile_rows = kBM; a.n_table = (d->rows + kBM - 1) / kBM;
+  STEP(launch_shrink<true>(a, st));
+  const GemmCall c = {(const bf16*)dy, lddy, (const bf16*)w, ldw, 1, a.planes, width, p.rp, (const bf16*)A, (int)lda, d->rank, d->dx, d->ld_dx, nullptr, d->inputs, d->outputs};
+  STEP(launch_gemm(c, segs, a.tile_seg, (Counters*)d->status_device, st));
+
+  GradArgs g;
+  memset(&g, 0, sizeof(g));
+  g.segs = segs; g.rank = d->rank; g.rp = p.rp; g.term_cols = width; g.boxes = (width + 63) / 64;
+  g.K = d->inputs; g.N = d->outputs; g.blocks_k = (d->inputs + 127) / 128;
+  g.splits = p.splits;
+  g.stride_a = (long long)d->n_adapters * d->rank * d->inputs;
+  g.stride_b = (long long)d->n_adapters * d->rank * d->outputs;
+  g.dA = p.splits > 1 ? (float*)(ws + p.parts) : d->dA;
+  g.dB = p.splits > 1 ? g.dA + p.splits * g.stride_a : d->dB;
+  g.tmem_cols = 32;
+  while (g.tmem_cols < (uint32_t)(2 * width)) g.tmem_cols *= 2;
+  g.counters = (Counters*)d->status_device;
+  CUtensorMap mx, mds, mdy, ms;
+  if (!make_map(&mx, x, d->inputs, d->rows, ldx, 1, 0, 64) || !make_map(&mdy, dy, d->outputs, d->rows, lddy, 1, 0, 64) ||
+      !make_map(&mds, a.planes, width, d->rows, width, 1, 0, 64) || !make_map(&ms, a.kept_planes, width, d->rows, width, 1, 0, 64))
+    return cudaErrorInvalidValue;
+  static DeviceSetup setup;
+  int sms = 0;
+  constexpr int kMost = kGradStages * (16384 + 3 * 8192) + 256 + kGradList * 8 + 1024;
+  static_assert(kMost <= 232448, "shared memory budget of one CTA");
+  STEP(device_setup(&setup, k_adapter_grad, kMost, &sms));
+  const size_t smem = kGradStages * (16384 + g.boxes * 8192) + 256 + kGradList * 8 + 1024;
+  STEP(launch_with(dim3(g.blocks_k + (d->outputs + 127) / 128, d->n_adapters, p.splits), 192, smem, st)(k_adapter_grad, mx, mds, mdy, ms, g));
+  if (p.splits > 1) {
+    const long long n = g.stride_a + g.stride_b;
+    STEP(launch_with((unsigned)std::min<long long>((n + 255) / 256, 148 * 16), 256, 0, st)(k_adapter_grad_join, g.dA, g.dB, g.stride_a, g.stride_b, p.splits, d->dA, d->dB));
+  }
+  return cudaSuccess;
+}
+
+}  // namespace adapters
+}  // namespace pbt

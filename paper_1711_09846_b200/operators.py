@@ -275,6 +275,8 @@ class AdapterProjection:
         d.inputs, d.outputs, d.rank, d.n_adapters, d.dtype = k, n, rank, count, _TYPES[weight.dtype]
         d.weight, d.ld_weight, d.A, d.B, d.scale = weight.data_ptr(), weight.stride(0), A.data_ptr(), B.data_ptr(), scale.data_ptr()
         d.bias = bias.data_ptr() if bias is not None else None
+        self._status = torch.zeros(8, dtype=torch.int32, device=weight.device)
+        d.status_device = self._status.data_ptr()
         d.row_offsets = d.adapter_ids = weight.data_ptr()
         _check(self.lib.pbt_adapter_query_workspace(C.byref(d), 0, C.byref(C.c_size_t(0))))
 
@@ -324,6 +326,13 @@ class AdapterProjection:
             d.dx, d.ld_dx, d.dA, d.dB = dx.data_ptr(), w.shape[1], d_a.data_ptr(), d_b.data_ptr()
             self._run(d, 1, self.lib.pbt_adapter_backward, s)
         return dx, d_a, d_b
+
+    def check(self):
+        """Waits for the enqueued calls and raises if one of the kernels' bounded waits ran out (PBT_ERR_TIMEOUT)."""
+        torch.cuda.synchronize(self.weight.device)
+        code = int(self._status[4].item())
+        if code:
+            raise PbtError(code, "a bounded wait inside an adapter kernel ran out")
 
     def _run(self, d, backward, call, s):
         nbytes = C.c_size_t(0)

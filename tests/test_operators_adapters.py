@@ -91,6 +91,7 @@ def _run(c, stream=None):
     where = (c["row_offsets"], c["adapter_ids"])
     y, kept = layer.forward(c["x"], *where, keep=True, stream=stream)
     dx, d_a, d_b = layer.backward(c["dy"], c["x"], kept, *where, stream=stream)
+    layer.check()
     return layer, dict(y=y, s=kept, dx=dx, dA=d_a, dB=d_b)
 
 
@@ -309,7 +310,7 @@ def test_adapter_arguments_are_checked_before_the_device_is_touched():
     assert lib.pbt_adapter_query_workspace(C.byref(desc()), 0, None) == 1
     for kw, code in ((dict(rows=-1), 1), (dict(inputs=0), 1), (dict(outputs=0), 1), (dict(rank=0), 2), (dict(rank=65), 2), (dict(dtype=2), 2),
                      (dict(n_adapters=0), 1), (dict(n_segments=-1), 1), (dict(weight=None), 1), (dict(A=None), 1), (dict(B=None), 1),
-                     (dict(scale=None), 1), (dict(row_offsets=None), 1), (dict(adapter_ids=None), 1), (dict(ld_weight=31), 1)):
+                     (dict(dtype=1), 1), (dict(scale=None), 1), (dict(row_offsets=None), 1), (dict(adapter_ids=None), 1), (dict(ld_weight=31), 1)):
         assert lib.pbt_adapter_forward(C.byref(desc(**kw)), None, 0, None) == code, kw
         assert lib.pbt_adapter_backward(C.byref(desc(**kw)), None, 0, None) == code, kw
         assert lib.pbt_last_error(None)
