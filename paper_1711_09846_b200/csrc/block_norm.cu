@@ -3,19 +3,24 @@
 // and the gradients of all of it.  b is the block's output, y the residual stream, u the next block's input.
 //
 // Memory-bound: the forward pass reads x, b, z and writes y, u once; the backward pass reads y, b, z, dy, du and writes
-// dx, db, dz once.  A row is held in registers by W warps (16-byte vectors where the layout allows them, single
-// elements otherwise), so nothing is read twice, and every sum is fp32 or wider.
+// dx, db, dz once.  With five streams in and three out the arithmetic (about 25 and 50 instructions an element written
+// out) is as long as the transfers, so it is kept short: pairs of elements in packed fp32 instructions, 16 elements a
+// thread so that a row's reductions are shared by many, and the rows on their way to shared memory (cp.async) while
+// earlier ones are worked on.  Every sum is fp32 or wider.
 //
-// Backward, with yh = y r_y, dh = du w_next and p = c sigmoid(z) w_post v:
-//   t1 = mean(dh yh),  dx = dy + r_y (dh - yh t1),  db = r_b (c g w_post dx - v t2),  t2 = mean(p dx)
-// t2 is taken apart as mean(p (dy + r_y dh)) - t1 mean(p r_y yh), so that the row needs ONE reduction of three sums and
-// not two that wait for one another.  Column sums (dw_post, dw_next, a per-member gate) stay in the registers of the
-// threads that own the columns while a block walks rows of one member; each row group leaves one partial, and a second
-// kernel adds the partials in a fixed order (no atomics: reproducible bit for bit).
+// Backward, with yh = y r_y, dh = du w_next and p = sigmoid(z) w_post v:
+//   t1 = mean(dh yh),  dx = dy + r_y (dh - yh t1),  db = r_b (c g w_post dx - c v t2),  t2 = mean(p dx)
+// t2 is taken apart as mean(p (dy + r_y dh)) - r_y t1 mean(p yh), so that the row needs ONE reduction of three sums and
+// not two that wait for one another.
+//
+// Work is dealt in consecutive rows, whatever the members: every row group (the warps of a row) gets the same number of
+// rows, to within one.  Column sums (dw_post, dw_next, a per-member gate) stay in the registers of the threads that own
+// the columns and are left as one partial result per (row group, member); a second kernel adds a member's partial results
+// in a fixed order (no atomics: reproducible bit for bit).
 #include <algorithm>
 #include <type_traits>
 
-#include "pbt_common.cuh"
+#include "tc_common.cuh"
 
 namespace pbt {
 void set_last_error(const char* msg);
@@ -40,32 +45,73 @@ struct NormArgs {
   float *rstd_block, *rstd_next;     // written by the forward pass, read by the backward pass
   char *dx, *dblock, *dgate;
   float *dpost, *dnext, *dscale;
-  float *partial, *partial_scale;    // [members][slices][sums][width], [members][blocks per member]
-  int warps_per_row, blocks_per_member, slices, sums;
+  float *partial, *partial_scale;    // [row groups + members][sums][width], [row groups + members][warps of a row]
+  int warps_per_row, groups, sums;   // groups: row groups of the grid
 };
 
+// first row (of all members' rows, one after the other) of row group g
+__device__ __forceinline__ long long norm_first_row(const NormArgs& a, int g) { return (long long)a.members * a.rows * g / a.groups; }
+// the row group that has row r: the last one whose first row is not behind r
+__device__ __forceinline__ int norm_group_of(const NormArgs& a, long long r) {
+  return (int)(((r + 1) * a.groups - 1) / ((long long)a.members * a.rows));
+}
+
+// Arithmetic of a thread: pairs of fp32 in the packed instructions for rows that are read in vectors, single fp32 or fp64
+// values otherwise.
+struct F2 { unsigned long long v; };
+__device__ __forceinline__ F2 pair(float a, float b) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 split(F2 a) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+  return r;
+}
+__device__ __forceinline__ F2 mul(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 add(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
+__device__ __forceinline__ float mul(float a, float b) { return __fmul_rn(a, b); }
+__device__ __forceinline__ float add(float a, float b) { return __fadd_rn(a, b); }
+__device__ __forceinline__ float fma(float a, float b, float c) { return __fmaf_rn(a, b, c); }
+__device__ __forceinline__ double mul(double a, double b) { return a * b; }
+__device__ __forceinline__ double add(double a, double b) { return a + b; }
+__device__ __forceinline__ double fma(double a, double b, double c) { return ::fma(a, b, c); }
+template <typename L, typename S> __device__ __forceinline__ L all(S x) {
+  if constexpr (std::is_same<L, F2>::value) return pair((float)x, (float)x);
+  else return (L)x;
+}
+__device__ __forceinline__ float total(F2 a) { const float2 f = split(a); return f.x + f.y; }
+__device__ __forceinline__ float total(float a) { return a; }
+__device__ __forceinline__ double total(double a) { return a; }
+
+// sigmoid(z) = 1 / (1 + 2^(-z log2 e)) by the special-function unit: relative error below (|z| + 3) 2^-22
+__device__ __forceinline__ float opened(float z) {
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.44269504f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+  return r;
+}
+__device__ __forceinline__ F2 opened(F2 z) { const float2 f = split(z); return pair(opened(f.x), opened(f.y)); }
+__device__ __forceinline__ double opened(double z) { return opened((float)z); }
+
+// V elements of type T as they lie in memory, and as N = V / (lanes of L) values of L.
 template <typename T, int V> struct Vec;
 template <> struct Vec<bf16, 8> {
   typedef uint4 Raw;
-  static __device__ __forceinline__ Raw load(const bf16* p) {
-    Raw r;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
-    return r;
-  }
   static __device__ __forceinline__ Raw zero() { return make_uint4(0u, 0u, 0u, 0u); }
-  static __device__ __forceinline__ void unpack(const Raw& r, float* f) {
+  static __device__ __forceinline__ void unpack(const Raw& r, F2* f) {
     const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[2 * i] = __uint_as_float(w[i] << 16);
-      f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
+    for (int i = 0; i < 4; ++i) f[i] = pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
   }
-  static __device__ __forceinline__ void store(bf16* p, const float* f) {
+  static __device__ __forceinline__ void store(bf16* p, const F2* f) {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      __nv_bfloat162 t = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+      const float2 v = split(f[i]);
+      __nv_bfloat162 t = __floats2bfloat162_rn(v.x, v.y);
       w[i] = *reinterpret_cast<uint32_t*>(&t);
     }
     *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -73,44 +119,45 @@ template <> struct Vec<bf16, 8> {
 };
 template <> struct Vec<float, 4> {
   typedef float4 Raw;
-  static __device__ __forceinline__ Raw load(const float* p) { return ld_stream(p); }
   static __device__ __forceinline__ Raw zero() { return make_float4(0.f, 0.f, 0.f, 0.f); }
-  static __device__ __forceinline__ void unpack(const Raw& r, float* f) { f[0] = r.x; f[1] = r.y; f[2] = r.z; f[3] = r.w; }
-  static __device__ __forceinline__ void store(float* p, const float* f) { st_stream(p, make_float4(f[0], f[1], f[2], f[3])); }
+  static __device__ __forceinline__ void unpack(const Raw& r, F2* f) { f[0] = pair(r.x, r.y); f[1] = pair(r.z, r.w); }
+  static __device__ __forceinline__ void store(float* p, const F2* f) {
+    const float2 a = split(f[0]), b = split(f[1]);
+    st_stream(p, make_float4(a.x, a.y, b.x, b.y));
+  }
 };
 template <> struct Vec<float, 1> {
   typedef float Raw;
   static __device__ __forceinline__ Raw load(const float* p) { return *p; }
   static __device__ __forceinline__ Raw zero() { return 0.f; }
-  static __device__ __forceinline__ void unpack(const Raw& r, float* f) { f[0] = r; }
-  static __device__ __forceinline__ void store(float* p, const float* f) { *p = f[0]; }
+  template <typename L> static __device__ __forceinline__ void unpack(const Raw& r, L* f) { f[0] = r; }
+  template <typename L> static __device__ __forceinline__ void store(float* p, const L* f) { *p = (float)f[0]; }
 };
 template <> struct Vec<bf16, 1> {
   typedef float Raw;
   static __device__ __forceinline__ Raw load(const bf16* p) { return __bfloat162float(*p); }
   static __device__ __forceinline__ Raw zero() { return 0.f; }
-  static __device__ __forceinline__ void unpack(const Raw& r, float* f) { f[0] = r; }
-  static __device__ __forceinline__ void store(bf16* p, const float* f) { *p = __float2bfloat16_rn(f[0]); }
+  template <typename L> static __device__ __forceinline__ void unpack(const Raw& r, L* f) { f[0] = r; }
+  template <typename L> static __device__ __forceinline__ void store(bf16* p, const L* f) { *p = __float2bfloat16_rn((float)f[0]); }
 };
 
 // V weights (fp32; 16-byte loads where V allows, the launcher has checked the alignment)
-template <int V>
-__device__ __forceinline__ void load_weights(const float* p, float* f) {
+template <int V, typename L>
+__device__ __forceinline__ void load_weights(const float* p, L* f) {
   if constexpr (V == 1) {
     f[0] = __ldg(p);
   } else {
 #pragma unroll
     for (int j = 0; j < V; j += 4) {
       const float4 w = __ldg(reinterpret_cast<const float4*>(p + j));
-      f[j] = w.x; f[j + 1] = w.y; f[j + 2] = w.z; f[j + 3] = w.w;
+      f[j / 2] = pair(w.x, w.y);
+      f[j / 2 + 1] = pair(w.z, w.w);
     }
   }
 }
 
-__device__ __forceinline__ float opened(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
-
-// Sum of N values over the W warps of a row group.  scratch: [2][N][32] floats, used alternately (`turn`), so that one
-// barrier per reduction is enough: a buffer is written again only after everybody has passed the next barrier.
+// Sum of N values over the W warps of a row group.  scratch: [2][32][N], used alternately (`turn`), so that one barrier
+// per reduction is enough: a buffer is written again only after everybody has passed the next barrier.
 template <int N, typename A>
 __device__ __forceinline__ void row_sum(A* v, int W, int group, A* scratch, int& turn) {
 #pragma unroll
@@ -119,280 +166,397 @@ __device__ __forceinline__ void row_sum(A* v, int W, int group, A* scratch, int&
     for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
   if (W == 1) return;
   const int warp = threadIdx.x >> 5;
-  A* buf = scratch + turn * N * 32;
+  A* buf = scratch + turn * 32 * N;
   turn ^= 1;
   if ((threadIdx.x & 31) == 0)
 #pragma unroll
-    for (int k = 0; k < N; ++k) buf[k * 32 + warp] = v[k];
+    for (int k = 0; k < N; ++k) buf[warp * N + k] = v[k];
+  __syncwarp();
   asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(W * 32) : "memory");
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    A s = 0;
-    for (int w = 0; w < W; ++w) s += buf[k * 32 + group * W + w];
-    v[k] = s;
+  for (int k = 0; k < N; ++k) v[k] = 0;
+  for (int w = 0; w < W; ++w)
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] += buf[(group * W + w) * N + k];
+}
+
+// Rows on their way from global memory: a thread copies its own 16-byte vectors into its own slots of shared memory,
+// several rows ahead of the one it works on, and reads nobody else's (so the ring needs no barrier).  Rows that cannot be
+// read in vectors are loaded when they are worked on.
+__device__ __forceinline__ void copy_ahead(void* slot, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(slot)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+template <typename T, int V, int ITEMS, int ARRAYS, int STAGES>
+struct RowRing {
+  typedef typename Vec<T, V>::Raw Raw;
+  uint4* slots;      // this thread's; its vectors are blockDim.x apart
+  const T* base[ARRAYS];
+  long long member[ARRAYS], row[ARRAYS];
+  bool have[ARRAYS];
+  int slot, step, nv, rows;
+  int m, i, left;    // the next row to ask for, and how many there are to ask for
+
+  __device__ __forceinline__ void set(int k, const NormTensor& t, bool used) {
+    base[k] = reinterpret_cast<const T*>(t.p);
+    member[k] = t.member;
+    row[k] = t.row;
+    have[k] = used;
   }
+  __device__ __forceinline__ uint4* at(int s, int k, int j) const { return slots + ((s * ARRAYS + k) * ITEMS + j) * (int)blockDim.x; }
+  // ask for the next row (for nothing behind the last one) into stage s
+  __device__ __forceinline__ void ask(int s) {
+    if constexpr (V > 1) {
+      if (left > 0) {
+#pragma unroll
+        for (int k = 0; k < ARRAYS; ++k)
+          if (have[k]) {
+            const T* p = base[k] + m * member[k] + i * row[k];
+#pragma unroll
+            for (int j = 0; j < ITEMS; ++j) {
+              const int e = slot + j * step;
+              if (e < nv) copy_ahead(at(s, k, j), p + e * V);
+            }
+          }
+        --left;
+        if (++i == rows) { i = 0; ++m; }
+      }
+      copy_commit();
+    }
+  }
+  // the oldest row asked for has arrived
+  __device__ __forceinline__ void wait() const {
+    if constexpr (V > 1) copy_wait<STAGES - 1>();
+  }
+  // vector j of array k of row (m, i), which stage s holds; zeros where there is none
+  template <typename L>
+  __device__ __forceinline__ void get(int m, int i, int s, int k, int j, L* f) const {
+    const int e = slot + j * step;
+    Raw r = Vec<T, V>::zero();
+    if (have[k] && e < nv) {
+      if constexpr (V > 1) r = *reinterpret_cast<const Raw*>(at(s, k, j));
+      else r = Vec<T, V>::load(base[k] + m * member[k] + i * row[k] + e);
+    }
+    Vec<T, V>::unpack(r, f);
+  }
+};
+
+// Stages of a ring: what fits 80 KB (two blocks per SM) for blocks of 256 threads and 160 KB for larger ones, at most three
+// (a row that is worked on and two on their way).
+template <int V, int ITEMS, int ARRAYS, int THREADS>
+__host__ __device__ constexpr int norm_stages() {
+  const int fit = (THREADS <= kNormThreads ? 80 : 160) * 1024 / (ARRAYS * ITEMS * 16 * THREADS);
+  return V == 1 || fit < 1 ? 1 : fit > 3 ? 3 : fit;
 }
 
 template <typename T, int V, int ITEMS, int THREADS>
 __global__ void __launch_bounds__(THREADS) k_norm_forward(const NormArgs a) {
   pdl_prologue();
+  extern __shared__ uint4 norm_ring[];
   __shared__ float scratch[2 * 32];
   typedef Vec<T, V> X;
+  typedef typename std::conditional<V == 1, float, F2>::type L;
+  constexpr int N = V == 1 ? 1 : V / 2, kStages = norm_stages<V, ITEMS, 3, THREADS>();
   const int W = a.warps_per_row, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int group = warp / W, slot = (warp % W) * 32 + lane, step = W * 32;
-  const long long r = (long long)blockIdx.x * (blockDim.x / (W * 32)) + group;
-  if (r >= (long long)a.members * a.rows) return;
-  const int m = (int)(r / a.rows), i = (int)(r % a.rows);
-  const int nv = a.width / V;
-  int turn = 0;
-
-  typename X::Raw xr[ITEMS], br[ITEMS], zr[ITEMS];
-  const T* xp = reinterpret_cast<const T*>(a.x.p) + m * a.x.member + i * a.x.row;
-  const T* bp = reinterpret_cast<const T*>(a.block.p) + m * a.block.member + i * a.block.row;
-  const T* zp = reinterpret_cast<const T*>(a.gate.p) + m * a.gate.member + i * a.gate.row;
+  const int group = warp / W, g = blockIdx.x * (blockDim.x / (W * 32)) + group;
+  if (g >= a.groups) return;
+  const bool block = a.block.p != nullptr, gate = a.gate.p != nullptr, next = a.u != nullptr;
+  long long r = norm_first_row(a, g);
+  const long long r_end = norm_first_row(a, g + 1);
+  int m = (int)(r / a.rows), i = (int)(r % a.rows);
+  RowRing<T, V, ITEMS, 3, kStages> ring;
+  ring.slots = norm_ring + threadIdx.x;
+  ring.slot = (warp % W) * 32 + lane; ring.step = W * 32; ring.nv = a.width / V; ring.rows = a.rows;
+  ring.m = m; ring.i = i; ring.left = (int)(r_end - r);
+  ring.set(0, a.x, true); ring.set(1, a.block, block); ring.set(2, a.gate, gate);
 #pragma unroll
-  for (int k = 0; k < ITEMS; ++k) {
-    const int c = slot + k * step;
-    xr[k] = c < nv ? X::load(xp + c * V) : X::zero();
-    if (a.block.p) br[k] = c < nv ? X::load(bp + c * V) : X::zero();
-    if (a.gate.p) zr[k] = c < nv ? X::load(zp + c * V) : X::zero();
-  }
-  float y[ITEMS][V];
-#pragma unroll
-  for (int k = 0; k < ITEMS; ++k) X::unpack(xr[k], y[k]);
-  const long long at = r * a.width;
-  if (a.block.p) {
-    float s[1] = {0.f};
-#pragma unroll
-    for (int k = 0; k < ITEMS; ++k) {
-      float b[V];
-      X::unpack(br[k], b);
-#pragma unroll
-      for (int j = 0; j < V; ++j) s[0] = __fmaf_rn(b[j], b[j], s[0]);
-    }
-    row_sum<1>(s, W, group, scratch, turn);
-    const float rb = rsqrtf(s[0] * a.inv_width + a.eps);
-    const float crb = rb * (a.scale ? a.scale[m] : 1.f);
-    if (a.rstd_block && slot == 0) a.rstd_block[r] = rb;
+  for (int s = 0; s < kStages; ++s) ring.ask(s);
+  int turn = 0, stage = 0;
+  for (; r < r_end; ++r) {
+    const long long at = r * a.width;
     const float* wp = a.post_weight + (long long)m * a.width;
-#pragma unroll
-    for (int k = 0; k < ITEMS; ++k) {
-      const int c = slot + k * step;
-      if (c >= nv) continue;
-      float b[V], z[V], w[V];
-      X::unpack(br[k], b);
-      load_weights<V>(wp + c * V, w);
-      if (a.gate.p) X::unpack(zr[k], z);
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        float t = b[j] * crb * w[j];
-        if (a.gate.p) t *= opened(z[j]);
-        y[k][j] += t;
-      }
-      X::store(reinterpret_cast<T*>(a.y) + at + c * V, y[k]);
-    }
-  }
-  if (a.u) {
-    float s[1] = {0.f};
-#pragma unroll
-    for (int k = 0; k < ITEMS; ++k)
-#pragma unroll
-      for (int j = 0; j < V; ++j) s[0] = __fmaf_rn(y[k][j], y[k][j], s[0]);
-    row_sum<1>(s, W, group, scratch, turn);
-    const float ry = rsqrtf(s[0] * a.inv_width + a.eps);
-    if (a.rstd_next && slot == 0) a.rstd_next[r] = ry;
     const float* wn = a.next_weight + (long long)m * a.width;
+    ring.wait();
+    L y[ITEMS][N];
 #pragma unroll
-    for (int k = 0; k < ITEMS; ++k) {
-      const int c = slot + k * step;
-      if (c >= nv) continue;
-      float w[V], u[V];
-      load_weights<V>(wn + c * V, w);
+    for (int k = 0; k < ITEMS; ++k) ring.get(m, i, stage, 0, k, y[k]);
+    if (block) {
+      L s = all<L>(0.f);
 #pragma unroll
-      for (int j = 0; j < V; ++j) u[j] = y[k][j] * ry * w[j];
-      X::store(reinterpret_cast<T*>(a.u) + at + c * V, u);
+      for (int k = 0; k < ITEMS; ++k) {
+        L b[N];
+        ring.get(m, i, stage, 1, k, b);
+#pragma unroll
+        for (int j = 0; j < N; ++j) s = fma(b[j], b[j], s);
+      }
+      float sum[1] = {total(s)};
+      row_sum<1>(sum, W, group, scratch, turn);
+      const float rb = rsqrtf(sum[0] * a.inv_width + a.eps);
+      const L crb = all<L>(a.scale ? a.scale[m] * rb : rb);
+      if (a.rstd_block && ring.slot == 0) a.rstd_block[r] = rb;
+#pragma unroll
+      for (int k = 0; k < ITEMS; ++k) {
+        const int e = ring.slot + k * ring.step;
+        if (e >= ring.nv) continue;
+        L b[N], w[N];
+        ring.get(m, i, stage, 1, k, b);
+        load_weights<V>(wp + e * V, w);
+#pragma unroll
+        for (int j = 0; j < N; ++j) b[j] = mul(mul(b[j], crb), w[j]);
+        if (gate) {
+          L z[N];
+          ring.get(m, i, stage, 2, k, z);
+#pragma unroll
+          for (int j = 0; j < N; ++j) y[k][j] = fma(b[j], opened(z[j]), y[k][j]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < N; ++j) y[k][j] = add(b[j], y[k][j]);
+        }
+        X::store(reinterpret_cast<T*>(a.y) + at + e * V, y[k]);
+      }
     }
+    ring.ask(stage);
+    if (++stage == kStages) stage = 0;
+    if (next) {
+      L s = all<L>(0.f);
+#pragma unroll
+      for (int k = 0; k < ITEMS; ++k)
+#pragma unroll
+        for (int j = 0; j < N; ++j) s = fma(y[k][j], y[k][j], s);
+      float sum[1] = {total(s)};
+      row_sum<1>(sum, W, group, scratch, turn);
+      const float ry = rsqrtf(sum[0] * a.inv_width + a.eps);
+      if (a.rstd_next && ring.slot == 0) a.rstd_next[r] = ry;
+#pragma unroll
+      for (int k = 0; k < ITEMS; ++k) {
+        const int e = ring.slot + k * ring.step;
+        if (e >= ring.nv) continue;
+        L w[N];
+        load_weights<V>(wn + e * V, w);
+#pragma unroll
+        for (int j = 0; j < N; ++j) w[j] = mul(mul(y[k][j], all<L>(ry)), w[j]);
+        X::store(reinterpret_cast<T*>(a.u) + at + e * V, w);
+      }
+    }
+    if (++i == a.rows) { i = 0; ++m; }
   }
 }
 
-// Sums of a row group, in the order in which a partial holds them: next, post, gate (the ones that exist).
-// Rows of at most 256 single elements are worked out in fp64 (inputs, results and column sums keep their types): dx and
+// Sums of a row group, in the order in which a partial result holds them: next, post, gate (the ones that exist).
+// A row is read from the ring twice, before and after its reduction, so that a thread's registers hold little besides its
+// column sums.
+// Rows of at most 32 single elements are worked out in fp64 (inputs, results and column sums keep their types): dx and
 // db are what is left of dh and dn after the projection on the row is taken away, and in rows of one or two columns
 // that is next to nothing, 1 - yh^2 of it, which fp32 loses altogether.
 template <typename T, int V, int ITEMS, int THREADS>
-__global__ void __launch_bounds__(THREADS) k_norm_backward(const NormArgs a) {
+__global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_norm_backward(const NormArgs a) {
   pdl_prologue();
+  extern __shared__ uint4 norm_ring[];
   typedef typename std::conditional<V == 1 && ITEMS == 1, double, float>::type A;
+  typedef typename std::conditional<V == 1, A, F2>::type L;           // a thread's values
+  typedef typename std::conditional<V == 1, float, F2>::type S;       // its column sums
   __shared__ A scratch[2 * 3 * 32];
-  __shared__ float scale_sum[32];
   typedef Vec<T, V> X;
+  constexpr int N = V == 1 ? 1 : V / 2, kStages = norm_stages<V, ITEMS, 5, THREADS>();
   const int W = a.warps_per_row, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int groups = blockDim.x / (W * 32), group = warp / W, slot = (warp % W) * 32 + lane, step = W * 32;
-  const int m = blockIdx.x / a.blocks_per_member, s = blockIdx.x % a.blocks_per_member;
-  const int nv = a.width / V;
-  const bool next = a.du.p != nullptr, block = a.block.p != nullptr, gate = a.gate.p != nullptr;
-  const float c = a.scale ? a.scale[m] : 1.f;
-  const float* wn = a.next_weight + (long long)m * a.width;
-  const float* wp = a.post_weight + (long long)m * a.width;
-  float acc_next[ITEMS][V], acc_post[ITEMS][V], acc_gate[ITEMS][V], acc_scale = 0.f;
+  const int group = warp / W, g = blockIdx.x * (blockDim.x / (W * 32)) + group;
+  if (g >= a.groups) return;
+  const bool next = a.du.p != nullptr, block = a.block.p != nullptr, gate = a.gate.p != nullptr, vector = gate && a.gate_vector;
+  long long r = norm_first_row(a, g);
+  const long long r_end = norm_first_row(a, g + 1);
+  int m = (int)(r / a.rows), i = (int)(r % a.rows);
+  enum { kDy, kDu, kY, kBlock, kGate };
+  RowRing<T, V, ITEMS, 5, kStages> ring;
+  ring.slots = norm_ring + threadIdx.x;
+  ring.slot = (warp % W) * 32 + lane; ring.step = W * 32; ring.nv = a.width / V; ring.rows = a.rows;
+  ring.m = m; ring.i = i; ring.left = (int)(r_end - r);
+  ring.set(kDy, a.dy, a.dy.p != nullptr); ring.set(kDu, a.du, next); ring.set(kY, a.x, next);
+  ring.set(kBlock, a.block, block); ring.set(kGate, a.gate, gate);
+#pragma unroll
+  for (int s = 0; s < kStages; ++s) ring.ask(s);
+  S acc_next[ITEMS][N], acc_post[ITEMS][N], acc_gate[ITEMS][N];
+  float acc_scale = 0.f;
 #pragma unroll
   for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
-    for (int j = 0; j < V; ++j) acc_next[k][j] = acc_post[k][j] = acc_gate[k][j] = 0.f;
-  int turn = 0;
-  for (int i = s * groups + group; i < a.rows; i += a.blocks_per_member * groups) {
-    const long long r = (long long)m * a.rows + i, at = r * a.width;
-    typename X::Raw yr[ITEMS], br[ITEMS], zr[ITEMS], dyr[ITEMS], dur[ITEMS];
-#pragma unroll
-    for (int k = 0; k < ITEMS; ++k) {
-      const int e = slot + k * step;
-      const bool in = e < nv;
-      dyr[k] = in && a.dy.p ? X::load(reinterpret_cast<const T*>(a.dy.p) + m * a.dy.member + i * a.dy.row + e * V) : X::zero();
-      if (next) {
-        yr[k] = in ? X::load(reinterpret_cast<const T*>(a.x.p) + m * a.x.member + i * a.x.row + e * V) : X::zero();
-        dur[k] = in ? X::load(reinterpret_cast<const T*>(a.du.p) + m * a.du.member + i * a.du.row + e * V) : X::zero();
-      }
-      if (block) br[k] = in ? X::load(reinterpret_cast<const T*>(a.block.p) + m * a.block.member + i * a.block.row + e * V) : X::zero();
-      if (gate) zr[k] = in ? X::load(reinterpret_cast<const T*>(a.gate.p) + m * a.gate.member + i * a.gate.row + e * V) : X::zero();
-    }
+    for (int j = 0; j < N; ++j) acc_next[k][j] = acc_post[k][j] = acc_gate[k][j] = all<S>(0.f);
+  int turn = 0, stage = 0;
+  for (; r < r_end; ++r) {
+    const long long at = r * a.width;
+    const float* wn = a.next_weight + (long long)m * a.width;
+    const float* wp = a.post_weight + (long long)m * a.width;
+    const A c = a.scale ? a.scale[m] : 1.f;
     const A ry = next ? a.rstd_next[r] : 0.f, rb = block ? a.rstd_block[r] : 0.f;
-    A sums[3] = {0, 0, 0};   // dh yh, p (dy + r_y dh), p r_y yh
+    const L lry = all<L>(ry), lrb = all<L>(rb);
+    ring.wait();
+    L part[3] = {all<L>(0.f), all<L>(0.f), all<L>(0.f)};   // r_y dh yh, p (dy + r_y dh), p yh, with p = g w_post v
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
-      const int e = slot + k * step;
-      if (e >= nv) continue;
-      float dy[V], du[V], y[V], b[V], z[V], w[V], q[V];
-      X::unpack(dyr[k], dy);
+      const int e = ring.slot + k * ring.step;
+      if (e >= ring.nv) continue;
+      L t[N], yh[N];      // dy + r_y dh
+      ring.get(m, i, stage, kDy, k, t);
       if (next) {
-        X::unpack(dur[k], du);
-        X::unpack(yr[k], y);
+        L du[N], w[N];
+        ring.get(m, i, stage, kDu, k, du);
+        ring.get(m, i, stage, kY, k, yh);
         load_weights<V>(wn + e * V, w);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          du[j] = mul(mul(du[j], lry), w[j]);
+          yh[j] = mul(yh[j], lry);
+          part[0] = fma(du[j], yh[j], part[0]);
+          t[j] = add(t[j], du[j]);
+        }
       }
       if (block) {
-        X::unpack(br[k], b);
-        load_weights<V>(wp + e * V, q);
-        if (gate) X::unpack(zr[k], z);
-      }
+        L b[N], w[N];
+        ring.get(m, i, stage, kBlock, k, b);
+        load_weights<V>(wp + e * V, w);
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        A dh = 0, yh = 0;
-        if (next) {
-          dh = (A)du[j] * w[j];
-          yh = y[j] * ry;
-          sums[0] += dh * yh;
+        for (int j = 0; j < N; ++j) b[j] = mul(mul(b[j], lrb), w[j]);
+        if (gate) {
+          L z[N];
+          ring.get(m, i, stage, kGate, k, z);
+#pragma unroll
+          for (int j = 0; j < N; ++j) b[j] = mul(b[j], opened(z[j]));
         }
-        if (block) {
-          A p = (A)c * q[j] * (b[j] * rb);
-          if (gate) p *= opened(z[j]);
-          sums[1] += p * (ry * dh + dy[j]);
-          sums[2] += p * (ry * yh);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          part[1] = fma(b[j], t[j], part[1]);
+          if (next) part[2] = fma(b[j], yh[j], part[2]);
         }
       }
     }
+    A sums[3] = {total(part[0]), total(part[1]), total(part[2])};
     row_sum<3>(sums, W, group, scratch, turn);
-    const A t1 = sums[0] / a.width, t2 = (sums[1] - t1 * sums[2]) / a.width;
+    const A t1 = sums[0] / a.width;                                             // r_y t1
+    const L lt1 = all<L>(-t1), lt2 = all<L>(-c * (sums[1] - t1 * sums[2]) / a.width), lc = all<L>(c);   // -r_y t1, -c t2
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
-      const int e = slot + k * step;
-      if (e >= nv) continue;
-      float dy[V];
-      A dx[V];
-      X::unpack(dyr[k], dy);
-#pragma unroll
-      for (int j = 0; j < V; ++j) dx[j] = dy[j];
+      const int e = ring.slot + k * ring.step;
+      if (e >= ring.nv) continue;
+      L dx[N];
+      ring.get(m, i, stage, kDy, k, dx);
       if (next) {
-        float du[V], y[V], w[V];
-        X::unpack(dur[k], du);
-        X::unpack(yr[k], y);
+        L du[N], y[N], w[N];
+        ring.get(m, i, stage, kDu, k, du);
+        ring.get(m, i, stage, kY, k, y);
         load_weights<V>(wn + e * V, w);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const A yh = y[j] * ry;
-          acc_next[k][j] += (float)(du[j] * yh);
-          dx[j] += ry * ((A)du[j] * w[j] - yh * t1);
+        for (int j = 0; j < N; ++j) {
+          const L yh = mul(y[j], lry);
+          if constexpr (std::is_same<L, S>::value) acc_next[k][j] = fma(du[j], yh, acc_next[k][j]);
+          else acc_next[k][j] += (float)(du[j] * yh);
+          dx[j] = fma(yh, lt1, fma(mul(du[j], lry), w[j], dx[j]));
         }
       }
-#pragma unroll
-      for (int j = 0; j < V; ++j) dy[j] = (float)dx[j];
-      X::store(reinterpret_cast<T*>(a.dx) + at + e * V, dy);
+      X::store(reinterpret_cast<T*>(a.dx) + at + e * V, dx);
       if (block) {
-        float b[V], z[V], q[V], db[V], dz[V];
-        X::unpack(br[k], b);
-        load_weights<V>(wp + e * V, q);
-        if (gate) X::unpack(zr[k], z);
+        L b[N], z[N], w[N];
+        ring.get(m, i, stage, kBlock, k, b);
+        load_weights<V>(wp + e * V, w);
+        if (gate) ring.get(m, i, stage, kGate, k, z);
+        L o_sum = all<L>(0.f);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const A g = gate ? opened(z[j]) : 1.f, v = b[j] * rb, gdx = g * dx[j];
-          const A dn = c * gdx, o = gdx * v * q[j];
-          acc_post[k][j] += (float)(dn * v);
-          acc_scale += (float)o;
-          db[j] = (float)(rb * (dn * q[j] - v * t2));
-          dz[j] = (float)(c * o * (1 - g));
+        for (int j = 0; j < N; ++j) {
+          const L open = gate ? opened(z[j]) : all<L>(1.f);
+          const L v = mul(b[j], lrb), gdx = mul(open, dx[j]), dn = mul(lc, gdx), vw = mul(v, w[j]);
+          const L o = mul(gdx, vw);
+          if constexpr (std::is_same<L, S>::value) acc_post[k][j] = fma(dn, v, acc_post[k][j]);
+          else acc_post[k][j] += (float)(dn * v);
+          o_sum = add(o_sum, o);
+          b[j] = mul(lrb, fma(v, lt2, mul(dn, w[j])));
+          z[j] = mul(mul(lc, o), fma(all<L>(-1.f), open, all<L>(1.f)));
         }
-        X::store(reinterpret_cast<T*>(a.dblock) + at + e * V, db);
-        if (gate && a.gate_vector) {
+        acc_scale += (float)total(o_sum);
+        X::store(reinterpret_cast<T*>(a.dblock) + at + e * V, b);
+        if (vector) {
 #pragma unroll
-          for (int j = 0; j < V; ++j) acc_gate[k][j] += dz[j];
+          for (int j = 0; j < N; ++j) {
+            if constexpr (std::is_same<L, S>::value) acc_gate[k][j] = add(acc_gate[k][j], z[j]);
+            else acc_gate[k][j] += (float)z[j];
+          }
         } else if (gate) {
-          X::store(reinterpret_cast<T*>(a.dgate) + at + e * V, dz);
+          X::store(reinterpret_cast<T*>(a.dgate) + at + e * V, z);
         }
       }
     }
-  }
-  float* out = a.partial + ((long long)m * a.slices + s * groups + group) * a.sums * a.width;
+    ring.ask(stage);
+    if (++stage == kStages) stage = 0;
+    if (++i < a.rows && r + 1 < r_end) continue;
+    // the last row here of this member: leave its sums.  The pairs (row group, member) ascend in g + m.
+    float* out = a.partial + (long long)(g + m) * a.sums * a.width;
 #pragma unroll
-  for (int k = 0; k < ITEMS; ++k) {
-    const int e = slot + k * step;
-    if (e >= nv) continue;
-    float* o = out;
-    if (next) { 
+    for (int k = 0; k < ITEMS; ++k) {
+      const int e = ring.slot + k * ring.step;
+      if (e >= ring.nv) continue;
+      float* o = out + e * V;
+      auto leave = [&](S* acc) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) o[e * V + j] = acc_next[k][j];
-      o += a.width;
+        for (int j = 0; j < N; ++j) {
+          if constexpr (V == 1) { o[j] = acc[j]; }
+          else { const float2 f = split(acc[j]); o[2 * j] = f.x; o[2 * j + 1] = f.y; }
+          acc[j] = all<S>(0.f);
+        }
+        o += a.width;
+      };
+      if (next) leave(acc_next[k]);
+      if (block) leave(acc_post[k]);
+      if (vector) leave(acc_gate[k]);
     }
     if (block) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) o[e * V + j] = acc_post[k][j];
-      o += a.width;
+      for (int o = 16; o > 0; o >>= 1) acc_scale += __shfl_xor_sync(0xFFFFFFFFu, acc_scale, o);
+      if (lane == 0) a.partial_scale[(long long)(g + m) * W + warp % W] = acc_scale;
+      acc_scale = 0.f;
     }
-    if (gate && a.gate_vector) {
-#pragma unroll
-      for (int j = 0; j < V; ++j) o[e * V + j] = acc_gate[k][j];
-    }
-  }
-  if (block) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) acc_scale += __shfl_xor_sync(0xFFFFFFFFu, acc_scale, o);
-    if (lane == 0) scale_sum[warp] = acc_scale;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      float t = 0.f;
-      for (int w = 0; w < (int)(blockDim.x >> 5); ++w) t += scale_sum[w];
-      a.partial_scale[blockIdx.x] = t;
-    }
+    i = 0;
+    ++m;
   }
 }
 
+// A member's column sums from the partial results of its row groups: a block takes 32 columns, its eight warps every
+// eighth row group, and adds the warps' sums in order.
 template <typename T>
 __global__ void __launch_bounds__(256) k_norm_columns(const NormArgs a) {
   pdl_prologue();
-  const int m = blockIdx.y, e = blockIdx.x * 256 + threadIdx.x;
+  __shared__ float part[8][33];
+  const int m = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, e = blockIdx.x * 32 + lane;
   const bool next = a.du.p != nullptr, block = a.block.p != nullptr;
-  if (e < a.width) {
-    const float* p = a.partial + (long long)m * a.slices * a.sums * a.width + e;
-    for (int q = 0; q < a.sums; ++q) {
-      float t = 0.f;
-      for (int s = 0; s < a.slices; ++s) t += p[((long long)s * a.sums + q) * a.width];
+  const int g0 = norm_group_of(a, (long long)m * a.rows), g1 = norm_group_of(a, (long long)(m + 1) * a.rows - 1);
+  for (int q = 0; q < a.sums; ++q) {
+    float t = 0.f;
+    if (e < a.width)
+      for (int g = g0 + warp; g <= g1; g += 8) t += a.partial[((long long)(g + m) * a.sums + q) * a.width + e];
+    part[warp][lane] = t;
+    __syncthreads();
+    if (warp == 0 && e < a.width) {
+      t = part[0][lane];
+#pragma unroll
+      for (int w = 1; w < 8; ++w) t += part[w][lane];
       const long long at = (long long)m * a.width + e;
       if (next && q == 0) a.dnext[at] = t;
       else if (q == (next ? 1 : 0)) a.dpost[at] = t;
       else Vec<T, 1>::store(reinterpret_cast<T*>(a.dgate) + at, &t);
     }
+    __syncthreads();
   }
-  if (block && blockIdx.x == 0 && threadIdx.x == 0 && a.dscale) {
+  if (block && blockIdx.x == 0 && a.dscale) {
+    const int n = (g1 - g0 + 1) * a.warps_per_row;
+    const float* p = a.partial_scale + (long long)(g0 + m) * a.warps_per_row;
     float t = 0.f;
-    for (int s = 0; s < a.blocks_per_member; ++s) t += a.partial_scale[m * a.blocks_per_member + s];
-    a.dscale[m] = t;
+    for (int k = threadIdx.x; k < n; k += 256) t += p[k];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
+    if (lane == 0) part[warp][0] = t;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int w = 1; w < 8; ++w) t += part[w][0];
+      a.dscale[m] = t;
+    }
   }
 }
 
@@ -461,63 +625,87 @@ void norm_shape(int width, int v, int items, int* warps, int* groups) {
   *groups = std::max(1, kNormThreads / 32 / *warps);
 }
 
-// Most vectors per thread.  Forward: a row of 8192 fits eight warps (single elements: 32).  Backward: the three column
-// sums of every element live in registers too, so a thread holds at most 16 elements and the widest rows take 16 warps.
-constexpr int norm_most(int v, bool backward) { return v == 1 ? 8 : !backward ? (v == 4 ? 8 : 4) : v == 4 ? 4 : 2; }
-
-// Vectors per thread: the smallest choice with at most eight warps per row, or the most there are.
-int norm_items(int width, int v, bool backward) {
-  const int nv = width / v, most = norm_most(v, backward);
-  int items = 1;
-  while (items < most && nv > items * 32 * 8) items *= 2;
-  return items;
+// A row fills the threads of a warp with up to 16 elements each before it takes another warp (fewer warps: cheaper
+// reductions); 8192 elements are 16 warps, and blocks have 256 threads up to 4096 elements, 512 beyond.
+struct NormShape { int items, warps, groups, threads; };
+NormShape norm_shape(int width, int v) {
+  const int nv = width / v;
+  NormShape s;
+  s.items = 1;
+  while (s.items * v < 16 && nv > s.items * 32) s.items *= 2;
+  s.warps = (nv + s.items * 32 - 1) / (s.items * 32);
+  s.groups = std::max(1, kNormThreads / 32 / s.warps);
+  s.threads = s.groups * s.warps * 32;
+  return s;
 }
 
-struct NormPlan { int v, items, warps, groups, blocks_per_member, slices, sums; size_t bytes; };
+// Blocks of the grid: `per_sm` per SM, or fewer so that every row group has a row.
+int norm_blocks(const pbt_block_norm_desc* d, int groups, int per_sm) {
+  const long long most = ((long long)d->members * d->rows + groups - 1) / groups;
+  return (int)std::max<long long>(1, std::min<long long>(per_sm * 148, most));
+}
+int norm_groups(const pbt_block_norm_desc* d, int groups, int blocks) {
+  return (int)std::max<long long>(1, std::min<long long>((long long)blocks * groups, (long long)d->members * d->rows));
+}
+
+struct NormPlan { int v, blocks, groups, sums; NormShape shape; size_t slots, bytes; };
 
 NormPlan norm_backward_plan(const pbt_block_norm_desc* d) {
   NormPlan p;
   p.v = norm_vector(d, true);
-  p.items = norm_items(d->width, p.v, true);
-  norm_shape(d->width, p.v, p.items, &p.warps, &p.groups);
-  const int want = (2 * 148 + d->members - 1) / d->members;   // two blocks per SM over all members
-  p.blocks_per_member = std::max(1, std::min(want, (d->rows + p.groups - 1) / p.groups));
-  p.slices = p.blocks_per_member * p.groups;
+  p.shape = norm_shape(d->width, p.v);
+  p.blocks = norm_blocks(d, p.shape.groups, p.shape.threads > kNormThreads ? 1 : 2);
+  p.groups = norm_groups(d, p.shape.groups, p.blocks);
   p.sums = (d->du ? 1 : 0) + (d->block ? 1 : 0) + (d->gate && d->gate_vector ? 1 : 0);
-  p.bytes = ((size_t)d->members * p.slices * p.sums * d->width + (size_t)d->members * p.blocks_per_member) * sizeof(float);
+  p.slots = (size_t)p.groups + d->members;
+  p.bytes = p.slots * ((size_t)p.sums * d->width + p.shape.warps) * sizeof(float);
   p.bytes = (p.bytes + 255) & ~(size_t)255;
   return p;
 }
 
+template <typename T, int V, int ITEMS, int THREADS>
+cudaError_t launch_norm_backward(unsigned grid, int threads, const NormArgs& a, cudaStream_t s) {
+  constexpr int per_thread = V == 1 ? 0 : norm_stages<V, ITEMS, 5, THREADS>() * 5 * ITEMS * 16;
+  static tc::DeviceSetup setup;
+  int sms = 0;
+  const cudaError_t e = tc::device_setup(&setup, k_norm_backward<T, V, ITEMS, THREADS>, per_thread * THREADS, &sms);
+  if (e != cudaSuccess) return e;
+  return launch_with(grid, threads, per_thread * threads, s)(k_norm_backward<T, V, ITEMS, THREADS>, a);
+}
+template <typename T, int V, int ITEMS, int THREADS>
+cudaError_t launch_norm_forward(unsigned grid, int threads, const NormArgs& a, cudaStream_t s) {
+  constexpr int per_thread = V == 1 ? 0 : norm_stages<V, ITEMS, 3, THREADS>() * 3 * ITEMS * 16;
+  static tc::DeviceSetup setup;
+  int sms = 0;
+  const cudaError_t e = tc::device_setup(&setup, k_norm_forward<T, V, ITEMS, THREADS>, per_thread * THREADS, &sms);
+  if (e != cudaSuccess) return e;
+  return launch_with(grid, threads, per_thread * threads, s)(k_norm_forward<T, V, ITEMS, THREADS>, a);
+}
+// The instantiations that norm_shape can ask for: blocks of 512 threads belong to 16 elements a thread.
 template <typename T, int V, int ITEMS>
-cudaError_t launch_norm_items(bool backward, unsigned grid, int threads, const NormArgs& a, cudaStream_t s) {
-  auto l = launch_with(grid, threads, 0, s);
-  if (threads > kNormThreads) {
-    // more than eight warps per row: the widest rows only
-    if constexpr (V == 1 && ITEMS == norm_most(V, false))
-      if (!backward) return l(k_norm_forward<T, V, ITEMS, 1024>, a);
-    if constexpr (ITEMS == norm_most(V, true))
-      if (backward) return l(k_norm_backward<T, V, ITEMS, (V == 1 ? 1024 : 512)>, a);
-    return cudaErrorInvalidValue;
-  }
-  if constexpr (ITEMS <= norm_most(V, true))
-    if (backward) return l(k_norm_backward<T, V, ITEMS, kNormThreads>, a);
-  if constexpr (ITEMS <= norm_most(V, false))
-    if (!backward) return l(k_norm_forward<T, V, ITEMS, kNormThreads>, a);
-  return cudaErrorInvalidValue;
+cudaError_t launch_norm(bool backward, const NormShape& p, unsigned grid, const NormArgs& a, cudaStream_t s) {
+  if constexpr (ITEMS * V == 16)
+    if (p.threads > kNormThreads)
+      return backward ? launch_norm_backward<T, V, ITEMS, 512>(grid, p.threads, a, s) : launch_norm_forward<T, V, ITEMS, 512>(grid, p.threads, a, s);
+  return backward ? launch_norm_backward<T, V, ITEMS, kNormThreads>(grid, p.threads, a, s)
+                  : launch_norm_forward<T, V, ITEMS, kNormThreads>(grid, p.threads, a, s);
 }
 template <typename T, int V>
-cudaError_t launch_norm(bool backward, int items, unsigned grid, int threads, const NormArgs& a, cudaStream_t s) {
-  switch (items) {
-    case 1: return launch_norm_items<T, V, 1>(backward, grid, threads, a, s);
-    case 2: return launch_norm_items<T, V, 2>(backward, grid, threads, a, s);
-    case 4: return launch_norm_items<T, V, 4>(backward, grid, threads, a, s);
-    default: return launch_norm_items<T, V, 8>(backward, grid, threads, a, s);
+cudaError_t launch_norm(bool backward, const NormShape& p, unsigned grid, const NormArgs& a, cudaStream_t s) {
+  if (p.items == 1) return launch_norm<T, V, 1>(backward, p, grid, a, s);
+  if constexpr (V <= 8)
+    if (p.items == 2) return launch_norm<T, V, 2>(backward, p, grid, a, s);
+  if constexpr (V <= 4)
+    if (p.items == 4) return launch_norm<T, V, 4>(backward, p, grid, a, s);
+  if constexpr (V == 1) {
+    if (p.items == 8) return launch_norm<T, V, 8>(backward, p, grid, a, s);
+    if (p.items == 16) return launch_norm<T, V, 16>(backward, p, grid, a, s);
   }
+  return cudaErrorInvalidValue;
 }
-cudaError_t launch_norm(bool bf, int v, bool backward, int items, unsigned grid, int threads, const NormArgs& a, cudaStream_t s) {
-  if (bf) return v == 1 ? launch_norm<bf16, 1>(backward, items, grid, threads, a, s) : launch_norm<bf16, 8>(backward, items, grid, threads, a, s);
-  return v == 1 ? launch_norm<float, 1>(backward, items, grid, threads, a, s) : launch_norm<float, 4>(backward, items, grid, threads, a, s);
+cudaError_t launch_norm(bool bf, int v, bool backward, const NormShape& p, unsigned grid, const NormArgs& a, cudaStream_t s) {
+  if (bf) return v == 1 ? launch_norm<bf16, 1>(backward, p, grid, a, s) : launch_norm<bf16, 8>(backward, p, grid, a, s);
+  return v == 1 ? launch_norm<float, 1>(backward, p, grid, a, s) : launch_norm<float, 4>(backward, p, grid, a, s);
 }
 
 }  // namespace
@@ -535,13 +723,11 @@ extern "C" int pbt_block_norm_forward(const pbt_block_norm_desc* d, void* stream
   NormArgs a;
   norm_fill(&a, d);
   const int v = norm_vector(d, false);
-  const int items = norm_items(d->width, v, false);
-  int groups = 1;
-  norm_shape(d->width, v, items, &a.warps_per_row, &groups);
-  const long long rows = (long long)d->members * d->rows, blocks = (rows + groups - 1) / groups;
-  if (blocks > 0x7FFFFFFFll) return norm_fail(PBT_ERR_UNSUPPORTED, "too many rows");
-  const int threads = groups * a.warps_per_row * 32;
-  const cudaError_t e = launch_norm(d->dtype == 1, v, false, items, (unsigned)blocks, threads, a, (cudaStream_t)stream);
+  const NormShape shape = norm_shape(d->width, v);
+  const int blocks = norm_blocks(d, shape.groups, shape.threads > kNormThreads ? 1 : 4);
+  a.warps_per_row = shape.warps;
+  a.groups = norm_groups(d, shape.groups, blocks);
+  const cudaError_t e = launch_norm(d->dtype == 1, v, false, shape, (unsigned)blocks, a, (cudaStream_t)stream);
   if (e != cudaSuccess) return norm_fail(PBT_ERR_CUDA, cudaGetErrorString(e));
   return PBT_OK;
 }
@@ -566,19 +752,27 @@ extern "C" int pbt_block_norm_backward(const pbt_block_norm_desc* d, void* works
   if (d->rows && ((d->du && (!d->x || !d->rstd_next)) || (d->block && (!d->dblock || !d->rstd_block)) || !d->dx))
     return norm_fail(PBT_ERR_INVALID_ARG, "y, dx, dblock or a reciprocal root is NULL");
   const NormPlan p = norm_backward_plan(d);
+  if (!d->rows) {   // no row contributes: the sums over rows are zero
+    const size_t n = (size_t)d->members * d->width;
+    cudaError_t e = cudaSuccess;
+    auto zero = [&](void* q, size_t bytes) { if (q && e == cudaSuccess) e = cudaMemsetAsync(q, 0, bytes, (cudaStream_t)stream); };
+    if (d->du) zero(d->dnext_weight, n * sizeof(float));
+    if (d->block) zero(d->dpost_weight, n * sizeof(float));
+    if (d->block) zero(d->dscale, d->members * sizeof(float));
+    if (d->gate && d->gate_vector) zero(d->dgate, n * (d->dtype ? 2 : 4));
+    return e == cudaSuccess ? PBT_OK : norm_fail(PBT_ERR_CUDA, cudaGetErrorString(e));
+  }
   if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < p.bytes)
     return norm_fail(PBT_ERR_WORKSPACE, "workspace missing, not 256-byte aligned or smaller than pbt_block_norm_query_workspace says");
   NormArgs a;
   norm_fill(&a, d);
-  a.warps_per_row = p.warps; a.blocks_per_member = p.blocks_per_member; a.slices = p.slices; a.sums = p.sums;
+  a.warps_per_row = p.shape.warps; a.groups = p.groups; a.sums = p.sums;
   a.partial = (float*)workspace;
-  a.partial_scale = a.partial + (long long)d->members * p.slices * p.sums * d->width;
-  const unsigned grid = (unsigned)d->members * p.blocks_per_member;
-  const int threads = p.groups * p.warps * 32;
+  a.partial_scale = a.partial + p.slots * p.sums * d->width;
   cudaStream_t s = (cudaStream_t)stream;
-  cudaError_t e = launch_norm(d->dtype == 1, p.v, true, p.items, grid, threads, a, s);
+  cudaError_t e = launch_norm(d->dtype == 1, p.v, true, p.shape, (unsigned)p.blocks, a, s);
   if (e == cudaSuccess) {
-    auto l = launch_with(dim3((d->width + 255) / 256, d->members), 256, 0, s);
+    auto l = launch_with(dim3((d->width + 31) / 32, d->members), 256, 0, s);
     e = d->dtype ? l(k_norm_columns<bf16>, a) : l(k_norm_columns<float>, a);
   }
   if (e != cudaSuccess) return norm_fail(PBT_ERR_CUDA, cudaGetErrorString(e));

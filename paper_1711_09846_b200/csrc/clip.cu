@@ -1,9 +1,13 @@
 // Global gradient norm over many tensors, and clipping, per group (population member):
 //   norm_g = sqrt(sum over the tensors of group g, all elements: e^2),   dst = src * min(1, limit_g / norm_g).
 //
-// Two launches over one table of chunks, sorted by group: the first leaves one partial sum of squares per chunk, the
-// second adds the partials of a chunk's group in a fixed order (no atomics: a run is reproducible bit for bit) and
-// scales.  Memory-bound: the floor is one read and one write of every element.
+// Memory-bound; the floor is ONE read and one write of every element, which asks for the gradients to stay on the chip
+// between the two.  One cooperative launch goes through the groups in waves: as many whole groups as fit the shared memory
+// of all SMs together (30 MB), or one larger group.  In a wave every CTA reads its share of the elements, keeps what fits
+// in its shared memory, leaves its sums of squares, meets the others at a grid barrier, and scales what it kept; what a
+// large group has beyond the 30 MB is read a second time, from L2 as long as the group fits there.  While a CTA waits at
+// the barrier the first bytes of its next wave are on their way into L2.
+// Sums are added in a fixed order (no atomics on values), so a run is reproducible bit for bit.
 #include <stdio.h>
 
 #include <algorithm>
@@ -17,14 +21,37 @@ void set_last_error(const char* msg);
 
 namespace {
 
-constexpr int kClipThreads = 256;
-constexpr int kClipChunk = 16384;   // elements
+constexpr int kClipThreads = 512;
+constexpr int kClipUnroll = 8;             // 16-byte loads of a thread in flight: 64 KB per SM
+constexpr int kClipCtas = 148;             // one per SM
+constexpr int kClipKeep = 208 * 1024;      // bytes of gradients a CTA keeps in shared memory
+constexpr long long kClipWave = (long long)kClipCtas * (kClipKeep - 4096);   // bytes of a wave of whole groups
+constexpr int kClipShare = 4096;           // smallest share of a CTA in a wave
+constexpr int kClipPieces = 64;            // table entries of a wave that are fetched ahead of it
+constexpr int kClipAhead = 96 * 1024;      // bytes of the next wave asked for at the barrier
+constexpr unsigned int kClipPolls = 1u << 24;
 
-struct ClipChunk {
+// A run of elements of one tensor that one CTA handles in one wave.
+struct __align__(16) ClipPiece {
   const char* src;
   char* dst;
-  int count;
-  int group_and_type;   // group * 2 + (1: bfloat16)
+  int count;       // elements
+  int kept;        // where the elements are kept in shared memory (same alignment as src), or -1
+  int group;
+  int bf;          // 1: bfloat16
+};
+
+struct ClipArgs {
+  const ClipPiece* pieces;
+  const int* first;        // [waves * CTAs + 1] first piece of every (wave, CTA)
+  const int* first_sum;    // [waves * CTAs] first partial sum of every (wave, CTA): one per group it touches
+  const int* group_sums;   // [groups + 1] partial sums of every group
+  double* sums;
+  unsigned int* barrier;   // arrivals, exits, status
+  int n_waves, n_groups;
+  float limit;
+  const float* limits;
+  float* norms;
 };
 
 __device__ __forceinline__ float clip_load(const bf16* p) { return __bfloat162float(*p); }
@@ -39,37 +66,166 @@ __device__ __forceinline__ S clip_block_sum(S v, S* scratch) {
   __syncthreads();
   if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
   __syncthreads();
-  S t = scratch[0];
-  for (int w = 1; w < kClipThreads / 32; ++w) t += scratch[w];
+  S t = scratch[threadIdx.x & (kClipThreads / 32 - 1)];
+#pragma unroll
+  for (int o = kClipThreads / 64; o > 0; o >>= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
   return t;
 }
 
-// Squares in fp32; where their sum leaves the range in which fp32 squares are exact to rounding (elements beyond
-// 1.8e19 or all below 1e-15), the chunk is summed again in fp64, so that only the norm itself can overflow.
+// 16 bytes of gradients
+template <typename T> struct Quad;
+template <> struct Quad<float> {
+  static constexpr int n = 4;
+  static __device__ __forceinline__ void get(const uint4& r, float* f) {
+    f[0] = __uint_as_float(r.x); f[1] = __uint_as_float(r.y); f[2] = __uint_as_float(r.z); f[3] = __uint_as_float(r.w);
+  }
+  static __device__ __forceinline__ uint4 put(const float* f) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  }
+};
+template <> struct Quad<bf16> {
+  static constexpr int n = 8;
+  static __device__ __forceinline__ void get(const uint4& r, float* f) {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+  static __device__ __forceinline__ uint4 put(const float* f) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      __nv_bfloat162 t = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+      w[i] = *reinterpret_cast<uint32_t*>(&t);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+
+// A piece is its elements up to the first 16-byte boundary, 16-byte vectors, and the rest.
+struct ClipSpan { int head, vectors, tail; };   // elements, vectors, first element of the rest
 template <typename T>
-__device__ double clip_sum_squares(const T* g, int n, double* scratch) {
-  float s = 0.f;
-  for (int i = threadIdx.x; i < n; i += kClipThreads) {
-    const float v = clip_load(g + i);
-    s = __fmaf_rn(v, v, s);
-  }
-  const float t = clip_block_sum(s, reinterpret_cast<float*>(scratch));
-  if (t > 1e-30f && t < 3e38f) return t;
-  double d = 0.0;
-  for (int i = threadIdx.x; i < n; i += kClipThreads) {
-    const double v = clip_load(g + i);
-    d = fma(v, v, d);
-  }
-  return clip_block_sum(d, scratch);
+__device__ __forceinline__ ClipSpan clip_span(const ClipPiece& p) {
+  ClipSpan s;
+  s.head = min(p.count, (int)((16 - ((uintptr_t)p.src & 15)) & 15) / (int)sizeof(T));
+  s.vectors = (p.count - s.head) / Quad<T>::n;
+  s.tail = s.head + s.vectors * Quad<T>::n;
+  return s;
 }
 
-__global__ void __launch_bounds__(kClipThreads) k_clip_norm(const ClipChunk* __restrict__ chunks, double* __restrict__ partial) {
-  pdl_prologue();
-  __shared__ double scratch[kClipThreads / 32];
-  const ClipChunk c = chunks[blockIdx.x];
-  const double s = (c.group_and_type & 1) ? clip_sum_squares(reinterpret_cast<const bf16*>(c.src), c.count, scratch)
-                                          : clip_sum_squares(reinterpret_cast<const float*>(c.src), c.count, scratch);
-  if (threadIdx.x == 0) partial[blockIdx.x] = s;
+// Pieces of a few hundred elements go to one warp each, in turn, so that a CTA has many of them in flight: the thread's
+// first vector and the distance to its next, or nothing for it to do.
+__device__ __forceinline__ bool clip_lanes(const ClipPiece& p, int index, int& lane, int& lanes) {
+  lane = threadIdx.x;
+  lanes = kClipThreads;
+  if (p.count > 1024) return true;
+  lane &= 31;
+  lanes = 32;
+  return (int)(threadIdx.x >> 5) == (index & (kClipThreads / 32 - 1));
+}
+
+template <typename T>
+__device__ __forceinline__ void clip_add(const uint4& v, float* sum) {
+  float f[Quad<T>::n];
+  Quad<T>::get(v, f);
+#pragma unroll
+  for (int e = 0; e < Quad<T>::n; ++e) sum[e & 3] = __fmaf_rn(f[e], f[e], sum[e & 3]);
+}
+
+template <typename T>
+__device__ __forceinline__ float clip_read(const ClipPiece& p, int index, char* keep) {
+  int i, lanes;
+  if (!clip_lanes(p, index, i, lanes)) return 0.f;
+  const ClipSpan s = clip_span<T>(p);
+  const T* g = reinterpret_cast<const T*>(p.src);
+  T* k = reinterpret_cast<T*>(keep + p.kept);
+  const uint4* gv = reinterpret_cast<const uint4*>(g + s.head);
+  uint4* kv = reinterpret_cast<uint4*>(k + s.head);
+  const bool kept = p.kept >= 0;
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  const int loose = s.head + p.count - s.tail;      // fewer than 16 elements
+  if (i < loose) {
+    const int at = i < s.head ? i : s.tail + i - s.head;
+    const T v = g[at];
+    if (kept) k[at] = v;
+    const float f = clip_load(&v);
+    sum[0] = f * f;
+  }
+  if (lanes == kClipThreads)
+    for (; i + (kClipUnroll - 1) * kClipThreads < s.vectors; i += kClipUnroll * kClipThreads) {
+      uint4 v[kClipUnroll];
+#pragma unroll
+      for (int u = 0; u < kClipUnroll; ++u) v[u] = __ldcg(gv + i + u * kClipThreads);
+#pragma unroll
+      for (int u = 0; u < kClipUnroll; ++u) {
+        if (kept) kv[i + u * kClipThreads] = v[u];
+        clip_add<T>(v[u], sum);
+      }
+    }
+#pragma unroll 4
+  for (; i < s.vectors; i += lanes) {
+    const uint4 v = __ldcg(gv + i);
+    if (kept) kv[i] = v;
+    clip_add<T>(v, sum);
+  }
+  return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+}
+
+template <typename T>
+__device__ __noinline__ double clip_read_wide(const char* src, int count) {
+  const T* g = reinterpret_cast<const T*>(src);
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < count; i += kClipThreads) {
+    const double v = clip_load(g + i);
+    sum = fma(v, v, sum);
+  }
+  return sum;
+}
+
+template <typename T>
+__device__ __forceinline__ uint4 clip_scaled(const uint4& v, float f) {
+  float e[Quad<T>::n];
+  Quad<T>::get(v, e);
+#pragma unroll
+  for (int j = 0; j < Quad<T>::n; ++j) e[j] *= f;
+  return Quad<T>::put(e);
+}
+
+template <typename T>
+__device__ __forceinline__ void clip_write(const ClipPiece& p, int index, const char* keep, float f) {
+  int i, lanes;
+  if (!clip_lanes(p, index, i, lanes)) return;
+  const ClipSpan s = clip_span<T>(p);
+  const T* g = p.kept >= 0 ? reinterpret_cast<const T*>(keep + p.kept) : reinterpret_cast<const T*>(p.src);
+  T* o = reinterpret_cast<T*>(p.dst);
+  const uint4* gv = reinterpret_cast<const uint4*>(g + s.head);
+  const int loose = s.head + p.count - s.tail;
+  if (i < loose) {
+    const int at = i < s.head ? i : s.tail + i - s.head;
+    clip_store(o + at, clip_load(g + at) * f);
+  }
+  uint4* ov = reinterpret_cast<uint4*>(o + s.head);
+  if (((uintptr_t)ov & 15) != 0) {     // a destination of another alignment than its source: element by element
+    for (; i < s.vectors; i += lanes) {
+      float e[Quad<T>::n];
+      Quad<T>::get(gv[i], e);
+#pragma unroll
+      for (int j = 0; j < Quad<T>::n; ++j) clip_store(o + s.head + i * Quad<T>::n + j, e[j] * f);
+    }
+    return;
+  }
+  if (lanes == kClipThreads)
+    for (; i + (kClipUnroll - 1) * kClipThreads < s.vectors; i += kClipUnroll * kClipThreads) {
+      uint4 v[kClipUnroll];
+#pragma unroll
+      for (int u = 0; u < kClipUnroll; ++u) v[u] = gv[i + u * kClipThreads];
+#pragma unroll
+      for (int u = 0; u < kClipUnroll; ++u) __stcs(ov + i + u * kClipThreads, clip_scaled<T>(v[u], f));
+    }
+#pragma unroll 4
+  for (; i < s.vectors; i += lanes) __stcs(ov + i, clip_scaled<T>(gv[i], f));
 }
 
 // min(1, limit / norm); a NaN norm makes the factor NaN (a diverged member stays visible), an infinite limit never clips
@@ -79,37 +235,126 @@ __device__ __forceinline__ float clip_factor(float limit, float norm) {
   return __fdiv_rn(limit, norm);
 }
 
-template <typename T>
-__device__ void clip_scale(const ClipChunk& c, float f) {
-  const T* g = reinterpret_cast<const T*>(c.src);
-  T* o = reinterpret_cast<T*>(c.dst);
-  for (int i = threadIdx.x; i < c.count; i += kClipThreads) clip_store(o + i, clip_load(g + i) * f);
+// Arrive at the grid barrier (thread 0, after the block's sums are written), and wait until `target` CTAs have arrived.
+// The wait is bounded; on expiry the status word is set, everybody leaves, and the norms that are missing stay NaN.
+__device__ __forceinline__ void clip_arrive(const ClipArgs& a) {
+  __threadfence();
+  atomicAdd(a.barrier, 1u);
+}
+__device__ __forceinline__ bool clip_wait(const ClipArgs& a, unsigned int target) {
+  volatile unsigned int* count = a.barrier;
+  volatile unsigned int* status = a.barrier + 2;
+  for (unsigned int i = 0; *count < target; ++i) {
+    if (i > kClipPolls || (i > 64 && *status)) {
+      *status = PBT_ERR_TIMEOUT;
+      return false;
+    }
+    __nanosleep(20);
+  }
+  __threadfence();
+  return true;
 }
 
-__global__ void __launch_bounds__(kClipThreads) k_clip_scale(const ClipChunk* __restrict__ chunks, int n_chunks,
-                                                             const double* __restrict__ partial,
-                                                             const int* __restrict__ group_begin, float limit,
-                                                             const float* __restrict__ limits, float* __restrict__ norms) {
+__global__ void __launch_bounds__(kClipThreads, 1) k_clip(const ClipArgs a) {
   pdl_prologue();
-  __shared__ double scratch[kClipThreads / 32];
-  ClipChunk c;
-  c.count = 0;
-  int group = (int)blockIdx.x - n_chunks;   // the blocks behind the chunks write the norms
-  if (group < 0) {
-    c = chunks[blockIdx.x];
-    group = c.group_and_type >> 1;
+  extern __shared__ __align__(16) char keep[];
+  __shared__ ClipPiece near[2][kClipPieces];
+  __shared__ double scratch[32];
+  __shared__ int go;
+  const int tid = threadIdx.x, b = blockIdx.x, ctas = gridDim.x;
+  if (b == 0)
+    for (int g = tid; g < a.n_groups; g += kClipThreads)
+      a.norms[g] = a.group_sums[g] == a.group_sums[g + 1] ? 0.f : __int_as_float(0x7FC00000);
+  auto fetch = [&](int w) {
+    if (w < a.n_waves) {
+      const int first = a.first[w * ctas + b], n = min(a.first[w * ctas + b + 1] - first, kClipPieces);
+      if (tid < n) near[w & 1][tid] = a.pieces[first + tid];
+    }
+  };
+  fetch(0);
+  __syncthreads();
+  for (int w = 0; w < a.n_waves; ++w) {
+    const int first = a.first[w * ctas + b], n = a.first[w * ctas + b + 1] - first;
+    int sum_at = a.first_sum[w * ctas + b];
+    auto piece = [&](int i) {      // two 16-byte loads, from shared memory for the entries that were fetched ahead
+      const ulonglong2* from = reinterpret_cast<const ulonglong2*>(i < kClipPieces ? &near[w & 1][i] : a.pieces + first + i);
+      const ulonglong2 where = from[0], what = from[1];
+      ClipPiece p;
+      p.src = reinterpret_cast<const char*>(where.x);
+      p.dst = reinterpret_cast<char*>(where.y);
+      p.count = (int)what.x;
+      p.kept = (int)(what.x >> 32);
+      p.group = (int)what.y;
+      p.bf = (int)(what.y >> 32);
+      return p;
+    };
+    for (int i = 0; i < n;) {                      // one group of the CTA's share after the other
+      const int begin = i, group = piece(i).group;
+      float sum = 0.f;
+      for (; i < n; ++i) {
+        const ClipPiece p = piece(i);
+        if (p.group != group) break;
+        sum += p.bf ? clip_read<bf16>(p, i, keep) : clip_read<float>(p, i, keep);
+      }
+      const float t = clip_block_sum(sum, reinterpret_cast<float*>(scratch));
+      double total = t;
+      // Squares are fp32; where their sum leaves the range in which that is exact to rounding (elements beyond 1.8e19, or
+      // all below 1e-15), the group's share is summed again in fp64, so that only the norm itself can overflow.
+      if (!(t > 1e-30f && t < 3e38f)) {
+        double d = 0.0;
+        for (int k = begin; k < i; ++k) {
+          const ClipPiece p = piece(k);
+          d += p.bf ? clip_read_wide<bf16>(p.src, p.count) : clip_read_wide<float>(p.src, p.count);
+        }
+        total = clip_block_sum(d, scratch);
+      }
+      if (tid == 0) a.sums[sum_at] = total;
+      ++sum_at;
+    }
+    if (tid == 0) clip_arrive(a);
+    fetch(w + 1);
+    __syncthreads();
+    if (w + 1 < a.n_waves) {
+      const int next = a.first[(w + 1) * ctas + b], m = a.first[(w + 1) * ctas + b + 1] - next;
+      if (tid < min(m, kClipPieces)) {
+        const ClipPiece& p = near[(w + 1) & 1][tid];
+        const uintptr_t from = ((uintptr_t)p.src + 15) & ~(uintptr_t)15;
+        long long bytes = (long long)((uintptr_t)p.src + (long long)p.count * (p.bf ? 2 : 4) - from) & ~15ll;
+        if (bytes > kClipAhead) bytes = kClipAhead;
+        if (bytes >= 16 && p.kept >= 0 && p.kept < kClipAhead)
+          asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"((uint32_t)bytes) : "memory");
+      }
+    }
+    if (tid == 0) go = clip_wait(a, (unsigned int)(w + 1) * ctas);
+    __syncthreads();
+    if (!go) break;
+    sum_at = a.first_sum[w * ctas + b];
+    for (int i = 0; i < n;) {
+      const int group = piece(i).group, s0 = a.group_sums[group], s1 = a.group_sums[group + 1];
+      double s = 0.0;
+      for (int k = s0 + tid; k < s1; k += kClipThreads) s += __ldcg(a.sums + k);
+      const float norm = (float)sqrt(clip_block_sum(s, scratch));
+      if (s0 == sum_at && tid == 0) a.norms[group] = norm;     // the CTA that holds the group's first sum
+      ++sum_at;
+      const float f = clip_factor(a.limits ? a.limits[group] : a.limit, norm);
+      for (; i < n; ++i) {
+        const ClipPiece p = piece(i);
+        if (p.group != group) break;
+        if (f == 1.f && p.src == p.dst) continue;
+        if (p.bf) clip_write<bf16>(p, i, keep, f);
+        else clip_write<float>(p, i, keep, f);
+      }
+    }
+    __syncthreads();     // `keep` and the tables are written again by the next wave
   }
-  double s = 0.0;
-  for (int i = group_begin[group] + threadIdx.x; i < group_begin[group + 1]; i += kClipThreads) s += partial[i];
-  const float norm = (float)sqrt(clip_block_sum(s, scratch));
-  if ((int)blockIdx.x >= n_chunks) {
-    if (threadIdx.x == 0) norms[group] = norm;
-    return;
+  // the last CTA to leave puts the barrier back for the next run
+  if (tid == 0) {
+    __threadfence();
+    if (atomicAdd(a.barrier + 1, 1u) == (unsigned int)ctas - 1) {
+      a.barrier[0] = 0;
+      a.barrier[1] = 0;
+    }
   }
-  const float f = clip_factor(limits ? limits[group] : limit, norm);
-  if (f == 1.f && c.src == c.dst) return;
-  if (c.group_and_type & 1) clip_scale<bf16>(c, f);
-  else clip_scale<float>(c, f);
 }
 
 int clip_fail(int code, const char* msg) {
@@ -119,35 +364,114 @@ int clip_fail(int code, const char* msg) {
 
 size_t clip_align(size_t n) { return (n + 255) & ~(size_t)255; }
 
-struct ClipLayout {
-  size_t partial, begin, chunks, total;
-};
-ClipLayout clip_layout(long long n_chunks, int n_groups) {
-  ClipLayout l;
-  l.partial = 0;
-  l.begin = clip_align((size_t)n_chunks * sizeof(double));
-  l.chunks = l.begin + clip_align((size_t)(n_groups + 1) * sizeof(int));
-  l.total = l.chunks + clip_align((size_t)n_chunks * sizeof(ClipChunk));
-  return l;
-}
-
-int clip_check(const pbt_clip_tensor* t, int n, int n_groups, long long* n_chunks) {
+int clip_check(const pbt_clip_tensor* t, int n, int n_groups) {
   if (n < 0 || n_groups < 1 || n_groups > (1 << 20)) return clip_fail(PBT_ERR_INVALID_ARG, "n_tensors must be >= 0 and n_groups in [1, 2^20]");
   if (n > 0 && !t) return clip_fail(PBT_ERR_INVALID_ARG, "tensors is NULL");
-  long long total = 0;
   for (int i = 0; i < n; ++i) {
     if (t[i].numel < 0 || (t[i].numel > 0 && (!t[i].src || !t[i].dst)))
       return clip_fail(PBT_ERR_INVALID_ARG, "a gradient tensor has a negative size or a NULL pointer");
+    if (t[i].numel > (1ll << 46)) return clip_fail(PBT_ERR_INVALID_ARG, "a gradient tensor is larger than any memory");
     if (t[i].dtype != 0 && t[i].dtype != 1) return clip_fail(PBT_ERR_UNSUPPORTED, "gradient tensors are float or bfloat16");
     if (t[i].group < 0 || t[i].group >= n_groups) return clip_fail(PBT_ERR_INVALID_ARG, "a tensor's group is out of range");
     const uintptr_t esz = t[i].dtype ? 2 : 4;
     if (((uintptr_t)t[i].src % esz) || ((uintptr_t)t[i].dst % esz))
       return clip_fail(PBT_ERR_INVALID_ARG, "a gradient tensor is not aligned to its element size");
-    total += (t[i].numel + kClipChunk - 1) / kClipChunk;
   }
-  if (total > (1ll << 30)) return clip_fail(PBT_ERR_UNSUPPORTED, "too many gradient elements for one call");
-  *n_chunks = total;
   return PBT_OK;
+}
+
+// Who handles what: waves of whole groups, every wave's bytes dealt to the CTAs in equal consecutive shares.
+struct ClipTable {
+  std::vector<ClipPiece> pieces;
+  std::vector<int> first, first_sum, group_sums;
+  int n_waves = 0, ctas = 1;
+};
+bool clip_table(const pbt_clip_tensor* t, int n_tensors, int n_groups, ClipTable* out) {
+  std::vector<int> order;
+  std::vector<long long> group_bytes(n_groups, 0);
+  long long total = 0;
+  for (int i = 0; i < n_tensors; ++i)
+    if (t[i].numel) {
+      order.push_back(i);
+      group_bytes[t[i].group] += t[i].numel * (t[i].dtype ? 2 : 4);
+      total += t[i].numel * (t[i].dtype ? 2 : 4);
+    }
+  if (total > (1ll << 40)) return false;
+  std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return t[a].group < t[b].group; });
+  std::vector<long long> wave_bytes;
+  std::vector<size_t> wave_end;          // in `order`
+  for (size_t i = 0; i < order.size();) {
+    const int g = t[order[i]].group;
+    size_t e = i;
+    while (e < order.size() && t[order[e]].group == g) ++e;
+    if (wave_bytes.empty() || wave_bytes.back() + group_bytes[g] > kClipWave) {
+      wave_bytes.push_back(0);
+      wave_end.push_back(i);
+    }
+    wave_bytes.back() += group_bytes[g];
+    wave_end.back() = e;
+    i = e;
+  }
+  out->n_waves = (int)wave_bytes.size();
+  long long most = 0;
+  for (long long b : wave_bytes) most = std::max(most, b);
+  out->ctas = (int)std::max<long long>(1, std::min<long long>(kClipCtas, (most + kClipShare - 1) / kClipShare));
+  out->group_sums.assign(n_groups + 1, 0);
+  size_t at = 0;
+  int sums = 0;
+  for (int w = 0; w < out->n_waves; ++w) {
+    const long long share = std::max<long long>(kClipShare, ((wave_bytes[w] + out->ctas - 1) / out->ctas + 15) / 16 * 16);
+    long long done = 0;                  // elements of tensor order[at] that are dealt
+    for (int c = 0; c < out->ctas; ++c) {
+      out->first.push_back((int)out->pieces.size());
+      out->first_sum.push_back(sums);
+      long long room = share;
+      int kept = 0, group = -1;
+      while (at < wave_end[w] && (room > 0 || c == out->ctas - 1)) {
+        const pbt_clip_tensor& x = t[order[at]];
+        const long long esz = x.dtype ? 2 : 4, left = x.numel - done;
+        const char* src = (const char*)x.src + done * esz;
+        const int phase = (int)((uintptr_t)src & 15);
+        long long take = left;
+        const long long space = (kClipKeep - kept - 16) / 16 * 16;   // for a piece that keeps its alignment
+        bool keeps = space >= 1024;
+        auto cut = [&](long long bytes) { take = std::min(take, std::max<long long>(1, (bytes - phase) / esz)); };
+        if (c < out->ctas - 1 && left * esz > room) cut((room + 15) / 16 * 16 + 16);   // pieces end on 16-byte boundaries
+        if (keeps) cut(space);
+        cut(1ll << 30);
+        out->pieces.push_back({src, (char*)x.dst + done * esz, (int)take, keeps ? kept + phase : -1, x.group, x.dtype});
+        if (keeps) kept += (int)((phase + take * esz + 15) / 16 * 16);
+        if (x.group != group) {
+          group = x.group;
+          ++sums;
+          out->group_sums[group + 1] = sums;
+        }
+        room -= take * esz;
+        done += take;
+        if (done == x.numel) { ++at; done = 0; }
+      }
+      if (out->pieces.size() > (1u << 30)) return false;
+    }
+  }
+  out->first.push_back((int)out->pieces.size());
+  for (int g = 0; g < n_groups; ++g) out->group_sums[g + 1] = std::max(out->group_sums[g], out->group_sums[g + 1]);
+  out->first_sum.push_back(sums);
+  return true;
+}
+
+struct ClipLayout {
+  size_t barrier, sums, group_sums, first, first_sum, pieces, total;
+};
+ClipLayout clip_layout(const ClipTable& t) {
+  ClipLayout l;
+  l.barrier = 0;
+  l.sums = 256;
+  l.group_sums = l.sums + clip_align((size_t)t.first_sum.back() * sizeof(double));
+  l.first = l.group_sums + clip_align(t.group_sums.size() * sizeof(int));
+  l.first_sum = l.first + clip_align(t.first.size() * sizeof(int));
+  l.pieces = l.first_sum + clip_align(t.first_sum.size() * sizeof(int));
+  l.total = l.pieces + clip_align(t.pieces.size() * sizeof(ClipPiece));
+  return l;
 }
 
 // A destination may be its own source (in place) and nothing else that this call reads or writes.
@@ -174,18 +498,22 @@ bool clip_overlap(const pbt_clip_tensor* t, int n) {
 }  // namespace pbt
 
 struct pbt_clip {
-  const pbt::ClipChunk* chunks;
-  double* partial;
-  const int* group_begin;
-  int n_chunks, n_groups;
+  pbt::ClipArgs args;
+  int ctas;
 };
 
 extern "C" int pbt_clip_query_workspace(const pbt_clip_tensor* tensors, int32_t n_tensors, int32_t n_groups, size_t* bytes) {
-  if (!bytes) return pbt::clip_fail(PBT_ERR_INVALID_ARG, "bytes is NULL");
-  long long n_chunks = 0;
-  const int rc = pbt::clip_check(tensors, n_tensors, n_groups, &n_chunks);
+  using namespace pbt;
+  if (!bytes) return clip_fail(PBT_ERR_INVALID_ARG, "bytes is NULL");
+  const int rc = clip_check(tensors, n_tensors, n_groups);
   if (rc) return rc;
-  *bytes = pbt::clip_layout(n_chunks, n_groups).total;
+  try {
+    ClipTable t;
+    if (!clip_table(tensors, n_tensors, n_groups, &t)) return clip_fail(PBT_ERR_UNSUPPORTED, "too many gradient elements for one call");
+    *bytes = clip_layout(t).total;
+  } catch (const std::bad_alloc&) {
+    return clip_fail(PBT_ERR_STATE, "out of host memory");
+  }
   return PBT_OK;
 }
 
@@ -194,43 +522,40 @@ extern "C" int pbt_clip_create(pbt_clip_t** out, const pbt_clip_tensor* tensors,
   using namespace pbt;
   if (!out) return clip_fail(PBT_ERR_INVALID_ARG, "out is NULL");
   *out = nullptr;
-  long long n_chunks = 0;
-  const int rc = clip_check(tensors, n_tensors, n_groups, &n_chunks);
+  const int rc = clip_check(tensors, n_tensors, n_groups);
   if (rc) return rc;
-  const ClipLayout l = clip_layout(n_chunks, n_groups);
-  if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < l.total)
-    return clip_fail(PBT_ERR_WORKSPACE, "workspace missing, not 256-byte aligned or smaller than pbt_clip_query_workspace says");
   try {
+    ClipTable t;
+    if (!clip_table(tensors, n_tensors, n_groups, &t)) return clip_fail(PBT_ERR_UNSUPPORTED, "too many gradient elements for one call");
+    const ClipLayout l = clip_layout(t);
+    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < l.total)
+      return clip_fail(PBT_ERR_WORKSPACE, "workspace missing, not 256-byte aligned or smaller than pbt_clip_query_workspace says");
     if (clip_overlap(tensors, n_tensors))
       return clip_fail(PBT_ERR_INVALID_ARG, "a destination overlaps another tensor of the call (only dst == src is allowed)");
-    std::vector<int> order(n_tensors), begin(n_groups + 1, 0);
-    for (int i = 0; i < n_tensors; ++i) order[i] = i;
-    std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return tensors[a].group < tensors[b].group; });
-    std::vector<ClipChunk> table;
-    table.reserve((size_t)n_chunks);
-    for (int i : order) {
-      const pbt_clip_tensor& t = tensors[i];
-      const long long esz = t.dtype ? 2 : 4;
-      for (long long at = 0; at < t.numel; at += kClipChunk) {
-        const long long left = t.numel - at;
-        table.push_back({(const char*)t.src + at * esz, (char*)t.dst + at * esz, (int)(left < kClipChunk ? left : kClipChunk),
-                         t.group * 2 + t.dtype});
-      }
-      begin[t.group + 1] = (int)table.size();
-    }
-    for (int g = 0; g < n_groups; ++g) begin[g + 1] = std::max(begin[g], begin[g + 1]);   // groups without elements
     char* base = (char*)workspace;
-    cudaError_t e = cudaMemcpyAsync(base + l.begin, begin.data(), begin.size() * sizeof(int), cudaMemcpyHostToDevice, (cudaStream_t)stream);
-    if (e == cudaSuccess && n_chunks)
-      e = cudaMemcpyAsync(base + l.chunks, table.data(), table.size() * sizeof(ClipChunk), cudaMemcpyHostToDevice, (cudaStream_t)stream);
-    if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);   // the tables above are this function's own
+    cudaStream_t s = (cudaStream_t)stream;
+    cudaError_t e = cudaMemsetAsync(base + l.barrier, 0, 256, s);
+    auto upload = [&](size_t at, const void* from, size_t bytes) {
+      if (e == cudaSuccess && bytes) e = cudaMemcpyAsync(base + at, from, bytes, cudaMemcpyHostToDevice, s);
+    };
+    upload(l.group_sums, t.group_sums.data(), t.group_sums.size() * sizeof(int));
+    upload(l.first, t.first.data(), t.first.size() * sizeof(int));
+    upload(l.first_sum, t.first_sum.data(), t.first_sum.size() * sizeof(int));
+    upload(l.pieces, t.pieces.data(), t.pieces.size() * sizeof(ClipPiece));
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);   // the tables above are this function's own
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_clip, cudaFuncAttributeMaxDynamicSharedMemorySize, kClipKeep);
     if (e != cudaSuccess) return clip_fail(PBT_ERR_CUDA, cudaGetErrorString(e));
     pbt_clip* p = new pbt_clip;
-    p->chunks = (const ClipChunk*)(base + l.chunks);
-    p->partial = (double*)(base + l.partial);
-    p->group_begin = (const int*)(base + l.begin);
-    p->n_chunks = (int)n_chunks;
-    p->n_groups = n_groups;
+    memset(&p->args, 0, sizeof(p->args));
+    p->args.pieces = (const ClipPiece*)(base + l.pieces);
+    p->args.first = (const int*)(base + l.first);
+    p->args.first_sum = (const int*)(base + l.first_sum);
+    p->args.group_sums = (const int*)(base + l.group_sums);
+    p->args.sums = (double*)(base + l.sums);
+    p->args.barrier = (unsigned int*)(base + l.barrier);
+    p->args.n_waves = t.n_waves;
+    p->args.n_groups = n_groups;
+    p->ctas = t.ctas;
     *out = p;
   } catch (const std::bad_alloc&) {
     return clip_fail(PBT_ERR_STATE, "out of host memory");
@@ -247,12 +572,24 @@ extern "C" int pbt_clip_run(pbt_clip_t* p, float limit, const float* limits_devi
   using namespace pbt;
   if (!p || !norms_out_device) return clip_fail(PBT_ERR_INVALID_ARG, "handle or norms_out_device is NULL");
   if (!limits_device && !(limit >= 0.f)) return clip_fail(PBT_ERR_INVALID_ARG, "the norm limit must be >= 0");
-  cudaStream_t s = (cudaStream_t)stream;
-  cudaError_t e = cudaSuccess;
-  if (p->n_chunks) e = launch_with(p->n_chunks, kClipThreads, 0, s)(k_clip_norm, p->chunks, p->partial);
-  if (e == cudaSuccess)
-    e = launch_with(p->n_chunks + p->n_groups, kClipThreads, 0, s)(k_clip_scale, p->chunks, p->n_chunks, p->partial, p->group_begin,
-                                                              limit, limits_device, norms_out_device);
+  ClipArgs a = p->args;
+  a.limit = limit;
+  a.limits = limits_device;
+  a.norms = norms_out_device;
+  void* args[] = {&a};
+  // cooperative: every CTA is resident, which the grid barrier relies on
+  const cudaError_t e = cudaLaunchCooperativeKernel((const void*)k_clip, dim3(p->ctas), dim3(kClipThreads), args, kClipKeep, (cudaStream_t)stream);
   if (e != cudaSuccess) return clip_fail(PBT_ERR_CUDA, cudaGetErrorString(e));
+  return PBT_OK;
+}
+
+extern "C" int pbt_clip_status(pbt_clip_t* p, void* stream) {
+  using namespace pbt;
+  if (!p) return clip_fail(PBT_ERR_INVALID_ARG, "handle is NULL");
+  unsigned int status = 0;
+  cudaError_t e = cudaMemcpyAsync(&status, p->args.barrier + 2, sizeof(status), cudaMemcpyDeviceToHost, (cudaStream_t)stream);
+  if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);
+  if (e != cudaSuccess) return clip_fail(PBT_ERR_CUDA, cudaGetErrorString(e));
+  if (status) return clip_fail((int)status, "the grid barrier of a clipping run timed out; its norms are NaN");
   return PBT_OK;
 }

@@ -27,29 +27,21 @@ def _require(ok, message: str) -> None:
         raise ValueError(message)
 
 
-class _On:
-    """Makes `device` and `stream` current for a call; inputs that live on another stream are kept until it is done."""
-
-    def __init__(self, device, stream, inputs=()):
-        self.handle = None
-        current = torch.cuda.current_stream(device)
-        if stream is None or stream == current:
-            self.stream, self.scope = current, (None if torch.cuda.current_device() == device.index else torch.cuda.device(device))
-        else:
-            _require(stream.device == device, "the stream belongs to another device than the tensors")
-            self.stream, self.scope = stream, torch.cuda.stream(stream)
-            for t in inputs:
-                if t is not None:
-                    t.record_stream(stream)
-
-    def __enter__(self):
-        if self.scope is not None:
-            self.scope.__enter__()
-        return self.stream.cuda_stream
-
-    def __exit__(self, *exc):
-        if self.scope is not None:
-            self.scope.__exit__(*exc)
+def _on(device, stream, inputs, work, *args):
+    """work(stream handle, *args) with `device` and `stream` current, so that what it allocates belongs to the stream.
+    When that is not the current stream, the memory of the inputs is kept until it is done with them."""
+    current = torch.cuda.current_stream(device)
+    if stream is None or stream == current:
+        if torch.cuda.current_device() == device.index:
+            return work(current.cuda_stream, *args)
+        with torch.cuda.device(device):
+            return work(current.cuda_stream, *args)
+    _require(stream.device == device, "the stream belongs to another device than the tensors")
+    for t in inputs:
+        if t is not None:
+            t.record_stream(stream)
+    with torch.cuda.stream(stream):
+        return work(stream.cuda_stream, *args)
 
 
 def _workspace(nbytes: int, device) -> torch.Tensor:
@@ -87,25 +79,35 @@ class GradientClip:
         nbytes = C.c_size_t(0)
         _check(self.lib.pbt_clip_query_workspace(table, len(grads), self.n_groups, C.byref(nbytes)))
         self._handle = C.c_void_p(None)
-        with _On(self.device, None) as s:
+
+        def create(s):
             self._ws = _workspace(nbytes.value, self.device)
             _check(self.lib.pbt_clip_create(C.byref(self._handle), table, len(grads), self.n_groups, self._ws.data_ptr(),
                                             nbytes.value, s))
+        _on(self.device, None, (), create)
 
     def run(self, max_norm, stream=None) -> torch.Tensor:
         """Clip every group to max_norm (a number, or a float32 tensor [n_groups] on the device); returns the norms
         before clipping, float32 [n_groups]."""
         limits, limit = None, 0.0
         if isinstance(max_norm, torch.Tensor):
-            _require(max_norm.dtype == torch.float32 and max_norm.device == self.device and max_norm.is_contiguous()
+            _require(max_norm.dtype is torch.float32 and max_norm.device == self.device and max_norm.is_contiguous()
                      and max_norm.numel() == self.n_groups, "max_norm is a number or a contiguous float32 tensor [n_groups] on the gradients' device")
             limits = max_norm.data_ptr()
         else:
             limit = float(max_norm)
-        with _On(self.device, stream, (max_norm,) if limits else ()) as s:
-            norms = torch.empty(self.n_groups, dtype=torch.float32, device=self.device)
-            _check(self.lib.pbt_clip_run(self._handle, limit, limits, norms.data_ptr(), s))
+        return _on(self.device, stream, (max_norm,) if limits else (), self._run, limit, limits)
+
+    def _run(self, s, limit, limits):
+        norms = torch.empty(self.n_groups, dtype=torch.float32, device=self.device)
+        rc = self.lib.pbt_clip_run(self._handle, limit, limits, norms.data_ptr(), s)
+        if rc:
+            _check(rc)
         return norms
+
+    def check(self):
+        """Waits for the runs on the current stream and raises if one of them timed out (PBT_ERR_TIMEOUT)."""
+        _check(self.lib.pbt_clip_status(self._handle, torch.cuda.current_stream(self.device).cuda_stream))
 
     def __del__(self):
         if getattr(self, "_handle", None):
@@ -119,7 +121,7 @@ class GradientClip:
 class BlockNormOut(NamedTuple):
     y: torch.Tensor                      # residual stream behind the block (x itself without a block)
     u: Optional[torch.Tensor]            # normalised input of the next block
-    rstd_block: Optional[torch.Tensor]   # reciprocal roots for the backward pass, float32 [members, rows]
+    rstd_block: Optional[torch.Tensor]   # with keep: reciprocal roots for the backward pass, float32 [members, rows]
     rstd_next: Optional[torch.Tensor]
 
 
@@ -134,117 +136,146 @@ class BlockNormGrads(NamedTuple):
 
 def _norm_desc(x, block, post_weight, gate, scale, next_weight):
     """The description of the inputs that both directions share; x stands for y in the backward pass."""
-    _require(x.is_cuda and x.dim() == 3 and x.dtype in _TYPES, "activations are CUDA tensors [members, rows, width], float32 or bfloat16")
-    m, rows, width = x.shape
+    if not (x.is_cuda and x.dim() == 3 and x.dtype in _TYPES):
+        raise ValueError("activations are CUDA tensors [members, rows, width], float32 or bfloat16")
+    shape = x.shape
+    m, rows, width = shape
     d = PbtBlockNormDesc()
     d.members, d.rows, d.width, d.dtype = m, rows, width, _TYPES[x.dtype]
-    d.x, d.x_member, d.x_row = _activation(x, x, "x")
+    d.x, d.x_member, d.x_row = _activation(x, x, shape, "x")
     if block is not None:
-        _require(post_weight is not None, "a block output needs post_weight")
-        d.block, d.block_member, d.block_row = _activation(block, x, "block")
+        if post_weight is None:
+            raise ValueError("a block output needs post_weight")
+        d.block, d.block_member, d.block_row = _activation(block, x, shape, "block")
         d.post_weight = _weight(post_weight, x, (m, width), "post_weight")
         if gate is not None:
             if gate.dim() == 2:
-                _require(gate.shape == (m, width) and gate.dtype == x.dtype and gate.device == x.device and gate.stride(1) == 1,
-                         "a gate vector is [members, width] of the activations' type")
+                _require(gate.shape == (m, width) and gate.dtype == x.dtype and gate.device == x.device
+                         and (gate.stride(1) == 1 or width == 1), "a gate vector is [members, width] of the activations' type")
                 d.gate, d.gate_member, d.gate_vector = gate.data_ptr(), gate.stride(0), 1
             else:
-                d.gate, d.gate_member, d.gate_row = _activation(gate, x, "gate")
+                d.gate, d.gate_member, d.gate_row = _activation(gate, x, shape, "gate")
         if scale is not None:
             d.scale = _weight(scale, x, (m,), "scale")
     else:
         _require(post_weight is None and gate is None and scale is None, "post_weight, gate and scale belong to a block output")
     if next_weight is not None:
         d.next_weight = _weight(next_weight, x, (m, width), "next_weight")
-    return d
+    return d, shape
 
 
-def _activation(t, like, name):
-    _require(t.shape == like.shape and t.dtype == like.dtype and t.device == like.device and (t.stride(2) == 1 or t.shape[2] == 1),
-             f"{name} has to have the activations' shape, type and device, with contiguous columns")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+def _activation(t, like, shape, name):
+    if t.shape != shape or t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{name} has to have the activations' shape, type and device")
+    member, row, column = t.stride()
+    if column != 1 and shape[2] != 1:
+        raise ValueError(f"{name} has to have contiguous columns")
+    return t.data_ptr(), member, row
 
 
 def _weight(t, like, shape, name):
-    _require(t.dtype == torch.float32 and t.shape == shape and t.device == like.device and t.is_contiguous(),
-             f"{name} has to be a contiguous float32 tensor {list(shape)} on the activations' device")
+    if t.shape != shape or t.dtype is not torch.float32 or t.device != like.device or not t.is_contiguous():
+        raise ValueError(f"{name} has to be a contiguous float32 tensor {list(shape)} on the activations' device")
     return t.data_ptr()
 
 
 def block_norm_forward(x, block=None, *, post_weight=None, gate=None, scale=None, next_weight=None, eps: float = 1e-6,
-                       stream=None) -> BlockNormOut:
+                       keep: bool = False, stream=None) -> BlockNormOut:
     """Norms before and after a residual block with its gate and residual scale (pbt_block_norm_forward):
     y = x + scale sigmoid(gate) rms(block) post_weight, u = rms(y) next_weight.
 
     x, block: [members, rows, width]; post_weight, next_weight: float32 [members, width]; gate: logits, one per element or
     [members, width], or None; scale: float32 [members] or None.  Without `block`, only u from x; without `next_weight`,
-    only y."""
-    _require(block is not None or next_weight is not None, "nothing to compute: neither a block output nor a next norm")
-    d = _norm_desc(x, block, post_weight, gate, scale, next_weight)
+    only y.  With `keep`, also the reciprocal roots that the backward pass takes."""
+    if block is None and next_weight is None:
+        raise ValueError("nothing to compute: neither a block output nor a next norm")
+    d, shape = _norm_desc(x, block, post_weight, gate, scale, next_weight)
     d.eps = eps
-    m, rows, width = x.shape
+    return _on(x.device, stream, (x, block, post_weight, gate, scale, next_weight), _norm_forward, d, shape, x, block is not None,
+               next_weight is not None, keep)
+
+
+def _norm_forward(s, d, shape, x, block, nxt, keep):
     y, u, rb, rn = x, None, None, None
-    with _On(x.device, stream, (x, block, post_weight, gate, scale, next_weight)) as s:
-        if block is not None:
-            y = torch.empty((m, rows, width), dtype=x.dtype, device=x.device)
-            rb = torch.empty((m, rows), dtype=torch.float32, device=x.device)
-            d.y, d.rstd_block = y.data_ptr(), rb.data_ptr()
-        if next_weight is not None:
-            u = torch.empty((m, rows, width), dtype=x.dtype, device=x.device)
-            rn = torch.empty((m, rows), dtype=torch.float32, device=x.device)
-            d.u, d.rstd_next = u.data_ptr(), rn.data_ptr()
-        if rows:                        # (tensors without elements have no address to hand over)
-            _check(load_library().pbt_block_norm_forward(C.byref(d), s))
+    if block:
+        y = torch.empty(shape, dtype=x.dtype, device=x.device)
+        d.y = y.data_ptr()
+        if keep:
+            rb = torch.empty(shape[:2], dtype=torch.float32, device=x.device)
+            d.rstd_block = rb.data_ptr()
+    if nxt:
+        u = torch.empty(shape, dtype=x.dtype, device=x.device)
+        d.u = u.data_ptr()
+        if keep:
+            rn = torch.empty(shape[:2], dtype=torch.float32, device=x.device)
+            d.rstd_next = rn.data_ptr()
+    if d.rows:                              # (tensors without elements have no address to hand over)
+        rc = load_library().pbt_block_norm_forward(C.byref(d), s)
+        if rc:
+            _check(rc)
     return BlockNormOut(y, u, rb, rn)
 
 
 def block_norm_backward(dy, du, y, block=None, *, post_weight=None, gate=None, scale=None, next_weight=None,
                         rstd_block=None, rstd_next=None, stream=None) -> BlockNormGrads:
     """Gradients of block_norm_forward from dy (the residual stream's, or None) and du (None without a next norm), with
-    the forward pass's y and reciprocal roots."""
+    the y and the reciprocal roots of a forward pass that kept them."""
     _require(du is not None or block is not None, "nothing to differentiate: neither du nor a block output")
     _require((du is None) == (next_weight is None), "du and next_weight belong together")
-    d = _norm_desc(y, block, post_weight, gate, scale, next_weight)
-    m, rows, width = y.shape
+    d, shape = _norm_desc(y, block, post_weight, gate, scale, next_weight)
     if dy is not None:
-        d.dy, d.dy_member, d.dy_row = _activation(dy, y, "dy")
+        d.dy, d.dy_member, d.dy_row = _activation(dy, y, shape, "dy")
     if du is not None:
-        d.du, d.du_member, d.du_row = _activation(du, y, "du")
-        _require(rstd_next is not None, "rstd_next is what the forward pass returned")
-        d.rstd_next = _weight(rstd_next, y, (m, rows), "rstd_next")
+        d.du, d.du_member, d.du_row = _activation(du, y, shape, "du")
+        _require(rstd_next is not None, "rstd_next is what the forward pass kept")
+        d.rstd_next = _weight(rstd_next, y, shape[:2], "rstd_next")
     if block is not None:
-        _require(rstd_block is not None, "rstd_block is what the forward pass returned")
-        d.rstd_block = _weight(rstd_block, y, (m, rows), "rstd_block")
-    lib = load_library()
-    nbytes = C.c_size_t(0)
-    dblock = dgate = dpost = dnext = dscale = None
+        _require(rstd_block is not None, "rstd_block is what the forward pass kept")
+        d.rstd_block = _weight(rstd_block, y, shape[:2], "rstd_block")
     inputs = (dy, du, y, block, post_weight, gate, scale, next_weight, rstd_block, rstd_next)
-    with _On(y.device, stream, inputs) as s:
-        dx = torch.empty((m, rows, width), dtype=y.dtype, device=y.device)
-        d.dx = dx.data_ptr()
-        if block is not None:
-            dblock = torch.empty((m, rows, width), dtype=y.dtype, device=y.device)
-            dpost = torch.empty((m, width), dtype=torch.float32, device=y.device)
-            dscale = torch.empty((m,), dtype=torch.float32, device=y.device)
-            d.dblock, d.dpost_weight, d.dscale = dblock.data_ptr(), dpost.data_ptr(), dscale.data_ptr()
-            if gate is not None:
-                dgate = torch.empty(gate.shape, dtype=y.dtype, device=y.device)
-                d.dgate = dgate.data_ptr()
-        if du is not None:
-            dnext = torch.empty((m, width), dtype=torch.float32, device=y.device)
-            d.dnext_weight = dnext.data_ptr()
-        if rows:
-            _check(lib.pbt_block_norm_query_workspace(C.byref(d), C.byref(nbytes)))
-            ws = _workspace(nbytes.value, y.device)
-            _check(lib.pbt_block_norm_backward(C.byref(d), ws.data_ptr(), nbytes.value, s))
-        else:                           # no row contributes: the sums over rows are zero
-            for t in (dpost, dscale, dnext, dgate):
-                if t is not None:
-                    t.zero_()
-    return BlockNormGrads(dx, dblock, dgate, dpost, dnext, dscale if scale is not None else None)
+    return _on(y.device, stream, inputs, _norm_backward, d, shape, y, gate, block is not None, du is not None, scale is not None)
+
+
+def _norm_backward(s, d, shape, y, gate, block, nxt, scaled):
+    lib, dtype, device = load_library(), y.dtype, y.device
+    vector = (shape[0], shape[2])
+    dblock = dgate = dpost = dnext = dscale = None
+    dx = torch.empty(shape, dtype=dtype, device=device)
+    d.dx = dx.data_ptr()
+    if block:
+        dblock = torch.empty(shape, dtype=dtype, device=device)
+        dpost = torch.empty(vector, dtype=torch.float32, device=device)
+        d.dblock, d.dpost_weight = dblock.data_ptr(), dpost.data_ptr()
+        if scaled:
+            dscale = torch.empty(shape[0], dtype=torch.float32, device=device)
+            d.dscale = dscale.data_ptr()
+        if gate is not None:
+            dgate = torch.empty(gate.shape, dtype=dtype, device=device)
+            d.dgate = dgate.data_ptr()
+    if nxt:
+        dnext = torch.empty(vector, dtype=torch.float32, device=device)
+        d.dnext_weight = dnext.data_ptr()
+    if d.rows:
+        nbytes = C.c_size_t(0)
+        _check(lib.pbt_block_norm_query_workspace(C.byref(d), C.byref(nbytes)))
+        ws = _workspace(nbytes.value, device)
+        _check(lib.pbt_block_norm_backward(C.byref(d), ws.data_ptr(), nbytes.value, s))
+    else:                                   # no row contributes: the sums over rows are zero
+        for t in (dpost, dscale, dnext, dgate):
+            if t is not None:
+                t.zero_()
+    return BlockNormGrads(dx, dblock, dgate, dpost, dnext, dscale)
 
 
 # --- adapters --------------------------------------------------------------------------------------------------------------
+
+
+def _row_stride(t, name):
+    row, column = t.stride()
+    columns = t.shape[1]
+    if column != 1 and columns != 1:
+        raise ValueError(f"{name} has to have contiguous columns")
+    return row if t.shape[0] > 1 else max(row, columns)      # (a single row may carry any stride)
 
 
 class AdapterProjection:
@@ -283,48 +314,53 @@ class AdapterProjection:
     def _call(self, x, row_offsets, adapter_ids):
         """The description of a call on these rows (a copy: calls from several threads do not share it)."""
         w = self.weight
-        _require(x.dim() == 2 and x.shape[1] == w.shape[1] and x.dtype == w.dtype and x.device == w.device and (x.stride(1) == 1 or x.shape[1] == 1),
-                 "x is [rows, inputs] of the weight's type and device, with contiguous columns")
+        device = w.device
+        if not (x.dim() == 2 and x.shape[1] == self._desc.inputs and x.dtype == w.dtype and x.device == device):
+            raise ValueError("x is [rows, inputs] of the weight's type and device")
         n = adapter_ids.numel()
-        _require(row_offsets.dtype == torch.int32 and adapter_ids.dtype == torch.int32 and row_offsets.numel() == n + 1
-                 and row_offsets.device == w.device and adapter_ids.device == w.device and row_offsets.is_contiguous() and adapter_ids.is_contiguous(),
-                 "row_offsets [segments + 1] and adapter_ids [segments] are contiguous int32 tensors on the weight's device")
+        if not (row_offsets.dtype is torch.int32 and adapter_ids.dtype is torch.int32 and row_offsets.numel() == n + 1 and row_offsets.device == device
+                and adapter_ids.device == device and row_offsets.is_contiguous() and adapter_ids.is_contiguous()):
+            raise ValueError("row_offsets [segments + 1] and adapter_ids [segments] are contiguous int32 tensors on the weight's device")
         d = PbtAdapterDesc.from_buffer_copy(self._desc)
         d.rows, d.n_segments = x.shape[0], n
         d.row_offsets, d.adapter_ids = row_offsets.data_ptr(), adapter_ids.data_ptr()
-        d.x, d.ld_x = x.data_ptr(), max(x.stride(0), x.shape[1])
+        d.x, d.ld_x = x.data_ptr(), _row_stride(x, "x")
         return d
 
     def forward(self, x, row_offsets, adapter_ids, keep: bool = False, stream=None):
         """y = x W^T + bias + scale_a (x A_a^T) B_a^T; with keep, also S = x A_a^T (float32 [rows, rank], defined for the
         rows that have an adapter), which the backward pass takes."""
         d, w = self._call(x, row_offsets, adapter_ids), self.weight
-        with _On(w.device, stream, (x, row_offsets, adapter_ids, w, self.A, self.B, self.scale, self.bias)) as s:
-            y = torch.empty((x.shape[0], w.shape[0]), dtype=w.dtype, device=w.device)
-            d.y, d.ld_y = y.data_ptr(), w.shape[0]
-            kept = None
-            if keep:
-                kept = torch.empty((x.shape[0], d.rank), dtype=torch.float32, device=w.device)
-                d.s = kept.data_ptr()
-            if x.shape[0]:
-                self._run(d, 0, self.lib.pbt_adapter_forward, s)
+        return _on(w.device, stream, (x, row_offsets, adapter_ids, w, self.A, self.B, self.scale, self.bias), self._forward, d, keep)
+
+    def _forward(self, s, d, keep):
+        w = self.weight
+        y = torch.empty((d.rows, d.outputs), dtype=w.dtype, device=w.device)
+        d.y, d.ld_y = y.data_ptr(), d.outputs
+        kept = None
+        if keep:
+            kept = torch.empty((d.rows, d.rank), dtype=torch.float32, device=w.device)
+            d.s = kept.data_ptr()
+        if d.rows:
+            self._run(d, 0, self.lib.pbt_adapter_forward, s)
         return (y, kept) if keep else y
 
     def backward(self, dy, x, kept, row_offsets, adapter_ids, stream=None):
         """(dx, dA, dB) from dy [rows, outputs], the forward pass's x and what it kept; dA and dB are float32."""
         d, w = self._call(x, row_offsets, adapter_ids), self.weight
-        rows = x.shape[0]
-        _require(dy.shape == (rows, w.shape[0]) and dy.dtype == w.dtype and dy.device == w.device and (dy.stride(1) == 1 or dy.shape[1] == 1),
-                 "dy is [rows, outputs] of the weight's type and device, with contiguous columns")
-        _require(kept.shape == (rows, d.rank) and kept.dtype == torch.float32 and kept.device == w.device and kept.is_contiguous(),
+        _require(dy.shape == (d.rows, d.outputs) and dy.dtype == w.dtype and dy.device == w.device, "dy is [rows, outputs] of the weight's type and device")
+        _require(kept.shape == (d.rows, d.rank) and kept.dtype is torch.float32 and kept.device == w.device and kept.is_contiguous(),
                  "kept is what forward(keep=True) returned")
-        d.dy, d.ld_dy, d.s = dy.data_ptr(), max(dy.stride(0), dy.shape[1]), kept.data_ptr()
-        with _On(w.device, stream, (x, dy, kept, row_offsets, adapter_ids, w, self.A, self.B, self.scale)) as s:
-            dx = torch.empty((rows, w.shape[1]), dtype=w.dtype, device=w.device)
-            d_a = torch.empty(self.A.shape, dtype=torch.float32, device=w.device)
-            d_b = torch.empty(self.B.shape, dtype=torch.float32, device=w.device)
-            d.dx, d.ld_dx, d.dA, d.dB = dx.data_ptr(), w.shape[1], d_a.data_ptr(), d_b.data_ptr()
-            self._run(d, 1, self.lib.pbt_adapter_backward, s)
+        d.dy, d.ld_dy, d.s = dy.data_ptr(), _row_stride(dy, "dy"), kept.data_ptr()
+        return _on(w.device, stream, (x, dy, kept, row_offsets, adapter_ids, w, self.A, self.B, self.scale), self._backward, d)
+
+    def _backward(self, s, d):
+        w = self.weight
+        dx = torch.empty((d.rows, d.inputs), dtype=w.dtype, device=w.device)
+        d_a = torch.empty((d.n_adapters, d.rank, d.inputs), dtype=torch.float32, device=w.device)
+        d_b = torch.empty((d.n_adapters, d.outputs, d.rank), dtype=torch.float32, device=w.device)
+        d.dx, d.ld_dx, d.dA, d.dB = dx.data_ptr(), d.inputs, d_a.data_ptr(), d_b.data_ptr()
+        self._run(d, 1, self.lib.pbt_adapter_backward, s)
         return dx, d_a, d_b
 
     def check(self):
@@ -335,7 +371,10 @@ class AdapterProjection:
             raise PbtError(code, "a bounded wait inside an adapter kernel ran out")
 
     def _run(self, d, backward, call, s):
-        nbytes = C.c_size_t(0)
-        _check(self.lib.pbt_adapter_query_workspace(C.byref(d), backward, C.byref(nbytes)))
-        ws = _workspace(nbytes.value, self.weight.device)
-        _check(call(C.byref(d), ws.data_ptr(), nbytes.value, s))
+        nbytes, at = C.c_size_t(0), C.byref(d)
+        rc = self.lib.pbt_adapter_query_workspace(at, backward, C.byref(nbytes))
+        if not rc:
+            ws = _workspace(nbytes.value, self.weight.device)
+            rc = call(at, ws.data_ptr(), nbytes.value, s)
+        if rc:
+            _check(rc)

@@ -89,7 +89,7 @@ def test_forward_and_backward_match_the_formulas(shape, gate, dtype):
             continue
         d, dy, du = _inputs(m, rows, width, dtype, gate, seed=sum(shape) + pad, pad=pad, block=block, nxt=nxt)
         kw = {k: d[k] for k in ("post_weight", "gate", "scale", "next_weight")}
-        out = pbt.block_norm_forward(d["x"], d["block"], eps=eps, **kw)
+        out = pbt.block_norm_forward(d["x"], d["block"], eps=eps, keep=True, **kw)
         want_y, want_u = _formula(_double(d), eps)
         if block:
             _close(out.y, want_y)
@@ -97,6 +97,8 @@ def test_forward_and_backward_match_the_formulas(shape, gate, dtype):
             assert torch.allclose(out.rstd_block.cpu().double(), r, rtol=VALUE)
         else:
             assert out.y is d["x"]
+        plain = pbt.block_norm_forward(d["x"], d["block"], eps=eps, **kw)
+        assert torch.equal(plain.y, out.y) and (plain.u is None or torch.equal(plain.u, out.u)) and plain.rstd_block is plain.rstd_next is None
         if nxt:
             _close(out.u, want_u)
             r = (want_y.square().mean(-1) + eps).rsqrt()
@@ -197,7 +199,7 @@ def test_backward_agrees_with_differences_of_the_forward_pass(gate):
 
     def run(e):
         kw = {k: e[k] for k in ("post_weight", "gate", "scale", "next_weight")}
-        return pbt.block_norm_forward(e["x"], e["block"], **kw), kw
+        return pbt.block_norm_forward(e["x"], e["block"], keep=True, **kw), kw
 
     def loss(e):
         out, _ = run(e)
@@ -231,7 +233,7 @@ def test_a_diverged_row_stays_in_its_row_and_member():
     dirty["x"][1, 4, 0] = float("inf")
     dirty["gate"][0, 3, :] = float("-inf")          # a closed gate: y is x there, exactly
     kd = {k: dirty[k] for k in kw}
-    out = pbt.block_norm_forward(dirty["x"], dirty["block"], **kd)
+    out = pbt.block_norm_forward(dirty["x"], dirty["block"], keep=True, **kd)
     assert torch.equal(out.y[0, 3], d["x"][0, 3])
     ok = torch.ones(3, 8, dtype=torch.bool)
     ok[1, 2] = ok[1, 4] = ok[0, 3] = False
@@ -249,14 +251,14 @@ def test_zero_rows_and_rows_of_zeros():
     import paper_1711_09846_b200 as pbt
     d, dy, du = _inputs(2, 0, 64, "float32", "vector", seed=1)
     kw = {k: d[k] for k in ("post_weight", "gate", "scale", "next_weight")}
-    out = pbt.block_norm_forward(d["x"], d["block"], **kw)
+    out = pbt.block_norm_forward(d["x"], d["block"], keep=True, **kw)
     assert out.y.shape == (2, 0, 64) and out.u.shape == (2, 0, 64)
     g = pbt.block_norm_backward(dy, du, out.y, d["block"], rstd_block=out.rstd_block, rstd_next=out.rstd_next, **kw)
     for t in (g.dgate, g.dpost_weight, g.dnext_weight, g.dscale):
         assert (t == 0).all()
     z = torch.zeros(1, 2, 64, device="cuda")
     w = torch.ones(1, 64, device="cuda")
-    out = pbt.block_norm_forward(z, z, post_weight=w, next_weight=w)
+    out = pbt.block_norm_forward(z, z, post_weight=w, next_weight=w, keep=True)
     assert (out.y == 0).all() and (out.u == 0).all() and torch.allclose(out.rstd_next, torch.full((1, 2), 1e3, device="cuda"))
 
 
@@ -266,11 +268,11 @@ def test_another_stream_gives_the_same_bits():
     import paper_1711_09846_b200 as pbt
     d, dy, du = _inputs(3, 50, 512, "bfloat16", "full", seed=4)
     kw = {k: d[k] for k in ("post_weight", "gate", "scale", "next_weight")}
-    out = pbt.block_norm_forward(d["x"], d["block"], **kw)
+    out = pbt.block_norm_forward(d["x"], d["block"], keep=True, **kw)
     g = pbt.block_norm_backward(dy, du, out.y, d["block"], rstd_block=out.rstd_block, rstd_next=out.rstd_next, **kw)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
-    out2 = pbt.block_norm_forward(d["x"], d["block"], stream=side, **kw)
+    out2 = pbt.block_norm_forward(d["x"], d["block"], stream=side, keep=True, **kw)
     g2 = pbt.block_norm_backward(dy, du, out2.y, d["block"], rstd_block=out2.rstd_block, rstd_next=out2.rstd_next, stream=side, **kw)
     torch.cuda.current_stream().wait_stream(side)
     for a, b in zip((*out, *g), (*out2, *g2)):
