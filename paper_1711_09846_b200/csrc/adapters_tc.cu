@@ -4,6 +4,8 @@
 //                      one (64-row tile, segment) pair per CTA, mma.sync fed by 16-byte loads straight from global memory
 //   k_adapter_gemm     y = x W^T + bias + c S B_a^T (or dx = dy W + dS A_a): the shared product on tcgen05, with the
 //                      low-rank product as one more block of the same contraction in the same TMEM accumulator
+//   k_adapter_rows     the same product for a few rows (one token of many requests): bound by reading W once, mma.sync
+//                      with W's rows as the tall operand, low-rank part in fp32 at the end
 //   k_adapter_grad     dA_a = dS^T x, dB_a = dy^T (c S): contractions over an adapter's rows on tcgen05, r columns wide
 //
 // Segments and tiles.  Output tiles are 128 consecutive rows whatever the segments; for every segment that reaches into
@@ -54,6 +56,8 @@ struct ShrinkArgs {
   Segments segs;
   int n_tiles;
   float* s;                           // fp32 result, not scaled (may be null)
+  float* scaled;                      // scaled fp32 result [rows][rank], for k_adapter_rows (null: planes instead)
+  int* row_adapter;                   // adapter of every row or -1, for k_adapter_rows
   bf16* planes; int terms;            // scaled result as `terms` bf16 summands side by side, [rows][terms * rp]
   const float* kept; bf16* kept_planes;   // a second fp32 matrix [rows][rank], split into three summands the same way
   int* tile_seg; int tile_rows, n_table;  // first segment of every output tile of the product that follows
@@ -89,12 +93,16 @@ __device__ __forceinline__ void store_terms(bf16* row, int rp, int col, float v,
 template <bool TRANS, int NT>
 __global__ void __launch_bounds__(256) k_adapter_shrink(const ShrinkArgs a) {
   pdl_prologue();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (k_adapter_rows may begin with its own operand)
   extern __shared__ __align__(16) uint8_t shrink_smem[];
   const int q = blockIdx.x, tid = threadIdx.x;
   const Segments& g = a.segs;
   if (q >= a.n_tiles + g.n) {
     const int i = (q - a.n_tiles - g.n) * 256 + tid;
-    if (i < a.n_table) a.tile_seg[i] = max(segment_of_row(g, i * a.tile_rows), 0);
+    if (i >= a.n_table) return;
+    const int row = i * a.tile_rows, j = segment_of_row(g, row);
+    if (a.row_adapter) a.row_adapter[i] = j >= 0 && row < segment_begin(g, j + 1) ? segment_adapter(g, j) : -1;
+    else a.tile_seg[i] = max(j, 0);
     return;
   }
   // The pairs (tile t, segment j) that meet ascend in t + j by at least one, so q = t + j names at most one of them: j is
@@ -199,7 +207,9 @@ __global__ void __launch_bounds__(256) k_adapter_shrink(const ShrinkArgs a) {
     if (c < a.rank) {
       for (int p = 0; p < parts; ++p) v += red[(((r >> 5) * parts + p) * 32 + (r & 31)) * (NT * 8) + c];
       if (a.s) a.s[row * a.rank + c] = v;
+      if (a.scaled) a.scaled[row * a.rank + c] = f * v;
     }
+    if (!a.planes) continue;
     store_terms(a.planes + row * width, a.rp, c, f * v, a.terms);
     if (a.kept) store_terms(a.kept_planes + row * 3 * a.rp, a.rp, c, c < a.rank ? f * a.kept[row * a.rank + c] : 0.f, 3);
   }
@@ -489,6 +499,108 @@ cudaError_t launch_gemm(const GemmCall& c, const Segments& segs, const int* tile
 }
 
 // ------------------------------------------------------------------------------------------------------------------
+// Few rows
+// ------------------------------------------------------------------------------------------------------------------
+constexpr int kRowsMost = 64;
+constexpr int kRowsOut = 16;      // output columns of a CTA
+
+struct RowsArgs {
+  const bf16* x; long long ldx;
+  const bf16* w; long long ldw;
+  const bf16* B; int pitch;       // [adapters][N][pitch]
+  const float* bias; const float* scaled; const int* row_adapter;
+  bf16* y; long long ldy;
+  int T, N, K, rank;
+};
+
+// y[t][n] for 16 columns n and all rows t: the eight warps take every eighth block of 64 inputs, W's rows are the tall
+// operand of mma.sync (16 x 16), eight rows of x the narrow one, both loaded in 16-byte pieces straight into fragments
+// (the order of the contraction index is the one the loads deliver, as in the shrink).  The warps' sums meet in shared
+// memory, where the low-rank part is added in fp32.  Launched while the shrink runs: only that last part waits for it.
+template <int GROUPS>
+__global__ void __launch_bounds__(256) k_adapter_rows(const RowsArgs a) {
+  __shared__ float red[8][kRowsOut][GROUPS * 8 + 1];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gr = lane >> 2, tq = lane & 3;
+  const int n0 = blockIdx.x * kRowsOut;
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  float acc[GROUPS][4] = {};
+  const bf16* w0 = a.w + (long long)(n0 + gr) * a.ldw + tq * 8;
+  const bf16* w1 = w0 + 8 * a.ldw;
+  const bool in0 = n0 + gr < a.N, in1 = n0 + gr + 8 < a.N;
+  for (int k0 = warp * 64; k0 < a.K; k0 += 512) {
+    uint4 wv[2][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bool in = k0 + h * 32 + tq * 8 < a.K;
+      wv[0][h] = in && in0 ? ld16(w0 + k0 + h * 32) : zero;
+      wv[1][h] = in && in1 ? ld16(w1 + k0 + h * 32) : zero;
+    }
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+      const int t = g * 8 + gr;
+      float sum[4] = {};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int k = k0 + h * 32 + tq * 8;
+        const uint4 xv = t < a.T && k < a.K ? __ldg(reinterpret_cast<const uint4*>(a.x + t * a.ldx + k)) : zero;
+        mma16816(sum, wv[0][h].x, wv[1][h].x, wv[0][h].y, wv[1][h].y, xv.x, xv.y);
+        mma16816(sum, wv[0][h].z, wv[1][h].z, wv[0][h].w, wv[1][h].w, xv.z, xv.w);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[g][e] += sum[e];
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) red[warp][gr + 8 * (e >> 1)][g * 8 + tq * 2 + (e & 1)] = acc[g][e];
+  __syncthreads();
+  asm volatile("griddepcontrol.wait;" ::: "memory");     // the shrink is complete and its results are visible
+  for (int i = threadIdx.x; i < a.T * kRowsOut; i += 256) {
+    const int t = i / kRowsOut, n = i % kRowsOut, col = n0 + n;
+    if (col >= a.N) continue;
+    float v = a.bias ? __ldg(a.bias + col) : 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v += red[k][n][t];
+    const int adapter = __ldcg(a.row_adapter + t);
+    if (adapter >= 0) {
+      const bf16* b = a.B + ((long long)adapter * a.N + col) * a.pitch;
+      const float* s = a.scaled + t * a.rank;
+      for (int j = 0; j < a.rank; j += 8) {
+        const uint4 bv = __ldg(reinterpret_cast<const uint4*>(b + j));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t pairs = word(bv, e >> 1);
+          if (j + e < a.rank) v = __fmaf_rn(__uint_as_float((e & 1) ? pairs & 0xFFFF0000u : pairs << 16), __ldcg(s + j + e), v);
+        }
+      }
+    }
+    a.y[t * a.ldy + col] = __float2bfloat16_rn(v);
+  }
+}
+
+template <int GROUPS>
+cudaError_t launch_rows(const RowsArgs& a, cudaStream_t s) {
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = dim3((a.N + kRowsOut - 1) / kRowsOut);
+  cfg.blockDim = dim3(256);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k_adapter_rows<GROUPS>, a);
+}
+cudaError_t launch_rows(const RowsArgs& a, cudaStream_t s) {
+  if (a.T <= 8) return launch_rows<1>(a, s);
+  if (a.T <= 16) return launch_rows<2>(a, s);
+  if (a.T <= 32) return launch_rows<4>(a, s);
+  return launch_rows<8>(a, s);
+}
+
+// ------------------------------------------------------------------------------------------------------------------
 // Gradients of the adapters
 // ------------------------------------------------------------------------------------------------------------------
 constexpr int kGradStages = 4, kGradChunk = 512, kGradList = 1024;
@@ -707,6 +819,7 @@ bool aligned(const void* p, long long ld) { return ((uintptr_t)p & 15) == 0 && l
 
 struct Plan {
   int rp, splits;
+  bool few;      // rows that k_adapter_rows takes
   bool pack_x, pack_w, pack_a, pack_b, pack_dy;
   size_t x, w, a, b, dy, planes, kept, table, parts, total;
 };
@@ -716,7 +829,7 @@ Plan plan(const pbt_adapter_desc* d, bool backward) {
   const size_t rows = (size_t)d->rows;
   p.rp = round_up(d->rank, 16);
   p.pack_x = !aligned(d->x, d->ld_x) || d->inputs % 8;     // (vector loads end with the row)
-  p.pack_w = !aligned(d->weight, d->ld_weight);
+  p.pack_w = !aligned(d->weight, d->ld_weight) || (!backward && d->rows <= kRowsMost && d->inputs % 8);
   p.pack_a = !aligned(d->A, d->inputs);
   p.pack_b = !aligned(d->B, d->rank);
   p.pack_dy = backward && (!aligned(d->dy, d->ld_dy) || d->outputs % 8);
@@ -734,9 +847,10 @@ Plan plan(const pbt_adapter_desc* d, bool backward) {
   p.a = take(p.pack_a, (size_t)d->n_adapters * d->rank * round_up(d->inputs, 8) * 2);
   p.b = take(p.pack_b, (size_t)d->n_adapters * d->outputs * round_up(d->rank, 8) * 2);
   p.dy = take(p.pack_dy, rows * round_up(d->outputs, 8) * 2);
-  p.planes = take(true, rows * p.rp * 2 * (backward ? 3 : 1));
+  p.few = !backward && d->rows <= kRowsMost;
+  p.planes = take(true, p.few ? rows * d->rank * sizeof(float) : rows * p.rp * 2 * (backward ? 3 : 1));
   p.kept = take(backward, rows * p.rp * 2 * 3);
-  p.table = take(true, ((rows + kBM - 1) / kBM) * sizeof(int));
+  p.table = take(true, (p.few ? rows : (rows + kBM - 1) / kBM) * sizeof(int));
   p.parts = take(backward && p.splits > 1, (size_t)p.splits * d->n_adapters * d->rank * ((size_t)d->inputs + d->outputs) * sizeof(float));
   p.total = std::max<size_t>(at, 256);
   return p;
@@ -771,7 +885,16 @@ cudaError_t tc_forward(const pbt_adapter_desc* d, const Segments& segs, char* ws
   a.x = (const bf16*)x; a.ldx = ldx; a.K = d->inputs;
   a.mats = (const bf16*)A; a.pitch = (int)lda; a.rank = d->rank; a.rp = p.rp;
   a.scale = d->scale; a.segs = segs;
-  a.s = d->s; a.planes = (bf16*)(ws + p.planes); a.terms = 1;
+  a.s = d->s;
+  if (p.few) {
+    a.scaled = (float*)(ws + p.planes);
+    a.row_adapter = (int*)(ws + p.table); a.tile_rows = 1; a.n_table = d->rows;
+    STEP(launch_shrink<false>(a, st));
+    const RowsArgs r = {(const bf16*)x, ldx, (const bf16*)w, ldw, (const bf16*)B, (int)ldb, d->bias, a.scaled, a.row_adapter, (bf16*)d->y, d->ld_y,
+                        d->rows, d->outputs, d->inputs, d->rank};
+    return launch_rows(r, st);
+  }
+  a.planes = (bf16*)(ws + p.planes); a.terms = 1;
   a.tile_seg = (int*)(ws + p.table); a.tile_rows = kBM; a.n_table = (d->rows + kBM - 1) / kBM;
   STEP(launch_shrink<false>(a, st));
   const GemmCall c = {(const bf16*)x, ldx, (const bf16*)w, ldw, 0, a.planes, p.rp, p.rp, (const bf16*)B, (int)ldb, d->rank, d->y, d->ld_y, d->bias, d->outputs, d->inputs};

@@ -189,10 +189,10 @@ __device__ __forceinline__ void copy_ahead(void* slot, const void* from) {
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-template <typename T, int V, int ITEMS, int ARRAYS, int STAGES>
+template <typename T, int V, int ITEMS, int ARRAYS, int STAGES, int THREADS>
 struct RowRing {
   typedef typename Vec<T, V>::Raw Raw;
-  uint4* slots;      // this thread's; its vectors are blockDim.x apart
+  uint4* slots;      // this thread's; its vectors are THREADS apart
   const T* base[ARRAYS];
   long long member[ARRAYS], row[ARRAYS];
   bool have[ARRAYS];
@@ -205,7 +205,7 @@ struct RowRing {
     row[k] = t.row;
     have[k] = used;
   }
-  __device__ __forceinline__ uint4* at(int s, int k, int j) const { return slots + ((s * ARRAYS + k) * ITEMS + j) * (int)blockDim.x; }
+  __device__ __forceinline__ uint4* at(int s, int k, int j) const { return slots + s * (ARRAYS * ITEMS * THREADS) + (k * ITEMS + j) * THREADS; }
   // ask for the next row (for nothing behind the last one) into stage s
   __device__ __forceinline__ void ask(int s) {
     if constexpr (V > 1) {
@@ -230,24 +230,19 @@ struct RowRing {
   __device__ __forceinline__ void wait() const {
     if constexpr (V > 1) copy_wait<STAGES - 1>();
   }
-  // vector j of array k of row (m, i), which stage s holds; zeros where there is none
+  // vector j of array k (which there is) of row (m, i), which stage s holds; the vector lies inside the row
   template <typename L>
   __device__ __forceinline__ void get(int m, int i, int s, int k, int j, L* f) const {
-    const int e = slot + j * step;
-    Raw r = Vec<T, V>::zero();
-    if (have[k] && e < nv) {
-      if constexpr (V > 1) r = *reinterpret_cast<const Raw*>(at(s, k, j));
-      else r = Vec<T, V>::load(base[k] + m * member[k] + i * row[k] + e);
-    }
-    Vec<T, V>::unpack(r, f);
+    if constexpr (V > 1) Vec<T, V>::unpack(*reinterpret_cast<const Raw*>(at(s, k, j)), f);
+    else Vec<T, V>::unpack(Vec<T, V>::load(base[k] + m * member[k] + i * row[k] + slot + j * step), f);
   }
 };
 
-// Stages of a ring: what fits 80 KB (two blocks per SM) for blocks of 256 threads and 160 KB for larger ones, at most three
-// (a row that is worked on and two on their way).
+// Stages of a ring: what fits the block's share of an SM's shared memory (four forward blocks of 256 threads, two backward
+// ones, or one of 512), at most three (a row that is worked on and two on their way).
 template <int V, int ITEMS, int ARRAYS, int THREADS>
 __host__ __device__ constexpr int norm_stages() {
-  const int fit = (THREADS <= kNormThreads ? 80 : 160) * 1024 / (ARRAYS * ITEMS * 16 * THREADS);
+  const int fit = (THREADS > kNormThreads ? 160 : ARRAYS == 3 ? 50 : 100) * 1024 / (ARRAYS * ITEMS * 16 * THREADS);
   return V == 1 || fit < 1 ? 1 : fit > 3 ? 3 : fit;
 }
 
@@ -266,7 +261,7 @@ __global__ void __launch_bounds__(THREADS) k_norm_forward(const NormArgs a) {
   long long r = norm_first_row(a, g);
   const long long r_end = norm_first_row(a, g + 1);
   int m = (int)(r / a.rows), i = (int)(r % a.rows);
-  RowRing<T, V, ITEMS, 3, kStages> ring;
+  RowRing<T, V, ITEMS, 3, kStages, THREADS> ring;
   ring.slots = norm_ring + threadIdx.x;
   ring.slot = (warp % W) * 32 + lane; ring.step = W * 32; ring.nv = a.width / V; ring.rows = a.rows;
   ring.m = m; ring.i = i; ring.left = (int)(r_end - r);
@@ -281,11 +276,19 @@ __global__ void __launch_bounds__(THREADS) k_norm_forward(const NormArgs a) {
     ring.wait();
     L y[ITEMS][N];
 #pragma unroll
-    for (int k = 0; k < ITEMS; ++k) ring.get(m, i, stage, 0, k, y[k]);
+    for (int k = 0; k < ITEMS; ++k) {
+      if (ring.slot + k * ring.step < ring.nv) {
+        ring.get(m, i, stage, 0, k, y[k]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) y[k][j] = all<L>(0.f);
+      }
+    }
     if (block) {
       L s = all<L>(0.f);
 #pragma unroll
       for (int k = 0; k < ITEMS; ++k) {
+        if (ring.slot + k * ring.step >= ring.nv) continue;
         L b[N];
         ring.get(m, i, stage, 1, k, b);
 #pragma unroll
@@ -363,16 +366,17 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_no
   const int W = a.warps_per_row, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int group = warp / W, g = blockIdx.x * (blockDim.x / (W * 32)) + group;
   if (g >= a.groups) return;
-  const bool next = a.du.p != nullptr, block = a.block.p != nullptr, gate = a.gate.p != nullptr, vector = gate && a.gate_vector;
+  const bool has_dy = a.dy.p != nullptr, next = a.du.p != nullptr, block = a.block.p != nullptr;
+  const bool gate = a.gate.p != nullptr, vector = gate && a.gate_vector;
   long long r = norm_first_row(a, g);
   const long long r_end = norm_first_row(a, g + 1);
   int m = (int)(r / a.rows), i = (int)(r % a.rows);
   enum { kDy, kDu, kY, kBlock, kGate };
-  RowRing<T, V, ITEMS, 5, kStages> ring;
+  RowRing<T, V, ITEMS, 5, kStages, THREADS> ring;
   ring.slots = norm_ring + threadIdx.x;
   ring.slot = (warp % W) * 32 + lane; ring.step = W * 32; ring.nv = a.width / V; ring.rows = a.rows;
   ring.m = m; ring.i = i; ring.left = (int)(r_end - r);
-  ring.set(kDy, a.dy, a.dy.p != nullptr); ring.set(kDu, a.du, next); ring.set(kY, a.x, next);
+  ring.set(kDy, a.dy, has_dy); ring.set(kDu, a.du, next); ring.set(kY, a.x, next);
   ring.set(kBlock, a.block, block); ring.set(kGate, a.gate, gate);
 #pragma unroll
   for (int s = 0; s < kStages; ++s) ring.ask(s);
@@ -397,7 +401,9 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_no
       const int e = ring.slot + k * ring.step;
       if (e >= ring.nv) continue;
       L t[N], yh[N];      // dy + r_y dh
-      ring.get(m, i, stage, kDy, k, t);
+#pragma unroll
+      for (int j = 0; j < N; ++j) t[j] = all<L>(0.f);
+      if (has_dy) ring.get(m, i, stage, kDy, k, t);
       if (next) {
         L du[N], w[N];
         ring.get(m, i, stage, kDu, k, du);
@@ -439,7 +445,9 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_no
       const int e = ring.slot + k * ring.step;
       if (e >= ring.nv) continue;
       L dx[N];
-      ring.get(m, i, stage, kDy, k, dx);
+#pragma unroll
+      for (int j = 0; j < N; ++j) dx[j] = all<L>(0.f);
+      if (has_dy) ring.get(m, i, stage, kDy, k, dx);
       if (next) {
         L du[N], y[N], w[N];
         ring.get(m, i, stage, kDu, k, du);
@@ -670,7 +678,7 @@ cudaError_t launch_norm_backward(unsigned grid, int threads, const NormArgs& a, 
   int sms = 0;
   const cudaError_t e = tc::device_setup(&setup, k_norm_backward<T, V, ITEMS, THREADS>, per_thread * THREADS, &sms);
   if (e != cudaSuccess) return e;
-  return launch_with(grid, threads, per_thread * threads, s)(k_norm_backward<T, V, ITEMS, THREADS>, a);
+  return launch_with(grid, threads, per_thread * THREADS, s)(k_norm_backward<T, V, ITEMS, THREADS>, a);
 }
 template <typename T, int V, int ITEMS, int THREADS>
 cudaError_t launch_norm_forward(unsigned grid, int threads, const NormArgs& a, cudaStream_t s) {
@@ -679,7 +687,7 @@ cudaError_t launch_norm_forward(unsigned grid, int threads, const NormArgs& a, c
   int sms = 0;
   const cudaError_t e = tc::device_setup(&setup, k_norm_forward<T, V, ITEMS, THREADS>, per_thread * THREADS, &sms);
   if (e != cudaSuccess) return e;
-  return launch_with(grid, threads, per_thread * threads, s)(k_norm_forward<T, V, ITEMS, THREADS>, a);
+  return launch_with(grid, threads, per_thread * THREADS, s)(k_norm_forward<T, V, ITEMS, THREADS>, a);
 }
 // The instantiations that norm_shape can ask for: blocks of 512 threads belong to 16 elements a thread.
 template <typename T, int V, int ITEMS>

@@ -27,21 +27,32 @@ def _require(ok, message: str) -> None:
         raise ValueError(message)
 
 
+# The handle of a device's current stream; the public torch.cuda.current_stream builds a Python object around it, which
+# costs more than the rest of a small call's checks together.
+_current_stream = torch._C._cuda_getCurrentRawStream
+
+
 def _on(device, stream, inputs, work, *args):
     """work(stream handle, *args) with `device` and `stream` current, so that what it allocates belongs to the stream.
     When that is not the current stream, the memory of the inputs is kept until it is done with them."""
-    current = torch.cuda.current_stream(device)
-    if stream is None or stream == current:
-        if torch.cuda.current_device() == device.index:
-            return work(current.cuda_stream, *args)
+    index = device.index
+    current = _current_stream(index)
+    if stream is None or (stream.cuda_stream == current and stream.device == device):
+        if torch.cuda.current_device() == index:
+            return work(current, *args)
         with torch.cuda.device(device):
-            return work(current.cuda_stream, *args)
+            return work(current, *args)
     _require(stream.device == device, "the stream belongs to another device than the tensors")
     for t in inputs:
         if t is not None:
             t.record_stream(stream)
     with torch.cuda.stream(stream):
         return work(stream.cuda_stream, *args)
+
+
+def _like(x) -> torch.Tensor:
+    """A contiguous tensor of x's shape and type."""
+    return torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
 
 
 def _workspace(nbytes: int, device) -> torch.Tensor:
@@ -107,7 +118,7 @@ class GradientClip:
 
     def check(self):
         """Waits for the runs on the current stream and raises if one of them timed out (PBT_ERR_TIMEOUT)."""
-        _check(self.lib.pbt_clip_status(self._handle, torch.cuda.current_stream(self.device).cuda_stream))
+        _check(self.lib.pbt_clip_status(self._handle, _current_stream(self.device.index)))
 
     def __del__(self):
         if getattr(self, "_handle", None):
@@ -198,13 +209,13 @@ def block_norm_forward(x, block=None, *, post_weight=None, gate=None, scale=None
 def _norm_forward(s, d, shape, x, block, nxt, keep):
     y, u, rb, rn = x, None, None, None
     if block:
-        y = torch.empty(shape, dtype=x.dtype, device=x.device)
+        y = _like(x)
         d.y = y.data_ptr()
         if keep:
             rb = torch.empty(shape[:2], dtype=torch.float32, device=x.device)
             d.rstd_block = rb.data_ptr()
     if nxt:
-        u = torch.empty(shape, dtype=x.dtype, device=x.device)
+        u = _like(x)
         d.u = u.data_ptr()
         if keep:
             rn = torch.empty(shape[:2], dtype=torch.float32, device=x.device)
@@ -237,20 +248,20 @@ def block_norm_backward(dy, du, y, block=None, *, post_weight=None, gate=None, s
 
 
 def _norm_backward(s, d, shape, y, gate, block, nxt, scaled):
-    lib, dtype, device = load_library(), y.dtype, y.device
+    lib, device = load_library(), y.device
     vector = (shape[0], shape[2])
     dblock = dgate = dpost = dnext = dscale = None
-    dx = torch.empty(shape, dtype=dtype, device=device)
+    dx = _like(y)
     d.dx = dx.data_ptr()
     if block:
-        dblock = torch.empty(shape, dtype=dtype, device=device)
+        dblock = _like(y)
         dpost = torch.empty(vector, dtype=torch.float32, device=device)
         d.dblock, d.dpost_weight = dblock.data_ptr(), dpost.data_ptr()
         if scaled:
             dscale = torch.empty(shape[0], dtype=torch.float32, device=device)
             d.dscale = dscale.data_ptr()
         if gate is not None:
-            dgate = torch.empty(gate.shape, dtype=dtype, device=device)
+            dgate = _like(gate)
             d.dgate = dgate.data_ptr()
     if nxt:
         dnext = torch.empty(vector, dtype=torch.float32, device=device)
