@@ -180,14 +180,23 @@ __device__ __forceinline__ void row_sum(A* v, int W, int group, A* scratch, int&
     for (int k = 0; k < N; ++k) v[k] += buf[(group * W + w) * N + k];
 }
 
-// Rows on their way from global memory: a thread copies its own 16-byte vectors into its own slots of shared memory,
-// several rows ahead of the one it works on, and reads nobody else's (so the ring needs no barrier).  Rows that cannot be
-// read in vectors are loaded when they are worked on.
+// Rows on their way from global memory to shared memory.
+//
+// Aligned rows (V > 1): a thread copies its own 16-byte vectors into its own slots, several rows ahead of the one it works
+// on, and reads nobody else's, so that the ring needs no barrier.
+// Other rows (V == 1; odd widths, odd strides): the row group copies the 16-byte granules that the row touches, one row at
+// a time, and reads single elements at the row's offset in them, so these need a barrier on either side of a row; the
+// other row groups of the SM have theirs in flight meanwhile.  (A granule that holds a byte of the row lies in the same page
+// as that byte.)
 __device__ __forceinline__ void copy_ahead(void* slot, const void* from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(slot)), "l"(from) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// bytes that the granules of an unaligned row of `width` elements can take
+template <typename T>
+__host__ __device__ __forceinline__ int norm_pitch(int width) { return (width * (int)sizeof(T) + 31) / 16 * 16; }
 
 template <typename T, int V, int ITEMS, int ARRAYS, int STAGES, int THREADS>
 struct RowRing {
@@ -196,7 +205,8 @@ struct RowRing {
   const T* base[ARRAYS];
   long long member[ARRAYS], row[ARRAYS];
   bool have[ARRAYS];
-  int slot, step, nv, rows;
+  int slot, step, nv, rows, group;
+  int pitch;         // V == 1: bytes of an array's row in shared memory
   int m, i, left;    // the next row to ask for, and how many there are to ask for
 
   __device__ __forceinline__ void set(int k, const NormTensor& t, bool used) {
@@ -206,9 +216,28 @@ struct RowRing {
     have[k] = used;
   }
   __device__ __forceinline__ uint4* at(int s, int k, int j) const { return slots + s * (ARRAYS * ITEMS * THREADS) + (k * ITEMS + j) * THREADS; }
+  __device__ __forceinline__ char* staged(int k) const { return reinterpret_cast<char*>(slots) + k * pitch; }
+  __device__ __forceinline__ void barrier() const {
+    if (step == 32) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(step) : "memory");
+  }
   // ask for the next row (for nothing behind the last one) into stage s
   __device__ __forceinline__ void ask(int s) {
-    if constexpr (V > 1) {
+    if constexpr (V == 1) {
+      barrier();     // everybody has read the row before
+      if (left > 0) {
+#pragma unroll
+        for (int k = 0; k < ARRAYS; ++k)
+          if (have[k]) {
+            const uintptr_t from = (uintptr_t)(base[k] + m * member[k] + i * row[k]);
+            const int n = (int)((from & 15) + nv * sizeof(T) + 15) / 16;
+            for (int e = slot; e < n; e += step) copy_ahead(staged(k) + e * 16, reinterpret_cast<const void*>((from & ~(uintptr_t)15) + e * 16));
+          }
+        --left;
+        if (++i == rows) { i = 0; ++m; }
+      }
+      copy_commit();
+    } else {
       if (left > 0) {
 #pragma unroll
         for (int k = 0; k < ARRAYS; ++k)
@@ -228,13 +257,17 @@ struct RowRing {
   }
   // the oldest row asked for has arrived
   __device__ __forceinline__ void wait() const {
-    if constexpr (V > 1) copy_wait<STAGES - 1>();
+    copy_wait<STAGES - 1>();
+    if constexpr (V == 1) barrier();
   }
   // vector j of array k (which there is) of row (m, i), which stage s holds; the vector lies inside the row
   template <typename L>
   __device__ __forceinline__ void get(int m, int i, int s, int k, int j, L* f) const {
     if constexpr (V > 1) Vec<T, V>::unpack(*reinterpret_cast<const Raw*>(at(s, k, j)), f);
-    else Vec<T, V>::unpack(Vec<T, V>::load(base[k] + m * member[k] + i * row[k] + slot + j * step), f);
+    else {
+      const uintptr_t from = (uintptr_t)(base[k] + m * member[k] + i * row[k]);
+      Vec<T, V>::unpack(Vec<T, V>::load(reinterpret_cast<const T*>(staged(k) + (from & 15)) + slot + j * step), f);
+    }
   }
 };
 
@@ -262,8 +295,9 @@ __global__ void __launch_bounds__(THREADS) k_norm_forward(const NormArgs a) {
   const long long r_end = norm_first_row(a, g + 1);
   int m = (int)(r / a.rows), i = (int)(r % a.rows);
   RowRing<T, V, ITEMS, 3, kStages, THREADS> ring;
-  ring.slots = norm_ring + threadIdx.x;
-  ring.slot = (warp % W) * 32 + lane; ring.step = W * 32; ring.nv = a.width / V; ring.rows = a.rows;
+  ring.slot = (warp % W) * 32 + lane; ring.step = W * 32; ring.nv = a.width / V; ring.rows = a.rows; ring.group = group;
+  ring.pitch = norm_pitch<T>(a.width);
+  ring.slots = V > 1 ? norm_ring + threadIdx.x : norm_ring + group * (3 * ring.pitch / 16);
   ring.m = m; ring.i = i; ring.left = (int)(r_end - r);
   ring.set(0, a.x, true); ring.set(1, a.block, block); ring.set(2, a.gate, gate);
 #pragma unroll
@@ -373,8 +407,9 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_no
   int m = (int)(r / a.rows), i = (int)(r % a.rows);
   enum { kDy, kDu, kY, kBlock, kGate };
   RowRing<T, V, ITEMS, 5, kStages, THREADS> ring;
-  ring.slots = norm_ring + threadIdx.x;
-  ring.slot = (warp % W) * 32 + lane; ring.step = W * 32; ring.nv = a.width / V; ring.rows = a.rows;
+  ring.slot = (warp % W) * 32 + lane; ring.step = W * 32; ring.nv = a.width / V; ring.rows = a.rows; ring.group = group;
+  ring.pitch = norm_pitch<T>(a.width);
+  ring.slots = V > 1 ? norm_ring + threadIdx.x : norm_ring + group * (5 * ring.pitch / 16);
   ring.m = m; ring.i = i; ring.left = (int)(r_end - r);
   ring.set(kDy, a.dy, has_dy); ring.set(kDu, a.du, next); ring.set(kY, a.x, next);
   ring.set(kBlock, a.block, block); ring.set(kGate, a.gate, gate);
@@ -526,36 +561,43 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_no
   }
 }
 
-// A member's column sums from the partial results of its row groups: a block takes 32 columns, its eight warps every
-// eighth row group, and adds the warps' sums in order.
-template <typename T>
+// A member's column sums (blockIdx.z: which of them) from the partial results of its row groups.  WAYS == 1: a thread adds up a
+// column.  WAYS == 8, for members with many row groups: a block takes 32 columns, its eight warps every eighth row group,
+// and adds the warps' sums in order.
+template <typename T, int WAYS>
 __global__ void __launch_bounds__(256) k_norm_columns(const NormArgs a) {
   pdl_prologue();
   __shared__ float part[8][33];
-  const int m = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, e = blockIdx.x * 32 + lane;
+  const int m = blockIdx.y, q = blockIdx.z, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int e = WAYS == 1 ? blockIdx.x * 256 + threadIdx.x : blockIdx.x * 32 + lane, way = WAYS == 1 ? 0 : warp;
   const bool next = a.du.p != nullptr, block = a.block.p != nullptr;
   const int g0 = norm_group_of(a, (long long)m * a.rows), g1 = norm_group_of(a, (long long)(m + 1) * a.rows - 1);
-  for (int q = 0; q < a.sums; ++q) {
-    float t = 0.f;
-    if (e < a.width)
-      for (int g = g0 + warp; g <= g1; g += 8) t += a.partial[((long long)(g + m) * a.sums + q) * a.width + e];
+  float t = 0.f;
+  if (e < a.width) {
+    const float* p = a.partial + ((long long)(g0 + way + m) * a.sums + q) * a.width + e;
+    const long long step = (long long)WAYS * a.sums * a.width;
+#pragma unroll 8
+    for (int g = g0 + way; g <= g1; g += WAYS, p += step) t += __ldcg(p);
+  }
+  if (WAYS > 1) {
     part[warp][lane] = t;
     __syncthreads();
-    if (warp == 0 && e < a.width) {
-      t = part[0][lane];
+    if (warp == 0) {
 #pragma unroll
       for (int w = 1; w < 8; ++w) t += part[w][lane];
-      const long long at = (long long)m * a.width + e;
-      if (next && q == 0) a.dnext[at] = t;
-      else if (q == (next ? 1 : 0)) a.dpost[at] = t;
-      else Vec<T, 1>::store(reinterpret_cast<T*>(a.dgate) + at, &t);
     }
     __syncthreads();
   }
-  if (block && blockIdx.x == 0 && a.dscale) {
+  if (e < a.width && (WAYS == 1 || warp == 0)) {
+    const long long at = (long long)m * a.width + e;
+    if (next && q == 0) a.dnext[at] = t;
+    else if (q == (next ? 1 : 0)) a.dpost[at] = t;
+    else Vec<T, 1>::store(reinterpret_cast<T*>(a.dgate) + at, &t);
+  }
+  if (block && blockIdx.x == 0 && q == 0 && a.dscale) {
     const int n = (g1 - g0 + 1) * a.warps_per_row;
     const float* p = a.partial_scale + (long long)(g0 + m) * a.warps_per_row;
-    float t = 0.f;
+    t = 0.f;
     for (int k = threadIdx.x; k < n; k += 256) t += p[k];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
@@ -566,6 +608,12 @@ __global__ void __launch_bounds__(256) k_norm_columns(const NormArgs a) {
       a.dscale[m] = t;
     }
   }
+}
+template <typename T>
+cudaError_t launch_norm_columns(const NormArgs& a, cudaStream_t s) {
+  // one thread a column is enough work for the SMs' latency while a member has few row groups (80 members: 8 each)
+  if (a.groups / a.members <= 16) return launch_with(dim3((a.width + 255) / 256, a.members, a.sums), 256, 0, s)(k_norm_columns<T, 1>, a);
+  return launch_with(dim3((a.width + 31) / 32, a.members, a.sums), 256, 0, s)(k_norm_columns<T, 8>, a);
 }
 
 int norm_fail(int code, const char* msg) {
@@ -673,21 +721,25 @@ NormPlan norm_backward_plan(const pbt_block_norm_desc* d) {
 
 template <typename T, int V, int ITEMS, int THREADS>
 cudaError_t launch_norm_backward(unsigned grid, int threads, const NormArgs& a, cudaStream_t s) {
-  constexpr int per_thread = V == 1 ? 0 : norm_stages<V, ITEMS, 5, THREADS>() * 5 * ITEMS * 16;
+  // unaligned rows: at most 16 elements and two granules' edges a thread
+  constexpr int most = V == 1 ? 5 * (THREADS * ITEMS * (int)sizeof(T) + THREADS / 32 * 32) : norm_stages<V, ITEMS, 5, THREADS>() * 5 * ITEMS * 16 * THREADS;
+  const int smem = V == 1 ? 5 * norm_pitch<T>(a.width) * (threads / (a.warps_per_row * 32)) : most;
   static tc::DeviceSetup setup;
   int sms = 0;
-  const cudaError_t e = tc::device_setup(&setup, k_norm_backward<T, V, ITEMS, THREADS>, per_thread * THREADS, &sms);
+  const cudaError_t e = tc::device_setup(&setup, k_norm_backward<T, V, ITEMS, THREADS>, most, &sms);
   if (e != cudaSuccess) return e;
-  return launch_with(grid, threads, per_thread * THREADS, s)(k_norm_backward<T, V, ITEMS, THREADS>, a);
+  return launch_with(grid, threads, smem, s)(k_norm_backward<T, V, ITEMS, THREADS>, a);
 }
 template <typename T, int V, int ITEMS, int THREADS>
 cudaError_t launch_norm_forward(unsigned grid, int threads, const NormArgs& a, cudaStream_t s) {
-  constexpr int per_thread = V == 1 ? 0 : norm_stages<V, ITEMS, 3, THREADS>() * 3 * ITEMS * 16;
+  // unaligned rows: at most 16 elements and two granules' edges a thread
+  constexpr int most = V == 1 ? 3 * (THREADS * ITEMS * (int)sizeof(T) + THREADS / 32 * 32) : norm_stages<V, ITEMS, 3, THREADS>() * 3 * ITEMS * 16 * THREADS;
+  const int smem = V == 1 ? 3 * norm_pitch<T>(a.width) * (threads / (a.warps_per_row * 32)) : most;
   static tc::DeviceSetup setup;
   int sms = 0;
-  const cudaError_t e = tc::device_setup(&setup, k_norm_forward<T, V, ITEMS, THREADS>, per_thread * THREADS, &sms);
+  const cudaError_t e = tc::device_setup(&setup, k_norm_forward<T, V, ITEMS, THREADS>, most, &sms);
   if (e != cudaSuccess) return e;
-  return launch_with(grid, threads, per_thread * THREADS, s)(k_norm_forward<T, V, ITEMS, THREADS>, a);
+  return launch_with(grid, threads, smem, s)(k_norm_forward<T, V, ITEMS, THREADS>, a);
 }
 // The instantiations that norm_shape can ask for: blocks of 512 threads belong to 16 elements a thread.
 template <typename T, int V, int ITEMS>
@@ -779,10 +831,7 @@ extern "C" int pbt_block_norm_backward(const pbt_block_norm_desc* d, void* works
   a.partial_scale = a.partial + p.slots * p.sums * d->width;
   cudaStream_t s = (cudaStream_t)stream;
   cudaError_t e = launch_norm(d->dtype == 1, p.v, true, p.shape, (unsigned)p.blocks, a, s);
-  if (e == cudaSuccess) {
-    auto l = launch_with(dim3((d->width + 31) / 32, d->members), 256, 0, s);
-    e = d->dtype ? l(k_norm_columns<bf16>, a) : l(k_norm_columns<float>, a);
-  }
+  if (e == cudaSuccess) e = d->dtype ? launch_norm_columns<bf16>(a, s) : launch_norm_columns<float>(a, s);
   if (e != cudaSuccess) return norm_fail(PBT_ERR_CUDA, cudaGetErrorString(e));
   return PBT_OK;
 }
