@@ -156,28 +156,56 @@ __device__ __forceinline__ void load_weights(const float* p, L* f) {
   }
 }
 
-// Sum of N values over the W warps of a row group.  scratch: [2][32][N], used alternately (`turn`), so that one barrier
-// per reduction is enough: a buffer is written again only after everybody has passed the next barrier.
-template <int N, typename A>
-__device__ __forceinline__ void row_sum(A* v, int W, int group, A* scratch, int& turn) {
+// Sum of a value over the W warps of a row group.  scratch: [2][32], used alternately (`turn`), so that one barrier per
+// reduction is enough: a buffer is written again only after everybody has passed the next barrier.
+__device__ __forceinline__ float row_sum(float v, int W, int group, float* scratch, int& turn) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-    for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
-  if (W == 1) return;
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+  if (W == 1) return v;
   const int warp = threadIdx.x >> 5;
-  A* buf = scratch + turn * 32 * N;
+  float* buf = scratch + turn * 32;
   turn ^= 1;
-  if ((threadIdx.x & 31) == 0)
-#pragma unroll
-    for (int k = 0; k < N; ++k) buf[warp * N + k] = v[k];
+  if ((threadIdx.x & 31) == 0) buf[warp] = v;
   __syncwarp();
   asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(W * 32) : "memory");
+  v = 0.f;
+  for (int w = 0; w < W; ++w) v += buf[group * W + w];
+  return v;
+}
+
+// The same for the backward pass's three sums (at most 16 warps).  The three are folded into one register on the way: after
+// the first exchange the halves of a warp go on with different sums, after the second its quarters, so that a warp needs
+// 6 shuffles and not 15; across warps the lanes read one partial sum each.  scratch: [2][64].
+template <typename A>
+__device__ __forceinline__ void row_sum3(A* v, int W, int group, A* scratch, int& turn) {
+  const unsigned all_lanes = 0xFFFFFFFFu;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const bool hi = lane & 16, odd = lane & 8;
+  A a = hi ? v[2] : v[0], b = hi ? (A)0 : v[1];
+  a += __shfl_xor_sync(all_lanes, hi ? v[0] : v[2], 16);
+  b += __shfl_xor_sync(all_lanes, hi ? v[1] : (A)0, 16);
+  A s = odd ? b : a;
+  s += __shfl_xor_sync(all_lanes, odd ? a : b, 8);
 #pragma unroll
-  for (int k = 0; k < N; ++k) v[k] = 0;
-  for (int w = 0; w < W; ++w)
+  for (int o = 4; o > 0; o >>= 1) s += __shfl_xor_sync(all_lanes, s, o);
+  // sum 0 is in lanes 0..7, sum 1 in 8..15, sum 2 in 16..23
+  if (W > 1) {
+    A* buf = scratch + turn * 64;
+    turn ^= 1;
+    if ((lane & 7) == 0) buf[warp * 4 + (lane >> 3)] = s;
+    __syncwarp();
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(W * 32) : "memory");
+    const A* mine = buf + group * W * 4;
+    s = lane < 4 * W ? mine[lane] : (A)0;
+    if (W > 8 && lane + 32 < 4 * W) s += mine[lane + 32];
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] += buf[(group * W + w) * N + k];
+    for (int o = 16; o > 2; o >>= 1) s += __shfl_xor_sync(all_lanes, s, o);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) v[k] = __shfl_sync(all_lanes, s, k);
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) v[k] = __shfl_sync(all_lanes, s, 8 * k);
 }
 
 // Rows on their way from global memory to shared memory.
@@ -328,9 +356,7 @@ __global__ void __launch_bounds__(THREADS) k_norm_forward(const NormArgs a) {
 #pragma unroll
         for (int j = 0; j < N; ++j) s = fma(b[j], b[j], s);
       }
-      float sum[1] = {total(s)};
-      row_sum<1>(sum, W, group, scratch, turn);
-      const float rb = rsqrtf(sum[0] * a.inv_width + a.eps);
+      const float rb = rsqrtf(row_sum(total(s), W, group, scratch, turn) * a.inv_width + a.eps);
       const L crb = all<L>(a.scale ? a.scale[m] * rb : rb);
       if (a.rstd_block && ring.slot == 0) a.rstd_block[r] = rb;
 #pragma unroll
@@ -362,9 +388,7 @@ __global__ void __launch_bounds__(THREADS) k_norm_forward(const NormArgs a) {
       for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
         for (int j = 0; j < N; ++j) s = fma(y[k][j], y[k][j], s);
-      float sum[1] = {total(s)};
-      row_sum<1>(sum, W, group, scratch, turn);
-      const float ry = rsqrtf(sum[0] * a.inv_width + a.eps);
+      const float ry = rsqrtf(row_sum(total(s), W, group, scratch, turn) * a.inv_width + a.eps);
       if (a.rstd_next && ring.slot == 0) a.rstd_next[r] = ry;
 #pragma unroll
       for (int k = 0; k < ITEMS; ++k) {
@@ -381,9 +405,13 @@ __global__ void __launch_bounds__(THREADS) k_norm_forward(const NormArgs a) {
   }
 }
 
+// acc += a b (column sums are fp32 or pairs of fp32)
+__device__ __forceinline__ void accumulate(F2& acc, F2 a, F2 b) { acc = fma(a, b, acc); }
+template <typename L> __device__ __forceinline__ void accumulate(float& acc, L a, L b) { acc += (float)(a * b); }
+
 // Sums of a row group, in the order in which a partial result holds them: next, post, gate (the ones that exist).
-// A row is read from the ring twice, before and after its reduction, so that a thread's registers hold little besides its
-// column sums.
+// Up to 8 elements a thread, what the first pass over a row works out stays in registers for the second; the widest
+// rows (16 elements a thread, whose column sums fill the registers) read the row from shared memory twice.
 // Rows of at most 32 single elements are worked out in fp64 (inputs, results and column sums keep their types): dx and
 // db are what is left of dh and dn after the projection on the row is taken away, and in rows of one or two columns
 // that is next to nothing, 1 - yh^2 of it, which fp32 loses altogether.
@@ -394,9 +422,11 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_no
   typedef typename std::conditional<V == 1 && ITEMS == 1, double, float>::type A;
   typedef typename std::conditional<V == 1, A, F2>::type L;           // a thread's values
   typedef typename std::conditional<V == 1, float, F2>::type S;       // its column sums
-  __shared__ A scratch[2 * 3 * 32];
+  __shared__ A scratch[2 * 64];
   typedef Vec<T, V> X;
   constexpr int N = V == 1 ? 1 : V / 2, kStages = norm_stages<V, ITEMS, 5, THREADS>();
+  constexpr bool kKeep = V * ITEMS <= 8;
+  constexpr int kKept = kKeep ? ITEMS : 1;
   const int W = a.warps_per_row, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int group = warp / W, g = blockIdx.x * (blockDim.x / (W * 32)) + group;
   if (g >= a.groups) return;
@@ -430,100 +460,84 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_no
     const A ry = next ? a.rstd_next[r] : 0.f, rb = block ? a.rstd_block[r] : 0.f;
     const L lry = all<L>(ry), lrb = all<L>(rb);
     ring.wait();
-    L part[3] = {all<L>(0.f), all<L>(0.f), all<L>(0.f)};   // r_y dh yh, p (dy + r_y dh), p yh, with p = g w_post v
-#pragma unroll
-    for (int k = 0; k < ITEMS; ++k) {
+    L sum_h = all<L>(0.f), sum_t = all<L>(0.f), sum_y = all<L>(0.f);   // r_y dh yh, p (dy + r_y dh), p yh, with p = g w_post v
+    L t[kKept][N], yh[kKept][N], open[kKept][N], v[kKept][N], w[kKept][N];   // dy + r_y dh, yh, sigmoid(z), v, w_post
+    // the vectors k of the row; `first`: with the sums that do not wait for the reduction
+    auto values = [&](int k, int to, bool first) {
       const int e = ring.slot + k * ring.step;
-      if (e >= ring.nv) continue;
-      L t[N], yh[N];      // dy + r_y dh
 #pragma unroll
-      for (int j = 0; j < N; ++j) t[j] = all<L>(0.f);
-      if (has_dy) ring.get(m, i, stage, kDy, k, t);
+      for (int j = 0; j < N; ++j) t[to][j] = yh[to][j] = all<L>(0.f);
+      if (has_dy) ring.get(m, i, stage, kDy, k, t[to]);
       if (next) {
-        L du[N], w[N];
+        L du[N], u[N];
         ring.get(m, i, stage, kDu, k, du);
-        ring.get(m, i, stage, kY, k, yh);
-        load_weights<V>(wn + e * V, w);
+        ring.get(m, i, stage, kY, k, yh[to]);
+        load_weights<V>(wn + e * V, u);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-          du[j] = mul(mul(du[j], lry), w[j]);
-          yh[j] = mul(yh[j], lry);
-          part[0] = fma(du[j], yh[j], part[0]);
-          t[j] = add(t[j], du[j]);
+          yh[to][j] = mul(yh[to][j], lry);
+          if (first) accumulate(acc_next[k][j], du[j], yh[to][j]);
+          u[j] = mul(mul(du[j], lry), u[j]);
+          if (first) sum_h = fma(u[j], yh[to][j], sum_h);
+          t[to][j] = add(t[to][j], u[j]);
         }
       }
       if (block) {
-        L b[N], w[N];
-        ring.get(m, i, stage, kBlock, k, b);
-        load_weights<V>(wp + e * V, w);
-#pragma unroll
-        for (int j = 0; j < N; ++j) b[j] = mul(mul(b[j], lrb), w[j]);
+        ring.get(m, i, stage, kBlock, k, v[to]);
+        load_weights<V>(wp + e * V, w[to]);
         if (gate) {
           L z[N];
           ring.get(m, i, stage, kGate, k, z);
 #pragma unroll
-          for (int j = 0; j < N; ++j) b[j] = mul(b[j], opened(z[j]));
+          for (int j = 0; j < N; ++j) open[to][j] = opened(z[j]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < N; ++j) open[to][j] = all<L>(1.f);
         }
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-          part[1] = fma(b[j], t[j], part[1]);
-          if (next) part[2] = fma(b[j], yh[j], part[2]);
+          v[to][j] = mul(v[to][j], lrb);
+          if (first) {
+            const L p = mul(mul(v[to][j], w[to][j]), open[to][j]);
+            sum_t = fma(p, t[to][j], sum_t);
+            sum_y = fma(p, yh[to][j], sum_y);
+          }
         }
       }
-    }
-    A sums[3] = {total(part[0]), total(part[1]), total(part[2])};
-    row_sum<3>(sums, W, group, scratch, turn);
+    };
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k)
+      if (ring.slot + k * ring.step < ring.nv) values(k, kKeep ? k : 0, true);
+    A sums[3] = {total(sum_h), total(sum_t), total(sum_y)};
+    row_sum3(sums, W, group, scratch, turn);
     const A t1 = sums[0] / a.width;                                             // r_y t1
-    const L lt1 = all<L>(-t1), lt2 = all<L>(-c * (sums[1] - t1 * sums[2]) / a.width), lc = all<L>(c);   // -r_y t1, -c t2
+    const L lt1 = all<L>(-t1), lt2 = all<L>(-c * rb * (sums[1] - t1 * sums[2]) / a.width);   // -r_y t1, -c r_b t2
+    const L lc = all<L>(c), lcrb = all<L>(c * rb), one = all<L>(1.f), minus = all<L>(-1.f);
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
-      const int e = ring.slot + k * ring.step;
+      const int e = ring.slot + k * ring.step, from = kKeep ? k : 0;
       if (e >= ring.nv) continue;
-      L dx[N];
+      if constexpr (!kKeep) values(k, 0, false);
 #pragma unroll
-      for (int j = 0; j < N; ++j) dx[j] = all<L>(0.f);
-      if (has_dy) ring.get(m, i, stage, kDy, k, dx);
-      if (next) {
-        L du[N], y[N], w[N];
-        ring.get(m, i, stage, kDu, k, du);
-        ring.get(m, i, stage, kY, k, y);
-        load_weights<V>(wn + e * V, w);
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-          const L yh = mul(y[j], lry);
-          if constexpr (std::is_same<L, S>::value) acc_next[k][j] = fma(du[j], yh, acc_next[k][j]);
-          else acc_next[k][j] += (float)(du[j] * yh);
-          dx[j] = fma(yh, lt1, fma(mul(du[j], lry), w[j], dx[j]));
-        }
-      }
-      X::store(reinterpret_cast<T*>(a.dx) + at + e * V, dx);
+      for (int j = 0; j < N; ++j) t[from][j] = fma(yh[from][j], lt1, t[from][j]);
+      X::store(reinterpret_cast<T*>(a.dx) + at + e * V, t[from]);
       if (block) {
-        L b[N], z[N], w[N];
-        ring.get(m, i, stage, kBlock, k, b);
-        load_weights<V>(wp + e * V, w);
-        if (gate) ring.get(m, i, stage, kGate, k, z);
-        L o_sum = all<L>(0.f);
+        L db[N], dz[N], o_sum = all<L>(0.f);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-          const L open = gate ? opened(z[j]) : all<L>(1.f);
-          const L v = mul(b[j], lrb), gdx = mul(open, dx[j]), dn = mul(lc, gdx), vw = mul(v, w[j]);
-          const L o = mul(gdx, vw);
-          if constexpr (std::is_same<L, S>::value) acc_post[k][j] = fma(dn, v, acc_post[k][j]);
-          else acc_post[k][j] += (float)(dn * v);
+          const L gdx = mul(open[from][j], t[from][j]), gwdx = mul(gdx, w[from][j]), o = mul(gwdx, v[from][j]);
+          accumulate(acc_post[k][j], mul(lc, gdx), v[from][j]);
           o_sum = add(o_sum, o);
-          b[j] = mul(lrb, fma(v, lt2, mul(dn, w[j])));
-          z[j] = mul(mul(lc, o), fma(all<L>(-1.f), open, all<L>(1.f)));
+          db[j] = fma(lcrb, gwdx, mul(v[from][j], lt2));
+          dz[j] = mul(mul(lc, o), fma(minus, open[from][j], one));
         }
         acc_scale += (float)total(o_sum);
-        X::store(reinterpret_cast<T*>(a.dblock) + at + e * V, b);
+        X::store(reinterpret_cast<T*>(a.dblock) + at + e * V, db);
         if (vector) {
 #pragma unroll
-          for (int j = 0; j < N; ++j) {
-            if constexpr (std::is_same<L, S>::value) acc_gate[k][j] = add(acc_gate[k][j], z[j]);
-            else acc_gate[k][j] += (float)z[j];
-          }
+          for (int j = 0; j < N; ++j) accumulate(acc_gate[k][j], dz[j], one);
         } else if (gate) {
-          X::store(reinterpret_cast<T*>(a.dgate) + at + e * V, z);
+          X::store(reinterpret_cast<T*>(a.dgate) + at + e * V, dz);
         }
       }
     }
@@ -681,16 +695,27 @@ void norm_shape(int width, int v, int items, int* warps, int* groups) {
   *groups = std::max(1, kNormThreads / 32 / *warps);
 }
 
-// A row fills the threads of a warp with up to 16 elements each before it takes another warp (fewer warps: cheaper
-// reductions); 8192 elements are 16 warps, and blocks have 256 threads up to 4096 elements, 512 beyond.
+// Elements of a thread (`items` vectors) and warps of a row.  Forward: 16 elements a thread before a row takes another warp
+// (fewer warps: cheaper reductions; 2048 bf16 columns 169 us with 16, 228 us with 8).  Backward: 8, which leaves registers
+// for what the first pass works out (344 us with 16), and 16 beyond 4096 columns.  Blocks have 256 threads as long as eight
+// warps hold a row, 512 beyond.  When rows are so few that a row group would get fewer than four, a row takes up to eight
+// warps instead: its latency is what counts then.
 struct NormShape { int items, warps, groups, threads; };
-NormShape norm_shape(int width, int v) {
-  const int nv = width / v;
+NormShape norm_shape(const pbt_block_norm_desc* d, int v, bool backward) {
+  const int nv = d->width / v, most = backward && d->width <= 4096 ? 8 : 16;
+  const long long rows = (long long)d->members * d->rows;
   NormShape s;
   s.items = 1;
-  while (s.items * v < 16 && nv > s.items * 32) s.items *= 2;
-  s.warps = (nv + s.items * 32 - 1) / (s.items * 32);
-  s.groups = std::max(1, kNormThreads / 32 / s.warps);
+  while (s.items * v < most && nv > s.items * 32) s.items *= 2;
+  auto fill = [&]() {
+    s.warps = (nv + s.items * 32 - 1) / (s.items * 32);
+    s.groups = std::max(1, kNormThreads / 32 / s.warps);
+  };
+  fill();
+  while (s.items > (v == 1 ? 2 : 1) && s.warps <= 4 && rows < 4ll * 2 * 148 * s.groups) {
+    s.items /= 2;
+    fill();
+  }
   s.threads = s.groups * s.warps * 32;
   return s;
 }
@@ -709,7 +734,7 @@ struct NormPlan { int v, blocks, groups, sums; NormShape shape; size_t slots, by
 NormPlan norm_backward_plan(const pbt_block_norm_desc* d) {
   NormPlan p;
   p.v = norm_vector(d, true);
-  p.shape = norm_shape(d->width, p.v);
+  p.shape = norm_shape(d, p.v, true);
   p.blocks = norm_blocks(d, p.shape.groups, p.shape.threads > kNormThreads ? 1 : 2);
   p.groups = norm_groups(d, p.shape.groups, p.blocks);
   p.sums = (d->du ? 1 : 0) + (d->block ? 1 : 0) + (d->gate && d->gate_vector ? 1 : 0);
@@ -741,20 +766,23 @@ cudaError_t launch_norm_forward(unsigned grid, int threads, const NormArgs& a, c
   if (e != cudaSuccess) return e;
   return launch_with(grid, threads, smem, s)(k_norm_forward<T, V, ITEMS, THREADS>, a);
 }
-// The instantiations that norm_shape can ask for: blocks of 512 threads belong to 16 elements a thread.
+// The instantiations that norm_shape can ask for: blocks of 512 threads belong to the most elements a thread.
 template <typename T, int V, int ITEMS>
 cudaError_t launch_norm(bool backward, const NormShape& p, unsigned grid, const NormArgs& a, cudaStream_t s) {
-  if constexpr (ITEMS * V == 16)
-    if (p.threads > kNormThreads)
-      return backward ? launch_norm_backward<T, V, ITEMS, 512>(grid, p.threads, a, s) : launch_norm_forward<T, V, ITEMS, 512>(grid, p.threads, a, s);
-  return backward ? launch_norm_backward<T, V, ITEMS, kNormThreads>(grid, p.threads, a, s)
-                  : launch_norm_forward<T, V, ITEMS, kNormThreads>(grid, p.threads, a, s);
+  if (!backward) {
+    if constexpr (ITEMS * V == 16)
+      if (p.threads > kNormThreads) return launch_norm_forward<T, V, ITEMS, 512>(grid, p.threads, a, s);
+    return launch_norm_forward<T, V, ITEMS, kNormThreads>(grid, p.threads, a, s);
+  }
+  if constexpr (ITEMS * V >= 8)
+    if (p.threads > kNormThreads) return launch_norm_backward<T, V, ITEMS, 512>(grid, p.threads, a, s);
+  if constexpr (ITEMS * V <= 8) return launch_norm_backward<T, V, ITEMS, kNormThreads>(grid, p.threads, a, s);
+  return cudaErrorInvalidValue;
 }
 template <typename T, int V>
 cudaError_t launch_norm(bool backward, const NormShape& p, unsigned grid, const NormArgs& a, cudaStream_t s) {
   if (p.items == 1) return launch_norm<T, V, 1>(backward, p, grid, a, s);
-  if constexpr (V <= 8)
-    if (p.items == 2) return launch_norm<T, V, 2>(backward, p, grid, a, s);
+  if (p.items == 2) return launch_norm<T, V, 2>(backward, p, grid, a, s);
   if constexpr (V <= 4)
     if (p.items == 4) return launch_norm<T, V, 4>(backward, p, grid, a, s);
   if constexpr (V == 1) {
@@ -783,7 +811,7 @@ extern "C" int pbt_block_norm_forward(const pbt_block_norm_desc* d, void* stream
   NormArgs a;
   norm_fill(&a, d);
   const int v = norm_vector(d, false);
-  const NormShape shape = norm_shape(d->width, v);
+  const NormShape shape = norm_shape(d, v, false);
   const int blocks = norm_blocks(d, shape.groups, shape.threads > kNormThreads ? 1 : 4);
   a.warps_per_row = shape.warps;
   a.groups = norm_groups(d, shape.groups, blocks);
