@@ -3,10 +3,11 @@
 // and the gradients of all of it.  b is the block's output, y the residual stream, u the next block's input.
 //
 // Memory-bound: the forward pass reads x, b, z and writes y, u once; the backward pass reads y, b, z, dy, du and writes
-// dx, db, dz once.  With five streams in and three out the arithmetic (about 25 and 50 instructions an element written
-// out) is as long as the transfers, so it is kept short: pairs of elements in packed fp32 instructions, 16 elements a
-// thread so that a row's reductions are shared by many, and the rows on their way to shared memory (cp.async) while
-// earlier ones are worked on.  Every sum is fp32 or wider.
+// dx, db, dz once.  With five streams in and three out the instructions are as long as the transfers, so they are kept
+// few: several elements a thread, so that a row's reductions and addresses are shared by many, running pointers, and the
+// rows on their way to shared memory (cp.async) while earlier ones are worked on.  (Packed fp32 pairs, fma.rn.f32x2, did
+// not pay: 297 us against 275 for the backward pass of 80 x 512 x 2048, the moves into register pairs cost more than the
+// halved arithmetic.)  Every sum is fp32 or wider.
 //
 // Backward, with yh = y r_y, dh = du w_next and p = sigmoid(z) w_post v:
 //   t1 = mean(dh yh),  dx = dy + r_y (dh - yh t1),  db = r_b (c g w_post dx - c v t2),  t2 = mean(p dx)
@@ -56,36 +57,6 @@ __device__ __forceinline__ int norm_group_of(const NormArgs& a, long long r) {
   return (int)(((r + 1) * a.groups - 1) / ((long long)a.members * a.rows));
 }
 
-// Arithmetic of a thread: pairs of fp32 in the packed instructions for rows that are read in vectors, single fp32 or fp64
-// values otherwise.
-struct F2 { unsigned long long v; };
-__device__ __forceinline__ F2 pair(float a, float b) {
-  F2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ float2 split(F2 a) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
-  return r;
-}
-__device__ __forceinline__ F2 mul(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
-__device__ __forceinline__ F2 add(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
-__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
-__device__ __forceinline__ float mul(float a, float b) { return __fmul_rn(a, b); }
-__device__ __forceinline__ float add(float a, float b) { return __fadd_rn(a, b); }
-__device__ __forceinline__ float fma(float a, float b, float c) { return __fmaf_rn(a, b, c); }
-__device__ __forceinline__ double mul(double a, double b) { return a * b; }
-__device__ __forceinline__ double add(double a, double b) { return a + b; }
-__device__ __forceinline__ double fma(double a, double b, double c) { return ::fma(a, b, c); }
-template <typename L, typename S> __device__ __forceinline__ L all(S x) {
-  if constexpr (std::is_same<L, F2>::value) return pair((float)x, (float)x);
-  else return (L)x;
-}
-__device__ __forceinline__ float total(F2 a) { const float2 f = split(a); return f.x + f.y; }
-__device__ __forceinline__ float total(float a) { return a; }
-__device__ __forceinline__ double total(double a) { return a; }
-
 // sigmoid(z) = 1 / (1 + 2^(-z log2 e)) by the special-function unit: relative error below (|z| + 3) 2^-22
 __device__ __forceinline__ float opened(float z) {
   float e, r;
@@ -93,25 +64,24 @@ __device__ __forceinline__ float opened(float z) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
   return r;
 }
-__device__ __forceinline__ F2 opened(F2 z) { const float2 f = split(z); return pair(opened(f.x), opened(f.y)); }
-__device__ __forceinline__ double opened(double z) { return opened((float)z); }
 
-// V elements of type T as they lie in memory, and as N = V / (lanes of L) values of L.
+// V elements of type T as they lie in memory, and as values of type L (float; double for V == 1).
 template <typename T, int V> struct Vec;
 template <> struct Vec<bf16, 8> {
   typedef uint4 Raw;
-  static __device__ __forceinline__ Raw zero() { return make_uint4(0u, 0u, 0u, 0u); }
-  static __device__ __forceinline__ void unpack(const Raw& r, F2* f) {
+  static __device__ __forceinline__ void unpack(const Raw& r, float* f) {
     const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
   }
-  static __device__ __forceinline__ void store(bf16* p, const F2* f) {
+  static __device__ __forceinline__ void store(bf16* p, const float* f) {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float2 v = split(f[i]);
-      __nv_bfloat162 t = __floats2bfloat162_rn(v.x, v.y);
+      __nv_bfloat162 t = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
       w[i] = *reinterpret_cast<uint32_t*>(&t);
     }
     *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -119,24 +89,18 @@ template <> struct Vec<bf16, 8> {
 };
 template <> struct Vec<float, 4> {
   typedef float4 Raw;
-  static __device__ __forceinline__ Raw zero() { return make_float4(0.f, 0.f, 0.f, 0.f); }
-  static __device__ __forceinline__ void unpack(const Raw& r, F2* f) { f[0] = pair(r.x, r.y); f[1] = pair(r.z, r.w); }
-  static __device__ __forceinline__ void store(float* p, const F2* f) {
-    const float2 a = split(f[0]), b = split(f[1]);
-    st_stream(p, make_float4(a.x, a.y, b.x, b.y));
-  }
+  static __device__ __forceinline__ void unpack(const Raw& r, float* f) { f[0] = r.x; f[1] = r.y; f[2] = r.z; f[3] = r.w; }
+  static __device__ __forceinline__ void store(float* p, const float* f) { st_stream(p, make_float4(f[0], f[1], f[2], f[3])); }
 };
 template <> struct Vec<float, 1> {
   typedef float Raw;
   static __device__ __forceinline__ Raw load(const float* p) { return *p; }
-  static __device__ __forceinline__ Raw zero() { return 0.f; }
   template <typename L> static __device__ __forceinline__ void unpack(const Raw& r, L* f) { f[0] = r; }
   template <typename L> static __device__ __forceinline__ void store(float* p, const L* f) { *p = (float)f[0]; }
 };
 template <> struct Vec<bf16, 1> {
   typedef float Raw;
   static __device__ __forceinline__ Raw load(const bf16* p) { return __bfloat162float(*p); }
-  static __device__ __forceinline__ Raw zero() { return 0.f; }
   template <typename L> static __device__ __forceinline__ void unpack(const Raw& r, L* f) { f[0] = r; }
   template <typename L> static __device__ __forceinline__ void store(bf16* p, const L* f) { *p = __float2bfloat16_rn((float)f[0]); }
 };
@@ -150,8 +114,7 @@ __device__ __forceinline__ void load_weights(const float* p, L* f) {
 #pragma unroll
     for (int j = 0; j < V; j += 4) {
       const float4 w = __ldg(reinterpret_cast<const float4*>(p + j));
-      f[j / 2] = pair(w.x, w.y);
-      f[j / 2 + 1] = pair(w.z, w.w);
+      f[j] = w.x; f[j + 1] = w.y; f[j + 2] = w.z; f[j + 3] = w.w;
     }
   }
 }
@@ -229,18 +192,19 @@ __host__ __device__ __forceinline__ int norm_pitch(int width) { return (width * 
 template <typename T, int V, int ITEMS, int ARRAYS, int STAGES, int THREADS>
 struct RowRing {
   typedef typename Vec<T, V>::Raw Raw;
-  uint4* slots;      // this thread's; its vectors are THREADS apart
-  const T* base[ARRAYS];
-  long long member[ARRAYS], row[ARRAYS];
+  uint4* slots;                  // this thread's (V > 1; its vectors are THREADS apart) or this row group's (V == 1)
+  const T* p[ARRAYS];            // the next row to ask for, at this thread's first vector (V == 1: at its first element)
+  long long row[ARRAYS], wrap[ARRAYS];   // to the next row, and from behind a member's last row to the next member's first
+  int shift[ARRAYS];             // V == 1: bytes between the first granule and the row that is staged
   bool have[ARRAYS];
   int slot, step, nv, rows, group;
-  int pitch;         // V == 1: bytes of an array's row in shared memory
-  int m, i, left;    // the next row to ask for, and how many there are to ask for
+  int pitch;                     // V == 1: bytes of an array's row in shared memory
+  int i, left;                   // the next row within its member, and how many there are to ask for
 
-  __device__ __forceinline__ void set(int k, const NormTensor& t, bool used) {
-    base[k] = reinterpret_cast<const T*>(t.p);
-    member[k] = t.member;
+  __device__ __forceinline__ void set(int k, const NormTensor& t, bool used, int m) {
+    p[k] = reinterpret_cast<const T*>(t.p) + m * t.member + i * t.row + (V > 1 ? slot * V : 0);
     row[k] = t.row;
+    wrap[k] = t.member - rows * t.row;
     have[k] = used;
   }
   __device__ __forceinline__ uint4* at(int s, int k, int j) const { return slots + s * (ARRAYS * ITEMS * THREADS) + (k * ITEMS + j) * THREADS; }
@@ -251,51 +215,40 @@ struct RowRing {
   }
   // ask for the next row (for nothing behind the last one) into stage s
   __device__ __forceinline__ void ask(int s) {
-    if constexpr (V == 1) {
-      barrier();     // everybody has read the row before
-      if (left > 0) {
+    if constexpr (V == 1) barrier();     // everybody has read the row before
+    if (left > 0) {
+      const bool last = ++i == rows;
+      if (last) i = 0;
+      --left;
 #pragma unroll
-        for (int k = 0; k < ARRAYS; ++k)
-          if (have[k]) {
-            const uintptr_t from = (uintptr_t)(base[k] + m * member[k] + i * row[k]);
-            const int n = (int)((from & 15) + nv * sizeof(T) + 15) / 16;
-            for (int e = slot; e < n; e += step) copy_ahead(staged(k) + e * 16, reinterpret_cast<const void*>((from & ~(uintptr_t)15) + e * 16));
+      for (int k = 0; k < ARRAYS; ++k)
+        if (have[k]) {
+          if constexpr (V > 1) {
+#pragma unroll
+            for (int j = 0; j < ITEMS; ++j)
+              if (slot + j * step < nv) copy_ahead(at(s, k, j), p[k] + j * (step * V));
+          } else {
+            shift[k] = (int)((uintptr_t)p[k] & 15);
+            const int n = (shift[k] + nv * (int)sizeof(T) + 15) / 16;
+            const char* from = reinterpret_cast<const char*>(p[k]) - shift[k];
+            for (int e = slot; e < n; e += step) copy_ahead(staged(k) + e * 16, from + e * 16);
           }
-        --left;
-        if (++i == rows) { i = 0; ++m; }
-      }
-      copy_commit();
-    } else {
-      if (left > 0) {
-#pragma unroll
-        for (int k = 0; k < ARRAYS; ++k)
-          if (have[k]) {
-            const T* p = base[k] + m * member[k] + i * row[k];
-#pragma unroll
-            for (int j = 0; j < ITEMS; ++j) {
-              const int e = slot + j * step;
-              if (e < nv) copy_ahead(at(s, k, j), p + e * V);
-            }
-          }
-        --left;
-        if (++i == rows) { i = 0; ++m; }
-      }
-      copy_commit();
+          p[k] += row[k];
+          if (last) p[k] += wrap[k];
+        }
     }
+    copy_commit();
   }
   // the oldest row asked for has arrived
   __device__ __forceinline__ void wait() const {
     copy_wait<STAGES - 1>();
     if constexpr (V == 1) barrier();
   }
-  // vector j of array k (which there is) of row (m, i), which stage s holds; the vector lies inside the row
+  // vector j of array k (which there is) of the oldest row, in stage s; the vector lies inside the row
   template <typename L>
-  __device__ __forceinline__ void get(int m, int i, int s, int k, int j, L* f) const {
+  __device__ __forceinline__ void get(int s, int k, int j, L* f) const {
     if constexpr (V > 1) Vec<T, V>::unpack(*reinterpret_cast<const Raw*>(at(s, k, j)), f);
-    else {
-      const uintptr_t from = (uintptr_t)(base[k] + m * member[k] + i * row[k]);
-      Vec<T, V>::unpack(Vec<T, V>::load(reinterpret_cast<const T*>(staged(k) + (from & 15)) + slot + j * step), f);
-    }
+    else Vec<T, V>::unpack(Vec<T, V>::load(reinterpret_cast<const T*>(staged(k) + shift[k]) + slot + j * step), f);
   }
 };
 
@@ -308,13 +261,12 @@ __host__ __device__ constexpr int norm_stages() {
 }
 
 template <typename T, int V, int ITEMS, int THREADS>
-__global__ void __launch_bounds__(THREADS) k_norm_forward(const NormArgs a) {
+__global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 4 : 1) k_norm_forward(const NormArgs a) {
   pdl_prologue();
   extern __shared__ uint4 norm_ring[];
   __shared__ float scratch[2 * 32];
   typedef Vec<T, V> X;
-  typedef typename std::conditional<V == 1, float, F2>::type L;
-  constexpr int N = V == 1 ? 1 : V / 2, kStages = norm_stages<V, ITEMS, 3, THREADS>();
+  constexpr int kStages = norm_stages<V, ITEMS, 3, THREADS>();
   const int W = a.warps_per_row, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int group = warp / W, g = blockIdx.x * (blockDim.x / (W * 32)) + group;
   if (g >= a.groups) return;
@@ -326,88 +278,91 @@ __global__ void __launch_bounds__(THREADS) k_norm_forward(const NormArgs a) {
   ring.slot = (warp % W) * 32 + lane; ring.step = W * 32; ring.nv = a.width / V; ring.rows = a.rows; ring.group = group;
   ring.pitch = norm_pitch<T>(a.width);
   ring.slots = V > 1 ? norm_ring + threadIdx.x : norm_ring + group * (3 * ring.pitch / 16);
-  ring.m = m; ring.i = i; ring.left = (int)(r_end - r);
-  ring.set(0, a.x, true); ring.set(1, a.block, block); ring.set(2, a.gate, gate);
+  ring.i = i; ring.left = (int)(r_end - r);
+  ring.set(0, a.x, true, m); ring.set(1, a.block, block, m); ring.set(2, a.gate, gate, m);
 #pragma unroll
   for (int s = 0; s < kStages; ++s) ring.ask(s);
+  const int first = ring.slot * V, far = ring.step * V;      // this thread's first element and the distance to its next vector
+  const float* wp = a.post_weight + (long long)m * a.width + first;
+  const float* wn = a.next_weight + (long long)m * a.width + first;
+  T* yp = reinterpret_cast<T*>(a.y) + r * a.width + first;
+  T* up = reinterpret_cast<T*>(a.u) + r * a.width + first;
+  float c = a.scale && block ? a.scale[m] : 1.f;
   int turn = 0, stage = 0;
-  for (; r < r_end; ++r) {
-    const long long at = r * a.width;
-    const float* wp = a.post_weight + (long long)m * a.width;
-    const float* wn = a.next_weight + (long long)m * a.width;
+  for (; r < r_end; ++r, yp += a.width, up += a.width) {
     ring.wait();
-    L y[ITEMS][N];
+    float y[ITEMS][V];
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
       if (ring.slot + k * ring.step < ring.nv) {
-        ring.get(m, i, stage, 0, k, y[k]);
+        ring.get(stage, 0, k, y[k]);
       } else {
 #pragma unroll
-        for (int j = 0; j < N; ++j) y[k][j] = all<L>(0.f);
+        for (int j = 0; j < V; ++j) y[k][j] = 0.f;
       }
     }
     if (block) {
-      L s = all<L>(0.f);
+      float s = 0.f;
 #pragma unroll
       for (int k = 0; k < ITEMS; ++k) {
         if (ring.slot + k * ring.step >= ring.nv) continue;
-        L b[N];
-        ring.get(m, i, stage, 1, k, b);
+        float b[V];
+        ring.get(stage, 1, k, b);
 #pragma unroll
-        for (int j = 0; j < N; ++j) s = fma(b[j], b[j], s);
+        for (int j = 0; j < V; ++j) s = __fmaf_rn(b[j], b[j], s);
       }
-      const float rb = rsqrtf(row_sum(total(s), W, group, scratch, turn) * a.inv_width + a.eps);
-      const L crb = all<L>(a.scale ? a.scale[m] * rb : rb);
+      const float rb = rsqrtf(row_sum(s, W, group, scratch, turn) * a.inv_width + a.eps);
+      const float crb = c * rb;
       if (a.rstd_block && ring.slot == 0) a.rstd_block[r] = rb;
 #pragma unroll
       for (int k = 0; k < ITEMS; ++k) {
-        const int e = ring.slot + k * ring.step;
-        if (e >= ring.nv) continue;
-        L b[N], w[N];
-        ring.get(m, i, stage, 1, k, b);
-        load_weights<V>(wp + e * V, w);
+        if (ring.slot + k * ring.step >= ring.nv) continue;
+        float b[V], w[V];
+        ring.get(stage, 1, k, b);
+        load_weights<V>(wp + k * far, w);
 #pragma unroll
-        for (int j = 0; j < N; ++j) b[j] = mul(mul(b[j], crb), w[j]);
+        for (int j = 0; j < V; ++j) b[j] = b[j] * crb * w[j];
         if (gate) {
-          L z[N];
-          ring.get(m, i, stage, 2, k, z);
+          float z[V];
+          ring.get(stage, 2, k, z);
 #pragma unroll
-          for (int j = 0; j < N; ++j) y[k][j] = fma(b[j], opened(z[j]), y[k][j]);
+          for (int j = 0; j < V; ++j) y[k][j] = __fmaf_rn(b[j], opened(z[j]), y[k][j]);
         } else {
 #pragma unroll
-          for (int j = 0; j < N; ++j) y[k][j] = add(b[j], y[k][j]);
+          for (int j = 0; j < V; ++j) y[k][j] += b[j];
         }
-        X::store(reinterpret_cast<T*>(a.y) + at + e * V, y[k]);
+        X::store(yp + k * far, y[k]);
       }
     }
     ring.ask(stage);
     if (++stage == kStages) stage = 0;
     if (next) {
-      L s = all<L>(0.f);
+      float s = 0.f;
 #pragma unroll
       for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
-        for (int j = 0; j < N; ++j) s = fma(y[k][j], y[k][j], s);
-      const float ry = rsqrtf(row_sum(total(s), W, group, scratch, turn) * a.inv_width + a.eps);
+        for (int j = 0; j < V; ++j) s = __fmaf_rn(y[k][j], y[k][j], s);
+      const float ry = rsqrtf(row_sum(s, W, group, scratch, turn) * a.inv_width + a.eps);
       if (a.rstd_next && ring.slot == 0) a.rstd_next[r] = ry;
 #pragma unroll
       for (int k = 0; k < ITEMS; ++k) {
-        const int e = ring.slot + k * ring.step;
-        if (e >= ring.nv) continue;
-        L w[N];
-        load_weights<V>(wn + e * V, w);
+        if (ring.slot + k * ring.step >= ring.nv) continue;
+        float w[V];
+        load_weights<V>(wn + k * far, w);
 #pragma unroll
-        for (int j = 0; j < N; ++j) w[j] = mul(mul(y[k][j], all<L>(ry)), w[j]);
-        X::store(reinterpret_cast<T*>(a.u) + at + e * V, w);
+        for (int j = 0; j < V; ++j) w[j] *= y[k][j] * ry;
+        X::store(up + k * far, w);
       }
     }
-    if (++i == a.rows) { i = 0; ++m; }
+    if (++i == a.rows && r + 1 < r_end) {
+      i = 0;
+      ++m;
+      wp += a.width;
+      wn += a.width;
+      if (a.scale && block) c = a.scale[m];
+    }
   }
 }
-
-// acc += a b (column sums are fp32 or pairs of fp32)
-__device__ __forceinline__ void accumulate(F2& acc, F2 a, F2 b) { acc = fma(a, b, acc); }
-template <typename L> __device__ __forceinline__ void accumulate(float& acc, L a, L b) { acc += (float)(a * b); }
 
 // Sums of a row group, in the order in which a partial result holds them: next, post, gate (the ones that exist).
 // Up to 8 elements a thread, what the first pass over a row works out stays in registers for the second; the widest
@@ -420,11 +375,9 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_no
   pdl_prologue();
   extern __shared__ uint4 norm_ring[];
   typedef typename std::conditional<V == 1 && ITEMS == 1, double, float>::type A;
-  typedef typename std::conditional<V == 1, A, F2>::type L;           // a thread's values
-  typedef typename std::conditional<V == 1, float, F2>::type S;       // its column sums
   __shared__ A scratch[2 * 64];
   typedef Vec<T, V> X;
-  constexpr int N = V == 1 ? 1 : V / 2, kStages = norm_stages<V, ITEMS, 5, THREADS>();
+  constexpr int kStages = norm_stages<V, ITEMS, 5, THREADS>();
   constexpr bool kKeep = V * ITEMS <= 8;
   constexpr int kKept = kKeep ? ITEMS : 1;
   const int W = a.warps_per_row, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -440,67 +393,82 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_no
   ring.slot = (warp % W) * 32 + lane; ring.step = W * 32; ring.nv = a.width / V; ring.rows = a.rows; ring.group = group;
   ring.pitch = norm_pitch<T>(a.width);
   ring.slots = V > 1 ? norm_ring + threadIdx.x : norm_ring + group * (5 * ring.pitch / 16);
-  ring.m = m; ring.i = i; ring.left = (int)(r_end - r);
-  ring.set(kDy, a.dy, has_dy); ring.set(kDu, a.du, next); ring.set(kY, a.x, next);
-  ring.set(kBlock, a.block, block); ring.set(kGate, a.gate, gate);
+  ring.i = i; ring.left = (int)(r_end - r);
+  ring.set(kDy, a.dy, has_dy, m); ring.set(kDu, a.du, next, m); ring.set(kY, a.x, next, m);
+  ring.set(kBlock, a.block, block, m); ring.set(kGate, a.gate, gate, m);
 #pragma unroll
   for (int s = 0; s < kStages; ++s) ring.ask(s);
-  S acc_next[ITEMS][N], acc_post[ITEMS][N], acc_gate[ITEMS][N];
+  float acc_next[ITEMS][V], acc_post[ITEMS][V], acc_gate[ITEMS][V];
   float acc_scale = 0.f;
 #pragma unroll
   for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
-    for (int j = 0; j < N; ++j) acc_next[k][j] = acc_post[k][j] = acc_gate[k][j] = all<S>(0.f);
+    for (int j = 0; j < V; ++j) acc_next[k][j] = acc_post[k][j] = acc_gate[k][j] = 0.f;
+  const int first = ring.slot * V, far = ring.step * V;      // this thread's first element and the distance to its next vector
+  T* dx = reinterpret_cast<T*>(a.dx) + r * a.width + first;
+  T* dblock = reinterpret_cast<T*>(a.dblock) + r * a.width + first;
+  T* dgate = reinterpret_cast<T*>(a.dgate) + r * a.width + first;
+  const float* rstd_next = a.rstd_next + r;
+  const float* rstd_block = a.rstd_block + r;
+  // the weights of the member at hand; the variant that keeps its values keeps these, too
+  A w_next[kKept][V], w_post[kKept][V];
+  A c = 1;
+  auto member = [&]() {
+    if (a.scale && block) c = a.scale[m];
+    if constexpr (kKeep) {
+#pragma unroll
+      for (int k = 0; k < ITEMS; ++k) {
+        if (ring.slot + k * ring.step >= ring.nv) continue;
+        if (next) load_weights<V>(a.next_weight + (long long)m * a.width + first + k * far, w_next[k]);
+        if (block) load_weights<V>(a.post_weight + (long long)m * a.width + first + k * far, w_post[k]);
+      }
+    }
+  };
+  member();
   int turn = 0, stage = 0;
   for (; r < r_end; ++r) {
-    const long long at = r * a.width;
-    const float* wn = a.next_weight + (long long)m * a.width;
-    const float* wp = a.post_weight + (long long)m * a.width;
-    const A c = a.scale ? a.scale[m] : 1.f;
-    const A ry = next ? a.rstd_next[r] : 0.f, rb = block ? a.rstd_block[r] : 0.f;
-    const L lry = all<L>(ry), lrb = all<L>(rb);
-    ring.wait();
-    L sum_h = all<L>(0.f), sum_t = all<L>(0.f), sum_y = all<L>(0.f);   // r_y dh yh, p (dy + r_y dh), p yh, with p = g w_post v
-    L t[kKept][N], yh[kKept][N], open[kKept][N], v[kKept][N], w[kKept][N];   // dy + r_y dh, yh, sigmoid(z), v, w_post
-    // the vectors k of the row; `first`: with the sums that do not wait for the reduction
-    auto values = [&](int k, int to, bool first) {
-      const int e = ring.slot + k * ring.step;
+    const A ry = next ? *rstd_next : 0.f, rb = block ? *rstd_block : 0.f;
+        ring.wait();
+    A sums[3] = {0, 0, 0};                                     // r_y dh yh, p (dy + r_y dh), p yh, with p = g w_post v
+    A t[kKept][V], yh[kKept][V], open[kKept][V], v[kKept][V];   // dy + r_y dh, yh, sigmoid(z), v
+    // the vectors k of the row; `once`: with the sums that do not wait for the reduction
+    auto values = [&](int k, int to, bool once) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) t[to][j] = yh[to][j] = all<L>(0.f);
-      if (has_dy) ring.get(m, i, stage, kDy, k, t[to]);
+      for (int j = 0; j < V; ++j) t[to][j] = yh[to][j] = 0;
+      if (has_dy) ring.get(stage, kDy, k, t[to]);
       if (next) {
-        L du[N], u[N];
-        ring.get(m, i, stage, kDu, k, du);
-        ring.get(m, i, stage, kY, k, yh[to]);
-        load_weights<V>(wn + e * V, u);
+        A du[V];
+        ring.get(stage, kDu, k, du);
+        ring.get(stage, kY, k, yh[to]);
+        if constexpr (!kKeep) load_weights<V>(a.next_weight + (long long)m * a.width + first + k * far, w_next[to]);
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-          yh[to][j] = mul(yh[to][j], lry);
-          if (first) accumulate(acc_next[k][j], du[j], yh[to][j]);
-          u[j] = mul(mul(du[j], lry), u[j]);
-          if (first) sum_h = fma(u[j], yh[to][j], sum_h);
-          t[to][j] = add(t[to][j], u[j]);
+        for (int j = 0; j < V; ++j) {
+          yh[to][j] *= ry;
+          if (once) acc_next[k][j] += (float)(du[j] * yh[to][j]);
+          du[j] *= ry * w_next[to][j];
+          if (once) sums[0] += du[j] * yh[to][j];
+          t[to][j] += du[j];
         }
       }
       if (block) {
-        ring.get(m, i, stage, kBlock, k, v[to]);
-        load_weights<V>(wp + e * V, w[to]);
+        ring.get(stage, kBlock, k, v[to]);
+        if constexpr (!kKeep) load_weights<V>(a.post_weight + (long long)m * a.width + first + k * far, w_post[to]);
         if (gate) {
-          L z[N];
-          ring.get(m, i, stage, kGate, k, z);
+          A z[V];
+          ring.get(stage, kGate, k, z);
 #pragma unroll
-          for (int j = 0; j < N; ++j) open[to][j] = opened(z[j]);
+          for (int j = 0; j < V; ++j) open[to][j] = opened((float)z[j]);
         } else {
 #pragma unroll
-          for (int j = 0; j < N; ++j) open[to][j] = all<L>(1.f);
+          for (int j = 0; j < V; ++j) open[to][j] = 1;
         }
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-          v[to][j] = mul(v[to][j], lrb);
-          if (first) {
-            const L p = mul(mul(v[to][j], w[to][j]), open[to][j]);
-            sum_t = fma(p, t[to][j], sum_t);
-            sum_y = fma(p, yh[to][j], sum_y);
+        for (int j = 0; j < V; ++j) {
+          v[to][j] *= rb;
+          if (once) {
+            const A p = v[to][j] * w_post[to][j] * open[to][j];
+            sums[1] += p * t[to][j];
+            sums[2] += p * yh[to][j];
           }
         }
       }
@@ -508,55 +476,62 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_no
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k)
       if (ring.slot + k * ring.step < ring.nv) values(k, kKeep ? k : 0, true);
-    A sums[3] = {total(sum_h), total(sum_t), total(sum_y)};
+    if constexpr (kKeep) {          // the row has left the stage
+      ring.ask(stage);
+      if (++stage == kStages) stage = 0;
+    }
     row_sum3(sums, W, group, scratch, turn);
-    const A t1 = sums[0] / a.width;                                             // r_y t1
-    const L lt1 = all<L>(-t1), lt2 = all<L>(-c * rb * (sums[1] - t1 * sums[2]) / a.width);   // -r_y t1, -c r_b t2
-    const L lc = all<L>(c), lcrb = all<L>(c * rb), one = all<L>(1.f), minus = all<L>(-1.f);
+    const A share = (A)1 / a.width;
+    const A t1 = sums[0] * share;                                             // r_y t1
+    const A crb = c * rb, t2 = crb * (sums[1] - t1 * sums[2]) * share;          // c r_b t2
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
-      const int e = ring.slot + k * ring.step, from = kKeep ? k : 0;
-      if (e >= ring.nv) continue;
+      const int from = kKeep ? k : 0;
+      if (ring.slot + k * ring.step >= ring.nv) continue;
       if constexpr (!kKeep) values(k, 0, false);
 #pragma unroll
-      for (int j = 0; j < N; ++j) t[from][j] = fma(yh[from][j], lt1, t[from][j]);
-      X::store(reinterpret_cast<T*>(a.dx) + at + e * V, t[from]);
+      for (int j = 0; j < V; ++j) t[from][j] -= yh[from][j] * t1;
+      X::store(dx + k * far, t[from]);
       if (block) {
-        L db[N], dz[N], o_sum = all<L>(0.f);
+        A db[V], dz[V];
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-          const L gdx = mul(open[from][j], t[from][j]), gwdx = mul(gdx, w[from][j]), o = mul(gwdx, v[from][j]);
-          accumulate(acc_post[k][j], mul(lc, gdx), v[from][j]);
-          o_sum = add(o_sum, o);
-          db[j] = fma(lcrb, gwdx, mul(v[from][j], lt2));
-          dz[j] = mul(mul(lc, o), fma(minus, open[from][j], one));
+        for (int j = 0; j < V; ++j) {
+          const A gdx = open[from][j] * t[from][j], gwdx = gdx * w_post[from][j], o = gwdx * v[from][j];
+          acc_post[k][j] += (float)(c * gdx * v[from][j]);
+          acc_scale += (float)o;
+          db[j] = crb * gwdx - v[from][j] * t2;
+          dz[j] = c * o * (1 - open[from][j]);
         }
-        acc_scale += (float)total(o_sum);
-        X::store(reinterpret_cast<T*>(a.dblock) + at + e * V, db);
+        X::store(dblock + k * far, db);
         if (vector) {
 #pragma unroll
-          for (int j = 0; j < N; ++j) accumulate(acc_gate[k][j], dz[j], one);
+          for (int j = 0; j < V; ++j) acc_gate[k][j] += (float)dz[j];
         } else if (gate) {
-          X::store(reinterpret_cast<T*>(a.dgate) + at + e * V, dz);
+          X::store(dgate + k * far, dz);
         }
       }
     }
-    ring.ask(stage);
-    if (++stage == kStages) stage = 0;
+    if constexpr (!kKeep) {
+      ring.ask(stage);
+      if (++stage == kStages) stage = 0;
+    }
+    dx += a.width;
+    dblock += a.width;
+    dgate += a.width;
+    ++rstd_next;
+    ++rstd_block;
     if (++i < a.rows && r + 1 < r_end) continue;
     // the last row here of this member: leave its sums.  The pairs (row group, member) ascend in g + m.
-    float* out = a.partial + (long long)(g + m) * a.sums * a.width;
+    float* out = a.partial + (long long)(g + m) * a.sums * a.width + first;
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
-      const int e = ring.slot + k * ring.step;
-      if (e >= ring.nv) continue;
-      float* o = out + e * V;
-      auto leave = [&](S* acc) {
+      if (ring.slot + k * ring.step >= ring.nv) continue;
+      float* o = out + k * far;
+      auto leave = [&](float* acc) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-          if constexpr (V == 1) { o[j] = acc[j]; }
-          else { const float2 f = split(acc[j]); o[2 * j] = f.x; o[2 * j + 1] = f.y; }
-          acc[j] = all<S>(0.f);
+        for (int j = 0; j < V; ++j) {
+          o[j] = acc[j];
+          acc[j] = 0.f;
         }
         o += a.width;
       };
@@ -572,6 +547,7 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_no
     }
     i = 0;
     ++m;
+    if (r + 1 < r_end) member();
   }
 }
 
@@ -686,13 +662,6 @@ void norm_fill(NormArgs* a, const pbt_block_norm_desc* d) {
   a->y = (char*)d->y; a->u = (char*)d->u; a->rstd_block = d->rstd_block; a->rstd_next = d->rstd_next;
   a->dx = (char*)d->dx; a->dblock = (char*)d->dblock; a->dgate = (char*)d->dgate;
   a->dpost = d->dpost_weight; a->dnext = d->dnext_weight; a->dscale = d->dscale;
-}
-
-// Warps of a row and rows of a block for `items` vectors per thread.
-void norm_shape(int width, int v, int items, int* warps, int* groups) {
-  const int nv = width / v;
-  *warps = std::max(1, (nv + items * 32 - 1) / (items * 32));
-  *groups = std::max(1, kNormThreads / 32 / *warps);
 }
 
 // Elements of a thread (`items` vectors) and warps of a row.  Forward: 16 elements a thread before a row takes another warp
