@@ -68,6 +68,9 @@ __device__ __forceinline__ uint4 ld16(const bf16* p) {
   asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
   return r;
 }
+__device__ __forceinline__ void copy16(void* slot, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(slot)), "l"(from) : "memory");
+}
 __device__ __forceinline__ void mma16816(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -88,13 +91,21 @@ __device__ __forceinline__ void store_terms(bf16* row, int rp, int col, float v,
 // A warp multiplies 32 rows by the adapter's matrix over every `parts`-th block of 64 columns.  The columns of a block are
 // dealt to the fragments in the order in which 16-byte loads deliver them (lane t of a quad holds columns 8t .. 8t+7 of
 // each half block); the sum over k does not mind, as long as both operands use the same order.  B_a lies with its ranks
-// contiguous, so its fragments are transposed on the way: 64 rows of it go through shared memory, stored so that the
+// contiguous, so its fragments are transposed on the way: 64 rows of it lie in shared memory in an order in which the
 // eight rows one ldmatrix takes are 128 consecutive bytes.
+// What bounds it is the bytes in flight: the blocks come through shared memory (cp.async, a warp's own ring of kShrinkStages
+// blocks, every lane reading back what it copied itself), 2 x 96 KB per SM at rank 16.
+template <int NT> struct ShrinkRing {
+  static constexpr int kStages = NT <= 2 ? 2 : NT == 4 ? 3 : 2;    // two CTAs of an SM share 227 KB up to rank 16, one beyond
+  static constexpr int kBytes = 4096 + NT * 1024;                  // a block of a warp: 32 rows of x, 8 NT rows of the matrix
+  static constexpr int kTotal = 8 * kStages * kBytes;
+};
 template <bool TRANS, int NT>
-__global__ void __launch_bounds__(256) k_adapter_shrink(const ShrinkArgs a) {
+__global__ void __launch_bounds__(256, NT <= 2 ? 2 : 1) k_adapter_shrink(const ShrinkArgs a) {
   pdl_prologue();
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (k_adapter_rows may begin with its own operand)
   extern __shared__ __align__(16) uint8_t shrink_smem[];
+  typedef ShrinkRing<NT> Ring;
   const int q = blockIdx.x, tid = threadIdx.x;
   const Segments& g = a.segs;
   if (q >= a.n_tiles + g.n) {
@@ -131,37 +142,67 @@ __global__ void __launch_bounds__(256) k_adapter_shrink(const ShrinkArgs a) {
     in[i] = row < hi;
     xrow[i] = a.x + (long long)row * a.ldx;
   }
-  uint8_t* stage = shrink_smem + warp * (NT * 1024);
-  const uint32_t stage_addr = smem_u32(stage);
+  uint8_t* ring = shrink_smem + warp * (Ring::kStages * Ring::kBytes);
+  // rows behind the tile are never copied: zero
   const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-  float acc[2][NT][4] = {};
-  for (int k0 = part * 64; k0 < a.K; k0 += parts * 64) {
-    uint4 xv[4][2], bv[TRANS ? 1 : NT][2];
+#pragma unroll
+  for (int s = 0; s < Ring::kStages; ++s)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int k = k0 + h * 32 + tq * 8;
+      uint8_t* to = ring + s * Ring::kBytes + h * 512 + lane * 16;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) xv[i][h] = in[i] && k < a.K ? ld16(xrow[i] + k) : zero;
-      if constexpr (!TRANS) {
+      for (int i = 0; i < 4; ++i)
+        if (!in[i]) *reinterpret_cast<uint4*>(to + i * 1024) = zero;
+    }
+  auto ask = [&](int k0, int s) {
+    uint8_t* to = ring + s * Ring::kBytes;
+    if (k0 < a.K) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const int r = n * 8 + gr;
-          bv[n][h] = r < a.rank && k < a.K ? __ldg(reinterpret_cast<const uint4*>(mat + (long long)r * a.pitch + k)) : zero;
+      for (int h = 0; h < 2; ++h) {
+        const int k = k0 + h * 32 + tq * 8;
+        if (k < a.K) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (in[i]) copy16(to + (2 * i + h) * 512 + lane * 16, xrow[i] + k);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(to + (2 * i + h) * 512 + lane * 16) = zero;     // behind the last column
+        }
+        if constexpr (!TRANS) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            const int r = n * 8 + gr;
+            uint8_t* slot = to + 4096 + (2 * n + h) * 512 + lane * 16;
+            if (r < a.rank && k < a.K) copy16(slot, mat + (long long)r * a.pitch + k);
+            else *reinterpret_cast<uint4*>(slot) = zero;
+          }
+        }
+      }
+      if constexpr (TRANS) {
+        for (int p = lane; p < 64 * nt8; p += 32) {
+          const int k = p / nt8, n = p % nt8;
+          uint8_t* slot = to + 4096 + n * 1024 + ((k & 32) + (k & 7) * 4 + ((k & 31) >> 3)) * 16;
+          if (k0 + k < a.K) copy16(slot, mat + (long long)(k0 + k) * a.pitch + n * 8);
+          else *reinterpret_cast<uint4*>(slot) = zero;
         }
       }
     }
-    if constexpr (TRANS) {
-      __syncwarp();   // the previous block's fragments have been read
-      for (int p = lane; p < 64 * nt8; p += 32) {
-        const int k = p / nt8, n = p % nt8;
-        const uint4 v = k0 + k < a.K ? __ldg(reinterpret_cast<const uint4*>(mat + (long long)(k0 + k) * a.pitch) + n) : zero;
-        *reinterpret_cast<uint4*>(stage + n * 1024 + ((k & 32) + (k & 7) * 4 + ((k & 31) >> 3)) * 16) = v;
-      }
-      __syncwarp();
-    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int s = 0; s < Ring::kStages; ++s) ask(part * 64 + s * parts * 64, s);
+  float acc[2][NT][4] = {};
+  int stage = 0;
+  for (int k0 = part * 64; k0 < a.K; k0 += parts * 64) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(Ring::kStages - 1) : "memory");
+    if constexpr (TRANS) __syncwarp();   // the other lanes' part of the matrix
+    const uint8_t* from = ring + stage * Ring::kBytes;
     float sum[2][NT][4] = {};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
+      uint4 xv[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) xv[i] = *reinterpret_cast<const uint4*>(from + (2 * i + h) * 512 + lane * 16);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         if (n >= nt8) continue;
@@ -169,18 +210,22 @@ __global__ void __launch_bounds__(256) k_adapter_shrink(const ShrinkArgs a) {
         if constexpr (TRANS) {
           // matrix m = lane / 8 holds, for step m / 2 and half m % 2, row 2t + e: column 8t + 4 (m / 2) + 2 (m % 2) + e of the block
           const int m = lane >> 3, c = lane & 7;
-          ldmatrix4_trans(b, stage_addr + n * 1024 + (h * 32 + (4 * (m >> 1) + 2 * (m & 1) + (c & 1)) * 4 + (c >> 1)) * 16);
+          ldmatrix4_trans(b, smem_u32(from) + 4096 + n * 1024 + (h * 32 + (4 * (m >> 1) + 2 * (m & 1) + (c & 1)) * 4 + (c >> 1)) * 16);
         } else {
-          b[0] = bv[n][h].x; b[1] = bv[n][h].y; b[2] = bv[n][h].z; b[3] = bv[n][h].w;
+          const uint4 bv = *reinterpret_cast<const uint4*>(from + 4096 + (2 * n + h) * 512 + lane * 16);
+          b[0] = bv.x; b[1] = bv.y; b[2] = bv.z; b[3] = bv.w;
         }
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
           for (int m = 0; m < 2; ++m)
-            mma16816(sum[m][n], word(xv[2 * m][h], 2 * s), word(xv[2 * m + 1][h], 2 * s), word(xv[2 * m][h], 2 * s + 1),
-                     word(xv[2 * m + 1][h], 2 * s + 1), b[2 * s], b[2 * s + 1]);
+            mma16816(sum[m][n], word(xv[2 * m], 2 * s), word(xv[2 * m + 1], 2 * s), word(xv[2 * m], 2 * s + 1), word(xv[2 * m + 1], 2 * s + 1),
+                     b[2 * s], b[2 * s + 1]);
       }
     }
+    if constexpr (TRANS) __syncwarp();   // every lane has read the block
+    ask(k0 + Ring::kStages * parts * 64, stage);
+    if (++stage == Ring::kStages) stage = 0;
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -188,7 +233,7 @@ __global__ void __launch_bounds__(256) k_adapter_shrink(const ShrinkArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[m][n][e] += sum[m][n][e];
   }
-  __syncthreads();   // the staging memory becomes the parts' sums: [warp][32 rows][8 NT]
+  __syncthreads();   // the rings' memory becomes the parts' sums: [warp][32 rows][8 NT]
   float* red = reinterpret_cast<float*>(shrink_smem);
 #pragma unroll
   for (int m = 0; m < 2; ++m)
@@ -219,9 +264,9 @@ template <bool TRANS, int NT>
 cudaError_t launch_shrink(const ShrinkArgs& a, unsigned grid, cudaStream_t s) {
   static DeviceSetup setup;
   int sms = 0;
-  const cudaError_t e = device_setup(&setup, k_adapter_shrink<TRANS, NT>, NT * 8192, &sms);
+  const cudaError_t e = device_setup(&setup, k_adapter_shrink<TRANS, NT>, ShrinkRing<NT>::kTotal, &sms);
   if (e != cudaSuccess) return e;
-  return launch_with(grid, 256, NT * 8192, s)(k_adapter_shrink<TRANS, NT>, a);
+  return launch_with(grid, 256, ShrinkRing<NT>::kTotal, s)(k_adapter_shrink<TRANS, NT>, a);
 }
 template <bool TRANS>
 cudaError_t launch_shrink(ShrinkArgs a, cudaStream_t s) {
@@ -607,8 +652,8 @@ constexpr int kGradStages = 4, kGradChunk = 512, kGradList = 1024;
 
 struct GradArgs {
   Segments segs;
-  int rank, rp, boxes, term_cols;      // boxes of 64 columns of the planes; term_cols = 3 rp
-  int K, N, blocks_k;                  // column blocks of dA come first, those of dB after them
+  int rank;
+  int K, N, blocks_k, blocks_n;        // column blocks of dA come first, those of dB after them
   int splits;
   float *dA, *dB;                      // [splits][adapters][...]: the results themselves when splits == 1
   long long stride_a, stride_b;        // elements of one split
@@ -621,16 +666,20 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
   return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag));
 }
 
-// One CTA: 128 columns of v (x for dA, dy for dB) of one adapter, over every splits-th chunk of 512 rows of it.  The 128
-// columns are the accumulator's lanes, its columns the three summands of the r ranks.  Both operands are read as they lie
-// (rows = contraction index: MN-major).  Where a block of 64 rows ends inside a segment's last box, the rows behind the
-// end (another member's) are cleared in shared memory in both operands before the MMA reads them.
-__global__ void __launch_bounds__(192) k_adapter_grad(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmDS,
+// A CTA works for one adapter (and, when there are splits, on every splits-th chunk of 512 of its rows) and takes column
+// blocks in turn: 128 columns of v (x for dA, dy for dB) are the accumulator's lanes, its columns the three summands of the
+// r ranks.  Both operands are read as they lie (rows = contraction index: MN-major).  Where a block of 64 rows ends
+// inside a box, the rows behind the end (another member's) are cleared in shared memory in both operands before the MMA
+// reads them.  The producer runs ahead into the next column block while the last one is drained, so that two CTAs per SM
+// keep 4 x 24 KB each on their way throughout (with a CTA per column block, 136 us at 80 members x 512 rows x 2048: the
+// pipeline filled and drained 2560 times).
+template <int RP>
+__global__ void __launch_bounds__(192, 2) k_adapter_grad(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmDS,
                                                       const __grid_constant__ CUtensorMap tmDY, const __grid_constant__ CUtensorMap tmS, const GradArgs a) {
   pdl_prologue();
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  const int stage_bytes = 16384 + a.boxes * 8192;
+  constexpr int kBoxes = (3 * RP + 63) / 64, stage_bytes = 16384 + kBoxes * 8192;
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + kGradStages * stage_bytes);
   uint64_t* empty = full + kGradStages;
   uint64_t* tfull = empty + kGradStages;
@@ -642,10 +691,6 @@ __global__ void __launch_bounds__(192) k_adapter_grad(const __grid_constant__ CU
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int adapter = blockIdx.y, z = blockIdx.z;
-  const bool is_b = (int)blockIdx.x >= a.blocks_k;
-  const int c0 = ((int)blockIdx.x - (is_b ? a.blocks_k : 0)) * 128;
-  const CUtensorMap* tmV = is_b ? &tmDY : &tmX;
-  const CUtensorMap* tmT = is_b ? &tmS : &tmDS;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kGradStages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 4); }
@@ -662,12 +707,11 @@ __global__ void __launch_bounds__(192) k_adapter_grad(const __grid_constant__ CU
   uint32_t stage = 0, phase = 0;   // producer, MMA warp
   int folds = 0;                   // MMA warp, epilogue: accumulators handed over so far
   bool ok = true;
-  float acc[kMaxRank];
-#pragma unroll
-  for (int i = 0; i < kMaxRank; ++i) acc[i] = 0.f;
+  const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)((3 * RP) >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 
-  // The adapter's segments, kGradList table entries at a time, as a list of row ranges in shared memory.
-  for (int base = 0; base < a.segs.n; base += kGradList) {
+  // The adapter's segments, kGradList table entries at a time, as a list of row ranges in shared memory.  One pass does for
+  // up to 1024 segments; later passes add to what the earlier ones left in dA and dB.
+  for (int base = 0; base == 0 || base < a.segs.n; base += kGradList) {
     __syncthreads();
     if (warp == 0) {
       int n = 0;
@@ -688,81 +732,100 @@ __global__ void __launch_bounds__(192) k_adapter_grad(const __grid_constant__ CU
     for (int i = 0; i < n; ++i)
       for (int t = list[i].x / kGradChunk; t * kGradChunk < list[i].y; ++t)
         if (t % a.splits == z) blocks += (min(list[i].y, (t + 1) * kGradChunk) - max(list[i].x, t * kGradChunk) + 63) / 64;
+    if (base > 0 && !blocks) continue;
 
-    if (warp == 0) {
-      if (lane == 0 && ok) {
+    for (int column = blockIdx.x; column < a.blocks_k + a.blocks_n && ok; column += gridDim.x) {
+      const bool is_b = column >= a.blocks_k;
+      const int c0 = (column - (is_b ? a.blocks_k : 0)) * 128;
+      if (warp == 0) {
+        if (lane == 0) {
+          const CUtensorMap* tmV = is_b ? &tmDY : &tmX;
+          const CUtensorMap* tmT = is_b ? &tmS : &tmDS;
+          for (int i = 0; i < n && ok; ++i)
+            for (int t = list[i].x / kGradChunk; t * kGradChunk < list[i].y && ok; ++t) {
+              if (t % a.splits != z) continue;
+              const int end = min(list[i].y, (t + 1) * kGradChunk);
+              for (int row = max(list[i].x, t * kGradChunk); row < end; row += 64) {
+                if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) { ok = false; break; }
+                uint8_t* sv = smem + stage * stage_bytes;
+                mbar_expect_tx(&full[stage], stage_bytes);
+                tma_load_3d(sv, tmV, &full[stage], c0, row, 0);
+                tma_load_3d(sv + 8192, tmV, &full[stage], c0 + 64, row, 0);
+                for (int b = 0; b < kBoxes; ++b) tma_load_3d(sv + 16384 + b * 8192, tmT, &full[stage], b * 64, row, 0);
+                if (++stage == kGradStages) { stage = 0; phase ^= 1; }
+              }
+            }
+        }
+        ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
+      } else if (warp == 1) {
+        int done = 0;
         for (int i = 0; i < n && ok; ++i)
           for (int t = list[i].x / kGradChunk; t * kGradChunk < list[i].y && ok; ++t) {
             if (t % a.splits != z) continue;
             const int end = min(list[i].y, (t + 1) * kGradChunk);
-            for (int row = max(list[i].x, t * kGradChunk); row < end; row += 64) {
-              if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) { ok = false; break; }
+            for (int row = max(list[i].x, t * kGradChunk); row < end; row += 64, ++done) {
+              const int acc_buf = folds & 1;
+              if ((done & 1) == 0) {
+                if (!warp_wait(&tempty[acc_buf], ((folds >> 1) & 1) ^ 1, abort_flag)) { ok = false; break; }
+              }
+              if (!warp_wait(&full[stage], phase, abort_flag)) { ok = false; break; }
               uint8_t* sv = smem + stage * stage_bytes;
-              mbar_expect_tx(&full[stage], stage_bytes);
-              tma_load_3d(sv, tmV, &full[stage], c0, row, 0);
-              tma_load_3d(sv + 8192, tmV, &full[stage], c0 + 64, row, 0);
-              for (int b = 0; b < a.boxes; ++b) tma_load_3d(sv + 16384 + b * 8192, tmT, &full[stage], b * 64, row, 0);
+              const int valid = end - row;
+              if (valid < 64) {   // rows are 128-byte lines of each box
+                for (int b = 0; b < 2 + kBoxes; ++b)
+                  for (int o = valid * 8 + lane; o < 64 * 8; o += 32) reinterpret_cast<uint4*>(sv + b * 8192)[o] = make_uint4(0u, 0u, 0u, 0u);
+                fence_async_smem();
+                __syncwarp();
+              }
+              if (lane == 0) {
+                tc_fence_after();
+                const uint32_t sa = smem_u32(sv), sb = sa + 16384;
+                const uint32_t tmem_d = tmem_base + (uint32_t)(acc_buf * (3 * RP));
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                  umma_bf16(tmem_d, smem_desc(sa + k * 2048, 8192, 1024), smem_desc(sb + k * 2048, 8192, 1024), idesc, ((done & 1) | k) != 0 ? 1u : 0u);
+                umma_commit(&empty[stage]);
+                if ((done & 1) == 1 || done + 1 == blocks) umma_commit(&tfull[acc_buf]);
+              }
+              __syncwarp();
+              if ((done & 1) == 1 || done + 1 == blocks) ++folds;
               if (++stage == kGradStages) { stage = 0; phase ^= 1; }
             }
           }
-      }
-    } else if (warp == 1) {
-      const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(a.term_cols >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
-      int done = 0;
-      for (int i = 0; i < n && ok; ++i)
-        for (int t = list[i].x / kGradChunk; t * kGradChunk < list[i].y && ok; ++t) {
-          if (t % a.splits != z) continue;
-          const int end = min(list[i].y, (t + 1) * kGradChunk);
-          for (int row = max(list[i].x, t * kGradChunk); row < end; row += 64, ++done) {
-            const int acc_buf = folds & 1;
-            if ((done & 1) == 0) {
-              if (!warp_wait(&tempty[acc_buf], ((folds >> 1) & 1) ^ 1, abort_flag)) { ok = false; break; }
-            }
-            if (!warp_wait(&full[stage], phase, abort_flag)) { ok = false; break; }
-            uint8_t* sv = smem + stage * stage_bytes;
-            const int valid = end - row;
-            if (valid < 64) {   // rows are 128-byte lines of each box
-              for (int b = 0; b < 2 + a.boxes; ++b)
-                for (int o = valid * 8 + lane; o < 64 * 8; o += 32) reinterpret_cast<uint4*>(sv + b * 8192)[o] = make_uint4(0u, 0u, 0u, 0u);
-              fence_async_smem();
-              __syncwarp();
-            }
-            if (lane == 0) {
-              tc_fence_after();
-              const uint32_t sa = smem_u32(sv), sb = sa + 16384;
-              const uint32_t tmem_d = tmem_base + (uint32_t)(acc_buf * a.term_cols);
+      } else {
+        const int q = warp & 3;
+        float acc[RP];
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                umma_bf16(tmem_d, smem_desc(sa + k * 2048, 8192, 1024), smem_desc(sb + k * 2048, 8192, 1024), idesc, ((done & 1) | k) != 0 ? 1u : 0u);
-              umma_commit(&empty[stage]);
-              if ((done & 1) == 1 || done + 1 == blocks) umma_commit(&tfull[acc_buf]);
-            }
-            __syncwarp();
-            if ((done & 1) == 1 || done + 1 == blocks) ++folds;
-            if (++stage == kGradStages) { stage = 0; phase ^= 1; }
+        for (int i = 0; i < RP; ++i) acc[i] = 0.f;
+        for (int f = 0; f < (blocks + 1) / 2 && ok; ++f, ++folds) {
+          const int acc_buf = folds & 1;
+          if (!warp_wait(&tfull[acc_buf], (folds >> 1) & 1, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t t0 = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc_buf * (3 * RP));
+#pragma unroll
+          for (int c = 0; c < RP; c += 16) {
+            uint32_t h[16], m[16], l[16];
+            tmem_ld16(t0 + c, h);
+            tmem_ld16(t0 + RP + c, m);
+            tmem_ld16(t0 + 2 * RP + c, l);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[c + i] += __uint_as_float(h[i]) + (__uint_as_float(m[i]) + __uint_as_float(l[i]));
           }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&tempty[acc_buf]);
         }
-    } else {
-      const int q = warp & 3;
-      for (int f = 0; f < (blocks + 1) / 2 && ok; ++f, ++folds) {
-        const int acc_buf = folds & 1;
-        if (!warp_wait(&tfull[acc_buf], (folds >> 1) & 1, abort_flag)) { ok = false; break; }
-        tc_fence_after();
-        const uint32_t t0 = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc_buf * a.term_cols);
+        const int col = c0 + q * 32 + lane;
+        if (ok && col < (is_b ? a.N : a.K)) {
+          // dA [rank][K]: a warp's lanes are neighbours; dB [N][rank]: a lane's ranks are
+          float* o = is_b ? a.dB + z * a.stride_b + ((long long)adapter * a.N + col) * a.rank
+                          : a.dA + z * a.stride_a + (long long)adapter * a.rank * a.K + col;
+          const long long step = is_b ? 1 : a.K;
 #pragma unroll
-        for (int c = 0; c < kMaxRank; c += 16) {
-          if (c >= a.rp) continue;
-          uint32_t h[16], m[16], l[16];
-          tmem_ld16(t0 + c, h);
-          tmem_ld16(t0 + a.rp + c, m);
-          tmem_ld16(t0 + 2 * a.rp + c, l);
-          tmem_ld_wait();
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[c + i] += __uint_as_float(h[i]) + (__uint_as_float(m[i]) + __uint_as_float(l[i]));
+          for (int i = 0; i < RP; ++i)
+            if (i < a.rank) o[i * step] = base > 0 ? o[i * step] + acc[i] : acc[i];
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&tempty[acc_buf]);
       }
     }
   }
@@ -777,23 +840,21 @@ __global__ void __launch_bounds__(192) k_adapter_grad(const __grid_constant__ CU
       if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) break;
       if (++stage == kGradStages) { stage = 0; phase ^= 1; }
     }
-  if (warp >= 2) {
-    const int col = c0 + (warp & 3) * 32 + lane;
-    if (!is_b && col < a.K) {
-      float* o = a.dA + z * a.stride_a + (long long)adapter * a.rank * a.K + col;
-#pragma unroll
-      for (int i = 0; i < kMaxRank; ++i)
-        if (i < a.rank) o[(long long)i * a.K] = acc[i];
-    } else if (is_b && col < a.N) {
-      float* o = a.dB + z * a.stride_b + ((long long)adapter * a.N + col) * a.rank;
-#pragma unroll
-      for (int i = 0; i < kMaxRank; ++i)
-        if (i < a.rank) o[i] = acc[i];
-    }
-  }
   tc_fence_before();
   __syncthreads();
   if (warp == 1) tmem_dealloc(tmem_base, a.tmem_cols);
+}
+
+template <int RP>
+cudaError_t launch_grad(const CUtensorMap& x, const CUtensorMap& ds, const CUtensorMap& dy, const CUtensorMap& kept, const GradArgs& g, cudaStream_t st) {
+  constexpr int kSmem = kGradStages * (16384 + (3 * RP + 63) / 64 * 8192) + 256 + kGradList * 8 + 1024;
+  static_assert(kSmem <= 232448, "shared memory budget of one CTA");
+  static DeviceSetup setup;
+  int sms = 0;
+  const cudaError_t e = device_setup(&setup, k_adapter_grad<RP>, kSmem, &sms);
+  if (e != cudaSuccess) return e;
+  const int work = g.segs.n_adapters * g.splits, per = (2 * sms + work - 1) / work;      // two CTAs per SM over all adapters and splits
+  return launch_with(dim3(std::min(per, g.blocks_k + g.blocks_n), g.segs.n_adapters, g.splits), 192, kSmem, st)(k_adapter_grad<RP>, x, ds, dy, kept, g);
 }
 
 // out = the splits' partial results, added in order
@@ -925,8 +986,8 @@ cudaError_t tc_backward(const pbt_adapter_desc* d, const Segments& segs, char* w
 
   GradArgs g;
   memset(&g, 0, sizeof(g));
-  g.segs = segs; g.rank = d->rank; g.rp = p.rp; g.term_cols = width; g.boxes = (width + 63) / 64;
-  g.K = d->inputs; g.N = d->outputs; g.blocks_k = (d->inputs + 127) / 128;
+  g.segs = segs; g.rank = d->rank;
+  g.K = d->inputs; g.N = d->outputs; g.blocks_k = (d->inputs + 127) / 128; g.blocks_n = (d->outputs + 127) / 128;
   g.splits = p.splits;
   g.stride_a = (long long)d->n_adapters * d->rank * d->inputs;
   g.stride_b = (long long)d->n_adapters * d->rank * d->outputs;
@@ -939,13 +1000,9 @@ cudaError_t tc_backward(const pbt_adapter_desc* d, const Segments& segs, char* w
   if (!make_map(&mx, x, d->inputs, d->rows, ldx, 1, 0, 64) || !make_map(&mdy, dy, d->outputs, d->rows, lddy, 1, 0, 64) ||
       !make_map(&mds, a.planes, width, d->rows, width, 1, 0, 64) || !make_map(&ms, a.kept_planes, width, d->rows, width, 1, 0, 64))
     return cudaErrorInvalidValue;
-  static DeviceSetup setup;
-  int sms = 0;
-  constexpr int kMost = kGradStages * (16384 + 3 * 8192) + 256 + kGradList * 8 + 1024;
-  static_assert(kMost <= 232448, "shared memory budget of one CTA");
-  STEP(device_setup(&setup, k_adapter_grad, kMost, &sms));
-  const size_t smem = kGradStages * (16384 + g.boxes * 8192) + 256 + kGradList * 8 + 1024;
-  STEP(launch_with(dim3(g.blocks_k + (d->outputs + 127) / 128, d->n_adapters, p.splits), 192, smem, st)(k_adapter_grad, mx, mds, mdy, ms, g));
+  const cudaError_t launched = p.rp == 16 ? launch_grad<16>(mx, mds, mdy, ms, g, st) : p.rp == 32 ? launch_grad<32>(mx, mds, mdy, ms, g, st)
+                             : p.rp == 48 ? launch_grad<48>(mx, mds, mdy, ms, g, st) : launch_grad<64>(mx, mds, mdy, ms, g, st);
+  STEP(launched);
   if (p.splits > 1) {
     const long long n = g.stride_a + g.stride_b;
     STEP(launch_with((unsigned)std::min<long long>((n + 255) / 256, 148 * 16), 256, 0, st)(k_adapter_grad_join, g.dA, g.dB, g.stride_a, g.stride_b, p.splits, d->dA, d->dB));
