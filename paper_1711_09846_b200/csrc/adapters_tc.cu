@@ -179,11 +179,16 @@ __global__ void __launch_bounds__(256, NT <= 2 ? 2 : 1) k_adapter_shrink(const S
         }
       }
       if constexpr (TRANS) {
-        for (int p = lane; p < 64 * nt8; p += 32) {
-          const int k = p / nt8, n = p % nt8;
+        auto row_piece = [&](int k, int n) {
           uint8_t* slot = to + 4096 + n * 1024 + ((k & 32) + (k & 7) * 4 + ((k & 31) >> 3)) * 16;
           if (k0 + k < a.K) copy16(slot, mat + (long long)(k0 + k) * a.pitch + n * 8);
           else *reinterpret_cast<uint4*>(slot) = zero;
+        };
+        if (nt8 == NT) {
+#pragma unroll
+          for (int p = 0; p < 2 * NT; ++p) row_piece((p * 32 + lane) / NT, (p * 32 + lane) % NT);
+        } else {
+          for (int p = lane; p < 64 * nt8; p += 32) row_piece(p / nt8, p % nt8);
         }
       }
     }
@@ -559,46 +564,79 @@ struct RowsArgs {
 };
 
 // y[t][n] for 16 columns n and all rows t: the eight warps take every eighth block of 64 inputs, W's rows are the tall
-// operand of mma.sync (16 x 16), eight rows of x the narrow one, both loaded in 16-byte pieces straight into fragments
-// (the order of the contraction index is the one the loads deliver, as in the shrink).  The warps' sums meet in shared
-// memory, where the low-rank part is added in fp32.  Launched while the shrink runs: only that last part waits for it.
+// operand of mma.sync (16 x 16), eight rows of x the narrow one, in the order of the contraction index that 16-byte loads
+// deliver (as in the shrink) and through the same kind of ring: a warp's own, every lane reading back what it copied.  With
+// plain loads the kernel waited for one group of rows of x after the other (64 rows, 2048 x 2048: 20 us against 8 us).
+// The warps' sums meet in shared memory, where the low-rank part is added in fp32.  Launched while the shrink runs: only that
+// last part waits for it.
+template <int GROUPS> struct RowsRing {
+  static constexpr int kStages = GROUPS == 8 ? 2 : GROUPS == 4 ? 3 : 4;
+  static constexpr int kVectors = 4 + 2 * GROUPS;                   // 16-byte vectors of a lane in a block of 64 inputs
+  static constexpr int kBytes = kVectors * 512;
+  static constexpr int kPitch = GROUPS * 8 + 1;                     // of the sums [8 warps][16 columns][rows]
+  static constexpr int kTotal = 8 * kStages * kBytes > 8 * kRowsOut * kPitch * 4 ? 8 * kStages * kBytes : 8 * kRowsOut * kPitch * 4;
+};
 template <int GROUPS>
 __global__ void __launch_bounds__(256) k_adapter_rows(const RowsArgs a) {
-  __shared__ float red[8][kRowsOut][GROUPS * 8 + 1];
+  extern __shared__ __align__(16) uint8_t rows_smem[];
+  typedef RowsRing<GROUPS> Ring;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gr = lane >> 2, tq = lane & 3;
   const int n0 = blockIdx.x * kRowsOut;
-  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-  float acc[GROUPS][4] = {};
-  const bf16* w0 = a.w + (long long)(n0 + gr) * a.ldw + tq * 8;
+  uint8_t* ring = rows_smem + warp * (Ring::kStages * Ring::kBytes) + lane * 16;
+  const bf16* w0 = a.w + (long long)(n0 + gr) * a.ldw;
   const bf16* w1 = w0 + 8 * a.ldw;
+  const bf16* x = a.x + gr * a.ldx;
   const bool in0 = n0 + gr < a.N, in1 = n0 + gr + 8 < a.N;
-  for (int k0 = warp * 64; k0 < a.K; k0 += 512) {
-    uint4 wv[2][2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const bool in = k0 + h * 32 + tq * 8 < a.K;
-      wv[0][h] = in && in0 ? ld16(w0 + k0 + h * 32) : zero;
-      wv[1][h] = in && in1 ? ld16(w1 + k0 + h * 32) : zero;
-    }
-#pragma unroll
-    for (int g = 0; g < GROUPS; ++g) {
-      const int t = g * 8 + gr;
-      float sum[4] = {};
+  auto put = [&](uint8_t* slot, const bf16* from, bool in) {
+    if (in) copy16(slot, from);
+    else *reinterpret_cast<uint4*>(slot) = make_uint4(0u, 0u, 0u, 0u);
+  };
+  auto ask = [&](int k0, int s) {
+    if (k0 < a.K) {
+      uint8_t* to = ring + s * Ring::kBytes;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int k = k0 + h * 32 + tq * 8;
-        const uint4 xv = t < a.T && k < a.K ? __ldg(reinterpret_cast<const uint4*>(a.x + t * a.ldx + k)) : zero;
+        const bool in = k < a.K;
+        put(to + h * 512, w0 + k, in && in0);
+        put(to + (2 + h) * 512, w1 + k, in && in1);
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) put(to + (4 + 2 * g + h) * 512, x + g * 8 * a.ldx + k, in && g * 8 + gr < a.T);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int s = 0; s < Ring::kStages; ++s) ask(warp * 64 + s * 512, s);
+  float acc[GROUPS][4] = {};
+  int stage = 0;
+  for (int k0 = warp * 64; k0 < a.K; k0 += 512) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(Ring::kStages - 1) : "memory");
+    const uint4* from = reinterpret_cast<const uint4*>(ring + stage * Ring::kBytes);
+    uint4 wv[2][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) { wv[0][h] = from[h * 32]; wv[1][h] = from[(2 + h) * 32]; }
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+      float sum[4] = {};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint4 xv = from[(4 + 2 * g + h) * 32];
         mma16816(sum, wv[0][h].x, wv[1][h].x, wv[0][h].y, wv[1][h].y, xv.x, xv.y);
         mma16816(sum, wv[0][h].z, wv[1][h].z, wv[0][h].w, wv[1][h].w, xv.z, xv.w);
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[g][e] += sum[e];
     }
+    ask(k0 + Ring::kStages * 512, stage);
+    if (++stage == Ring::kStages) stage = 0;
   }
+  __syncthreads();     // the rings' memory becomes the warps' sums
+  float* red = reinterpret_cast<float*>(rows_smem);
 #pragma unroll
   for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) red[warp][gr + 8 * (e >> 1)][g * 8 + tq * 2 + (e & 1)] = acc[g][e];
+    for (int e = 0; e < 4; ++e) red[(warp * kRowsOut + gr + 8 * (e >> 1)) * Ring::kPitch + g * 8 + tq * 2 + (e & 1)] = acc[g][e];
   __syncthreads();
   asm volatile("griddepcontrol.wait;" ::: "memory");     // the shrink is complete and its results are visible
   for (int i = threadIdx.x; i < a.T * kRowsOut; i += 256) {
@@ -606,7 +644,7 @@ __global__ void __launch_bounds__(256) k_adapter_rows(const RowsArgs a) {
     if (col >= a.N) continue;
     float v = a.bias ? __ldg(a.bias + col) : 0.f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v += red[k][n][t];
+    for (int k = 0; k < 8; ++k) v += red[(k * kRowsOut + n) * Ring::kPitch + t];
     const int adapter = __ldcg(a.row_adapter + t);
     if (adapter >= 0) {
       const bf16* b = a.B + ((long long)adapter * a.N + col) * a.pitch;
@@ -626,10 +664,15 @@ __global__ void __launch_bounds__(256) k_adapter_rows(const RowsArgs a) {
 
 template <int GROUPS>
 cudaError_t launch_rows(const RowsArgs& a, cudaStream_t s) {
+  static DeviceSetup setup;
+  int sms = 0;
+  const cudaError_t e = device_setup(&setup, k_adapter_rows<GROUPS>, RowsRing<GROUPS>::kTotal, &sms);
+  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
   cfg.gridDim = dim3((a.N + kRowsOut - 1) / kRowsOut);
   cfg.blockDim = dim3(256);
+  cfg.dynamicSmemBytes = RowsRing<GROUPS>::kTotal;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -666,8 +709,8 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
   return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag));
 }
 
-// A CTA works for one adapter (and, when there are splits, on every splits-th chunk of 512 of its rows) and takes column
-// blocks in turn: 128 columns of v (x for dA, dy for dB) are the accumulator's lanes, its columns the three summands of the
+// Work items are (adapter, split, column block): an adapter's gradient in 128 columns, over all its rows or, when there are
+// splits, over every splits-th chunk of 512 of them.  A CTA takes an equal share of consecutive items.  128 columns of v (x for dA, dy for dB) are the accumulator's lanes, its columns the three summands of the
 // r ranks.  Both operands are read as they lie (rows = contraction index: MN-major).  Where a block of 64 rows ends
 // inside a box, the rows behind the end (another member's) are cleared in shared memory in both operands before the MMA
 // reads them.  The producer runs ahead into the next column block while the last one is drained, so that two CTAs per SM
@@ -690,7 +733,6 @@ __global__ void __launch_bounds__(192, 2) k_adapter_grad(const __grid_constant__
   __shared__ int list_n;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int adapter = blockIdx.y, z = blockIdx.z;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kGradStages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 4); }
@@ -709,122 +751,130 @@ __global__ void __launch_bounds__(192, 2) k_adapter_grad(const __grid_constant__
   bool ok = true;
   const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)((3 * RP) >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 
-  // The adapter's segments, kGradList table entries at a time, as a list of row ranges in shared memory.  One pass does for
-  // up to 1024 segments; later passes add to what the earlier ones left in dA and dB.
-  for (int base = 0; base == 0 || base < a.segs.n; base += kGradList) {
-    __syncthreads();
-    if (warp == 0) {
-      int n = 0;
-      for (int i0 = base; i0 < min(a.segs.n, base + kGradList); i0 += 32) {   // (kGradList is a multiple of 32)
-        const int i = i0 + lane;
-        const bool have = i < a.segs.n && segment_adapter(a.segs, i) == adapter;
-        const int2 r = have ? make_int2(segment_begin(a.segs, i), segment_begin(a.segs, i + 1)) : make_int2(0, 0);
-        const bool keep = have && r.x < r.y;
-        const uint32_t votes = __ballot_sync(0xFFFFFFFFu, keep);
-        if (keep) list[n + __popc(votes & ((1u << lane) - 1u))] = r;
-        n += __popc(votes);
-      }
-      if (lane == 0) list_n = n;
-    }
-    __syncthreads();
-    const int n = list_n;
-    int blocks = 0;   // blocks of 64 rows in this list that belong to this split
-    for (int i = 0; i < n; ++i)
-      for (int t = list[i].x / kGradChunk; t * kGradChunk < list[i].y; ++t)
-        if (t % a.splits == z) blocks += (min(list[i].y, (t + 1) * kGradChunk) - max(list[i].x, t * kGradChunk) + 63) / 64;
-    if (base > 0 && !blocks) continue;
-
-    for (int column = blockIdx.x; column < a.blocks_k + a.blocks_n && ok; column += gridDim.x) {
-      const bool is_b = column >= a.blocks_k;
-      const int c0 = (column - (is_b ? a.blocks_k : 0)) * 128;
+  const int columns = a.blocks_k + a.blocks_n;
+  const long long items = (long long)a.segs.n_adapters * a.splits * columns;
+  const long long item_end = items * (blockIdx.x + 1) / gridDim.x;
+  for (long long item = items * blockIdx.x / gridDim.x; item < item_end;) {
+    const int owner = (int)(item / columns), adapter = owner / a.splits, z = owner % a.splits;
+    const int first = (int)(item % columns), last = (int)min((long long)columns, first + item_end - item);   // columns of this adapter and split
+    item += last - first;
+    // The adapter's segments, kGradList table entries at a time, as a list of row ranges in shared memory.  One pass does for
+    // up to 1024 segments; later passes add to what the earlier ones left in dA and dB.
+    for (int base = 0; base == 0 || base < a.segs.n; base += kGradList) {
+      __syncthreads();
       if (warp == 0) {
-        if (lane == 0) {
-          const CUtensorMap* tmV = is_b ? &tmDY : &tmX;
-          const CUtensorMap* tmT = is_b ? &tmS : &tmDS;
+        int n = 0;
+        for (int i0 = base; i0 < min(a.segs.n, base + kGradList); i0 += 32) {   // (kGradList is a multiple of 32)
+          const int i = i0 + lane;
+          const bool have = i < a.segs.n && segment_adapter(a.segs, i) == adapter;
+          const int2 r = have ? make_int2(segment_begin(a.segs, i), segment_begin(a.segs, i + 1)) : make_int2(0, 0);
+          const bool keep = have && r.x < r.y;
+          const uint32_t votes = __ballot_sync(0xFFFFFFFFu, keep);
+          if (keep) list[n + __popc(votes & ((1u << lane) - 1u))] = r;
+          n += __popc(votes);
+        }
+        if (lane == 0) list_n = n;
+      }
+      __syncthreads();
+      const int n = list_n;
+      int blocks = 0;   // blocks of 64 rows in this list that belong to this split
+      for (int i = 0; i < n; ++i)
+        for (int t = list[i].x / kGradChunk; t * kGradChunk < list[i].y; ++t)
+          if (t % a.splits == z) blocks += (min(list[i].y, (t + 1) * kGradChunk) - max(list[i].x, t * kGradChunk) + 63) / 64;
+      if (base > 0 && !blocks) continue;
+
+      for (int column = first; column < last && ok; ++column) {
+        const bool is_b = column >= a.blocks_k;
+        const int c0 = (column - (is_b ? a.blocks_k : 0)) * 128;
+        if (warp == 0) {
+          if (lane == 0) {
+            const CUtensorMap* tmV = is_b ? &tmDY : &tmX;
+            const CUtensorMap* tmT = is_b ? &tmS : &tmDS;
+            for (int i = 0; i < n && ok; ++i)
+              for (int t = list[i].x / kGradChunk; t * kGradChunk < list[i].y && ok; ++t) {
+                if (t % a.splits != z) continue;
+                const int end = min(list[i].y, (t + 1) * kGradChunk);
+                for (int row = max(list[i].x, t * kGradChunk); row < end; row += 64) {
+                  if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) { ok = false; break; }
+                  uint8_t* sv = smem + stage * stage_bytes;
+                  mbar_expect_tx(&full[stage], stage_bytes);
+                  tma_load_3d(sv, tmV, &full[stage], c0, row, 0);
+                  tma_load_3d(sv + 8192, tmV, &full[stage], c0 + 64, row, 0);
+                  for (int b = 0; b < kBoxes; ++b) tma_load_3d(sv + 16384 + b * 8192, tmT, &full[stage], b * 64, row, 0);
+                  if (++stage == kGradStages) { stage = 0; phase ^= 1; }
+                }
+              }
+          }
+          ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
+        } else if (warp == 1) {
+          int done = 0;
           for (int i = 0; i < n && ok; ++i)
             for (int t = list[i].x / kGradChunk; t * kGradChunk < list[i].y && ok; ++t) {
               if (t % a.splits != z) continue;
               const int end = min(list[i].y, (t + 1) * kGradChunk);
-              for (int row = max(list[i].x, t * kGradChunk); row < end; row += 64) {
-                if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) { ok = false; break; }
+              for (int row = max(list[i].x, t * kGradChunk); row < end; row += 64, ++done) {
+                const int acc_buf = folds & 1;
+                if ((done & 1) == 0) {
+                  if (!warp_wait(&tempty[acc_buf], ((folds >> 1) & 1) ^ 1, abort_flag)) { ok = false; break; }
+                }
+                if (!warp_wait(&full[stage], phase, abort_flag)) { ok = false; break; }
                 uint8_t* sv = smem + stage * stage_bytes;
-                mbar_expect_tx(&full[stage], stage_bytes);
-                tma_load_3d(sv, tmV, &full[stage], c0, row, 0);
-                tma_load_3d(sv + 8192, tmV, &full[stage], c0 + 64, row, 0);
-                for (int b = 0; b < kBoxes; ++b) tma_load_3d(sv + 16384 + b * 8192, tmT, &full[stage], b * 64, row, 0);
+                const int valid = end - row;
+                if (valid < 64) {   // rows are 128-byte lines of each box
+                  for (int b = 0; b < 2 + kBoxes; ++b)
+                    for (int o = valid * 8 + lane; o < 64 * 8; o += 32) reinterpret_cast<uint4*>(sv + b * 8192)[o] = make_uint4(0u, 0u, 0u, 0u);
+                  fence_async_smem();
+                  __syncwarp();
+                }
+                if (lane == 0) {
+                  tc_fence_after();
+                  const uint32_t sa = smem_u32(sv), sb = sa + 16384;
+                  const uint32_t tmem_d = tmem_base + (uint32_t)(acc_buf * (3 * RP));
+#pragma unroll
+                  for (int k = 0; k < 4; ++k)
+                    umma_bf16(tmem_d, smem_desc(sa + k * 2048, 8192, 1024), smem_desc(sb + k * 2048, 8192, 1024), idesc, ((done & 1) | k) != 0 ? 1u : 0u);
+                  umma_commit(&empty[stage]);
+                  if ((done & 1) == 1 || done + 1 == blocks) umma_commit(&tfull[acc_buf]);
+                }
+                __syncwarp();
+                if ((done & 1) == 1 || done + 1 == blocks) ++folds;
                 if (++stage == kGradStages) { stage = 0; phase ^= 1; }
               }
             }
-        }
-        ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
-      } else if (warp == 1) {
-        int done = 0;
-        for (int i = 0; i < n && ok; ++i)
-          for (int t = list[i].x / kGradChunk; t * kGradChunk < list[i].y && ok; ++t) {
-            if (t % a.splits != z) continue;
-            const int end = min(list[i].y, (t + 1) * kGradChunk);
-            for (int row = max(list[i].x, t * kGradChunk); row < end; row += 64, ++done) {
-              const int acc_buf = folds & 1;
-              if ((done & 1) == 0) {
-                if (!warp_wait(&tempty[acc_buf], ((folds >> 1) & 1) ^ 1, abort_flag)) { ok = false; break; }
-              }
-              if (!warp_wait(&full[stage], phase, abort_flag)) { ok = false; break; }
-              uint8_t* sv = smem + stage * stage_bytes;
-              const int valid = end - row;
-              if (valid < 64) {   // rows are 128-byte lines of each box
-                for (int b = 0; b < 2 + kBoxes; ++b)
-                  for (int o = valid * 8 + lane; o < 64 * 8; o += 32) reinterpret_cast<uint4*>(sv + b * 8192)[o] = make_uint4(0u, 0u, 0u, 0u);
-                fence_async_smem();
-                __syncwarp();
-              }
-              if (lane == 0) {
-                tc_fence_after();
-                const uint32_t sa = smem_u32(sv), sb = sa + 16384;
-                const uint32_t tmem_d = tmem_base + (uint32_t)(acc_buf * (3 * RP));
+        } else {
+          const int q = warp & 3;
+          float acc[RP];
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                  umma_bf16(tmem_d, smem_desc(sa + k * 2048, 8192, 1024), smem_desc(sb + k * 2048, 8192, 1024), idesc, ((done & 1) | k) != 0 ? 1u : 0u);
-                umma_commit(&empty[stage]);
-                if ((done & 1) == 1 || done + 1 == blocks) umma_commit(&tfull[acc_buf]);
-              }
-              __syncwarp();
-              if ((done & 1) == 1 || done + 1 == blocks) ++folds;
-              if (++stage == kGradStages) { stage = 0; phase ^= 1; }
+          for (int i = 0; i < RP; ++i) acc[i] = 0.f;
+          for (int f = 0; f < (blocks + 1) / 2 && ok; ++f, ++folds) {
+            const int acc_buf = folds & 1;
+            if (!warp_wait(&tfull[acc_buf], (folds >> 1) & 1, abort_flag)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t t0 = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc_buf * (3 * RP));
+#pragma unroll
+            for (int c = 0; c < RP; c += 16) {
+              uint32_t h[16], m[16], l[16];
+              tmem_ld16(t0 + c, h);
+              tmem_ld16(t0 + RP + c, m);
+              tmem_ld16(t0 + 2 * RP + c, l);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) acc[c + i] += __uint_as_float(h[i]) + (__uint_as_float(m[i]) + __uint_as_float(l[i]));
             }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&tempty[acc_buf]);
           }
-      } else {
-        const int q = warp & 3;
-        float acc[RP];
+          const int col = c0 + q * 32 + lane;
+          if (ok && col < (is_b ? a.N : a.K)) {
+            // dA [rank][K]: a warp's lanes are neighbours; dB [N][rank]: a lane's ranks are
+            float* o = is_b ? a.dB + z * a.stride_b + ((long long)adapter * a.N + col) * a.rank
+                            : a.dA + z * a.stride_a + (long long)adapter * a.rank * a.K + col;
+            const long long step = is_b ? 1 : a.K;
 #pragma unroll
-        for (int i = 0; i < RP; ++i) acc[i] = 0.f;
-        for (int f = 0; f < (blocks + 1) / 2 && ok; ++f, ++folds) {
-          const int acc_buf = folds & 1;
-          if (!warp_wait(&tfull[acc_buf], (folds >> 1) & 1, abort_flag)) { ok = false; break; }
-          tc_fence_after();
-          const uint32_t t0 = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc_buf * (3 * RP));
-#pragma unroll
-          for (int c = 0; c < RP; c += 16) {
-            uint32_t h[16], m[16], l[16];
-            tmem_ld16(t0 + c, h);
-            tmem_ld16(t0 + RP + c, m);
-            tmem_ld16(t0 + 2 * RP + c, l);
-            tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[c + i] += __uint_as_float(h[i]) + (__uint_as_float(m[i]) + __uint_as_float(l[i]));
+            for (int i = 0; i < RP; ++i)
+              if (i < a.rank) o[i * step] = base > 0 ? o[i * step] + acc[i] : acc[i];
           }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&tempty[acc_buf]);
-        }
-        const int col = c0 + q * 32 + lane;
-        if (ok && col < (is_b ? a.N : a.K)) {
-          // dA [rank][K]: a warp's lanes are neighbours; dB [N][rank]: a lane's ranks are
-          float* o = is_b ? a.dB + z * a.stride_b + ((long long)adapter * a.N + col) * a.rank
-                          : a.dA + z * a.stride_a + (long long)adapter * a.rank * a.K + col;
-          const long long step = is_b ? 1 : a.K;
-#pragma unroll
-          for (int i = 0; i < RP; ++i)
-            if (i < a.rank) o[i * step] = base > 0 ? o[i * step] + acc[i] : acc[i];
         }
       }
     }
@@ -853,8 +903,9 @@ cudaError_t launch_grad(const CUtensorMap& x, const CUtensorMap& ds, const CUten
   int sms = 0;
   const cudaError_t e = device_setup(&setup, k_adapter_grad<RP>, kSmem, &sms);
   if (e != cudaSuccess) return e;
-  const int work = g.segs.n_adapters * g.splits, per = (2 * sms + work - 1) / work;      // two CTAs per SM over all adapters and splits
-  return launch_with(dim3(std::min(per, g.blocks_k + g.blocks_n), g.segs.n_adapters, g.splits), 192, kSmem, st)(k_adapter_grad<RP>, x, ds, dy, kept, g);
+  const long long items = (long long)g.segs.n_adapters * g.splits * (g.blocks_k + g.blocks_n);
+  const int resident = (RP == 16 ? 2 : 1) * sms;      // two CTAs per SM where shared memory allows it
+  return launch_with((unsigned)std::min<long long>(resident, items), 192, kSmem, st)(k_adapter_grad<RP>, x, ds, dy, kept, g);
 }
 
 // out = the splits' partial results, added in order
