@@ -6,6 +6,7 @@
 // fp32: the shared product is the library's fp32-ALU GEMM; the low-rank parts are small beside it (r / K of its work)
 // and each runs as one pass over the rows.
 #include <algorithm>
+#include <type_traits>
 
 #include "adapters.cuh"
 
@@ -19,8 +20,8 @@ namespace {
 // f: the adapter's scale or 1.
 template <bool TRANS>
 __global__ void __launch_bounds__(256) k_adapter_shrink_f32(const float* __restrict__ x, long long ldx, int K, const float* __restrict__ mats,
-                                                               int rank, const float* __restrict__ scale, Segments segs,
-                                                               float* __restrict__ s) {
+                                                            int rank, const float* __restrict__ scale, Segments segs,
+                                                            float* __restrict__ s) {
   pdl_prologue();
   const int row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (row >= segs.rows) return;
@@ -33,6 +34,7 @@ __global__ void __launch_bounds__(256) k_adapter_shrink_f32(const float* __restr
   const float f = scale ? scale[a] : 1.f;
   for (int r0 = 0; r0 < rank; r0 += 8) {
     float acc[8] = {};
+#pragma unroll 4
     for (int k = lane; k < K; k += 32) {
       const float v = xr[k];
 #pragma unroll
@@ -48,67 +50,112 @@ __global__ void __launch_bounds__(256) k_adapter_shrink_f32(const float* __restr
   }
 }
 
-// out[row][n] += f sum_j s[row][j] m_a(n, j); m_a is B_a [N][rank] or, TRANS, A_a [rank][N].
-template <bool TRANS>
-__global__ void __launch_bounds__(256) k_adapter_expand_f32(float* out, long long ld_out, int N,
-                                                               const float* __restrict__ mats, int rank,
-                                                               const float* __restrict__ scale, Segments segs,
-                                                               const float* __restrict__ s) {
+constexpr int kExpandRows = 32;
+
+// out[row][n] += f sum_j s[row][j] m_a(n, j); m_a is B_a [N][rank] or, TRANS, A_a [rank][N].  A block has 32 rows and 256
+// columns; a thread keeps its column of the adapter's matrix in registers from row to row.
+template <bool TRANS, int RANK>
+__global__ void __launch_bounds__(256) k_adapter_expand_f32(float* out, long long ld_out, int N, const float* __restrict__ mats, int rank,
+                                                            const float* __restrict__ scale, Segments segs, const float* __restrict__ s) {
   pdl_prologue();
-  const int row = blockIdx.x, n = blockIdx.y * 256 + threadIdx.x;
-  __shared__ float sr[kMaxRank];
-  const int j = segment_of_row(segs, row);
-  const int a = j >= 0 && row < segment_begin(segs, j + 1) ? segment_adapter(segs, j) : -1;
-  if (a < 0) return;
-  if (threadIdx.x < rank) sr[threadIdx.x] = s[(long long)row * rank + threadIdx.x];
+  __shared__ float sr[kExpandRows][RANK];
+  __shared__ int owner[kExpandRows];
+  const int row0 = blockIdx.x * kExpandRows, rows = min(kExpandRows, segs.rows - row0), n = blockIdx.y * 256 + threadIdx.x;
+  if (threadIdx.x < rows) {
+    const int row = row0 + threadIdx.x, j = segment_of_row(segs, row);
+    owner[threadIdx.x] = j >= 0 && row < segment_begin(segs, j + 1) ? segment_adapter(segs, j) : -1;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < rows * rank; i += 256) {
+    const int r = i / rank;
+    sr[r][i % rank] = owner[r] >= 0 ? s[(long long)row0 * rank + i] * (scale ? scale[owner[r]] : 1.f) : 0.f;
+  }
   __syncthreads();
   if (n >= N) return;
-  const float* m = mats + (long long)a * rank * N;
-  float acc = 0.f;
-  for (int i = 0; i < rank; ++i) acc = __fmaf_rn(sr[i], TRANS ? m[(long long)i * N + n] : m[(long long)n * rank + i], acc);
-  out[row * ld_out + n] += scale ? scale[a] * acc : acc;
+  float m[RANK];
+  int have = -1;
+  for (int r0 = 0; r0 < rows; r0 += 4) {
+    float v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (r0 + u < rows && owner[r0 + u] >= 0) v[u] = out[(row0 + r0 + u) * ld_out + n];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int r = r0 + u;
+      if (r >= rows || owner[r] < 0) continue;
+      if (owner[r] != have) {
+        have = owner[r];
+        const float* p = mats + (long long)have * rank * N;
+#pragma unroll
+        for (int i = 0; i < RANK; ++i)
+          if (i < rank) m[i] = TRANS ? p[(long long)i * N + n] : p[(long long)n * rank + i];
+      }
+      float acc = 0.f;
+#pragma unroll
+      for (int i = 0; i < RANK; ++i)
+        if (i < rank) acc = __fmaf_rn(sr[r][i], m[i], acc);
+      out[(row0 + r) * ld_out + n] = v[u] + acc;
+    }
+  }
 }
 
-// g_a(j, n) = f_a sum over the rows of adapter a of s[row][j] v[row][n], written as [rank][N] or, TRANS, [N][rank].
-// A block owns 64 columns of one adapter; its 256 threads take every fourth row and add up in shared memory.
-template <bool TRANS, int RANK>
-__global__ void __launch_bounds__(256) k_adapter_grad_f32(const float* __restrict__ v, long long ldv, int N, const float* __restrict__ s,
-                                                             int rank, const float* __restrict__ scale, Segments segs,
-                                                             float* __restrict__ g) {
+struct GradSide {
+  const float* v; long long ldv;
+  const float* s;
+  const float* scale;        // or null
+  float* g;
+  int N, blocks;
+  bool columns_first;        // g is [N][rank], else [rank][N]
+};
+
+// g_a(j, n) = f_a sum over the rows of adapter a of s[row][j] v[row][n]: dA from (dS, x) and dB from (S, dy) in one launch.  A
+// block owns 64 columns of one adapter and side; its 256 threads take every fourth row, four rows at a time, and add up in
+// shared memory.
+template <int RANK>
+__global__ void __launch_bounds__(256) k_adapter_grad_f32(const GradSide x, const GradSide dy, int rank, Segments segs) {
   pdl_prologue();
   __shared__ float sum[3][RANK][64];
-  const int col = threadIdx.x & 63, part = threadIdx.x >> 6, n = blockIdx.x * 64 + col, a = blockIdx.y;
+  const bool second = (int)blockIdx.x >= x.blocks;
+  const GradSide& side = second ? dy : x;
+  const int col = threadIdx.x & 63, part = threadIdx.x >> 6, n = ((int)blockIdx.x - (second ? x.blocks : 0)) * 64 + col, a = blockIdx.y;
+  const float* v = side.v + min(n, side.N - 1);
   float acc[RANK] = {};
   for (int j = 0; j < segs.n; ++j) {
     if (segment_adapter(segs, j) != a) continue;
     const int end = segment_begin(segs, j + 1);
-    for (int row = segment_begin(segs, j) + part; row < end; row += 4) {
-      const float x = n < N ? v[row * ldv + n] : 0.f;
-      const float* sr = s + (long long)row * rank;
+    for (int row = segment_begin(segs, j) + part; row < end; row += 16) {
+      float y[4];
 #pragma unroll
-      for (int i = 0; i < RANK; ++i) if (i < rank) acc[i] = __fmaf_rn(__ldg(sr + i), x, acc[i]);
+      for (int u = 0; u < 4; ++u) y[u] = row + 4 * u < end ? v[(row + 4 * u) * side.ldv] : 0.f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (row + 4 * u >= end) continue;
+        const float* sr = side.s + (long long)(row + 4 * u) * rank;
+#pragma unroll
+        for (int i = 0; i < RANK; ++i) if (i < rank) acc[i] = __fmaf_rn(__ldg(sr + i), y[u], acc[i]);
+      }
     }
   }
   if (part > 0)
 #pragma unroll
     for (int i = 0; i < RANK; ++i) sum[part - 1][i][col] = acc[i];
   __syncthreads();
-  if (part > 0 || n >= N) return;
-  const float f = scale ? scale[a] : 1.f;
-  float* out = g + (long long)a * rank * N;
+  if (part > 0 || n >= side.N) return;
+  const float f = side.scale ? side.scale[a] : 1.f;
+  float* out = side.g + (long long)a * rank * side.N;
 #pragma unroll
   for (int i = 0; i < RANK; ++i)
-    if (i < rank) out[TRANS ? (long long)n * rank + i : (long long)i * N + n] = f * (acc[i] + sum[0][i][col] + sum[1][i][col] + sum[2][i][col]);
+    if (i < rank) out[side.columns_first ? (long long)n * rank + i : (long long)i * side.N + n] = f * (acc[i] + sum[0][i][col] + sum[1][i][col] + sum[2][i][col]);
 }
 
-template <bool TRANS>
-cudaError_t launch_grad_f32(const float* v, long long ldv, int N, const float* s, int rank, const float* scale, const Segments& segs,
-                               float* g, cudaStream_t st) {
-  auto l = launch_with(dim3((N + 63) / 64, segs.n_adapters), 256, 0, st);
-  if (rank <= 8) return l(k_adapter_grad_f32<TRANS, 8>, v, ldv, N, s, rank, scale, segs, g);
-  if (rank <= 16) return l(k_adapter_grad_f32<TRANS, 16>, v, ldv, N, s, rank, scale, segs, g);
-  if (rank <= 32) return l(k_adapter_grad_f32<TRANS, 32>, v, ldv, N, s, rank, scale, segs, g);
-  return l(k_adapter_grad_f32<TRANS, 64>, v, ldv, N, s, rank, scale, segs, g);
+// f(integral_constant) with the smallest of 4, 8, 16, 32, 64 that holds the rank
+template <typename F>
+cudaError_t with_rank(int rank, F f) {
+  if (rank <= 4) return f(std::integral_constant<int, 4>());
+  if (rank <= 8) return f(std::integral_constant<int, 8>());
+  if (rank <= 16) return f(std::integral_constant<int, 16>());
+  if (rank <= 32) return f(std::integral_constant<int, 32>());
+  return f(std::integral_constant<int, 64>());
 }
 
 int fail(int code, const char* msg) {
@@ -145,8 +192,10 @@ cudaError_t forward_f32(const pbt_adapter_desc* d, const Segments& segs, float* 
   g.bias = d->bias;
   e = launch_gemm_simt(g, st);
   if (e != cudaSuccess) return e;
-  return launch_with(dim3(d->rows, (d->outputs + 255) / 256), 256, 0, st)(k_adapter_expand_f32<false>, y, d->ld_y, d->outputs, (const float*)d->B, d->rank,
-                                                                     d->scale, segs, s);
+  return with_rank(d->rank, [&](auto r) {
+    return launch_with(dim3((d->rows + kExpandRows - 1) / kExpandRows, (d->outputs + 255) / 256), 256, 0, st)(
+        k_adapter_expand_f32<false, decltype(r)::value>, y, d->ld_y, d->outputs, (const float*)d->B, d->rank, d->scale, segs, s);
+  });
 }
 
 cudaError_t backward_f32(const pbt_adapter_desc* d, const Segments& segs, float* ds, cudaStream_t st) {
@@ -163,12 +212,16 @@ cudaError_t backward_f32(const pbt_adapter_desc* d, const Segments& segs, float*
   g.C = dx; g.ldc = d->ld_dx;
   e = launch_gemm_simt(g, st);
   if (e != cudaSuccess) return e;
-  e = launch_with(dim3(d->rows, (d->inputs + 255) / 256), 256, 0, st)(k_adapter_expand_f32<true>, dx, d->ld_dx, d->inputs, (const float*)d->A, d->rank, nullptr,
-                                                                 segs, ds);
+  e = with_rank(d->rank, [&](auto r) {
+    return launch_with(dim3((d->rows + kExpandRows - 1) / kExpandRows, (d->inputs + 255) / 256), 256, 0, st)(
+        k_adapter_expand_f32<true, decltype(r)::value>, dx, d->ld_dx, d->inputs, (const float*)d->A, d->rank, nullptr, segs, ds);
+  });
   if (e != cudaSuccess) return e;
-  e = launch_grad_f32<false>(x, d->ld_x, d->inputs, ds, d->rank, nullptr, segs, d->dA, st);
-  if (e != cudaSuccess) return e;
-  return launch_grad_f32<true>(dy, d->ld_dy, d->outputs, d->s, d->rank, d->scale, segs, d->dB, st);
+  const GradSide a = {x, d->ld_x, ds, nullptr, d->dA, d->inputs, (d->inputs + 63) / 64, false};
+  const GradSide b = {dy, d->ld_dy, d->s, d->scale, d->dB, d->outputs, (d->outputs + 63) / 64, true};
+  return with_rank(d->rank, [&](auto r) {
+    return launch_with(dim3(a.blocks + b.blocks, d->n_adapters), 256, 0, st)(k_adapter_grad_f32<decltype(r)::value>, a, b, d->rank, segs);
+  });
 }
 
 // fp32: S of a forward pass that does not keep it, dS of a backward pass

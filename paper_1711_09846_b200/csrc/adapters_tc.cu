@@ -43,6 +43,25 @@ __global__ void __launch_bounds__(256) k_pack_rows(const bf16* __restrict__ src,
   }
 }
 
+// Launches a kernel that may begin while its predecessor in the stream, a shrink, still runs: the shrink says so
+// (griddepcontrol.launch_dependents, once all its CTAs are running and thus everything before it is complete), and the kernel
+// waits for the shrink's end (griddepcontrol.wait) in the threads that read its results, before they do.
+template <typename... KArgs, typename... Args>
+cudaError_t launch_after(unsigned grid, unsigned threads, size_t smem, cudaStream_t s, void (*kernel)(KArgs...), Args&&... args) {
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, KArgs(static_cast<Args&&>(args))...);
+}
+
 // ------------------------------------------------------------------------------------------------------------------
 // Shrink
 // ------------------------------------------------------------------------------------------------------------------
@@ -345,12 +364,13 @@ struct GemmSmem {
 
 // Roles as in the member-batched GEMM: warp 0 TMA producer, warp 1 MMA issuer, 8 epilogue warps, double-buffered
 // accumulator.  After a tile's k-blocks both walk its segments: one more stage each, 128 rows of the low-rank operand and
-// the adapter's matrix (columns past the rank are out of the tensor map and arrive as zeros).
+// the adapter's matrix (columns past the rank are out of the tensor map and arrive as zeros).  Launched while the shrink
+// runs; the two threads that read what it leaves (the tiles' first segments, the planes through TMA) wait for its end
+// after the k-blocks of their first tile.
 template <int BN, int STAGES, bool B_MN>
 __global__ void __launch_bounds__(64 + 32 * kGemmEpiWarps, 1)
 k_adapter_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmP,
                const __grid_constant__ CUtensorMap tmL, const TcParams p, const LowRank low) {
-  pdl_prologue();
   using L = GemmSmem<BN, STAGES>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -382,7 +402,6 @@ k_adapter_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       bool ok = true;
       for (int tile = blockIdx.x; tile < p.num_tiles && ok; tile += gridDim.x) {
         const int tm = tile / p.tiles_n, m0 = tm * kBM, n0 = (tile % p.tiles_n) * BN;
-        const int first = __ldg(low.tile_seg + tm);
         for (int kb = 0; kb < p.k_blocks; ++kb) {
           if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) { ok = false; break; }
           uint8_t* sa = smem + stage * L::kStageBytes;
@@ -398,7 +417,8 @@ k_adapter_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           }
           if (++stage == STAGES) { stage = 0; phase ^= 1; }
         }
-        SegmentWalk walk(low.segs, first, m0, kBM);
+        if (tile == blockIdx.x) asm volatile("griddepcontrol.wait;" ::: "memory");
+        SegmentWalk walk(low.segs, __ldcg(low.tile_seg + tm), m0, kBM);
         int adapter, lo, hi;
         while (ok && walk.next(adapter, lo, hi)) {
           if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) { ok = false; break; }
@@ -434,7 +454,6 @@ k_adapter_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       bool ok = true;
       for (int tile = blockIdx.x; tile < p.num_tiles && ok; tile += gridDim.x, ++it) {
         const int tm = tile / p.tiles_n, m0 = tm * kBM;
-        const int first = __ldg(low.tile_seg + tm);
         const int acc = it & 1;
         if (!mbar_wait(&tempty[acc], ((it >> 1) & 1) ^ 1, abort_flag)) { ok = false; break; }
         tc_fence_after();
@@ -450,7 +469,8 @@ k_adapter_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           umma_commit(&empty[stage]);
           if (++stage == STAGES) { stage = 0; phase ^= 1; }
         }
-        SegmentWalk walk(low.segs, first, m0, kBM);
+        if (tile == blockIdx.x) asm volatile("griddepcontrol.wait;" ::: "memory");
+        SegmentWalk walk(low.segs, __ldcg(low.tile_seg + tm), m0, kBM);
         int adapter, lo, hi;
         while (ok && walk.next(adapter, lo, hi)) {
           if (!mbar_wait(&full[stage], phase, abort_flag)) { ok = false; break; }
@@ -508,8 +528,8 @@ cudaError_t launch_gemm(const CUtensorMap* maps, TcParams& p, const LowRank& low
   if (e != cudaSuccess) return e;
   p.tiles_n = (p.N + BN - 1) / BN;
   p.num_tiles = p.tiles_m * p.tiles_n;
-  return launch_with(p.num_tiles < sms ? p.num_tiles : sms, 64 + 32 * kGemmEpiWarps, L::kTotal, s)(k_adapter_gemm<BN, STAGES, B_MN>, maps[0], maps[1], maps[2],
-                                                                                                maps[3], p, low);
+  return launch_after(p.num_tiles < sms ? p.num_tiles : sms, 64 + 32 * kGemmEpiWarps, L::kTotal, s, k_adapter_gemm<BN, STAGES, B_MN>, maps[0], maps[1], maps[2],
+                      maps[3], p, low);
 }
 
 // C[rows][N] = X[rows][K] B^T + bias + low-rank; B is [N][K], or [K][N] when b_mn; the low-rank matrices alike over ranks.
@@ -532,8 +552,10 @@ cudaError_t launch_gemm(const GemmCall& c, const Segments& segs, const int* tile
   p.bias = c.bias;
   p.counters = counters;
   const LowRank low = {segs, tile_seg, c.rp / 16};
-  // 256-wide tiles once they go round the SMs; below that, twice as many tiles of half the width
-  const bool wide = (long long)p.tiles_m * ((c.N + 255) / 256) >= 148;
+  // 128-wide tiles when the 256-wide ones would leave most of their last wave idle: a wave of half tiles costs a little more
+  // than half a wave of full ones (the model of the member-batched GEMM; 3001 rows x 784 -> 1024: 96 wide tiles, one wave)
+  const long long wide_tiles = (long long)p.tiles_m * ((c.N + 255) / 256), narrow_tiles = (long long)p.tiles_m * ((c.N + 127) / 128);
+  const bool wide = 1.15 * (double)((narrow_tiles + 147) / 148) >= 2.0 * (double)((wide_tiles + 147) / 148);
   CUtensorMap maps[4];
   bool ok = make_map(&maps[0], c.x, c.K, segs.rows, c.ldx, 1, 0, kBM) && make_map(&maps[2], c.planes, c.rp, segs.rows, c.ld_planes, 1, 0, kBM);
   if (!c.b_mn) {
@@ -574,7 +596,8 @@ template <int GROUPS> struct RowsRing {
   static constexpr int kVectors = 4 + 2 * GROUPS;                   // 16-byte vectors of a lane in a block of 64 inputs
   static constexpr int kBytes = kVectors * 512;
   static constexpr int kPitch = GROUPS * 8 + 1;                     // of the sums [8 warps][16 columns][rows]
-  static constexpr int kTotal = 8 * kStages * kBytes > 8 * kRowsOut * kPitch * 4 ? 8 * kStages * kBytes : 8 * kRowsOut * kPitch * 4;
+  static constexpr int kSums = 8 * kRowsOut * kPitch * 4 + GROUPS * 8 * (kMaxRank + 1) * 4;   // and the rows' S and adapters
+  static constexpr int kTotal = 8 * kStages * kBytes > kSums ? 8 * kStages * kBytes : kSums;
 };
 template <int GROUPS>
 __global__ void __launch_bounds__(256) k_adapter_rows(const RowsArgs a) {
@@ -637,28 +660,48 @@ __global__ void __launch_bounds__(256) k_adapter_rows(const RowsArgs a) {
   for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
     for (int e = 0; e < 4; ++e) red[(warp * kRowsOut + gr + 8 * (e >> 1)) * Ring::kPitch + g * 8 + tq * 2 + (e & 1)] = acc[g][e];
-  __syncthreads();
+  float* low = red + 8 * kRowsOut * Ring::kPitch;          // scaled S of the rows
+  int* owner = reinterpret_cast<int*>(low + GROUPS * 8 * kMaxRank);
   asm volatile("griddepcontrol.wait;" ::: "memory");     // the shrink is complete and its results are visible
-  for (int i = threadIdx.x; i < a.T * kRowsOut; i += 256) {
-    const int t = i / kRowsOut, n = i % kRowsOut, col = n0 + n;
-    if (col >= a.N) continue;
-    float v = a.bias ? __ldg(a.bias + col) : 0.f;
+  for (int i = threadIdx.x; i < a.T * a.rank; i += 256) low[(i / a.rank) * a.pitch + i % a.rank] = __ldcg(a.scaled + i);
+  if (threadIdx.x < a.T) owner[threadIdx.x] = __ldcg(a.row_adapter + threadIdx.x);
+  __syncthreads();
+  // a thread has one column and every 16th row, whose adapters' matrices it asks for together
+  const int n = threadIdx.x % kRowsOut, col = n0 + n;
+  if (col >= a.N) return;
+  const float bias = a.bias ? __ldg(a.bias + col) : 0.f;
+  constexpr int kMine = (GROUPS * 8 + 15) / 16;
+  float v[kMine];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v += red[(k * kRowsOut + n) * Ring::kPitch + t];
-    const int adapter = __ldcg(a.row_adapter + t);
-    if (adapter >= 0) {
-      const bf16* b = a.B + ((long long)adapter * a.N + col) * a.pitch;
-      const float* s = a.scaled + t * a.rank;
-      for (int j = 0; j < a.rank; j += 8) {
-        const uint4 bv = __ldg(reinterpret_cast<const uint4*>(b + j));
+  for (int u = 0; u < kMine; ++u) {
+    const int t = threadIdx.x / kRowsOut + 16 * u;
+    v[u] = bias;
+    if (t < a.T)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[u] += red[(k * kRowsOut + n) * Ring::kPitch + t];
+  }
+  for (int j = 0; j < a.rank; j += 8) {
+    uint4 bv[kMine];
+#pragma unroll
+    for (int u = 0; u < kMine; ++u) {
+      const int t = threadIdx.x / kRowsOut + 16 * u, adapter = t < a.T ? owner[t] : -1;
+      bv[u] = adapter >= 0 ? __ldg(reinterpret_cast<const uint4*>(a.B + ((long long)adapter * a.N + col) * a.pitch + j)) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int u = 0; u < kMine; ++u) {
+      const int t = threadIdx.x / kRowsOut + 16 * u;
+      if (t < a.T && owner[t] >= 0)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const uint32_t pairs = word(bv, e >> 1);
-          if (j + e < a.rank) v = __fmaf_rn(__uint_as_float((e & 1) ? pairs & 0xFFFF0000u : pairs << 16), __ldcg(s + j + e), v);
+          const uint32_t pairs = word(bv[u], e >> 1);
+          if (j + e < a.rank) v[u] = __fmaf_rn(__uint_as_float((e & 1) ? pairs & 0xFFFF0000u : pairs << 16), low[t * a.pitch + j + e], v[u]);
         }
-      }
     }
-    a.y[t * a.ldy + col] = __float2bfloat16_rn(v);
+  }
+#pragma unroll
+  for (int u = 0; u < kMine; ++u) {
+    const int t = threadIdx.x / kRowsOut + 16 * u;
+    if (t < a.T) a.y[t * a.ldy + col] = __float2bfloat16_rn(v[u]);
   }
 }
 
@@ -668,18 +711,7 @@ cudaError_t launch_rows(const RowsArgs& a, cudaStream_t s) {
   int sms = 0;
   const cudaError_t e = device_setup(&setup, k_adapter_rows<GROUPS>, RowsRing<GROUPS>::kTotal, &sms);
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg;
-  memset(&cfg, 0, sizeof(cfg));
-  cfg.gridDim = dim3((a.N + kRowsOut - 1) / kRowsOut);
-  cfg.blockDim = dim3(256);
-  cfg.dynamicSmemBytes = RowsRing<GROUPS>::kTotal;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k_adapter_rows<GROUPS>, a);
+  return launch_after((a.N + kRowsOut - 1) / kRowsOut, 256, RowsRing<GROUPS>::kTotal, s, k_adapter_rows<GROUPS>, a);
 }
 cudaError_t launch_rows(const RowsArgs& a, cudaStream_t s) {
   if (a.T <= 8) return launch_rows<1>(a, s);
