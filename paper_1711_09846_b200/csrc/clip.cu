@@ -28,6 +28,7 @@ constexpr int kClipKeep = 208 * 1024;      // bytes of gradients a CTA keeps in 
 constexpr long long kClipWave = (long long)kClipCtas * (kClipKeep - 4096);   // bytes of a wave of whole groups
 constexpr int kClipShare = 4096;           // smallest share of a CTA in a wave
 constexpr int kClipPieces = 64;            // table entries of a wave that are fetched ahead of it
+constexpr int kClipRuns = 32;              // groups of a CTA's share that are worked on together
 constexpr int kClipAhead = 96 * 1024;      // bytes of the next wave asked for at the barrier
 constexpr unsigned int kClipPolls = 1u << 24;
 
@@ -37,15 +38,18 @@ struct __align__(16) ClipPiece {
   char* dst;
   int count;       // elements
   int kept;        // where the elements are kept in shared memory (same alignment as src), or -1
-  int group;
-  int bf;          // 1: bfloat16
+  int group2;      // 2 * group + (1: bfloat16)
+  int sum;         // where the CTA's sum of this group goes
+  int sum_begin, sum_end;   // the group's sums
+  int pad[2];
+  __device__ int group() const { return group2 >> 1; }
+  __device__ bool bf() const { return group2 & 1; }
 };
 
 struct ClipArgs {
   const ClipPiece* pieces;
   const int* first;        // [waves * CTAs + 1] first piece of every (wave, CTA)
-  const int* first_sum;    // [waves * CTAs] first partial sum of every (wave, CTA): one per group it touches
-  const int* group_sums;   // [groups + 1] partial sums of every group
+  const int* empty;        // [groups] 1: the group has no elements
   double* sums;
   unsigned int* barrier;   // arrivals, exits, status
   int n_waves, n_groups;
@@ -60,16 +64,10 @@ __device__ __forceinline__ void clip_store(bf16* p, float v) { *p = __float2bflo
 __device__ __forceinline__ void clip_store(float* p, float v) { *p = v; }
 
 template <typename S>
-__device__ __forceinline__ S clip_block_sum(S v, S* scratch) {
+__device__ __forceinline__ S clip_warp_sum(S v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
-  __syncthreads();
-  S t = scratch[threadIdx.x & (kClipThreads / 32 - 1)];
-#pragma unroll
-  for (int o = kClipThreads / 64; o > 0; o >>= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
-  return t;
+  return v;
 }
 
 // 16 bytes of gradients
@@ -174,10 +172,10 @@ __device__ __forceinline__ float clip_read(const ClipPiece& p, int index, char* 
 }
 
 template <typename T>
-__device__ __noinline__ double clip_read_wide(const char* src, int count) {
-  const T* g = reinterpret_cast<const T*>(src);
+__device__ __noinline__ double clip_read_wide(const ClipPiece& p) {      // by one warp
+  const T* g = reinterpret_cast<const T*>(p.src);
   double sum = 0.0;
-  for (int i = threadIdx.x; i < count; i += kClipThreads) {
+  for (int i = threadIdx.x & 31; i < p.count; i += 32) {
     const double v = clip_load(g + i);
     sum = fma(v, v, sum);
   }
@@ -235,7 +233,7 @@ __device__ __forceinline__ float clip_factor(float limit, float norm) {
   return __fdiv_rn(limit, norm);
 }
 
-// Arrive at the grid barrier (thread 0, after the block's sums are written), and wait until `target` CTAs have arrived.
+// Arrive at the grid barrier (thread 0, after the block's sums are written and fenced), and wait until `target` CTAs have arrived.
 // The wait is bounded; on expiry the status word is set, everybody leaves, and the norms that are missing stay NaN.
 __device__ __forceinline__ void clip_arrive(const ClipArgs& a) {
   __threadfence();
@@ -255,62 +253,77 @@ __device__ __forceinline__ bool clip_wait(const ClipArgs& a, unsigned int target
   return true;
 }
 
+constexpr int kClipWarps = kClipThreads / 32;
+
 __global__ void __launch_bounds__(kClipThreads, 1) k_clip(const ClipArgs a) {
   pdl_prologue();
   extern __shared__ __align__(16) char keep[];
   __shared__ ClipPiece near[2][kClipPieces];
-  __shared__ double scratch[32];
-  __shared__ int go;
-  const int tid = threadIdx.x, b = blockIdx.x, ctas = gridDim.x;
+  __shared__ float warp_sums[kClipRuns][kClipWarps];
+  __shared__ int run_first[kClipRuns + 1];
+  __shared__ float factor[kClipRuns];
+  __shared__ int go, wide;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, b = blockIdx.x, ctas = gridDim.x;
   if (b == 0)
-    for (int g = tid; g < a.n_groups; g += kClipThreads)
-      a.norms[g] = a.group_sums[g] == a.group_sums[g + 1] ? 0.f : __int_as_float(0x7FC00000);
-  auto fetch = [&](int w) {
+    for (int g = tid; g < a.n_groups; g += kClipThreads) a.norms[g] = a.empty[g] ? 0.f : __int_as_float(0x7FC00000);
+  auto fetch = [&](int w) {       // 16 bytes a thread
     if (w < a.n_waves) {
-      const int first = a.first[w * ctas + b], n = min(a.first[w * ctas + b + 1] - first, kClipPieces);
-      if (tid < n) near[w & 1][tid] = a.pieces[first + tid];
+      const int first = a.first[w * ctas + b], n = min(a.first[w * ctas + b + 1] - first, kClipPieces) * (int)(sizeof(ClipPiece) / 16);
+      for (int i = tid; i < n; i += kClipThreads) reinterpret_cast<uint4*>(near[w & 1])[i] = reinterpret_cast<const uint4*>(a.pieces + first)[i];
     }
   };
   fetch(0);
   __syncthreads();
   for (int w = 0; w < a.n_waves; ++w) {
     const int first = a.first[w * ctas + b], n = a.first[w * ctas + b + 1] - first;
-    int sum_at = a.first_sum[w * ctas + b];
-    auto piece = [&](int i) {      // two 16-byte loads, from shared memory for the entries that were fetched ahead
-      const ulonglong2* from = reinterpret_cast<const ulonglong2*>(i < kClipPieces ? &near[w & 1][i] : a.pieces + first + i);
-      const ulonglong2 where = from[0], what = from[1];
-      ClipPiece p;
-      p.src = reinterpret_cast<const char*>(where.x);
-      p.dst = reinterpret_cast<char*>(where.y);
-      p.count = (int)what.x;
-      p.kept = (int)(what.x >> 32);
-      p.group = (int)what.y;
-      p.bf = (int)(what.y >> 32);
-      return p;
-    };
-    for (int i = 0; i < n;) {                      // one group of the CTA's share after the other
-      const int begin = i, group = piece(i).group;
-      float sum = 0.f;
-      for (; i < n; ++i) {
-        const ClipPiece p = piece(i);
-        if (p.group != group) break;
-        sum += p.bf ? clip_read<bf16>(p, i, keep) : clip_read<float>(p, i, keep);
-      }
-      const float t = clip_block_sum(sum, reinterpret_cast<float*>(scratch));
-      double total = t;
-      // Squares are fp32; where their sum leaves the range in which that is exact to rounding (elements beyond 1.8e19, or
-      // all below 1e-15), the group's share is summed again in fp64, so that only the norm itself can overflow.
-      if (!(t > 1e-30f && t < 3e38f)) {
-        double d = 0.0;
-        for (int k = begin; k < i; ++k) {
-          const ClipPiece p = piece(k);
-          d += p.bf ? clip_read_wide<bf16>(p.src, p.count) : clip_read_wide<float>(p.src, p.count);
+    auto piece = [&](int i) -> const ClipPiece& { return i < kClipPieces ? near[w & 1][i] : a.pieces[first + i]; };
+    // A run is the CTA's pieces of one group.  kClipRuns of them at a time: the warps add up squares on their own and meet
+    // once, whatever the number of runs.
+    for (int i = 0; i < n;) {
+      int runs = 0;
+      const int start = i;
+      while (i < n) {
+        const int group = piece(i).group2 >> 1;
+        float sum = 0.f;
+        if (runs == kClipRuns) break;
+        if (tid == 0) run_first[runs] = i;
+        for (; i < n; ++i) {
+          const ClipPiece& p = piece(i);
+          if (p.group2 >> 1 != group) break;
+          sum += p.bf() ? clip_read<bf16>(p, i, keep) : clip_read<float>(p, i, keep);
         }
-        total = clip_block_sum(d, scratch);
+        sum = clip_warp_sum(sum);
+        if (lane == 0) warp_sums[runs][warp] = sum;
+        ++runs;
       }
-      if (tid == 0) a.sums[sum_at] = total;
-      ++sum_at;
+      if (tid == 0) {
+        run_first[runs] = i;
+        wide = 0;
+      }
+      __syncthreads();
+      if (tid < runs) {
+        float t = warp_sums[tid][0];
+        for (int k = 1; k < kClipWarps; ++k) t += warp_sums[tid][k];
+        // Squares are fp32; where their sum leaves the range in which that is exact to rounding (elements beyond 1.8e19, or
+        // all below 1e-15), the run is summed again in fp64 below, so that only the norm itself can overflow.
+        if (t > 1e-30f && t < 3e38f) a.sums[piece(run_first[tid]).sum] = t;
+        else wide = 1;
+      }
+      __syncthreads();
+      if (wide)
+        for (int q = warp; q < runs; q += kClipWarps) {
+          float t = lane < kClipWarps ? warp_sums[q][lane] : 0.f;
+          t = clip_warp_sum(t);
+          if (t > 1e-30f && t < 3e38f) continue;
+          double d = 0.0;
+          for (int k = run_first[q]; k < run_first[q + 1]; ++k) d += piece(k).bf() ? clip_read_wide<bf16>(piece(k)) : clip_read_wide<float>(piece(k));
+          d = clip_warp_sum(d);
+          if (lane == 0) a.sums[piece(run_first[q]).sum] = d;
+        }
+      if (wide || i < n || start > 0) __syncthreads();     // before the tables are used again, and before thread 0 arrives
     }
+    __threadfence();
+    __syncthreads();
     if (tid == 0) clip_arrive(a);
     fetch(w + 1);
     __syncthreads();
@@ -319,7 +332,7 @@ __global__ void __launch_bounds__(kClipThreads, 1) k_clip(const ClipArgs a) {
       if (tid < min(m, kClipPieces)) {
         const ClipPiece& p = near[(w + 1) & 1][tid];
         const uintptr_t from = ((uintptr_t)p.src + 15) & ~(uintptr_t)15;
-        long long bytes = (long long)((uintptr_t)p.src + (long long)p.count * (p.bf ? 2 : 4) - from) & ~15ll;
+        long long bytes = (long long)((uintptr_t)p.src + (long long)p.count * (p.bf() ? 2 : 4) - from) & ~15ll;
         if (bytes > kClipAhead) bytes = kClipAhead;
         if (bytes >= 16 && p.kept >= 0 && p.kept < kClipAhead)
           asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"((uint32_t)bytes) : "memory");
@@ -328,22 +341,41 @@ __global__ void __launch_bounds__(kClipThreads, 1) k_clip(const ClipArgs a) {
     if (tid == 0) go = clip_wait(a, (unsigned int)(w + 1) * ctas);
     __syncthreads();
     if (!go) break;
-    sum_at = a.first_sum[w * ctas + b];
     for (int i = 0; i < n;) {
-      const int group = piece(i).group, s0 = a.group_sums[group], s1 = a.group_sums[group + 1];
-      double s = 0.0;
-      for (int k = s0 + tid; k < s1; k += kClipThreads) s += __ldcg(a.sums + k);
-      const float norm = (float)sqrt(clip_block_sum(s, scratch));
-      if (s0 == sum_at && tid == 0) a.norms[group] = norm;     // the CTA that holds the group's first sum
-      ++sum_at;
-      const float f = clip_factor(a.limits ? a.limits[group] : a.limit, norm);
-      for (; i < n; ++i) {
-        const ClipPiece p = piece(i);
-        if (p.group != group) break;
-        if (f == 1.f && p.src == p.dst) continue;
-        if (p.bf) clip_write<bf16>(p, i, keep, f);
-        else clip_write<float>(p, i, keep, f);
+      // the runs' factors, a warp each, then all of their elements
+      const int start = i;
+      int runs = 0;
+      for (int k = i; k < n;) {
+        const int group = piece(k).group2 >> 1;
+        if (runs == kClipRuns) break;
+        if (runs % kClipWarps == warp) {
+          const ClipPiece& p = piece(k);
+          const float limit = a.limits ? __ldg(a.limits + group) : a.limit;
+          double s = 0.0;
+          for (int q = p.sum_begin + lane; q < p.sum_end; q += 32) s += __ldcg(a.sums + q);
+          s = clip_warp_sum(s);
+          const float norm = (float)sqrt(s);
+          if (lane == 0) {
+            factor[runs] = clip_factor(limit, norm);
+            if (p.sum == p.sum_begin) a.norms[group] = norm;     // the CTA that holds the group's first sum
+          }
+        }
+        ++runs;
+        while (k < n && piece(k).group2 >> 1 == group) ++k;
       }
+      __syncthreads();
+      for (int q = 0; q < runs; ++q) {
+        const int group = piece(i).group2 >> 1;
+        const float f = factor[q];
+        for (; i < n; ++i) {
+          const ClipPiece& p = piece(i);
+          if (p.group2 >> 1 != group) break;
+          if (f == 1.f && p.src == p.dst) continue;
+          if (p.bf()) clip_write<bf16>(p, i, keep, f);
+          else clip_write<float>(p, i, keep, f);
+        }
+      }
+      if (i < n || start > 0) __syncthreads();     // `factor` is written again
     }
     __syncthreads();     // `keep` and the tables are written again by the next wave
   }
@@ -383,7 +415,8 @@ int clip_check(const pbt_clip_tensor* t, int n, int n_groups) {
 // Who handles what: waves of whole groups, every wave's bytes dealt to the CTAs in equal consecutive shares.
 struct ClipTable {
   std::vector<ClipPiece> pieces;
-  std::vector<int> first, first_sum, group_sums;
+  std::vector<int> first, empty;
+  int n_sums = 0;
   int n_waves = 0, ctas = 1;
 };
 bool clip_table(const pbt_clip_tensor* t, int n_tensors, int n_groups, ClipTable* out) {
@@ -416,7 +449,7 @@ bool clip_table(const pbt_clip_tensor* t, int n_tensors, int n_groups, ClipTable
   long long most = 0;
   for (long long b : wave_bytes) most = std::max(most, b);
   out->ctas = (int)std::max<long long>(1, std::min<long long>(kClipCtas, (most + kClipShare - 1) / kClipShare));
-  out->group_sums.assign(n_groups + 1, 0);
+  std::vector<int> begin(n_groups, 0), end(n_groups, 0);      // sums of every group
   size_t at = 0;
   int sums = 0;
   for (int w = 0; w < out->n_waves; ++w) {
@@ -424,7 +457,6 @@ bool clip_table(const pbt_clip_tensor* t, int n_tensors, int n_groups, ClipTable
     long long done = 0;                  // elements of tensor order[at] that are dealt
     for (int c = 0; c < out->ctas; ++c) {
       out->first.push_back((int)out->pieces.size());
-      out->first_sum.push_back(sums);
       long long room = share;
       int kept = 0, group = -1;
       while (at < wave_end[w] && (room > 0 || c == out->ctas - 1)) {
@@ -439,13 +471,13 @@ bool clip_table(const pbt_clip_tensor* t, int n_tensors, int n_groups, ClipTable
         if (c < out->ctas - 1 && left * esz > room) cut((room + 15) / 16 * 16 + 16);   // pieces end on 16-byte boundaries
         if (keeps) cut(space);
         cut(1ll << 30);
-        out->pieces.push_back({src, (char*)x.dst + done * esz, (int)take, keeps ? kept + phase : -1, x.group, x.dtype});
-        if (keeps) kept += (int)((phase + take * esz + 15) / 16 * 16);
         if (x.group != group) {
           group = x.group;
-          ++sums;
-          out->group_sums[group + 1] = sums;
+          if (begin[group] == end[group]) begin[group] = sums;
+          end[group] = ++sums;
         }
+        out->pieces.push_back({src, (char*)x.dst + done * esz, (int)take, keeps ? kept + phase : -1, x.group * 2 + x.dtype, sums - 1, 0, 0, {0, 0}});
+        if (keeps) kept += (int)((phase + take * esz + 15) / 16 * 16);
         room -= take * esz;
         done += take;
         if (done == x.numel) { ++at; done = 0; }
@@ -454,22 +486,25 @@ bool clip_table(const pbt_clip_tensor* t, int n_tensors, int n_groups, ClipTable
     }
   }
   out->first.push_back((int)out->pieces.size());
-  for (int g = 0; g < n_groups; ++g) out->group_sums[g + 1] = std::max(out->group_sums[g], out->group_sums[g + 1]);
-  out->first_sum.push_back(sums);
+  for (ClipPiece& p : out->pieces) {
+    p.sum_begin = begin[p.group2 >> 1];
+    p.sum_end = end[p.group2 >> 1];
+  }
+  for (int g = 0; g < n_groups; ++g) out->empty.push_back(begin[g] == end[g]);
+  out->n_sums = sums;
   return true;
 }
 
 struct ClipLayout {
-  size_t barrier, sums, group_sums, first, first_sum, pieces, total;
+  size_t barrier, sums, empty, first, pieces, total;
 };
 ClipLayout clip_layout(const ClipTable& t) {
   ClipLayout l;
   l.barrier = 0;
   l.sums = 256;
-  l.group_sums = l.sums + clip_align((size_t)t.first_sum.back() * sizeof(double));
-  l.first = l.group_sums + clip_align(t.group_sums.size() * sizeof(int));
-  l.first_sum = l.first + clip_align(t.first.size() * sizeof(int));
-  l.pieces = l.first_sum + clip_align(t.first_sum.size() * sizeof(int));
+  l.empty = l.sums + clip_align((size_t)t.n_sums * sizeof(double));
+  l.first = l.empty + clip_align(t.empty.size() * sizeof(int));
+  l.pieces = l.first + clip_align(t.first.size() * sizeof(int));
   l.total = l.pieces + clip_align(t.pieces.size() * sizeof(ClipPiece));
   return l;
 }
@@ -538,9 +573,8 @@ extern "C" int pbt_clip_create(pbt_clip_t** out, const pbt_clip_tensor* tensors,
     auto upload = [&](size_t at, const void* from, size_t bytes) {
       if (e == cudaSuccess && bytes) e = cudaMemcpyAsync(base + at, from, bytes, cudaMemcpyHostToDevice, s);
     };
-    upload(l.group_sums, t.group_sums.data(), t.group_sums.size() * sizeof(int));
+    upload(l.empty, t.empty.data(), t.empty.size() * sizeof(int));
     upload(l.first, t.first.data(), t.first.size() * sizeof(int));
-    upload(l.first_sum, t.first_sum.data(), t.first_sum.size() * sizeof(int));
     upload(l.pieces, t.pieces.data(), t.pieces.size() * sizeof(ClipPiece));
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);   // the tables above are this function's own
     if (e == cudaSuccess) e = cudaFuncSetAttribute(k_clip, cudaFuncAttributeMaxDynamicSharedMemorySize, kClipKeep);
@@ -549,8 +583,7 @@ extern "C" int pbt_clip_create(pbt_clip_t** out, const pbt_clip_tensor* tensors,
     memset(&p->args, 0, sizeof(p->args));
     p->args.pieces = (const ClipPiece*)(base + l.pieces);
     p->args.first = (const int*)(base + l.first);
-    p->args.first_sum = (const int*)(base + l.first_sum);
-    p->args.group_sums = (const int*)(base + l.group_sums);
+    p->args.empty = (const int*)(base + l.empty);
     p->args.sums = (double*)(base + l.sums);
     p->args.barrier = (unsigned int*)(base + l.barrier);
     p->args.n_waves = t.n_waves;

@@ -244,27 +244,26 @@ def block_norm_backward(dy, du, y, block=None, *, post_weight=None, gate=None, s
         _require(rstd_block is not None, "rstd_block is what the forward pass kept")
         d.rstd_block = _weight(rstd_block, y, shape[:2], "rstd_block")
     inputs = (dy, du, y, block, post_weight, gate, scale, next_weight, rstd_block, rstd_next)
-    return _on(y.device, stream, inputs, _norm_backward, d, shape, y, gate, block is not None, du is not None, scale is not None)
+    return _on(y.device, stream, inputs, _norm_backward, d, y, gate, post_weight, scale, next_weight)
 
 
-def _norm_backward(s, d, shape, y, gate, block, nxt, scaled):
+def _norm_backward(s, d, y, gate, post_weight, scale, next_weight):
     lib, device = load_library(), y.device
-    vector = (shape[0], shape[2])
     dblock = dgate = dpost = dnext = dscale = None
     dx = _like(y)
     d.dx = dx.data_ptr()
-    if block:
+    if post_weight is not None:
         dblock = _like(y)
-        dpost = torch.empty(vector, dtype=torch.float32, device=device)
+        dpost = torch.empty_like(post_weight)
         d.dblock, d.dpost_weight = dblock.data_ptr(), dpost.data_ptr()
-        if scaled:
-            dscale = torch.empty(shape[0], dtype=torch.float32, device=device)
+        if scale is not None:
+            dscale = torch.empty_like(scale)
             d.dscale = dscale.data_ptr()
         if gate is not None:
             dgate = _like(gate)
             d.dgate = dgate.data_ptr()
-    if nxt:
-        dnext = torch.empty(vector, dtype=torch.float32, device=device)
+    if next_weight is not None:
+        dnext = torch.empty_like(next_weight)
         d.dnext_weight = dnext.data_ptr()
     if d.rows:
         nbytes = C.c_size_t(0)
@@ -346,7 +345,7 @@ class AdapterProjection:
 
     def _forward(self, s, d, keep):
         w = self.weight
-        y = torch.empty((d.rows, d.outputs), dtype=w.dtype, device=w.device)
+        y = w.new_empty((d.rows, d.outputs))
         d.y, d.ld_y = y.data_ptr(), d.outputs
         kept = None
         if keep:
@@ -367,7 +366,7 @@ class AdapterProjection:
 
     def _backward(self, s, d):
         w = self.weight
-        dx = torch.empty((d.rows, d.inputs), dtype=w.dtype, device=w.device)
+        dx = w.new_empty((d.rows, d.inputs))
         d_a = torch.empty((d.n_adapters, d.rank, d.inputs), dtype=torch.float32, device=w.device)
         d_b = torch.empty((d.n_adapters, d.outputs, d.rank), dtype=torch.float32, device=w.device)
         d.dx, d.ld_dx, d.dA, d.dB = dx.data_ptr(), d.inputs, d_a.data_ptr(), d_b.data_ptr()
