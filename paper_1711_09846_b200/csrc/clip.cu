@@ -2,11 +2,19 @@
 //   norm_g = sqrt(sum over the tensors of group g, all elements: e^2),   dst = src * min(1, limit_g / norm_g).
 //
 // Memory-bound; the floor is ONE read and one write of every element, which asks for the gradients to stay on the chip
-// between the two.  One cooperative launch goes through the groups in waves: as many whole groups as fit the shared memory
-// of all SMs together (30 MB), or one larger group.  In a wave every CTA reads its share of the elements, keeps what fits
-// in its shared memory, leaves its sums of squares, meets the others at a grid barrier, and scales what it kept; what a
-// large group has beyond the 30 MB is read a second time, from L2 as long as the group fits there.  While a CTA waits at
-// the barrier the first bytes of its next wave are on their way into L2.
+// between the two.
+//
+// Groups that fit the shared memory of all SMs together (30 MB): one cooperative launch goes through them in waves of as many
+// whole groups as fit.  In a wave every CTA reads its share of the elements, keeps it in shared memory, leaves its sums of
+// squares, meets the others at a grid barrier, and scales what it kept.  What is kept comes by bulk copies, all of them asked
+// for when the wave begins (208 KB per SM in flight); while a CTA waits at the barrier the first bytes of its next wave are
+// on their way into L2.
+//
+// Larger groups are streamed twice, all of them together: sums of 64 KB chunks, the groups' factors, and the scaling.  Keeping
+// half of a 58.7 MB group in shared memory and the rest in L2 saves a third of the traffic, but meeting after each group costs
+// more (80 such groups: 2.57 ms, 12 us to read a group, 10.5 to write it and 9 to meet and to find the factor; with two teams of
+// CTAs on alternate groups 2.90 ms, L2 does not hold both).
+//
 // Sums are added in a fixed order (no atomics on values), so a run is reproducible bit for bit.
 #include <stdio.h>
 
@@ -14,7 +22,7 @@
 #include <new>
 #include <vector>
 
-#include "pbt_common.cuh"
+#include "tc_common.cuh"
 
 namespace pbt {
 void set_last_error(const char* msg);
@@ -42,7 +50,6 @@ struct __align__(16) ClipPiece {
   int sum;         // where the CTA's sum of this group goes
   int sum_begin, sum_end;   // the group's sums
   int pad[2];
-  __device__ int group() const { return group2 >> 1; }
   __device__ bool bf() const { return group2 & 1; }
 };
 
@@ -130,6 +137,36 @@ __device__ __forceinline__ void clip_add(const uint4& v, float* sum) {
   Quad<T>::get(v, f);
 #pragma unroll
   for (int e = 0; e < Quad<T>::n; ++e) sum[e & 3] = __fmaf_rn(f[e], f[e], sum[e & 3]);
+}
+
+// Pieces that a bulk copy brings (those of the table's fetched entries that are kept and not small): their vectors.
+__device__ __forceinline__ bool clip_bulk(const ClipPiece& p, int index) { return index < kClipPieces && p.kept >= 0 && p.count > 1024; }
+template <typename T>
+__device__ __forceinline__ void clip_ask(const ClipPiece& p, char* keep, uint64_t* bar) {
+  const ClipSpan s = clip_span<T>(p);
+  const uint32_t bytes = (uint32_t)s.vectors * 16, to = tc::smem_u32(keep + p.kept + s.head * sizeof(T));
+  tc::mbar_expect_tx(bar, bytes);
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(to), "l"(p.src + s.head * sizeof(T)), "r"(bytes), "r"(tc::smem_u32(bar)) : "memory");
+}
+template <typename T>
+__device__ __forceinline__ float clip_sum_kept(const ClipPiece& p, char* keep) {
+  const ClipSpan s = clip_span<T>(p);
+  const T* g = reinterpret_cast<const T*>(p.src);
+  T* k = reinterpret_cast<T*>(keep + p.kept);
+  const uint4* kv = reinterpret_cast<const uint4*>(k + s.head);
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  const int i0 = threadIdx.x, loose = s.head + p.count - s.tail;
+  if (i0 < loose) {
+    const int at = i0 < s.head ? i0 : s.tail + i0 - s.head;
+    const T v = g[at];
+    k[at] = v;
+    const float f = clip_load(&v);
+    sum[0] = f * f;
+  }
+#pragma unroll 4
+  for (int i = i0; i < s.vectors; i += kClipThreads) clip_add<T>(kv[i], sum);
+  return (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
 
 template <typename T>
@@ -262,7 +299,8 @@ __global__ void __launch_bounds__(kClipThreads, 1) k_clip(const ClipArgs a) {
   __shared__ float warp_sums[kClipRuns][kClipWarps];
   __shared__ int run_first[kClipRuns + 1];
   __shared__ float factor[kClipRuns];
-  __shared__ int go, wide;
+  __shared__ uint64_t arrived[kClipPieces];     // bulk copies of the fetched entries
+  __shared__ int go, wide, gave_up;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, b = blockIdx.x, ctas = gridDim.x;
   if (b == 0)
     for (int g = tid; g < a.n_groups; g += kClipThreads) a.norms[g] = a.empty[g] ? 0.f : __int_as_float(0x7FC00000);
@@ -273,10 +311,20 @@ __global__ void __launch_bounds__(kClipThreads, 1) k_clip(const ClipArgs a) {
     }
   };
   fetch(0);
+  if (tid < kClipPieces) tc::mbar_init(&arrived[tid], 1);
+  if (tid == 0) gave_up = 0;
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  unsigned long long turns = 0;      // bit i: parity of the next use of arrived[i]
   __syncthreads();
   for (int w = 0; w < a.n_waves; ++w) {
     const int first = a.first[w * ctas + b], n = a.first[w * ctas + b + 1] - first;
     auto piece = [&](int i) -> const ClipPiece& { return i < kClipPieces ? near[w & 1][i] : a.pieces[first + i]; };
+    const int asked = min(n, kClipPieces);
+    if (tid < asked && clip_bulk(piece(tid), tid)) {
+      tc::fence_async_smem();        // the wave before has read these bytes (and all threads have met since)
+      if (piece(tid).bf()) clip_ask<bf16>(piece(tid), keep, &arrived[tid]);
+      else clip_ask<float>(piece(tid), keep, &arrived[tid]);
+    }
     // A run is the CTA's pieces of one group.  kClipRuns of them at a time: the warps add up squares on their own and meet
     // once, whatever the number of runs.
     for (int i = 0; i < n;) {
@@ -284,13 +332,20 @@ __global__ void __launch_bounds__(kClipThreads, 1) k_clip(const ClipArgs a) {
       const int start = i;
       while (i < n) {
         const int group = piece(i).group2 >> 1;
+        const int begin = i;
         float sum = 0.f;
         if (runs == kClipRuns) break;
         if (tid == 0) run_first[runs] = i;
         for (; i < n; ++i) {
           const ClipPiece& p = piece(i);
           if (p.group2 >> 1 != group) break;
-          sum += p.bf() ? clip_read<bf16>(p, i, keep) : clip_read<float>(p, i, keep);
+          if (!clip_bulk(p, i)) sum += p.bf() ? clip_read<bf16>(p, i, keep) : clip_read<float>(p, i, keep);
+        }
+        for (int k = begin; k < min(i, asked); ++k) {      // what the bulk copies have brought meanwhile
+          const ClipPiece& p = piece(k);
+          if (!clip_bulk(p, k)) continue;
+          if (!tc::mbar_wait(&arrived[k], (uint32_t)(turns >> k) & 1u, &gave_up)) gave_up = 1;
+          sum += p.bf() ? clip_sum_kept<bf16>(p, keep) : clip_sum_kept<float>(p, keep);
         }
         sum = clip_warp_sum(sum);
         if (lane == 0) warp_sums[runs][warp] = sum;
@@ -322,6 +377,8 @@ __global__ void __launch_bounds__(kClipThreads, 1) k_clip(const ClipArgs a) {
         }
       if (wide || i < n || start > 0) __syncthreads();     // before the tables are used again, and before thread 0 arrives
     }
+    for (int k = 0; k < asked; ++k)
+      if (clip_bulk(piece(k), k)) turns ^= 1ull << k;
     __threadfence();
     __syncthreads();
     if (tid == 0) clip_arrive(a);
@@ -338,7 +395,10 @@ __global__ void __launch_bounds__(kClipThreads, 1) k_clip(const ClipArgs a) {
           asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"((uint32_t)bytes) : "memory");
       }
     }
-    if (tid == 0) go = clip_wait(a, (unsigned int)(w + 1) * ctas);
+    if (tid == 0) {
+      if (gave_up) a.barrier[2] = PBT_ERR_TIMEOUT;
+      go = !gave_up && clip_wait(a, (unsigned int)(w + 1) * ctas);
+    }
     __syncthreads();
     if (!go) break;
     for (int i = 0; i < n;) {
@@ -352,6 +412,7 @@ __global__ void __launch_bounds__(kClipThreads, 1) k_clip(const ClipArgs a) {
           const ClipPiece& p = piece(k);
           const float limit = a.limits ? __ldg(a.limits + group) : a.limit;
           double s = 0.0;
+#pragma unroll 8
           for (int q = p.sum_begin + lane; q < p.sum_end; q += 32) s += __ldcg(a.sums + q);
           s = clip_warp_sum(s);
           const float norm = (float)sqrt(s);
@@ -389,6 +450,139 @@ __global__ void __launch_bounds__(kClipThreads, 1) k_clip(const ClipArgs a) {
   }
 }
 
+// ---- groups that do not fit: one block per chunk ----
+constexpr int kStreamThreads = 256;
+constexpr int kStreamChunk = 64 * 1024;      // bytes
+
+struct StreamArgs {
+  const ClipPiece* chunks;       // kept is -1, sum the chunk's own index
+  const int* groups;             // the large groups, and for each its sums' range
+  int n_chunks, n_groups;
+  double* sums;
+  float* factors;                // of every group of the call
+  float limit;
+  const float* limits;
+  float* norms;
+};
+
+template <typename T>
+__device__ __forceinline__ float stream_sum(const ClipPiece& p) {
+  const ClipSpan s = clip_span<T>(p);
+  const T* g = reinterpret_cast<const T*>(p.src);
+  const uint4* gv = reinterpret_cast<const uint4*>(g + s.head);
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  int i = threadIdx.x;
+  for (; i + 7 * kStreamThreads < s.vectors; i += 8 * kStreamThreads) {
+    uint4 v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = __ldcs(gv + i + u * kStreamThreads);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) clip_add<T>(v[u], sum);
+  }
+  for (; i < s.vectors; i += kStreamThreads) clip_add<T>(gv[i], sum);
+  const int loose = s.head + p.count - s.tail;
+  if ((int)threadIdx.x < loose) {
+    const float f = clip_load(g + ((int)threadIdx.x < s.head ? threadIdx.x : s.tail + threadIdx.x - s.head));
+    sum[0] = __fmaf_rn(f, f, sum[0]);
+  }
+  return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+}
+template <typename T>
+__device__ __noinline__ double stream_sum_wide(const ClipPiece& p) {
+  const T* g = reinterpret_cast<const T*>(p.src);
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < p.count; i += kStreamThreads) {
+    const double v = clip_load(g + i);
+    sum = fma(v, v, sum);
+  }
+  return sum;
+}
+
+__global__ void __launch_bounds__(kStreamThreads) k_clip_sums(const StreamArgs a) {
+  pdl_prologue();
+  __shared__ float part[kStreamThreads / 32];
+  __shared__ double part_wide[kStreamThreads / 32];
+  const ClipPiece p = a.chunks[blockIdx.x];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const float s = clip_warp_sum(p.bf() ? stream_sum<bf16>(p) : stream_sum<float>(p));
+  if (lane == 0) part[warp] = s;
+  __syncthreads();
+  float t = part[0];
+#pragma unroll
+  for (int k = 1; k < kStreamThreads / 32; ++k) t += part[k];
+  if (t > 1e-30f && t < 3e38f) {      // (as in k_clip)
+    if (threadIdx.x == 0) a.sums[blockIdx.x] = t;
+    return;
+  }
+  const double d = clip_warp_sum(p.bf() ? stream_sum_wide<bf16>(p) : stream_sum_wide<float>(p));
+  if (lane == 0) part_wide[warp] = d;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double all = part_wide[0];
+    for (int k = 1; k < kStreamThreads / 32; ++k) all += part_wide[k];
+    a.sums[blockIdx.x] = all;
+  }
+}
+
+__global__ void __launch_bounds__(kStreamThreads) k_clip_factors(const StreamArgs a) {
+  pdl_prologue();
+  __shared__ double part[kStreamThreads / 32];
+  const int group = a.groups[3 * blockIdx.x], begin = a.groups[3 * blockIdx.x + 1], end = a.groups[3 * blockIdx.x + 2];
+  double s = 0.0;
+  for (int q = begin + threadIdx.x; q < end; q += kStreamThreads) s += a.sums[q];
+  s = clip_warp_sum(s);
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int k = 1; k < kStreamThreads / 32; ++k) s += part[k];
+    const float norm = (float)sqrt(s);
+    a.norms[group] = norm;
+    a.factors[group] = clip_factor(a.limits ? a.limits[group] : a.limit, norm);
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void stream_scale(const ClipPiece& p, float f) {
+  const ClipSpan s = clip_span<T>(p);
+  const T* g = reinterpret_cast<const T*>(p.src);
+  T* o = reinterpret_cast<T*>(p.dst);
+  const uint4* gv = reinterpret_cast<const uint4*>(g + s.head);
+  uint4* ov = reinterpret_cast<uint4*>(o + s.head);
+  const int loose = s.head + p.count - s.tail;
+  if ((int)threadIdx.x < loose) {
+    const int at = (int)threadIdx.x < s.head ? threadIdx.x : s.tail + threadIdx.x - s.head;
+    clip_store(o + at, clip_load(g + at) * f);
+  }
+  int i = threadIdx.x;
+  if (((uintptr_t)ov & 15) != 0) {     // a destination of another alignment than its source: element by element
+    for (; i < s.vectors; i += kStreamThreads) {
+      float e[Quad<T>::n];
+      Quad<T>::get(gv[i], e);
+#pragma unroll
+      for (int j = 0; j < Quad<T>::n; ++j) clip_store(o + s.head + i * Quad<T>::n + j, e[j] * f);
+    }
+    return;
+  }
+  for (; i + 3 * kStreamThreads < s.vectors; i += 4 * kStreamThreads) {
+    uint4 v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = __ldcs(gv + i + u * kStreamThreads);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) __stcs(ov + i + u * kStreamThreads, clip_scaled<T>(v[u], f));
+  }
+  for (; i < s.vectors; i += kStreamThreads) __stcs(ov + i, clip_scaled<T>(gv[i], f));
+}
+
+// from the last chunk to the first: the last ones that k_clip_sums has read are still in L2
+__global__ void __launch_bounds__(kStreamThreads) k_clip_scale(const StreamArgs a) {
+  pdl_prologue();
+  const ClipPiece p = a.chunks[a.n_chunks - 1 - (int)blockIdx.x];
+  const float f = __ldg(a.factors + (p.group2 >> 1));
+  if (f == 1.f && p.src == p.dst) return;
+  if (p.bf()) stream_scale<bf16>(p, f);
+  else stream_scale<float>(p, f);
+}
+
 int clip_fail(int code, const char* msg) {
   set_last_error(msg);
   return code;
@@ -414,8 +608,8 @@ int clip_check(const pbt_clip_tensor* t, int n, int n_groups) {
 
 // Who handles what: waves of whole groups, every wave's bytes dealt to the CTAs in equal consecutive shares.
 struct ClipTable {
-  std::vector<ClipPiece> pieces;
-  std::vector<int> first, empty;
+  std::vector<ClipPiece> pieces, chunks;      // of the waves, of the streamed groups
+  std::vector<int> first, empty, large;       // large: (group, first sum, end) of every streamed group
   int n_sums = 0;
   int n_waves = 0, ctas = 1;
 };
@@ -431,6 +625,24 @@ bool clip_table(const pbt_clip_tensor* t, int n_tensors, int n_groups, ClipTable
     }
   if (total > (1ll << 40)) return false;
   std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return t[a].group < t[b].group; });
+  for (int i : order) {
+    const pbt_clip_tensor& x = t[i];
+    if (group_bytes[x.group] <= kClipWave) continue;
+    const long long esz = x.dtype ? 2 : 4;
+    if (out->large.empty() || out->large[out->large.size() - 3] != x.group) {
+      const int at = (int)out->chunks.size();
+      out->large.insert(out->large.end(), {x.group, at, at});
+    }
+    for (long long done = 0; done < x.numel;) {
+      const char* src = (const char*)x.src + done * esz;
+      const long long take = std::min(x.numel - done, (kStreamChunk - (long long)((uintptr_t)src & 15)) / esz);   // chunks end on 16-byte boundaries
+      const int at = (int)out->chunks.size();
+      out->chunks.push_back({src, (char*)x.dst + done * esz, (int)take, -1, x.group * 2 + x.dtype, at, 0, 0, {0, 0}});
+      done += take;
+    }
+    out->large.back() = (int)out->chunks.size();
+  }
+  order.erase(std::remove_if(order.begin(), order.end(), [&](int i) { return group_bytes[t[i].group] > kClipWave; }), order.end());
   std::vector<long long> wave_bytes;
   std::vector<size_t> wave_end;          // in `order`
   for (size_t i = 0; i < order.size();) {
@@ -490,13 +702,13 @@ bool clip_table(const pbt_clip_tensor* t, int n_tensors, int n_groups, ClipTable
     p.sum_begin = begin[p.group2 >> 1];
     p.sum_end = end[p.group2 >> 1];
   }
-  for (int g = 0; g < n_groups; ++g) out->empty.push_back(begin[g] == end[g]);
+  for (int g = 0; g < n_groups; ++g) out->empty.push_back(group_bytes[g] == 0);
   out->n_sums = sums;
   return true;
 }
 
 struct ClipLayout {
-  size_t barrier, sums, empty, first, pieces, total;
+  size_t barrier, sums, empty, first, pieces, large, factors, chunk_sums, chunks, total;
 };
 ClipLayout clip_layout(const ClipTable& t) {
   ClipLayout l;
@@ -505,7 +717,11 @@ ClipLayout clip_layout(const ClipTable& t) {
   l.empty = l.sums + clip_align((size_t)t.n_sums * sizeof(double));
   l.first = l.empty + clip_align(t.empty.size() * sizeof(int));
   l.pieces = l.first + clip_align(t.first.size() * sizeof(int));
-  l.total = l.pieces + clip_align(t.pieces.size() * sizeof(ClipPiece));
+  l.large = l.pieces + clip_align(t.pieces.size() * sizeof(ClipPiece));
+  l.factors = l.large + clip_align(t.large.size() * sizeof(int));
+  l.chunk_sums = l.factors + clip_align(t.large.empty() ? 0 : t.empty.size() * sizeof(float));
+  l.chunks = l.chunk_sums + clip_align(t.chunks.size() * sizeof(double));
+  l.total = l.chunks + clip_align(t.chunks.size() * sizeof(ClipPiece));
   return l;
 }
 
@@ -534,7 +750,9 @@ bool clip_overlap(const pbt_clip_tensor* t, int n) {
 
 struct pbt_clip {
   pbt::ClipArgs args;
+  pbt::StreamArgs stream;
   int ctas;
+  bool some_empty;      // groups without elements: their norms are k_clip's to write
 };
 
 extern "C" int pbt_clip_query_workspace(const pbt_clip_tensor* tensors, int32_t n_tensors, int32_t n_groups, size_t* bytes) {
@@ -576,6 +794,8 @@ extern "C" int pbt_clip_create(pbt_clip_t** out, const pbt_clip_tensor* tensors,
     upload(l.empty, t.empty.data(), t.empty.size() * sizeof(int));
     upload(l.first, t.first.data(), t.first.size() * sizeof(int));
     upload(l.pieces, t.pieces.data(), t.pieces.size() * sizeof(ClipPiece));
+    upload(l.large, t.large.data(), t.large.size() * sizeof(int));
+    upload(l.chunks, t.chunks.data(), t.chunks.size() * sizeof(ClipPiece));
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);   // the tables above are this function's own
     if (e == cudaSuccess) e = cudaFuncSetAttribute(k_clip, cudaFuncAttributeMaxDynamicSharedMemorySize, kClipKeep);
     if (e != cudaSuccess) return clip_fail(PBT_ERR_CUDA, cudaGetErrorString(e));
@@ -589,6 +809,14 @@ extern "C" int pbt_clip_create(pbt_clip_t** out, const pbt_clip_tensor* tensors,
     p->args.n_waves = t.n_waves;
     p->args.n_groups = n_groups;
     p->ctas = t.ctas;
+    p->some_empty = std::find(t.empty.begin(), t.empty.end(), 1) != t.empty.end();
+    memset(&p->stream, 0, sizeof(p->stream));
+    p->stream.chunks = (const ClipPiece*)(base + l.chunks);
+    p->stream.groups = (const int*)(base + l.large);
+    p->stream.n_chunks = (int)t.chunks.size();
+    p->stream.n_groups = (int)t.large.size() / 3;
+    p->stream.sums = (double*)(base + l.chunk_sums);
+    p->stream.factors = (float*)(base + l.factors);
     *out = p;
   } catch (const std::bad_alloc&) {
     return clip_fail(PBT_ERR_STATE, "out of host memory");
@@ -609,9 +837,22 @@ extern "C" int pbt_clip_run(pbt_clip_t* p, float limit, const float* limits_devi
   a.limit = limit;
   a.limits = limits_device;
   a.norms = norms_out_device;
-  void* args[] = {&a};
-  // cooperative: every CTA is resident, which the grid barrier relies on
-  const cudaError_t e = cudaLaunchCooperativeKernel((const void*)k_clip, dim3(p->ctas), dim3(kClipThreads), args, kClipKeep, (cudaStream_t)stream);
+  cudaStream_t st = (cudaStream_t)stream;
+  cudaError_t e = cudaSuccess;
+  if (a.n_waves || p->some_empty) {
+    void* args[] = {&a};
+    // cooperative: every CTA is resident, which the grid barrier relies on
+    e = cudaLaunchCooperativeKernel((const void*)k_clip, dim3(p->ctas), dim3(kClipThreads), args, kClipKeep, st);
+  }
+  if (p->stream.n_chunks) {
+    StreamArgs q = p->stream;
+    q.limit = limit;
+    q.limits = limits_device;
+    q.norms = norms_out_device;
+    if (e == cudaSuccess) e = launch_with(q.n_chunks, kStreamThreads, 0, st)(k_clip_sums, q);
+    if (e == cudaSuccess) e = launch_with(q.n_groups, kStreamThreads, 0, st)(k_clip_factors, q);
+    if (e == cudaSuccess) e = launch_with(q.n_chunks, kStreamThreads, 0, st)(k_clip_scale, q);
+  }
   if (e != cudaSuccess) return clip_fail(PBT_ERR_CUDA, cudaGetErrorString(e));
   return PBT_OK;
 }

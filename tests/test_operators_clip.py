@@ -42,6 +42,7 @@ SIZES = {
     "around a chunk": [16383, 16384, 16385, 32768 + 5, 3],
     "empty among them": [0, 5, 0, 129, 0],
     "large": [3_000_001, 1_000_003],
+    "beyond the shared memory of all SMs": [17_000_003, 33, 5, 70_001],
 }
 
 
@@ -114,18 +115,19 @@ def test_clip_a_diverged_member_touches_nobody_else(bad):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("count", [20_000, 8_000_000])
 @pytest.mark.parametrize("value", [1e25, 1e-25, 0.0])
-def test_clip_squares_beyond_the_range_of_fp32(value):
+def test_clip_squares_beyond_the_range_of_fp32(value, count):
     import torch
     import paper_1711_09846_b200 as pbt
-    g = torch.full((20_000,), value, device="cuda")
+    g = torch.full((count,), value, device="cuda")
     out = torch.empty_like(g)
     clip = pbt.GradientClip([g], out=[out])
     norm = clip.run(value).item()
-    want = float(g[0].double().item()) * math.sqrt(20_000)
+    want = float(g[0].double().item()) * math.sqrt(count)
     assert abs(norm - want) <= want * NORM_TOL
     if value:
-        assert abs(out[7].item() - want / 20_000) <= want / 20_000 * OUT_TOL["float32"] * 2
+        assert abs(out[7].item() - want / count) <= want / count * OUT_TOL["float32"] * 2
 
 
 @pytest.mark.gpu
