@@ -512,8 +512,6 @@ int pbt_clip_destroy(pbt_clip_t* p);
  * workspace serves one run at a time: runs on several streams have to be ordered.
  */
 int pbt_clip_run(pbt_clip_t* p, float limit, const float* limits_device, float* norms_out_device, void* stream);
-/* PBT_ERR_TIMEOUT if the bounded grid barrier of a run expired (norms it did not reach are NaN); synchronises. */
-int pbt_clip_status(pbt_clip_t* p, void* stream);
 
 /*
  * Norms before and after a residual block, fused with the block's gate and residual scale.  Per member m and row i:

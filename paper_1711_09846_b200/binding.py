@@ -113,7 +113,7 @@ EXPORTS = [
     "pbt_get_hparams", "pbt_set_hparams", "pbt_get_copy_map", "pbt_get_best", "pbt_get_last_loss",
     "pbt_set_batch", "pbt_step_host", "pbt_prefetch_host_batch", "pbt_step_prefetched", "pbt_get_launch_count", "pbt_profile_begin", "pbt_profile_end", "pbt_profile_get",
     "pbt_grouped_gemm", "pbt_selftest_bounded_wait", "pbt_energy_fitness_static", "pbt_last_error",
-    "pbt_clip_query_workspace", "pbt_clip_create", "pbt_clip_destroy", "pbt_clip_run", "pbt_clip_status",
+    "pbt_clip_query_workspace", "pbt_clip_create", "pbt_clip_destroy", "pbt_clip_run",
     "pbt_block_norm_forward", "pbt_block_norm_query_workspace", "pbt_block_norm_backward",
     "pbt_adapter_query_workspace", "pbt_adapter_forward", "pbt_adapter_backward",
 ]
@@ -175,7 +175,6 @@ def load_library() -> C.CDLL:
     lib.pbt_clip_create.argtypes = [C.POINTER(vp), vp, C.c_int32, C.c_int32, vp, C.c_size_t, vp]
     lib.pbt_clip_destroy.argtypes = [vp]
     lib.pbt_clip_run.argtypes = [vp, C.c_float, vp, vp, vp]
-    lib.pbt_clip_status.argtypes = [vp, vp]
     lib.pbt_block_norm_forward.argtypes = [C.POINTER(PbtBlockNormDesc), vp]
     lib.pbt_block_norm_query_workspace.argtypes = [C.POINTER(PbtBlockNormDesc), C.POINTER(C.c_size_t)]
     lib.pbt_block_norm_backward.argtypes = [C.POINTER(PbtBlockNormDesc), vp, C.c_size_t, vp]

@@ -43,25 +43,6 @@ __global__ void __launch_bounds__(256) k_pack_rows(const bf16* __restrict__ src,
   }
 }
 
-// Launches a kernel that may begin while its predecessor in the stream, a shrink, still runs: the shrink says so
-// (griddepcontrol.launch_dependents, once all its CTAs are running and thus everything before it is complete), and the kernel
-// waits for the shrink's end (griddepcontrol.wait) in the threads that read its results, before they do.
-template <typename... KArgs, typename... Args>
-cudaError_t launch_after(unsigned grid, unsigned threads, size_t smem, cudaStream_t s, void (*kernel)(KArgs...), Args&&... args) {
-  cudaLaunchConfig_t cfg;
-  memset(&cfg, 0, sizeof(cfg));
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, KArgs(static_cast<Args&&>(args))...);
-}
-
 // ------------------------------------------------------------------------------------------------------------------
 // Shrink
 // ------------------------------------------------------------------------------------------------------------------

@@ -81,6 +81,26 @@ struct LaunchCfg {
   }
 };
 inline LaunchCfg launch_with(dim3 grid, dim3 block, size_t smem, cudaStream_t stream) { return LaunchCfg{grid, block, smem, stream}; }
+
+// Launches a kernel that may begin while its predecessor in the stream still runs, whatever pbt_spec.programmatic_launches
+// says.  The predecessor allows it (griddepcontrol.launch_dependents, which takes effect once all its blocks are running, so
+// that everything before it is complete), and the kernel waits for its end (griddepcontrol.wait) in the threads that read what it
+// leaves or write what it reads, before they do.
+template <typename... KArgs, typename... Args>
+cudaError_t launch_after(unsigned grid, unsigned threads, size_t smem, cudaStream_t s, void (*kernel)(KArgs...), Args&&... args) {
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, KArgs(static_cast<Args&&>(args))...);
+}
 #endif
 
 // ---------------------------------------------------------------------------

@@ -92,7 +92,7 @@ class GradientClip:
         self._handle = C.c_void_p(None)
 
         def create(s):
-            self._ws = _workspace(nbytes.value, self.device)
+            self._ws, self._home = _workspace(nbytes.value, self.device), s
             _check(self.lib.pbt_clip_create(C.byref(self._handle), table, len(grads), self.n_groups, self._ws.data_ptr(),
                                             nbytes.value, s))
         _on(self.device, None, (), create)
@@ -107,18 +107,17 @@ class GradientClip:
             limits = max_norm.data_ptr()
         else:
             limit = float(max_norm)
-        return _on(self.device, stream, (max_norm,) if limits else (), self._run, limit, limits)
+        inputs = () if stream is None else (max_norm if limits else None, *self._keep[0], *self._keep[1])
+        return _on(self.device, stream, inputs, self._run, limit, limits)
 
     def _run(self, s, limit, limits):
+        if s != self._home:      # keeps the workspace until the run is done, should the object go first
+            self._ws.record_stream(torch.cuda.current_stream(self.device))
         norms = torch.empty(self.n_groups, dtype=torch.float32, device=self.device)
         rc = self.lib.pbt_clip_run(self._handle, limit, limits, norms.data_ptr(), s)
         if rc:
             _check(rc)
         return norms
-
-    def check(self):
-        """Waits for the runs on the current stream and raises if one of them timed out (PBT_ERR_TIMEOUT)."""
-        _check(self.lib.pbt_clip_status(self._handle, _current_stream(self.device.index)))
 
     def __del__(self):
         if getattr(self, "_handle", None):
@@ -317,6 +316,7 @@ class AdapterProjection:
         d.weight, d.ld_weight, d.A, d.B, d.scale = weight.data_ptr(), weight.stride(0), A.data_ptr(), B.data_ptr(), scale.data_ptr()
         d.bias = bias.data_ptr() if bias is not None else None
         self._status = torch.zeros(8, dtype=torch.int32, device=weight.device)
+        torch.cuda.current_stream(weight.device).synchronize()      # the calls may be on any stream
         d.status_device = self._status.data_ptr()
         d.row_offsets = d.adapter_ids = weight.data_ptr()
         _check(self.lib.pbt_adapter_query_workspace(C.byref(d), 0, C.byref(C.c_size_t(0))))

@@ -1,6 +1,6 @@
 """Gradient clipping (GradientClip / pbt_clip_*) against the definition in 64 bits.
 
-Tolerances.  A chunk's squares are summed in fp32 by 256 threads, at most 64 terms each (or half a dozen vectors), then in a
+Tolerances.  A chunk's squares are summed in fp32 by 256 threads, at most 64 terms each, then in a
 tree, and the chunks' sums in fp64: relative error of the sum of squares below (64 + 8) 2^-24, of the norm half of that,
 plus one rounding: 40 2^-24 = 2.4e-6.  A clipped element has the norm's error, one division and one multiplication on top:
 2.6e-6 in fp32; in bf16 its rounding (2^-8) dominates."""
@@ -128,6 +128,22 @@ def test_clip_squares_beyond_the_range_of_fp32(value, count):
     assert abs(norm - want) <= want * NORM_TOL
     if value:
         assert abs(out[7].item() - want / count) <= want / count * OUT_TOL["float32"] * 2
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("groups, n_groups", [([0, 1, 2, 3], 6), ([3, 1, 0, 1], 6), ([5, 5, 5, 5], 6), ([2, 0, 2, 1], 3)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_clip_many_megabytes_in_several_groups(groups, n_groups, in_place):
+    """Groups larger than L2's part, small ones and empty ones, in every order."""
+    import torch
+    import paper_1711_09846_b200 as pbt
+    gen = torch.Generator(device="cuda").manual_seed(n_groups)
+    grads = [torch.randn(n, generator=gen, device="cuda") for n in (13_000_001, 4_000_003, 9_000_000, 17)]
+    out = None if in_place else [torch.empty_like(g) for g in grads]
+    limits = [0.5 + k for k in range(n_groups)]
+    ref_norms, ref_out = _reference(grads, groups, n_groups, limits)
+    norms = pbt.GradientClip(grads, groups, out=out, n_groups=n_groups).run(torch.tensor(limits, device="cuda"))
+    _check(norms, grads if in_place else out, ref_norms, ref_out)
 
 
 @pytest.mark.gpu
