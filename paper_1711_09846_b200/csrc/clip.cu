@@ -40,6 +40,35 @@ struct __align__(16) ClipPiece {
   __device__ bool bf() const { return group2 & 1; }
 };
 
+// A tensor of the call.  Its chunks end on 16-byte boundaries of the source, but for the last one.
+struct ClipTensor {
+  const char* src;
+  char* dst;
+  long long numel;
+  int group2;
+  int first;       // its first chunk
+  __host__ __device__ long long per() const { return kClipChunk / (group2 & 1 ? 2 : 4); }
+  __host__ __device__ long long head() const { return (kClipChunk - (long long)((uintptr_t)src & 15)) / (group2 & 1 ? 2 : 4); }
+  __host__ __device__ long long chunks() const { return 1 + (numel > head() ? (numel - head() + per() - 1) / per() : 0); }
+  __host__ __device__ ClipPiece chunk(int k) const {
+    const long long from = k ? head() + (k - 1) * per() : 0, to = head() + k * per(), end = to < numel ? to : numel, esz = group2 & 1 ? 2 : 4;
+    return {src + from * esz, dst + from * esz, (int)(end - from), group2, {0, 0}};
+  }
+};
+
+// The table of chunks, when a handle is made: 140 thousand chunks of 80 tensors would take the host milliseconds.
+__global__ void k_clip_table(const ClipTensor* tensors, int n_tensors, ClipPiece* chunks, int n_chunks) {
+  const int c = blockIdx.x * blockDim.x + threadIdx.x;
+  if (c >= n_chunks) return;
+  int lo = 0, hi = n_tensors;      // the last tensor whose first chunk is not behind c
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (tensors[mid].first <= c) lo = mid;
+    else hi = mid;
+  }
+  chunks[c] = tensors[lo].chunk(c - tensors[lo].first);
+}
+
 struct ClipArgs {
   const ClipPiece* chunks;
   const int* begin;              // [groups + 1] first chunk of every group
@@ -274,34 +303,30 @@ int clip_check(const pbt_clip_tensor* t, int n, int n_groups) {
 }
 
 struct ClipTable {
-  std::vector<ClipPiece> chunks;
+  std::vector<ClipTensor> tensors;     // that have elements, by group
   std::vector<int> begin, empty;
-  std::vector<int> waves;      // first chunk of every wave, and the number of chunks
+  std::vector<int> waves;              // first chunk of every wave, and the number of chunks
+  int chunks;
 };
 bool clip_table(const pbt_clip_tensor* t, int n_tensors, int n_groups, ClipTable* out) {
   std::vector<int> order;
-  long long bytes = 0;
+  std::vector<long long> size(n_groups, 0);
   for (int i = 0; i < n_tensors; ++i)
     if (t[i].numel) {
       order.push_back(i);
-      bytes += t[i].numel * (t[i].dtype ? 2 : 4);
+      size[t[i].group] += t[i].numel * (t[i].dtype ? 2 : 4);
     }
-  if (bytes / kClipChunk + 2ll * n_tensors > (1ll << 30)) return false;
   std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return t[a].group < t[b].group; });
   out->begin.assign(n_groups + 1, 0);
-  std::vector<long long> size(n_groups, 0);
-  for (int i : order) size[t[i].group] += t[i].numel * (t[i].dtype ? 2 : 4);
+  long long chunks = 0;
   for (int i : order) {
-    const pbt_clip_tensor& x = t[i];
-    const long long esz = x.dtype ? 2 : 4;
-    for (long long done = 0; done < x.numel;) {
-      const char* src = (const char*)x.src + done * esz;
-      const long long take = std::min(x.numel - done, (kClipChunk - (long long)((uintptr_t)src & 15)) / esz);   // chunks end on 16-byte boundaries
-      out->chunks.push_back({src, (char*)x.dst + done * esz, (int)take, x.group * 2 + x.dtype, {0, 0}});
-      done += take;
-    }
-    out->begin[x.group + 1] = (int)out->chunks.size();
+    const ClipTensor x = {(const char*)t[i].src, (char*)t[i].dst, t[i].numel, t[i].group * 2 + t[i].dtype, (int)chunks};
+    out->tensors.push_back(x);
+    chunks += x.chunks();
+    if (chunks > (1 << 30)) return false;
+    out->begin[t[i].group + 1] = (int)chunks;
   }
+  out->chunks = (int)chunks;
   long long wave = 0;
   out->waves.assign(1, 0);
   for (int g = 0; g < n_groups; ++g) {
@@ -313,23 +338,24 @@ bool clip_table(const pbt_clip_tensor* t, int n_tensors, int n_groups, ClipTable
     }
     wave += size[g];
   }
-  out->waves.push_back((int)out->chunks.size());
+  out->waves.push_back(out->chunks);
   return true;
 }
 
 struct ClipLayout {
-  size_t done, sums, factors, begin, empty, chunks, total;
+  size_t done, sums, factors, begin, empty, tensors, chunks, total;
 };
 ClipLayout clip_layout(const ClipTable& t) {
   const size_t groups = t.begin.size() - 1;
   ClipLayout l;
   l.done = 0;
   l.sums = clip_align(groups * sizeof(unsigned int));
-  l.factors = l.sums + clip_align(t.chunks.size() * sizeof(double));
+  l.factors = l.sums + clip_align((size_t)t.chunks * sizeof(double));
   l.begin = l.factors + clip_align(groups * sizeof(float));
   l.empty = l.begin + clip_align(t.begin.size() * sizeof(int));
-  l.chunks = l.empty + clip_align(t.empty.size() * sizeof(int));
-  l.total = l.chunks + clip_align(t.chunks.size() * sizeof(ClipPiece));
+  l.tensors = l.empty + clip_align(t.empty.size() * sizeof(int));
+  l.chunks = l.tensors + clip_align(t.tensors.size() * sizeof(ClipTensor));
+  l.total = l.chunks + clip_align((size_t)t.chunks * sizeof(ClipPiece));
   return l;
 }
 
@@ -399,8 +425,12 @@ extern "C" int pbt_clip_create(pbt_clip_t** out, const pbt_clip_tensor* tensors,
     };
     upload(l.begin, t.begin.data(), t.begin.size() * sizeof(int));
     upload(l.empty, t.empty.data(), t.empty.size() * sizeof(int));
-    upload(l.chunks, t.chunks.data(), t.chunks.size() * sizeof(ClipPiece));
-    if (e == cudaSuccess) e = cudaStreamSynchronize(s);   // the tables above are this function's own
+    upload(l.tensors, t.tensors.data(), t.tensors.size() * sizeof(ClipTensor));
+    if (e == cudaSuccess && t.chunks) {
+      k_clip_table<<<(t.chunks + 255) / 256, 256, 0, s>>>((const ClipTensor*)(base + l.tensors), (int)t.tensors.size(), (ClipPiece*)(base + l.chunks), t.chunks);
+      e = cudaGetLastError();
+    }
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);   // the host's tables are this function's own, and runs may be on any stream
     if (e != cudaSuccess) return clip_fail(PBT_ERR_CUDA, cudaGetErrorString(e));
     pbt_clip* p = new pbt_clip();
     p->args.chunks = (const ClipPiece*)(base + l.chunks);
