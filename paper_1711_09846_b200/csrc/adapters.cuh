@@ -22,6 +22,9 @@ size_t tc_workspace(const pbt_adapter_desc* d, bool backward);
 cudaError_t tc_forward(const pbt_adapter_desc* d, const Segments& segs, char* workspace, cudaStream_t s);
 cudaError_t tc_backward(const pbt_adapter_desc* d, const Segments& segs, char* workspace, cudaStream_t s);
 
+// dA and dB as the sums of their splits, in order (parts: [splits][size] each)
+cudaError_t join_gradients(const float* parts_a, const float* parts_b, long long size_a, long long size_b, int splits, float* dA, float* dB, cudaStream_t s);
+
 #ifdef __CUDACC__
 __device__ __forceinline__ int segment_begin(const Segments& s, int j) { return min(max(__ldg(s.offsets + j), 0), s.rows); }
 __device__ __forceinline__ int segment_adapter(const Segments& s, int j) {
@@ -37,6 +40,14 @@ __device__ __forceinline__ int segment_of_row(const Segments& s, int row) {
     else hi = mid;
   }
   return lo - 1;
+}
+// The same for a whole warp, in one trip to memory instead of one per halving (offsets ascend: those at or before the row count).
+__device__ __forceinline__ int segment_of_row_warp(const Segments& s, int row) {
+  if (s.n > 1024) return segment_of_row(s, row);
+  int count = 0;
+  for (int i = threadIdx.x & 31; i < s.n; i += 32) count += segment_begin(s, i) <= row;
+  count = __reduce_add_sync(0xFFFFFFFFu, count);
+  return count - 1;
 }
 #endif
 

@@ -993,6 +993,11 @@ cudaError_t pack(const void*& src, long long& ld, long long rows, int cols, char
 
 }  // namespace
 
+cudaError_t join_gradients(const float* parts_a, const float* parts_b, long long size_a, long long size_b, int splits, float* dA, float* dB, cudaStream_t s) {
+  const long long n = size_a + size_b;
+  return launch_with((unsigned)std::min<long long>((n + 255) / 256, 148 * 16), 256, 0, s)(k_adapter_grad_join, parts_a, parts_b, size_a, size_b, splits, dA, dB);
+}
+
 size_t tc_workspace(const pbt_adapter_desc* d, bool backward) { return plan(d, backward).total; }
 
 #define STEP(call) do { const cudaError_t e_ = (call); if (e_ != cudaSuccess) return e_; } while (0)
@@ -1068,8 +1073,7 @@ cudaError_t tc_backward(const pbt_adapter_desc* d, const Segments& segs, char* w
                              : p.rp == 48 ? launch_grad<48>(mx, mds, mdy, ms, g, st) : launch_grad<64>(mx, mds, mdy, ms, g, st);
   STEP(launched);
   if (p.splits > 1) {
-    const long long n = g.stride_a + g.stride_b;
-    STEP(launch_with((unsigned)std::min<long long>((n + 255) / 256, 148 * 16), 256, 0, st)(k_adapter_grad_join, g.dA, g.dB, g.stride_a, g.stride_b, p.splits, d->dA, d->dB));
+    STEP(join_gradients(g.dA, g.dB, g.stride_a, g.stride_b, p.splits, d->dA, d->dB, st));
   }
   return cudaSuccess;
 }
