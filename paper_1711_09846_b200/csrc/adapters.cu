@@ -268,7 +268,7 @@ struct GradSide {
 // 156 us, by rows 221), or every fourth row (added up in shared memory; 256 -> 512, rank 32: 118 us, by ranks, which read every row
 // four times, 139).
 template <int RANK>
-__global__ void __launch_bounds__(256, 4) k_adapter_grad_f32(const GradSide x, const GradSide dy, int rank, Segments segs) {
+__global__ void __launch_bounds__(256, RANK == 32 ? 3 : 4) k_adapter_grad_f32(const GradSide x, const GradSide dy, int rank, Segments segs) {
   pdl_prologue();
   constexpr bool kByRank = RANK >= 64;
   constexpr int R = kByRank ? RANK / 4 : RANK, kRowParts = kByRank ? 1 : 4;
