@@ -80,11 +80,15 @@ __device__ __forceinline__ void ldmatrix4_trans(uint32_t* r, uint32_t addr) {
 }
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
-__device__ __forceinline__ void store_terms(bf16* row, int rp, int col, float v, int terms) {
-  for (int t = 0; t < terms; ++t) {
-    const bf16 h = __float2bfloat16_rn(v);
-    row[t * rp + col] = h;
-    v -= __bfloat162float(h);
+// two neighbouring columns (col is even), as one summand or three
+__device__ __forceinline__ void store_terms(bf16* row, int rp, int col, float v0, float v1, bool three) {
+#pragma unroll
+  for (int t = 0; t < 3; ++t) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(v0, v1);
+    *reinterpret_cast<__nv_bfloat162*>(row + t * rp + col) = h;
+    if (!three) return;
+    v0 -= __low2float(h);
+    v1 -= __high2float(h);
   }
 }
 
@@ -196,6 +200,19 @@ __global__ void __launch_bounds__(256, NT <= 2 ? 2 : 1) k_adapter_shrink(const S
   };
 #pragma unroll
   for (int s = 0; s < Ring::kStages; ++s) ask(part * 64 + s * parts * 64, s);
+  // the second matrix's elements that this thread splits at the end: a pair of columns each
+  constexpr int kPairs = NT < 2 ? 2 : NT;
+  const int half = a.rp / 2;
+  const float f = __ldg(a.scale + adapter);
+  float second[kPairs][2] = {};
+  if (a.kept)
+#pragma unroll
+    for (int u = 0; u < kPairs; ++u) {
+      const int i = tid + u * 256, r = i / half, c = i % half * 2;
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        if (r < hi - lo && c + e < a.rank) second[u][e] = __ldg(a.kept + (long long)(lo + r) * a.rank + c + e);
+    }
   float acc[2][NT][4] = {};
   int stage = 0;
   for (int k0 = part * 64; k0 < a.K; k0 += parts * 64) {
@@ -248,20 +265,23 @@ __global__ void __launch_bounds__(256, NT <= 2 ? 2 : 1) k_adapter_shrink(const S
       for (int e = 0; e < 2; ++e)
         *reinterpret_cast<float2*>(&red[(warp * 32 + m * 16 + gr + 8 * e) * (NT * 8) + n * 8 + tq * 2]) = make_float2(acc[m][n][2 * e], acc[m][n][2 * e + 1]);
   __syncthreads();
-  const float f = a.scale[adapter];
   const int width = a.terms * a.rp;
-  for (int i = tid; i < (hi - lo) * a.rp; i += 256) {
-    const int r = i / a.rp, c = i % a.rp;
+#pragma unroll
+  for (int u = 0; u < kPairs; ++u) {
+    const int i = tid + u * 256, r = i / half, c = i % half * 2;
+    if (r >= hi - lo) break;
     const long long row = lo + r;
-    float v = 0.f;
-    if (c < a.rank) {
-      for (int p = 0; p < parts; ++p) v += red[(((r >> 5) * parts + p) * 32 + (r & 31)) * (NT * 8) + c];
-      if (a.s) a.s[row * a.rank + c] = v;
-      if (a.scaled) a.scaled[row * a.rank + c] = f * v;
-    }
+    float v[2] = {0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      if (c + e < a.rank) {
+        for (int p = 0; p < parts; ++p) v[e] += red[(((r >> 5) * parts + p) * 32 + (r & 31)) * (NT * 8) + c + e];
+        if (a.s) a.s[row * a.rank + c + e] = v[e];
+        if (a.scaled) a.scaled[row * a.rank + c + e] = f * v[e];
+      }
     if (!a.planes) continue;
-    store_terms(a.planes + row * width, a.rp, c, f * v, a.terms);
-    if (a.kept) store_terms(a.kept_planes + row * 3 * a.rp, a.rp, c, c < a.rank ? f * a.kept[row * a.rank + c] : 0.f, 3);
+    store_terms(a.planes + row * width, a.rp, c, f * v[0], f * v[1], a.terms == 3);
+    if (a.kept) store_terms(a.kept_planes + row * 3 * a.rp, a.rp, c, f * second[u][0], f * second[u][1], true);
   }
 }
 
