@@ -72,6 +72,9 @@ __global__ void __launch_bounds__(256) k_adapter_shrink_f32(const float* __restr
 // diverged adapter reaches its own rows only).  The CTA's threads are KG groups that share a chunk's k, so that small tiles keep
 // eight warps busy.  Chunks come by cp.async, 16 bytes at a time where the operand's rows allow it, else element by element.
 // Bound by the ALUs' issue: 2048 x 256 -> 512, rank 4 takes 22 us, 0.3 of the fp32 rate; 8192 x 512 -> 512 140 us, 0.4.
+// A narrow tile with more segments than 2 + rank / 16 leaves the low-rank part to its last step, where every thread multiplies out its own
+// elements (60 single rows, 72 -> 200, rank 4: a whole call 11 us, with chunks 24; 871 rows in segments of 13, 104 -> 152, rank 64, which has
+// chunks: 18.5 us, element by element 25).
 // A thread's rows and columns are BM / TM and BN / TN apart (columns of a TRANS chunk adjacent): the vectors that a warp reads
 // then lie in different banks.
 template <int BM_, int BN_, int TM_, int TN_, int BK_, int STAGES_>
@@ -167,7 +170,8 @@ __global__ void __launch_bounds__(256, 2) k_adapter_product_f32(const ProductArg
     if (lane == 0) n_segs = n;
   }
   __syncthreads();
-  const int turns = chunks + n_segs * low_chunks;
+  const bool direct = P::BM <= 16 && n_segs > 2 + a.rank / 16;
+  const int turns = chunks + (direct ? 0 : n_segs * low_chunks);
   for (int t = first; t < P::STAGES - 1; ++t) {
     if (t < turns) load(t);
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -229,6 +233,26 @@ __global__ void __launch_bounds__(256, 2) k_adapter_product_f32(const ProductArg
     float v = product_smem[row * P::BN + n];
 #pragma unroll
     for (int q = 1; q < P::KG; ++q) v += product_smem[(q * P::BM + row) * P::BN + n];
+    if (direct)
+      for (int q = 0; q < n_segs; ++q) {
+        if (row < seg_lo[q] || row >= seg_hi[q]) continue;
+        const int adapter = seg_adapter[q];
+        const float* s = a.s + (long long)(row0 + row) * a.rank;
+        const float* m = a.mats + (long long)adapter * a.rank * a.N + (TRANS ? n0 + n : (long long)(n0 + n) * a.rank);
+        float low = 0.f;
+        if (!TRANS && a.vec_s && a.vec_m) {
+#pragma unroll 8
+          for (int j = 0; j < a.rank; j += 4) {
+            const float4 u = __ldg(reinterpret_cast<const float4*>(s + j)), w = __ldg(reinterpret_cast<const float4*>(m + j));
+            low = __fmaf_rn(u.x, w.x, __fmaf_rn(u.y, w.y, __fmaf_rn(u.z, w.z, __fmaf_rn(u.w, w.w, low))));
+          }
+        } else {
+#pragma unroll 8
+          for (int j = 0; j < a.rank; ++j) low = __fmaf_rn(__ldg(s + j), __ldg(TRANS ? m + (long long)j * a.N : m + j), low);
+        }
+        v = __fmaf_rn(a.scale ? __ldg(a.scale + adapter) : 1.f, low, v);
+        break;
+      }
     a.y[(row0 + row) * a.ldy + n0 + n] = v + bias;
   }
 }

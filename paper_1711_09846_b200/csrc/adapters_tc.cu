@@ -19,6 +19,7 @@
 // cores' accumulation truncates (about 2^-24 of the accumulator per instruction), so chains are kept short: the shrink
 // folds its accumulators into fp32 registers every 64 columns, the gradients every 128 rows.
 #include <algorithm>
+#include <type_traits>
 
 #include "adapters.cuh"
 #include "tc_epilogue.cuh"
@@ -306,7 +307,9 @@ cudaError_t launch_shrink(ShrinkArgs a, cudaStream_t s) {
 // ------------------------------------------------------------------------------------------------------------------
 // Shared product with the low-rank block
 // ------------------------------------------------------------------------------------------------------------------
-constexpr int kGemmStages128 = 4, kGemmStages256 = 3, kGemmEpiWarps = 8;
+// The wide tiles have four epilogue warps and a fourth stage where a CTA has several tiles (a training step of 40960 x 2048 -> 2048: 691 us,
+// with eight warps and three stages 715; 10240 x 1024 -> 1024: 115 and 126), eight where its only tile's epilogue is not hidden behind
+// the next one (3001 x 784 -> 1024, one wave: 19.1 us, with four warps 22.5).
 
 struct LowRank {
   Segments segs;
@@ -351,28 +354,28 @@ __device__ __forceinline__ void umma_bf16_rows(uint32_t tmem_d, uint64_t adesc, 
       : "memory");
 }
 
-template <int BN, int STAGES>
+template <int BN, int STAGES, int EPI>
 struct GemmSmem {
   static constexpr int kABytes = kBM * kBK * 2;
   static constexpr int kBBytes = BN * kBK * 2;
   static constexpr int kStageBytes = kABytes + kBBytes;
   static constexpr int kEpiOffset = STAGES * kStageBytes;
   static constexpr int kEpiBytesPerWarp = 32 * kEpiPitch * 4;
-  static constexpr int kBarOffset = kEpiOffset + kGemmEpiWarps * kEpiBytesPerWarp;
+  static constexpr int kBarOffset = kEpiOffset + EPI * kEpiBytesPerWarp;
   static constexpr int kTotal = kBarOffset + 256 + 1024;
   static_assert(kTotal <= 232448, "shared memory budget of one CTA");
 };
 
-// Roles as in the member-batched GEMM: warp 0 TMA producer, warp 1 MMA issuer, 8 epilogue warps, double-buffered
+// Roles as in the member-batched GEMM: warp 0 TMA producer, warp 1 MMA issuer, EPI epilogue warps, double-buffered
 // accumulator.  After a tile's k-blocks both walk its segments: one more stage each, 128 rows of the low-rank operand and
 // the adapter's matrix (columns past the rank are out of the tensor map and arrive as zeros).  Launched while the shrink
 // runs; the two threads that read what it leaves (the tiles' first segments, the planes through TMA) wait for its end
 // after the k-blocks of their first tile.
-template <int BN, int STAGES, bool B_MN>
-__global__ void __launch_bounds__(64 + 32 * kGemmEpiWarps, 1)
+template <int BN, int STAGES, int EPI, bool B_MN>
+__global__ void __launch_bounds__(64 + 32 * EPI, 1)
 k_adapter_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmP,
                const __grid_constant__ CUtensorMap tmL, const TcParams p, const LowRank low) {
-  using L = GemmSmem<BN, STAGES>;
+  using L = GemmSmem<BN, STAGES, EPI>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBarOffset);
@@ -386,7 +389,7 @@ k_adapter_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(&tfull[a], 1); mbar_init(&tempty[a], kGemmEpiWarps); }
+    for (int a = 0; a < 2; ++a) { mbar_init(&tfull[a], 1); mbar_init(&tempty[a], EPI); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -504,7 +507,7 @@ k_adapter_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       const int acc = it & 1;
       if (!mbar_wait(&tfull[acc], (it >> 1) & 1, abort_flag)) { ok = false; break; }
       tc_fence_after();
-      epilogue_tile<BN, kGemmEpiWarps>(p, buf, tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN), 0, m0, n0, q, half, lane, vec_ok);
+      epilogue_tile<BN, EPI>(p, buf, tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN), 0, m0, n0, q, half, lane, vec_ok);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&tempty[acc]);
@@ -520,16 +523,16 @@ k_adapter_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   if (warp == 1) tmem_dealloc(tmem_base, kTmemCols);
 }
 
-template <int BN, int STAGES, bool B_MN>
+template <int BN, int STAGES, int EPI, bool B_MN>
 cudaError_t launch_gemm(const CUtensorMap* maps, TcParams& p, const LowRank& low, cudaStream_t s) {
-  using L = GemmSmem<BN, STAGES>;
+  using L = GemmSmem<BN, STAGES, EPI>;
   static DeviceSetup setup;
   int sms = 0;
-  const cudaError_t e = device_setup(&setup, k_adapter_gemm<BN, STAGES, B_MN>, L::kTotal, &sms);
+  const cudaError_t e = device_setup(&setup, k_adapter_gemm<BN, STAGES, EPI, B_MN>, L::kTotal, &sms);
   if (e != cudaSuccess) return e;
   p.tiles_n = (p.N + BN - 1) / BN;
   p.num_tiles = p.tiles_m * p.tiles_n;
-  return launch_after(p.num_tiles < sms ? p.num_tiles : sms, 64 + 32 * kGemmEpiWarps, L::kTotal, s, k_adapter_gemm<BN, STAGES, B_MN>, maps[0], maps[1], maps[2],
+  return launch_after(p.num_tiles < sms ? p.num_tiles : sms, 64 + 32 * EPI, L::kTotal, s, k_adapter_gemm<BN, STAGES, EPI, B_MN>, maps[0], maps[1], maps[2],
                       maps[3], p, low);
 }
 
@@ -567,14 +570,18 @@ cudaError_t launch_gemm(const GemmCall& c, const Segments& segs, const int* tile
     ok = ok && make_map(&maps[3], c.mats, c.N, c.rank, c.mat_pitch, segs.n_adapters, (long long)c.rank * c.mat_pitch, kBK);
   }
   if (!ok) return cudaErrorInvalidValue;
-  if (c.b_mn) return wide ? launch_gemm<256, kGemmStages256, true>(maps, p, low, s) : launch_gemm<128, kGemmStages128, true>(maps, p, low, s);
-  return wide ? launch_gemm<256, kGemmStages256, false>(maps, p, low, s) : launch_gemm<128, kGemmStages128, false>(maps, p, low, s);
+  const bool one_wave = wide_tiles <= 148;
+  auto launch = [&](auto b_mn) {
+    if (!wide) return launch_gemm<128, 4, 8, decltype(b_mn)::value>(maps, p, low, s);
+    return one_wave ? launch_gemm<256, 3, 8, decltype(b_mn)::value>(maps, p, low, s) : launch_gemm<256, 4, 4, decltype(b_mn)::value>(maps, p, low, s);
+  };
+  return c.b_mn ? launch(std::true_type()) : launch(std::false_type());
 }
 
 // ------------------------------------------------------------------------------------------------------------------
 // Few rows
 // ------------------------------------------------------------------------------------------------------------------
-constexpr int kRowsMost = 64;
+constexpr int kRowsMost = 64;      // rows of a CTA
 constexpr int kRowsOut = 16;      // output columns of a CTA
 
 struct RowsArgs {
@@ -605,11 +612,11 @@ __global__ void __launch_bounds__(256) k_adapter_rows(const RowsArgs a) {
   extern __shared__ __align__(16) uint8_t rows_smem[];
   typedef RowsRing<GROUPS> Ring;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gr = lane >> 2, tq = lane & 3;
-  const int n0 = blockIdx.x * kRowsOut;
+  const int n0 = blockIdx.x * kRowsOut, t0 = blockIdx.y * kRowsMost, T = min(a.T - t0, kRowsMost);
   uint8_t* ring = rows_smem + warp * (Ring::kStages * Ring::kBytes) + lane * 16;
   const bf16* w0 = a.w + (long long)(n0 + gr) * a.ldw;
   const bf16* w1 = w0 + 8 * a.ldw;
-  const bf16* x = a.x + gr * a.ldx;
+  const bf16* x = a.x + (t0 + gr) * a.ldx;
   const bool in0 = n0 + gr < a.N, in1 = n0 + gr + 8 < a.N;
   auto put = [&](uint8_t* slot, const bf16* from, bool in) {
     if (in) copy16(slot, from);
@@ -625,7 +632,7 @@ __global__ void __launch_bounds__(256) k_adapter_rows(const RowsArgs a) {
         put(to + h * 512, w0 + k, in && in0);
         put(to + (2 + h) * 512, w1 + k, in && in1);
 #pragma unroll
-        for (int g = 0; g < GROUPS; ++g) put(to + (4 + 2 * g + h) * 512, x + g * 8 * a.ldx + k, in && g * 8 + gr < a.T);
+        for (int g = 0; g < GROUPS; ++g) put(to + (4 + 2 * g + h) * 512, x + g * 8 * a.ldx + k, in && g * 8 + gr < T);
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -664,8 +671,8 @@ __global__ void __launch_bounds__(256) k_adapter_rows(const RowsArgs a) {
   float* low = red + 8 * kRowsOut * Ring::kPitch;          // scaled S of the rows
   int* owner = reinterpret_cast<int*>(low + GROUPS * 8 * kMaxRank);
   asm volatile("griddepcontrol.wait;" ::: "memory");     // the shrink is complete and its results are visible
-  for (int i = threadIdx.x; i < a.T * a.rank; i += 256) low[(i / a.rank) * a.pitch + i % a.rank] = __ldcg(a.scaled + i);
-  if (threadIdx.x < a.T) owner[threadIdx.x] = __ldcg(a.row_adapter + threadIdx.x);
+  for (int i = threadIdx.x; i < T * a.rank; i += 256) low[(i / a.rank) * a.pitch + i % a.rank] = __ldcg(a.scaled + (long long)t0 * a.rank + i);
+  if (threadIdx.x < T) owner[threadIdx.x] = __ldcg(a.row_adapter + t0 + threadIdx.x);
   __syncthreads();
   // a thread has one column and every 16th row, whose adapters' matrices it asks for together
   const int n = threadIdx.x % kRowsOut, col = n0 + n;
@@ -677,7 +684,7 @@ __global__ void __launch_bounds__(256) k_adapter_rows(const RowsArgs a) {
   for (int u = 0; u < kMine; ++u) {
     const int t = threadIdx.x / kRowsOut + 16 * u;
     v[u] = bias;
-    if (t < a.T)
+    if (t < T)
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[u] += red[(k * kRowsOut + n) * Ring::kPitch + t];
   }
@@ -685,13 +692,13 @@ __global__ void __launch_bounds__(256) k_adapter_rows(const RowsArgs a) {
     uint4 bv[kMine];
 #pragma unroll
     for (int u = 0; u < kMine; ++u) {
-      const int t = threadIdx.x / kRowsOut + 16 * u, adapter = t < a.T ? owner[t] : -1;
+      const int t = threadIdx.x / kRowsOut + 16 * u, adapter = t < T ? owner[t] : -1;
       bv[u] = adapter >= 0 ? __ldg(reinterpret_cast<const uint4*>(a.B + ((long long)adapter * a.N + col) * a.pitch + j)) : make_uint4(0u, 0u, 0u, 0u);
     }
 #pragma unroll
     for (int u = 0; u < kMine; ++u) {
       const int t = threadIdx.x / kRowsOut + 16 * u;
-      if (t < a.T && owner[t] >= 0)
+      if (t < T && owner[t] >= 0)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const uint32_t pairs = word(bv[u], e >> 1);
@@ -702,7 +709,7 @@ __global__ void __launch_bounds__(256) k_adapter_rows(const RowsArgs a) {
 #pragma unroll
   for (int u = 0; u < kMine; ++u) {
     const int t = threadIdx.x / kRowsOut + 16 * u;
-    if (t < a.T) a.y[t * a.ldy + col] = __float2bfloat16_rn(v[u]);
+    if (t < T) a.y[(t0 + t) * a.ldy + col] = __float2bfloat16_rn(v[u]);
   }
 }
 
@@ -712,7 +719,7 @@ cudaError_t launch_rows(const RowsArgs& a, cudaStream_t s) {
   int sms = 0;
   const cudaError_t e = device_setup(&setup, k_adapter_rows<GROUPS>, RowsRing<GROUPS>::kTotal, &sms);
   if (e != cudaSuccess) return e;
-  return launch_after((a.N + kRowsOut - 1) / kRowsOut, 256, RowsRing<GROUPS>::kTotal, s, k_adapter_rows<GROUPS>, a);
+  return launch_after(dim3((a.N + kRowsOut - 1) / kRowsOut, (a.T + kRowsMost - 1) / kRowsMost), 256, RowsRing<GROUPS>::kTotal, s, k_adapter_rows<GROUPS>, a);
 }
 cudaError_t launch_rows(const RowsArgs& a, cudaStream_t s) {
   if (a.T <= 8) return launch_rows<1>(a, s);
@@ -974,7 +981,14 @@ Plan plan(const pbt_adapter_desc* d, bool backward) {
   const size_t rows = (size_t)d->rows;
   p.rp = round_up(d->rank, 16);
   p.pack_x = !aligned(d->x, d->ld_x) || d->inputs % 8;     // (vector loads end with the row)
-  p.pack_w = !aligned(d->weight, d->ld_weight) || (!backward && d->rows <= kRowsMost && d->inputs % 8);
+  // Few rows, or many short segments: the product has a low-rank block for every segment of a 128-row tile (12 us and 0.4 for each), k_adapter_rows
+  // a wave of CTAs for every 148 of its 64 rows x 16 columns (6 us and 8.5 for each, less below 1024 inputs).  1024 -> 1024, rank 16: 128 single rows 12.4 us, as a product
+  // 57; 64 segments of four rows 18.6 and 24.7; 2048 -> 2048, 80 segments of four rows 49 and 33;
+  // 512 -> 512, rank 8 the same 12.4 and 22.6.
+  const long long waves = ((long long)((d->rows + kRowsMost - 1) / kRowsMost) * ((d->outputs + kRowsOut - 1) / kRowsOut) + 147) / 148;
+  const int tile_segments = std::min(kBM, d->n_segments / ((d->rows + kBM - 1) / kBM + (d->rows == 0)));
+  p.few = !backward && (d->rows <= kRowsMost || std::min(21, 1 + d->inputs / 48) * waves < 15 + tile_segments);
+  p.pack_w = !aligned(d->weight, d->ld_weight) || (p.few && d->inputs % 8);
   p.pack_a = !aligned(d->A, d->inputs);
   p.pack_b = !aligned(d->B, d->rank);
   p.pack_dy = backward && (!aligned(d->dy, d->ld_dy) || d->outputs % 8);
@@ -992,7 +1006,6 @@ Plan plan(const pbt_adapter_desc* d, bool backward) {
   p.a = take(p.pack_a, (size_t)d->n_adapters * d->rank * round_up(d->inputs, 8) * 2);
   p.b = take(p.pack_b, (size_t)d->n_adapters * d->outputs * round_up(d->rank, 8) * 2);
   p.dy = take(p.pack_dy, rows * round_up(d->outputs, 8) * 2);
-  p.few = !backward && d->rows <= kRowsMost;
   p.planes = take(true, p.few ? rows * d->rank * sizeof(float) : rows * p.rp * 2 * (backward ? 3 : 1));
   p.kept = take(backward, rows * p.rp * 2 * 3);
   p.table = take(true, (p.few ? rows : (rows + kBM - 1) / kBM) * sizeof(int));

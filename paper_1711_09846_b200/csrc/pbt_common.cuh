@@ -87,10 +87,10 @@ inline LaunchCfg launch_with(dim3 grid, dim3 block, size_t smem, cudaStream_t st
 // that everything before it is complete), and the kernel waits for its end (griddepcontrol.wait) in the threads that read what it
 // leaves or write what it reads, before they do.
 template <typename... KArgs, typename... Args>
-cudaError_t launch_after(unsigned grid, unsigned threads, size_t smem, cudaStream_t s, void (*kernel)(KArgs...), Args&&... args) {
+cudaError_t launch_after(dim3 grid, unsigned threads, size_t smem, cudaStream_t s, void (*kernel)(KArgs...), Args&&... args) {
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
