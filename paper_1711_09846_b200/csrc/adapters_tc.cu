@@ -1,7 +1,7 @@
 // bf16 adapters on the tensor cores.  Three kernels carry both directions:
 //
 //   k_adapter_shrink   S = x A_a^T (or dS = c dy B_a): a product with r <= 64 columns, bound by reading x once; rows of
-//                      one (64-row tile, segment) pair per CTA, mma.sync fed by 16-byte loads straight from global memory
+//                      one (tile of at most 64 rows, segment) pair per CTA, mma.sync fed by 16-byte loads straight from global memory
 //   k_adapter_gemm     y = x W^T + bias + c S B_a^T (or dx = dy W + dS A_a): the shared product on tcgen05, with the
 //                      low-rank product as one more block of the same contraction in the same TMEM accumulator
 //   k_adapter_rows     the same product for a few rows (one token of many requests): bound by reading W once, mma.sync
@@ -33,21 +33,38 @@ using namespace tc;
 // ------------------------------------------------------------------------------------------------------------------
 // Operands whose rows are not multiples of 16 bytes are copied once into rows that are.
 // ------------------------------------------------------------------------------------------------------------------
-__global__ void __launch_bounds__(256) k_pack_rows(const bf16* __restrict__ src, long long ld, long long rows, int cols, bf16* __restrict__ dst,
-                                                   int ld_dst) {
+struct PackJob {
+  const bf16* src; long long ld;
+  bf16* dst;
+  long long rows;
+  int cols, to;                // elements of a row, and rounded up to 8
+  unsigned block0;             // its first block
+};
+struct PackJobs {
+  PackJob job[5];
+  int n;
+};
+// All operands of a call in one launch; a thread has 8 elements.
+__global__ void __launch_bounds__(256) k_pack_rows(const PackJobs a) {
   pdl_prologue();
-  const long long n = rows * ld_dst;
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
-    const long long r = i / ld_dst;
-    const int c = (int)(i % ld_dst);
-    dst[i] = c < cols ? src[r * ld + c] : __float2bfloat16_rn(0.f);
-  }
+  int q = 0;
+  while (q + 1 < a.n && blockIdx.x >= a.job[q + 1].block0) ++q;
+  const PackJob j = a.job[q];
+  const long long i = (long long)(blockIdx.x - j.block0) * 256 + threadIdx.x;
+  const int per_row = j.to / 8;
+  const long long row = i / per_row;
+  if (row >= j.rows) return;
+  const int c = (int)(i - row * per_row) * 8;
+  const bf16* from = j.src + row * j.ld + c;
+  __align__(16) bf16 v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = c + e < j.cols ? from[e] : __float2bfloat16_rn(0.f);
+  *reinterpret_cast<uint4*>(j.dst + row * j.to + c) = *reinterpret_cast<const uint4*>(v);
 }
 
 // ------------------------------------------------------------------------------------------------------------------
 // Shrink
 // ------------------------------------------------------------------------------------------------------------------
-constexpr int kShrinkRows = 64;
 
 struct ShrinkArgs {
   const bf16* x; long long ldx; int K;
@@ -55,7 +72,7 @@ struct ShrinkArgs {
   int rank, rp;                       // rp: columns of a plane, the rank rounded up to 16
   const float* scale;
   Segments segs;
-  int n_tiles;
+  int tile, n_tiles;                  // rows of a tile
   float* s;                           // fp32 result, not scaled (may be null)
   float* scaled;                      // scaled fp32 result [rows][rank], for k_adapter_rows (null: planes instead)
   int* row_adapter;                   // adapter of every row or -1, for k_adapter_rows
@@ -126,17 +143,18 @@ __global__ void __launch_bounds__(256, NT <= 2 ? 2 : 1) k_adapter_shrink(const S
   int j = -1;
   for (int base = 0; base < g.n; base += 256) {
     const int i = base + tid;
-    j += __syncthreads_count(i < g.n && segment_begin(g, i) / kShrinkRows + i <= q);
+    j += __syncthreads_count(i < g.n && segment_begin(g, i) / a.tile + i <= q);
   }
   if (j < 0) return;
   const int t = q - j;
   const int adapter = segment_adapter(g, j);
-  const int lo = max(segment_begin(g, j), t * kShrinkRows), hi = min(segment_begin(g, j + 1), (t + 1) * kShrinkRows);
+  const int lo = max(segment_begin(g, j), t * a.tile), hi = min(segment_begin(g, j + 1), min((t + 1) * a.tile, g.rows));
   if (lo >= hi || adapter < 0) return;
 
   const int warp = tid >> 5, lane = tid & 31, gr = lane >> 2, tq = lane & 3;
   const int groups = hi - lo > 32 ? 2 : 1, parts = 8 / groups;     // few rows: more warps share the columns
   const int group = warp / parts, part = warp % parts;
+  const bool both = hi - lo > 16;     // rows for the second fragment of 16
   const int nt8 = TRANS ? a.pitch / 8 : (a.rank + 7) / 8;
   const bf16* mat = a.mats + (long long)adapter * (TRANS ? (long long)a.K : (long long)a.rank) * a.pitch;
   const bf16* xrow[4];
@@ -242,7 +260,7 @@ __global__ void __launch_bounds__(256, NT <= 2 ? 2 : 1) k_adapter_shrink(const S
         for (int s = 0; s < 2; ++s)
 #pragma unroll
           for (int m = 0; m < 2; ++m)
-            mma16816(sum[m][n], word(xv[2 * m], 2 * s), word(xv[2 * m + 1], 2 * s), word(xv[2 * m], 2 * s + 1), word(xv[2 * m + 1], 2 * s + 1),
+            if (m == 0 || both) mma16816(sum[m][n], word(xv[2 * m], 2 * s), word(xv[2 * m + 1], 2 * s), word(xv[2 * m], 2 * s + 1), word(xv[2 * m + 1], 2 * s + 1),
                      b[2 * s], b[2 * s + 1]);
       }
     }
@@ -296,7 +314,11 @@ cudaError_t launch_shrink(const ShrinkArgs& a, unsigned grid, cudaStream_t s) {
 }
 template <bool TRANS>
 cudaError_t launch_shrink(ShrinkArgs a, cudaStream_t s) {
-  a.n_tiles = (a.segs.rows + kShrinkRows - 1) / kShrinkRows;
+  // A CTA's time is its matrix instructions: smaller tiles, whose warps share the columns, while there are SMs for them (242 rows x 1496 -> 1096
+  // in two segments, rank 64: a training step 72 us, with tiles of 64 rows 94)
+  a.tile = 64;
+  while (a.tile > 16 && a.segs.rows / a.tile + a.segs.n < 148) a.tile /= 2;
+  a.n_tiles = (a.segs.rows + a.tile - 1) / a.tile;
   const unsigned grid = (unsigned)(a.n_tiles + a.segs.n + (a.n_table + 255) / 256);
   if (a.rank <= 8) return launch_shrink<TRANS, 1>(a, grid, s);
   if (a.rank <= 16) return launch_shrink<TRANS, 2>(a, grid, s);
@@ -1014,15 +1036,21 @@ Plan plan(const pbt_adapter_desc* d, bool backward) {
   return p;
 }
 
-cudaError_t pack(const void*& src, long long& ld, long long rows, int cols, char* dst, cudaStream_t s) {
-  const int to = round_up(cols, 8);
-  const long long n = rows * to;
-  const unsigned grid = (unsigned)std::max<long long>(1, std::min<long long>((n + 1023) / 1024, 148 * 16));
-  const cudaError_t e = launch_with(grid, 256, 0, s)(k_pack_rows, (const bf16*)src, ld, rows, cols, (bf16*)dst, to);
-  src = dst;
-  ld = to;
-  return e;
-}
+// collects an operand to pack, and stands for the packed one from then on
+struct Packer {
+  PackJobs jobs;
+  unsigned blocks;
+  Packer() : blocks(0) { jobs.n = 0; }
+  void add(bool want, const void*& src, long long& ld, long long rows, int cols, char* dst) {
+    if (!want) return;
+    const int to = round_up(cols, 8);
+    jobs.job[jobs.n++] = {(const bf16*)src, ld, (bf16*)dst, rows, cols, to, blocks};
+    blocks += (unsigned)((rows * (to / 8) + 255) / 256);
+    src = dst;
+    ld = to;
+  }
+  cudaError_t run(cudaStream_t s) const { return blocks ? launch_with(blocks, 256, 0, s)(k_pack_rows, jobs) : cudaSuccess; }
+};
 
 }  // namespace
 
@@ -1039,10 +1067,12 @@ cudaError_t tc_forward(const pbt_adapter_desc* d, const Segments& segs, char* ws
   const Plan p = plan(d, false);
   const void *x = d->x, *w = d->weight, *A = d->A, *B = d->B;
   long long ldx = d->ld_x, ldw = d->ld_weight, lda = d->inputs, ldb = d->rank;
-  if (p.pack_x) STEP(pack(x, ldx, d->rows, d->inputs, ws + p.x, st));
-  if (p.pack_w) STEP(pack(w, ldw, d->outputs, d->inputs, ws + p.w, st));
-  if (p.pack_a) STEP(pack(A, lda, (long long)d->n_adapters * d->rank, d->inputs, ws + p.a, st));
-  if (p.pack_b) STEP(pack(B, ldb, (long long)d->n_adapters * d->outputs, d->rank, ws + p.b, st));
+  Packer pk;
+  pk.add(p.pack_x, x, ldx, d->rows, d->inputs, ws + p.x);
+  pk.add(p.pack_w, w, ldw, d->outputs, d->inputs, ws + p.w);
+  pk.add(p.pack_a, A, lda, (long long)d->n_adapters * d->rank, d->inputs, ws + p.a);
+  pk.add(p.pack_b, B, ldb, (long long)d->n_adapters * d->outputs, d->rank, ws + p.b);
+  STEP(pk.run(st));
   ShrinkArgs a;
   memset(&a, 0, sizeof(a));
   a.x = (const bf16*)x; a.ldx = ldx; a.K = d->inputs;
@@ -1068,11 +1098,13 @@ cudaError_t tc_backward(const pbt_adapter_desc* d, const Segments& segs, char* w
   const Plan p = plan(d, true);
   const void *x = d->x, *w = d->weight, *A = d->A, *B = d->B, *dy = d->dy;
   long long ldx = d->ld_x, ldw = d->ld_weight, lda = d->inputs, ldb = d->rank, lddy = d->ld_dy;
-  if (p.pack_x) STEP(pack(x, ldx, d->rows, d->inputs, ws + p.x, st));
-  if (p.pack_w) STEP(pack(w, ldw, d->outputs, d->inputs, ws + p.w, st));
-  if (p.pack_a) STEP(pack(A, lda, (long long)d->n_adapters * d->rank, d->inputs, ws + p.a, st));
-  if (p.pack_b) STEP(pack(B, ldb, (long long)d->n_adapters * d->outputs, d->rank, ws + p.b, st));
-  if (p.pack_dy) STEP(pack(dy, lddy, d->rows, d->outputs, ws + p.dy, st));
+  Packer pk;
+  pk.add(p.pack_x, x, ldx, d->rows, d->inputs, ws + p.x);
+  pk.add(p.pack_w, w, ldw, d->outputs, d->inputs, ws + p.w);
+  pk.add(p.pack_a, A, lda, (long long)d->n_adapters * d->rank, d->inputs, ws + p.a);
+  pk.add(p.pack_b, B, ldb, (long long)d->n_adapters * d->outputs, d->rank, ws + p.b);
+  pk.add(p.pack_dy, dy, lddy, d->rows, d->outputs, ws + p.dy);
+  STEP(pk.run(st));
   const int width = 3 * p.rp;
   ShrinkArgs a;
   memset(&a, 0, sizeof(a));
