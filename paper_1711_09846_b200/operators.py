@@ -153,36 +153,37 @@ class BlockNormGrads(NamedTuple):
 
 def _norm_desc(x, block, post_weight, gate, scale, next_weight):
     """The description of the inputs that both directions share; x stands for y in the backward pass."""
-    if not (x.is_cuda and x.dim() == 3 and x.dtype in _TYPES):
+    shape, dtype, device = kind = x.shape, x.dtype, x.device
+    if not (x.is_cuda and len(shape) == 3 and dtype in _TYPES):
         raise ValueError("activations are CUDA tensors [members, rows, width], float32 or bfloat16")
-    shape = x.shape
     m, rows, width = shape
     d = PbtBlockNormDesc()
-    d.members, d.rows, d.width, d.dtype = m, rows, width, _TYPES[x.dtype]
-    d.x, d.x_member, d.x_row = _activation(x, x, shape, "x")
+    d.members, d.rows, d.width, d.dtype = m, rows, width, _TYPES[dtype]
+    d.x, d.x_member, d.x_row = _activation(x, kind, "x")
     if block is not None:
         if post_weight is None:
             raise ValueError("a block output needs post_weight")
-        d.block, d.block_member, d.block_row = _activation(block, x, shape, "block")
-        d.post_weight = _weight(post_weight, x, (m, width), "post_weight")
+        d.block, d.block_member, d.block_row = _activation(block, kind, "block")
+        d.post_weight = _weight(post_weight, (m, width), device, "post_weight")
         if gate is not None:
             if gate.dim() == 2:
-                _require(gate.shape == (m, width) and gate.dtype == x.dtype and gate.device == x.device
+                _require(gate.shape == (m, width) and gate.dtype == dtype and gate.device == device
                          and (gate.stride(1) == 1 or width == 1), "a gate vector is [members, width] of the activations' type")
                 d.gate, d.gate_member, d.gate_vector = gate.data_ptr(), gate.stride(0), 1
             else:
-                d.gate, d.gate_member, d.gate_row = _activation(gate, x, shape, "gate")
+                d.gate, d.gate_member, d.gate_row = _activation(gate, kind, "gate")
         if scale is not None:
-            d.scale = _weight(scale, x, (m,), "scale")
+            d.scale = _weight(scale, (m,), device, "scale")
     else:
         _require(post_weight is None and gate is None and scale is None, "post_weight, gate and scale belong to a block output")
     if next_weight is not None:
-        d.next_weight = _weight(next_weight, x, (m, width), "next_weight")
-    return d, shape
+        d.next_weight = _weight(next_weight, (m, width), device, "next_weight")
+    return d, kind
 
 
-def _activation(t, like, shape, name):
-    if t.shape != shape or t.dtype != like.dtype or t.device != like.device:
+def _activation(t, kind, name):
+    shape, dtype, device = kind
+    if t.shape != shape or t.dtype is not dtype or t.device != device:
         raise ValueError(f"{name} has to have the activations' shape, type and device")
     member, row, column = t.stride()
     if column != 1 and shape[2] != 1:
@@ -190,8 +191,8 @@ def _activation(t, like, shape, name):
     return t.data_ptr(), member, row
 
 
-def _weight(t, like, shape, name):
-    if t.shape != shape or t.dtype is not torch.float32 or t.device != like.device or not t.is_contiguous():
+def _weight(t, shape, device, name):
+    if t.shape != shape or t.dtype is not torch.float32 or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name} has to be a contiguous float32 tensor {list(shape)} on the activations' device")
     return t.data_ptr()
 
@@ -206,9 +207,9 @@ def block_norm_forward(x, block=None, *, post_weight=None, gate=None, scale=None
     only y.  With `keep`, also the reciprocal roots that the backward pass takes."""
     if block is None and next_weight is None:
         raise ValueError("nothing to compute: neither a block output nor a next norm")
-    d, shape = _norm_desc(x, block, post_weight, gate, scale, next_weight)
+    d, kind = _norm_desc(x, block, post_weight, gate, scale, next_weight)
     d.eps = eps
-    return _on(x.device, stream, (x, block, post_weight, gate, scale, next_weight), _norm_forward, d, shape, x, block is not None,
+    return _on(kind[2], stream, (x, block, post_weight, gate, scale, next_weight), _norm_forward, d, kind[0], x, block is not None,
                next_weight is not None, keep)
 
 
@@ -239,18 +240,18 @@ def block_norm_backward(dy, du, y, block=None, *, post_weight=None, gate=None, s
     the y and the reciprocal roots of a forward pass that kept them."""
     _require(du is not None or block is not None, "nothing to differentiate: neither du nor a block output")
     _require((du is None) == (next_weight is None), "du and next_weight belong together")
-    d, shape = _norm_desc(y, block, post_weight, gate, scale, next_weight)
+    d, kind = _norm_desc(y, block, post_weight, gate, scale, next_weight)
     if dy is not None:
-        d.dy, d.dy_member, d.dy_row = _activation(dy, y, shape, "dy")
+        d.dy, d.dy_member, d.dy_row = _activation(dy, kind, "dy")
     if du is not None:
-        d.du, d.du_member, d.du_row = _activation(du, y, shape, "du")
+        d.du, d.du_member, d.du_row = _activation(du, kind, "du")
         _require(rstd_next is not None, "rstd_next is what the forward pass kept")
-        d.rstd_next = _weight(rstd_next, y, shape[:2], "rstd_next")
+        d.rstd_next = _weight(rstd_next, kind[0][:2], kind[2], "rstd_next")
     if block is not None:
         _require(rstd_block is not None, "rstd_block is what the forward pass kept")
-        d.rstd_block = _weight(rstd_block, y, shape[:2], "rstd_block")
+        d.rstd_block = _weight(rstd_block, kind[0][:2], kind[2], "rstd_block")
     inputs = (dy, du, y, block, post_weight, gate, scale, next_weight, rstd_block, rstd_next)
-    return _on(y.device, stream, inputs, _norm_backward, d, y, gate, post_weight, scale, next_weight)
+    return _on(kind[2], stream, inputs, _norm_backward, d, y, gate, post_weight, scale, next_weight)
 
 
 def _norm_backward(s, d, y, gate, post_weight, scale, next_weight):
