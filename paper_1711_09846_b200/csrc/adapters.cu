@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(256) k_adapter_shrink_f32(const float* __restr
 // the tile, S and its adapter's matrix, whose products are added to the segment's rows alone (not multiplied by zero elsewhere: a
 // diverged adapter reaches its own rows only).  The CTA's threads are KG groups that share a chunk's k, so that small tiles keep
 // eight warps busy.  Chunks come by cp.async, 16 bytes at a time where the operand's rows allow it, else element by element.
-// Bound by the ALUs' issue: 2048 x 256 -> 512, rank 4 takes 22 us, 0.3 of the fp32 rate; 8192 x 512 -> 512 140 us, 0.4.
+// Bound by the ALUs' issue: 2048 x 256 -> 512, rank 4 takes 26 us, 0.28 of the fp32 rate; 8192 x 512 -> 512 about 140 us, 0.4.
 // A narrow tile with more segments than 2 + rank / 16 leaves the low-rank part to its last step, where every thread multiplies out its own
 // elements (60 single rows, 72 -> 200, rank 4: a whole call 11 us, with chunks 24; 871 rows in segments of 13, 104 -> 152, rank 64, which has
 // chunks: 18.5 us, element by element 25).

@@ -578,10 +578,11 @@ cudaError_t launch_gemm(const GemmCall& c, const Segments& segs, const int* tile
   p.bias = c.bias;
   p.counters = counters;
   const LowRank low = {segs, tile_seg, c.rp / 16};
-  // 128-wide tiles when the 256-wide ones would leave most of their last wave idle: a wave of half tiles costs a little more
-  // than half a wave of full ones (the model of the member-batched GEMM; 3001 rows x 784 -> 1024: 96 wide tiles, one wave)
+  // 128-wide tiles when the 256-wide ones would leave most of their last wave idle; a wave of narrow ones counts 1.35 times half a wave of
+  // wide ones (1024 x 1024 -> 1024, one wave of either: 12.4 us, wide 14.5; 6400 rows, three narrow or two wide: 31 and 27; 4096 rows, two or one:
+  // 22.7 and 20.5; 4096 x 2048 -> 2048: 56 and 39).
   const long long wide_tiles = (long long)p.tiles_m * ((c.N + 255) / 256), narrow_tiles = (long long)p.tiles_m * ((c.N + 127) / 128);
-  const bool wide = 1.15 * (double)((narrow_tiles + 147) / 148) >= 2.0 * (double)((wide_tiles + 147) / 148);
+  const bool wide = 1.35 * (double)((narrow_tiles + 147) / 148) >= 2.0 * (double)((wide_tiles + 147) / 148);
   CUtensorMap maps[4];
   bool ok = make_map(&maps[0], c.x, c.K, segs.rows, c.ldx, 1, 0, kBM) && make_map(&maps[2], c.planes, c.rp, segs.rows, c.ld_planes, 1, 0, kBM);
   if (!c.b_mn) {
@@ -603,7 +604,9 @@ cudaError_t launch_gemm(const GemmCall& c, const Segments& segs, const int* tile
 // ------------------------------------------------------------------------------------------------------------------
 // Few rows
 // ------------------------------------------------------------------------------------------------------------------
-constexpr int kRowsMost = 64;      // rows of a CTA
+// Rows of a CTA, and the rows up to which the kernel takes every call: 64 rows of one segment, 2048 -> 2048, rank 16 12.4 us, by the product 18.6;
+// 8 rows, 1024 -> 1024 8.3 and 12.4.
+constexpr int kRowsMost = 64;
 constexpr int kRowsOut = 16;      // output columns of a CTA
 
 struct RowsArgs {
@@ -1014,9 +1017,10 @@ Plan plan(const pbt_adapter_desc* d, bool backward) {
   p.pack_a = !aligned(d->A, d->inputs);
   p.pack_b = !aligned(d->B, d->rank);
   p.pack_dy = backward && (!aligned(d->dy, d->ld_dy) || d->outputs % 8);
-  // enough CTAs for two per SM, at most one split per chunk of rows
-  const int blocks = (d->inputs + 127) / 128 + (d->outputs + 127) / 128;
-  p.splits = std::max(1, std::min((2 * 148 + blocks * d->n_adapters - 1) / (blocks * d->n_adapters), (d->rows + kGradChunk - 1) / kGradChunk));
+  // Splits of the adapters' rows in the gradients: enough CTAs for two per SM, at most one for every chunk of an adapter's share of the rows
+  // (a training step of 4096 x 1024 -> 1024 with one adapter: 53 us, without splits 76; 2048 x 512 -> 512 with sixteen: 36 with three, 31 without).
+  const long long blocks = ((d->inputs + 127ll) / 128 + (d->outputs + 127ll) / 128) * d->n_adapters, chunk = (long long)d->n_adapters * kGradChunk;
+  p.splits = (int)std::max(1ll, std::min((2 * 148 + blocks - 1) / blocks, (d->rows + chunk - 1) / chunk));
   size_t at = 0;
   auto take = [&](bool want, size_t bytes) {
     const size_t here = at;

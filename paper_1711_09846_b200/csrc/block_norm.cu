@@ -601,7 +601,8 @@ __global__ void __launch_bounds__(256) k_norm_columns(const NormArgs a) {
 }
 template <typename T>
 cudaError_t launch_norm_columns(const NormArgs& a, cudaStream_t s) {
-  // one thread a column is enough work for the SMs' latency while a member has few row groups (80 members: 8 each)
+  // one thread a column is enough work for the SMs' latency while a member has few row groups (80 x 512 x 2048, 8 each: the backward pass 278 us,
+  // with eight warps a column 295; 1 x 4096 x 1024, 592: 55 and 33)
   if (a.groups / a.members <= 16) return launch_with(dim3((a.width + 255) / 256, a.members, a.sums), 256, 0, s)(k_norm_columns<T, 1>, a);
   return launch_with(dim3((a.width + 31) / 32, a.members, a.sums), 256, 0, s)(k_norm_columns<T, 8>, a);
 }
