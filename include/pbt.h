@@ -526,6 +526,7 @@ int pbt_clip_run(pbt_clip_t* p, float limit, const float* limits_device, float* 
  * Backward, given dy (gradient that reaches y through the residual stream; NULL: zero) and du (NULL: no next norm), with
  * x holding y and the two reciprocal roots that the forward pass wrote: dx, dblock, dgate (type and shape of gate: summed
  * over the rows for gate_vector), dpost_weight, dnext_weight (float [members][width]), dscale (float [members] or NULL).
+ * The calls only enqueue; sums over rows are added in a fixed order (reproducible bit for bit).
  */
 typedef struct pbt_block_norm_desc {
   int32_t members, rows, width;
@@ -563,6 +564,8 @@ int pbt_block_norm_backward(const pbt_block_norm_desc* desc, void* workspace, si
  * one without rows).  Sums are fp32; a bfloat16 pass rounds S (dS) to bfloat16 for the second product of y (dx), but not
  * for dB (dA).  rank <= 64.  Elements have to be aligned to their size only.
  * A row depends on its own segment's adapter alone: NaN or infinite weights of one adapter reach no row of another.
+ * The calls only enqueue; results are reproducible bit for bit.  Should a bounded wait of a bfloat16 kernel run out, the fifth
+ * 32-bit word of status_device becomes PBT_ERR_TIMEOUT and the results are void.
  */
 typedef struct pbt_adapter_desc {
   int32_t rows, inputs, outputs, rank, n_adapters, n_segments;
