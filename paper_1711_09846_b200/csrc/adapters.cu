@@ -25,6 +25,7 @@ __global__ void __launch_bounds__(256) k_adapter_shrink_f32(const float* __restr
                                                             int rank, const float* __restrict__ scale, Segments segs,
                                                             float* __restrict__ s) {
   pdl_prologue();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the product may begin with its own operands
   const int lane = threadIdx.x & 31, rank_groups = (rank + 7) / 8, w = blockIdx.x * 8 + (threadIdx.x >> 5);
   const int row0 = w / rank_groups * R, r0 = w % rank_groups * 8, rows = min(R, segs.rows - row0);
   if (rows <= 0) return;
@@ -129,7 +130,6 @@ __device__ __forceinline__ void copy_box(uint32_t to, const float* from, long lo
 
 template <typename P, bool TRANS>
 __global__ void __launch_bounds__(256, 2) k_adapter_product_f32(const ProductArgs a) {
-  pdl_prologue();
   extern __shared__ __align__(16) float product_smem[];
   __shared__ int seg_lo[P::BM], seg_hi[P::BM], seg_adapter[P::BM], n_segs;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -172,7 +172,14 @@ __global__ void __launch_bounds__(256, 2) k_adapter_product_f32(const ProductArg
   __syncthreads();
   const bool direct = P::BM <= 16 && n_segs > 2 + a.rank / 16;
   const int turns = chunks + (direct ? 0 : n_segs * low_chunks);
+  // S is there from here on; k_adapter_grad_f32 may begin, too: it needs dS and nothing of this kernel's
+  bool waited = false;
+  auto low_rank = [&]() {
+    if (!waited) asm volatile("griddepcontrol.wait;\n\tgriddepcontrol.launch_dependents;" ::: "memory");
+    waited = true;
+  };
   for (int t = first; t < P::STAGES - 1; ++t) {
+    low_rank();
     if (t < turns) load(t);
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
@@ -184,6 +191,7 @@ __global__ void __launch_bounds__(256, 2) k_adapter_product_f32(const ProductArg
   for (int t = 0; t < turns; ++t) {
     asm volatile("cp.async.wait_group %0;" ::"n"(P::STAGES - 2) : "memory");
     __syncthreads();
+    if (t + P::STAGES - 1 >= chunks) low_rank();
     if (t + P::STAGES - 1 < turns) load(t + P::STAGES - 1);
     asm volatile("cp.async.commit_group;" ::: "memory");
     const float *sa = product_smem + (t % P::STAGES) * P::kStage, *sb = sa + P::kA;
@@ -219,6 +227,7 @@ __global__ void __launch_bounds__(256, 2) k_adapter_product_f32(const ProductArg
     }
   }
 
+  low_rank();
   // the groups' sums, in their order
   __syncthreads();
 #pragma unroll
@@ -264,6 +273,9 @@ cudaError_t launch_product(const ProductArgs& a, cudaStream_t st) {
   const cudaError_t e = tc::device_setup(&setup, k_adapter_product_f32<P, TRANS>, P::kBytes, &sms);
   if (e != cudaSuccess) return e;
   const unsigned tiles = (unsigned)(((a.segs.rows + P::BM - 1) / P::BM) * (long long)((a.N + P::BN - 1) / P::BN));
+  // Narrow tiles begin while the shrink runs (64 single rows, 256 -> 256: 12.3 us, after it 14.5).  Wide ones would crowd on the SMs that it leaves
+  // free, and a CTA that shares its SM takes twice its time (1024 rows 256 -> 256: 31 us, after it 22.6).
+  if (P::BM <= 16) return launch_after(tiles, 256, P::kBytes, st, k_adapter_product_f32<P, TRANS>, a);
   return launch_with(tiles, 256, P::kBytes, st)(k_adapter_product_f32<P, TRANS>, a);
 }
 template <bool TRANS>
@@ -293,7 +305,6 @@ struct GradSide {
 // four times, 139).
 template <int RANK>
 __global__ void __launch_bounds__(256, RANK == 32 ? 3 : 4) k_adapter_grad_f32(const GradSide x, const GradSide dy, int rank, Segments segs) {
-  pdl_prologue();
   constexpr bool kByRank = RANK >= 64;
   constexpr int R = kByRank ? RANK / 4 : RANK, kRowParts = kByRank ? 1 : 4;
   __shared__ float sum[kByRank ? 1 : 3][kByRank ? 1 : RANK][64];
@@ -347,6 +358,7 @@ __global__ void __launch_bounds__(256, RANK == 32 ? 3 : 4) k_adapter_grad_f32(co
 #pragma unroll
   for (int i = 0; i < R; ++i)
     if (i < ranks) out[side.columns_first ? (long long)n * rank + r0 + i : (long long)(r0 + i) * side.N + n] = f * acc[i];
+  asm volatile("griddepcontrol.wait;" ::: "memory");     // what follows in the stream follows the product, too (every block has a thread here)
 }
 
 // f(integral_constant) with the smallest of 4, 8, 16, 32, 64 that holds the rank
@@ -418,7 +430,7 @@ cudaError_t backward_f32(const pbt_adapter_desc* d, const Segments& segs, float*
   const GradSide a = {x, d->ld_x, ds, nullptr, splits > 1 ? parts : d->dA, size_a, d->inputs, (d->inputs + 63) / 64, false};
   const GradSide b = {dy, d->ld_dy, d->s, d->scale, splits > 1 ? parts + splits * size_a : d->dB, size_b, d->outputs, (d->outputs + 63) / 64, true};
   e = with_rank(d->rank, [&](auto r) {
-    return launch_with(dim3(a.blocks + b.blocks, d->n_adapters, splits), 256, 0, st)(k_adapter_grad_f32<decltype(r)::value>, a, b, d->rank, segs);
+    return launch_after(dim3(a.blocks + b.blocks, d->n_adapters, splits), 256, 0, st, k_adapter_grad_f32<decltype(r)::value>, a, b, d->rank, segs);
   });
   return e == cudaSuccess && splits > 1 ? join_gradients(a.g, b.g, size_a, size_b, splits, d->dA, d->dB, st) : e;
 }
