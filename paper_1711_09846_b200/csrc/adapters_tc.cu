@@ -81,11 +81,6 @@ struct ShrinkArgs {
   int* tile_seg; int tile_rows, n_table;  // first segment of every output tile of the product that follows
 };
 
-__device__ __forceinline__ uint4 ld16(const bf16* p) {
-  uint4 r;
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
-  return r;
-}
 __device__ __forceinline__ void copy16(void* slot, const void* from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(slot)), "l"(from) : "memory");
 }
