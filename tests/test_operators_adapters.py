@@ -322,3 +322,26 @@ def test_adapter_arguments_are_checked_before_the_device_is_touched():
     assert lib.pbt_adapter_backward(C.byref(desc()), None, 0, None) == 3
     assert lib.pbt_adapter_forward(None, None, 0, None) == 1
     assert lib.pbt_adapter_forward(C.byref(desc(rows=0)), None, 0, None) == 0
+
+
+# Every way through the kernels: several CTAs of rows in the few-rows kernel, wide and narrow fp32 tiles with many segments,
+# rows split between CTAs in the gradients, ranks dealt to parts, all operands packed at once.
+WAYS = {
+    "single tokens, several row groups": ([1] * 150, [(5 * k) % 11 - 1 for k in range(150)], 264, 392, 16, 10),
+    "single tokens, largest rank": ([1] * 40, [(3 * k) % 7 for k in range(40)], 136, 296, 64, 7),
+    "short segments in wide tiles": ([5] * 140, [(3 * k) % 9 - 1 for k in range(140)], 96, 520, 12, 8),
+    "one long adapter": ([2100, 3], [1, 0], 128, 72, 8, 2),
+    "one long adapter, largest rank": ([1500, 70], [0, 1], 72, 136, 64, 2),
+    "odd rank of many parts": ([90, 200], [1, 0], 80, 64, 61, 2),
+    "everything unaligned": ([60, 1, 139], [2, 0, 1], 131, 77, 13, 3),
+    "rank one, many segments": ([2] * 33, [k % 4 for k in range(33)], 33, 65, 1, 4),
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("name", sorted(WAYS))
+def test_every_way_through_the_kernels_matches_the_formulas(name, dtype):
+    lengths, ids, inputs, outputs, rank, adapters = WAYS[name]
+    for lead in (0, 3):
+        _verify(_case(dtype, lengths, ids, inputs, outputs, rank, adapters, seed=len(name), lead=lead))
