@@ -105,11 +105,27 @@ template <> struct Vec<bf16, 1> {
   template <typename L> static __device__ __forceinline__ void store(bf16* p, const L* f) { *p = __float2bfloat16_rn((float)f[0]); }
 };
 
+template <> struct Vec<float, 2> {
+  typedef float2 Raw;
+  static __device__ __forceinline__ Raw load(const float* p) { return *reinterpret_cast<const float2*>(p); }
+  static __device__ __forceinline__ void unpack(const Raw& r, float* f) { f[0] = r.x; f[1] = r.y; }
+  static __device__ __forceinline__ void store(float* p, const float* f) { *reinterpret_cast<float2*>(p) = make_float2(f[0], f[1]); }
+};
+template <> struct Vec<bf16, 2> {
+  typedef uint32_t Raw;
+  static __device__ __forceinline__ Raw load(const bf16* p) { return *reinterpret_cast<const uint32_t*>(p); }
+  static __device__ __forceinline__ void unpack(const Raw& r, float* f) { f[0] = __uint_as_float(r << 16); f[1] = __uint_as_float(r & 0xFFFF0000u); }
+  static __device__ __forceinline__ void store(bf16* p, const float* f) { *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(f[0], f[1]); }
+};
+
 // V weights (fp32; 16-byte loads where V allows, the launcher has checked the alignment)
 template <int V, typename L>
 __device__ __forceinline__ void load_weights(const float* p, L* f) {
   if constexpr (V == 1) {
     f[0] = __ldg(p);
+  } else if constexpr (V == 2) {
+    const float2 w = __ldg(reinterpret_cast<const float2*>(p));
+    f[0] = w.x; f[1] = w.y;
   } else {
 #pragma unroll
     for (int j = 0; j < V; j += 4) {
@@ -173,10 +189,10 @@ __device__ __forceinline__ void row_sum3(A* v, int W, int group, A* scratch, int
 
 // Rows on their way from global memory to shared memory.
 //
-// Aligned rows (V > 1): a thread copies its own 16-byte vectors into its own slots, several rows ahead of the one it works
+// Aligned rows (V > 2): a thread copies its own 16-byte vectors into its own slots, several rows ahead of the one it works
 // on, and reads nobody else's, so that the ring needs no barrier.
-// Other rows (V == 1; odd widths, odd strides): the row group copies the 16-byte granules that the row touches, one row at
-// a time, and reads single elements at the row's offset in them, so these need a barrier on either side of a row; the
+// Other rows (V <= 2: pairs or single elements): the row group copies the 16-byte granules that the row touches, one row at
+// a time, and reads them at the row's offset in them, so these need a barrier on either side of a row; the
 // other row groups of the SM have theirs in flight meanwhile.  (A granule that holds a byte of the row lies in the same page
 // as that byte.)
 __device__ __forceinline__ void copy_ahead(void* slot, const void* from) {
@@ -192,17 +208,17 @@ __host__ __device__ __forceinline__ int norm_pitch(int width) { return (width * 
 template <typename T, int V, int ITEMS, int ARRAYS, int STAGES, int THREADS>
 struct RowRing {
   typedef typename Vec<T, V>::Raw Raw;
-  uint4* slots;                  // this thread's (V > 1; its vectors are THREADS apart) or this row group's (V == 1)
-  const T* p[ARRAYS];            // the next row to ask for, at this thread's first vector (V == 1: at its first element)
+  uint4* slots;                  // this thread's (V > 2; its vectors are THREADS apart) or this row group's (V <= 2)
+  const T* p[ARRAYS];            // the next row to ask for, at this thread's first vector (V <= 2: at its first element)
   long long row[ARRAYS], wrap[ARRAYS];   // to the next row, and from behind a member's last row to the next member's first
-  int shift[ARRAYS];             // V == 1: bytes between the first granule and the row that is staged
+  int shift[ARRAYS];             // V <= 2: bytes between the first granule and the row that is staged
   bool have[ARRAYS];
   int slot, step, nv, rows, group;
-  int pitch;                     // V == 1: bytes of an array's row in shared memory
+  int pitch;                     // V <= 2: bytes of an array's row in shared memory
   int i, left;                   // the next row within its member, and how many there are to ask for
 
   __device__ __forceinline__ void set(int k, const NormTensor& t, bool used, int m) {
-    p[k] = reinterpret_cast<const T*>(t.p) + m * t.member + i * t.row + (V > 1 ? slot * V : 0);
+    p[k] = reinterpret_cast<const T*>(t.p) + m * t.member + i * t.row + (V > 2 ? slot * V : 0);
     row[k] = t.row;
     wrap[k] = t.member - rows * t.row;
     have[k] = used;
@@ -215,7 +231,7 @@ struct RowRing {
   }
   // ask for the next row (for nothing behind the last one) into stage s
   __device__ __forceinline__ void ask(int s) {
-    if constexpr (V == 1) barrier();     // everybody has read the row before
+    if constexpr (V <= 2) barrier();     // everybody has read the row before
     if (left > 0) {
       const bool last = ++i == rows;
       if (last) i = 0;
@@ -223,13 +239,13 @@ struct RowRing {
 #pragma unroll
       for (int k = 0; k < ARRAYS; ++k)
         if (have[k]) {
-          if constexpr (V > 1) {
+          if constexpr (V > 2) {
 #pragma unroll
             for (int j = 0; j < ITEMS; ++j)
               if (slot + j * step < nv) copy_ahead(at(s, k, j), p[k] + j * (step * V));
           } else {
             shift[k] = (int)((uintptr_t)p[k] & 15);
-            const int n = (shift[k] + nv * (int)sizeof(T) + 15) / 16;
+            const int n = (shift[k] + nv * V * (int)sizeof(T) + 15) / 16;
             const char* from = reinterpret_cast<const char*>(p[k]) - shift[k];
             for (int e = slot; e < n; e += step) copy_ahead(staged(k) + e * 16, from + e * 16);
           }
@@ -242,13 +258,13 @@ struct RowRing {
   // the oldest row asked for has arrived
   __device__ __forceinline__ void wait() const {
     copy_wait<STAGES - 1>();
-    if constexpr (V == 1) barrier();
+    if constexpr (V <= 2) barrier();
   }
   // vector j of array k (which there is) of the oldest row, in stage s; the vector lies inside the row
   template <typename L>
   __device__ __forceinline__ void get(int s, int k, int j, L* f) const {
-    if constexpr (V > 1) Vec<T, V>::unpack(*reinterpret_cast<const Raw*>(at(s, k, j)), f);
-    else Vec<T, V>::unpack(Vec<T, V>::load(reinterpret_cast<const T*>(staged(k) + shift[k]) + slot + j * step), f);
+    if constexpr (V > 2) Vec<T, V>::unpack(*reinterpret_cast<const Raw*>(at(s, k, j)), f);
+    else Vec<T, V>::unpack(Vec<T, V>::load(reinterpret_cast<const T*>(staged(k) + shift[k]) + (slot + j * step) * V), f);
   }
 };
 
@@ -257,7 +273,7 @@ struct RowRing {
 template <int V, int ITEMS, int ARRAYS, int THREADS>
 __host__ __device__ constexpr int norm_stages() {
   const int fit = (THREADS > kNormThreads ? 160 : ARRAYS == 3 ? 50 : 100) * 1024 / (ARRAYS * ITEMS * 16 * THREADS);
-  return V == 1 || fit < 1 ? 1 : fit > 3 ? 3 : fit;
+  return V <= 2 || fit < 1 ? 1 : fit > 3 ? 3 : fit;
 }
 
 template <typename T, int V, int ITEMS, int THREADS>
@@ -277,7 +293,7 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 4 : 1) k_no
   RowRing<T, V, ITEMS, 3, kStages, THREADS> ring;
   ring.slot = (warp % W) * 32 + lane; ring.step = W * 32; ring.nv = a.width / V; ring.rows = a.rows; ring.group = group;
   ring.pitch = norm_pitch<T>(a.width);
-  ring.slots = V > 1 ? norm_ring + threadIdx.x : norm_ring + group * (3 * ring.pitch / 16);
+  ring.slots = V > 2 ? norm_ring + threadIdx.x : norm_ring + group * (3 * ring.pitch / 16);
   ring.i = i; ring.left = (int)(r_end - r);
   ring.set(0, a.x, true, m); ring.set(1, a.block, block, m); ring.set(2, a.gate, gate, m);
 #pragma unroll
@@ -392,7 +408,7 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_no
   RowRing<T, V, ITEMS, 5, kStages, THREADS> ring;
   ring.slot = (warp % W) * 32 + lane; ring.step = W * 32; ring.nv = a.width / V; ring.rows = a.rows; ring.group = group;
   ring.pitch = norm_pitch<T>(a.width);
-  ring.slots = V > 1 ? norm_ring + threadIdx.x : norm_ring + group * (5 * ring.pitch / 16);
+  ring.slots = V > 2 ? norm_ring + threadIdx.x : norm_ring + group * (5 * ring.pitch / 16);
   ring.i = i; ring.left = (int)(r_end - r);
   ring.set(kDy, a.dy, has_dy, m); ring.set(kDu, a.du, next, m); ring.set(kY, a.x, next, m);
   ring.set(kBlock, a.block, block, m); ring.set(kGate, a.gate, gate, m);
@@ -612,29 +628,34 @@ int norm_fail(int code, const char* msg) {
   return code;
 }
 
-// Elements per vector: 16-byte vectors if the width and every pointer and stride allow them, single elements otherwise.
+// Elements per vector: 16-byte vectors if the width and every pointer and stride allow them, else pairs (but for the narrow rows that are
+// worked out in fp64), else single elements.  19 x 231 x 2050 bf16: pairs 35 us forward and 84 backward, single elements 51 and 128 (2048 columns in
+// 16-byte vectors: 21 and 47).
 int norm_vector(const pbt_block_norm_desc* d, bool backward) {
-  const int v = d->dtype ? 8 : 4;
-  if (d->width % v) return 1;
   const int esz = d->dtype ? 2 : 4;
-  bool ok = true;
-  auto in = [&](const void* p, int64_t member, int64_t row) {
-    if (p) ok = ok && ((uintptr_t)p & 15) == 0 && (member * esz) % 16 == 0 && (row * esz) % 16 == 0;
+  auto fits = [&](int v) {
+    const int bytes = v * esz;      // of a vector; weights are read with at most 16 bytes at a time
+    bool ok = d->width % v == 0;
+    auto in = [&](const void* p, int64_t member, int64_t row) {
+      if (p) ok = ok && (uintptr_t)p % bytes == 0 && (member * esz) % bytes == 0 && (row * esz) % bytes == 0;
+    };
+    auto flat = [&](const void* p) { if (p) ok = ok && (uintptr_t)p % bytes == 0; };
+    auto weights = [&](const void* p) { if (p) ok = ok && (uintptr_t)p % std::min(16, v * 4) == 0; };
+    in(d->x, d->x_member, d->x_row);
+    in(d->block, d->block_member, d->block_row);
+    in(d->gate, d->gate_member, d->gate_row);
+    weights(d->post_weight);
+    weights(d->next_weight);
+    if (backward) {
+      in(d->dy, d->dy_member, d->dy_row);
+      in(d->du, d->du_member, d->du_row);
+      flat(d->dx); flat(d->dblock); flat(d->dgate);
+    } else {
+      flat(d->y); flat(d->u);
+    }
+    return ok;
   };
-  auto flat = [&](const void* p) { if (p) ok = ok && ((uintptr_t)p & 15) == 0; };
-  in(d->x, d->x_member, d->x_row);
-  in(d->block, d->block_member, d->block_row);
-  in(d->gate, d->gate_member, d->gate_row);
-  flat(d->post_weight);
-  flat(d->next_weight);
-  if (backward) {
-    in(d->dy, d->dy_member, d->dy_row);
-    in(d->du, d->du_member, d->du_row);
-    flat(d->dx); flat(d->dblock); flat(d->dgate);
-  } else {
-    flat(d->y); flat(d->u);
-  }
-  return ok ? v : 1;
+  return fits(16 / esz) ? 16 / esz : d->width > 32 && fits(2) ? 2 : 1;
 }
 
 int norm_check(const pbt_block_norm_desc* d) {
@@ -717,8 +738,8 @@ NormPlan norm_backward_plan(const pbt_block_norm_desc* d) {
 template <typename T, int V, int ITEMS, int THREADS>
 cudaError_t launch_norm_backward(unsigned grid, int threads, const NormArgs& a, cudaStream_t s) {
   // unaligned rows: at most 16 elements and two granules' edges a thread
-  constexpr int most = V == 1 ? 5 * (THREADS * ITEMS * (int)sizeof(T) + THREADS / 32 * 32) : norm_stages<V, ITEMS, 5, THREADS>() * 5 * ITEMS * 16 * THREADS;
-  const int smem = V == 1 ? 5 * norm_pitch<T>(a.width) * (threads / (a.warps_per_row * 32)) : most;
+  constexpr int most = V <= 2 ? 5 * (THREADS * ITEMS * V * (int)sizeof(T) + THREADS / 32 * 32) : norm_stages<V, ITEMS, 5, THREADS>() * 5 * ITEMS * 16 * THREADS;
+  const int smem = V <= 2 ? 5 * norm_pitch<T>(a.width) * (threads / (a.warps_per_row * 32)) : most;
   static tc::DeviceSetup setup;
   int sms = 0;
   const cudaError_t e = tc::device_setup(&setup, k_norm_backward<T, V, ITEMS, THREADS>, most, &sms);
@@ -728,8 +749,8 @@ cudaError_t launch_norm_backward(unsigned grid, int threads, const NormArgs& a, 
 template <typename T, int V, int ITEMS, int THREADS>
 cudaError_t launch_norm_forward(unsigned grid, int threads, const NormArgs& a, cudaStream_t s) {
   // unaligned rows: at most 16 elements and two granules' edges a thread
-  constexpr int most = V == 1 ? 3 * (THREADS * ITEMS * (int)sizeof(T) + THREADS / 32 * 32) : norm_stages<V, ITEMS, 3, THREADS>() * 3 * ITEMS * 16 * THREADS;
-  const int smem = V == 1 ? 3 * norm_pitch<T>(a.width) * (threads / (a.warps_per_row * 32)) : most;
+  constexpr int most = V <= 2 ? 3 * (THREADS * ITEMS * V * (int)sizeof(T) + THREADS / 32 * 32) : norm_stages<V, ITEMS, 3, THREADS>() * 3 * ITEMS * 16 * THREADS;
+  const int smem = V <= 2 ? 3 * norm_pitch<T>(a.width) * (threads / (a.warps_per_row * 32)) : most;
   static tc::DeviceSetup setup;
   int sms = 0;
   const cudaError_t e = tc::device_setup(&setup, k_norm_forward<T, V, ITEMS, THREADS>, most, &sms);
@@ -755,15 +776,16 @@ cudaError_t launch_norm(bool backward, const NormShape& p, unsigned grid, const 
   if (p.items == 2) return launch_norm<T, V, 2>(backward, p, grid, a, s);
   if constexpr (V <= 4)
     if (p.items == 4) return launch_norm<T, V, 4>(backward, p, grid, a, s);
-  if constexpr (V == 1) {
+  if constexpr (V <= 2)
     if (p.items == 8) return launch_norm<T, V, 8>(backward, p, grid, a, s);
+  if constexpr (V == 1) {
     if (p.items == 16) return launch_norm<T, V, 16>(backward, p, grid, a, s);
   }
   return cudaErrorInvalidValue;
 }
 cudaError_t launch_norm(bool bf, int v, bool backward, const NormShape& p, unsigned grid, const NormArgs& a, cudaStream_t s) {
-  if (bf) return v == 1 ? launch_norm<bf16, 1>(backward, p, grid, a, s) : launch_norm<bf16, 8>(backward, p, grid, a, s);
-  return v == 1 ? launch_norm<float, 1>(backward, p, grid, a, s) : launch_norm<float, 4>(backward, p, grid, a, s);
+  if (bf) return v == 1 ? launch_norm<bf16, 1>(backward, p, grid, a, s) : v == 2 ? launch_norm<bf16, 2>(backward, p, grid, a, s) : launch_norm<bf16, 8>(backward, p, grid, a, s);
+  return v == 1 ? launch_norm<float, 1>(backward, p, grid, a, s) : v == 2 ? launch_norm<float, 2>(backward, p, grid, a, s) : launch_norm<float, 4>(backward, p, grid, a, s);
 }
 
 }  // namespace
