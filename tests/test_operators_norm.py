@@ -329,3 +329,12 @@ def test_norm_arguments_are_checked_before_the_device_is_touched():
     assert lib.pbt_block_norm_backward(C.byref(desc(**ok)), None, 0, None) == 3
     for kw in (dict(du=None), dict(dnext_weight=None), dict(dx=None), dict(rstd_next=None)):
         assert lib.pbt_block_norm_backward(C.byref(desc(**{**ok, **kw})), None, 0, None) == 1, kw
+
+
+# Even widths whose rows are no multiples of 16 bytes, around the limits of the widths that a warp, a block and a thread take.
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("gate", ["none", "vector", "full"])
+@pytest.mark.parametrize("shape", [(2, 5, 30), (2, 5, 34), (3, 40, 66), (2, 7, 514), (4, 50, 1002), (2, 30, 2050), (1, 9, 4098), (1, 3, 8190)], ids=str)
+def test_rows_of_even_width_match_the_formulas(shape, gate, dtype):
+    test_forward_and_backward_match_the_formulas(shape, gate, dtype)
