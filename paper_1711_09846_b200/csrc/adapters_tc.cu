@@ -13,9 +13,10 @@
 // the instruction (the disable-output-lane mask: a TMEM lane is a row).  Rows are therefore independent of one another's
 // adapters exactly, not up to a multiplication with zero: an adapter that has diverged to NaN reaches only its own rows.
 //
-// Precision.  The low-rank operand of a bf16 result is S (dS) rounded once to bf16, like every GEMM operand of a bf16
-// population; the result is rounded to bf16 anyway.  dA and dB are fp32 results, so their operand is S (dS) as the sum of
-// three bf16 numbers (24 bits), whose three products land in separate accumulator columns and are added in fp32.  The tensor
+// Precision.  S and dS are fp32, the tensor cores take bf16.  The low-rank operand of a bf16 result is S (dS) as the sum of two bf16
+// numbers, which leaves out less than 2^-16 of it, 2^-7 of what the result's own rounding does; one number (2^-9) raised the error of
+// y on 3001 ragged rows, rank 8, from 0.00166 to 0.00181.  dA and dB are fp32 results, so their operand is the sum of
+// three (24 bits), whose three products land in separate accumulator columns and are added in fp32.  The tensor
 // cores' accumulation truncates (about 2^-24 of the accumulator per instruction), so chains are kept short: the shrink
 // folds its accumulators into fp32 registers every 64 columns, the gradients every 128 rows.
 #include <algorithm>
@@ -93,15 +94,21 @@ __device__ __forceinline__ void ldmatrix4_trans(uint32_t* r, uint32_t addr) {
 }
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
-// two neighbouring columns (col is even), as one summand or three
+// The next bf16 summand of v, which becomes the rest.  Nothing is left of an infinite v (inf - inf would make its row NaN); a finite
+// one beyond the largest bf16 is cut instead of rounded, so that it stays finite.
+__device__ __forceinline__ float next_term(float& v) {
+  float h = __bfloat162float(__float2bfloat16_rn(v));
+  if (isinf(h)) h = __uint_as_float(__float_as_uint(v) & 0xFFFF0000u);
+  v = isinf(h) ? 0.f : v - h;
+  return h;
+}
+// two neighbouring columns (col is even), as two summands or three
 __device__ __forceinline__ void store_terms(bf16* row, int rp, int col, float v0, float v1, bool three) {
 #pragma unroll
   for (int t = 0; t < 3; ++t) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(v0, v1);
-    *reinterpret_cast<__nv_bfloat162*>(row + t * rp + col) = h;
-    if (!three) return;
-    v0 -= __low2float(h);
-    v1 -= __high2float(h);
+    if (t == 2 && !three) return;
+    const float h0 = next_term(v0), h1 = next_term(v1);
+    *reinterpret_cast<__nv_bfloat162*>(row + t * rp + col) = __floats2bfloat162_rn(h0, h1);
   }
 }
 
@@ -328,10 +335,14 @@ cudaError_t launch_shrink(ShrinkArgs a, cudaStream_t s) {
 // with eight warps and three stages 715; 10240 x 1024 -> 1024: 115 and 126), eight where its only tile's epilogue is not hidden behind
 // the next one (3001 x 784 -> 1024, one wave: 19.1 us, with four warps 22.5).
 
+// A segment's low-rank block is its two summands of S against the same matrix.  Up to rank 32 both lie in one stage of 64 columns,
+// beyond it each has a stage, which brings the matrix again.
 struct LowRank {
   Segments segs;
   const int* tile_seg;
-  int steps;        // MMA steps of 16 ranks
+  int rp;           // columns of a summand
+  int stages;       // of a segment
+  int steps;        // MMA steps of 16 ranks for a summand
 };
 
 // The segments that reach into rows [m0, m0 + tile_rows): walked in the same order by the roles of a CTA.
@@ -384,8 +395,8 @@ struct GemmSmem {
 };
 
 // Roles as in the member-batched GEMM: warp 0 TMA producer, warp 1 MMA issuer, EPI epilogue warps, double-buffered
-// accumulator.  After a tile's k-blocks both walk its segments: one more stage each, 128 rows of the low-rank operand and
-// the adapter's matrix (columns past the rank are out of the tensor map and arrive as zeros).  Launched while the shrink
+// accumulator.  After a tile's k-blocks both walk its segments: one more stage each (two beyond rank 32), 128 rows of the low-rank operand
+// and the adapter's matrix (columns past the rank are out of the tensor map and arrive as zeros).  Launched while the shrink
 // runs; the two threads that read what it leaves (the tiles' first segments, the planes through TMA) wait for its end
 // after the k-blocks of their first tile.  From then on k_adapter_grad may begin beside it: it needs the shrink's results and none of
 // this kernel's (training steps of 112 rows 87 -> 203: 45 us one after the other, 35 so; 1500 rows 1001 -> 603: 69 and 58).
@@ -442,20 +453,21 @@ k_adapter_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         if (tile == blockIdx.x) asm volatile("griddepcontrol.wait;\n\tgriddepcontrol.launch_dependents;" ::: "memory");
         SegmentWalk walk(low.segs, __ldcg(low.tile_seg + tm), m0, kBM);
         int adapter, lo, hi;
-        while (ok && walk.next(adapter, lo, hi)) {
-          if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) { ok = false; break; }
-          uint8_t* sa = smem + stage * L::kStageBytes;
-          uint8_t* sb = sa + L::kABytes;
-          mbar_expect_tx(&full[stage], L::kStageBytes);
-          tma_load_3d(sa, &tmP, &full[stage], 0, m0, 0);
-          if constexpr (!B_MN) {
-            tma_load_3d(sb, &tmL, &full[stage], 0, n0, adapter);
-          } else {
+        while (ok && walk.next(adapter, lo, hi))
+          for (int part = 0; part < low.stages; ++part) {
+            if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) { ok = false; break; }
+            uint8_t* sa = smem + stage * L::kStageBytes;
+            uint8_t* sb = sa + L::kABytes;
+            mbar_expect_tx(&full[stage], L::kStageBytes);
+            tma_load_3d(sa, &tmP, &full[stage], part * low.rp, m0, 0);
+            if constexpr (!B_MN) {
+              tma_load_3d(sb, &tmL, &full[stage], 0, n0, adapter);
+            } else {
 #pragma unroll
-            for (int j = 0; j < BN / 64; ++j) tma_load_3d(sb + j * 8192, &tmL, &full[stage], n0 + j * 64, 0, adapter);
+              for (int j = 0; j < BN / 64; ++j) tma_load_3d(sb + j * 8192, &tmL, &full[stage], n0 + j * 64, 0, adapter);
+            }
+            if (++stage == STAGES) { stage = 0; phase ^= 1; }
           }
-          if (++stage == STAGES) { stage = 0; phase ^= 1; }
-        }
       }
       if (!ok) {
         *abort_flag = 1;
@@ -495,16 +507,20 @@ k_adapter_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         SegmentWalk walk(low.segs, __ldcg(low.tile_seg + tm), m0, kBM);
         int adapter, lo, hi;
         while (ok && walk.next(adapter, lo, hi)) {
-          if (!mbar_wait(&full[stage], phase, abort_flag)) { ok = false; break; }
-          tc_fence_after();
-          const uint32_t sa = smem_u32(smem + stage * L::kStageBytes), sb = sa + L::kABytes;
           uint32_t off[4];
 #pragma unroll
           for (int w = 0; w < 4; ++w) off[w] = rows_off(m0 + 32 * w, lo, hi);
-          for (int k = 0; k < low.steps; ++k)
-            umma_bf16_rows(tmem_d, smem_desc(sa + k * 32, 16, 1024), B_MN ? smem_desc(sb + k * 2048, 8192, 1024) : smem_desc(sb + k * 32, 16, 1024), idesc, off);
-          umma_commit(&empty[stage]);
-          if (++stage == STAGES) { stage = 0; phase ^= 1; }
+          for (int part = 0; part < low.stages; ++part) {
+            if (!mbar_wait(&full[stage], phase, abort_flag)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t sa = smem_u32(smem + stage * L::kStageBytes), sb = sa + L::kABytes;
+            for (int term = part; term < 2; term += low.stages)
+              for (int k = 0; k < low.steps; ++k)
+                umma_bf16_rows(tmem_d, smem_desc(sa + (term - part) * low.rp * 2 + k * 32, 16, 1024),
+                               B_MN ? smem_desc(sb + k * 2048, 8192, 1024) : smem_desc(sb + k * 32, 16, 1024), idesc, off);
+            umma_commit(&empty[stage]);
+            if (++stage == STAGES) { stage = 0; phase ^= 1; }
+          }
         }
         if (ok) umma_commit(&tfull[acc]);
       }
@@ -573,14 +589,14 @@ cudaError_t launch_gemm(const GemmCall& c, const Segments& segs, const int* tile
   p.C = c.c; p.ldc = c.ldc; p.out_dtype = kBF16;
   p.bias = c.bias;
   p.counters = counters;
-  const LowRank low = {segs, tile_seg, c.rp / 16};
+  const LowRank low = {segs, tile_seg, c.rp, 2 * c.rp <= kBK ? 1 : 2, c.rp / 16};
   // 128-wide tiles when the 256-wide ones would leave most of their last wave idle; a wave of narrow ones counts 1.35 times half a wave of
   // wide ones (1024 x 1024 -> 1024, one wave of either: 12.4 us, wide 14.5; 6400 rows, three narrow or two wide: 31 and 27; 4096 rows, two or one:
   // 22.7 and 20.5; 4096 x 2048 -> 2048: 56 and 39).
   const long long wide_tiles = (long long)p.tiles_m * ((c.N + 255) / 256), narrow_tiles = (long long)p.tiles_m * ((c.N + 127) / 128);
   const bool wide = 1.35 * (double)((narrow_tiles + 147) / 148) >= 2.0 * (double)((wide_tiles + 147) / 148);
   CUtensorMap maps[4];
-  bool ok = make_map(&maps[0], c.x, c.K, segs.rows, c.ldx, 1, 0, kBM) && make_map(&maps[2], c.planes, c.rp, segs.rows, c.ld_planes, 1, 0, kBM);
+  bool ok = make_map(&maps[0], c.x, c.K, segs.rows, c.ldx, 1, 0, kBM) && make_map(&maps[2], c.planes, 2 * c.rp, segs.rows, c.ld_planes, 1, 0, kBM);
   if (!c.b_mn) {
     ok = ok && make_map(&maps[1], c.b, c.K, c.N, c.ldb, 1, 0, wide ? 256 : 128);
     ok = ok && make_map(&maps[3], c.mats, c.mat_pitch, c.N, c.mat_pitch, segs.n_adapters, (long long)c.N * c.mat_pitch, wide ? 256 : 128);
@@ -1028,7 +1044,7 @@ Plan plan(const pbt_adapter_desc* d, bool backward) {
   p.a = take(p.pack_a, (size_t)d->n_adapters * d->rank * round_up(d->inputs, 8) * 2);
   p.b = take(p.pack_b, (size_t)d->n_adapters * d->outputs * round_up(d->rank, 8) * 2);
   p.dy = take(p.pack_dy, rows * round_up(d->outputs, 8) * 2);
-  p.planes = take(true, p.few ? rows * d->rank * sizeof(float) : rows * p.rp * 2 * (backward ? 3 : 1));
+  p.planes = take(true, p.few ? rows * d->rank * sizeof(float) : rows * p.rp * 2 * (backward ? 3 : 2));
   p.kept = take(backward, rows * p.rp * 2 * 3);
   p.table = take(true, (p.few ? rows : (rows + kBM - 1) / kBM) * sizeof(int));
   p.parts = take(backward && p.splits > 1, (size_t)p.splits * d->n_adapters * d->rank * ((size_t)d->inputs + d->outputs) * sizeof(float));
@@ -1087,10 +1103,10 @@ cudaError_t tc_forward(const pbt_adapter_desc* d, const Segments& segs, char* ws
                         d->rows, d->outputs, d->inputs, d->rank};
     return launch_rows(r, st);
   }
-  a.planes = (bf16*)(ws + p.planes); a.terms = 1;
+  a.planes = (bf16*)(ws + p.planes); a.terms = 2;
   a.tile_seg = (int*)(ws + p.table); a.tile_rows = kBM; a.n_table = (d->rows + kBM - 1) / kBM;
   STEP(launch_shrink<false>(a, st));
-  const GemmCall c = {(const bf16*)x, ldx, (const bf16*)w, ldw, 0, a.planes, p.rp, p.rp, (const bf16*)B, (int)ldb, d->rank, d->y, d->ld_y, d->bias, d->outputs, d->inputs};
+  const GemmCall c = {(const bf16*)x, ldx, (const bf16*)w, ldw, 0, a.planes, 2 * p.rp, p.rp, (const bf16*)B, (int)ldb, d->rank, d->y, d->ld_y, d->bias, d->outputs, d->inputs};
   return launch_gemm(c, segs, a.tile_seg, (Counters*)d->status_device, st);
 }
 

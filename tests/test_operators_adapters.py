@@ -345,3 +345,51 @@ def test_every_way_through_the_kernels_matches_the_formulas(name, dtype):
     lengths, ids, inputs, outputs, rank, adapters = WAYS[name]
     for lead in (0, 3):
         _verify(_case(dtype, lengths, ids, inputs, outputs, rank, adapters, seed=len(name), lead=lead))
+
+
+# The product kernel's low-rank operand: with W = 0 the result is the low-rank part alone, and its error is that of its own rounding to
+# bf16.  An operand that is held to 2^-16 adds less than 2^-7 of that error, independently: 2^-15 of its root mean square; the fp32 sums add
+# less.  One per cent covers both.  An operand of 8 bits, whose error is as large as the result's, adds about 40 %.
+@pytest.mark.gpu
+@pytest.mark.parametrize("rank", [4, 16, 29, 32, 33, 48, 64])
+def test_the_low_rank_part_of_a_bf16_product_has_the_error_of_its_rounding(rank):
+    import torch
+    c = _case("bfloat16", [300, 30, 70], [1, 0, 1], 512, 512, rank, 2, seed=rank)      # (too many rows for the few-rows kernel)
+    c["weight"].zero_()
+    c["bias"].zero_()
+    _, out = _run(c)
+    ref = _reference(c)
+    for name in ("y", "dx"):
+        value = ref[name][0]
+        got, rounded = ((t.cpu().double() - value).square().mean().sqrt().item() for t in (out[name], value.to(torch.bfloat16)))
+        assert got <= 1.01 * rounded, (name, got / rounded)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [40, 400])
+def test_a_low_rank_operand_at_the_end_of_the_range(rows):
+    """S beyond the largest bf16 but not the largest float, and infinite S: the products are those of the formula."""
+    import torch
+    import paper_1711_09846_b200 as pbt
+    k = n = 512
+    x = torch.zeros(rows, k, device="cuda", dtype=torch.bfloat16)
+    x[:, :2] = 1.0
+    a = torch.zeros(1, 8, k, device="cuda", dtype=torch.bfloat16)
+    a[0, 0, 0], a[0, 0, 1] = 3.3895313892515355e38, 1e36
+    b = torch.zeros(1, n, 8, device="cuda", dtype=torch.bfloat16)
+    b[0, :, 0] = 2.0 ** -126
+    w = torch.zeros(n, k, device="cuda", dtype=torch.bfloat16)
+    where = [torch.tensor(v, dtype=torch.int32, device="cuda") for v in ([0, rows], [0])]
+    layer = pbt.AdapterProjection(w, a, b, torch.ones(1, device="cuda"))
+    y, kept = layer.forward(x, *where, keep=True)
+    assert torch.isfinite(kept).all()
+    want = (a[0, 0, 0].double() + a[0, 0, 1].double()) * 2.0 ** -126
+    assert (y.double() / want - 1).abs().max() <= 2.0 ** -8
+    dy = torch.zeros(rows, n, device="cuda", dtype=torch.bfloat16)
+    dy[0, 0] = 2.0 ** -10
+    _, _, d_b = layer.backward(dy, x, kept, *where)
+    assert torch.isfinite(d_b).all() and abs(d_b[0, 0, 0].double() / (kept[0, 0].double() * 2.0 ** -10) - 1) <= 2.0 ** -20
+    a[0, 0, 1] = 3.3895313892515355e38
+    y, kept = layer.forward(x, *where, keep=True)
+    assert torch.isinf(kept[:, 0]).all() and torch.isinf(y).all()
+    layer.check()
