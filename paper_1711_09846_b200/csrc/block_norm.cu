@@ -57,13 +57,46 @@ __device__ __forceinline__ int norm_group_of(const NormArgs& a, long long r) {
   return (int)(((r + 1) * a.groups - 1) / ((long long)a.members * a.rows));
 }
 
-// sigmoid(z) = 1 / (1 + 2^(-z log2 e)) by the special-function unit: relative error below (|z| + 3) 2^-22
+// sigmoid(z) = 1 / (1 + 2^(-z log2 e)) by the special-function unit: relative error below (|z| + 3) 2^-22 for z >= -87; below that
+// the result, less than 2^-125, may be 0
 __device__ __forceinline__ float opened(float z) {
   float e, r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.44269504f));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
   return r;
 }
+// sigmoid(z) and 1 - sigmoid(z) for the backward pass, both with the error above for |z| <= 87, beyond which the smaller may be 0.  (1 minus a
+// rounded sigmoid is off by 6 % at z = 16 and 0 from 17 on: a gate that is open would have no gradient.)
+// BOTH: two numbers, e / (1 + e) being the second one; e is held to 2^127, whose reciprocal is 0, so that a closed gate is exactly closed.
+// Else one, the smaller of the two with the sign of z: 1 minus it is the other one without cancellation.  Two registers an element pay where
+// the weights of the next norm make room for them: 19 x 231 x 2048 bf16 45 us, with one 49; 19 x 231 x 2048 fp32, which keeps those weights,
+// 61 us, with one 58.
+template <bool BOTH> struct GateParts {
+  float o, c;
+  __device__ __forceinline__ void of(float z) {
+    float t, e;
+    asm("min.NaN.f32 %0, %1, 0f42FE0000;" : "=f"(t) : "f"(z * -1.44269504f));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(o) : "f"(1.f + e));
+    c = e * o;
+  }
+  __device__ __forceinline__ void none() { o = 1.f; c = 0.f; }
+  template <typename A> __device__ __forceinline__ A open() const { return o; }
+  template <typename A> __device__ __forceinline__ A closed() const { return c; }
+};
+template <> struct GateParts<false> {
+  float smaller;
+  __device__ __forceinline__ void of(float z) {
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(z) * -1.44269504f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+    smaller = copysignf(e * r, z);
+  }
+  __device__ __forceinline__ void none() { smaller = 0.f; }
+  __device__ __forceinline__ bool negative() const { return __float_as_int(smaller) < 0; }      // (-0 is)
+  template <typename A> __device__ __forceinline__ A open() const { return negative() ? -(A)smaller : 1 - (A)smaller; }
+  template <typename A> __device__ __forceinline__ A closed() const { return negative() ? 1 + (A)smaller : (A)smaller; }
+};
 
 // V elements of type T as they lie in memory, and as values of type L (float; double for V == 1).
 template <typename T, int V> struct Vec;
@@ -396,6 +429,7 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_no
   constexpr int kStages = norm_stages<V, ITEMS, 5, THREADS>();
   constexpr bool kKeep = V * ITEMS <= 8;
   constexpr int kKept = kKeep ? ITEMS : 1;
+  constexpr bool kBoth = kKeep && V == 8, kKeepNext = kKeep && !kBoth;
   const int W = a.warps_per_row, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int group = warp / W, g = blockIdx.x * (blockDim.x / (W * 32)) + group;
   if (g >= a.groups) return;
@@ -426,7 +460,7 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_no
   T* dgate = reinterpret_cast<T*>(a.dgate) + r * a.width + first;
   const float* rstd_next = a.rstd_next + r;
   const float* rstd_block = a.rstd_block + r;
-  // the weights of the member at hand; the variant that keeps its values keeps these, too
+  // the weights of the member at hand; the variants that keep their values keep these, too (but for the next norm's, see GateParts)
   A w_next[kKept][V], w_post[kKept][V];
   A c = 1;
   auto member = [&]() {
@@ -435,7 +469,8 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_no
 #pragma unroll
       for (int k = 0; k < ITEMS; ++k) {
         if (ring.slot + k * ring.step >= ring.nv) continue;
-        if (next) load_weights<V>(a.next_weight + (long long)m * a.width + first + k * far, w_next[k]);
+        if constexpr (kKeepNext)
+          if (next) load_weights<V>(a.next_weight + (long long)m * a.width + first + k * far, w_next[k]);
         if (block) load_weights<V>(a.post_weight + (long long)m * a.width + first + k * far, w_post[k]);
       }
     }
@@ -444,9 +479,10 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_no
   int turn = 0, stage = 0;
   for (; r < r_end; ++r) {
     const A ry = next ? *rstd_next : 0.f, rb = block ? *rstd_block : 0.f;
-        ring.wait();
+    ring.wait();
     A sums[3] = {0, 0, 0};                                     // r_y dh yh, p (dy + r_y dh), p yh, with p = g w_post v
-    A t[kKept][V], yh[kKept][V], open[kKept][V], v[kKept][V];   // dy + r_y dh, yh, sigmoid(z), v
+    A t[kKept][V], yh[kKept][V], v[kKept][V];   // dy + r_y dh, yh, v
+    GateParts<kBoth> parts[kKept][V];
     // the vectors k of the row; `once`: with the sums that do not wait for the reduction
     auto values = [&](int k, int to, bool once) {
 #pragma unroll
@@ -456,7 +492,7 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_no
         A du[V];
         ring.get(stage, kDu, k, du);
         ring.get(stage, kY, k, yh[to]);
-        if constexpr (!kKeep) load_weights<V>(a.next_weight + (long long)m * a.width + first + k * far, w_next[to]);
+        if constexpr (!kKeepNext) load_weights<V>(a.next_weight + (long long)m * a.width + first + k * far, w_next[to]);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           yh[to][j] *= ry;
@@ -473,16 +509,16 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_no
           A z[V];
           ring.get(stage, kGate, k, z);
 #pragma unroll
-          for (int j = 0; j < V; ++j) open[to][j] = opened((float)z[j]);
+          for (int j = 0; j < V; ++j) parts[to][j].of((float)z[j]);
         } else {
 #pragma unroll
-          for (int j = 0; j < V; ++j) open[to][j] = 1;
+          for (int j = 0; j < V; ++j) parts[to][j].none();
         }
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           v[to][j] *= rb;
           if (once) {
-            const A p = v[to][j] * w_post[to][j] * open[to][j];
+            const A p = v[to][j] * w_post[to][j] * parts[to][j].template open<A>();
             sums[1] += p * t[to][j];
             sums[2] += p * yh[to][j];
           }
@@ -512,11 +548,11 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_no
         A db[V], dz[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          const A gdx = open[from][j] * t[from][j], gwdx = gdx * w_post[from][j], o = gwdx * v[from][j];
-          acc_post[k][j] += (float)(c * gdx * v[from][j]);
+          const A gdx = parts[from][j].template open<A>() * t[from][j], gwdx = gdx * w_post[from][j], o = gwdx * v[from][j];
+          acc_post[k][j] += (float)(gdx * v[from][j]);
           acc_scale += (float)o;
           db[j] = crb * gwdx - v[from][j] * t2;
-          dz[j] = c * o * (1 - open[from][j]);
+          dz[j] = c * o * parts[from][j].template closed<A>();
         }
         X::store(dblock + k * far, db);
         if (vector) {
@@ -552,7 +588,11 @@ __global__ void __launch_bounds__(THREADS, THREADS <= kNormThreads ? 2 : 1) k_no
         o += a.width;
       };
       if (next) leave(acc_next[k]);
-      if (block) leave(acc_post[k]);
+      if (block) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc_post[k][j] *= (float)c;      // the member's scale, once for all its rows
+        leave(acc_post[k]);
+      }
       if (vector) leave(acc_gate[k]);
     }
     if (block) {

@@ -338,3 +338,32 @@ def test_norm_arguments_are_checked_before_the_device_is_touched():
 @pytest.mark.parametrize("shape", [(2, 5, 30), (2, 5, 34), (3, 40, 66), (2, 7, 514), (4, 50, 1002), (2, 30, 2050), (1, 9, 4098), (1, 3, 8190)], ids=str)
 def test_rows_of_even_width_match_the_formulas(shape, gate, dtype):
     test_forward_and_backward_match_the_formulas(shape, gate, dtype)
+
+
+# The gradient of gates that are nearly open or nearly closed, element by element.  Without a next norm dx is dy, so dz = c dy v w g (1 - g)
+# is a product of seven factors: 16 eps, and twice the sigmoid's (|z| + 3) 2^-22, relative to the element itself (which is no
+# difference of larger numbers); bf16 adds its rounding, a gate vector the sum over its rows.
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("gate", ["vector", "full"])
+@pytest.mark.parametrize("shape", [(2, 3, 7), (2, 3, 8), (1, 4, 64), (2, 3, 34), (1, 2, 33), (1, 3, 2048), (1, 2, 4104), (1, 2, 4099)], ids=str)
+def test_the_gradient_of_a_saturated_gate_is_exact_to_rounding(shape, gate, dtype):
+    import torch
+    import paper_1711_09846_b200 as pbt
+    m, rows, width = shape
+    d, dy, _ = _inputs(m, rows, width, dtype, gate, seed=sum(shape), nxt=False)
+    at = torch.tensor([8.0, -8.0, 12.0, -12.0, 16.0, -16.0, 20.0, -20.0, 60.0, -60.0, 0.0], device="cuda")
+    d["gate"].copy_(at[torch.arange(d["gate"].numel(), device="cuda").view(d["gate"].shape) % 11])
+    kw = {k: d[k] for k in ("post_weight", "gate", "scale")}
+    out = pbt.block_norm_forward(d["x"], d["block"], keep=True, **kw)
+    got = pbt.block_norm_backward(dy, None, out.y, d["block"], rstd_block=out.rstd_block, **kw).dgate.cpu().double()
+    f = _double(d)
+    z = f["gate"] if gate == "full" else f["gate"][:, None]
+    dz = f["scale"].view(-1, 1, 1) * dy.cpu().double() * f["block"] * out.rstd_block.cpu().double()[..., None] * f["post_weight"][:, None] \
+        * torch.sigmoid(z) * torch.sigmoid(-z)
+    tol = (16 * EPS32 + 2 * (z.abs() + 3) * 2.0 ** -22) * dz.abs()
+    if gate == "vector":
+        dz, tol = dz.sum(1), (tol + (rows + 16) * EPS32 * dz.abs()).sum(1)
+    if dtype == "bfloat16":
+        tol = tol + 2.0 ** -8 * dz.abs()
+    assert ((got - dz).abs() <= tol + 1e-37).all(), ((got - dz).abs() / (tol + 1e-37)).max()
