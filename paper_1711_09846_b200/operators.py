@@ -28,10 +28,17 @@ def _require(ok, message: str) -> None:
 
 
 # What torch.cuda.current_stream, current_device and caching_allocator_alloc / _delete rest on, without the Python objects
-# around them: those cost a small call more than all of its checks (a workspace as a tensor 1.5 to 2.4 us, like this 0.5).
-_current_stream = torch._C._cuda_getCurrentRawStream
-_current_device = torch._C._cuda_getDevice
-_allocate, _release = torch._C._cuda_cudaCachingAllocator_raw_alloc, torch._C._cuda_cudaCachingAllocator_raw_delete
+# around them: those cost a small call more than all of its checks (a workspace as a tensor 1.5 to 2.4 us, like this 0.5).  Bound at the first
+# call, which has CUDA tensors: a torch build without CUDA lacks them.
+_current_device = _allocate = _release = None
+
+
+def _current_stream(index):
+    global _current_stream, _current_device, _allocate, _release
+    _current_device = torch._C._cuda_getDevice
+    _allocate, _release = torch._C._cuda_cudaCachingAllocator_raw_alloc, torch._C._cuda_cudaCachingAllocator_raw_delete
+    _current_stream = torch._C._cuda_getCurrentRawStream
+    return _current_stream(index)
 
 
 def _on(device, stream, inputs, work, *args):
