@@ -2,6 +2,8 @@
 #pragma once
 #include <cuda.h>
 
+#include <atomic>
+
 #include "pbt_common.cuh"
 
 namespace pbt {
@@ -164,17 +166,16 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
+inline EncodeTiledFn look_up_encode_fn() {
+  void* p = nullptr;
+  cudaDriverEntryPointQueryResult qres;
+  if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) == cudaSuccess && qres == cudaDriverEntryPointSuccess)
+    return reinterpret_cast<EncodeTiledFn>(p);
+  return nullptr;
+}
+// looked up once; threads whose first calls meet wait for the one that does it
 inline EncodeTiledFn encode_fn() {
-  static EncodeTiledFn fn = nullptr;
-  static bool tried = false;
-  if (!tried) {
-    tried = true;
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult qres;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) == cudaSuccess &&
-        qres == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeTiledFn>(p);
-  }
+  static const EncodeTiledFn fn = look_up_encode_fn();
   return fn;
 }
 
@@ -199,11 +200,11 @@ inline bool make_map(CUtensorMap* map, const void* base, long long cols, long lo
 
 // Per-device launch set-up.  The opt-in shared-memory size is an attribute of the function ON ONE DEVICE, and the SM
 // count differs between devices, so both are resolved for the device that is current at the launch and remembered
-// per device ordinal (a process may drive several GPUs).  Returns the SM count through *sms.
+// per device ordinal (a process may drive several GPUs).  Returns the SM count through *sms.  Calls may come from several threads: two that are
+// first at the same time both do it, with the same outcome.
 struct DeviceSetup {
   static constexpr int kMaxDevices = 64;
-  bool configured[kMaxDevices];
-  int sms[kMaxDevices];
+  std::atomic<int> sms[kMaxDevices];      // 0: not set up yet
 };
 template <typename Kernel>
 inline cudaError_t device_setup(DeviceSetup* st, Kernel kernel, int smem_bytes, int* sms) {
@@ -211,18 +212,14 @@ inline cudaError_t device_setup(DeviceSetup* st, Kernel kernel, int smem_bytes, 
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   const bool cached = dev >= 0 && dev < DeviceSetup::kMaxDevices;
-  if (!cached || !st->configured[dev]) {
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes);
-    if (e != cudaSuccess) return e;
-    int n = 0;
-    e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
-    if (e != cudaSuccess) return e;
-    if (n <= 0) n = 148;
-    if (cached) { st->sms[dev] = n; st->configured[dev] = true; }
-    *sms = n;
-    return cudaSuccess;
-  }
-  *sms = st->sms[dev];
+  *sms = cached ? st->sms[dev].load(std::memory_order_acquire) : 0;
+  if (*sms > 0) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes);
+  if (e != cudaSuccess) return e;
+  e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return e;
+  if (*sms <= 0) *sms = 148;
+  if (cached) st->sms[dev].store(*sms, std::memory_order_release);
   return cudaSuccess;
 }
 
