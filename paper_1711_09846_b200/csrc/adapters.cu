@@ -246,18 +246,18 @@ __global__ void __launch_bounds__(256, 2) k_adapter_product_f32(const ProductArg
       for (int q = 0; q < n_segs; ++q) {
         if (row < seg_lo[q] || row >= seg_hi[q]) continue;
         const int adapter = seg_adapter[q];
-        const float* s = a.s + (long long)(row0 + row) * a.rank;
+        const float* s = a.s + (long long)(row0 + row) * a.rank;      // (written while this kernel runs already: no read-only loads)
         const float* m = a.mats + (long long)adapter * a.rank * a.N + (TRANS ? n0 + n : (long long)(n0 + n) * a.rank);
         float low = 0.f;
         if (!TRANS && a.vec_s && a.vec_m) {
 #pragma unroll 8
           for (int j = 0; j < a.rank; j += 4) {
-            const float4 u = __ldg(reinterpret_cast<const float4*>(s + j)), w = __ldg(reinterpret_cast<const float4*>(m + j));
+            const float4 u = __ldcg(reinterpret_cast<const float4*>(s + j)), w = __ldg(reinterpret_cast<const float4*>(m + j));
             low = __fmaf_rn(u.x, w.x, __fmaf_rn(u.y, w.y, __fmaf_rn(u.z, w.z, __fmaf_rn(u.w, w.w, low))));
           }
         } else {
 #pragma unroll 8
-          for (int j = 0; j < a.rank; ++j) low = __fmaf_rn(__ldg(s + j), __ldg(TRANS ? m + (long long)j * a.N : m + j), low);
+          for (int j = 0; j < a.rank; ++j) low = __fmaf_rn(__ldcg(s + j), __ldg(TRANS ? m + (long long)j * a.N : m + j), low);
         }
         v = __fmaf_rn(a.scale ? __ldg(a.scale + adapter) : 1.f, low, v);
         break;

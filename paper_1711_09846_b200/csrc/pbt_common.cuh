@@ -45,11 +45,12 @@ __host__ __device__ inline U4 philox4x32_10(uint32_t c0, uint32_t c1, uint32_t c
 }
 
 // ---------------------------------------------------------------------------
-// Launching.  Every kernel of the library is launched through launch_with and begins with pdl_prologue().  When
-// programmatic launches are switched on, the launch carries the programmatic-stream-serialization attribute: the
+// Launching.  Every kernel is launched through launch_with and begins with pdl_prologue(), but for the ones that begin beside their
+// predecessor in any case (launch_after below).  When
+// programmatic launches are switched on, a launch through launch_with carries the programmatic-stream-serialization attribute: the
 // grid may be scheduled while its predecessor in the stream drains, and its threads wait in griddepcontrol.wait
 // until the predecessor has completed and its writes are visible, so the data dependences are exactly those of
-// stream order.  No kernel triggers its successor early: a successor made resident ahead of time competes with the
+// stream order.  No kernel of a population's step triggers its successor early: a successor made resident ahead of time competes with the
 // running kernel for the SM, and measured slower (C2 0.246 vs 0.227 ms per step).  With the implicit trigger at
 // grid completion the gain over plain stream order inside a replayed CUDA graph is nil on this GPU (C2 0.226 vs
 // 0.227 ms, C4 1.770 vs 1.758 ms per step), so plain stream order is the default and the attribute is opt-in
@@ -85,7 +86,9 @@ inline LaunchCfg launch_with(dim3 grid, dim3 block, size_t smem, cudaStream_t st
 // Launches a kernel that may begin while its predecessor in the stream still runs, whatever pbt_spec.programmatic_launches
 // says.  The predecessor allows it (griddepcontrol.launch_dependents, which takes effect once all its blocks are running, so
 // that everything before it is complete), and the kernel waits for its end (griddepcontrol.wait) in the threads that read what it
-// leaves or write what it reads, before they do.
+// leaves or write what it reads, before they do.  What the predecessor writes is read past the read-only path (__ldcg, cp.async, TMA), since it
+// changes while the kernel runs.  Every grid waits in some thread before it ends, so that whatever follows in the stream, waiting or not, follows
+// the predecessor, too.
 template <typename... KArgs, typename... Args>
 cudaError_t launch_after(dim3 grid, unsigned threads, size_t smem, cudaStream_t s, void (*kernel)(KArgs...), Args&&... args) {
   cudaLaunchConfig_t cfg;

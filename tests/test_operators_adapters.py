@@ -393,3 +393,24 @@ def test_a_low_rank_operand_at_the_end_of_the_range(rows):
     y, kept = layer.forward(x, *where, keep=True)
     assert torch.isinf(kept[:, 0]).all() and torch.isinf(y).all()
     layer.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rank", [4, 16, 13])
+def test_calls_that_follow_one_another_read_their_own_low_rank_rows(rank, dtype):
+    """Calls without a pause share a workspace, and the product begins while the shrink writes it: bit for bit what a call alone gives."""
+    import torch
+    import paper_1711_09846_b200 as pbt
+    n = 60
+    c = _case(dtype, [1] * n, [(3 * k) % 11 - 1 for k in range(n)], 72, 200, rank, 10, seed=rank)
+    layer = pbt.AdapterProjection(c["weight"], c["A"], c["B"], c["scale"], bias=c["bias"])
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    xs = [torch.randn(c["x"].shape, generator=gen, device="cuda").to(c["x"].dtype) for _ in range(40)]
+    alone = []
+    for x in xs:
+        alone.append(layer.forward(x, c["row_offsets"], c["adapter_ids"]))
+        torch.cuda.synchronize()
+    together = [layer.forward(x, c["row_offsets"], c["adapter_ids"]) for x in xs]
+    layer.check()
+    assert all(torch.equal(a, b) for a, b in zip(alone, together))
