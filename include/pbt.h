@@ -562,7 +562,7 @@ int pbt_block_norm_backward(const pbt_block_norm_desc* desc, void* workspace, si
  * scale float [n_adapters].  s float [rows][rank]: written by the forward pass unless NULL (rows without an adapter are
  * left alone), read by the backward pass.  dA, dB are float in the shapes of A and B, written for every adapter (zero for
  * one without rows).  Sums are fp32; a bfloat16 pass cuts S (dS) to 16 bits for the second product of y (dx), but not
- * for dB (dA).  rank <= 64.  Elements have to be aligned to their size only.
+ * for dB (dA).  rank <= 64; rows, inputs and outputs < 2^31 - 4096, n_segments <= 2^30.  Elements have to be aligned to their size only.
  * A row depends on its own segment's adapter alone: NaN or infinite weights of one adapter reach no row of another.
  * The calls only enqueue; results are reproducible bit for bit.  Should a bounded wait of a bfloat16 kernel run out, the fifth
  * 32-bit word of status_device becomes PBT_ERR_TIMEOUT and the results are void.

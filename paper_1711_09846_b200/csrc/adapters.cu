@@ -380,6 +380,10 @@ int check(const pbt_adapter_desc* d) {
   if (!d) return fail(PBT_ERR_INVALID_ARG, "desc is NULL");
   if (d->rows < 0 || d->inputs < 1 || d->outputs < 1 || d->n_adapters < 1 || d->n_segments < 0)
     return fail(PBT_ERR_INVALID_ARG, "inputs, outputs and n_adapters must be positive, rows and n_segments >= 0");
+  // the kernels work out the ends of their tiles in 32 bits
+  constexpr int kMost = 0x7FFFFFFF - 4096;
+  if (d->rows > kMost || d->inputs > kMost || d->outputs > kMost || d->n_segments > (1 << 30))
+    return fail(PBT_ERR_UNSUPPORTED, "more than 2^31 - 4097 rows, inputs or outputs, or more than 2^30 segments");
   if (d->rank < 1 || d->rank > kMaxRank) return fail(PBT_ERR_UNSUPPORTED, "rank must be in [1, 64]");
   if (d->n_adapters > 65535) return fail(PBT_ERR_UNSUPPORTED, "more than 65535 adapters");
   if (d->dtype != 0 && d->dtype != 1) return fail(PBT_ERR_UNSUPPORTED, "operands are float or bfloat16");

@@ -15,6 +15,7 @@ import torch
 from .binding import PbtAdapterDesc, PbtBlockNormDesc, PbtClipTensor, PbtError, load_library
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1}
+_MOST = 0x7FFFFFFF      # what the library's 32-bit sizes hold; ctypes would cut a larger one without a word
 
 
 def _check(rc: int) -> None:
@@ -92,6 +93,7 @@ class GradientClip:
         _require(grads, "no gradient tensors")
         _require(len(groups) == len(grads) and len(out) == len(grads), "grads, groups and out differ in length")
         self.n_groups = max(groups) + 1 if n_groups is None else int(n_groups)
+        _require(max(groups) < _MOST and -_MOST <= min(groups) and abs(self.n_groups) <= _MOST, "groups are 32-bit numbers")
         self.device = grads[0].device
         table = (PbtClipTensor * len(grads))()
         for e, g, o, k in zip(table, grads, out, groups):
@@ -164,6 +166,8 @@ def _norm_desc(x, block, post_weight, gate, scale, next_weight):
     if not (x.is_cuda and len(shape) == 3 and dtype in _TYPES):
         raise ValueError("activations are CUDA tensors [members, rows, width], float32 or bfloat16")
     m, rows, width = shape
+    if m > _MOST or rows > _MOST or width > _MOST:
+        raise ValueError("activations have at most 2^31 - 1 members, rows and columns")
     d = PbtBlockNormDesc()
     d.members, d.rows, d.width, d.dtype = m, rows, width, _TYPES[dtype]
     d.x, d.x_member, d.x_row = _activation(x, kind, "x")
@@ -318,6 +322,7 @@ class AdapterProjection:
         _require(A.dim() == 3 and A.shape[2] == k and A.dtype == weight.dtype and A.device == weight.device and A.is_contiguous(),
                  "A is a contiguous [adapters, rank, inputs] of the weight's type and device")
         count, rank = A.shape[0], A.shape[1]
+        _require(max(n, k, count, rank) <= _MOST, "inputs, outputs, adapters and rank are at most 2^31 - 1")
         _require(B.shape == (count, n, rank) and B.dtype == weight.dtype and B.device == weight.device and B.is_contiguous(),
                  "B is a contiguous [adapters, outputs, rank] of the weight's type and device")
         for t, shape, name in ((scale, (count,), "scale"), (bias, (n,), "bias")):
@@ -345,6 +350,8 @@ class AdapterProjection:
         if not (row_offsets.dtype is torch.int32 and adapter_ids.dtype is torch.int32 and row_offsets.numel() == n + 1 and row_offsets.device == device
                 and adapter_ids.device == device and row_offsets.is_contiguous() and adapter_ids.is_contiguous()):
             raise ValueError("row_offsets [segments + 1] and adapter_ids [segments] are contiguous int32 tensors on the weight's device")
+        if x.shape[0] > _MOST or n > _MOST:
+            raise ValueError("a call has at most 2^31 - 1 rows and segments")
         d = PbtAdapterDesc.from_buffer_copy(self._desc)
         d.rows, d.n_segments = x.shape[0], n
         d.row_offsets, d.adapter_ids = row_offsets.data_ptr(), adapter_ids.data_ptr()
