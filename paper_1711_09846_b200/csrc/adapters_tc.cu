@@ -411,7 +411,8 @@ k_adapter_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   uint64_t* empty = full + STAGES;
   uint64_t* tfull = empty + STAGES;
   uint64_t* tempty = tfull + 2;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty + 2);
+  uint64_t* idle = tempty + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(idle + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   constexpr uint32_t kTmemCols = 2 * BN;
 
@@ -419,6 +420,7 @@ k_adapter_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
     for (int a = 0; a < 2; ++a) { mbar_init(&tfull[a], 1); mbar_init(&tempty[a], EPI); }
+    mbar_init(idle, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -474,7 +476,8 @@ k_adapter_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         atomicCAS(&p.counters->status, 0, PBT_ERR_TIMEOUT);
         p.counters->status_info = 31;
       }
-      // every stage this thread armed has landed and been read before the CTA exits
+      // every stage this thread armed has landed before the CTA exits, and been read unless a wait ran out
+      for (int s = 0; s < STAGES; ++s) mbar_wait_out(&full[s], s < (int)stage ? phase : phase ^ 1);
       for (int s = 0; s < STAGES && ok; ++s) {
         if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) break;
         if (++stage == STAGES) { stage = 0; phase ^= 1; }
@@ -529,6 +532,8 @@ k_adapter_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         atomicCAS(&p.counters->status, 0, PBT_ERR_TIMEOUT);
         p.counters->status_info = 32;
       }
+      umma_commit(idle);        // no instruction reads shared memory or writes the accumulators when they are given back
+      mbar_wait_out(idle, 0);
     }
   } else {
     const int q = warp & 3, e = warp - 2, half = e >> 2;
@@ -803,15 +808,17 @@ __global__ void __launch_bounds__(192, 2) k_adapter_grad(const __grid_constant__
   uint64_t* empty = full + kGradStages;
   uint64_t* tfull = empty + kGradStages;
   uint64_t* tempty = tfull + 2;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty + 2);
+  uint64_t* idle = tempty + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(idle + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  int2* list = reinterpret_cast<int2*>(tempty + 4);
+  int2* list = reinterpret_cast<int2*>(idle + 2);
   __shared__ int list_n;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kGradStages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 4); }
+    mbar_init(idle, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -960,12 +967,17 @@ __global__ void __launch_bounds__(192, 2) k_adapter_grad(const __grid_constant__
     atomicCAS(&a.counters->status, 0, PBT_ERR_TIMEOUT);
     a.counters->status_info = 40 + min(warp, 2);
   }
-  // the last commits into `empty` have landed before the CTA exits
-  if (warp == 0 && lane == 0 && ok)
-    for (int s = 0; s < kGradStages; ++s) {
+  // as in k_adapter_gemm: what was asked for has landed, the last commits into `empty` too unless a wait ran out, and the tensor cores are idle
+  if (warp == 0 && lane == 0) {
+    for (int s = 0; s < kGradStages; ++s) mbar_wait_out(&full[s], s < (int)stage ? phase : phase ^ 1);
+    for (int s = 0; s < kGradStages && ok; ++s) {
       if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) break;
       if (++stage == kGradStages) { stage = 0; phase ^= 1; }
     }
+  } else if (warp == 1 && lane == 0) {
+    umma_commit(idle);
+    mbar_wait_out(idle, 0);
+  }
   tc_fence_before();
   __syncthreads();
   if (warp == 1) tmem_dealloc(tmem_base, a.tmem_cols);
