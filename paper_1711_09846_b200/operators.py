@@ -335,6 +335,7 @@ class AdapterProjection:
         d.weight, d.ld_weight, d.A, d.B, d.scale = weight.data_ptr(), weight.stride(0), A.data_ptr(), B.data_ptr(), scale.data_ptr()
         d.bias = bias.data_ptr() if bias is not None else None
         self._status = torch.zeros(8, dtype=torch.int32, device=weight.device)
+        self._home = _current_stream(weight.device.index)
         torch.cuda.current_stream(weight.device).synchronize()      # the calls may be on any stream
         d.status_device = self._status.data_ptr()
         d.row_offsets = d.adapter_ids = weight.data_ptr()
@@ -402,6 +403,8 @@ class AdapterProjection:
             raise PbtError(code, "a bounded wait inside an adapter kernel ran out")
 
     def _run(self, d, backward, call, s):
+        if s != self._home:      # keeps the status words until the call is done, should the object go first
+            self._status.record_stream(torch.cuda.current_stream(self.weight.device))
         nbytes, at = C.c_size_t(0), C.byref(d)
         rc = self.lib.pbt_adapter_query_workspace(at, backward, C.byref(nbytes))
         if not rc:

@@ -414,3 +414,32 @@ def test_calls_that_follow_one_another_read_their_own_low_rank_rows(rank, dtype)
     together = [layer.forward(x, c["row_offsets"], c["adapter_ids"]) for x in xs]
     layer.check()
     assert all(torch.equal(a, b) for a, b in zip(alone, together))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("current", [False, True])
+def test_the_status_words_outlive_a_call_on_another_stream(current, backward):
+    """The kernels hold their address: with the layer gone, its words are nobody else's memory before the other stream is done."""
+    import torch
+    import paper_1711_09846_b200 as pbt
+    c = _case("bfloat16", [40, 60], [0, 1], 64, 64, 8, 2)
+    where = (c["row_offsets"], c["adapter_ids"])
+    layer = pbt.AdapterProjection(c["weight"], c["A"], c["B"], c["scale"])
+    _, kept = layer.forward(c["x"], *where, keep=True)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)       # a tenth of a second
+    with torch.cuda.stream(side if current else None):
+        stream = None if current else side
+        if backward:
+            layer.backward(c["dy"], c["x"], kept, *where, stream=stream)
+        else:
+            layer.forward(c["x"], *where, stream=stream)
+    at = layer._status.data_ptr()
+    del layer
+    others = [torch.zeros(8, dtype=torch.int32, device="cuda") for _ in range(200)]
+    assert not side.query()
+    assert at not in [t.data_ptr() for t in others]
+    torch.cuda.synchronize()
