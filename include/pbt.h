@@ -558,7 +558,7 @@ int pbt_block_norm_backward(const pbt_block_norm_desc* desc, void* workspace, si
  *   forward   S = x A_a^T (fp32),  y = x W^T + bias + scale_a S B_a^T
  *   backward  dS = scale_a dy B_a,  dx = dy W + dS A_a,  dA_a = sum dS^T x,  dB_a = scale_a sum dy^T S
  * W [outputs][inputs] with row stride ld_weight, A [n_adapters][rank][inputs] and B [n_adapters][outputs][rank]
- * contiguous, x / y / dy / dx with any row stride; all of one type (0 float, 1 bfloat16).  bias float [outputs] or NULL,
+ * contiguous, x / y / dy / dx with any row stride of at least a row; all of one type (0 float, 1 bfloat16).  bias float [outputs] or NULL,
  * scale float [n_adapters].  s float [rows][rank]: written by the forward pass unless NULL (rows without an adapter are
  * left alone), read by the backward pass.  dA, dB are float in the shapes of A and B, written for every adapter (zero for
  * one without rows).  Sums are fp32; a bfloat16 pass cuts S (dS) to 16 bits for the second product of y (dx), but not

@@ -316,7 +316,7 @@ class AdapterProjection:
     (outside [0, adapters): none); both int32 on the device.  One token per request is a batch of segments of length 1."""
 
     def __init__(self, weight, A, B, scale, bias=None):
-        _require(weight.is_cuda and weight.dim() == 2 and weight.dtype in _TYPES and weight.stride(1) == 1,
+        _require(weight.is_cuda and weight.dim() == 2 and weight.dtype in _TYPES and (weight.stride(1) == 1 or weight.shape[1] == 1),
                  "weight is a CUDA tensor [outputs, inputs], float32 or bfloat16, with contiguous columns")
         n, k = weight.shape
         _require(A.dim() == 3 and A.shape[2] == k and A.dtype == weight.dtype and A.device == weight.device and A.is_contiguous(),
@@ -332,7 +332,7 @@ class AdapterProjection:
         self.lib = load_library()
         d = self._desc = PbtAdapterDesc()
         d.inputs, d.outputs, d.rank, d.n_adapters, d.dtype = k, n, rank, count, _TYPES[weight.dtype]
-        d.weight, d.ld_weight, d.A, d.B, d.scale = weight.data_ptr(), weight.stride(0), A.data_ptr(), B.data_ptr(), scale.data_ptr()
+        d.weight, d.ld_weight, d.A, d.B, d.scale = weight.data_ptr(), _row_stride(weight, "weight"), A.data_ptr(), B.data_ptr(), scale.data_ptr()
         d.bias = bias.data_ptr() if bias is not None else None
         self._status = torch.zeros(8, dtype=torch.int32, device=weight.device)
         self._home = _current_stream(weight.device.index)

@@ -443,3 +443,17 @@ def test_the_status_words_outlive_a_call_on_another_stream(current, backward):
     assert not side.query()
     assert at not in [t.data_ptr() for t in others]
     torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("inputs, outputs", [(1, 40), (24, 1), (1, 1)])
+def test_a_weight_of_one_row_or_column_may_have_any_stride_across_it(inputs, outputs, dtype):
+    import torch
+    c = _case(dtype, [30, 50], [1, 0], inputs, outputs, 4, 2, seed=inputs)
+    w = c["weight"]
+    _, whole = _run(c)
+    for strides in (((1, 7), (3, 5)) if inputs == 1 else ((0, 1), (1, 1))):
+        c["weight"] = torch.empty(4096, device="cuda", dtype=w.dtype).as_strided((outputs, inputs), strides).copy_(w)
+        _, out = _run(c)
+        assert all(torch.equal(out[name], whole[name]) for name in whole)
