@@ -508,8 +508,8 @@ int pbt_clip_create(pbt_clip_t** out, const pbt_clip_tensor* tensors_host, int32
 int pbt_clip_destroy(pbt_clip_t* p);
 /*
  * One pass: norms_out_device [n_groups] floats (before clipping).  The limit is limits_device[g] (device floats, e.g. a
- * hyperparameter of every member), or `limit` for all groups if limits_device is NULL.  Only enqueues.  The handle's
- * workspace serves one run at a time: runs on several streams have to be ordered.
+ * hyperparameter of every member; norms_out_device may be the same array), or `limit` for all groups if limits_device is NULL.
+ * Only enqueues.  The handle's workspace serves one run at a time: runs on several streams have to be ordered.
  */
 int pbt_clip_run(pbt_clip_t* p, float limit, const float* limits_device, float* norms_out_device, void* stream);
 

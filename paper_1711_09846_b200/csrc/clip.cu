@@ -222,8 +222,9 @@ __device__ __forceinline__ void clip_norm(const ClipArgs& a, int chunk) {
   for (int q = begin + threadIdx.x; q < end; q += kClipThreads) s += __ldcg(a.sums + q);
   const float norm = (float)sqrt(clip_block_sum(s, scratch_wide));
   if (threadIdx.x == 0) {
+    const float limit = a.limits ? a.limits[group] : a.limit;      // (before the norm, which may take its place)
     a.norms[group] = norm;
-    a.factors[group] = clip_factor(a.limits ? a.limits[group] : a.limit, norm);
+    a.factors[group] = clip_factor(limit, norm);
     a.done[group] = 0;
   }
 }

@@ -204,3 +204,17 @@ def test_clip_arguments_are_checked_before_the_device_is_touched():
         setattr(t[0], field, keep)
     assert lib.pbt_clip_run(None, 1.0, None, None, None) == 1
     assert lib.pbt_clip_destroy(None) == 0
+
+
+@pytest.mark.gpu
+def test_clip_norms_may_take_the_place_of_the_limits():
+    import torch
+    import paper_1711_09846_b200 as pbt
+    grads = [torch.randn(n, device="cuda") for n in (70_001, 5, 40_000)]
+    out = [torch.empty_like(g) for g in grads]
+    limits = [2.5, 0.25, 1e6]
+    both = torch.tensor(limits, device="cuda")
+    clip = pbt.GradientClip(grads, [0, 1, 2], out=out)
+    assert clip.lib.pbt_clip_run(clip._handle, 0.0, both.data_ptr(), both.data_ptr(), torch.cuda.current_stream().cuda_stream) == 0
+    ref_norms, ref_out = _reference(grads, [0, 1, 2], 3, limits)
+    _check(both, out, ref_norms, ref_out)
