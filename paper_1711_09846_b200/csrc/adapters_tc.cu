@@ -1030,13 +1030,13 @@ Plan plan(const pbt_adapter_desc* d, bool backward) {
   const size_t rows = (size_t)d->rows;
   p.rp = round_up(d->rank, 16);
   p.pack_x = !aligned(d->x, d->ld_x) || d->inputs % 8;     // (vector loads end with the row)
-  // Few rows, or many short segments: the product has a low-rank block for every segment of a 128-row tile (12 us and 0.4 for each), k_adapter_rows
-  // a wave of CTAs for every 148 of its 64 rows x 16 columns (6 us and 8.5 for each, less below 1024 inputs).  1024 -> 1024, rank 16: 128 single rows 12.4 us, as a product
-  // 57; 64 segments of four rows 18.6 and 24.7; 2048 -> 2048, 80 segments of four rows 49 and 33;
-  // 512 -> 512, rank 8 the same 12.4 and 22.6.
+  // Few rows, or many short segments: the product has a low-rank block for every segment of a 128-row tile (12 us and 0.5 for each), k_adapter_rows
+  // a wave of CTAs for every 148 of its 64 rows x 16 columns (6 us and 8.5 for each, less below 1024 inputs).  1024 -> 1024, rank 16: 128 single rows 12 us,
+  // as a product 80; 64 segments of four rows 18 and 30; 2048 -> 2048, 80 segments of four rows 49 and 35;
+  // 512 -> 512, rank 8 the same 12 and 27.  (Beyond rank 32 both take about twice that.)
   const long long waves = ((long long)((d->rows + kRowsMost - 1) / kRowsMost) * ((d->outputs + kRowsOut - 1) / kRowsOut) + 147) / 148;
   const int tile_segments = std::min(kBM, d->n_segments / ((d->rows + kBM - 1) / kBM + (d->rows == 0)));
-  p.few = !backward && (d->rows <= kRowsMost || std::min(21, 1 + d->inputs / 48) * waves < 15 + tile_segments);
+  p.few = !backward && (d->rows <= kRowsMost || std::min(21, 1 + d->inputs / 48) * waves < 15 + tile_segments * 4 / 3);
   p.pack_w = !aligned(d->weight, d->ld_weight) || (p.few && d->inputs % 8);
   p.pack_a = !aligned(d->A, d->inputs);
   p.pack_b = !aligned(d->B, d->rank);
