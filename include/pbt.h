@@ -520,7 +520,9 @@ int pbt_clip_run(pbt_clip_t* p, float limit, const float* limits_device, float* 
  * b: the output of the block, x / y: the residual stream before / after it, u: the input of the next block.
  * block == NULL: only the norm before a block (u from x; y is x and is not written).  u == NULL: only the norm after it.
  * gate: one logit per element, or (gate_vector) one per member and column, or NULL (sigmoid replaced by 1); scale NULL: 1.
- * Inputs may have any member and row stride (in elements); columns are contiguous; results are contiguous.  Weights are
+ * Inputs may have any member and row stride (in elements); columns are contiguous; results are contiguous.  Rows that are no
+ * multiples of 16 bytes are fetched in the aligned 16-byte pieces that hold them: up to 15 bytes on either side of an input are read, never
+ * used, and never beyond the piece (so never beyond a page).  Weights are
  * float [members][width], scale float [members]; width <= 8192.  Sums are fp32; each result is rounded once.
  *
  * Backward, given dy (gradient that reaches y through the residual stream; NULL: zero) and du (NULL: no next norm), with

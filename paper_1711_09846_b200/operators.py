@@ -4,6 +4,9 @@ block norms, gradient clipping.
 Thin wrappers over the pbt_adapter_*, pbt_block_norm_* and pbt_clip_* calls of the C ABI: argument checks, result allocation and
 marshalling; every computation runs in the library's CUDA kernels.  Each call only enqueues work, on `stream` (a torch
 stream) or the current stream of the tensors' device; results are allocated for that stream.
+
+The calls build no autograd graph: their backward passes are calls of the caller's, and inputs that require a gradient are
+taken as plain numbers.  To put an operator into a graph, call the pair from a torch.autograd.Function.
 """
 from __future__ import annotations
 
@@ -83,7 +86,12 @@ class GradientClip:
 
     grads: CUDA tensors, contiguous, float32 or bfloat16, where the gradients live; groups: the group (population member)
     of each tensor (default: one group for all); out: tensors that receive the clipped gradients (default: in place).
-    Every run() reads the tensors' current contents."""
+    Every run() reads the tensors' current contents.
+
+    For gradients that stay where they are, like the slabs of a population: making the object sorts and checks the
+    tensors, uploads their table and waits for it (0.3 ms for 96 tensors, 2 ms for 640), which run() then saves.  A loop that
+    allocates its gradients anew (autograd's default after set_to_none) should keep them in place, or pays for that every
+    step.  An object serves one run at a time: runs on several streams have to be ordered."""
 
     def __init__(self, grads: Sequence[torch.Tensor], groups: Optional[Sequence[int]] = None,
                  out: Optional[Sequence[torch.Tensor]] = None, n_groups: Optional[int] = None):
