@@ -675,8 +675,8 @@ int norm_fail(int code, const char* msg) {
 }
 
 // Elements per vector: 16-byte vectors if the width and every pointer and stride allow them, else pairs (but for the narrow rows that are
-// worked out in fp64), else single elements.  19 x 231 x 2050 bf16: pairs 35 us forward and 84 backward, single elements 51 and 128 (2048 columns in
-// 16-byte vectors: 21 and 47).
+// worked out in fp64), else single elements.  19 x 231 x 2050 bf16: pairs 35 us forward and 89 backward, single elements 53 and 132 (2048 columns in
+// 16-byte vectors: 23 and 48).
 int norm_vector(const pbt_block_norm_desc* d, bool backward) {
   const int esz = d->dtype ? 2 : 4;
   auto fits = [&](int v) {
