@@ -591,6 +591,70 @@ int pbt_adapter_query_workspace(const pbt_adapter_desc* desc, int backward, size
 int pbt_adapter_forward(const pbt_adapter_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
 int pbt_adapter_backward(const pbt_adapter_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Which elements of which member a dropout drops.  Nothing is stored: 16 random bits an element come from Philox4x32-10 with
+ *   key = seed,  counter = (first_member + m, step, 5 + site, row * ceil(width / 8) + column / 8),
+ * whose four words are the bits of eight neighbouring columns (word c / 2, the lower half for even c).  An element is dropped where its
+ * bits are below t = round(65536 rate) (ties to even; the rate is cut to [0, 1], NaN counts as 0), and otherwise multiplied by
+ * 65536 / (65536 - t), the scale of the rate that is really drawn, so that the expectation is exact; t = 65536 drops everything.  A dropped
+ * element is zero whatever it was.  The draws depend on the member's index in the whole population, its own step and the element's place
+ * alone: the same in both directions, for any layout, and for a member on another GPU (first_member).
+ */
+typedef struct pbt_drop_rule {
+  const float* rate;      /* device [members], read when the kernels run (a hyperparameter of every member); NULL: rate_all */
+  const int64_t* steps;   /* device [members]: the members' own step counts (their lower 32 bits count); NULL: step */
+  uint64_t seed;
+  int64_t step;
+  float rate_all;
+  int32_t site;           /* which dropout of the network: 0 .. 2^30 */
+  int32_t first_member;   /* index of the call's first member in the whole population */
+} pbt_drop_rule;
+
+/*
+ * Dropout of activations [members][rows][width]: y = residual + keep x / (1 - rate); residual may be NULL.  The gradient of x is the
+ * same call on dy without a residual.  x and residual have any member and row stride (elements), columns are contiguous; y is
+ * contiguous and overlaps neither.  dtype 0 float, 1 bfloat16; each result is rounded once.  rows * ceil(width / 8) < 2^32,
+ * members <= 65535.  Only enqueues.
+ */
+typedef struct pbt_dropout_desc {
+  int32_t members, rows, width, dtype;
+  const void* x; int64_t x_member, x_row;
+  const void* residual; int64_t residual_member, residual_row;
+  void* y;
+  pbt_drop_rule rule;
+} pbt_dropout_desc;
+int pbt_dropout(const pbt_dropout_desc* desc, void* stream);
+
+/*
+ * Gated units of a population: member m has weight [2 hidden][width], the gate's rows first, then the up-projection's, and
+ *   g = x Wg^T,  u = x Wu^T,  h = keep / (1 - rate) act(g) u
+ *   dg = keep / (1 - rate) dh u act'(g),  du = keep / (1 - rate) dh act(g),  dx = [dg du] W,  dW = [dg du]^T x
+ * keep, rate: `drop` (its width is `hidden`), or NULL: nothing is dropped.  activation: 0 silu, 1 gelu (with the error function), 2 relu, 3 sigmoid.
+ * Activations [members][rows][...]; x, dh and weight have any member stride (0: one weight for all members; dweight is each
+ * member's own all the same) and any row stride of at least a row, in elements; columns are contiguous, results, too.  All of one type (0 float,
+ * 1 bfloat16), products are summed in fp32.  g and u stay fp32: `kept` float [members][rows][2][hidden rounded up to 8] is written by the forward
+ * pass unless NULL and read by the backward pass, which works them out anew where it is NULL.  For bfloat16, dg and du are rounded once, as operands of dx and dW.
+ * members <= 65535; rows, width and 2 hidden < 2^22.  rows = 0: dweight is zero.  The calls only enqueue; results are reproducible bit for bit.
+ * status_device: 32 zeroed bytes of device memory, as for pbt_grouped_gemm (bfloat16).
+ */
+typedef struct pbt_gated_desc {
+  int32_t members, rows, width, hidden;
+  int32_t dtype, activation;
+  const void* x; int64_t x_member, x_row;
+  const void* weight; int64_t weight_member, weight_row;
+  const pbt_drop_rule* drop;    /* host */
+  void* h;
+  float* kept;
+  const void* dh; int64_t dh_member, dh_row;
+  void* dx; void* dweight;
+  void* status_device;
+} pbt_gated_desc;
+/* Bytes of device workspace (256-byte aligned base) of one forward (backward == 0) or backward call of this description, its pointers
+ * (kept or not, alignment) and strides included. */
+int pbt_gated_query_workspace(const pbt_gated_desc* desc, int backward, size_t* bytes);
+int pbt_gated_forward(const pbt_gated_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
+int pbt_gated_backward(const pbt_gated_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
+
 const char* pbt_last_error(const pbt_t* p); /* p may be NULL: error of the last failed create/query */
 
 #ifdef __cplusplus

@@ -2,7 +2,8 @@
 from .binding import (EXPORTS, energy_fitness_static, grouped_gemm, selftest_bounded_wait, PbtError, Population, library_path, load_library, param_count,  # noqa: F401
                       spec_from_config)
 
-_OPERATORS = ("AdapterProjection", "BlockNormGrads", "BlockNormOut", "GradientClip", "block_norm_backward", "block_norm_forward")
+_OPERATORS = ("AdapterProjection", "BlockNormGrads", "BlockNormOut", "Dropout", "GatedUnit", "GradientClip", "block_norm_backward", "block_norm_forward",
+              "dropout_backward", "dropout_forward")
 
 
 def __getattr__(name):

@@ -104,6 +104,27 @@ class PbtAdapterDesc(C.Structure):
                 ("dA", C.c_void_p), ("dB", C.c_void_p), ("status_device", C.c_void_p)]
 
 
+class PbtDropRule(C.Structure):
+    _fields_ = [("rate", C.c_void_p), ("steps", C.c_void_p), ("seed", C.c_uint64), ("step", C.c_int64), ("rate_all", C.c_float),
+                ("site", C.c_int32), ("first_member", C.c_int32)]
+
+
+class PbtDropoutDesc(C.Structure):
+    _fields_ = [("members", C.c_int32), ("rows", C.c_int32), ("width", C.c_int32), ("dtype", C.c_int32),
+                ("x", C.c_void_p), ("x_member", C.c_int64), ("x_row", C.c_int64),
+                ("residual", C.c_void_p), ("residual_member", C.c_int64), ("residual_row", C.c_int64),
+                ("y", C.c_void_p), ("rule", PbtDropRule)]
+
+
+class PbtGatedDesc(C.Structure):
+    _fields_ = [("members", C.c_int32), ("rows", C.c_int32), ("width", C.c_int32), ("hidden", C.c_int32), ("dtype", C.c_int32), ("activation", C.c_int32),
+                ("x", C.c_void_p), ("x_member", C.c_int64), ("x_row", C.c_int64),
+                ("weight", C.c_void_p), ("weight_member", C.c_int64), ("weight_row", C.c_int64),
+                ("drop", C.POINTER(PbtDropRule)), ("h", C.c_void_p), ("kept", C.c_void_p),
+                ("dh", C.c_void_p), ("dh_member", C.c_int64), ("dh_row", C.c_int64),
+                ("dx", C.c_void_p), ("dweight", C.c_void_p), ("status_device", C.c_void_p)]
+
+
 EXPORTS = [
     "pbt_query_workspace", "pbt_param_count", "pbt_create", "pbt_destroy", "pbt_step", "pbt_step_subset", "pbt_eval",
     "pbt_exploit_explore", "pbt_exploit_explore_ready", "pbt_exploit_explore_global", "pbt_set_global_history",
@@ -116,6 +137,7 @@ EXPORTS = [
     "pbt_clip_query_workspace", "pbt_clip_create", "pbt_clip_destroy", "pbt_clip_run",
     "pbt_block_norm_forward", "pbt_block_norm_query_workspace", "pbt_block_norm_backward",
     "pbt_adapter_query_workspace", "pbt_adapter_forward", "pbt_adapter_backward",
+    "pbt_dropout", "pbt_gated_query_workspace", "pbt_gated_forward", "pbt_gated_backward",
 ]
 
 _LIB = None
@@ -181,6 +203,10 @@ def load_library() -> C.CDLL:
     lib.pbt_adapter_query_workspace.argtypes = [C.POINTER(PbtAdapterDesc), C.c_int, C.POINTER(C.c_size_t)]
     lib.pbt_adapter_forward.argtypes = [C.POINTER(PbtAdapterDesc), vp, C.c_size_t, vp]
     lib.pbt_adapter_backward.argtypes = [C.POINTER(PbtAdapterDesc), vp, C.c_size_t, vp]
+    lib.pbt_dropout.argtypes = [C.POINTER(PbtDropoutDesc), vp]
+    lib.pbt_gated_query_workspace.argtypes = [C.POINTER(PbtGatedDesc), C.c_int, C.POINTER(C.c_size_t)]
+    lib.pbt_gated_forward.argtypes = [C.POINTER(PbtGatedDesc), vp, C.c_size_t, vp]
+    lib.pbt_gated_backward.argtypes = [C.POINTER(PbtGatedDesc), vp, C.c_size_t, vp]
     lib.pbt_last_error.argtypes = [vp]
     lib.pbt_last_error.restype = C.c_char_p
     for name in EXPORTS:

@@ -1,0 +1,235 @@
+// Gated units of a population, h = keep / (1 - rate) act(x Wg^T) (x Wu^T) per member, and their gradients: entry points and the
+// kernels that work element by element.
+//
+// The products run in the framework's member-batched GEMMs; g and u stay in fp32 between the two (as bf16 they would add their
+// own rounding to that of h and of every gradient).
+#include "gated.cuh"
+
+namespace pbt {
+void set_last_error(const char* msg);
+
+namespace gated {
+namespace {
+
+using dropout::kGroup;
+
+int fail(int code, const char* msg) {
+  set_last_error(msg);
+  return code;
+}
+
+int round_up(int n, int m) { return (n + m - 1) / m * m; }
+
+__device__ __forceinline__ float as_float(float v) { return v; }
+__device__ __forceinline__ float as_float(bf16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ void store(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store(bf16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+// One thread has eight neighbouring hidden units of a row: one block of the generator.
+template <typename T>
+struct CellArgs {
+  const float* z; int pitch;                      // [members][rows][2][pitch]: g, then u
+  const T* dh; long long dh_member, dh_row;
+  T* out; long long out_pitch;                    // h [members][rows][hidden], or [dg du] [members][rows][out_pitch]
+  uint32_t rows, hidden, groups;
+  int activation, drop;
+  pbt_drop_rule rule;
+};
+
+template <typename T, bool BACKWARD>
+__global__ void __launch_bounds__(256) k_gated_cells(const CellArgs<T> a) {
+  pdl_prologue();
+  const int m = blockIdx.y;
+  const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (uint64_t)a.rows * a.groups) return;
+  const uint32_t row = (uint32_t)i / a.groups, c0 = ((uint32_t)i - row * a.groups) * kGroup, n = min(a.hidden - c0, (uint32_t)kGroup);
+  const long long at = (long long)m * a.rows + row;
+  const float* z = a.z + at * 2 * a.pitch + c0;
+  T* out = a.out + at * a.out_pitch + c0;
+  dropout::Draw d = {};
+  U4 w = {};
+  if (a.drop) d = dropout::draw_of(a.rule, m);
+  if (d.on) w = dropout::draw_group(d, (uint32_t)i);
+  const T* dh = BACKWARD ? a.dh + m * a.dh_member + row * a.dh_row + c0 : nullptr;
+#pragma unroll
+  for (int c = 0; c < kGroup; ++c) {
+    if (c >= n) break;
+    const float f = !d.on ? 1.f : d.scale;
+    const bool in = !d.on || dropout::kept(w, c, d.limit);
+    if (BACKWARD) {
+      float slope;
+      const float act = activation(a.activation, z[c], &slope), v = f * as_float(dh[c]);
+      store(out + c, in ? v * z[a.pitch + c] * slope : 0.f);
+      store(out + a.hidden + c, in ? v * act : 0.f);
+    } else {
+      store(out + c, in ? f * (activation(a.activation, z[c]) * z[a.pitch + c]) : 0.f);
+    }
+  }
+}
+
+// What a call does and where things lie in its workspace.
+struct Plan {
+  int pitch;              // of g and u
+  int dz_pitch;
+  size_t z, dz, bytes;    // offsets (z: only where the caller keeps none)
+};
+Plan plan_of(const pbt_gated_desc* d, bool backward) {
+  Plan p = {};
+  p.pitch = round_up(d->hidden, kGroup);
+  p.dz_pitch = round_up(2 * d->hidden, kGroup);
+  const size_t rows = (size_t)d->members * d->rows, size = d->dtype ? 2 : 4;
+  auto take = [&](size_t bytes) { const size_t at = p.bytes; p.bytes += (bytes + 255) & ~(size_t)255; return at; };
+  if (!d->kept) p.z = take(rows * 2 * p.pitch * sizeof(float));
+  if (backward) p.dz = take(rows * p.dz_pitch * size);
+  if (!p.bytes) p.bytes = 256;
+  return p;
+}
+
+template <typename T>
+CellArgs<T> cells_of(const pbt_gated_desc* d, const Plan& p, const float* z) {
+  CellArgs<T> a = {};
+  a.z = z; a.pitch = p.pitch;
+  a.rows = (uint32_t)d->rows; a.hidden = (uint32_t)d->hidden; a.groups = (uint32_t)(p.pitch / kGroup);
+  a.activation = d->activation; a.drop = d->drop != nullptr;
+  if (d->drop) a.rule = *d->drop;
+  return a;
+}
+template <typename T, bool BACKWARD>
+cudaError_t launch_cells(const pbt_gated_desc* d, const CellArgs<T>& a, cudaStream_t s) {
+  const dim3 grid((unsigned)(((uint64_t)a.rows * a.groups + 255) / 256), (unsigned)d->members);
+  return launch_with(grid, 256, 0, s)(k_gated_cells<T, BACKWARD>, a);
+}
+
+GemmArgs product(const pbt_gated_desc* d) {
+  GemmArgs g;
+  memset(&g, 0, sizeof(g));
+  g.batch = d->members;
+  g.in_dtype = g.out_dtype = d->dtype ? kBF16 : kF32;
+  return g;
+}
+
+// g and u of all rows, fp32
+cudaError_t project(const pbt_gated_desc* d, const Plan& p, float* z, cudaStream_t s) {
+  GemmArgs g = product(d);
+  g.M = d->rows; g.N = d->hidden; g.K = d->width;
+  g.out_dtype = kF32;
+  g.A = d->x; g.lda = d->x_row; g.strideA = d->x_member;
+  g.ldb = d->weight_row; g.strideB = d->weight_member;
+  g.ldc = 2 * p.pitch; g.strideC = (long long)d->rows * 2 * p.pitch;
+  for (int half = 0; half < 2; ++half) {
+    g.B = (const char*)d->weight + half * (long long)d->hidden * d->weight_row * (d->dtype ? 2 : 4);
+    g.C = z + half * p.pitch;
+    const cudaError_t e = launch_gemm_simt(g, s);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+template <typename T>
+cudaError_t forward(const pbt_gated_desc* d, char* ws, cudaStream_t s) {
+  const Plan p = plan_of(d, false);
+  float* z = d->kept ? d->kept : (float*)(ws + p.z);
+  const cudaError_t e = project(d, p, z, s);
+  if (e != cudaSuccess) return e;
+  CellArgs<T> a = cells_of<T>(d, p, z);
+  a.out = (T*)d->h; a.out_pitch = d->hidden;
+  return launch_cells<T, false>(d, a, s);
+}
+
+template <typename T>
+cudaError_t backward(const pbt_gated_desc* d, char* ws, cudaStream_t s) {
+  const Plan p = plan_of(d, true);
+  const float* z = d->kept;
+  cudaError_t e = cudaSuccess;
+  if (!z) {
+    z = (const float*)(ws + p.z);
+    e = project(d, p, (float*)(ws + p.z), s);
+    if (e != cudaSuccess) return e;
+  }
+  T* dz = (T*)(ws + p.dz);
+  CellArgs<T> a = cells_of<T>(d, p, z);
+  a.dh = (const T*)d->dh; a.dh_member = d->dh_member; a.dh_row = d->dh_row;
+  a.out = dz; a.out_pitch = p.dz_pitch;
+  e = launch_cells<T, true>(d, a, s);
+  if (e != cudaSuccess) return e;
+  GemmArgs g = product(d);
+  g.A = dz; g.lda = p.dz_pitch; g.strideA = (long long)d->rows * p.dz_pitch;
+  g.M = d->rows; g.N = d->width; g.K = 2 * d->hidden;
+  g.B = d->weight; g.ldb = d->weight_row; g.strideB = d->weight_member; g.b_mn = 1;
+  g.C = d->dx; g.ldc = d->width; g.strideC = (long long)d->rows * d->width;
+  e = launch_gemm_simt(g, s);
+  if (e != cudaSuccess) return e;
+  g.a_mn = 1;
+  g.M = 2 * d->hidden; g.K = d->rows;
+  g.B = d->x; g.ldb = d->x_row; g.strideB = d->x_member;
+  g.C = d->dweight; g.strideC = 2ll * d->hidden * d->width;
+  return launch_gemm_simt(g, s);
+}
+
+int check(const pbt_gated_desc* d) {
+  if (!d) return fail(PBT_ERR_INVALID_ARG, "desc is NULL");
+  if (d->members < 1 || d->rows < 0 || d->width < 1 || d->hidden < 1) return fail(PBT_ERR_INVALID_ARG, "members, width and hidden must be positive, rows >= 0");
+  if (d->members > 65535) return fail(PBT_ERR_UNSUPPORTED, "more than 65535 members");
+  if (d->rows >= 1 << 22 || d->width >= 1 << 22 || d->hidden >= 1 << 21) return fail(PBT_ERR_UNSUPPORTED, "rows, width and 2 hidden must stay below 2^22");
+  // tiles are counted in 32 bits (the smallest have 64 rows and 64 columns)
+  auto tiles = [&](long long m, long long n) { return (m + 63) / 64 * ((n + 63) / 64) * d->members > 0x7FFFFFFFll; };
+  if (tiles(d->rows, 2ll * d->hidden) || tiles(d->rows, d->width) || tiles(2ll * d->hidden, d->width))
+    return fail(PBT_ERR_UNSUPPORTED, "more than 2^31 - 1 tiles of 64 x 64 elements in a call: split the members or the rows");
+  if (d->dtype != 0 && d->dtype != 1) return fail(PBT_ERR_UNSUPPORTED, "operands are float or bfloat16");
+  if (d->activation < 0 || d->activation > 3) return fail(PBT_ERR_UNSUPPORTED, "activation is 0 (silu), 1 (gelu), 2 (relu) or 3 (sigmoid)");
+  if (!d->weight) return fail(PBT_ERR_INVALID_ARG, "weight is NULL");
+  if (d->dtype == 1 && !d->status_device) return fail(PBT_ERR_INVALID_ARG, "status_device is required by the tensor-core kernels");
+  if (d->weight_row < d->width || d->weight_member < 0) return fail(PBT_ERR_INVALID_ARG, "weight_row is smaller than a row, or weight_member negative");
+  if (d->rows && (!d->x || d->x_row < d->width || d->x_member < 0)) return fail(PBT_ERR_INVALID_ARG, "x is NULL, its row stride smaller than a row or its member stride negative");
+  return d->drop ? dropout::check_rule(d->drop, d->members, d->rows, d->hidden) : PBT_OK;
+}
+
+int check_workspace(const pbt_gated_desc* d, bool backward, const void* workspace, size_t bytes) {
+  if (workspace && ((uintptr_t)workspace & 255) == 0 && bytes >= plan_of(d, backward).bytes) return PBT_OK;
+  return fail(PBT_ERR_WORKSPACE, "workspace missing, not 256-byte aligned or smaller than pbt_gated_query_workspace says");
+}
+
+}  // namespace
+}  // namespace gated
+}  // namespace pbt
+
+extern "C" int pbt_gated_query_workspace(const pbt_gated_desc* d, int backward, size_t* bytes) {
+  using namespace pbt::gated;
+  if (!bytes) return fail(PBT_ERR_INVALID_ARG, "bytes is NULL");
+  const int rc = check(d);
+  if (rc) return rc;
+  *bytes = plan_of(d, backward != 0).bytes;
+  return PBT_OK;
+}
+
+extern "C" int pbt_gated_forward(const pbt_gated_desc* d, void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace pbt;
+  using namespace pbt::gated;
+  int rc = check(d);
+  if (rc) return rc;
+  if (!d->rows) return PBT_OK;
+  if (!d->h) return fail(PBT_ERR_INVALID_ARG, "h is NULL");
+  rc = check_workspace(d, false, workspace, workspace_bytes);
+  if (rc) return rc;
+  const cudaError_t e = d->dtype ? forward<bf16>(d, (char*)workspace, (cudaStream_t)stream) : forward<float>(d, (char*)workspace, (cudaStream_t)stream);
+  return e == cudaSuccess ? PBT_OK : fail(PBT_ERR_CUDA, cudaGetErrorString(e));
+}
+
+extern "C" int pbt_gated_backward(const pbt_gated_desc* d, void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace pbt;
+  using namespace pbt::gated;
+  int rc = check(d);
+  if (rc) return rc;
+  if (!d->dweight) return fail(PBT_ERR_INVALID_ARG, "dweight is NULL");
+  cudaError_t e;
+  if (!d->rows) {
+    e = cudaMemsetAsync(d->dweight, 0, (size_t)d->members * 2 * d->hidden * d->width * (d->dtype ? 2 : 4), (cudaStream_t)stream);
+  } else {
+    if (!d->dx || !d->dh || d->dh_row < d->hidden || d->dh_member < 0)
+      return fail(PBT_ERR_INVALID_ARG, "dx or dh is NULL, the row stride of dh smaller than a row or its member stride negative");
+    rc = check_workspace(d, true, workspace, workspace_bytes);
+    if (rc) return rc;
+    e = d->dtype ? backward<bf16>(d, (char*)workspace, (cudaStream_t)stream) : backward<float>(d, (char*)workspace, (cudaStream_t)stream);
+  }
+  return e == cudaSuccess ? PBT_OK : fail(PBT_ERR_CUDA, cudaGetErrorString(e));
+}

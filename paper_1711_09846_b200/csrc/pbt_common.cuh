@@ -16,7 +16,7 @@ typedef __nv_bfloat16 bf16;
 // Philox4x32-10 (Salmon et al., SC'11, Section 3.3), device + host.
 // counter = (member, round_or_step, stream, block), key = (seed_lo, seed_hi)
 // ---------------------------------------------------------------------------
-enum PhiloxStream : uint32_t { kStreamExploit = 0, kStreamExplore = 1, kStreamBatch = 2, kStreamInit = 3, kStreamInterp = 4 };
+enum PhiloxStream : uint32_t { kStreamExploit = 0, kStreamExplore = 1, kStreamBatch = 2, kStreamInit = 3, kStreamInterp = 4, kStreamDropout = 5 /* and on, one for every site */ };
 
 struct U4 {
   uint32_t x[4];

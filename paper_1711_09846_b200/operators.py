@@ -1,7 +1,7 @@
-"""Operators of a population that fine-tunes adapters on shared blocks: low-rank adapters beside a shared projection,
-block norms, gradient clipping.
+"""Operators of populations that train residual blocks: low-rank adapters beside a shared projection, gated units with a weight of
+every member's own, dropout, block norms, gradient clipping.
 
-Thin wrappers over the pbt_adapter_*, pbt_block_norm_* and pbt_clip_* calls of the C ABI: argument checks, result allocation and
+Thin wrappers over the pbt_adapter_*, pbt_gated_*, pbt_dropout, pbt_block_norm_* and pbt_clip_* calls of the C ABI: argument checks, result allocation and
 marshalling; every computation runs in the library's CUDA kernels.  Each call only enqueues work, on `stream` (a torch
 stream) or the current stream of the tensors' device; results are allocated for that stream.
 
@@ -11,11 +11,12 @@ taken as plain numbers.  To put an operator into a graph, call the pair from a t
 from __future__ import annotations
 
 import ctypes as C
-from typing import NamedTuple, Optional, Sequence
+from typing import NamedTuple, Optional, Sequence, Union
 
 import torch
 
-from .binding import PbtAdapterDesc, PbtBlockNormDesc, PbtClipTensor, PbtError, load_library
+from .binding import (PbtAdapterDesc, PbtBlockNormDesc, PbtClipTensor, PbtDropoutDesc, PbtDropRule, PbtError, PbtGatedDesc,
+                      load_library)
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1}
 _MOST = 0x7FFFFFFF      # what the library's 32-bit sizes hold; ctypes would cut a larger one without a word
@@ -419,3 +420,192 @@ class AdapterProjection:
             rc = _with_workspace(call, at, nbytes.value, s)
         if rc:
             _check(rc)
+
+
+# --- dropout -----------------------------------------------------------------------------------------------------------------
+
+
+class Dropout(NamedTuple):
+    """Which elements of which member are dropped (pbt_drop_rule).  No mask is stored: both directions draw it from
+    (seed; member, the member's step, site, place of the element).
+
+    rate: a number, or float32 [members] on the device (a hyperparameter of every member, read when the kernels run); seed: 0 .. 2^64 - 1;
+    step: a number, or int64 [members] on the device (the members' own step counts: what a captured graph that is
+    replayed has to take, or it draws the same masks again); site: which dropout of the network (two with the same site and width draw
+    the same); first_member: index of the first member in the whole population, for a shard of it."""
+    rate: Union[float, torch.Tensor]
+    seed: int
+    step: Union[int, torch.Tensor]
+    site: int = 0
+    first_member: int = 0
+
+
+def _drop_rule(drop, members, device):
+    rate, seed, step, site, first = drop
+    rates = steps = None
+    if isinstance(rate, torch.Tensor):
+        if not (rate.dtype is torch.float32 and rate.shape == (members,) and rate.device == device and rate.is_contiguous()):
+            raise ValueError("a dropout's rate is a number or a contiguous float32 tensor [members] on the activations' device")
+        rates, rate = rate.data_ptr(), 0.0
+    if isinstance(step, torch.Tensor):
+        if not (step.dtype is torch.int64 and step.shape == (members,) and step.device == device and step.is_contiguous()):
+            raise ValueError("a dropout's step is a number or a contiguous int64 tensor [members] on the activations' device")
+        steps, step = step.data_ptr(), 0
+    if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 63 and 0 <= site <= 1 << 30 and 0 <= first <= _MOST):
+        raise ValueError("a dropout's seed is a number of 64 bits; step, site (at most 2^30) and first_member are not negative")
+    return PbtDropRule(rates, steps, seed, step, rate, site, first)
+
+
+def _drop_inputs(drop):
+    return () if drop is None else tuple(t for t in (drop.rate, drop.step) if isinstance(t, torch.Tensor))
+
+
+def dropout_forward(x, dropout: Dropout, residual=None, stream=None):
+    """residual + keep x / (1 - rate) (pbt_dropout); x and residual: [members, rows, width], float32 or bfloat16, with contiguous columns."""
+    shape, dtype, device = kind = x.shape, x.dtype, x.device
+    if not (x.is_cuda and len(shape) == 3 and dtype in _TYPES):
+        raise ValueError("activations are CUDA tensors [members, rows, width], float32 or bfloat16")
+    m, rows, width = shape
+    if m > _MOST or rows > _MOST or width > _MOST:
+        raise ValueError("activations have at most 2^31 - 1 members, rows and columns")
+    d = PbtDropoutDesc()
+    d.members, d.rows, d.width, d.dtype = m, rows, width, _TYPES[dtype]
+    d.x, d.x_member, d.x_row = _activation(x, kind, "x")
+    if residual is not None:
+        d.residual, d.residual_member, d.residual_row = _activation(residual, kind, "residual")
+    d.rule = _drop_rule(dropout, m, device)
+    inputs = () if stream is None else (x, residual, *_drop_inputs(dropout))
+    return _on(device, stream, inputs, _dropout, d, x)
+
+
+def _dropout(s, d, x):
+    y = _like(x)
+    d.y = y.data_ptr()
+    rc = load_library().pbt_dropout(C.byref(d), s)
+    if rc:
+        _check(rc)
+    return y
+
+
+def dropout_backward(dy, dropout: Dropout, stream=None):
+    """The gradient of dropout_forward's x: the same elements of dy, scaled (the residual's gradient is dy itself)."""
+    return dropout_forward(dy, dropout, None, stream)
+
+
+# --- gated units -------------------------------------------------------------------------------------------------------------
+
+_ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2, "sigmoid": 3}
+
+
+class GatedUnit:
+    """The gated hidden layer of a feed-forward block, for every member of a population its own (pbt_gated_*):
+    h = keep / (1 - rate) act(x Wg^T) (x Wu^T).
+
+    weight: [members, 2 hidden, width], the gate's rows first, then the up-projection's; float32 or bfloat16, contiguous columns, any
+    member and row stride (weight.expand(...): one for all members).  It is used where it lies: update it in place between calls.
+    activation: "silu", "gelu" (with the error function), "relu" or "sigmoid".  The projection behind it is a plain product: grouped_gemm, or
+    AdapterProjection where it is shared.
+
+    Activations are [members, rows, ...] of the weight's type with contiguous columns; one token of every member has rows = 1."""
+
+    def __init__(self, weight, activation: str = "silu"):
+        _require(weight.is_cuda and weight.dim() == 3 and weight.dtype in _TYPES and (weight.stride(2) == 1 or weight.shape[2] == 1),
+                 "weight is a CUDA tensor [members, 2 hidden, width], float32 or bfloat16, with contiguous columns")
+        m, n, k = weight.shape
+        _require(n > 0 and n % 2 == 0, "weight has the gate's rows and as many of the up-projection")
+        _require(activation in _ACTIVATIONS, "activation is " + ", ".join(_ACTIVATIONS))
+        _require(max(m, n, k) <= _MOST, "members, hidden and width are at most 2^31 - 1")
+        self.weight, self.hidden = weight, n // 2
+        self.lib = load_library()
+        d = self._desc = PbtGatedDesc()
+        d.members, d.width, d.hidden, d.dtype, d.activation = m, k, n // 2, _TYPES[weight.dtype], _ACTIVATIONS[activation]
+        d.weight, d.weight_member, d.weight_row = weight.data_ptr(), weight.stride(0), weight.stride(1)
+        self._status = torch.zeros(8, dtype=torch.int32, device=weight.device)
+        self._home = _current_stream(weight.device.index)
+        torch.cuda.current_stream(weight.device).synchronize()      # the calls may be on any stream
+        d.status_device = self._status.data_ptr()
+        _check(self.lib.pbt_gated_query_workspace(C.byref(d), 0, C.byref(C.c_size_t(0))))
+
+    def _call(self, x, dropout):
+        """The description of a call on these rows (a copy: calls from several threads do not share it), and the dropout it points to."""
+        w, shape = self.weight, x.shape
+        if not (len(shape) == 3 and shape[0] == self._desc.members and shape[2] == self._desc.width and x.dtype == w.dtype and x.device == w.device):
+            raise ValueError("x is [members, rows, width] of the weight's members, width, type and device")
+        if shape[1] > _MOST:
+            raise ValueError("a call has at most 2^31 - 1 rows")
+        d = PbtGatedDesc.from_buffer_copy(self._desc)
+        d.rows = shape[1]
+        d.x, d.x_member, d.x_row = _rows_of(x, "x")
+        rule = None
+        if dropout is not None:
+            rule = _drop_rule(dropout, d.members, w.device)
+            d.drop = C.pointer(rule)
+        return d, rule
+
+    def forward(self, x, dropout: Optional[Dropout] = None, keep: bool = False, stream=None):
+        """h [members, rows, hidden]; with keep, also g and u in float32 for the backward pass (8 bytes a hidden unit; without
+        them it works them out anew, which costs two thirds of a forward pass more)."""
+        d, _rule = self._call(x, dropout)
+        inputs = () if stream is None else (x, self.weight, *_drop_inputs(dropout))
+        return _on(self.weight.device, stream, inputs, self._forward, d, keep)
+
+    def _forward(self, s, d, keep):
+        w = self.weight
+        h = w.new_empty((d.members, d.rows, d.hidden))
+        d.h = h.data_ptr()
+        kept = None
+        if keep:
+            kept = torch.empty((d.members, d.rows, 2, (d.hidden + 7) // 8 * 8), dtype=torch.float32, device=w.device)
+            d.kept = kept.data_ptr()
+        if d.rows:
+            self._run(d, 0, self.lib.pbt_gated_forward, s)
+        return (h, kept) if keep else h
+
+    def backward(self, dh, x, kept=None, dropout: Optional[Dropout] = None, stream=None):
+        """(dx, dweight) from dh [members, rows, hidden], the forward pass's x, what it kept (or None) and its dropout.  dweight is
+        [members, 2 hidden, width] of the weight's type, every member's own even where the weight is one for all."""
+        d, _rule = self._call(x, dropout)
+        w = self.weight
+        if not (dh.shape == (d.members, d.rows, d.hidden) and dh.dtype == w.dtype and dh.device == w.device):
+            raise ValueError("dh is [members, rows, hidden] of the weight's type and device")
+        d.dh, d.dh_member, d.dh_row = _rows_of(dh, "dh")
+        if kept is not None:
+            if not (kept.shape == (d.members, d.rows, 2, (d.hidden + 7) // 8 * 8) and kept.dtype is torch.float32 and kept.device == w.device
+                    and kept.is_contiguous()):
+                raise ValueError("kept is what forward(keep=True) returned")
+            d.kept = kept.data_ptr()
+        inputs = () if stream is None else (dh, x, kept, w, *_drop_inputs(dropout))
+        return _on(w.device, stream, inputs, self._backward, d)
+
+    def _backward(self, s, d):
+        w = self.weight
+        dx = w.new_empty((d.members, d.rows, d.width))
+        dweight = w.new_empty((d.members, 2 * d.hidden, d.width))
+        d.dx, d.dweight = dx.data_ptr(), dweight.data_ptr()
+        self._run(d, 1, self.lib.pbt_gated_backward, s)
+        return dx, dweight
+
+    def check(self):
+        """Waits for the enqueued calls and raises if one of the kernels' bounded waits ran out (PBT_ERR_TIMEOUT)."""
+        torch.cuda.synchronize(self.weight.device)
+        code = int(self._status[4].item())
+        if code:
+            raise PbtError(code, "a bounded wait inside a kernel ran out")
+
+    def _run(self, d, backward, call, s):
+        if s != self._home:      # keeps the status words until the call is done, should the object go first
+            self._status.record_stream(torch.cuda.current_stream(self.weight.device))
+        nbytes, at = C.c_size_t(0), C.byref(d)
+        rc = self.lib.pbt_gated_query_workspace(at, backward, C.byref(nbytes))
+        if not rc:
+            rc = _with_workspace(call, at, nbytes.value, s)
+        if rc:
+            _check(rc)
+
+
+def _rows_of(t, name):
+    member, row, column = t.stride()
+    rows, columns = t.shape[1], t.shape[2]
+    if column != 1 and columns != 1:
+        raise ValueError(f"{name} has to have contiguous columns")
+    return t.data_ptr(), member, row if rows > 1 else max(row, columns)      # (a single row may carry any stride)
