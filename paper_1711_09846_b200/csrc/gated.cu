@@ -69,9 +69,10 @@ __global__ void __launch_bounds__(256) k_gated_cells(const CellArgs<T> a) {
 
 // What a call does and where things lie in its workspace.
 struct Plan {
-  int pitch;              // of g and u
+  int pitch;                      // of g and u
   int dz_pitch;
-  size_t z, dz, bytes;    // offsets (z: only where the caller keeps none)
+  size_t z, dz, x, w, bytes;      // offsets; z: only where the caller keeps none and it is needed
+  bool has_z, pack_x, pack_w;     // pack: bf16 rows that are not multiples of 16 bytes are laid out anew
 };
 Plan plan_of(const pbt_gated_desc* d, bool backward) {
   Plan p = {};
@@ -79,10 +80,42 @@ Plan plan_of(const pbt_gated_desc* d, bool backward) {
   p.dz_pitch = round_up(2 * d->hidden, kGroup);
   const size_t rows = (size_t)d->members * d->rows, size = d->dtype ? 2 : 4;
   auto take = [&](size_t bytes) { const size_t at = p.bytes; p.bytes += (bytes + 255) & ~(size_t)255; return at; };
-  if (!d->kept) p.z = take(rows * 2 * p.pitch * sizeof(float));
+  p.has_z = !d->kept && (backward || !d->dtype);
+  if (p.has_z) p.z = take(rows * 2 * p.pitch * sizeof(float));
   if (backward) p.dz = take(rows * p.dz_pitch * size);
+  if (d->dtype) {
+    // (the kernel for few rows reads whole vectors; tensor maps end at the last element wherever that is)
+    const bool odd = (!backward || !d->kept) && tc_few_rows(d) && d->width % 8;
+    p.pack_x = odd || !tc_aligned(d->x, d->x_row, d->x_member, d->members);
+    p.pack_w = odd || !tc_aligned(d->weight, d->weight_row, d->weight_member, d->members);
+    const size_t width = round_up(d->width, 8);
+    if (p.pack_x) p.x = take(rows * width * size);
+    if (p.pack_w) p.w = take((d->weight_member ? d->members : 1) * 2 * (size_t)d->hidden * width * size);
+  }
   if (!p.bytes) p.bytes = 256;
   return p;
+}
+
+// x and the weight as the kernels take them, packed where that is needed
+struct Operands {
+  Operand x, w;
+};
+cudaError_t operands_of(const pbt_gated_desc* d, const Plan& p, char* ws, Operands* o, cudaStream_t s) {
+  o->x = {(const bf16*)d->x, d->x_row, d->x_member};
+  o->w = {(const bf16*)d->weight, d->weight_row, d->members > 1 ? d->weight_member : 0};
+  const int width = round_up(d->width, 8);
+  PackSource jobs[2];
+  int n = 0;
+  if (p.pack_x) {
+    jobs[n++] = {o->x, (bf16*)(ws + p.x), d->members, d->rows, d->width};
+    o->x = {(const bf16*)(ws + p.x), width, (long long)d->rows * width};
+  }
+  if (p.pack_w) {
+    const int members = o->w.member ? d->members : 1;
+    jobs[n++] = {o->w, (bf16*)(ws + p.w), members, 2 * d->hidden, d->width};
+    o->w = {(const bf16*)(ws + p.w), width, members > 1 ? 2ll * d->hidden * width : 0};
+  }
+  return n ? tc_pack(jobs, n, s) : cudaSuccess;
 }
 
 template <typename T>
@@ -108,16 +141,15 @@ GemmArgs product(const pbt_gated_desc* d) {
   return g;
 }
 
-// g and u of all rows, fp32
-cudaError_t project(const pbt_gated_desc* d, const Plan& p, float* z, cudaStream_t s) {
+// fp32: g and u of all rows
+cudaError_t project_f32(const pbt_gated_desc* d, const Plan& p, float* z, cudaStream_t s) {
   GemmArgs g = product(d);
   g.M = d->rows; g.N = d->hidden; g.K = d->width;
-  g.out_dtype = kF32;
   g.A = d->x; g.lda = d->x_row; g.strideA = d->x_member;
   g.ldb = d->weight_row; g.strideB = d->weight_member;
   g.ldc = 2 * p.pitch; g.strideC = (long long)d->rows * 2 * p.pitch;
   for (int half = 0; half < 2; ++half) {
-    g.B = (const char*)d->weight + half * (long long)d->hidden * d->weight_row * (d->dtype ? 2 : 4);
+    g.B = (const float*)d->weight + half * (long long)d->hidden * d->weight_row;
     g.C = z + half * p.pitch;
     const cudaError_t e = launch_gemm_simt(g, s);
     if (e != cudaSuccess) return e;
@@ -125,15 +157,25 @@ cudaError_t project(const pbt_gated_desc* d, const Plan& p, float* z, cudaStream
   return cudaSuccess;
 }
 
-template <typename T>
 cudaError_t forward(const pbt_gated_desc* d, char* ws, cudaStream_t s) {
   const Plan p = plan_of(d, false);
+  if (d->dtype) {
+    Operands o;
+    const cudaError_t e = operands_of(d, p, ws, &o, s);
+    return e == cudaSuccess ? tc_forward(d, o.x, o.w, d->h, d->kept, p.pitch, s) : e;
+  }
   float* z = d->kept ? d->kept : (float*)(ws + p.z);
-  const cudaError_t e = project(d, p, z, s);
+  const cudaError_t e = project_f32(d, p, z, s);
   if (e != cudaSuccess) return e;
-  CellArgs<T> a = cells_of<T>(d, p, z);
-  a.out = (T*)d->h; a.out_pitch = d->hidden;
-  return launch_cells<T, false>(d, a, s);
+  CellArgs<float> a = cells_of<float>(d, p, z);
+  a.out = (float*)d->h; a.out_pitch = d->hidden;
+  return launch_cells<float, false>(d, a, s);
+}
+
+// the faster of the tensor-core products, which take rows of any number here: tensor maps fill what is missing with zeros
+cudaError_t run_product(const pbt_gated_desc* d, const GemmArgs& g, cudaStream_t s) {
+  if (!d->dtype) return launch_gemm_simt(g, s);
+  return gemm_tc_pair_preferred(g) ? launch_gemm_tc_pair(g, (Counters*)d->status_device, s) : launch_gemm_tc(g, (Counters*)d->status_device, s);
 }
 
 template <typename T>
@@ -141,11 +183,14 @@ cudaError_t backward(const pbt_gated_desc* d, char* ws, cudaStream_t s) {
   const Plan p = plan_of(d, true);
   const float* z = d->kept;
   cudaError_t e = cudaSuccess;
-  if (!z) {
-    z = (const float*)(ws + p.z);
-    e = project(d, p, (float*)(ws + p.z), s);
-    if (e != cudaSuccess) return e;
+  Operands o = {};
+  if (d->dtype) e = operands_of(d, p, ws, &o, s);
+  if (e == cudaSuccess && !z) {
+    float* made = (float*)(ws + p.z);
+    e = d->dtype ? tc_forward(d, o.x, o.w, nullptr, made, p.pitch, s) : project_f32(d, p, made, s);
+    z = made;
   }
+  if (e != cudaSuccess) return e;
   T* dz = (T*)(ws + p.dz);
   CellArgs<T> a = cells_of<T>(d, p, z);
   a.dh = (const T*)d->dh; a.dh_member = d->dh_member; a.dh_row = d->dh_row;
@@ -155,15 +200,20 @@ cudaError_t backward(const pbt_gated_desc* d, char* ws, cudaStream_t s) {
   GemmArgs g = product(d);
   g.A = dz; g.lda = p.dz_pitch; g.strideA = (long long)d->rows * p.dz_pitch;
   g.M = d->rows; g.N = d->width; g.K = 2 * d->hidden;
-  g.B = d->weight; g.ldb = d->weight_row; g.strideB = d->weight_member; g.b_mn = 1;
+  g.b_mn = 1;
+  g.B = d->dtype ? (const void*)o.w.p : d->weight;
+  g.ldb = d->dtype ? o.w.row : d->weight_row;
+  g.strideB = d->dtype ? o.w.member : d->weight_member;
   g.C = d->dx; g.ldc = d->width; g.strideC = (long long)d->rows * d->width;
-  e = launch_gemm_simt(g, s);
+  e = run_product(d, g, s);
   if (e != cudaSuccess) return e;
   g.a_mn = 1;
   g.M = 2 * d->hidden; g.K = d->rows;
-  g.B = d->x; g.ldb = d->x_row; g.strideB = d->x_member;
+  g.B = d->dtype ? (const void*)o.x.p : d->x;
+  g.ldb = d->dtype ? o.x.row : d->x_row;
+  g.strideB = d->dtype ? o.x.member : d->x_member;
   g.C = d->dweight; g.strideC = 2ll * d->hidden * d->width;
-  return launch_gemm_simt(g, s);
+  return run_product(d, g, s);
 }
 
 int check(const pbt_gated_desc* d) {
@@ -211,7 +261,7 @@ extern "C" int pbt_gated_forward(const pbt_gated_desc* d, void* workspace, size_
   if (!d->h) return fail(PBT_ERR_INVALID_ARG, "h is NULL");
   rc = check_workspace(d, false, workspace, workspace_bytes);
   if (rc) return rc;
-  const cudaError_t e = d->dtype ? forward<bf16>(d, (char*)workspace, (cudaStream_t)stream) : forward<float>(d, (char*)workspace, (cudaStream_t)stream);
+  const cudaError_t e = forward(d, (char*)workspace, (cudaStream_t)stream);
   return e == cudaSuccess ? PBT_OK : fail(PBT_ERR_CUDA, cudaGetErrorString(e));
 }
 

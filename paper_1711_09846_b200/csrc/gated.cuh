@@ -7,6 +7,22 @@ namespace gated {
 
 enum Activation : int { kSilu = 0, kGelu = 1, kRelu = 2, kSigmoid = 3 };
 
+// An operand of the tensor cores: [members][rows][...], 16-byte aligned rows; member 0: the same for all members.
+struct Operand {
+  const bf16* p;
+  long long row, member;
+};
+// bf16 (gated_tc.cu): h (or null) and g, u in fp32 (or null), [members][rows][2][pitch]
+bool tc_aligned(const void* p, long long row, long long member, int members);
+inline bool tc_few_rows(const pbt_gated_desc* d) { return d->rows <= 64; }      // a kernel that reads whole vectors of a row
+struct PackSource {
+  Operand from;
+  bf16* to;                      // rows of a multiple of 8 elements
+  int members, rows, cols;
+};
+cudaError_t tc_pack(const PackSource* src, int n, cudaStream_t s);      // one or two
+cudaError_t tc_forward(const pbt_gated_desc* d, const Operand& x, const Operand& w, void* h, float* z, int pitch, cudaStream_t s);
+
 #ifdef __CUDACC__
 // act(g)
 __device__ __forceinline__ float activation(int kind, float g) {
