@@ -24,41 +24,172 @@ struct Args {
   pbt_drop_rule rule;
 };
 
-__device__ __forceinline__ float as_float(float v) { return v; }
-__device__ __forceinline__ float as_float(bf16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ void store(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store(bf16* p, float v) { *p = __float2bfloat16_rn(v); }
+template <typename T>
+struct Raw {      // eight elements as they lie in memory
+  uint4 a, b;
+};
+template <typename T>
+__device__ __forceinline__ Raw<T> load8(const T* p) {
+  Raw<T> r;
+  r.a = load16(p);
+  if (sizeof(T) == 4) r.b = load16(p + 4);
+  return r;
+}
+__device__ __forceinline__ Eight values(const Raw<bf16>& r) { return unpack(r.a); }
+__device__ __forceinline__ Eight values(const Raw<float>& r) { return unpack(r.a, r.b); }
 
-template <typename T, bool RESIDUAL>
+// element by element: the kept ones scaled, the others zero
+__device__ __forceinline__ float drop(float x, bool in, float scale) { return in ? x * scale : 0.f; }
+
+// Whole groups in 16-byte vectors, U of them a thread, 256 apart, so that all their loads are under way before the first draw.
+// FLAT: rows follow one another without gaps, and a group's number in the member is its place, too.
+template <typename T, bool RESIDUAL, bool FLAT, int U>
 __global__ void __launch_bounds__(256) k_dropout(const Args<T> a) {
   pdl_prologue();
   const int m = blockIdx.y;
+  const uint32_t total = a.rows * a.groups, first = blockIdx.x * (256 * U) + threadIdx.x;
+  const T* x = a.x + m * a.x_member;
+  const T* r = RESIDUAL ? a.residual + m * a.residual_member : nullptr;
+  T* y = a.y + (long long)m * a.rows * a.width;
   const Draw d = draw_of(a.rule, m);
+  Raw<T> vx[U], vr[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const uint32_t i = first + u * 256;
+    if (i >= total || i < first) continue;
+    long long at_x = (long long)i * kGroup, at_r = at_x;
+    if (!FLAT) {
+      const uint32_t row = i / a.groups, c = (i - row * a.groups) * kGroup;
+      at_x = row * a.x_row + c;
+      at_r = row * a.residual_row + c;
+    }
+    vx[u] = load8(x + at_x);
+    if (RESIDUAL) vr[u] = load8(r + at_r);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const uint32_t i = first + u * 256;
+    if (i >= total || i < first) continue;
+    Eight e = values(vx[u]);
+    if (d.on) {
+      const U4 w = draw_group(d, i);
+#pragma unroll
+      for (int c = 0; c < kGroup; ++c) e.v[c] = drop(e.v[c], kept(w, c, d.limit), d.scale);
+    }
+    if (RESIDUAL) {
+      const Eight q = values(vr[u]);
+#pragma unroll
+      for (int c = 0; c < kGroup; ++c) e.v[c] += q.v[c];
+    }
+    store8(y + (long long)i * kGroup, e);
+  }
+}
+
+// Any width from 8 on, all activations without gaps: a thread has eight elements that follow one another from a 16-byte boundary, which belong to
+// two or three groups and one or two rows (the second one perhaps of the next member).  I: 32 bits as far as they hold every place (a 64-bit
+// division costs as much as the draws).
+template <typename T, bool RESIDUAL, typename I>
+__global__ void __launch_bounds__(256) k_dropout_odd(const Args<T> a, I total) {
+  pdl_prologue();
+  const I at = ((I)blockIdx.x * 256 + threadIdx.x) * kGroup;
+  if (at >= total) return;
+  const bool whole = total - at >= kGroup;
+  const I line = at / a.width;                               // row of all members' rows
+  const uint32_t col = (uint32_t)(at - line * a.width), m = (uint32_t)(line / a.rows), row = (uint32_t)(line - (I)m * a.rows), left = a.width - col;
+  Eight e, q;
+  if (whole) {
+    e = values(load8(a.x + at));
+    if (RESIDUAL) q = values(load8(a.residual + at));
+  } else {
+#pragma unroll
+    for (int c = 0; c < kGroup; ++c) {
+      e.v[c] = c < total - at ? as_float(a.x[at + c]) : 0.f;
+      if (RESIDUAL) q.v[c] = c < total - at ? as_float(a.residual[at + c]) : 0.f;
+    }
+  }
+  const Draw d = draw_of(a.rule, m);
+  const uint32_t block = row * a.groups + col / kGroup, shift = col % kGroup;
+  uint32_t bits = kept_bits(d, block) >> shift;
+  float scale = d.on ? d.scale : 1.f, next_scale = scale;
+  if (shift && left > kGroup - shift) bits |= kept_bits(d, block + 1) << (kGroup - shift);
+  if (left < kGroup && left < total - at) {
+    Draw next = d;
+    const bool same = row + 1 < a.rows;
+    if (!same) {
+      next = draw_of(a.rule, m + 1);
+      next_scale = next.on ? next.scale : 1.f;
+    }
+    bits = (bits & ((1u << left) - 1u)) | kept_bits(next, same ? (row + 1) * a.groups : 0u) << left;
+  }
+#pragma unroll
+  for (int c = 0; c < kGroup; ++c) {
+    e.v[c] = drop(e.v[c], bits >> c & 1u, c < left ? scale : next_scale);
+    if (RESIDUAL) e.v[c] += q.v[c];
+  }
+  if (whole) {
+    store8(a.y + at, e);
+  } else {
+#pragma unroll
+    for (int c = 0; c < kGroup; ++c)
+      if (c < total - at) store(a.y + at + c, e.v[c]);
+  }
+}
+
+// Any width, strides and alignment: a thread has a group.
+template <typename T, bool RESIDUAL>
+__global__ void __launch_bounds__(256) k_dropout_strided(const Args<T> a) {
+  pdl_prologue();
+  const int m = blockIdx.y;
   const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= (uint64_t)a.rows * a.groups) return;
   const uint32_t row = (uint32_t)i / a.groups, c0 = ((uint32_t)i - row * a.groups) * kGroup, n = min(a.width - c0, (uint32_t)kGroup);
   const T* x = a.x + m * a.x_member + row * a.x_row + c0;
   const T* r = RESIDUAL ? a.residual + m * a.residual_member + row * a.residual_row + c0 : nullptr;
   T* y = a.y + ((long long)m * a.rows + row) * a.width + c0;
-  U4 w = {};
-  if (d.on) w = draw_group(d, (uint32_t)i);
+  const Draw d = draw_of(a.rule, m);
+  const uint32_t bits = kept_bits(d, (uint32_t)i);
+  const float scale = d.on ? d.scale : 1.f;
 #pragma unroll
   for (int c = 0; c < kGroup; ++c) {
     if (c >= n) break;
-    float v = !d.on ? as_float(x[c]) : kept(w, c, d.limit) ? as_float(x[c]) * d.scale : 0.f;
+    float v = drop(as_float(x[c]), bits >> c & 1u, scale);
     if (RESIDUAL) v += as_float(r[c]);
     store(y + c, v);
   }
 }
 
-template <typename T>
+template <typename T, bool RESIDUAL>
 cudaError_t launch(const pbt_dropout_desc* d, cudaStream_t s) {
   const uint32_t groups = (uint32_t)((d->width + kGroup - 1) / kGroup);
   const Args<T> a = {(const T*)d->x, d->x_member, d->x_row, (const T*)d->residual, d->residual_member, d->residual_row, (T*)d->y,
                      (uint32_t)d->rows, (uint32_t)d->width, groups, d->rule};
-  const dim3 grid((unsigned)(((uint64_t)d->rows * groups + 255) / 256), (unsigned)d->members);
-  return d->residual ? launch_with(grid, 256, 0, s)(k_dropout<T, true>, a) : launch_with(grid, 256, 0, s)(k_dropout<T, false>, a);
+  const uint64_t per_member = (uint64_t)d->rows * groups;
+  const long long cells = (long long)d->rows * d->width, step = 16 / sizeof(T);
+  const bool many = d->members > 1;
+  auto whole = [&](const void* p, long long member, long long row) {       // vectors at every group
+    return ((uintptr_t)p & 15) == 0 && (d->rows == 1 || row % step == 0) && (!many || member % step == 0);
+  };
+  auto gapless = [&](long long member, long long row) { return (d->rows == 1 || row == d->width) && (!many || member == cells); };
+  const bool vectors = d->width % kGroup == 0 && ((uintptr_t)d->y & 15) == 0 && whole(d->x, d->x_member, d->x_row) &&
+                       (!RESIDUAL || whole(d->residual, d->residual_member, d->residual_row));
+  auto grid = [&](int per_block) { return dim3((unsigned)((per_member + per_block - 1) / per_block), (unsigned)d->members); };
+  if (vectors) {
+    const bool flat = d->rows == 1 || (d->x_row == d->width && (!RESIDUAL || d->residual_row == d->width));
+    // two groups a thread once every SM has its fill of threads
+    const bool large = per_member * d->members >= 148ull * 2048 * 2;
+    if (flat) return large ? launch_with(grid(512), 256, 0, s)(k_dropout<T, RESIDUAL, true, 2>, a) : launch_with(grid(256), 256, 0, s)(k_dropout<T, RESIDUAL, true, 1>, a);
+    return large ? launch_with(grid(512), 256, 0, s)(k_dropout<T, RESIDUAL, false, 2>, a) : launch_with(grid(256), 256, 0, s)(k_dropout<T, RESIDUAL, false, 1>, a);
+  }
+  const long long total = cells * d->members, blocks = (total + 256 * kGroup - 1) / (256 * kGroup);
+  const uintptr_t bases = (uintptr_t)d->x | (uintptr_t)d->y | (RESIDUAL ? (uintptr_t)d->residual : 0);
+  if (d->width >= kGroup && (bases & 15) == 0 && blocks <= 0x7FFFFFFF && gapless(d->x_member, d->x_row) && (!RESIDUAL || gapless(d->residual_member, d->residual_row))) {
+    if (total < 0xFFFFF000ll) return launch_with((unsigned)blocks, 256, 0, s)(k_dropout_odd<T, RESIDUAL, uint32_t>, a, (uint32_t)total);
+    return launch_with((unsigned)blocks, 256, 0, s)(k_dropout_odd<T, RESIDUAL, unsigned long long>, a, (unsigned long long)total);
+  }
+  return launch_with(grid(256), 256, 0, s)(k_dropout_strided<T, RESIDUAL>, a);
 }
+template <typename T>
+cudaError_t launch(const pbt_dropout_desc* d, cudaStream_t s) { return d->residual ? launch<T, true>(d, s) : launch<T, false>(d, s); }
 
 }  // namespace
 

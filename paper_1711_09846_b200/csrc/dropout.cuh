@@ -37,6 +37,53 @@ __device__ __forceinline__ Draw draw_of(const pbt_drop_rule& r, int m) {
 // lower half adds below it changes no comparison with limit, whose lower half is all ones).
 __device__ __forceinline__ U4 draw_group(const Draw& d, uint32_t block) { return philox4x32_10(d.member, d.step, d.stream, block, d.seed); }
 __device__ __forceinline__ bool kept(const U4& w, int c, uint32_t limit) { return ((c & 1) ? w.x[c >> 1] : w.x[c >> 1] << 16) > limit; }
+// bit c: column c is kept
+__device__ __forceinline__ uint32_t kept_bits(const Draw& d, uint32_t block) {
+  if (!d.on) return 0xFFu;
+  const U4 w = draw_group(d, block);
+  uint32_t bits = 0;
+#pragma unroll
+  for (int c = 0; c < kGroup; ++c) bits |= kept(w, c, d.limit) ? 1u << c : 0u;
+  return bits;
+}
+
+// Eight neighbouring elements as 16-byte vectors
+struct Eight {
+  float v[kGroup];
+};
+__device__ __forceinline__ uint4 load16(const void* p) {
+  uint4 q;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "l"(p));
+  return q;
+}
+__device__ __forceinline__ Eight unpack(const uint4& a) {       // bf16
+  Eight e;
+  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { e.v[2 * i] = __uint_as_float(w[i] << 16); e.v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+  return e;
+}
+__device__ __forceinline__ Eight unpack(const uint4& a, const uint4& b) {
+  return {__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
+          __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)};
+}
+__device__ __forceinline__ void store8(bf16* p, const Eight& e) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 t = __floats2bfloat162_rn(e.v[2 * i], e.v[2 * i + 1]);
+    w[i] = *reinterpret_cast<const uint32_t*>(&t);
+  }
+  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void store8(float* p, const Eight& e) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(e.v[0], e.v[1], e.v[2], e.v[3]);
+  reinterpret_cast<float4*>(p)[1] = make_float4(e.v[4], e.v[5], e.v[6], e.v[7]);
+}
+__device__ __forceinline__ float as_float(float v) { return v; }
+__device__ __forceinline__ float as_float(bf16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ void store(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store(bf16* p, float v) { *p = __float2bfloat16_rn(v); }
 #endif
 
 }  // namespace dropout

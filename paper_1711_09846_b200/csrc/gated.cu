@@ -11,7 +11,13 @@ void set_last_error(const char* msg);
 namespace gated {
 namespace {
 
+using dropout::as_float;
+using dropout::Eight;
 using dropout::kGroup;
+using dropout::load16;
+using dropout::store;
+using dropout::store8;
+using dropout::unpack;
 
 int fail(int code, const char* msg) {
   set_last_error(msg);
@@ -19,11 +25,6 @@ int fail(int code, const char* msg) {
 }
 
 int round_up(int n, int m) { return (n + m - 1) / m * m; }
-
-__device__ __forceinline__ float as_float(float v) { return v; }
-__device__ __forceinline__ float as_float(bf16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ void store(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store(bf16* p, float v) { *p = __float2bfloat16_rn(v); }
 
 // One thread has eight neighbouring hidden units of a row: one block of the generator.
 template <typename T>
@@ -36,34 +37,61 @@ struct CellArgs {
   pbt_drop_rule rule;
 };
 
-template <typename T, bool BACKWARD>
+// VEC: 16-byte loads and stores everywhere.  The backward pass reads 8 + 2 bytes a hidden unit and writes 4 (bf16).
+template <typename T, bool BACKWARD, bool VEC>
 __global__ void __launch_bounds__(256) k_gated_cells(const CellArgs<T> a) {
   pdl_prologue();
   const int m = blockIdx.y;
   const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= (uint64_t)a.rows * a.groups) return;
-  const uint32_t row = (uint32_t)i / a.groups, c0 = ((uint32_t)i - row * a.groups) * kGroup, n = min(a.hidden - c0, (uint32_t)kGroup);
+  const uint32_t row = (uint32_t)i / a.groups, c0 = ((uint32_t)i - row * a.groups) * kGroup, n = VEC ? kGroup : min(a.hidden - c0, (uint32_t)kGroup);
   const long long at = (long long)m * a.rows + row;
-  const float* z = a.z + at * 2 * a.pitch + c0;
+  const float* z = a.z + at * 2 * a.pitch + c0;           // (the pitch is a multiple of eight: whole groups)
   T* out = a.out + at * a.out_pitch + c0;
-  dropout::Draw d = {};
-  U4 w = {};
-  if (a.drop) d = dropout::draw_of(a.rule, m);
-  if (d.on) w = dropout::draw_group(d, (uint32_t)i);
-  const T* dh = BACKWARD ? a.dh + m * a.dh_member + row * a.dh_row + c0 : nullptr;
+  const T* from = BACKWARD ? a.dh + m * a.dh_member + row * a.dh_row + c0 : nullptr;
+  const uint4 z0 = load16(z), z1 = load16(z + 4), z2 = load16(z + a.pitch), z3 = load16(z + a.pitch + 4);
+  Eight dh;
+  if (BACKWARD) {
+    if (!VEC) {
+#pragma unroll
+      for (int c = 0; c < kGroup; ++c) dh.v[c] = c < n ? as_float(from[c]) : 0.f;
+    } else if constexpr (sizeof(T) == 2) {
+      dh = unpack(load16(from));
+    } else {
+      dh = unpack(load16(from), load16(from + 4));
+    }
+  }
+  const Eight g = unpack(z0, z1), u = unpack(z2, z3);
+  uint32_t in = 0xFFu;
+  float f = 1.f;
+  if (a.drop) {
+    const dropout::Draw d = dropout::draw_of(a.rule, m);
+    in = dropout::kept_bits(d, (uint32_t)i);
+    if (d.on) f = d.scale;
+  }
+  Eight first, second;
+#pragma unroll
+  for (int c = 0; c < kGroup; ++c) {
+    const bool keep = in >> c & 1u;
+    if (BACKWARD) {
+      float slope;
+      const float act = activation(a.activation, g.v[c], &slope), v = f * dh.v[c];
+      first.v[c] = keep ? v * u.v[c] * slope : 0.f;
+      second.v[c] = keep ? v * act : 0.f;
+    } else {
+      first.v[c] = keep ? f * (activation(a.activation, g.v[c]) * u.v[c]) : 0.f;
+    }
+  }
+  if (VEC) {
+    store8(out, first);
+    if (BACKWARD) store8(out + a.hidden, second);
+    return;
+  }
 #pragma unroll
   for (int c = 0; c < kGroup; ++c) {
     if (c >= n) break;
-    const float f = !d.on ? 1.f : d.scale;
-    const bool in = !d.on || dropout::kept(w, c, d.limit);
-    if (BACKWARD) {
-      float slope;
-      const float act = activation(a.activation, z[c], &slope), v = f * as_float(dh[c]);
-      store(out + c, in ? v * z[a.pitch + c] * slope : 0.f);
-      store(out + a.hidden + c, in ? v * act : 0.f);
-    } else {
-      store(out + c, in ? f * (activation(a.activation, z[c]) * z[a.pitch + c]) : 0.f);
-    }
+    store(out + c, first.v[c]);
+    if (BACKWARD) store(out + a.hidden + c, second.v[c]);
   }
 }
 
@@ -84,10 +112,8 @@ Plan plan_of(const pbt_gated_desc* d, bool backward) {
   if (p.has_z) p.z = take(rows * 2 * p.pitch * sizeof(float));
   if (backward) p.dz = take(rows * p.dz_pitch * size);
   if (d->dtype) {
-    // (the kernel for few rows reads whole vectors; tensor maps end at the last element wherever that is)
-    const bool odd = (!backward || !d->kept) && tc_few_rows(d) && d->width % 8;
-    p.pack_x = odd || !tc_aligned(d->x, d->x_row, d->x_member, d->members);
-    p.pack_w = odd || !tc_aligned(d->weight, d->weight_row, d->weight_member, d->members);
+    p.pack_x = !tc_aligned(d->x, d->x_row, d->x_member, d->members);
+    p.pack_w = !tc_aligned(d->weight, d->weight_row, d->weight_member, d->members);
     const size_t width = round_up(d->width, 8);
     if (p.pack_x) p.x = take(rows * width * size);
     if (p.pack_w) p.w = take((d->weight_member ? d->members : 1) * 2 * (size_t)d->hidden * width * size);
@@ -130,7 +156,11 @@ CellArgs<T> cells_of(const pbt_gated_desc* d, const Plan& p, const float* z) {
 template <typename T, bool BACKWARD>
 cudaError_t launch_cells(const pbt_gated_desc* d, const CellArgs<T>& a, cudaStream_t s) {
   const dim3 grid((unsigned)(((uint64_t)a.rows * a.groups + 255) / 256), (unsigned)d->members);
-  return launch_with(grid, 256, 0, s)(k_gated_cells<T, BACKWARD>, a);
+  // (dh: any base, row and member stride that keeps 16 bytes; what this library lays out has them where hidden is a multiple of eight)
+  constexpr int kStep = 16 / sizeof(T);
+  const bool vec = d->hidden % kGroup == 0 && ((uintptr_t)a.out & 15) == 0 && a.out_pitch % kStep == 0 &&
+                   (!BACKWARD || (((uintptr_t)a.dh & 15) == 0 && (d->rows == 1 || a.dh_row % kStep == 0) && (d->members == 1 || a.dh_member % kStep == 0)));
+  return vec ? launch_with(grid, 256, 0, s)(k_gated_cells<T, BACKWARD, true>, a) : launch_with(grid, 256, 0, s)(k_gated_cells<T, BACKWARD, false>, a);
 }
 
 GemmArgs product(const pbt_gated_desc* d) {

@@ -14,7 +14,6 @@ struct Operand {
 };
 // bf16 (gated_tc.cu): h (or null) and g, u in fp32 (or null), [members][rows][2][pitch]
 bool tc_aligned(const void* p, long long row, long long member, int members);
-inline bool tc_few_rows(const pbt_gated_desc* d) { return d->rows <= 64; }      // a kernel that reads whole vectors of a row
 struct PackSource {
   Operand from;
   bf16* to;                      // rows of a multiple of 8 elements

@@ -2,8 +2,8 @@
 //
 //   k_gated_tc_pair / k_gated_tc   tiles of 256 (128) rows and 128 (64) hidden units: the B operand of one tcgen05 product is the gate's weight
 //                                  rows and the up-projection's for the same hidden units, so that g and u of a hidden unit meet in one TMEM lane
-//   k_gated_rows                   a few rows (single tokens): bound by reading the weight once, mma.sync with eight gate rows and the eight
-//                                  up rows of the same hidden units as the tall operand: g and u meet in one thread
+//   k_gated_rows                   a few rows (single tokens): bound by reading the weight once, which is the tall operand there; clusters of CTAs
+//                                  share a contraction
 //
 // h is rounded once, from fp32 g and u.
 #include <algorithm>
@@ -17,6 +17,8 @@ namespace gated {
 namespace {
 
 using namespace tc;
+using dropout::Eight;
+using dropout::store8;
 
 // ------------------------------------------------------------------------------------------------------------------
 // Tiles
@@ -324,131 +326,193 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_gated_tc(const __grid_constan
 // ------------------------------------------------------------------------------------------------------------------
 // Few rows
 // ------------------------------------------------------------------------------------------------------------------
-constexpr int kRowsOut = 8;       // hidden units of a CTA
-
-__device__ __forceinline__ void copy16(void* slot, const void* from) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(slot)), "l"(from) : "memory");
-}
-__device__ __forceinline__ void mma16816(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
+// Up to 128 rows a member: bound by reading the weight once, so the weight is the tall operand.  A CTA has 64 hidden units, whose gate and up rows
+// are the 128 lanes of the accumulator, and all rows of x as its N columns; a cluster of `splits` CTAs shares the contraction.  The partial sums meet
+// in shared memory, where every CTA of the cluster adds up its own share of the rows over all CTAs' partial sums (in their order), and g and u
+// of a hidden unit meet, too.
+constexpr int kRowsUnits = 64, kRowsPitch = 2 * kRowsUnits + 4;      // floats of a row's partial sums: 64 g, 64 u
+constexpr int kRowsMost = 128;
+constexpr int kRowsThreads = 192;
+constexpr int kRowsSplits = 8;
 
 struct RowsParams {
-  Operand x, w;
-  int rows, hidden, width;        // width: elements of a row that exist, a multiple of 8
-  int activation, drop;
+  int rows, hidden, k_blocks;
+  int x_batched, w_batched;
+  int activation, drop, vec;
   bf16* h;                        // or null
   float* z; int pitch;            // or null
   pbt_drop_rule rule;
+  Counters* counters;
+};
+template <int N>
+struct RowsTile {
+  static constexpr int kStage = (128 + N) * kBK * 2;
+  static constexpr int kStages = N <= 32 ? 5 : N == 64 ? 4 : 6;          // two CTAs of an SM share its memory, one with 128 rows
+  static constexpr int kSums = N * kRowsPitch * 4;
+  static constexpr int kBars = kStages * kStage > kSums ? kStages * kStage : (kSums + 255) / 256 * 256;
+  static constexpr int kTotal = kBars + 256 + 1024;
+  static constexpr uint32_t kCols = N < 32 ? 32 : N;
+  static_assert(kTotal <= 232448, "shared memory of one CTA");
 };
 
-// 8 hidden units of a member and all its rows: the eight warps take every eighth block of 64 inputs.  Eight gate rows and eight up rows of the
-// weight are the tall operand of mma.sync (16 x 16), eight rows of x the narrow one; the contraction index runs in the order in which
-// 16-byte loads deliver it, in both operands.  Blocks come through a ring of the warp's own (cp.async), every lane reading back what it copied.
-// The warps' sums meet in shared memory.
-template <int GROUPS> struct RowsRing {
-  static constexpr int kStages = GROUPS == 8 ? 2 : GROUPS == 4 ? 3 : 4;
-  static constexpr int kVectors = 4 + 2 * GROUPS;                   // 16-byte vectors of a lane in a block of 64 inputs
-  static constexpr int kBytes = kVectors * 512;
-  static constexpr int kPitch = GROUPS * 8 + 1;                     // of the sums [8 warps][8 gates, 8 ups][rows]
-  static constexpr int kSums = 8 * 2 * kRowsOut * kPitch * 4;
-  static constexpr int kTotal = 8 * kStages * kBytes > kSums ? 8 * kStages * kBytes : kSums;
-};
-template <int GROUPS>
-__global__ void __launch_bounds__(256) k_gated_rows(const RowsParams a) {
-  pdl_prologue();
-  extern __shared__ __align__(16) uint8_t rows_smem[];
-  typedef RowsRing<GROUPS> Ring;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gr = lane >> 2, tq = lane & 3;
-  const int n0 = blockIdx.x * kRowsOut, m = blockIdx.y, T = a.rows;
-  uint8_t* ring = rows_smem + warp * (Ring::kStages * Ring::kBytes) + lane * 16;
-  const bf16* w0 = a.w.p + m * a.w.member + (long long)(n0 + gr) * a.w.row;
-  const bf16* w1 = w0 + a.hidden * a.w.row;
-  const bf16* x = a.x.p + m * a.x.member + gr * a.x.row;
-  const bool in_w = n0 + gr < a.hidden;
-  auto put = [&](uint8_t* slot, const bf16* from, bool in) {
-    if (in) copy16(slot, from);
-    else *reinterpret_cast<uint4*>(slot) = make_uint4(0u, 0u, 0u, 0u);
-  };
-  auto ask = [&](int k0, int s) {
-    if (k0 < a.width) {
-      uint8_t* to = ring + s * Ring::kBytes;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int k = k0 + h * 32 + tq * 8;
-        const bool in = k < a.width;
-        put(to + h * 512, w0 + k, in && in_w);
-        put(to + (2 + h) * 512, w1 + k, in && in_w);
-#pragma unroll
-        for (int g = 0; g < GROUPS; ++g) put(to + (4 + 2 * g + h) * 512, x + g * 8 * a.x.row + k, in && g * 8 + gr < T);
-      }
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-#pragma unroll
-  for (int s = 0; s < Ring::kStages; ++s) ask(warp * 64 + s * 512, s);
-  float acc[GROUPS][4] = {};      // [0, 1]: gate, [2, 3]: up, of two rows
-  int stage = 0;
-  for (int k0 = warp * 64; k0 < a.width; k0 += 512) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(Ring::kStages - 1) : "memory");
-    const uint4* from = reinterpret_cast<const uint4*>(ring + stage * Ring::kBytes);
-    uint4 wv[2][2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) { wv[0][h] = from[h * 32]; wv[1][h] = from[(2 + h) * 32]; }
-#pragma unroll
-    for (int g = 0; g < GROUPS; ++g)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint4 xv = from[(4 + 2 * g + h) * 32];
-        mma16816(acc[g], wv[0][h].x, wv[1][h].x, wv[0][h].y, wv[1][h].y, xv.x, xv.y);
-        mma16816(acc[g], wv[0][h].z, wv[1][h].z, wv[0][h].w, wv[1][h].w, xv.z, xv.w);
-      }
-    ask(k0 + Ring::kStages * 512, stage);
-    if (++stage == Ring::kStages) stage = 0;
-  }
-  asm volatile("cp.async.wait_all;" ::: "memory");
-  __syncthreads();     // the rings' memory becomes the warps' sums
-  float* red = reinterpret_cast<float*>(rows_smem);
-#pragma unroll
-  for (int g = 0; g < GROUPS; ++g)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) red[(warp * 2 * kRowsOut + gr + 8 * (e >> 1)) * Ring::kPitch + g * 8 + tq * 2 + (e & 1)] = acc[g][e];
-  __syncthreads();
-  const int n = threadIdx.x % kRowsOut, col = n0 + n;
-  if (col >= a.hidden) return;
-  dropout::Draw d = {};
-  if (a.drop) d = dropout::draw_of(a.rule, m);
-  for (int t = threadIdx.x / kRowsOut; t < T; t += 256 / kRowsOut) {
-    float g = 0.f, u = 0.f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      g += red[(k * 2 * kRowsOut + n) * Ring::kPitch + t];
-      u += red[(k * 2 * kRowsOut + kRowsOut + n) * Ring::kPitch + t];
-    }
-    const long long row = (long long)m * T + t;
-    if (a.z) {
-      a.z[row * 2 * a.pitch + col] = g;
-      a.z[row * 2 * a.pitch + a.pitch + col] = u;
-    }
-    if (!a.h) continue;
-    float v = activation(a.activation, g) * u;
-    if (d.on) {
-      static_assert(kRowsOut == dropout::kGroup, "a CTA's hidden units are one block of the generator");
-      const U4 w = dropout::draw_group(d, (uint32_t)t * (uint32_t)gridDim.x + blockIdx.x);
-      v = dropout::kept(w, n, d.limit) ? v * d.scale : 0.f;
-    }
-    a.h[row * a.hidden + col] = __float2bfloat16_rn(v);
-  }
+__device__ __forceinline__ float4 ld_cluster(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
 }
 
-template <int GROUPS>
-cudaError_t launch_rows(const RowsParams& a, int members, cudaStream_t s) {
+template <int N>
+__global__ void __launch_bounds__(kRowsThreads, N <= 64 ? 2 : 1) k_gated_rows(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW, const RowsParams p) {
+  pdl_prologue();
+  typedef RowsTile<N> L;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBars);
+  uint64_t* empty = full + L::kStages;
+  uint64_t* done = empty + L::kStages;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int splits = (int)cluster_size(), rank = (int)cluster_ctarank();
+  const int n0 = (int)(blockIdx.x / splits) * kRowsUnits, m = blockIdx.y;
+  const int kb0 = p.k_blocks * rank / splits, kb1 = p.k_blocks * (rank + 1) / splits;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < L::kStages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+    mbar_init(done, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) tmem_alloc(tmem_slot, L::kCols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  float* sums = reinterpret_cast<float*>(smem);
+  auto give_up = [&](int where) {
+    *abort_flag = 1;
+    atomicCAS(&p.counters->status, 0, PBT_ERR_TIMEOUT);
+    p.counters->status_info = where;
+  };
+
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t stage = 0, phase = 0;
+      bool ok = true;
+      for (int kb = kb0; kb < kb1; ++kb) {
+        if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) { ok = false; break; }
+        uint8_t* to = smem + stage * L::kStage;
+        mbar_expect_tx(&full[stage], L::kStage);
+        tma_load_3d(to, &tmW, &full[stage], kb * kBK, n0, p.w_batched ? m : 0);
+        tma_load_3d(to + kRowsUnits * kBK * 2, &tmW, &full[stage], kb * kBK, p.hidden + n0, p.w_batched ? m : 0);
+        tma_load_3d(to + 2 * kRowsUnits * kBK * 2, &tmX, &full[stage], kb * kBK, 0, p.x_batched ? m : 0);
+        if (++stage == L::kStages) { stage = 0; phase ^= 1; }
+      }
+      if (!ok) give_up(41);
+      // every stage that was armed has landed before its memory is used again
+      for (int s = 0; s < L::kStages; ++s) mbar_wait_out(&full[s], s < (int)stage ? phase : phase ^ 1);
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+      uint32_t stage = 0, phase = 0;
+      bool ok = true;
+      for (int kb = kb0; kb < kb1; ++kb) {
+        if (!mbar_wait(&full[stage], phase, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t sa = smem_u32(smem + stage * L::kStage), sb = sa + 2 * kRowsUnits * kBK * 2;
+#pragma unroll
+        for (int k = 0; k < kBK / 16; ++k)
+          umma_bf16(tmem, smem_desc(sa + k * 32, 16, 1024), smem_desc(sb + k * 32, 16, 1024), idesc, (kb > kb0 || k > 0) ? 1u : 0u);
+        umma_commit(&empty[stage]);
+        if (++stage == L::kStages) { stage = 0; phase ^= 1; }
+      }
+      if (!ok) give_up(42);
+      umma_commit(done);          // (also where a wait ran out: no instruction reads shared memory any more)
+      mbar_wait_out(done, 0);
+      tc_fence_before();
+    }
+  }
+  __syncthreads();                // all loads have landed and all products are complete: the ring's memory becomes the sums
+  const bool ok = *abort_flag == 0;
+  if (warp >= 2 && ok) {
+    tc_fence_after();
+    const int q = warp & 3;
+    constexpr int kCols = N < 32 ? N : 32;
+#pragma unroll 1
+    for (int c0 = 0; c0 < N && c0 < p.rows; c0 += kCols) {
+      uint32_t v[kCols];
+      tmem_ld_cols<kCols>(tmem + ((uint32_t)(q * 32) << 16) + c0, v);
+      tmem_ld_wait();
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) sums[(c0 + c) * kRowsPitch + q * 32 + lane] = __uint_as_float(v[c]);
+    }
+    tc_fence_before();
+  }
+  cluster_sync_all();
+  // a thread has eight hidden units of a row
+  for (int i = threadIdx.x; i < N / splits * (kRowsUnits / 8); i += kRowsThreads) {
+    const int t = rank * (N / splits) + i / (kRowsUnits / 8), j = i % (kRowsUnits / 8) * 8, col = n0 + j;
+    if (!ok || t >= p.rows || col >= p.hidden) continue;
+    float g[8] = {}, u[8] = {};
+    const uint32_t at = smem_u32(sums + t * kRowsPitch + j);
+    for (int s = 0; s < splits; ++s) {
+      const uint32_t from = map_to_cta(at, s);
+#pragma unroll
+      for (int e = 0; e < 8; e += 4) {
+        const float4 a = ld_cluster(from + e * 4), b = ld_cluster(from + (kRowsUnits + e) * 4);
+        g[e] += a.x; g[e + 1] += a.y; g[e + 2] += a.z; g[e + 3] += a.w;
+        u[e] += b.x; u[e + 1] += b.y; u[e + 2] += b.z; u[e + 3] += b.w;
+      }
+    }
+    const long long row = (long long)m * p.rows + t;
+    if (p.z) {                    // (whole groups: the pitch is a multiple of eight)
+      float* z = p.z + row * 2 * p.pitch + col;
+      store8(z, {g[0], g[1], g[2], g[3], g[4], g[5], g[6], g[7]});
+      store8(z + p.pitch, {u[0], u[1], u[2], u[3], u[4], u[5], u[6], u[7]});
+    }
+    if (!p.h) continue;
+    Eight v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v.v[e] = activation(p.activation, g[e]) * u[e];
+    if (p.drop) {
+      const dropout::Draw d = dropout::draw_of(p.rule, m);
+      const uint32_t in = dropout::kept_bits(d, (uint32_t)t * (uint32_t)((p.hidden + 7) / 8) + (uint32_t)(col / 8));
+      const float f = d.on ? d.scale : 1.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v.v[e] = (in >> e & 1u) ? v.v[e] * f : 0.f;
+    }
+    bf16* h = p.h + row * p.hidden + col;
+    if (p.vec) {
+      store8(h, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (col + e < p.hidden) h[e] = __float2bfloat16_rn(v.v[e]);
+    }
+  }
+  cluster_sync_all();             // no CTA leaves while another reads its sums
+  if (warp == 1) tmem_dealloc(tmem, L::kCols);
+}
+
+template <int N>
+cudaError_t launch_rows(const pbt_gated_desc* d, const RowsParams& p, const CUtensorMap& tmX, const CUtensorMap& tmW, int splits, cudaStream_t s) {
   static DeviceSetup setup;
   int sms = 0;
-  const cudaError_t e = device_setup(&setup, k_gated_rows<GROUPS>, RowsRing<GROUPS>::kTotal, &sms);
+  const cudaError_t e = device_setup(&setup, k_gated_rows<N>, RowsTile<N>::kTotal, &sms);
   if (e != cudaSuccess) return e;
-  return launch_with(dim3((a.hidden + kRowsOut - 1) / kRowsOut, members), 256, RowsRing<GROUPS>::kTotal, s)(k_gated_rows<GROUPS>, a);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((d->hidden + kRowsUnits - 1) / kRowsUnits * splits), (unsigned)d->members);
+  cfg.blockDim = dim3(kRowsThreads);
+  cfg.dynamicSmemBytes = RowsTile<N>::kTotal;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)splits;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k_gated_rows<N>, tmX, tmW, p);
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -500,17 +564,37 @@ cudaError_t tc_pack(const PackSource* src, int n, cudaStream_t s) {
   return launch_with((unsigned)blocks, 256, 0, s)(k_gated_pack, a);
 }
 
-cudaError_t tc_rows_forward(const pbt_gated_desc* d, const Operand& x, const Operand& w, void* h, float* z, int pitch, cudaStream_t s) {
-  RowsParams a = {x, w, d->rows, d->hidden, (d->width + 7) / 8 * 8, d->activation, d->drop != nullptr, (bf16*)h, z, pitch, {}};
-  if (d->drop) a.rule = *d->drop;
-  if (d->rows <= 8) return launch_rows<1>(a, d->members, s);
-  if (d->rows <= 16) return launch_rows<2>(a, d->members, s);
-  if (d->rows <= 32) return launch_rows<4>(a, d->members, s);
-  return launch_rows<8>(a, d->members, s);
+static cudaError_t rows_forward(const pbt_gated_desc* d, const Operand& x, const Operand& w, void* h, float* z, int pitch, cudaStream_t s) {
+  RowsParams p = {};
+  p.rows = d->rows; p.hidden = d->hidden;
+  p.k_blocks = (d->width + kBK - 1) / kBK;
+  p.x_batched = d->members > 1 && x.member != 0;
+  p.w_batched = d->members > 1 && w.member != 0;
+  p.activation = d->activation;
+  p.drop = d->drop != nullptr;
+  if (d->drop) p.rule = *d->drop;
+  p.vec = d->hidden % 8 == 0 && ((uintptr_t)h & 15) == 0;
+  p.h = (bf16*)h; p.z = z; p.pitch = pitch;
+  p.counters = (Counters*)d->status_device;
+  const int n = d->rows <= 16 ? 16 : d->rows <= 32 ? 32 : d->rows <= 64 ? 64 : 128;
+  CUtensorMap tmX, tmW;
+  if (!make_map(&tmX, x.p, d->width, d->rows, x.row, p.x_batched ? d->members : 1, x.member, n) ||
+      !make_map(&tmW, w.p, d->width, 2ll * d->hidden, w.row, p.w_batched ? d->members : 1, w.member, kRowsUnits))
+    return cudaErrorInvalidValue;
+  // as many parts of the contraction as there are SMs to spare for, four blocks of it each at least
+  const long long tiles = (long long)((d->hidden + kRowsUnits - 1) / kRowsUnits) * d->members, room = n <= 64 ? 296 : 148;
+  int splits = 1;
+  while (splits < kRowsSplits && tiles * splits * 2 <= room && p.k_blocks >= splits * 2 * 4) splits *= 2;
+  switch (n) {
+    case 16: return launch_rows<16>(d, p, tmX, tmW, splits, s);
+    case 32: return launch_rows<32>(d, p, tmX, tmW, splits, s);
+    case 64: return launch_rows<64>(d, p, tmX, tmW, splits, s);
+    default: return launch_rows<128>(d, p, tmX, tmW, splits, s);
+  }
 }
 
 cudaError_t tc_forward(const pbt_gated_desc* d, const Operand& x, const Operand& w, void* h, float* z, int pitch, cudaStream_t s) {
-  if (tc_few_rows(d)) return tc_rows_forward(d, x, w, h, z, pitch, s);
+  if (d->rows <= kRowsMost) return rows_forward(d, x, w, h, z, pitch, s);
   TileParams p;
   memset(&p, 0, sizeof(p));
   p.rows = d->rows; p.hidden = d->hidden;
