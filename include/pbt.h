@@ -650,7 +650,7 @@ typedef struct pbt_gated_desc {
   void* status_device;
 } pbt_gated_desc;
 /* Bytes of device workspace (256-byte aligned base) of one forward (backward == 0) or backward call of this description, its pointers
- * (kept or not, alignment) and strides included. */
+ * (kept or not, alignment) and strides included; 0: workspace may be NULL. */
 int pbt_gated_query_workspace(const pbt_gated_desc* desc, int backward, size_t* bytes);
 int pbt_gated_forward(const pbt_gated_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
 int pbt_gated_backward(const pbt_gated_desc* desc, void* workspace, size_t workspace_bytes, void* stream);

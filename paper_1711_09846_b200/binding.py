@@ -120,7 +120,7 @@ class PbtGatedDesc(C.Structure):
     _fields_ = [("members", C.c_int32), ("rows", C.c_int32), ("width", C.c_int32), ("hidden", C.c_int32), ("dtype", C.c_int32), ("activation", C.c_int32),
                 ("x", C.c_void_p), ("x_member", C.c_int64), ("x_row", C.c_int64),
                 ("weight", C.c_void_p), ("weight_member", C.c_int64), ("weight_row", C.c_int64),
-                ("drop", C.POINTER(PbtDropRule)), ("h", C.c_void_p), ("kept", C.c_void_p),
+                ("drop", C.c_void_p), ("h", C.c_void_p), ("kept", C.c_void_p),
                 ("dh", C.c_void_p), ("dh_member", C.c_int64), ("dh_row", C.c_int64),
                 ("dx", C.c_void_p), ("dweight", C.c_void_p), ("status_device", C.c_void_p)]
 

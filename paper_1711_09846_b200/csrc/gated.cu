@@ -3,6 +3,8 @@
 //
 // The products run in the framework's member-batched GEMMs; g and u stay in fp32 between the two (as bf16 they would add their
 // own rounding to that of h and of every gradient).
+#include <algorithm>
+
 #include "gated.cuh"
 
 namespace pbt {
@@ -118,7 +120,6 @@ Plan plan_of(const pbt_gated_desc* d, bool backward) {
     if (p.pack_x) p.x = take(rows * width * size);
     if (p.pack_w) p.w = take((d->weight_member ? d->members : 1) * 2 * (size_t)d->hidden * width * size);
   }
-  if (!p.bytes) p.bytes = 256;
   return p;
 }
 
@@ -202,10 +203,18 @@ cudaError_t forward(const pbt_gated_desc* d, char* ws, cudaStream_t s) {
   return launch_cells<float, false>(d, a, s);
 }
 
-// the faster of the tensor-core products, which take rows of any number here: tensor maps fill what is missing with zeros
+// The faster of the tensor-core products, which take any number of rows here: tensor maps fill what is missing with zeros.  In waves of 128 x 256 (a pair:
+// 256 x 256) tiles; launch_gemm_tc halves its tiles where that shortens the last wave.  A pair's cost less from contractions of 384 on (40 members,
+// 512 rows, 1024 -> 1024: dW 10 us less, 8 x 160, 2048 -> 2048: 4 us more).
 cudaError_t run_product(const pbt_gated_desc* d, const GemmArgs& g, cudaStream_t s) {
   if (!d->dtype) return launch_gemm_simt(g, s);
-  return gemm_tc_pair_preferred(g) ? launch_gemm_tc_pair(g, (Counters*)d->status_device, s) : launch_gemm_tc(g, (Counters*)d->status_device, s);
+  auto waves = [&](int rows, int cols, int at_once) {
+    const long long tiles = (long long)((g.M + rows - 1) / rows) * ((g.N + cols - 1) / cols) * g.batch;
+    return (double)((tiles + at_once - 1) / at_once);
+  };
+  const double pair = (g.K >= 384 ? 0.95 : 1.03) * waves(256, 256, 74), single = std::min(waves(128, 256, 148), 0.575 * waves(128, 128, 148));
+  Counters* counters = (Counters*)d->status_device;
+  return g.M >= 256 && g.N >= 256 && pair < single ? launch_gemm_tc_pair(g, counters, s) : launch_gemm_tc(g, counters, s);
 }
 
 template <typename T>
@@ -235,7 +244,8 @@ cudaError_t backward(const pbt_gated_desc* d, char* ws, cudaStream_t s) {
   g.ldb = d->dtype ? o.w.row : d->weight_row;
   g.strideB = d->dtype ? o.w.member : d->weight_member;
   g.C = d->dx; g.ldc = d->width; g.strideC = (long long)d->rows * d->width;
-  e = run_product(d, g, s);
+  if (d->dtype && tc_dx_few(d)) e = tc_dx(d, {(const bf16*)dz, p.dz_pitch, (long long)d->rows * p.dz_pitch}, o.w, s);
+  else e = run_product(d, g, s);
   if (e != cudaSuccess) return e;
   g.a_mn = 1;
   g.M = 2 * d->hidden; g.K = d->rows;
@@ -243,6 +253,7 @@ cudaError_t backward(const pbt_gated_desc* d, char* ws, cudaStream_t s) {
   g.ldb = d->dtype ? o.x.row : d->x_row;
   g.strideB = d->dtype ? o.x.member : d->x_member;
   g.C = d->dweight; g.strideC = 2ll * d->hidden * d->width;
+  if (d->dtype && tc_outer_supported(d)) return tc_outer(d, (const bf16*)dz, p.dz_pitch, o.x, s);
   return run_product(d, g, s);
 }
 
@@ -265,7 +276,8 @@ int check(const pbt_gated_desc* d) {
 }
 
 int check_workspace(const pbt_gated_desc* d, bool backward, const void* workspace, size_t bytes) {
-  if (workspace && ((uintptr_t)workspace & 255) == 0 && bytes >= plan_of(d, backward).bytes) return PBT_OK;
+  const size_t need = plan_of(d, backward).bytes;
+  if (!need || (workspace && ((uintptr_t)workspace & 255) == 0 && bytes >= need)) return PBT_OK;
   return fail(PBT_ERR_WORKSPACE, "workspace missing, not 256-byte aligned or smaller than pbt_gated_query_workspace says");
 }
 

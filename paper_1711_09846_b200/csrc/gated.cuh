@@ -21,6 +21,12 @@ struct PackSource {
 };
 cudaError_t tc_pack(const PackSource* src, int n, cudaStream_t s);      // one or two
 cudaError_t tc_forward(const pbt_gated_desc* d, const Operand& x, const Operand& w, void* h, float* z, int pitch, cudaStream_t s);
+// dx = [dg du] W by CTAs that share a contraction, for few rows
+bool tc_dx_few(const pbt_gated_desc* d);
+cudaError_t tc_dx(const pbt_gated_desc* d, const Operand& dz, const Operand& w, cudaStream_t s);
+// dW of a few rows
+bool tc_outer_supported(const pbt_gated_desc* d);
+cudaError_t tc_outer(const pbt_gated_desc* d, const bf16* dz, int dz_pitch, const Operand& x, cudaStream_t s);
 
 #ifdef __CUDACC__
 // act(g)

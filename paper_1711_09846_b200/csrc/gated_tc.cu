@@ -326,20 +326,24 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_gated_tc(const __grid_constan
 // ------------------------------------------------------------------------------------------------------------------
 // Few rows
 // ------------------------------------------------------------------------------------------------------------------
-// Up to 128 rows a member: bound by reading the weight once, so the weight is the tall operand.  A CTA has 64 hidden units, whose gate and up rows
-// are the 128 lanes of the accumulator, and all rows of x as its N columns; a cluster of `splits` CTAs shares the contraction.  The partial sums meet
-// in shared memory, where every CTA of the cluster adds up its own share of the rows over all CTAs' partial sums (in their order), and g and u
-// of a hidden unit meet, too.
-constexpr int kRowsUnits = 64, kRowsPitch = 2 * kRowsUnits + 4;      // floats of a row's partial sums: 64 g, 64 u
-constexpr int kRowsMost = 128;
+// Bound by reading the weight once, so the weight is the tall operand and up to 128 rows are the N columns of the accumulator; clusters of CTAs share a
+// contraction.  Two products take this form:
+//   forward   128 lanes: 64 hidden units' gate and up rows of the weight; N columns: rows of x
+//   dx        128 lanes: columns of the weight, read as it lies (its rows are the contraction: MN-major); N columns: rows of [dg du]
+// The partial sums of a cluster meet in shared memory, where every CTA adds up its own share of the rows over all CTAs' partial sums (in their
+// order); there g and u of a hidden unit meet, too.
+// Rows up to which the forward pass takes this form (32 rows, 2048 -> 4096: 12 us, in tiles 15; 50 rows of 8 members, 1024 -> 1024: 12.3 and 10.8).
+constexpr int kRowsForward = 32;
+constexpr int kRowsLanes = 128, kRowsPitch = kRowsLanes + 4;      // floats of a row's partial sums
 constexpr int kRowsThreads = 192;
 constexpr int kRowsSplits = 8;
 
 struct RowsParams {
-  int rows, hidden, k_blocks;
-  int x_batched, w_batched;
+  int rows, blocks;               // blocks of N rows of a member
+  int hidden, width, k_blocks;
+  int a_batched, b_batched;
   int activation, drop, vec;
-  bf16* h;                        // or null
+  bf16* out;                      // h (or null), dx
   float* z; int pitch;            // or null
   pbt_drop_rule rule;
   Counters* counters;
@@ -347,7 +351,8 @@ struct RowsParams {
 template <int N>
 struct RowsTile {
   static constexpr int kStage = (128 + N) * kBK * 2;
-  static constexpr int kStages = N <= 32 ? 5 : N == 64 ? 4 : 6;          // two CTAs of an SM share its memory, one with 128 rows
+  static constexpr int kStages = 3;
+  static constexpr int kPerSm = N == 16 ? 4 : N <= 64 ? 3 : 2;          // CTAs that share an SM: one's set-up and end beside another's loads
   static constexpr int kSums = N * kRowsPitch * 4;
   static constexpr int kBars = kStages * kStage > kSums ? kStages * kStage : (kSums + 255) / 256 * 256;
   static constexpr int kTotal = kBars + 256 + 1024;
@@ -361,10 +366,11 @@ __device__ __forceinline__ float4 ld_cluster(uint32_t addr) {
   return v;
 }
 
-template <int N>
-__global__ void __launch_bounds__(kRowsThreads, N <= 64 ? 2 : 1) k_gated_rows(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW, const RowsParams p) {
+template <int N, bool DX>
+__global__ void __launch_bounds__(kRowsThreads, RowsTile<N>::kPerSm) k_gated_rows(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const RowsParams p) {
   pdl_prologue();
   typedef RowsTile<N> L;
+  constexpr int kUnits = DX ? kRowsLanes : kRowsLanes / 2;       // hidden units, or columns of dx
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBars);
@@ -374,8 +380,8 @@ __global__ void __launch_bounds__(kRowsThreads, N <= 64 ? 2 : 1) k_gated_rows(co
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int splits = (int)cluster_size(), rank = (int)cluster_ctarank();
-  const int n0 = (int)(blockIdx.x / splits) * kRowsUnits, m = blockIdx.y;
-  const int kb0 = p.k_blocks * rank / splits, kb1 = p.k_blocks * (rank + 1) / splits;
+  const int n0 = (int)(blockIdx.x / splits) * kUnits, m = blockIdx.y / p.blocks, t0 = (int)(blockIdx.y % p.blocks) * N;
+  const int kb0 = (int)((long long)p.k_blocks * rank / splits), kb1 = (int)((long long)p.k_blocks * (rank + 1) / splits);
   if (threadIdx.x == 0) {
     for (int s = 0; s < L::kStages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
     mbar_init(done, 1);
@@ -403,9 +409,13 @@ __global__ void __launch_bounds__(kRowsThreads, N <= 64 ? 2 : 1) k_gated_rows(co
         if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) { ok = false; break; }
         uint8_t* to = smem + stage * L::kStage;
         mbar_expect_tx(&full[stage], L::kStage);
-        tma_load_3d(to, &tmW, &full[stage], kb * kBK, n0, p.w_batched ? m : 0);
-        tma_load_3d(to + kRowsUnits * kBK * 2, &tmW, &full[stage], kb * kBK, p.hidden + n0, p.w_batched ? m : 0);
-        tma_load_3d(to + 2 * kRowsUnits * kBK * 2, &tmX, &full[stage], kb * kBK, 0, p.x_batched ? m : 0);
+        const int k0 = kb * kBK, ma = p.a_batched ? m : 0;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          if (DX) tma_load_3d(to + half * 8192, &tmA, &full[stage], n0 + half * 64, k0, ma);
+          else tma_load_3d(to + half * 8192, &tmA, &full[stage], k0, half * p.hidden + n0, ma);
+        }
+        tma_load_3d(to + 16384, &tmB, &full[stage], k0, t0, p.b_batched ? m : 0);
         if (++stage == L::kStages) { stage = 0; phase ^= 1; }
       }
       if (!ok) give_up(41);
@@ -414,16 +424,16 @@ __global__ void __launch_bounds__(kRowsThreads, N <= 64 ? 2 : 1) k_gated_rows(co
     }
   } else if (warp == 1) {
     if (lane == 0) {
-      const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+      const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)DX << 15) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(kRowsLanes >> 4) << 24);
       uint32_t stage = 0, phase = 0;
       bool ok = true;
       for (int kb = kb0; kb < kb1; ++kb) {
         if (!mbar_wait(&full[stage], phase, abort_flag)) { ok = false; break; }
         tc_fence_after();
-        const uint32_t sa = smem_u32(smem + stage * L::kStage), sb = sa + 2 * kRowsUnits * kBK * 2;
+        const uint32_t sa = smem_u32(smem + stage * L::kStage), sb = sa + 16384;
 #pragma unroll
         for (int k = 0; k < kBK / 16; ++k)
-          umma_bf16(tmem, smem_desc(sa + k * 32, 16, 1024), smem_desc(sb + k * 32, 16, 1024), idesc, (kb > kb0 || k > 0) ? 1u : 0u);
+          umma_bf16(tmem, DX ? smem_desc(sa + k * 2048, 8192, 1024) : smem_desc(sa + k * 32, 16, 1024), smem_desc(sb + k * 32, 16, 1024), idesc, (kb > kb0 || k > 0) ? 1u : 0u);
         umma_commit(&empty[stage]);
         if (++stage == L::kStages) { stage = 0; phase ^= 1; }
       }
@@ -440,7 +450,7 @@ __global__ void __launch_bounds__(kRowsThreads, N <= 64 ? 2 : 1) k_gated_rows(co
     const int q = warp & 3;
     constexpr int kCols = N < 32 ? N : 32;
 #pragma unroll 1
-    for (int c0 = 0; c0 < N && c0 < p.rows; c0 += kCols) {
+    for (int c0 = 0; c0 < N && t0 + c0 < p.rows; c0 += kCols) {
       uint32_t v[kCols];
       tmem_ld_cols<kCols>(tmem + ((uint32_t)(q * 32) << 16) + c0, v);
       tmem_ld_wait();
@@ -450,59 +460,71 @@ __global__ void __launch_bounds__(kRowsThreads, N <= 64 ? 2 : 1) k_gated_rows(co
     tc_fence_before();
   }
   cluster_sync_all();
-  // a thread has eight hidden units of a row
-  for (int i = threadIdx.x; i < N / splits * (kRowsUnits / 8); i += kRowsThreads) {
-    const int t = rank * (N / splits) + i / (kRowsUnits / 8), j = i % (kRowsUnits / 8) * 8, col = n0 + j;
-    if (!ok || t >= p.rows || col >= p.hidden) continue;
-    float g[8] = {}, u[8] = {};
-    const uint32_t at = smem_u32(sums + t * kRowsPitch + j);
+  // a thread has eight hidden units (columns) of a row
+  for (int i = threadIdx.x; i < N / splits * (kUnits / 8); i += kRowsThreads) {
+    const int c = rank * (N / splits) + i / (kUnits / 8), t = t0 + c, j = i % (kUnits / 8) * 8, col = n0 + j, end = DX ? p.width : p.hidden;
+    if (!ok || t >= p.rows || col >= end) continue;
+    Eight g = {}, u = {};
+    const uint32_t at = smem_u32(sums + c * kRowsPitch + j);
     for (int s = 0; s < splits; ++s) {
       const uint32_t from = map_to_cta(at, s);
 #pragma unroll
       for (int e = 0; e < 8; e += 4) {
-        const float4 a = ld_cluster(from + e * 4), b = ld_cluster(from + (kRowsUnits + e) * 4);
-        g[e] += a.x; g[e + 1] += a.y; g[e + 2] += a.z; g[e + 3] += a.w;
-        u[e] += b.x; u[e + 1] += b.y; u[e + 2] += b.z; u[e + 3] += b.w;
+        const float4 a = ld_cluster(from + e * 4);
+        g.v[e] += a.x; g.v[e + 1] += a.y; g.v[e + 2] += a.z; g.v[e + 3] += a.w;
+        if (!DX) {
+          const float4 b = ld_cluster(from + (kUnits + e) * 4);
+          u.v[e] += b.x; u.v[e + 1] += b.y; u.v[e + 2] += b.z; u.v[e + 3] += b.w;
+        }
       }
     }
     const long long row = (long long)m * p.rows + t;
-    if (p.z) {                    // (whole groups: the pitch is a multiple of eight)
-      float* z = p.z + row * 2 * p.pitch + col;
-      store8(z, {g[0], g[1], g[2], g[3], g[4], g[5], g[6], g[7]});
-      store8(z + p.pitch, {u[0], u[1], u[2], u[3], u[4], u[5], u[6], u[7]});
-    }
-    if (!p.h) continue;
-    Eight v;
+    if (!DX) {
+      if (p.z) {                  // (whole groups: the pitch is a multiple of eight)
+        float* z = p.z + row * 2 * p.pitch + col;
+        store8(z, g);
+        store8(z + p.pitch, u);
+      }
+      if (!p.out) continue;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v.v[e] = activation(p.activation, g[e]) * u[e];
-    if (p.drop) {
-      const dropout::Draw d = dropout::draw_of(p.rule, m);
-      const uint32_t in = dropout::kept_bits(d, (uint32_t)t * (uint32_t)((p.hidden + 7) / 8) + (uint32_t)(col / 8));
-      const float f = d.on ? d.scale : 1.f;
+      for (int e = 0; e < 8; ++e) g.v[e] = activation(p.activation, g.v[e]) * u.v[e];
+      if (p.drop) {
+        const dropout::Draw d = dropout::draw_of(p.rule, m);
+        const uint32_t in = dropout::kept_bits(d, (uint32_t)t * (uint32_t)((p.hidden + 7) / 8) + (uint32_t)(col / 8));
+        const float f = d.on ? d.scale : 1.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v.v[e] = (in >> e & 1u) ? v.v[e] * f : 0.f;
+        for (int e = 0; e < 8; ++e) g.v[e] = (in >> e & 1u) ? g.v[e] * f : 0.f;
+      }
     }
-    bf16* h = p.h + row * p.hidden + col;
+    bf16* out = p.out + row * end + col;
     if (p.vec) {
-      store8(h, v);
+      store8(out, g);
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (col + e < p.hidden) h[e] = __float2bfloat16_rn(v.v[e]);
+        if (col + e < end) out[e] = __float2bfloat16_rn(g.v[e]);
     }
   }
   cluster_sync_all();             // no CTA leaves while another reads its sums
   if (warp == 1) tmem_dealloc(tmem, L::kCols);
 }
 
-template <int N>
-cudaError_t launch_rows(const pbt_gated_desc* d, const RowsParams& p, const CUtensorMap& tmX, const CUtensorMap& tmW, int splits, cudaStream_t s) {
+// the parts of a contraction: as many as there are places for CTAs, four blocks each at least
+int rows_splits(long long tiles, int k_blocks, long long places) {
+  int splits = 1;
+  while (splits < kRowsSplits && tiles * splits * 2 <= places && k_blocks >= splits * 2 * 4) splits *= 2;
+  return splits;
+}
+template <int N, bool DX>
+cudaError_t launch_rows(const pbt_gated_desc* d, const RowsParams& p, const CUtensorMap& tmA, const CUtensorMap& tmB, cudaStream_t s) {
   static DeviceSetup setup;
   int sms = 0;
-  const cudaError_t e = device_setup(&setup, k_gated_rows<N>, RowsTile<N>::kTotal, &sms);
+  const cudaError_t e = device_setup(&setup, k_gated_rows<N, DX>, RowsTile<N>::kTotal, &sms);
   if (e != cudaSuccess) return e;
+  const unsigned units = DX ? (d->width + 127) / 128 : (d->hidden + 63) / 64, blocks = (unsigned)p.blocks * d->members;
+  const int splits = rows_splits((long long)units * blocks, p.k_blocks, (long long)sms * RowsTile<N>::kPerSm);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((d->hidden + kRowsUnits - 1) / kRowsUnits * splits), (unsigned)d->members);
+  cfg.gridDim = dim3(units * splits, blocks);
   cfg.blockDim = dim3(kRowsThreads);
   cfg.dynamicSmemBytes = RowsTile<N>::kTotal;
   cfg.stream = s;
@@ -512,7 +534,105 @@ cudaError_t launch_rows(const pbt_gated_desc* d, const RowsParams& p, const CUte
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k_gated_rows<N>, tmX, tmW, p);
+  return cudaLaunchKernelEx(&cfg, k_gated_rows<N, DX>, tmA, tmB, p);
+}
+template <bool DX>
+cudaError_t launch_rows(const pbt_gated_desc* d, RowsParams& p, const CUtensorMap& tmA, const Operand& b, int k, cudaStream_t s) {
+  const int n = d->rows <= 16 ? 16 : d->rows <= 32 ? 32 : d->rows <= 64 ? 64 : 128;
+  p.rows = d->rows; p.hidden = d->hidden; p.width = d->width;
+  p.blocks = (d->rows + n - 1) / n;
+  p.k_blocks = (k + kBK - 1) / kBK;
+  p.b_batched = d->members > 1 && b.member != 0;
+  p.vec = (DX ? d->width : d->hidden) % 8 == 0 && ((uintptr_t)p.out & 15) == 0;
+  p.counters = (Counters*)d->status_device;
+  CUtensorMap tmB;
+  if (!make_map(&tmB, b.p, k, d->rows, b.row, p.b_batched ? d->members : 1, b.member, n)) return cudaErrorInvalidValue;
+  switch (n) {
+    case 16: return launch_rows<16, DX>(d, p, tmA, tmB, s);
+    case 32: return launch_rows<32, DX>(d, p, tmA, tmB, s);
+    case 64: return launch_rows<64, DX>(d, p, tmA, tmB, s);
+    default: return launch_rows<128, DX>(d, p, tmA, tmB, s);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// dW of a few rows
+// ------------------------------------------------------------------------------------------------------------------
+// dW = [dg du]^T x with a contraction over at most 32 rows is bound by writing dW (72 members, one row, 344 -> 736: a whole backward pass 40 us, by the
+// plain product 94).  A CTA writes 128 x 128 elements: a warp has 16 rows of them, one or
+// two mma.sync steps each, and sends them through shared memory as whole 16-byte vectors.
+constexpr int kOuterMost = 32, kOuterTile = 128, kOuterHalf = 64, kOuterPitch = kOuterTile + 8;      // (a pitch of 17 x 16 bytes: ldmatrix without conflicts)
+struct OuterParams {
+  const bf16* dz; int dz_pitch;
+  Operand x;
+  bf16* dw;
+  int rows, hidden2, width, vec;
+};
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t* r, uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma16816(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <int STEPS>
+__global__ void __launch_bounds__(256) k_gated_outer(const OuterParams p) {
+  pdl_prologue();
+  __shared__ __align__(16) bf16 sd[STEPS * 16][kOuterPitch], sx[STEPS * 16][kOuterPitch];
+  __shared__ __align__(16) bf16 out[8][16][kOuterHalf + 8];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int c0 = blockIdx.x * kOuterTile, n0 = blockIdx.y * kOuterTile, m = blockIdx.z;
+  const bf16* dz = p.dz + (long long)m * p.rows * p.dz_pitch + n0;
+  const bf16* x = p.x.p + m * p.x.member + c0;
+#pragma unroll
+  for (int i = threadIdx.x; i < STEPS * 16 * (kOuterTile / 8); i += 256) {
+    const int t = i / (kOuterTile / 8), c = i % (kOuterTile / 8) * 8;
+    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+    // (a row's last vector may end behind its last element, inside the same 16 bytes: those columns are not written)
+    *reinterpret_cast<uint4*>(&sd[t][c]) = t < p.rows && n0 + c < p.hidden2 ? __ldg(reinterpret_cast<const uint4*>(dz + (long long)t * p.dz_pitch + c)) : none;
+    *reinterpret_cast<uint4*>(&sx[t][c]) = t < p.rows && c0 + c < p.width ? __ldg(reinterpret_cast<const uint4*>(x + t * p.x.row + c)) : none;
+  }
+  __syncthreads();
+  const int q = lane >> 3, r = lane & 7, gr = lane >> 2, tq = lane & 3;
+  uint32_t a[STEPS][4];
+#pragma unroll
+  for (int k = 0; k < STEPS; ++k) ldmatrix4_trans(a[k], smem_u32(&sd[k * 16 + (q >> 1) * 8 + r][warp * 16 + (q & 1) * 8]));
+  const int rows = min(16, p.hidden2 - n0 - warp * 16);
+  bf16* dw = p.dw + ((long long)m * p.hidden2 + n0 + warp * 16) * p.width + c0;
+#pragma unroll
+  for (int h = 0; h < kOuterTile; h += kOuterHalf) {
+#pragma unroll
+    for (int c = 0; c < kOuterHalf; c += 16) {
+      float acc[2][4] = {};
+#pragma unroll
+      for (int k = 0; k < STEPS; ++k) {
+        uint32_t b[4];
+        ldmatrix4_trans(b, smem_u32(&sx[k * 16 + (q & 1) * 8 + r][h + c + (q >> 1) * 8]));
+        mma16816(acc[0], a[k], b[0], b[1]);
+        mma16816(acc[1], a[k], b[2], b[3]);
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        *reinterpret_cast<__nv_bfloat162*>(&out[warp][gr][c + j * 8 + tq * 2]) = __floats2bfloat162_rn(acc[j][0], acc[j][1]);
+        *reinterpret_cast<__nv_bfloat162*>(&out[warp][gr + 8][c + j * 8 + tq * 2]) = __floats2bfloat162_rn(acc[j][2], acc[j][3]);
+      }
+    }
+    __syncwarp();
+    if (p.vec) {
+#pragma unroll
+      for (int i = lane; i < 16 * (kOuterHalf / 8); i += 32) {
+        const int row = i / (kOuterHalf / 8), c = i % (kOuterHalf / 8) * 8;
+        if (row < rows && c0 + h + c < p.width)
+          *reinterpret_cast<uint4*>(dw + (long long)row * p.width + h + c) = *reinterpret_cast<const uint4*>(&out[warp][row][c]);
+      }
+    } else {
+      for (int row = 0; row < rows; ++row)
+#pragma unroll
+        for (int c = lane; c < kOuterHalf; c += 32)
+          if (c0 + h + c < p.width) dw[(long long)row * p.width + h + c] = out[warp][row][c];
+    }
+    __syncwarp();
+  }
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -524,23 +644,51 @@ struct PackJob {
   int members, rows, cols, to;    // elements of a row, and rounded up to 8
   unsigned block0;                // its first block
 };
+constexpr int kPackEach = 4;      // vectors of a thread
 struct PackJobs {
   PackJob job[2];
   int n;
 };
 __global__ void __launch_bounds__(256) k_gated_pack(const PackJobs a) {
   pdl_prologue();
-  const PackJob& j = a.job[a.n > 1 && blockIdx.x >= a.job[1].block0];
-  const long long i = (long long)(blockIdx.x - j.block0) * 256 + threadIdx.x;
-  const int per_row = j.to / 8;
-  const long long at = i / per_row;
-  if (at >= (long long)j.members * j.rows) return;
-  const int c = (int)(i - at * per_row) * 8, m = (int)(at / j.rows);
-  const bf16* from = j.src + m * j.member + (at - (long long)m * j.rows) * j.row + c;
-  __align__(16) bf16 v[8];
+  const bool second = a.n > 1 && blockIdx.x >= a.job[1].block0;
+  const PackJob j = second ? a.job[1] : a.job[0];
+  const long long first = (long long)(blockIdx.x - j.block0) * (256 * kPackEach) + threadIdx.x, rows = (long long)j.members * j.rows;
+  const uint32_t per_row = j.to / 8;
+  uint4 a0[kPackEach], a1[kPackEach];
+  int off[kPackEach], n[kPackEach];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = c + e < j.cols ? from[e] : __float2bfloat16_rn(0.f);
-  *reinterpret_cast<uint4*>(j.dst + at * j.to + c) = *reinterpret_cast<const uint4*>(v);
+  for (int u = 0; u < kPackEach; ++u) {
+    const long long i = first + u * 256;
+    n[u] = 0;
+    if (i >= rows * per_row) continue;
+    // (a 64-bit division costs more than the rest)
+    const long long at = i <= 0xFFFFFFFFll ? (uint32_t)i / per_row : i / per_row;
+    const int c = (int)(i - at * per_row) * 8, m = (int)(at <= 0xFFFFFFFFll ? (uint32_t)at / (uint32_t)j.rows : at / j.rows);
+    // the 16-byte pieces that hold the eight elements, the second one only if an element of the row lies in it
+    const uintptr_t addr = (uintptr_t)(j.src + m * j.member + (at - (long long)m * j.rows) * j.row + c);
+    const uint4* piece = reinterpret_cast<const uint4*>(addr & ~(uintptr_t)15);
+    off[u] = (int)(addr & 15) / 2;
+    n[u] = min(8, j.cols - c);
+    a0[u] = __ldg(piece);
+    a1[u] = off[u] + n[u] > 8 ? __ldg(piece + 1) : make_uint4(0u, 0u, 0u, 0u);
+  }
+#pragma unroll
+  for (int u = 0; u < kPackEach; ++u) {
+    if (!n[u]) continue;
+    const uint32_t w[8] = {a0[u].x, a0[u].y, a0[u].z, a0[u].w, a1[u].x, a1[u].y, a1[u].z, a1[u].w};      // (off + 7 < 16)
+    const int q = off[u] >> 1;
+    uint32_t v[5], o[4];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) v[i] = q == 0 ? w[i] : q == 1 ? w[i + 1] : q == 2 ? w[i + 2] : w[i + 3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      o[i] = (off[u] & 1) ? __funnelshift_r(v[i], v[i + 1], 16) : v[i];
+      if (2 * i >= n[u]) o[i] = 0u;
+      else if (2 * i + 1 >= n[u]) o[i] &= 0xFFFFu;
+    }
+    *reinterpret_cast<uint4*>(j.dst + (first + u * 256) * 8) = make_uint4(o[0], o[1], o[2], o[3]);
+  }
 }
 
 }  // namespace
@@ -557,7 +705,7 @@ cudaError_t tc_pack(const PackSource* src, int n, cudaStream_t s) {
     const PackSource& q = src[i];
     const int to = (q.cols + 7) / 8 * 8;
     a.job[i] = {q.from.p, q.from.row, q.from.member, q.to, q.members, q.rows, q.cols, to, (unsigned)blocks};
-    blocks += ((unsigned long long)q.members * q.rows * (to / 8) + 255) / 256;
+    blocks += ((unsigned long long)q.members * q.rows * (to / 8) + 256 * kPackEach - 1) / (256 * kPackEach);
   }
   if (blocks > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
   a.n = n;
@@ -566,35 +714,39 @@ cudaError_t tc_pack(const PackSource* src, int n, cudaStream_t s) {
 
 static cudaError_t rows_forward(const pbt_gated_desc* d, const Operand& x, const Operand& w, void* h, float* z, int pitch, cudaStream_t s) {
   RowsParams p = {};
-  p.rows = d->rows; p.hidden = d->hidden;
-  p.k_blocks = (d->width + kBK - 1) / kBK;
-  p.x_batched = d->members > 1 && x.member != 0;
-  p.w_batched = d->members > 1 && w.member != 0;
+  p.a_batched = d->members > 1 && w.member != 0;
   p.activation = d->activation;
   p.drop = d->drop != nullptr;
   if (d->drop) p.rule = *d->drop;
-  p.vec = d->hidden % 8 == 0 && ((uintptr_t)h & 15) == 0;
-  p.h = (bf16*)h; p.z = z; p.pitch = pitch;
-  p.counters = (Counters*)d->status_device;
-  const int n = d->rows <= 16 ? 16 : d->rows <= 32 ? 32 : d->rows <= 64 ? 64 : 128;
-  CUtensorMap tmX, tmW;
-  if (!make_map(&tmX, x.p, d->width, d->rows, x.row, p.x_batched ? d->members : 1, x.member, n) ||
-      !make_map(&tmW, w.p, d->width, 2ll * d->hidden, w.row, p.w_batched ? d->members : 1, w.member, kRowsUnits))
-    return cudaErrorInvalidValue;
-  // as many parts of the contraction as there are SMs to spare for, four blocks of it each at least
-  const long long tiles = (long long)((d->hidden + kRowsUnits - 1) / kRowsUnits) * d->members, room = n <= 64 ? 296 : 148;
-  int splits = 1;
-  while (splits < kRowsSplits && tiles * splits * 2 <= room && p.k_blocks >= splits * 2 * 4) splits *= 2;
-  switch (n) {
-    case 16: return launch_rows<16>(d, p, tmX, tmW, splits, s);
-    case 32: return launch_rows<32>(d, p, tmX, tmW, splits, s);
-    case 64: return launch_rows<64>(d, p, tmX, tmW, splits, s);
-    default: return launch_rows<128>(d, p, tmX, tmW, splits, s);
-  }
+  p.out = (bf16*)h; p.z = z; p.pitch = pitch;
+  CUtensorMap tmA;
+  if (!make_map(&tmA, w.p, d->width, 2ll * d->hidden, w.row, p.a_batched ? d->members : 1, w.member, 64)) return cudaErrorInvalidValue;
+  return launch_rows<false>(d, p, tmA, x, d->width, s);
+}
+
+// dx takes it up to 32 rows, and where larger tiles would leave a third of the SMs without one (one member's 500 rows, 2048 -> 2048: a whole backward pass
+// 38 us, by the plain product 46; 20 x 250, 1024 -> 512, 320 tiles: 56 and 54).
+bool tc_dx_few(const pbt_gated_desc* d) {
+  return d->rows <= kRowsForward || (long long)((d->rows + 127) / 128) * ((d->width + 127) / 128) * d->members <= 100;
+}
+cudaError_t tc_dx(const pbt_gated_desc* d, const Operand& dz, const Operand& w, cudaStream_t s) {
+  RowsParams p = {};
+  p.a_batched = d->members > 1 && w.member != 0;
+  p.out = (bf16*)d->dx;
+  CUtensorMap tmA;
+  if (!make_map(&tmA, w.p, d->width, 2ll * d->hidden, w.row, p.a_batched ? d->members : 1, w.member, kBK)) return cudaErrorInvalidValue;
+  return launch_rows<true>(d, p, tmA, dz, 2 * d->hidden, s);
+}
+
+bool tc_outer_supported(const pbt_gated_desc* d) { return d->rows <= kOuterMost; }
+cudaError_t tc_outer(const pbt_gated_desc* d, const bf16* dz, int dz_pitch, const Operand& x, cudaStream_t s) {
+  const OuterParams p = {dz, dz_pitch, x, (bf16*)d->dweight, d->rows, 2 * d->hidden, d->width, d->width % 8 == 0 && ((uintptr_t)d->dweight & 15) == 0};
+  const dim3 grid((unsigned)((d->width + kOuterTile - 1) / kOuterTile), (unsigned)((2 * d->hidden + kOuterTile - 1) / kOuterTile), (unsigned)d->members);
+  return d->rows <= 16 ? launch_with(grid, 256, 0, s)(k_gated_outer<1>, p) : launch_with(grid, 256, 0, s)(k_gated_outer<2>, p);
 }
 
 cudaError_t tc_forward(const pbt_gated_desc* d, const Operand& x, const Operand& w, void* h, float* z, int pitch, cudaStream_t s) {
-  if (d->rows <= kRowsMost) return rows_forward(d, x, w, h, z, pitch, s);
+  if (d->rows <= kRowsForward) return rows_forward(d, x, w, h, z, pitch, s);
   TileParams p;
   memset(&p, 0, sizeof(p));
   p.rows = d->rows; p.hidden = d->hidden;
@@ -608,15 +760,21 @@ cudaError_t tc_forward(const pbt_gated_desc* d, const Operand& x, const Operand&
   if (d->drop) p.rule = *d->drop;
   p.counters = (Counters*)d->status_device;
 
-  int dev = 0, sms = 148;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  static DeviceSetup setup_pair, setup_wide, setup_narrow;
+  int sms = 0;
+  cudaError_t e = device_setup(&setup_pair, k_gated_tc_pair, Tile<true, 128, kPairStages>::kTotal, &sms);
+  if (e == cudaSuccess) e = device_setup(&setup_wide, k_gated_tc<128, 3>, Tile<false, 128, 3>::kTotal, &sms);
+  if (e == cudaSuccess) e = device_setup(&setup_narrow, k_gated_tc<64, 4>, Tile<false, 64, 4>::kTotal, &sms);
   if (e != cudaSuccess) return e;
+  // The kernel whose waves of tiles are the shortest together, in waves of a CTA's wide tiles.  A narrow tile has half the products and takes 0.6 of the
+  // time; a pair's costs less the longer the contraction (8 members x 160 rows, 2048 -> 2048, two waves of pairs or wide tiles, four of narrow ones: 34,
+  // 39 and 47 us; 40 x 512, 1024 -> 1024, 9, 9 and 18: 76, 81 and 102; 60 x 400, 300 -> 2000, 26, 26 and 52: 182, 160 and 187; 14 x 290, 1536 -> 336, 2, 1
+  // and 2: 25, 17.5 and 21; 5 x 301, 1008 -> 515, one of each: 14, 14 and 10.6).
   auto waves = [&](int rows, int units, int at_once) {
     const long long tiles = (long long)((d->rows + rows - 1) / rows) * ((d->hidden + units - 1) / units) * d->members;
     return (double)((tiles + at_once - 1) / at_once);
   };
-  const double pair = 0.96 * waves(256, 128, sms / 2), wide = waves(128, 128, sms), narrow = 0.6 * waves(128, 64, sms);
+  const double pair = (0.85 + 1.3 / p.k_blocks) * waves(256, 128, sms / 2), wide = waves(128, 128, sms), narrow = 0.6 * waves(128, 64, sms);
   const int hn = narrow < wide && narrow < pair ? 64 : 128;
   const bool use_pair = hn == 128 && pair <= wide;
   const int rows = use_pair ? 256 : 128;
@@ -636,16 +794,12 @@ cudaError_t tc_forward(const pbt_gated_desc* d, const Operand& x, const Operand&
          make_map(&maps.u, z + pitch, pitch, all, 2 * pitch, d->members, all * 2 * pitch, 32, 4, 32, 128);
   if (!ok) return cudaErrorInvalidValue;
 
-  auto launch = [&](auto kernel, DeviceSetup* setup, int bytes, int at_once, int ctas) {
-    int count = 0;
-    const cudaError_t err = device_setup(setup, kernel, bytes, &count);
-    if (err != cudaSuccess) return err;
+  auto launch = [&](auto kernel, int bytes, int at_once, int ctas) {
     return launch_with((unsigned)(ctas * std::min(p.num_tiles, at_once)), kTcThreads, bytes, s)(kernel, maps, p);
   };
-  static DeviceSetup setup_pair, setup_wide, setup_narrow;
-  if (use_pair) return launch(k_gated_tc_pair, &setup_pair, Tile<true, 128, kPairStages>::kTotal, sms / 2, 2);
-  if (hn == 128) return launch(k_gated_tc<128, 3>, &setup_wide, Tile<false, 128, 3>::kTotal, sms, 1);
-  return launch(k_gated_tc<64, 4>, &setup_narrow, Tile<false, 64, 4>::kTotal, sms, 1);
+  if (use_pair) return launch(k_gated_tc_pair, Tile<true, 128, kPairStages>::kTotal, sms / 2, 2);
+  if (hn == 128) return launch(k_gated_tc<128, 3>, Tile<false, 128, 3>::kTotal, sms, 1);
+  return launch(k_gated_tc<64, 4>, Tile<false, 64, 4>::kTotal, sms, 1);
 }
 
 }  // namespace gated

@@ -443,12 +443,13 @@ class Dropout(NamedTuple):
 def _drop_rule(drop, members, device):
     rate, seed, step, site, first = drop
     rates = steps = None
-    if isinstance(rate, torch.Tensor):
-        if not (rate.dtype is torch.float32 and rate.shape == (members,) and rate.device == device and rate.is_contiguous()):
+    tensor, shape = torch.Tensor, (members,)
+    if isinstance(rate, tensor):
+        if not (rate.dtype is torch.float32 and rate.shape == shape and rate.device == device and rate.is_contiguous()):
             raise ValueError("a dropout's rate is a number or a contiguous float32 tensor [members] on the activations' device")
         rates, rate = rate.data_ptr(), 0.0
-    if isinstance(step, torch.Tensor):
-        if not (step.dtype is torch.int64 and step.shape == (members,) and step.device == device and step.is_contiguous()):
+    if isinstance(step, tensor):
+        if not (step.dtype is torch.int64 and step.shape == shape and step.device == device and step.is_contiguous()):
             raise ValueError("a dropout's step is a number or a contiguous int64 tensor [members] on the activations' device")
         steps, step = step.data_ptr(), 0
     if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 63 and 0 <= site <= 1 << 30 and 0 <= first <= _MOST):
@@ -468,14 +469,10 @@ def dropout_forward(x, dropout: Dropout, residual=None, stream=None):
     m, rows, width = shape
     if m > _MOST or rows > _MOST or width > _MOST:
         raise ValueError("activations have at most 2^31 - 1 members, rows and columns")
-    d = PbtDropoutDesc()
-    d.members, d.rows, d.width, d.dtype = m, rows, width, _TYPES[dtype]
-    d.x, d.x_member, d.x_row = _activation(x, kind, "x")
-    if residual is not None:
-        d.residual, d.residual_member, d.residual_row = _activation(residual, kind, "residual")
-    d.rule = _drop_rule(dropout, m, device)
-    inputs = () if stream is None else (x, residual, *_drop_inputs(dropout))
-    return _on(device, stream, inputs, _dropout, d, x)
+    at, member, row = _activation(x, kind, "x")
+    other, other_member, other_row = (None, 0, 0) if residual is None else _activation(residual, kind, "residual")
+    d = PbtDropoutDesc(m, rows, width, _TYPES[dtype], at, member, row, other, other_member, other_row, None, _drop_rule(dropout, m, device))
+    return _on(device, stream, () if stream is None else (x, residual, *_drop_inputs(dropout)), _dropout, d, x)
 
 
 def _dropout(s, d, x):
@@ -494,6 +491,7 @@ def dropout_backward(dy, dropout: Dropout, stream=None):
 
 # --- gated units -------------------------------------------------------------------------------------------------------------
 
+_NO_WORKSPACE = 3      # PBT_ERR_WORKSPACE
 _ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2, "sigmoid": 3}
 
 
@@ -527,7 +525,8 @@ class GatedUnit:
         _check(self.lib.pbt_gated_query_workspace(C.byref(d), 0, C.byref(C.c_size_t(0))))
 
     def _call(self, x, dropout):
-        """The description of a call on these rows (a copy: calls from several threads do not share it), and the dropout it points to."""
+        """The description of a call on these rows (a copy: calls from several threads do not share it), and the dropout it points to, which has to
+        live until the call has been enqueued."""
         w, shape = self.weight, x.shape
         if not (len(shape) == 3 and shape[0] == self._desc.members and shape[2] == self._desc.width and x.dtype == w.dtype and x.device == w.device):
             raise ValueError("x is [members, rows, width] of the weight's members, width, type and device")
@@ -539,7 +538,7 @@ class GatedUnit:
         rule = None
         if dropout is not None:
             rule = _drop_rule(dropout, d.members, w.device)
-            d.drop = C.pointer(rule)
+            d.drop = C.addressof(rule)
         return d, rule
 
     def forward(self, x, dropout: Optional[Dropout] = None, keep: bool = False, stream=None):
@@ -595,10 +594,14 @@ class GatedUnit:
     def _run(self, d, backward, call, s):
         if s != self._home:      # keeps the status words until the call is done, should the object go first
             self._status.record_stream(torch.cuda.current_stream(self.weight.device))
-        nbytes, at = C.c_size_t(0), C.byref(d)
-        rc = self.lib.pbt_gated_query_workspace(at, backward, C.byref(nbytes))
-        if not rc:
-            rc = _with_workspace(call, at, nbytes.value, s)
+        at = C.byref(d)
+        # a bfloat16 forward pass needs a workspace for rows of odd sizes only: asking for its size costs a small call as much as its checks
+        rc = _NO_WORKSPACE if backward or not d.dtype else call(at, None, 0, s)
+        if rc == _NO_WORKSPACE:
+            nbytes = C.c_size_t(0)
+            rc = self.lib.pbt_gated_query_workspace(at, backward, C.byref(nbytes))
+            if not rc:
+                rc = _with_workspace(call, at, nbytes.value, s)
         if rc:
             _check(rc)
 

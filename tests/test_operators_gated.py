@@ -367,8 +367,9 @@ def test_nothing_is_written_beside_the_results(shape, dtype):
         whole, ws = between(n.value)
         places[f"workspace {backward}"] = (whole, ws)
         assert call(C.byref(d), ws.data_ptr(), n.value, s) == 0
-        assert call(C.byref(d), ws.data_ptr(), n.value - 1, s) == 3 and call(C.byref(d), ws.data_ptr() + 16, n.value, s) == 3
-        assert call(C.byref(d), None, n.value, s) == 3
+        if n.value:
+            assert call(C.byref(d), ws.data_ptr(), n.value - 1, s) == 3 and call(C.byref(d), ws.data_ptr() + 16, n.value, s) == 3
+            assert call(C.byref(d), None, n.value, s) == 3
     torch.cuda.synchronize()
     for k, (whole, t) in places.items():
         assert (whole[:guard] == 0x5A).all() and (whole[-guard:] == 0x5A).all(), k
@@ -397,7 +398,7 @@ def test_the_c_calls_refuse_what_they_cannot_do():
     common = [(1, dict(members=0)), (1, dict(rows=-1)), (1, dict(width=0)), (1, dict(hidden=0)), (2, dict(members=65536)), (2, dict(rows=1 << 22)),
               (2, dict(width=1 << 22)), (2, dict(hidden=1 << 21)), (2, dict(members=65535, rows=1 << 20, hidden=1 << 20, width=1 << 20, x_row=1 << 20, weight_row=1 << 20)),
               (2, dict(dtype=2)), (2, dict(activation=4)), (2, dict(activation=-1)), (1, dict(weight=None)), (1, dict(weight_row=7)), (1, dict(weight_member=-8)),
-              (1, dict(x=None)), (1, dict(x_row=7)), (1, dict(x_member=-1)), (1, dict(status_device=None)), (1, dict(drop=C.pointer(rule)))]
+              (1, dict(x=None)), (1, dict(x_row=7)), (1, dict(x_member=-1)), (1, dict(status_device=None)), (1, dict(drop=C.addressof(rule)))]
     for code, kw in common:
         for backward in (0, 1):
             assert lib.pbt_gated_query_workspace(C.byref(desc(**kw)), backward, C.byref(n)) == code, kw
@@ -407,7 +408,10 @@ def test_the_c_calls_refuse_what_they_cannot_do():
     for kw in (dict(dh=None), dict(dx=None), dict(dweight=None), dict(dh_row=7), dict(dh_member=-1)):
         assert lib.pbt_gated_backward(C.byref(desc(**kw)), 4096, 1 << 60, None) == 1, kw
     assert lib.pbt_gated_forward(C.byref(desc(rows=0, x=None, h=None)), None, 0, None) == 0         # nothing to do
-    assert lib.pbt_gated_forward(C.byref(desc()), None, 1 << 20, None) == 3
+    for kw in (dict(dtype=0, kept=None), dict(x=4098), dict(weight_row=9)):       # these need one
+        assert lib.pbt_gated_query_workspace(C.byref(desc(**kw)), 0, C.byref(n)) == 0 and n.value > 0
+        assert lib.pbt_gated_forward(C.byref(desc(**kw)), None, 1 << 20, None) == 3 and lib.pbt_gated_backward(C.byref(desc(**kw)), None, 1 << 20, None) == 3
+    assert lib.pbt_gated_query_workspace(C.byref(desc()), 0, C.byref(n)) == 0 and n.value == 0
 
 
 @pytest.mark.gpu
