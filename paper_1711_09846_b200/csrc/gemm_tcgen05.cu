@@ -157,7 +157,8 @@ k_gemm_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
     int it = 0;
     bool ok = true;
     const int esz = p.out_dtype == kBF16 ? 2 : 4;
-    const bool vec_ok = (((uintptr_t)p.C & 15) == 0) && ((p.ldc * esz) % 16 == 0) && ((p.strideC * esz) % 16 == 0) &&
+    // (four elements go at a time: 8 bytes of bf16, 16 of fp32)
+    const bool vec_ok = (((uintptr_t)p.C & (4 * esz - 1)) == 0) && (p.ldc % 4 == 0) && (p.strideC % 4 == 0) &&
                         (!p.mask || ((((uintptr_t)p.mask & 7) == 0) && (p.ldmask % 4 == 0) && (p.strideMask % 4 == 0))) &&
                         (!p.bias || ((((uintptr_t)p.bias & 15) == 0) && (p.strideBias % 4 == 0)));
     for (int tile = blockIdx.x; tile < p.num_tiles && ok; tile += gridDim.x, ++it) {

@@ -108,6 +108,38 @@ __device__ __forceinline__ void epilogue_tile(const TcParams& p, float* buf, uin
     }
     return;
   }
+  if (!vec_ok && p.out_dtype == kBF16 && !p.mask) {
+    // Rows of C that allow no vectors: a warp writes whole rows of the chunk, 64 consecutive bytes, two rows at a time in pairs of columns where
+    // C allows that.  Four neighbouring columns a lane, one by one, as below, touch four rows with every store (1030 x 1001 outputs, K = 301, five
+    // problems: 22.7 us).
+    const bool pairs = (((uintptr_t)p.C & 3) == 0) && p.ldc % 2 == 0 && p.strideC % 2 == 0;
+    const int rows = min(32, p.M - m0 - q * 32);
+    bf16* c = reinterpret_cast<bf16*>(p.C) + member * p.strideC + (long long)(m0 + q * 32) * p.ldc;
+    if (n0 + half * 32 < p.N) tmem_ld32(tacc + half * 32, r);
+#pragma unroll 1
+    for (int c0 = half * 32; c0 < BN && n0 + c0 < p.N; c0 += kChunkStep) {
+      tmem_ld_wait();
+      __syncwarp();
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        *reinterpret_cast<uint4*>(&buf[lane * kEpiPitch + j * 4]) = make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
+      if (c0 + kChunkStep < BN && n0 + c0 + kChunkStep < p.N) tmem_ld32(tacc + c0 + kChunkStep, r);
+      __syncwarp();
+      const int sub = pairs ? lane >> 4 : 0, at = pairs ? (lane & 15) * 2 : lane, col = n0 + c0 + at;
+      const float b0 = bias && col < p.N ? bias[col] : 0.f, b1 = bias && pairs && col + 1 < p.N ? bias[col + 1] : 0.f;
+      if (col < p.N) {
+#pragma unroll 8
+        for (int row = sub; row < rows; row += pairs ? 2 : 1) {
+          float v0 = buf[row * kEpiPitch + at] + b0, v1 = pairs ? buf[row * kEpiPitch + at + 1] + b1 : 0.f;
+          if (p.relu) { v0 = fmaxf(v0, 0.f); v1 = fmaxf(v1, 0.f); }
+          bf16* to = c + (long long)row * p.ldc + col;
+          if (pairs && col + 1 < p.N) *reinterpret_cast<__nv_bfloat162*>(to) = __floats2bfloat162_rn(v0, v1);
+          else *to = __float2bfloat16_rn(v0);
+        }
+      }
+    }
+    return;
+  }
   if (n0 + half * 32 < p.N) tmem_ld32(tacc + half * 32, r);
 #pragma unroll 1
   for (int c0 = half * 32; c0 < BN; c0 += kChunkStep) {
