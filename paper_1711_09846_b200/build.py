@@ -18,7 +18,7 @@ OBJ = os.path.join(HERE, "_build")
 
 SOURCES = ["pbt_api.cu", "kernels_misc.cu", "kernels_opt.cu", "kernels_exploit.cu", "gemm_simt.cu",
            "gemm_tcgen05.cu", "gemm_tcgen05_pair.cu", "wgrad_adam_tcgen05.cu", "energy_static.cu",
-           "clip.cu", "block_norm.cu", "adapters.cu", "adapters_tc.cu", "dropout.cu", "gated.cu", "gated_tc.cu"]
+           "clip.cu", "block_norm.cu", "adapters.cu", "adapters_tc.cu", "dropout.cu", "gated.cu", "gated_tc.cu", "gated_f32.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
 

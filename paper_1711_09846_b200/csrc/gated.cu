@@ -1,8 +1,8 @@
-// Gated units of a population, h = keep / (1 - rate) act(x Wg^T) (x Wu^T) per member, and their gradients: entry points and the
-// kernels that work element by element.
+// Gated units of a population, h = keep / (1 - rate) act(x Wg^T) (x Wu^T) per member, and their gradients: entry points and the element-wise part of
+// the backward pass.  The products are in gated_tc.cu (bf16) and gated_f32.cu, and in the framework's member-batched GEMMs.
 //
-// The products run in the framework's member-batched GEMMs; g and u stay in fp32 between the two (as bf16 they would add their
-// own rounding to that of h and of every gradient).
+// g and u stay in fp32 for the backward pass: as bf16 numbers they would add their own rounding to that of every gradient (dg and du have it once, as operands),
+// and a kept fp32 pair costs 0.2 ms of 2 for 80 members x 512 rows x 2048 hidden units, working it out anew 0.5.
 #include <algorithm>
 
 #include "gated.cuh"
@@ -28,19 +28,19 @@ int fail(int code, const char* msg) {
 
 int round_up(int n, int m) { return (n + m - 1) / m * m; }
 
-// One thread has eight neighbouring hidden units of a row: one block of the generator.
+// dg and du of a row's hidden units from g, u and dh; a thread has eight neighbouring ones, a block of the generator.
 template <typename T>
 struct CellArgs {
   const float* z; int pitch;                      // [members][rows][2][pitch]: g, then u
   const T* dh; long long dh_member, dh_row;
-  T* out; long long out_pitch;                    // h [members][rows][hidden], or [dg du] [members][rows][out_pitch]
+  T* out; long long out_pitch;                    // [dg du] [members][rows][out_pitch]
   uint32_t rows, hidden, groups;
   int activation, drop;
   pbt_drop_rule rule;
 };
 
-// VEC: 16-byte loads and stores everywhere.  The backward pass reads 8 + 2 bytes a hidden unit and writes 4 (bf16).
-template <typename T, bool BACKWARD, bool VEC>
+// VEC: 16-byte loads and stores everywhere.  Bound by its bytes, 14 a hidden unit in bf16 (80 x 512 x 2048: 189 us, 6.2 TB/s).
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) k_gated_cells(const CellArgs<T> a) {
   pdl_prologue();
   const int m = blockIdx.y;
@@ -50,18 +50,16 @@ __global__ void __launch_bounds__(256) k_gated_cells(const CellArgs<T> a) {
   const long long at = (long long)m * a.rows + row;
   const float* z = a.z + at * 2 * a.pitch + c0;           // (the pitch is a multiple of eight: whole groups)
   T* out = a.out + at * a.out_pitch + c0;
-  const T* from = BACKWARD ? a.dh + m * a.dh_member + row * a.dh_row + c0 : nullptr;
+  const T* from = a.dh + m * a.dh_member + row * a.dh_row + c0;
   const uint4 z0 = load16(z), z1 = load16(z + 4), z2 = load16(z + a.pitch), z3 = load16(z + a.pitch + 4);
   Eight dh;
-  if (BACKWARD) {
-    if (!VEC) {
+  if (!VEC) {
 #pragma unroll
-      for (int c = 0; c < kGroup; ++c) dh.v[c] = c < n ? as_float(from[c]) : 0.f;
-    } else if constexpr (sizeof(T) == 2) {
-      dh = unpack(load16(from));
-    } else {
-      dh = unpack(load16(from), load16(from + 4));
-    }
+    for (int c = 0; c < kGroup; ++c) dh.v[c] = c < n ? as_float(from[c]) : 0.f;
+  } else if constexpr (sizeof(T) == 2) {
+    dh = unpack(load16(from));
+  } else {
+    dh = unpack(load16(from), load16(from + 4));
   }
   const Eight g = unpack(z0, z1), u = unpack(z2, z3);
   uint32_t in = 0xFFu;
@@ -71,29 +69,25 @@ __global__ void __launch_bounds__(256) k_gated_cells(const CellArgs<T> a) {
     in = dropout::kept_bits(d, (uint32_t)i);
     if (d.on) f = d.scale;
   }
-  Eight first, second;
+  Eight dg, du;
 #pragma unroll
   for (int c = 0; c < kGroup; ++c) {
     const bool keep = in >> c & 1u;
-    if (BACKWARD) {
-      float slope;
-      const float act = activation(a.activation, g.v[c], &slope), v = f * dh.v[c];
-      first.v[c] = keep ? v * u.v[c] * slope : 0.f;
-      second.v[c] = keep ? v * act : 0.f;
-    } else {
-      first.v[c] = keep ? f * (activation(a.activation, g.v[c]) * u.v[c]) : 0.f;
-    }
+    float slope;
+    const float act = activation(a.activation, g.v[c], &slope), v = f * dh.v[c];
+    dg.v[c] = keep ? v * u.v[c] * slope : 0.f;
+    du.v[c] = keep ? v * act : 0.f;
   }
-  if (VEC) {
-    store8(out, first);
-    if (BACKWARD) store8(out + a.hidden, second);
-    return;
-  }
+  if constexpr (VEC) {
+    store8(out, dg);
+    store8(out + a.hidden, du);
+  } else {
 #pragma unroll
-  for (int c = 0; c < kGroup; ++c) {
-    if (c >= n) break;
-    store(out + c, first.v[c]);
-    if (BACKWARD) store(out + a.hidden + c, second.v[c]);
+    for (int c = 0; c < kGroup; ++c) {
+      if (c >= n) break;
+      store(out + c, dg.v[c]);
+      store(out + a.hidden + c, du.v[c]);
+    }
   }
 }
 
@@ -101,8 +95,8 @@ __global__ void __launch_bounds__(256) k_gated_cells(const CellArgs<T> a) {
 struct Plan {
   int pitch;                      // of g and u
   int dz_pitch;
-  size_t z, dz, x, w, bytes;      // offsets; z: only where the caller keeps none and it is needed
-  bool has_z, pack_x, pack_w;     // pack: bf16 rows that are not multiples of 16 bytes are laid out anew
+  size_t z, dz, x, w, bytes;      // offsets; z: a backward pass for which nothing was kept
+  bool pack_x, pack_w;     // pack: bf16 rows that are not multiples of 16 bytes are laid out anew
 };
 Plan plan_of(const pbt_gated_desc* d, bool backward) {
   Plan p = {};
@@ -110,8 +104,7 @@ Plan plan_of(const pbt_gated_desc* d, bool backward) {
   p.dz_pitch = round_up(2 * d->hidden, kGroup);
   const size_t rows = (size_t)d->members * d->rows, size = d->dtype ? 2 : 4;
   auto take = [&](size_t bytes) { const size_t at = p.bytes; p.bytes += (bytes + 255) & ~(size_t)255; return at; };
-  p.has_z = !d->kept && (backward || !d->dtype);
-  if (p.has_z) p.z = take(rows * 2 * p.pitch * sizeof(float));
+  if (!d->kept && backward) p.z = take(rows * 2 * p.pitch * sizeof(float));
   if (backward) p.dz = take(rows * p.dz_pitch * size);
   if (d->dtype) {
     p.pack_x = !tc_aligned(d->x, d->x_row, d->x_member, d->members);
@@ -154,38 +147,22 @@ CellArgs<T> cells_of(const pbt_gated_desc* d, const Plan& p, const float* z) {
   if (d->drop) a.rule = *d->drop;
   return a;
 }
-template <typename T, bool BACKWARD>
+template <typename T>
 cudaError_t launch_cells(const pbt_gated_desc* d, const CellArgs<T>& a, cudaStream_t s) {
   const dim3 grid((unsigned)(((uint64_t)a.rows * a.groups + 255) / 256), (unsigned)d->members);
   // (dh: any base, row and member stride that keeps 16 bytes; what this library lays out has them where hidden is a multiple of eight)
   constexpr int kStep = 16 / sizeof(T);
   const bool vec = d->hidden % kGroup == 0 && ((uintptr_t)a.out & 15) == 0 && a.out_pitch % kStep == 0 &&
-                   (!BACKWARD || (((uintptr_t)a.dh & 15) == 0 && (d->rows == 1 || a.dh_row % kStep == 0) && (d->members == 1 || a.dh_member % kStep == 0)));
-  return vec ? launch_with(grid, 256, 0, s)(k_gated_cells<T, BACKWARD, true>, a) : launch_with(grid, 256, 0, s)(k_gated_cells<T, BACKWARD, false>, a);
+                   ((uintptr_t)a.dh & 15) == 0 && (d->rows == 1 || a.dh_row % kStep == 0) && (d->members == 1 || a.dh_member % kStep == 0);
+  return vec ? launch_with(grid, 256, 0, s)(k_gated_cells<T, true>, a) : launch_with(grid, 256, 0, s)(k_gated_cells<T, false>, a);
 }
 
 GemmArgs product(const pbt_gated_desc* d) {
   GemmArgs g;
   memset(&g, 0, sizeof(g));
   g.batch = d->members;
-  g.in_dtype = g.out_dtype = d->dtype ? kBF16 : kF32;
+  g.in_dtype = g.out_dtype = kBF16;
   return g;
-}
-
-// fp32: g and u of all rows
-cudaError_t project_f32(const pbt_gated_desc* d, const Plan& p, float* z, cudaStream_t s) {
-  GemmArgs g = product(d);
-  g.M = d->rows; g.N = d->hidden; g.K = d->width;
-  g.A = d->x; g.lda = d->x_row; g.strideA = d->x_member;
-  g.ldb = d->weight_row; g.strideB = d->weight_member;
-  g.ldc = 2 * p.pitch; g.strideC = (long long)d->rows * 2 * p.pitch;
-  for (int half = 0; half < 2; ++half) {
-    g.B = (const float*)d->weight + half * (long long)d->hidden * d->weight_row;
-    g.C = z + half * p.pitch;
-    const cudaError_t e = launch_gemm_simt(g, s);
-    if (e != cudaSuccess) return e;
-  }
-  return cudaSuccess;
 }
 
 cudaError_t forward(const pbt_gated_desc* d, char* ws, cudaStream_t s) {
@@ -195,19 +172,13 @@ cudaError_t forward(const pbt_gated_desc* d, char* ws, cudaStream_t s) {
     const cudaError_t e = operands_of(d, p, ws, &o, s);
     return e == cudaSuccess ? tc_forward(d, o.x, o.w, d->h, d->kept, p.pitch, s) : e;
   }
-  float* z = d->kept ? d->kept : (float*)(ws + p.z);
-  const cudaError_t e = project_f32(d, p, z, s);
-  if (e != cudaSuccess) return e;
-  CellArgs<float> a = cells_of<float>(d, p, z);
-  a.out = (float*)d->h; a.out_pitch = d->hidden;
-  return launch_cells<float, false>(d, a, s);
+  return f32_forward(d, (float*)d->h, d->kept, p.pitch, s);
 }
 
 // The faster of the tensor-core products, which take any number of rows here: tensor maps fill what is missing with zeros.  In waves of 128 x 256 (a pair:
 // 256 x 256) tiles; launch_gemm_tc halves its tiles where that shortens the last wave.  A pair's cost less from contractions of 384 on (40 members,
 // 512 rows, 1024 -> 1024: dW 10 us less, 8 x 160, 2048 -> 2048: 4 us more).
 cudaError_t run_product(const pbt_gated_desc* d, const GemmArgs& g, cudaStream_t s) {
-  if (!d->dtype) return launch_gemm_simt(g, s);
   auto waves = [&](int rows, int cols, int at_once) {
     const long long tiles = (long long)((g.M + rows - 1) / rows) * ((g.N + cols - 1) / cols) * g.batch;
     return (double)((tiles + at_once - 1) / at_once);
@@ -226,7 +197,7 @@ cudaError_t backward(const pbt_gated_desc* d, char* ws, cudaStream_t s) {
   if (d->dtype) e = operands_of(d, p, ws, &o, s);
   if (e == cudaSuccess && !z) {
     float* made = (float*)(ws + p.z);
-    e = d->dtype ? tc_forward(d, o.x, o.w, nullptr, made, p.pitch, s) : project_f32(d, p, made, s);
+    e = d->dtype ? tc_forward(d, o.x, o.w, nullptr, made, p.pitch, s) : f32_forward(d, nullptr, made, p.pitch, s);
     z = made;
   }
   if (e != cudaSuccess) return e;
@@ -234,26 +205,23 @@ cudaError_t backward(const pbt_gated_desc* d, char* ws, cudaStream_t s) {
   CellArgs<T> a = cells_of<T>(d, p, z);
   a.dh = (const T*)d->dh; a.dh_member = d->dh_member; a.dh_row = d->dh_row;
   a.out = dz; a.out_pitch = p.dz_pitch;
-  e = launch_cells<T, true>(d, a, s);
+  e = launch_cells<T>(d, a, s);
   if (e != cudaSuccess) return e;
+  if (!d->dtype) return f32_backward(d, (const float*)dz, p.dz_pitch, s);
   GemmArgs g = product(d);
   g.A = dz; g.lda = p.dz_pitch; g.strideA = (long long)d->rows * p.dz_pitch;
   g.M = d->rows; g.N = d->width; g.K = 2 * d->hidden;
   g.b_mn = 1;
-  g.B = d->dtype ? (const void*)o.w.p : d->weight;
-  g.ldb = d->dtype ? o.w.row : d->weight_row;
-  g.strideB = d->dtype ? o.w.member : d->weight_member;
+  g.B = o.w.p; g.ldb = o.w.row; g.strideB = o.w.member;
   g.C = d->dx; g.ldc = d->width; g.strideC = (long long)d->rows * d->width;
-  if (d->dtype && tc_dx_few(d)) e = tc_dx(d, {(const bf16*)dz, p.dz_pitch, (long long)d->rows * p.dz_pitch}, o.w, s);
+  if (tc_dx_few(d)) e = tc_dx(d, {(const bf16*)dz, p.dz_pitch, (long long)d->rows * p.dz_pitch}, o.w, s);
   else e = run_product(d, g, s);
   if (e != cudaSuccess) return e;
   g.a_mn = 1;
   g.M = 2 * d->hidden; g.K = d->rows;
-  g.B = d->dtype ? (const void*)o.x.p : d->x;
-  g.ldb = d->dtype ? o.x.row : d->x_row;
-  g.strideB = d->dtype ? o.x.member : d->x_member;
+  g.B = o.x.p; g.ldb = o.x.row; g.strideB = o.x.member;
   g.C = d->dweight; g.strideC = 2ll * d->hidden * d->width;
-  if (d->dtype && tc_outer_supported(d)) return tc_outer(d, (const bf16*)dz, p.dz_pitch, o.x, s);
+  if (tc_outer_supported(d)) return tc_outer(d, (const bf16*)dz, p.dz_pitch, o.x, s);
   return run_product(d, g, s);
 }
 

@@ -27,6 +27,9 @@ cudaError_t tc_dx(const pbt_gated_desc* d, const Operand& dz, const Operand& w, 
 // dW of a few rows
 bool tc_outer_supported(const pbt_gated_desc* d);
 cudaError_t tc_outer(const pbt_gated_desc* d, const bf16* dz, int dz_pitch, const Operand& x, cudaStream_t s);
+// float (gated_f32.cu): h (or null) and g, u (or null); dx and dW
+cudaError_t f32_forward(const pbt_gated_desc* d, float* h, float* z, int pitch, cudaStream_t s);
+cudaError_t f32_backward(const pbt_gated_desc* d, const float* dz, int dz_pitch, cudaStream_t s);
 
 #ifdef __CUDACC__
 // act(g)

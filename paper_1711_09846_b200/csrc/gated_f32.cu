@@ -1,0 +1,305 @@
+// fp32 gated units on the ALUs (their results are good to some 2^-24 of the sums' terms, which the tensor cores' formats do not give): the three
+// products of a step as one kernel over tiles of 64 x 64,
+//   forward   g, u = x W^T with the activation, the product and dropout in its epilogue
+//   dx        [dg du] W
+//   dW        [dg du]^T x
+// Bound by the ALUs' issue: 40 members, 128 rows, 512 -> 512.
+#include <algorithm>
+
+#include "gated.cuh"
+#include "tc_common.cuh"
+
+namespace pbt {
+namespace gated {
+namespace {
+
+using dropout::Eight;
+using dropout::store8;
+
+constexpr int kK = 16, kStages = 3, kSplits = 8, kCols = 64, kThreadCols = 8;
+constexpr int kPitchK = kK + 4;           // floats of a staged row of k: the vectors that eight lanes read lie in different banks
+constexpr int kPitchSum = kCols + 4;
+
+// A tile of BM rows and 64 columns (forward: 32 hidden units' g and u); a thread has TM x 8 of its elements, a warp's lanes are 4 x 8 of the threads.
+template <int BM_, int TM_>
+struct Shape {
+  static constexpr int BM = BM_, TM = TM_, kThreadRows = BM / TM, kThreads = kThreadRows * (kCols / kThreadCols), kPerSm = (TM == 8 ? 384 : 512) / kThreads;
+  static constexpr int kA = BM * kPitchK > kK * (BM + 4) ? BM * kPitchK : kK * (BM + 4), kB = kCols * kPitchK, kStage = kA + kB;      // floats
+  static constexpr int kFloats = kStages * kStage > BM * kPitchSum ? kStages * kStage : BM * kPitchSum;
+  static_assert(kCols * kPitchK >= kK * (kCols + 4) && kThreads % 32 == 0, "the ring holds either layout");
+};
+typedef Shape<128, 8> Tall;
+typedef Shape<64, 8> Short;
+typedef Shape<16, 2> Few;
+
+struct ProductParams {
+  const float* a; long long lda, a_member;      // [M][K], or [K][M]
+  const float* b; long long ldb, b_member;      // [N][K], or [K][N]; forward: row n of the first half of the columns and n + hidden
+  float* c; long long ldc, c_member;            // [M][N]; forward: h, or null
+  int M, N, K;                                  // forward: N hidden units
+  int tiles_n;
+  bool vec_a, vec_b, vec_c;
+  // forward
+  float* z; int pitch;
+  int activation, drop;
+  pbt_drop_rule rule;
+};
+
+// a box of ROWS rows and COLS floats into staged rows of PITCH, `rows` x `cols` of which exist (the others are zero)
+template <int THREADS, int ROWS, int COLS, int PITCH>
+__device__ __forceinline__ void copy_box(uint32_t to, const float* from, long long ld, int rows, int cols, bool vectors) {
+  if (vectors) {
+    constexpr int kStep = THREADS / (COLS / 4);
+    const int r0 = threadIdx.x / (COLS / 4), c = threadIdx.x % (COLS / 4) * 4, bytes = min(max(cols - c, 0), 4) * 4;
+    const float* at = from + r0 * ld + c;
+    const long long step = kStep * ld;
+    to += (r0 * PITCH + c) * 4;
+#pragma unroll
+    for (int i = 0; i < ROWS / kStep; ++i) {
+      const int have = r0 + i * kStep < rows ? bytes : 0;
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + i * kStep * PITCH * 4), "l"(have ? at : from), "r"(have) : "memory");
+      at += step;
+    }
+  } else {
+    constexpr int kStep = THREADS / COLS;
+    const int r0 = threadIdx.x / COLS, c = threadIdx.x % COLS, bytes = c < cols ? 4 : 0;
+    const float* at = from + r0 * ld + c;
+    const long long step = kStep * ld;
+    to += (r0 * PITCH + c) * 4;
+#pragma unroll 4
+    for (int i = 0; i < ROWS / kStep; ++i) {
+      const int have = r0 + i * kStep < rows ? bytes : 0;
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + i * kStep * PITCH * 4), "l"(have ? at : from), "r"(have) : "memory");
+      at += step;
+    }
+  }
+}
+
+// K goes in slices of 16 through a ring of cp.async stages as the operands lie: staged rows of k are read as vectors of four k, rows of m or n as
+// vectors of four of those.  The CTAs of a cluster share the contraction; every one adds up its share of the tile's rows over all their sums, in
+// their order.
+template <typename S, bool A_MN, bool B_MN, bool GATED>
+__global__ void __launch_bounds__(S::kThreads, S::kPerSm) k_gated_product_f32(const ProductParams p) {
+  pdl_prologue();
+  extern __shared__ __align__(16) float f32_smem[];
+  constexpr int BM = S::BM, TM = S::TM, kThreads = S::kThreads, kPitchM = BM + 4, kPitchN = kCols + 4;
+  static_assert(!A_MN || TM == 8, "rows of m are read in vectors");
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tx = lane & 7, ty = warp * 4 + (lane >> 3);
+  const int splits = (int)tc::cluster_size(), rank = (int)tc::cluster_ctarank(), tile = blockIdx.x / splits, m = blockIdx.y;
+  constexpr int kUnits = GATED ? kCols / 2 : kCols;
+  const int m0 = tile / p.tiles_n * BM, n0 = tile % p.tiles_n * kUnits, rows = min(BM, p.M - m0), cols = min(kUnits, p.N - n0);
+  const int slices = (p.K + kK - 1) / kK, s0 = (int)((long long)slices * rank / splits), s1 = (int)((long long)slices * (rank + 1) / splits);
+  const float* A = p.a + m * p.a_member + (A_MN ? m0 : m0 * p.lda);
+  const float* B = p.b + m * p.b_member + (B_MN ? n0 : n0 * p.ldb);
+  const float* B2 = B + p.N * p.ldb;              // forward: the up-projection's rows
+  const uint32_t base = (uint32_t)__cvta_generic_to_shared(f32_smem);
+
+  int slot = 0;                                   // of the slice that is asked for next
+  auto load = [&](int s) {
+    if (s < s1) {
+      const uint32_t sa = base + slot * S::kStage * 4, sb = sa + S::kA * 4;
+      const int k0 = s * kK, ks = p.K - k0;
+      if (A_MN) copy_box<kThreads, kK, BM, kPitchM>(sa, A + k0 * p.lda, p.lda, ks, rows, p.vec_a);
+      else copy_box<kThreads, BM, kK, kPitchK>(sa, A + k0, p.lda, rows, ks, p.vec_a);
+      if (GATED) {
+        copy_box<kThreads, kUnits, kK, kPitchK>(sb, B + k0, p.ldb, cols, ks, p.vec_b);
+        copy_box<kThreads, kUnits, kK, kPitchK>(sb + kUnits * kPitchK * 4, B2 + k0, p.ldb, cols, ks, p.vec_b);
+      } else if (B_MN) {
+        copy_box<kThreads, kK, kCols, kPitchN>(sb, B + k0 * p.ldb, p.ldb, ks, cols, p.vec_b);
+      } else {
+        copy_box<kThreads, kCols, kK, kPitchK>(sb, B + k0, p.ldb, cols, ks, p.vec_b);
+      }
+    }
+    slot = slot + 1 == kStages ? 0 : slot + 1;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  auto row_of = [&](int i) { return A_MN ? (i >> 2) * (BM / 2) + ty * 4 + (i & 3) : ty + i * S::kThreadRows; };
+  auto col_of = [&](int j) { return B_MN ? (j >> 2) * (kCols / 2) + tx * 4 + (j & 3) : tx + j * 8; };
+
+  float acc[TM][8] = {};
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s) load(s0 + s);
+  int at = 0;
+#pragma unroll 1
+  for (int s = s0; s < s1; ++s) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+    __syncthreads();
+    load(s + kStages - 1);
+    const float *sa = f32_smem + at * S::kStage, *sb = sa + S::kA;
+    at = at + 1 == kStages ? 0 : at + 1;
+#pragma unroll
+    for (int k = 0; k < kK; k += 4) {
+      float b[4][8];            // [k][column]
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float4 q = *reinterpret_cast<const float4*>(B_MN ? sb + (k + (i & 3)) * kPitchN + (i >> 2) * (kCols / 2) + tx * 4 : sb + col_of(i) * kPitchK + k);
+        if (B_MN) { const int j = (i >> 2) * 4; b[i & 3][j] = q.x; b[i & 3][j + 1] = q.y; b[i & 3][j + 2] = q.z; b[i & 3][j + 3] = q.w; }
+        else { b[0][i] = q.x; b[1][i] = q.y; b[2][i] = q.z; b[3][i] = q.w; }
+      }
+      if (A_MN) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int h = 0; h < TM / 4; ++h) {
+            const float4 q = *reinterpret_cast<const float4*>(sa + (k + i) * kPitchM + h * (BM / 2) + ty * 4);
+            const float a[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+              for (int j = 0; j < 8; ++j) acc[h * 4 + r][j] = __fmaf_rn(a[r], b[i][j], acc[h * 4 + r][j]);
+          }
+      } else {
+#pragma unroll
+        for (int r = 0; r < TM; ++r) {
+          const float4 q = *reinterpret_cast<const float4*>(sa + row_of(r) * kPitchK + k);
+          const float a[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[r][j] = __fmaf_rn(a[i], b[i][j], acc[r][j]);
+        }
+      }
+    }
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();              // the ring's memory becomes the sums
+#pragma unroll
+  for (int r = 0; r < TM; ++r)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f32_smem[row_of(r) * kPitchSum + col_of(j)] = acc[r][j];
+  tc::cluster_sync_all();
+  auto sum = [&](int r, int c, float* v) {      // four neighbouring columns
+    const uint32_t at = base + (r * kPitchSum + c) * 4;
+    v[0] = v[1] = v[2] = v[3] = 0.f;
+    for (int s = 0; s < splits; ++s) {
+      float4 q;
+      asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(q.x), "=f"(q.y), "=f"(q.z), "=f"(q.w) : "r"(tc::map_to_cta(at, s)) : "memory");
+      v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w;
+    }
+  };
+  const int share = BM / splits, first = rank * share;
+  if (GATED) {
+    // a thread has eight hidden units of a row
+    for (int i = threadIdx.x; i < share * (kUnits / 8); i += kThreads) {
+      const int r = first + i / (kUnits / 8), c = i % (kUnits / 8) * 8, col = n0 + c;
+      if (r >= rows || c >= cols) continue;
+      Eight g, u;
+      sum(r, c, g.v);
+      sum(r, c + 4, g.v + 4);
+      sum(r, kUnits + c, u.v);
+      sum(r, kUnits + c + 4, u.v + 4);
+      const long long row = (long long)m * p.M + m0 + r;
+      if (p.z) {                // (whole groups: the pitch is a multiple of eight)
+        float* z = p.z + row * 2 * p.pitch + col;
+        store8(z, g);
+        store8(z + p.pitch, u);
+      }
+      if (!p.c) continue;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) g.v[e] = activation(p.activation, g.v[e]) * u.v[e];
+      if (p.drop) {
+        const dropout::Draw d = dropout::draw_of(p.rule, m);
+        const uint32_t in = dropout::kept_bits(d, (uint32_t)(m0 + r) * (uint32_t)((p.N + 7) / 8) + (uint32_t)(col / 8));
+        const float f = d.on ? d.scale : 1.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) g.v[e] = (in >> e & 1u) ? f * g.v[e] : 0.f;
+      }
+      float* h = p.c + row * p.ldc + col;
+      if (p.vec_c) {
+        store8(h, g);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (c + e < cols) h[e] = g.v[e];
+      }
+    }
+  } else {
+    for (int i = threadIdx.x; i < share * (kCols / 4); i += kThreads) {
+      const int r = first + i / (kCols / 4), c = i % (kCols / 4) * 4;
+      if (r >= rows || c >= cols) continue;
+      float v[4];
+      sum(r, c, v);
+      float* to = p.c + m * p.c_member + (m0 + r) * p.ldc + n0 + c;
+      if (p.vec_c) {
+        *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (c + e < cols) to[e] = v[e];
+      }
+    }
+  }
+  tc::cluster_sync_all();       // no CTA leaves while another reads its sums
+}
+
+template <typename S, bool A_MN, bool B_MN, bool GATED>
+cudaError_t launch(const pbt_gated_desc* d, ProductParams p, cudaStream_t s) {
+  static tc::DeviceSetup setup;
+  int sms = 0;
+  const cudaError_t e = tc::device_setup(&setup, k_gated_product_f32<S, A_MN, B_MN, GATED>, S::kFloats * 4, &sms);
+  if (e != cudaSuccess) return e;
+  constexpr int kUnits = GATED ? kCols / 2 : kCols;
+  p.tiles_n = (p.N + kUnits - 1) / kUnits;
+  const long long tiles = (long long)((p.M + S::BM - 1) / S::BM) * p.tiles_n;
+  // as many parts of the contraction as there are places for CTAs, two slices each at least
+  int splits = 1;
+  while (splits < kSplits && tiles * d->members * splits * 2 <= (long long)S::kPerSm * sms && (p.K + kK - 1) / kK >= splits * 2 * 2) splits *= 2;
+  if (tiles * splits > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(tiles * splits), (unsigned)d->members);
+  cfg.blockDim = dim3(S::kThreads);
+  cfg.dynamicSmemBytes = S::kFloats * 4;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)splits;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k_gated_product_f32<S, A_MN, B_MN, GATED>, p);
+}
+// Tall tiles where every SM has one at least, few rows in a tile of their own
+template <bool A_MN, bool B_MN, bool GATED>
+cudaError_t launch(const pbt_gated_desc* d, ProductParams p, cudaStream_t s) {
+  auto vectors = [&](const void* q, long long ld, long long member) {
+    return ((uintptr_t)q & 15) == 0 && ld % 4 == 0 && (d->members == 1 || member % 4 == 0);
+  };
+  p.vec_a = vectors(p.a, p.lda, p.a_member);
+  p.vec_b = vectors(p.b, p.ldb, p.b_member);
+  p.vec_c = vectors(p.c, p.ldc, p.c_member) && p.N % (GATED ? 8 : 4) == 0;
+  if constexpr (!A_MN)
+    if (p.M <= Few::BM) return launch<Few, A_MN, B_MN, GATED>(d, p, s);
+  const long long tall = (long long)((p.M + Tall::BM - 1) / Tall::BM) * ((p.N * (GATED ? 2 : 1) + kCols - 1) / kCols) * d->members;
+  return p.M > Short::BM && tall >= 148 ? launch<Tall, A_MN, B_MN, GATED>(d, p, s) : launch<Short, A_MN, B_MN, GATED>(d, p, s);
+}
+
+}  // namespace
+
+cudaError_t f32_forward(const pbt_gated_desc* d, float* h, float* z, int pitch, cudaStream_t s) {
+  ProductParams p = {};
+  p.a = (const float*)d->x; p.lda = d->x_row; p.a_member = d->x_member;
+  p.b = (const float*)d->weight; p.ldb = d->weight_row; p.b_member = d->weight_member;
+  p.c = h; p.ldc = d->hidden; p.c_member = (long long)d->rows * d->hidden;
+  p.M = d->rows; p.N = d->hidden; p.K = d->width;
+  p.z = z; p.pitch = pitch;
+  p.activation = d->activation; p.drop = d->drop != nullptr;
+  if (d->drop) p.rule = *d->drop;
+  return launch<false, false, true>(d, p, s);
+}
+
+cudaError_t f32_backward(const pbt_gated_desc* d, const float* dz, int dz_pitch, cudaStream_t s) {
+  ProductParams p = {};
+  p.a = dz; p.lda = dz_pitch; p.a_member = (long long)d->rows * dz_pitch;
+  p.b = (const float*)d->weight; p.ldb = d->weight_row; p.b_member = d->weight_member;
+  p.c = (float*)d->dx; p.ldc = d->width; p.c_member = (long long)d->rows * d->width;
+  p.M = d->rows; p.N = d->width; p.K = 2 * d->hidden;
+  const cudaError_t e = launch<false, true, false>(d, p, s);
+  if (e != cudaSuccess) return e;
+  p.b = (const float*)d->x; p.ldb = d->x_row; p.b_member = d->x_member;
+  p.c = (float*)d->dweight; p.c_member = 2ll * d->hidden * d->width;
+  p.M = 2 * d->hidden; p.K = d->rows;
+  return launch<true, true, false>(d, p, s);
+}
+
+}  // namespace gated
+}  // namespace pbt
