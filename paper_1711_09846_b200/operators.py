@@ -425,60 +425,62 @@ class AdapterProjection:
 # --- dropout -----------------------------------------------------------------------------------------------------------------
 
 
-class Dropout(NamedTuple):
+class Dropout:
     """Which elements of which member are dropped (pbt_drop_rule).  No mask is stored: both directions draw it from
     (seed; member, the member's step, site, place of the element).
 
     rate: a number, or float32 [members] on the device (a hyperparameter of every member, read when the kernels run); seed: 0 .. 2^64 - 1;
     step: a number, or int64 [members] on the device (the members' own step counts: what a captured graph that is
     replayed has to take, or it draws the same masks again); site: which dropout of the network (two with the same site and width draw
-    the same); first_member: index of the first member in the whole population, for a shard of it."""
-    rate: Union[float, torch.Tensor]
-    seed: int
-    step: Union[int, torch.Tensor]
-    site: int = 0
-    first_member: int = 0
+    the same); first_member: index of the first member in the whole population, for a shard of it.
 
+    The tensors are used where they lie: update them in place between calls.  Both passes of a step take the same object (or an equal one)."""
+    __slots__ = ("rate", "seed", "step", "site", "first_member", "tensors", "members", "device", "rule")
 
-def _drop_rule(drop, members, device):
-    rate, seed, step, site, first = drop
-    rates = steps = None
-    tensor, shape = torch.Tensor, (members,)
-    if isinstance(rate, tensor):
-        if not (rate.dtype is torch.float32 and rate.shape == shape and rate.device == device and rate.is_contiguous()):
-            raise ValueError("a dropout's rate is a number or a contiguous float32 tensor [members] on the activations' device")
-        rates, rate = rate.data_ptr(), 0.0
-    if isinstance(step, tensor):
-        if not (step.dtype is torch.int64 and step.shape == shape and step.device == device and step.is_contiguous()):
-            raise ValueError("a dropout's step is a number or a contiguous int64 tensor [members] on the activations' device")
-        steps, step = step.data_ptr(), 0
-    if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 63 and 0 <= site <= 1 << 30 and 0 <= first <= _MOST):
-        raise ValueError("a dropout's seed is a number of 64 bits; step, site (at most 2^30) and first_member are not negative")
-    return PbtDropRule(rates, steps, seed, step, rate, site, first)
+    def __init__(self, rate: Union[float, torch.Tensor], seed: int, step: Union[int, torch.Tensor], site: int = 0, first_member: int = 0):
+        self.rate, self.seed, self.step, self.site, self.first_member = rate, seed, step, site, first_member
+        self.tensors, rates, steps = (), None, None
+        if isinstance(rate, torch.Tensor):
+            _require(rate.is_cuda and rate.dtype is torch.float32 and rate.dim() == 1 and rate.is_contiguous(),
+                     "a dropout's rate is a number or a contiguous float32 tensor [members] on the device")
+            self.tensors, rates, rate = (rate,), rate.data_ptr(), 0.0
+        if isinstance(step, torch.Tensor):
+            _require(step.is_cuda and step.dtype is torch.int64 and step.dim() == 1 and step.is_contiguous(),
+                     "a dropout's step is a number or a contiguous int64 tensor [members] on the device")
+            self.tensors, steps, step = (*self.tensors, step), step.data_ptr(), 0
+        _require(0 <= seed < 1 << 64 and 0 <= step < 1 << 63 and 0 <= site <= 1 << 30 and 0 <= first_member <= _MOST,
+                 "a dropout's seed is a number of 64 bits; step, site (at most 2^30) and first_member are not negative")
+        _require(0 <= rate <= 1, "a dropout's rate lies in [0, 1]")
+        self.members, self.device = (self.tensors[0].shape[0], self.tensors[0].device) if self.tensors else (None, None)
+        _require(all(t.shape[0] == self.members and t.device == self.device for t in self.tensors), "a dropout's rate and step differ in members or device")
+        self.rule = PbtDropRule(rates, steps, seed, step, rate, site, first_member)
 
-
-def _drop_inputs(drop):
-    return () if drop is None else tuple(t for t in (drop.rate, drop.step) if isinstance(t, torch.Tensor))
+    def _for(self, members, device) -> PbtDropRule:
+        if self.members is not None and (self.members != members or self.device != device):
+            raise ValueError("a dropout's rate and step are [members] of the activations, on their device")
+        return self.rule
 
 
 def dropout_forward(x, dropout: Dropout, residual=None, stream=None):
     """residual + keep x / (1 - rate) (pbt_dropout); x and residual: [members, rows, width], float32 or bfloat16, with contiguous columns."""
-    shape, dtype, device = kind = x.shape, x.dtype, x.device
+    shape, dtype, device = x.shape, x.dtype, x.device
     if not (x.is_cuda and len(shape) == 3 and dtype in _TYPES):
         raise ValueError("activations are CUDA tensors [members, rows, width], float32 or bfloat16")
     m, rows, width = shape
     if m > _MOST or rows > _MOST or width > _MOST:
         raise ValueError("activations have at most 2^31 - 1 members, rows and columns")
-    at, member, row = _activation(x, kind, "x")
-    other, other_member, other_row = (None, 0, 0) if residual is None else _activation(residual, kind, "residual")
-    d = PbtDropoutDesc(m, rows, width, _TYPES[dtype], at, member, row, other, other_member, other_row, None, _drop_rule(dropout, m, device))
-    return _on(device, stream, () if stream is None else (x, residual, *_drop_inputs(dropout)), _dropout, d, x)
+    member, row, column = x.stride()
+    if column != 1 and width != 1:
+        raise ValueError("x has to have contiguous columns")
+    other, other_member, other_row = (None, 0, 0) if residual is None else _activation(residual, (shape, dtype, device), "residual")
+    d = PbtDropoutDesc(m, rows, width, _TYPES[dtype], x.data_ptr(), member, row, other, other_member, other_row, None, dropout._for(m, device))
+    return _on(device, stream, () if stream is None else (x, residual, *dropout.tensors), _dropout, d, x)
 
 
 def _dropout(s, d, x):
     y = _like(x)
     d.y = y.data_ptr()
-    rc = load_library().pbt_dropout(C.byref(d), s)
+    rc = load_library().pbt_dropout(d, s)
     if rc:
         _check(rc)
     return y
@@ -525,27 +527,25 @@ class GatedUnit:
         _check(self.lib.pbt_gated_query_workspace(C.byref(d), 0, C.byref(C.c_size_t(0))))
 
     def _call(self, x, dropout):
-        """The description of a call on these rows (a copy: calls from several threads do not share it), and the dropout it points to, which has to
-        live until the call has been enqueued."""
+        """The description of a call on these rows (a copy: calls from several threads do not share it)."""
         w, shape = self.weight, x.shape
-        if not (len(shape) == 3 and shape[0] == self._desc.members and shape[2] == self._desc.width and x.dtype == w.dtype and x.device == w.device):
+        device = w.device
+        d = PbtGatedDesc.from_buffer_copy(self._desc)
+        if not (len(shape) == 3 and shape[0] == d.members and shape[2] == d.width and x.dtype is w.dtype and x.device == device):
             raise ValueError("x is [members, rows, width] of the weight's members, width, type and device")
         if shape[1] > _MOST:
             raise ValueError("a call has at most 2^31 - 1 rows")
-        d = PbtGatedDesc.from_buffer_copy(self._desc)
         d.rows = shape[1]
         d.x, d.x_member, d.x_row = _rows_of(x, "x")
-        rule = None
         if dropout is not None:
-            rule = _drop_rule(dropout, d.members, w.device)
-            d.drop = C.addressof(rule)
-        return d, rule
+            d.drop = C.addressof(dropout._for(d.members, device))
+        return d
 
     def forward(self, x, dropout: Optional[Dropout] = None, keep: bool = False, stream=None):
         """h [members, rows, hidden]; with keep, also g and u in float32 for the backward pass (8 bytes a hidden unit; without
         them it works them out anew, which costs two thirds of a forward pass more)."""
-        d, _rule = self._call(x, dropout)
-        inputs = () if stream is None else (x, self.weight, *_drop_inputs(dropout))
+        d = self._call(x, dropout)
+        inputs = () if stream is None else (x, self.weight, *(dropout.tensors if dropout else ()))
         return _on(self.weight.device, stream, inputs, self._forward, d, keep)
 
     def _forward(self, s, d, keep):
@@ -563,7 +563,7 @@ class GatedUnit:
     def backward(self, dh, x, kept=None, dropout: Optional[Dropout] = None, stream=None):
         """(dx, dweight) from dh [members, rows, hidden], the forward pass's x, what it kept (or None) and its dropout.  dweight is
         [members, 2 hidden, width] of the weight's type, every member's own even where the weight is one for all."""
-        d, _rule = self._call(x, dropout)
+        d = self._call(x, dropout)
         w = self.weight
         if not (dh.shape == (d.members, d.rows, d.hidden) and dh.dtype == w.dtype and dh.device == w.device):
             raise ValueError("dh is [members, rows, hidden] of the weight's type and device")
@@ -573,7 +573,7 @@ class GatedUnit:
                     and kept.is_contiguous()):
                 raise ValueError("kept is what forward(keep=True) returned")
             d.kept = kept.data_ptr()
-        inputs = () if stream is None else (dh, x, kept, w, *_drop_inputs(dropout))
+        inputs = () if stream is None else (dh, x, kept, w, *(dropout.tensors if dropout else ()))
         return _on(w.device, stream, inputs, self._backward, d)
 
     def _backward(self, s, d):
@@ -595,8 +595,8 @@ class GatedUnit:
         if s != self._home:      # keeps the status words until the call is done, should the object go first
             self._status.record_stream(torch.cuda.current_stream(self.weight.device))
         at = C.byref(d)
-        # a bfloat16 forward pass needs a workspace for rows of odd sizes only: asking for its size costs a small call as much as its checks
-        rc = _NO_WORKSPACE if backward or not d.dtype else call(at, None, 0, s)
+        # a forward pass needs a workspace for bfloat16 rows of odd sizes only: asking for its size costs a small call as much as its checks
+        rc = _NO_WORKSPACE if backward else call(at, None, 0, s)
         if rc == _NO_WORKSPACE:
             nbytes = C.c_size_t(0)
             rc = self.lib.pbt_gated_query_workspace(at, backward, C.byref(nbytes))

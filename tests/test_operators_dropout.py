@@ -238,18 +238,17 @@ def test_refusals_and_empty_batches():
     x = torch.ones(2, 3, 16, device="cuda")
     ok = pbt.Dropout(0.5, 1, 2)
     assert pbt.dropout_forward(x[:, :0], ok).shape == (2, 0, 16)
-    bad = [(x.cpu(), ok, None), (x[0], ok, None), (x.double(), ok, None), (x, ok, x.bfloat16()), (x, ok, x[:1]), (x, ok, x.cpu()),
-           (x.transpose(1, 2), ok, None)]
-    for change in (dict(rate=torch.ones(3, device="cuda")), dict(rate=torch.ones(2)), dict(rate=torch.ones(2, device="cuda").double()),
-                   dict(rate=torch.ones(4, device="cuda")[::2]), dict(step=torch.ones(2, device="cuda")), dict(step=torch.ones(2, dtype=torch.int64)),
-                   dict(step=-1), dict(step=1 << 63), dict(seed=-1), dict(seed=1 << 64), dict(site=-1), dict(site=1 << 31), dict(first_member=-1),
-                   dict(first_member=1 << 32)):
-        bad.append((x, ok._replace(**change), None))
-    for a, drop, r in bad:
+    for a, r in ((x.cpu(), None), (x[0], None), (x.double(), None), (x, x.bfloat16()), (x, x[:1]), (x, x.cpu()), (x.transpose(1, 2), None), (x, x.transpose(1, 2))):
         with pytest.raises(ValueError):
-            pbt.dropout_forward(a, drop, residual=r)
-    for rate in (1.5, -0.1, float("nan")):
-        with pytest.raises(pbt.PbtError):
-            pbt.dropout_forward(x, ok._replace(rate=rate))
+            pbt.dropout_forward(a, ok, residual=r)
+    two, three = torch.ones(2, device="cuda"), torch.ones(3, device="cuda")
+    for drop in (pbt.Dropout(three, 1, 2), pbt.Dropout(0.5, 1, three.long())):           # of another number of members
+        with pytest.raises(ValueError):
+            pbt.dropout_forward(x, drop)
+    for args in (dict(rate=two.cpu()), dict(rate=two.double()), dict(rate=torch.ones(4, device="cuda")[::2]), dict(rate=x[0]), dict(step=two), dict(step=two.long().cpu()),
+                 dict(rate=two, step=three.long()), dict(step=-1), dict(step=1 << 63), dict(seed=-1), dict(seed=1 << 64), dict(site=-1), dict(site=1 << 31),
+                 dict(first_member=-1), dict(first_member=1 << 32), dict(rate=1.5), dict(rate=-0.1), dict(rate=float("nan"))):
+        with pytest.raises(ValueError):
+            pbt.Dropout(**{**dict(rate=0.5, seed=1, step=2), **args})
     with pytest.raises(pbt.PbtError):
-        pbt.dropout_forward(x, ok._replace(first_member=0x7FFFFFFF))
+        pbt.dropout_forward(x, pbt.Dropout(0.5, 1, 2, first_member=0x7FFFFFFF))

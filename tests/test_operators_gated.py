@@ -356,7 +356,7 @@ def test_nothing_is_written_beside_the_results(shape, dtype):
         return t, t[guard:guard + n]
     sizes = dict(h=m * rows * hidden * size, kept=m * rows * 2 * ((hidden + 7) // 8 * 8) * 4, dx=m * rows * width * size, dweight=m * 2 * hidden * width * size)
     places = {k: between(n) for k, n in sizes.items()}
-    d, _rule = layer._call(c["x"], c["dropout"])
+    d = layer._call(c["x"], c["dropout"])
     d.dh, d.dh_member, d.dh_row = c["dh"].data_ptr(), c["dh"].stride(0), c["dh"].stride(1)
     for k, (_, t) in places.items():
         setattr(d, k, t.data_ptr())
@@ -408,10 +408,12 @@ def test_the_c_calls_refuse_what_they_cannot_do():
     for kw in (dict(dh=None), dict(dx=None), dict(dweight=None), dict(dh_row=7), dict(dh_member=-1)):
         assert lib.pbt_gated_backward(C.byref(desc(**kw)), 4096, 1 << 60, None) == 1, kw
     assert lib.pbt_gated_forward(C.byref(desc(rows=0, x=None, h=None)), None, 0, None) == 0         # nothing to do
-    for kw in (dict(dtype=0, kept=None), dict(x=4098), dict(weight_row=9)):       # these need one
+    for kw in (dict(x=4098), dict(weight_row=9)):       # these need one
         assert lib.pbt_gated_query_workspace(C.byref(desc(**kw)), 0, C.byref(n)) == 0 and n.value > 0
         assert lib.pbt_gated_forward(C.byref(desc(**kw)), None, 1 << 20, None) == 3 and lib.pbt_gated_backward(C.byref(desc(**kw)), None, 1 << 20, None) == 3
-    assert lib.pbt_gated_query_workspace(C.byref(desc()), 0, C.byref(n)) == 0 and n.value == 0
+    for dtype in (0, 1):
+        assert lib.pbt_gated_query_workspace(C.byref(desc(dtype=dtype)), 0, C.byref(n)) == 0 and n.value == 0
+    assert lib.pbt_gated_query_workspace(C.byref(desc(x_row=9, dtype=0)), 0, C.byref(n)) == 0 and n.value == 0
 
 
 @pytest.mark.gpu
@@ -439,7 +441,7 @@ def test_refusals_and_empty_batches():
     with pytest.raises(ValueError):
         layer.forward(x, dropout=pbt.Dropout(torch.ones(3, device="cuda"), 1, 2))
     with pytest.raises(pbt.PbtError):
-        layer.forward(x, dropout=pbt.Dropout(1.5, 1, 2))
+        layer.forward(x, dropout=pbt.Dropout(0.5, 1, 2, first_member=0x7FFFFFFF))
     with pytest.raises(pbt.PbtError):
         layer.forward(x[:, :1].expand(2, 3, 24))       # rows that lie on one another
     many = torch.empty(2, 1, 24, device="cuda").expand(2, 2 ** 32 + 3, 24)
