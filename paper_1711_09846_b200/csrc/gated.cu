@@ -43,6 +43,7 @@ struct CellArgs {
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) k_gated_cells(const CellArgs<T> a) {
   pdl_prologue();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the products may begin with their other operands
   const int m = blockIdx.y;
   const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= (uint64_t)a.rows * a.groups) return;
@@ -208,20 +209,21 @@ cudaError_t backward(const pbt_gated_desc* d, char* ws, cudaStream_t s) {
   e = launch_cells<T>(d, a, s);
   if (e != cudaSuccess) return e;
   if (!d->dtype) return f32_backward(d, (const float*)dz, p.dz_pitch, s);
+  const Operand left = {(const bf16*)dz, p.dz_pitch, (long long)d->rows * p.dz_pitch};
+  if (tc_gradients_few(d)) return tc_gradients(d, left, o.w, o.x, s);
   GemmArgs g = product(d);
   g.A = dz; g.lda = p.dz_pitch; g.strideA = (long long)d->rows * p.dz_pitch;
   g.M = d->rows; g.N = d->width; g.K = 2 * d->hidden;
   g.b_mn = 1;
   g.B = o.w.p; g.ldb = o.w.row; g.strideB = o.w.member;
   g.C = d->dx; g.ldc = d->width; g.strideC = (long long)d->rows * d->width;
-  if (tc_dx_few(d)) e = tc_dx(d, {(const bf16*)dz, p.dz_pitch, (long long)d->rows * p.dz_pitch}, o.w, s);
+  if (tc_dx_few(d)) e = tc_dx(d, left, o.w, s);
   else e = run_product(d, g, s);
   if (e != cudaSuccess) return e;
   g.a_mn = 1;
   g.M = 2 * d->hidden; g.K = d->rows;
   g.B = o.x.p; g.ldb = o.x.row; g.strideB = o.x.member;
   g.C = d->dweight; g.strideC = 2ll * d->hidden * d->width;
-  if (tc_outer_supported(d)) return tc_outer(d, (const bf16*)dz, p.dz_pitch, o.x, s);
   return run_product(d, g, s);
 }
 

@@ -21,17 +21,36 @@ struct PackSource {
 };
 cudaError_t tc_pack(const PackSource* src, int n, cudaStream_t s);      // one or two
 cudaError_t tc_forward(const pbt_gated_desc* d, const Operand& x, const Operand& w, void* h, float* z, int pitch, cudaStream_t s);
-// dx = [dg du] W by CTAs that share a contraction, for few rows
+// dx = [dg du] W by CTAs that share a contraction, for few rows; launched right behind the kernel that makes dg and du
 bool tc_dx_few(const pbt_gated_desc* d);
 cudaError_t tc_dx(const pbt_gated_desc* d, const Operand& dz, const Operand& w, cudaStream_t s);
-// dW of a few rows
-bool tc_outer_supported(const pbt_gated_desc* d);
-cudaError_t tc_outer(const pbt_gated_desc* d, const bf16* dz, int dz_pitch, const Operand& x, cudaStream_t s);
+// dx and dW of still fewer rows in one launch
+bool tc_gradients_few(const pbt_gated_desc* d);
+cudaError_t tc_gradients(const pbt_gated_desc* d, const Operand& dz, const Operand& w, const Operand& x, cudaStream_t s);
 // float (gated_f32.cu): h (or null) and g, u (or null); dx and dW
 cudaError_t f32_forward(const pbt_gated_desc* d, float* h, float* z, int pitch, cudaStream_t s);
 cudaError_t f32_backward(const pbt_gated_desc* d, const float* dz, int dz_pitch, cudaStream_t s);
 
 #ifdef __CUDACC__
+// Launches clusters of `cluster` CTAs; `after`: they may begin while the predecessor in the stream still runs (see launch_after).
+template <typename... KArgs, typename... Args>
+cudaError_t launch_clusters(dim3 grid, unsigned threads, size_t smem, unsigned cluster, bool after, cudaStream_t s, void (*kernel)(KArgs...), Args&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = after ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, KArgs(static_cast<Args&&>(args))...);
+}
+
 // act(g)
 __device__ __forceinline__ float activation(int kind, float g) {
   if (kind == kRelu) return g <= 0.f ? 0.f : g;                       // (NaN stays NaN)

@@ -79,13 +79,10 @@ __device__ __forceinline__ void copy_box(uint32_t to, const float* from, long lo
 // vectors of four of those.  The CTAs of a cluster share the contraction; every one adds up its share of the tile's rows over all their sums, in
 // their order.
 template <typename S, bool A_MN, bool B_MN, bool GATED>
-__global__ void __launch_bounds__(S::kThreads, S::kPerSm) k_gated_product_f32(const ProductParams p) {
-  pdl_prologue();
-  extern __shared__ __align__(16) float f32_smem[];
+__device__ __forceinline__ void product_tile(const ProductParams& p, float* f32_smem, int tile, int m, int splits, int rank) {
   constexpr int BM = S::BM, TM = S::TM, kThreads = S::kThreads, kPitchM = BM + 4, kPitchN = kCols + 4;
   static_assert(!A_MN || TM == 8, "rows of m are read in vectors");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tx = lane & 7, ty = warp * 4 + (lane >> 3);
-  const int splits = (int)tc::cluster_size(), rank = (int)tc::cluster_ctarank(), tile = blockIdx.x / splits, m = blockIdx.y;
   constexpr int kUnits = GATED ? kCols / 2 : kCols;
   const int m0 = tile / p.tiles_n * BM, n0 = tile % p.tiles_n * kUnits, rows = min(BM, p.M - m0), cols = min(kUnits, p.N - n0);
   const int slices = (p.K + kK - 1) / kK, s0 = (int)((long long)slices * rank / splits), s1 = (int)((long long)slices * (rank + 1) / splits);
@@ -167,9 +164,15 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) k_gated_product_f32(co
   for (int r = 0; r < TM; ++r)
 #pragma unroll
     for (int j = 0; j < 8; ++j) f32_smem[row_of(r) * kPitchSum + col_of(j)] = acc[r][j];
-  tc::cluster_sync_all();
+  if (splits > 1) tc::cluster_sync_all();
+  else __syncthreads();
   auto sum = [&](int r, int c, float* v) {      // four neighbouring columns
     const uint32_t at = base + (r * kPitchSum + c) * 4;
+    if (splits == 1) {
+      const float4 q = *reinterpret_cast<const float4*>(f32_smem + r * kPitchSum + c);
+      v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+      return;
+    }
     v[0] = v[1] = v[2] = v[3] = 0.f;
     for (int s = 0; s < splits; ++s) {
       float4 q;
@@ -229,48 +232,88 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) k_gated_product_f32(co
       }
     }
   }
-  tc::cluster_sync_all();       // no CTA leaves while another reads its sums
+  if (splits > 1) tc::cluster_sync_all();       // no CTA leaves while another reads its sums
 }
 
-template <typename S, bool A_MN, bool B_MN, bool GATED>
-cudaError_t launch(const pbt_gated_desc* d, ProductParams p, cudaStream_t s) {
-  static tc::DeviceSetup setup;
-  int sms = 0;
-  const cudaError_t e = tc::device_setup(&setup, k_gated_product_f32<S, A_MN, B_MN, GATED>, S::kFloats * 4, &sms);
-  if (e != cudaSuccess) return e;
-  constexpr int kUnits = GATED ? kCols / 2 : kCols;
-  p.tiles_n = (p.N + kUnits - 1) / kUnits;
-  const long long tiles = (long long)((p.M + S::BM - 1) / S::BM) * p.tiles_n;
-  // as many parts of the contraction as there are places for CTAs, two slices each at least
-  int splits = 1;
-  while (splits < kSplits && tiles * d->members * splits * 2 <= (long long)S::kPerSm * sms && (p.K + kK - 1) / kK >= splits * 2 * 2) splits *= 2;
-  if (tiles * splits > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(tiles * splits), (unsigned)d->members);
-  cfg.blockDim = dim3(S::kThreads);
-  cfg.dynamicSmemBytes = S::kFloats * 4;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)splits;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k_gated_product_f32<S, A_MN, B_MN, GATED>, p);
+template <typename S>
+__global__ void __launch_bounds__(S::kThreads, S::kPerSm) k_gated_forward_f32(const ProductParams p) {
+  pdl_prologue();
+  extern __shared__ __align__(16) float f32_smem[];
+  const int splits = (int)tc::cluster_size();
+  product_tile<S, false, false, true>(p, f32_smem, blockIdx.x / splits, blockIdx.y, splits, (int)tc::cluster_ctarank());
 }
-// Tall tiles where every SM has one at least, few rows in a tile of their own
-template <bool A_MN, bool B_MN, bool GATED>
-cudaError_t launch(const pbt_gated_desc* d, ProductParams p, cudaStream_t s) {
+// The CTAs of dx first, then those of dW, a cluster or one for a tile; launched while the kernel that makes dg and du runs.
+struct GradientParams {
+  ProductParams dx, dw;
+  int dx_tiles, dw_tiles, dx_splits, dw_splits, dx_blocks, members;      // tiles of a member; CTAs of a tile (1, or the cluster's); CTAs of all members
+  long long blocks;                                              // CTAs that have work (dx's are a whole number of clusters)
+};
+template <typename SX, typename SW>
+struct GradientShape {
+  static constexpr int kFloats = SX::kFloats > SW::kFloats ? SX::kFloats : SW::kFloats, kPerSm = SX::kPerSm < SW::kPerSm ? SX::kPerSm : SW::kPerSm;
+  static_assert(SX::kThreads == SW::kThreads, "one launch");
+};
+template <typename SX, typename SW>
+__global__ void __launch_bounds__(SX::kThreads, GradientShape<SX, SW>::kPerSm) k_gated_gradients_f32(const GradientParams p) {
+  extern __shared__ __align__(16) float f32_smem[];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int rank = (int)tc::cluster_ctarank();
+  if ((int)blockIdx.x < p.dx_blocks) {
+    const int i = (int)blockIdx.x / p.dx_splits;
+    if (i < p.dx_tiles * p.members) product_tile<SX, false, true, false>(p.dx, f32_smem, i % p.dx_tiles, i / p.dx_tiles, p.dx_splits, p.dx_splits > 1 ? rank : 0);
+  } else if (blockIdx.x < p.blocks) {
+    const int i = ((int)blockIdx.x - p.dx_blocks) / p.dw_splits;
+    product_tile<SW, true, true, false>(p.dw, f32_smem, i % p.dw_tiles, i / p.dw_tiles, p.dw_splits, p.dw_splits > 1 ? rank : 0);
+  }
+}
+
+void fill(const pbt_gated_desc* d, ProductParams* p, bool gated) {
   auto vectors = [&](const void* q, long long ld, long long member) {
     return ((uintptr_t)q & 15) == 0 && ld % 4 == 0 && (d->members == 1 || member % 4 == 0);
   };
-  p.vec_a = vectors(p.a, p.lda, p.a_member);
-  p.vec_b = vectors(p.b, p.ldb, p.b_member);
-  p.vec_c = vectors(p.c, p.ldc, p.c_member) && p.N % (GATED ? 8 : 4) == 0;
-  if constexpr (!A_MN)
-    if (p.M <= Few::BM) return launch<Few, A_MN, B_MN, GATED>(d, p, s);
-  const long long tall = (long long)((p.M + Tall::BM - 1) / Tall::BM) * ((p.N * (GATED ? 2 : 1) + kCols - 1) / kCols) * d->members;
-  return p.M > Short::BM && tall >= 148 ? launch<Tall, A_MN, B_MN, GATED>(d, p, s) : launch<Short, A_MN, B_MN, GATED>(d, p, s);
+  p->vec_a = vectors(p->a, p->lda, p->a_member);
+  p->vec_b = vectors(p->b, p->ldb, p->b_member);
+  p->vec_c = vectors(p->c, p->ldc, p->c_member) && p->N % (gated ? 8 : 4) == 0;
+  const int units = gated ? kCols / 2 : kCols;
+  p->tiles_n = (p->N + units - 1) / units;
+}
+template <typename S>
+long long tiles_of(const ProductParams& p) { return (long long)((p.M + S::BM - 1) / S::BM) * p.tiles_n; }
+// as many parts of a contraction as there are places for CTAs, two slices each at least
+int splits_of(long long tiles, int K, long long places) {
+  int splits = 1;
+  while (splits < kSplits && tiles * splits * 2 <= places && (K + kK - 1) / kK >= splits * 2 * 2) splits *= 2;
+  return splits;
+}
+// Tall tiles where every SM has one at least
+bool tall(const pbt_gated_desc* d, const ProductParams& p) { return p.M > Short::BM && tiles_of<Tall>(p) * d->members >= 148; }
+
+template <typename S>
+cudaError_t launch_forward(const pbt_gated_desc* d, const ProductParams& p, cudaStream_t s) {
+  static tc::DeviceSetup setup;
+  int sms = 0;
+  const cudaError_t e = tc::device_setup(&setup, k_gated_forward_f32<S>, S::kFloats * 4, &sms);
+  if (e != cudaSuccess) return e;
+  const long long tiles = tiles_of<S>(p);
+  const int splits = splits_of(tiles * d->members, p.K, (long long)S::kPerSm * sms);
+  if (tiles * splits > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
+  return launch_clusters(dim3((unsigned)(tiles * splits), (unsigned)d->members), S::kThreads, S::kFloats * 4, splits, false, s, k_gated_forward_f32<S>, p);
+}
+template <typename SX, typename SW>
+cudaError_t launch_gradients(const pbt_gated_desc* d, const ProductParams& dx, const ProductParams& dw, cudaStream_t s) {
+  typedef GradientShape<SX, SW> G;
+  static tc::DeviceSetup setup;
+  int sms = 0;
+  const cudaError_t e = tc::device_setup(&setup, k_gated_gradients_f32<SX, SW>, G::kFloats * 4, &sms);
+  if (e != cudaSuccess) return e;
+  const long long tx = tiles_of<SX>(dx) * d->members, tw = tiles_of<SW>(dw) * d->members, places = (long long)G::kPerSm * sms;
+  const int sx = splits_of(tx, dx.K, places), sw = splits_of(tw, dw.K, places), cluster = std::max(sx, sw);
+  GradientParams p = {dx, dw, (int)tiles_of<SX>(dx), (int)tiles_of<SW>(dw), sx > 1 ? cluster : 1, sw > 1 ? cluster : 1, 0, d->members, 0};
+  const long long first = (tx * p.dx_splits + cluster - 1) / cluster * cluster;
+  p.blocks = first + tw * p.dw_splits;
+  if (p.blocks + cluster > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
+  p.dx_blocks = (int)first;
+  return launch_clusters(dim3((unsigned)((p.blocks + cluster - 1) / cluster * cluster)), SX::kThreads, G::kFloats * 4, cluster, true, s, k_gated_gradients_f32<SX, SW>, p);
 }
 
 }  // namespace
@@ -284,7 +327,9 @@ cudaError_t f32_forward(const pbt_gated_desc* d, float* h, float* z, int pitch, 
   p.z = z; p.pitch = pitch;
   p.activation = d->activation; p.drop = d->drop != nullptr;
   if (d->drop) p.rule = *d->drop;
-  return launch<false, false, true>(d, p, s);
+  fill(d, &p, true);
+  if (p.M <= Few::BM) return launch_forward<Few>(d, p, s);
+  return tall(d, p) ? launch_forward<Tall>(d, p, s) : launch_forward<Short>(d, p, s);
 }
 
 cudaError_t f32_backward(const pbt_gated_desc* d, const float* dz, int dz_pitch, cudaStream_t s) {
@@ -293,12 +338,14 @@ cudaError_t f32_backward(const pbt_gated_desc* d, const float* dz, int dz_pitch,
   p.b = (const float*)d->weight; p.ldb = d->weight_row; p.b_member = d->weight_member;
   p.c = (float*)d->dx; p.ldc = d->width; p.c_member = (long long)d->rows * d->width;
   p.M = d->rows; p.N = d->width; p.K = 2 * d->hidden;
-  const cudaError_t e = launch<false, true, false>(d, p, s);
-  if (e != cudaSuccess) return e;
-  p.b = (const float*)d->x; p.ldb = d->x_row; p.b_member = d->x_member;
-  p.c = (float*)d->dweight; p.c_member = 2ll * d->hidden * d->width;
-  p.M = 2 * d->hidden; p.K = d->rows;
-  return launch<true, true, false>(d, p, s);
+  ProductParams dw = p;
+  dw.b = (const float*)d->x; dw.ldb = d->x_row; dw.b_member = d->x_member;
+  dw.c = (float*)d->dweight; dw.c_member = 2ll * d->hidden * d->width;
+  dw.M = 2 * d->hidden; dw.K = d->rows;
+  fill(d, &p, false);
+  fill(d, &dw, false);
+  if (p.M <= Few::BM) return launch_gradients<Few, Short>(d, p, dw, s);
+  return tall(d, p) ? launch_gradients<Tall, Tall>(d, p, dw, s) : launch_gradients<Short, Short>(d, p, dw, s);
 }
 
 }  // namespace gated

@@ -366,12 +366,10 @@ __device__ __forceinline__ float4 ld_cluster(uint32_t addr) {
   return v;
 }
 
-template <int N, bool DX>
-__global__ void __launch_bounds__(kRowsThreads, RowsTile<N>::kPerSm) k_gated_rows(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const RowsParams p) {
-  pdl_prologue();
+template <int N, bool DX, int THREADS>
+__device__ __forceinline__ void rows_product(const CUtensorMap& tmA, const CUtensorMap& tmB, const RowsParams& p, uint8_t* smem_raw, int tile, int m, int t0) {
   typedef RowsTile<N> L;
   constexpr int kUnits = DX ? kRowsLanes : kRowsLanes / 2;       // hidden units, or columns of dx
-  extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBars);
   uint64_t* empty = full + L::kStages;
@@ -379,8 +377,7 @@ __global__ void __launch_bounds__(kRowsThreads, RowsTile<N>::kPerSm) k_gated_row
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int splits = (int)cluster_size(), rank = (int)cluster_ctarank();
-  const int n0 = (int)(blockIdx.x / splits) * kUnits, m = blockIdx.y / p.blocks, t0 = (int)(blockIdx.y % p.blocks) * N;
+  const int splits = (int)cluster_size(), rank = (int)cluster_ctarank(), n0 = tile * kUnits;
   const int kb0 = (int)((long long)p.k_blocks * rank / splits), kb1 = (int)((long long)p.k_blocks * (rank + 1) / splits);
   if (threadIdx.x == 0) {
     for (int s = 0; s < L::kStages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
@@ -405,17 +402,26 @@ __global__ void __launch_bounds__(kRowsThreads, RowsTile<N>::kPerSm) k_gated_row
     if (lane == 0) {
       uint32_t stage = 0, phase = 0;
       bool ok = true;
-      for (int kb = kb0; kb < kb1; ++kb) {
-        if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) { ok = false; break; }
-        uint8_t* to = smem + stage * L::kStage;
-        mbar_expect_tx(&full[stage], L::kStage);
-        const int k0 = kb * kBK, ma = p.a_batched ? m : 0;
+      const int ma = p.a_batched ? m : 0, mb = p.b_batched ? m : 0;
+      auto load_a = [&](int kb, uint8_t* to, uint64_t* bar) {
+        mbar_expect_tx(bar, L::kStage);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          if (DX) tma_load_3d(to + half * 8192, &tmA, &full[stage], n0 + half * 64, k0, ma);
-          else tma_load_3d(to + half * 8192, &tmA, &full[stage], k0, half * p.hidden + n0, ma);
+          if (DX) tma_load_3d(to + half * 8192, &tmA, bar, n0 + half * 64, kb * kBK, ma);
+          else tma_load_3d(to + half * 8192, &tmA, bar, kb * kBK, half * p.hidden + n0, ma);
         }
-        tma_load_3d(to + 16384, &tmB, &full[stage], k0, t0, p.b_batched ? m : 0);
+      };
+      // the weight of the first blocks is asked for before dg and du are there
+      const int first = DX ? min(L::kStages, kb1 - kb0) : 0;
+      for (int i = 0; i < first; ++i) load_a(kb0 + i, smem + i * L::kStage, &full[i]);
+      if (DX) asm volatile("griddepcontrol.wait;\n\tgriddepcontrol.launch_dependents;" ::: "memory");      // dW may begin: it needs nothing of dx
+      for (int kb = kb0; kb < kb1; ++kb) {
+        uint8_t* to = smem + stage * L::kStage;
+        if (kb - kb0 >= first) {
+          if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) { ok = false; break; }
+          load_a(kb, to, &full[stage]);
+        }
+        tma_load_3d(to + 16384, &tmB, &full[stage], kb * kBK, t0, mb);
         if (++stage == L::kStages) { stage = 0; phase ^= 1; }
       }
       if (!ok) give_up(41);
@@ -445,7 +451,7 @@ __global__ void __launch_bounds__(kRowsThreads, RowsTile<N>::kPerSm) k_gated_row
   }
   __syncthreads();                // all loads have landed and all products are complete: the ring's memory becomes the sums
   const bool ok = *abort_flag == 0;
-  if (warp >= 2 && ok) {
+  if (warp >= 2 && warp < 6 && ok) {
     tc_fence_after();
     const int q = warp & 3;
     constexpr int kCols = N < 32 ? N : 32;
@@ -461,7 +467,7 @@ __global__ void __launch_bounds__(kRowsThreads, RowsTile<N>::kPerSm) k_gated_row
   }
   cluster_sync_all();
   // a thread has eight hidden units (columns) of a row
-  for (int i = threadIdx.x; i < N / splits * (kUnits / 8); i += kRowsThreads) {
+  for (int i = threadIdx.x; i < N / splits * (kUnits / 8); i += THREADS) {
     const int c = rank * (N / splits) + i / (kUnits / 8), t = t0 + c, j = i % (kUnits / 8) * 8, col = n0 + j, end = DX ? p.width : p.hidden;
     if (!ok || t >= p.rows || col >= end) continue;
     Eight g = {}, u = {};
@@ -508,6 +514,13 @@ __global__ void __launch_bounds__(kRowsThreads, RowsTile<N>::kPerSm) k_gated_row
   cluster_sync_all();             // no CTA leaves while another reads its sums
   if (warp == 1) tmem_dealloc(tmem, L::kCols);
 }
+// DX: launched while the kernel that makes dg and du runs
+template <int N, bool DX>
+__global__ void __launch_bounds__(kRowsThreads, RowsTile<N>::kPerSm) k_gated_rows(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const RowsParams p) {
+  if (!DX) pdl_prologue();
+  extern __shared__ uint8_t smem_raw[];
+  rows_product<N, DX, kRowsThreads>(tmA, tmB, p, smem_raw, (int)(blockIdx.x / cluster_size()), blockIdx.y / p.blocks, (int)(blockIdx.y % p.blocks) * N);
+}
 
 // the parts of a contraction: as many as there are places for CTAs, four blocks each at least
 int rows_splits(long long tiles, int k_blocks, long long places) {
@@ -523,44 +536,33 @@ cudaError_t launch_rows(const pbt_gated_desc* d, const RowsParams& p, const CUte
   if (e != cudaSuccess) return e;
   const unsigned units = DX ? (d->width + 127) / 128 : (d->hidden + 63) / 64, blocks = (unsigned)p.blocks * d->members;
   const int splits = rows_splits((long long)units * blocks, p.k_blocks, (long long)sms * RowsTile<N>::kPerSm);
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(units * splits, blocks);
-  cfg.blockDim = dim3(kRowsThreads);
-  cfg.dynamicSmemBytes = RowsTile<N>::kTotal;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)splits;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k_gated_rows<N, DX>, tmA, tmB, p);
+  return launch_clusters(dim3(units * splits, blocks), kRowsThreads, RowsTile<N>::kTotal, splits, DX, s, k_gated_rows<N, DX>, tmA, tmB, p);
 }
-template <bool DX>
-cudaError_t launch_rows(const pbt_gated_desc* d, RowsParams& p, const CUtensorMap& tmA, const Operand& b, int k, cudaStream_t s) {
-  const int n = d->rows <= 16 ? 16 : d->rows <= 32 ? 32 : d->rows <= 64 ? 64 : 128;
-  p.rows = d->rows; p.hidden = d->hidden; p.width = d->width;
-  p.blocks = (d->rows + n - 1) / n;
-  p.k_blocks = (k + kBK - 1) / kBK;
-  p.b_batched = d->members > 1 && b.member != 0;
-  p.vec = (DX ? d->width : d->hidden) % 8 == 0 && ((uintptr_t)p.out & 15) == 0;
-  p.counters = (Counters*)d->status_device;
-  CUtensorMap tmB;
-  if (!make_map(&tmB, b.p, k, d->rows, b.row, p.b_batched ? d->members : 1, b.member, n)) return cudaErrorInvalidValue;
-  switch (n) {
-    case 16: return launch_rows<16, DX>(d, p, tmA, tmB, s);
-    case 32: return launch_rows<32, DX>(d, p, tmA, tmB, s);
-    case 64: return launch_rows<64, DX>(d, p, tmA, tmB, s);
-    default: return launch_rows<128, DX>(d, p, tmA, tmB, s);
-  }
+int rows_columns(const pbt_gated_desc* d) { return d->rows <= 16 ? 16 : d->rows <= 32 ? 32 : d->rows <= 64 ? 64 : 128; }
+// what the two products of this form have in common; k: their contraction
+bool rows_params(const pbt_gated_desc* d, bool dx, const Operand& b, int k, RowsParams* p, CUtensorMap* tmB) {
+  const int n = rows_columns(d);
+  p->rows = d->rows; p->hidden = d->hidden; p->width = d->width;
+  p->blocks = (d->rows + n - 1) / n;
+  p->k_blocks = (k + kBK - 1) / kBK;
+  p->b_batched = d->members > 1 && b.member != 0;
+  p->vec = (dx ? d->width : d->hidden) % 8 == 0 && ((uintptr_t)p->out & 15) == 0;
+  p->counters = (Counters*)d->status_device;
+  return make_map(tmB, b.p, k, d->rows, b.row, p->b_batched ? d->members : 1, b.member, n);
+}
+// dx: the weight as it lies, and everything that does not go by the number of rows
+bool dx_params(const pbt_gated_desc* d, const Operand& dz, const Operand& w, RowsParams* p, CUtensorMap* tmA, CUtensorMap* tmB) {
+  p->a_batched = d->members > 1 && w.member != 0;
+  p->out = (bf16*)d->dx;
+  return make_map(tmA, w.p, d->width, 2ll * d->hidden, w.row, p->a_batched ? d->members : 1, w.member, kBK) && rows_params(d, true, dz, 2 * d->hidden, p, tmB);
 }
 
 // ------------------------------------------------------------------------------------------------------------------
 // dW of a few rows
 // ------------------------------------------------------------------------------------------------------------------
 // dW = [dg du]^T x with a contraction over at most 32 rows is bound by writing dW (72 members, one row, 344 -> 736: a whole backward pass 40 us, by the
-// plain product 94).  A CTA writes 128 x 128 elements: a warp has 16 rows of them, one or
-// two mma.sync steps each, and sends them through shared memory as whole 16-byte vectors.
+// plain product 94).  A CTA writes 128 x 128 elements: a warp has 16 rows of them, one or two mma.sync steps each, and sends them through shared memory as
+// whole 16-byte vectors.  It runs beside dx, which reads the weight meanwhile.
 constexpr int kOuterMost = 32, kOuterTile = 128, kOuterHalf = 64, kOuterPitch = kOuterTile + 8;      // (a pitch of 17 x 16 bytes: ldmatrix without conflicts)
 struct OuterParams {
   const bf16* dz; int dz_pitch;
@@ -576,21 +578,30 @@ __device__ __forceinline__ void mma16816(float* d, const uint32_t* a, uint32_t b
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 template <int STEPS>
-__global__ void __launch_bounds__(256) k_gated_outer(const OuterParams p) {
-  pdl_prologue();
-  __shared__ __align__(16) bf16 sd[STEPS * 16][kOuterPitch], sx[STEPS * 16][kOuterPitch];
-  __shared__ __align__(16) bf16 out[8][16][kOuterHalf + 8];
+struct OuterShared {
+  bf16 d[STEPS * 16][kOuterPitch], x[STEPS * 16][kOuterPitch];
+  bf16 out[8][16][kOuterHalf + 8];
+};
+template <int STEPS>
+__device__ __forceinline__ void outer_product(const OuterParams& p, OuterShared<STEPS>& sm, int c0, int n0, int m, bool wait) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int c0 = blockIdx.x * kOuterTile, n0 = blockIdx.y * kOuterTile, m = blockIdx.z;
   const bf16* dz = p.dz + (long long)m * p.rows * p.dz_pitch + n0;
   const bf16* x = p.x.p + m * p.x.member + c0;
+  auto &sd = sm.d, &sx = sm.x;
+  auto& out = sm.out;
+  const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+  constexpr int kVectors = kOuterTile / 8;
+  // (a row's last vector may end behind its last element, inside the same 16 bytes: those columns are not written)
 #pragma unroll
-  for (int i = threadIdx.x; i < STEPS * 16 * (kOuterTile / 8); i += 256) {
-    const int t = i / (kOuterTile / 8), c = i % (kOuterTile / 8) * 8;
-    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-    // (a row's last vector may end behind its last element, inside the same 16 bytes: those columns are not written)
-    *reinterpret_cast<uint4*>(&sd[t][c]) = t < p.rows && n0 + c < p.hidden2 ? __ldg(reinterpret_cast<const uint4*>(dz + (long long)t * p.dz_pitch + c)) : none;
+  for (int i = threadIdx.x; i < STEPS * 16 * kVectors; i += 256) {
+    const int t = i / kVectors, c = i % kVectors * 8;
     *reinterpret_cast<uint4*>(&sx[t][c]) = t < p.rows && c0 + c < p.width ? __ldg(reinterpret_cast<const uint4*>(x + t * p.x.row + c)) : none;
+  }
+  if (wait) asm volatile("griddepcontrol.wait;" ::: "memory");        // dg and du are there (and read past the read-only path)
+#pragma unroll
+  for (int i = threadIdx.x; i < STEPS * 16 * kVectors; i += 256) {
+    const int t = i / kVectors, c = i % kVectors * 8;
+    *reinterpret_cast<uint4*>(&sd[t][c]) = t < p.rows && n0 + c < p.hidden2 ? __ldcg(reinterpret_cast<const uint4*>(dz + (long long)t * p.dz_pitch + c)) : none;
   }
   __syncthreads();
   const int q = lane >> 3, r = lane & 7, gr = lane >> 2, tq = lane & 3;
@@ -633,6 +644,61 @@ __global__ void __launch_bounds__(256) k_gated_outer(const OuterParams p) {
     }
     __syncwarp();
   }
+}
+
+struct FewParams {
+  RowsParams dx;
+  OuterParams dw;
+  int dx_tiles, dx_blocks, dw_columns, dw_rows;      // tiles of a member, CTAs of all members
+  long long blocks;                                  // CTAs that have work
+};
+template <int N>
+struct FewShared {
+  static constexpr int kOuter = (int)sizeof(OuterShared<N / 16>) + 16;
+  static constexpr int kTotal = RowsTile<N>::kTotal > kOuter ? RowsTile<N>::kTotal : kOuter;
+};
+// Clusters of CTAs for dx first, then a CTA for every tile of dW; launched while the kernel that makes dg and du runs.
+template <int N>
+__global__ void __launch_bounds__(256, N == 16 ? 4 : 3) k_gated_few_gradients(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const FewParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  if ((int)blockIdx.x < p.dx_blocks) {
+    const int cluster = (int)(blockIdx.x / cluster_size());
+    rows_product<N, true, 256>(tmA, tmB, p.dx, smem_raw, cluster % p.dx_tiles, cluster / p.dx_tiles, 0);
+    return;
+  }
+  if (blockIdx.x < p.blocks) {
+    const int i = (int)blockIdx.x - p.dx_blocks, per_member = p.dw_columns * p.dw_rows, m = i / per_member, rest = i % per_member;
+    outer_product<N / 16>(p.dw, *reinterpret_cast<OuterShared<N / 16>*>(((uintptr_t)smem_raw + 15) & ~(uintptr_t)15), rest % p.dw_columns * kOuterTile,
+                          rest / p.dw_columns * kOuterTile, m, true);
+  }
+}
+// A tile of dW alone, beside dx: launched when all CTAs of dx run, that is, when dg and du are complete; it ends after dx.
+template <int STEPS>
+__global__ void __launch_bounds__(256) k_gated_outer(const OuterParams p) {
+  __shared__ __align__(16) OuterShared<STEPS> sm;
+  outer_product<STEPS>(p, sm, blockIdx.x * kOuterTile, blockIdx.y * kOuterTile, blockIdx.z, false);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+template <int N>
+cudaError_t launch_few(const pbt_gated_desc* d, FewParams& p, const CUtensorMap& tmA, const CUtensorMap& tmB, cudaStream_t s) {
+  static DeviceSetup setup;
+  int sms = 0;
+  const cudaError_t e = device_setup(&setup, k_gated_few_gradients<N>, FewShared<N>::kTotal, &sms);
+  if (e != cudaSuccess) return e;
+  p.dx_tiles = (d->width + kRowsLanes - 1) / kRowsLanes;
+  p.dw_columns = (d->width + kOuterTile - 1) / kOuterTile;
+  p.dw_rows = (2 * d->hidden + kOuterTile - 1) / kOuterTile;
+  const int splits = rows_splits((long long)p.dx_tiles * d->members, p.dx.k_blocks, (long long)sms * (N == 16 ? 4 : 3));
+  const long long dx = (long long)p.dx_tiles * d->members * splits, dw = (long long)p.dw_columns * p.dw_rows * d->members;
+  // Together while there is a place for every CTA (one token, 1024 -> 2048: a backward pass 8.7 us, one after the other 11.9); beyond that tiles of dW that
+  // take the place of CTAs of dx hold them up (16 members x 5 rows, 1024 -> 1024: 55 and 35).
+  if (dx + dw > (long long)sms * (N == 16 ? 4 : 3)) {
+    const cudaError_t first = launch_rows<N, true>(d, p.dx, tmA, tmB, s);
+    return first != cudaSuccess ? first : launch_after(dim3((unsigned)p.dw_columns, (unsigned)p.dw_rows, (unsigned)d->members), 256, 0, s, k_gated_outer<N / 16>, p.dw);
+  }
+  p.dx_blocks = (int)dx;
+  p.blocks = dx + dw;
+  return launch_clusters(dim3((unsigned)((p.blocks + splits - 1) / splits * splits)), 256, FewShared<N>::kTotal, splits, true, s, k_gated_few_gradients<N>, tmA, tmB, p);
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -719,30 +785,31 @@ static cudaError_t rows_forward(const pbt_gated_desc* d, const Operand& x, const
   p.drop = d->drop != nullptr;
   if (d->drop) p.rule = *d->drop;
   p.out = (bf16*)h; p.z = z; p.pitch = pitch;
-  CUtensorMap tmA;
-  if (!make_map(&tmA, w.p, d->width, 2ll * d->hidden, w.row, p.a_batched ? d->members : 1, w.member, 64)) return cudaErrorInvalidValue;
-  return launch_rows<false>(d, p, tmA, x, d->width, s);
+  CUtensorMap tmA, tmB;
+  if (!make_map(&tmA, w.p, d->width, 2ll * d->hidden, w.row, p.a_batched ? d->members : 1, w.member, 64) || !rows_params(d, false, x, d->width, &p, &tmB))
+    return cudaErrorInvalidValue;
+  return rows_columns(d) == 16 ? launch_rows<16, false>(d, p, tmA, tmB, s) : launch_rows<32, false>(d, p, tmA, tmB, s);
 }
 
-// dx takes it up to 32 rows, and where larger tiles would leave a third of the SMs without one (one member's 500 rows, 2048 -> 2048: a whole backward pass
+// dx beyond the rows of tc_gradients: where larger tiles would leave a third of the SMs without one (one member's 500 rows, 2048 -> 2048: a whole backward pass
 // 38 us, by the plain product 46; 20 x 250, 1024 -> 512, 320 tiles: 56 and 54).
 bool tc_dx_few(const pbt_gated_desc* d) {
-  return d->rows <= kRowsForward || (long long)((d->rows + 127) / 128) * ((d->width + 127) / 128) * d->members <= 100;
+  return (long long)((d->rows + 127) / 128) * ((d->width + 127) / 128) * d->members <= 100;      // (blocks of rows times members stay below 65536)
 }
 cudaError_t tc_dx(const pbt_gated_desc* d, const Operand& dz, const Operand& w, cudaStream_t s) {
   RowsParams p = {};
-  p.a_batched = d->members > 1 && w.member != 0;
-  p.out = (bf16*)d->dx;
-  CUtensorMap tmA;
-  if (!make_map(&tmA, w.p, d->width, 2ll * d->hidden, w.row, p.a_batched ? d->members : 1, w.member, kBK)) return cudaErrorInvalidValue;
-  return launch_rows<true>(d, p, tmA, dz, 2 * d->hidden, s);
+  CUtensorMap tmA, tmB;
+  if (!dx_params(d, dz, w, &p, &tmA, &tmB)) return cudaErrorInvalidValue;
+  return rows_columns(d) == 64 ? launch_rows<64, true>(d, p, tmA, tmB, s) : launch_rows<128, true>(d, p, tmA, tmB, s);
 }
 
-bool tc_outer_supported(const pbt_gated_desc* d) { return d->rows <= kOuterMost; }
-cudaError_t tc_outer(const pbt_gated_desc* d, const bf16* dz, int dz_pitch, const Operand& x, cudaStream_t s) {
-  const OuterParams p = {dz, dz_pitch, x, (bf16*)d->dweight, d->rows, 2 * d->hidden, d->width, d->width % 8 == 0 && ((uintptr_t)d->dweight & 15) == 0};
-  const dim3 grid((unsigned)((d->width + kOuterTile - 1) / kOuterTile), (unsigned)((2 * d->hidden + kOuterTile - 1) / kOuterTile), (unsigned)d->members);
-  return d->rows <= 16 ? launch_with(grid, 256, 0, s)(k_gated_outer<1>, p) : launch_with(grid, 256, 0, s)(k_gated_outer<2>, p);
+bool tc_gradients_few(const pbt_gated_desc* d) { return d->rows <= kOuterMost; }
+cudaError_t tc_gradients(const pbt_gated_desc* d, const Operand& dz, const Operand& w, const Operand& x, cudaStream_t s) {
+  FewParams p = {};
+  CUtensorMap tmA, tmB;
+  if (!dx_params(d, dz, w, &p.dx, &tmA, &tmB)) return cudaErrorInvalidValue;
+  p.dw = {dz.p, (int)dz.row, x, (bf16*)d->dweight, d->rows, 2 * d->hidden, d->width, d->width % 8 == 0 && ((uintptr_t)d->dweight & 15) == 0};
+  return rows_columns(d) == 16 ? launch_few<16>(d, p, tmA, tmB, s) : launch_few<32>(d, p, tmA, tmB, s);
 }
 
 cudaError_t tc_forward(const pbt_gated_desc* d, const Operand& x, const Operand& w, void* h, float* z, int pitch, cudaStream_t s) {

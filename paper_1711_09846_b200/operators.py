@@ -574,12 +574,12 @@ class GatedUnit:
                 raise ValueError("kept is what forward(keep=True) returned")
             d.kept = kept.data_ptr()
         inputs = () if stream is None else (dh, x, kept, w, *(dropout.tensors if dropout else ()))
-        return _on(w.device, stream, inputs, self._backward, d)
+        return _on(w.device, stream, inputs, self._backward, d, x)
 
-    def _backward(self, s, d):
+    def _backward(self, s, d, x):
         w = self.weight
-        dx = w.new_empty((d.members, d.rows, d.width))
-        dweight = w.new_empty((d.members, 2 * d.hidden, d.width))
+        dx = _like(x)
+        dweight = _like(w)
         d.dx, d.dweight = dx.data_ptr(), dweight.data_ptr()
         self._run(d, 1, self.lib.pbt_gated_backward, s)
         return dx, dweight
