@@ -16,21 +16,36 @@ namespace {
 using dropout::Eight;
 using dropout::store8;
 
-constexpr int kK = 16, kStages = 3, kSplits = 8, kCols = 64, kThreadCols = 8;
-constexpr int kPitchK = kK + 4;           // floats of a staged row of k: the vectors that eight lanes read lie in different banks
-constexpr int kPitchSum = kCols + 4;
+constexpr int kK = 16, kStages = 3, kSplits = 8, kCols = 64;
+constexpr int kPitchN = kCols + 4;        // floats of a staged row of columns, and of the sums
 
 // A tile of BM rows and 64 columns (forward: 32 hidden units' g and u); a thread has TM x 8 of its elements, a warp's lanes are 4 x 8 of the threads.
-template <int BM_, int TM_>
+template <int BM_, int TM_, int WARPS>
 struct Shape {
-  static constexpr int BM = BM_, TM = TM_, kThreadRows = BM / TM, kThreads = kThreadRows * (kCols / kThreadCols), kPerSm = (TM == 8 ? 384 : 512) / kThreads;
-  static constexpr int kA = BM * kPitchK > kK * (BM + 4) ? BM * kPitchK : kK * (BM + 4), kB = kCols * kPitchK, kStage = kA + kB;      // floats
-  static constexpr int kFloats = kStages * kStage > BM * kPitchSum ? kStages * kStage : BM * kPitchSum;
-  static_assert(kCols * kPitchK >= kK * (kCols + 4) && kThreads % 32 == 0, "the ring holds either layout");
+  static constexpr int BM = BM_, TM = TM_, kThreads = BM / TM * 8, kPerSm = WARPS * 32 / kThreads, kPitchM = BM + 4;
+  static constexpr int kA = kK * kPitchM, kB = kK * kPitchN, kStage = kA + kB;      // floats
+  static constexpr int kFloats = kStages * kStage > BM * kPitchN ? kStages * kStage : BM * kPitchN;
+  static_assert(kThreads % 32 == 0 && (TM == 8 || TM == 4 || TM == 2), "whole warps; rows in vectors");
 };
-typedef Shape<128, 8> Tall;
-typedef Shape<64, 8> Short;
-typedef Shape<16, 2> Few;
+typedef Shape<128, 8, 12> Tall;
+typedef Shape<64, 8, 12> Short;
+typedef Shape<32, 4, 16> Half;
+typedef Shape<16, 2, 16> Few;
+
+// two fp32 multiply-adds in one instruction
+__device__ __forceinline__ void fma2(unsigned long long& d, unsigned long long a, unsigned long long b) {
+  asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(d) : "l"(a), "l"(b));
+}
+__device__ __forceinline__ unsigned long long both(float v) {
+  unsigned long long d;
+  asm("mov.b64 %0, {%1, %1};" : "=l"(d) : "f"(v));
+  return d;
+}
+__device__ __forceinline__ float2 halves(unsigned long long v) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+  return f;
+}
 
 struct ProductParams {
   const float* a; long long lda, a_member;      // [M][K], or [K][M]
@@ -45,50 +60,70 @@ struct ProductParams {
   pbt_drop_rule rule;
 };
 
-// a box of ROWS rows and COLS floats into staged rows of PITCH, `rows` x `cols` of which exist (the others are zero)
-template <int THREADS, int ROWS, int COLS, int PITCH>
-__device__ __forceinline__ void copy_box(uint32_t to, const float* from, long long ld, int rows, int cols, bool vectors) {
+// a box of kK rows and COLS floats into staged rows of PITCH, `rows` x `cols` of which exist (the others are zero)
+template <int THREADS, int COLS, int PITCH>
+__device__ __forceinline__ void copy_rows(uint32_t to, const float* from, long long ld, int rows, int cols, bool vectors) {
   if (vectors) {
     constexpr int kStep = THREADS / (COLS / 4);
+    static_assert(kStep >= 1 && kK % kStep == 0, "whole steps");
     const int r0 = threadIdx.x / (COLS / 4), c = threadIdx.x % (COLS / 4) * 4, bytes = min(max(cols - c, 0), 4) * 4;
     const float* at = from + r0 * ld + c;
     const long long step = kStep * ld;
     to += (r0 * PITCH + c) * 4;
 #pragma unroll
-    for (int i = 0; i < ROWS / kStep; ++i) {
+    for (int i = 0; i < kK / kStep; ++i) {
       const int have = r0 + i * kStep < rows ? bytes : 0;
       asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + i * kStep * PITCH * 4), "l"(have ? at : from), "r"(have) : "memory");
       at += step;
     }
   } else {
-    constexpr int kStep = THREADS / COLS;
-    const int r0 = threadIdx.x / COLS, c = threadIdx.x % COLS, bytes = c < cols ? 4 : 0;
-    const float* at = from + r0 * ld + c;
-    const long long step = kStep * ld;
-    to += (r0 * PITCH + c) * 4;
+    constexpr int kStep = THREADS > COLS ? THREADS / COLS : 1, kEach = COLS > THREADS ? COLS / THREADS : 1;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int r0 = threadIdx.x / COLS, c = threadIdx.x % COLS + e * THREADS, bytes = c < cols ? 4 : 0;
+      const float* at = from + r0 * ld + c;
+      const long long step = kStep * ld;
+      const uint32_t out = to + (r0 * PITCH + c) * 4;
 #pragma unroll 4
-    for (int i = 0; i < ROWS / kStep; ++i) {
-      const int have = r0 + i * kStep < rows ? bytes : 0;
-      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + i * kStep * PITCH * 4), "l"(have ? at : from), "r"(have) : "memory");
-      at += step;
+      for (int i = 0; i < kK / kStep; ++i) {
+        const int have = r0 + i * kStep < rows ? bytes : 0;
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(out + i * kStep * PITCH * 4), "l"(have ? at : from), "r"(have) : "memory");
+        at += step;
+      }
     }
   }
 }
+// The same of ROWS rows and kK floats, turned on the way: a staged row holds the box's column.  Single elements, of any alignment: a warp takes 64 bytes of
+// two rows (staged as they lie, with vectors of k read for the products, 40 members, 128 rows, 512 -> 512 took 160 us, the loop over rows of m and n x).
+template <int THREADS, int ROWS, int PITCH>
+__device__ __forceinline__ void copy_turned(uint32_t to, const float* from, long long ld, int rows, int cols) {
+  constexpr int kStep = THREADS / kK;
+  static_assert(ROWS % kStep == 0, "whole steps");
+  const int r0 = threadIdx.x / kK, k = threadIdx.x % kK, bytes = k < cols ? 4 : 0;
+  const float* at = from + r0 * ld + k;
+  const long long step = kStep * ld;
+  to += (k * PITCH + r0) * 4;
+#pragma unroll 8
+  for (int i = 0; i < ROWS / kStep; ++i) {
+    const int have = r0 + i * kStep < rows ? bytes : 0;
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + i * kStep * 4), "l"(have ? at : from), "r"(have) : "memory");
+    at += step;
+  }
+}
 
-// K goes in slices of 16 through a ring of cp.async stages as the operands lie: staged rows of k are read as vectors of four k, rows of m or n as
-// vectors of four of those.  The CTAs of a cluster share the contraction; every one adds up its share of the tile's rows over all their sums, in
-// their order.
-template <typename S, bool A_MN, bool B_MN, bool GATED>
+// K goes in slices of 16 through a ring of cp.async stages, rows of m and of n for every k.  The CTAs of a cluster share the contraction; every one adds up its
+// share of the tile's rows over all their sums, in their order.  Bound by shared memory: a thread's 8 x 8 multiply-adds take 16 values from it, a warp's
+// loads as many cycles as its products (which go two to an instruction, or their issue would be the limit: 264 us instead of 226 for both gradients of
+// 40 x 128, 512 -> 512).
+template <typename S, bool A_MN, bool GATED>
 __device__ __forceinline__ void product_tile(const ProductParams& p, float* f32_smem, int tile, int m, int splits, int rank) {
-  constexpr int BM = S::BM, TM = S::TM, kThreads = S::kThreads, kPitchM = BM + 4, kPitchN = kCols + 4;
-  static_assert(!A_MN || TM == 8, "rows of m are read in vectors");
+  constexpr int BM = S::BM, TM = S::TM, kThreads = S::kThreads, kPitchM = S::kPitchM, kUnits = GATED ? kCols / 2 : kCols;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tx = lane & 7, ty = warp * 4 + (lane >> 3);
-  constexpr int kUnits = GATED ? kCols / 2 : kCols;
   const int m0 = tile / p.tiles_n * BM, n0 = tile % p.tiles_n * kUnits, rows = min(BM, p.M - m0), cols = min(kUnits, p.N - n0);
   const int slices = (p.K + kK - 1) / kK, s0 = (int)((long long)slices * rank / splits), s1 = (int)((long long)slices * (rank + 1) / splits);
   const float* A = p.a + m * p.a_member + (A_MN ? m0 : m0 * p.lda);
-  const float* B = p.b + m * p.b_member + (B_MN ? n0 : n0 * p.ldb);
-  const float* B2 = B + p.N * p.ldb;              // forward: the up-projection's rows
+  const float* B = p.b + m * p.b_member + (GATED ? n0 * p.ldb : n0);      // forward: [N][K], else [K][N]
+  const float* B2 = B + p.N * p.ldb;                                      // forward: the up-projection's rows
   const uint32_t base = (uint32_t)__cvta_generic_to_shared(f32_smem);
 
   int slot = 0;                                   // of the slice that is asked for next
@@ -96,24 +131,21 @@ __device__ __forceinline__ void product_tile(const ProductParams& p, float* f32_
     if (s < s1) {
       const uint32_t sa = base + slot * S::kStage * 4, sb = sa + S::kA * 4;
       const int k0 = s * kK, ks = p.K - k0;
-      if (A_MN) copy_box<kThreads, kK, BM, kPitchM>(sa, A + k0 * p.lda, p.lda, ks, rows, p.vec_a);
-      else copy_box<kThreads, BM, kK, kPitchK>(sa, A + k0, p.lda, rows, ks, p.vec_a);
+      if (A_MN) copy_rows<kThreads, BM, kPitchM>(sa, A + k0 * p.lda, p.lda, ks, rows, p.vec_a);
+      else copy_turned<kThreads, BM, kPitchM>(sa, A + k0, p.lda, rows, ks);
       if (GATED) {
-        copy_box<kThreads, kUnits, kK, kPitchK>(sb, B + k0, p.ldb, cols, ks, p.vec_b);
-        copy_box<kThreads, kUnits, kK, kPitchK>(sb + kUnits * kPitchK * 4, B2 + k0, p.ldb, cols, ks, p.vec_b);
-      } else if (B_MN) {
-        copy_box<kThreads, kK, kCols, kPitchN>(sb, B + k0 * p.ldb, p.ldb, ks, cols, p.vec_b);
+        copy_turned<kThreads, kUnits, kPitchN>(sb, B + k0, p.ldb, cols, ks);
+        copy_turned<kThreads, kUnits, kPitchN>(sb + kUnits * 4, B2 + k0, p.ldb, cols, ks);
       } else {
-        copy_box<kThreads, kCols, kK, kPitchK>(sb, B + k0, p.ldb, cols, ks, p.vec_b);
+        copy_rows<kThreads, kCols, kPitchN>(sb, B + k0 * p.ldb, p.ldb, ks, cols, p.vec_b);
       }
     }
     slot = slot + 1 == kStages ? 0 : slot + 1;
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  auto row_of = [&](int i) { return A_MN ? (i >> 2) * (BM / 2) + ty * 4 + (i & 3) : ty + i * S::kThreadRows; };
-  auto col_of = [&](int j) { return B_MN ? (j >> 2) * (kCols / 2) + tx * 4 + (j & 3) : tx + j * 8; };
+  auto row_of = [&](int i) { return TM >= 4 ? (i >> 2) * (BM / 2) + ty * 4 + (i & 3) : ty * TM + i; };
 
-  float acc[TM][8] = {};
+  unsigned long long acc[TM][4] = {};             // pairs of neighbouring columns: 4 tx .. and 32 + 4 tx ..
 #pragma unroll
   for (int s = 0; s < kStages - 1; ++s) load(s0 + s);
   int at = 0;
@@ -125,36 +157,26 @@ __device__ __forceinline__ void product_tile(const ProductParams& p, float* f32_
     const float *sa = f32_smem + at * S::kStage, *sb = sa + S::kA;
     at = at + 1 == kStages ? 0 : at + 1;
 #pragma unroll
-    for (int k = 0; k < kK; k += 4) {
-      float b[4][8];            // [k][column]
+    for (int k = 0; k < kK; ++k) {
+      const ulonglong2 b0 = *reinterpret_cast<const ulonglong2*>(sb + k * kPitchN + tx * 4), b1 = *reinterpret_cast<const ulonglong2*>(sb + k * kPitchN + kCols / 2 + tx * 4);
+      float a[TM];
+      if constexpr (TM >= 4) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float4 q = *reinterpret_cast<const float4*>(B_MN ? sb + (k + (i & 3)) * kPitchN + (i >> 2) * (kCols / 2) + tx * 4 : sb + col_of(i) * kPitchK + k);
-        if (B_MN) { const int j = (i >> 2) * 4; b[i & 3][j] = q.x; b[i & 3][j + 1] = q.y; b[i & 3][j + 2] = q.z; b[i & 3][j + 3] = q.w; }
-        else { b[0][i] = q.x; b[1][i] = q.y; b[2][i] = q.z; b[3][i] = q.w; }
-      }
-      if (A_MN) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int h = 0; h < TM / 4; ++h) {
-            const float4 q = *reinterpret_cast<const float4*>(sa + (k + i) * kPitchM + h * (BM / 2) + ty * 4);
-            const float a[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-              for (int j = 0; j < 8; ++j) acc[h * 4 + r][j] = __fmaf_rn(a[r], b[i][j], acc[h * 4 + r][j]);
-          }
-      } else {
-#pragma unroll
-        for (int r = 0; r < TM; ++r) {
-          const float4 q = *reinterpret_cast<const float4*>(sa + row_of(r) * kPitchK + k);
-          const float a[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) acc[r][j] = __fmaf_rn(a[i], b[i][j], acc[r][j]);
+        for (int h = 0; h < TM / 4; ++h) {
+          const float4 q = *reinterpret_cast<const float4*>(sa + k * kPitchM + h * (BM / 2) + ty * 4);
+          a[h * 4] = q.x; a[h * 4 + 1] = q.y; a[h * 4 + 2] = q.z; a[h * 4 + 3] = q.w;
         }
+      } else {
+        const float2 q = *reinterpret_cast<const float2*>(sa + k * kPitchM + ty * 2);
+        a[0] = q.x; a[1] = q.y;
+      }
+#pragma unroll
+      for (int r = 0; r < TM; ++r) {
+        const unsigned long long a2 = both(a[r]);
+        fma2(acc[r][0], a2, b0.x);
+        fma2(acc[r][1], a2, b0.y);
+        fma2(acc[r][2], a2, b1.x);
+        fma2(acc[r][3], a2, b1.y);
       }
     }
   }
@@ -163,13 +185,13 @@ __device__ __forceinline__ void product_tile(const ProductParams& p, float* f32_
 #pragma unroll
   for (int r = 0; r < TM; ++r)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f32_smem[row_of(r) * kPitchSum + col_of(j)] = acc[r][j];
+    for (int j = 0; j < 4; ++j) *reinterpret_cast<float2*>(f32_smem + row_of(r) * kPitchN + (j >> 1) * (kCols / 2) + tx * 4 + (j & 1) * 2) = halves(acc[r][j]);
   if (splits > 1) tc::cluster_sync_all();
   else __syncthreads();
   auto sum = [&](int r, int c, float* v) {      // four neighbouring columns
-    const uint32_t at = base + (r * kPitchSum + c) * 4;
+    const uint32_t at = base + (r * kPitchN + c) * 4;
     if (splits == 1) {
-      const float4 q = *reinterpret_cast<const float4*>(f32_smem + r * kPitchSum + c);
+      const float4 q = *reinterpret_cast<const float4*>(f32_smem + r * kPitchN + c);
       v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
       return;
     }
@@ -240,7 +262,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSm) k_gated_forward_f32(co
   pdl_prologue();
   extern __shared__ __align__(16) float f32_smem[];
   const int splits = (int)tc::cluster_size();
-  product_tile<S, false, false, true>(p, f32_smem, blockIdx.x / splits, blockIdx.y, splits, (int)tc::cluster_ctarank());
+  product_tile<S, false, true>(p, f32_smem, blockIdx.x / splits, blockIdx.y, splits, (int)tc::cluster_ctarank());
 }
 // The CTAs of dx first, then those of dW, a cluster or one for a tile; launched while the kernel that makes dg and du runs.
 struct GradientParams {
@@ -260,10 +282,11 @@ __global__ void __launch_bounds__(SX::kThreads, GradientShape<SX, SW>::kPerSm) k
   const int rank = (int)tc::cluster_ctarank();
   if ((int)blockIdx.x < p.dx_blocks) {
     const int i = (int)blockIdx.x / p.dx_splits;
-    if (i < p.dx_tiles * p.members) product_tile<SX, false, true, false>(p.dx, f32_smem, i % p.dx_tiles, i / p.dx_tiles, p.dx_splits, p.dx_splits > 1 ? rank : 0);
+    if (i < p.dx_tiles * p.members) product_tile<SX, false, false>(p.dx, f32_smem, i % p.dx_tiles, i / p.dx_tiles, p.dx_splits, p.dx_splits > 1 ? rank : 0);
   } else if (blockIdx.x < p.blocks) {
     const int i = ((int)blockIdx.x - p.dx_blocks) / p.dw_splits;
-    product_tile<SW, true, true, false>(p.dw, f32_smem, i % p.dw_tiles, i / p.dw_tiles, p.dw_splits, p.dw_splits > 1 ? rank : 0);
+    if (p.dw_splits == 1) product_tile<SW, true, false>(p.dw, f32_smem, i % p.dw_tiles, i / p.dw_tiles, 1, 0);
+    else product_tile<SW, true, false>(p.dw, f32_smem, i % p.dw_tiles, i / p.dw_tiles, p.dw_splits, rank);
   }
 }
 
@@ -329,6 +352,7 @@ cudaError_t f32_forward(const pbt_gated_desc* d, float* h, float* z, int pitch, 
   if (d->drop) p.rule = *d->drop;
   fill(d, &p, true);
   if (p.M <= Few::BM) return launch_forward<Few>(d, p, s);
+  if (p.M <= Half::BM) return launch_forward<Half>(d, p, s);
   return tall(d, p) ? launch_forward<Tall>(d, p, s) : launch_forward<Short>(d, p, s);
 }
 
@@ -345,6 +369,7 @@ cudaError_t f32_backward(const pbt_gated_desc* d, const float* dz, int dz_pitch,
   fill(d, &p, false);
   fill(d, &dw, false);
   if (p.M <= Few::BM) return launch_gradients<Few, Short>(d, p, dw, s);
+  if (p.M <= Half::BM) return launch_gradients<Half, Short>(d, p, dw, s);
   return tall(d, p) ? launch_gradients<Tall, Tall>(d, p, dw, s) : launch_gradients<Short, Short>(d, p, dw, s);
 }
 
