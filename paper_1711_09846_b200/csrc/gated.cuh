@@ -58,6 +58,21 @@ __device__ __forceinline__ float activation(int kind, float g) {
   const float s = __fdividef(1.f, 1.f + __expf(-g));
   return kind == kSilu ? g * s : s;
 }
+// The same for a bf16 result.  The error function's complement as t exp(-x^2 + P(t)), t = 1 / (1 + x / 2), P fitted to be 8e-6 of the value off at most, a 500th
+// of the result's rounding: 14 instructions (erfcf, three times as many, made the epilogue the limit: 3 x 777 rows, 784 -> 1000: 21.4 us, with silu 17.7).
+__device__ __forceinline__ float activation_bf16(int kind, float g) {
+  if (kind != kGelu) return activation(kind, g);
+  const float x = fabsf(g) * 0.70710678f, t = __fdividef(1.f, fmaf(0.5f, x, 1.f));
+  float q = fmaf(0.33007830f, t, -1.02315712f);        // P / ln 2, less 1 for the half in front of erfc
+  q = fmaf(q, t, 0.68456119f);
+  q = fmaf(q, t, 0.36707783f);
+  q = fmaf(q, t, 1.46868443f);
+  q = fmaf(q, t, -2.82723355f);
+  float e;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fmaf(x * x, -1.44269504f, q)));
+  const float tail = t * e;
+  return g * (g < 0.f ? tail : 1.f - tail);
+}
 // act(g) and act'(g).  1 - sigmoid is taken without a difference of nearly equal numbers.
 __device__ __forceinline__ float activation(int kind, float g, float* slope) {
   if (kind == kRelu) {

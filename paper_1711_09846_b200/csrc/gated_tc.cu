@@ -62,7 +62,7 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
 template <int KIND>
 __device__ __forceinline__ void apply(const uint32_t* g, uint32_t* u) {
 #pragma unroll
-  for (int c = 0; c < 32; ++c) u[c] = __float_as_uint(activation(KIND, __uint_as_float(g[c])) * __uint_as_float(u[c]));
+  for (int c = 0; c < 32; ++c) u[c] = __float_as_uint(activation_bf16(KIND, __uint_as_float(g[c])) * __uint_as_float(u[c]));
 }
 __device__ __forceinline__ void apply(int kind, const uint32_t* g, uint32_t* u) {
   switch (kind) {
@@ -493,7 +493,7 @@ __device__ __forceinline__ void rows_product(const CUtensorMap& tmA, const CUten
       }
       if (!p.out) continue;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) g.v[e] = activation(p.activation, g.v[e]) * u.v[e];
+      for (int e = 0; e < 8; ++e) g.v[e] = activation_bf16(p.activation, g.v[e]) * u.v[e];
       if (p.drop) {
         const dropout::Draw d = dropout::draw_of(p.rule, m);
         const uint32_t in = dropout::kept_bits(d, (uint32_t)t * (uint32_t)((p.hidden + 7) / 8) + (uint32_t)(col / 8));
