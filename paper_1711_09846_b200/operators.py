@@ -516,72 +516,77 @@ class GatedUnit:
         _require(activation in _ACTIVATIONS, "activation is " + ", ".join(_ACTIVATIONS))
         _require(max(m, n, k) <= _MOST, "members, hidden and width are at most 2^31 - 1")
         self.weight, self.hidden = weight, n // 2
+        self._members, self._width, self._dtype, self._device = m, k, weight.dtype, weight.device
+        self._pitch = (self.hidden + 7) // 8 * 8                    # of g and u
         self.lib = load_library()
         d = self._desc = PbtGatedDesc()
         d.members, d.width, d.hidden, d.dtype, d.activation = m, k, n // 2, _TYPES[weight.dtype], _ACTIVATIONS[activation]
         d.weight, d.weight_member, d.weight_row = weight.data_ptr(), weight.stride(0), weight.stride(1)
         self._status = torch.zeros(8, dtype=torch.int32, device=weight.device)
+        self._floats = torch.empty(0, device=weight.device)         # (new_empty of a tensor costs less than torch.empty with a type and a device)
         self._home = _current_stream(weight.device.index)
         torch.cuda.current_stream(weight.device).synchronize()      # the calls may be on any stream
         d.status_device = self._status.data_ptr()
         _check(self.lib.pbt_gated_query_workspace(C.byref(d), 0, C.byref(C.c_size_t(0))))
 
-    def _call(self, x, dropout):
+    def _call(self, x, dropout, kept):
         """The description of a call on these rows (a copy: calls from several threads do not share it)."""
-        w, shape = self.weight, x.shape
-        device = w.device
-        d = PbtGatedDesc.from_buffer_copy(self._desc)
-        if not (len(shape) == 3 and shape[0] == d.members and shape[2] == d.width and x.dtype is w.dtype and x.device == device):
+        shape, width = x.shape, self._width
+        if not (len(shape) == 3 and shape[0] == self._members and shape[2] == width and x.dtype is self._dtype and x.device == self._device):
             raise ValueError("x is [members, rows, width] of the weight's members, width, type and device")
-        if shape[1] > _MOST:
+        rows = shape[1]
+        if rows > _MOST:
             raise ValueError("a call has at most 2^31 - 1 rows")
-        d.rows = shape[1]
-        d.x, d.x_member, d.x_row = _rows_of(x, "x")
+        member, row, column = x.stride()
+        if column != 1 and width != 1:
+            raise ValueError("x has to have contiguous columns")
+        d = PbtGatedDesc.from_buffer_copy(self._desc)
+        d.rows, d.x, d.x_member, d.x_row = rows, x.data_ptr(), member, row if rows > 1 else max(row, width)      # (a single row may carry any stride)
         if dropout is not None:
-            d.drop = C.addressof(dropout._for(d.members, device))
-        return d
+            d.drop = C.addressof(dropout._for(self._members, self._device))
+        if kept is not None:
+            if not (kept.shape == (self._members, rows, 2, self._pitch) and kept.dtype is torch.float32 and kept.device == self._device and kept.is_contiguous()):
+                raise ValueError("kept is what forward(keep=True) returned")
+            d.kept = kept.data_ptr()
+        return d, rows
 
     def forward(self, x, dropout: Optional[Dropout] = None, keep: bool = False, stream=None):
         """h [members, rows, hidden]; with keep, also g and u in float32 for the backward pass (8 bytes a hidden unit; without
         them it works them out anew, which costs two thirds of a forward pass more)."""
-        d = self._call(x, dropout)
+        d, rows = self._call(x, dropout, None)
         inputs = () if stream is None else (x, self.weight, *(dropout.tensors if dropout else ()))
-        return _on(self.weight.device, stream, inputs, self._forward, d, keep)
+        return _on(self._device, stream, inputs, self._forward, d, rows, keep)
 
-    def _forward(self, s, d, keep):
-        w = self.weight
-        h = w.new_empty((d.members, d.rows, d.hidden))
+    def _forward(self, s, d, rows, keep):
+        h = self.weight.new_empty((self._members, rows, self.hidden))
         d.h = h.data_ptr()
         kept = None
         if keep:
-            kept = torch.empty((d.members, d.rows, 2, (d.hidden + 7) // 8 * 8), dtype=torch.float32, device=w.device)
+            kept = self._floats.new_empty((self._members, rows, 2, self._pitch))
             d.kept = kept.data_ptr()
-        if d.rows:
-            self._run(d, 0, self.lib.pbt_gated_forward, s)
+        if rows:
+            # a forward pass needs a workspace for bfloat16 rows of odd sizes only: asking for its size costs a small call as much as its checks
+            rc = self.lib.pbt_gated_forward(d, None, 0, s)
+            if rc:
+                self._run(d, 0, self.lib.pbt_gated_forward, s, rc)
+            elif s != self._home:
+                self._keep_status()
         return (h, kept) if keep else h
 
     def backward(self, dh, x, kept=None, dropout: Optional[Dropout] = None, stream=None):
         """(dx, dweight) from dh [members, rows, hidden], the forward pass's x, what it kept (or None) and its dropout.  dweight is
         [members, 2 hidden, width] of the weight's type, every member's own even where the weight is one for all."""
-        d = self._call(x, dropout)
-        w = self.weight
-        if not (dh.shape == (d.members, d.rows, d.hidden) and dh.dtype == w.dtype and dh.device == w.device):
+        d, rows = self._call(x, dropout, kept)
+        if not (dh.shape == (self._members, rows, self.hidden) and dh.dtype is self._dtype and dh.device == self._device):
             raise ValueError("dh is [members, rows, hidden] of the weight's type and device")
         d.dh, d.dh_member, d.dh_row = _rows_of(dh, "dh")
-        if kept is not None:
-            if not (kept.shape == (d.members, d.rows, 2, (d.hidden + 7) // 8 * 8) and kept.dtype is torch.float32 and kept.device == w.device
-                    and kept.is_contiguous()):
-                raise ValueError("kept is what forward(keep=True) returned")
-            d.kept = kept.data_ptr()
-        inputs = () if stream is None else (dh, x, kept, w, *(dropout.tensors if dropout else ()))
-        return _on(w.device, stream, inputs, self._backward, d, x)
+        inputs = () if stream is None else (dh, x, kept, self.weight, *(dropout.tensors if dropout else ()))
+        return _on(self._device, stream, inputs, self._backward, d, x)
 
     def _backward(self, s, d, x):
-        w = self.weight
-        dx = _like(x)
-        dweight = _like(w)
+        dx, dweight = _like(x), _like(self.weight)
         d.dx, d.dweight = dx.data_ptr(), dweight.data_ptr()
-        self._run(d, 1, self.lib.pbt_gated_backward, s)
+        self._run(d, 1, self.lib.pbt_gated_backward, s, _NO_WORKSPACE)
         return dx, dweight
 
     def check(self):
@@ -591,17 +596,19 @@ class GatedUnit:
         if code:
             raise PbtError(code, "a bounded wait inside a kernel ran out")
 
-    def _run(self, d, backward, call, s):
-        if s != self._home:      # keeps the status words until the call is done, should the object go first
-            self._status.record_stream(torch.cuda.current_stream(self.weight.device))
-        at = C.byref(d)
-        # a forward pass needs a workspace for bfloat16 rows of odd sizes only: asking for its size costs a small call as much as its checks
-        rc = _NO_WORKSPACE if backward else call(at, None, 0, s)
+    def _keep_status(self):
+        """Keeps the status words until the current stream's calls are done, should the object go first."""
+        self._status.record_stream(torch.cuda.current_stream(self._device))
+
+    def _run(self, d, backward, call, s, rc):
+        """The call with a workspace, after an answer `rc` to one without."""
+        if s != self._home:
+            self._keep_status()
         if rc == _NO_WORKSPACE:
             nbytes = C.c_size_t(0)
-            rc = self.lib.pbt_gated_query_workspace(at, backward, C.byref(nbytes))
+            rc = self.lib.pbt_gated_query_workspace(d, backward, C.byref(nbytes))
             if not rc:
-                rc = _with_workspace(call, at, nbytes.value, s)
+                rc = _with_workspace(call, d, nbytes.value, s)
         if rc:
             _check(rc)
 
