@@ -637,10 +637,13 @@ __device__ __forceinline__ void outer_product(const OuterParams& p, OuterShared<
           *reinterpret_cast<uint4*>(dw + (long long)row * p.width + h + c) = *reinterpret_cast<const uint4*>(&out[warp][row][c]);
       }
     } else {
-      for (int row = 0; row < rows; ++row)
-#pragma unroll
-        for (int c = lane; c < kOuterHalf; c += 32)
-          if (c0 + h + c < p.width) dw[(long long)row * p.width + h + c] = out[warp][row][c];
+      for (int row = 0; row < rows; ++row) {       // pairs of columns from the row's first 4-byte boundary on
+        bf16* to = dw + (long long)row * p.width + h;
+        const int odd = (int)((uintptr_t)to >> 1) & 1, c = 2 * lane + odd, left = min(kOuterHalf, p.width - c0 - h);
+        if (c + 1 < left) *reinterpret_cast<__nv_bfloat162*>(to + c) = __nv_bfloat162(out[warp][row][c], out[warp][row][c + 1]);
+        else if (c < left) to[c] = out[warp][row][c];
+        if (odd && lane == 0 && left > 0) to[0] = out[warp][row][0];
+      }
     }
     __syncwarp();
   }
@@ -704,10 +707,23 @@ cudaError_t launch_few(const pbt_gated_desc* d, FewParams& p, const CUtensorMap&
 // ------------------------------------------------------------------------------------------------------------------
 // Operands whose rows are not multiples of 16 bytes are copied once into rows that are, both in one launch.
 // ------------------------------------------------------------------------------------------------------------------
+// n / d for n < 2^31 in two instructions (the quotient of a product with a rounded reciprocal of 32 bits; the error stays below 1 / d there)
+struct Divisor {
+  uint32_t factor, shift;
+};
+Divisor divisor(uint32_t d) {
+  uint32_t s = 0;
+  while (s < 31 && (1u << s) < d) ++s;                          // 2^(s - 1) < d <= 2^s
+  return {(uint32_t)(((1ull << (31 + s)) + d - 1) / d), s};     // (d = 1: 2^31)
+}
+__device__ __forceinline__ uint32_t quotient(uint32_t n, Divisor d) { return (uint32_t)(((uint64_t)n * d.factor) >> 31) >> d.shift; }
+
 struct PackJob {
   const bf16* src; long long row, member;
   bf16* dst;
-  int members, rows, cols, to;    // elements of a row, and rounded up to 8
+  int rows, cols, per_row;        // elements of a row, vectors of a packed one
+  uint32_t vectors;
+  Divisor by_row, by_member;      // vectors of a row; rows of a member
   unsigned block0;                // its first block
 };
 constexpr int kPackEach = 4;      // vectors of a thread
@@ -715,24 +731,23 @@ struct PackJobs {
   PackJob job[2];
   int n;
 };
+// Eight elements from any place as a vector: the 16-byte pieces that hold them, the second one only if an element of the row lies in it, shifted together.
+// Bound by issue as much as by the transfers.
 __global__ void __launch_bounds__(256) k_gated_pack(const PackJobs a) {
   pdl_prologue();
   const bool second = a.n > 1 && blockIdx.x >= a.job[1].block0;
   const PackJob j = second ? a.job[1] : a.job[0];
-  const long long first = (long long)(blockIdx.x - j.block0) * (256 * kPackEach) + threadIdx.x, rows = (long long)j.members * j.rows;
-  const uint32_t per_row = j.to / 8;
+  const uint32_t first = (blockIdx.x - j.block0) * (256 * kPackEach) + threadIdx.x;
   uint4 a0[kPackEach], a1[kPackEach];
   int off[kPackEach], n[kPackEach];
 #pragma unroll
   for (int u = 0; u < kPackEach; ++u) {
-    const long long i = first + u * 256;
+    const uint32_t i = first + u * 256;
     n[u] = 0;
-    if (i >= rows * per_row) continue;
-    // (a 64-bit division costs more than the rest)
-    const long long at = i <= 0xFFFFFFFFll ? (uint32_t)i / per_row : i / per_row;
-    const int c = (int)(i - at * per_row) * 8, m = (int)(at <= 0xFFFFFFFFll ? (uint32_t)at / (uint32_t)j.rows : at / j.rows);
-    // the 16-byte pieces that hold the eight elements, the second one only if an element of the row lies in it
-    const uintptr_t addr = (uintptr_t)(j.src + m * j.member + (at - (long long)m * j.rows) * j.row + c);
+    if (i >= j.vectors) continue;
+    const uint32_t at = quotient(i, j.by_row), m = quotient(at, j.by_member);
+    const int c = (int)(i - at * j.per_row) * 8;
+    const uintptr_t addr = (uintptr_t)(j.src + m * j.member + (long long)(at - m * j.rows) * j.row + c);
     const uint4* piece = reinterpret_cast<const uint4*>(addr & ~(uintptr_t)15);
     off[u] = (int)(addr & 15) / 2;
     n[u] = min(8, j.cols - c);
@@ -742,18 +757,21 @@ __global__ void __launch_bounds__(256) k_gated_pack(const PackJobs a) {
 #pragma unroll
   for (int u = 0; u < kPackEach; ++u) {
     if (!n[u]) continue;
-    const uint32_t w[8] = {a0[u].x, a0[u].y, a0[u].z, a0[u].w, a1[u].x, a1[u].y, a1[u].z, a1[u].w};      // (off + 7 < 16)
-    const int q = off[u] >> 1;
-    uint32_t v[5], o[4];
+    uint32_t w[8] = {a0[u].x, a0[u].y, a0[u].z, a0[u].w, a1[u].x, a1[u].y, a1[u].z, a1[u].w};      // (off + 7 < 16)
+    if (off[u] & 4)
 #pragma unroll
-    for (int i = 0; i < 5; ++i) v[i] = q == 0 ? w[i] : q == 1 ? w[i + 1] : q == 2 ? w[i + 2] : w[i + 3];
+      for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    if (off[u] & 2)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      o[i] = (off[u] & 1) ? __funnelshift_r(v[i], v[i + 1], 16) : v[i];
-      if (2 * i >= n[u]) o[i] = 0u;
-      else if (2 * i + 1 >= n[u]) o[i] &= 0xFFFFu;
-    }
-    *reinterpret_cast<uint4*>(j.dst + (first + u * 256) * 8) = make_uint4(o[0], o[1], o[2], o[3]);
+      for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+    const uint32_t bits = (off[u] & 1) * 16;
+    uint32_t o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = __funnelshift_r(w[i], w[i + 1], bits);
+    if (n[u] < 8)                 // a row's last vector: zeros behind its last element
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = 2 * i >= n[u] ? 0u : 2 * i + 1 >= n[u] ? o[i] & 0xFFFFu : o[i];
+    *reinterpret_cast<uint4*>(j.dst + (long long)(first + u * 256) * 8) = make_uint4(o[0], o[1], o[2], o[3]);
   }
 }
 
@@ -766,16 +784,17 @@ bool tc_aligned(const void* p, long long row, long long member, int members) {
 
 cudaError_t tc_pack(const PackSource* src, int n, cudaStream_t s) {
   PackJobs a = {};
-  unsigned long long blocks = 0;
+  unsigned blocks = 0;
   for (int i = 0; i < n; ++i) {
     const PackSource& q = src[i];
-    const int to = (q.cols + 7) / 8 * 8;
-    a.job[i] = {q.from.p, q.from.row, q.from.member, q.to, q.members, q.rows, q.cols, to, (unsigned)blocks};
-    blocks += ((unsigned long long)q.members * q.rows * (to / 8) + 256 * kPackEach - 1) / (256 * kPackEach);
+    const int per_row = (q.cols + 7) / 8;
+    const unsigned long long vectors = (unsigned long long)q.members * q.rows * per_row;
+    if (vectors > 0x7FFFF000ull) return cudaErrorInvalidConfiguration;      // (a 32 GB operand)
+    a.job[i] = {q.from.p, q.from.row, q.from.member, q.to, q.rows, q.cols, per_row, (uint32_t)vectors, divisor(per_row), divisor(q.rows), blocks};
+    blocks += (unsigned)((vectors + 256 * kPackEach - 1) / (256 * kPackEach));
   }
-  if (blocks > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
   a.n = n;
-  return launch_with((unsigned)blocks, 256, 0, s)(k_gated_pack, a);
+  return launch_with(blocks, 256, 0, s)(k_gated_pack, a);
 }
 
 static cudaError_t rows_forward(const pbt_gated_desc* d, const Operand& x, const Operand& w, void* h, float* z, int pitch, cudaStream_t s) {
