@@ -230,9 +230,9 @@ __device__ __forceinline__ void gated_tiles(const TileMaps& maps, const TilePara
       }
       if (!ok) give_up(31);
       // Every stage that was armed has landed before the CTA ends, and been read unless a wait ran out.  What a pair's second CTA loads is
-      // counted by the leader alone; when one of them gave up, it may not be counted at all, and has a millisecond to land.
+      // counted by the leader alone; when one of them gave up, a stage may never be complete or not be counted, and what is under way has a millisecond to land.
       if (rank == 0)
-        for (int s = 0; s < STAGES; ++s) mbar_wait_out(&full[s], s < (int)stage ? phase : phase ^ 1);
+        for (int s = 0; s < STAGES; ++s) mbar_wait_out(&full[s], s < (int)stage ? phase : phase ^ 1, PAIR && *abort_flag ? 1u << 14 : 1u << 22);
       for (int i = 0; PAIR && !ok && i < 16384; ++i) __nanosleep(64);
       for (int s = 0; s < STAGES && ok; ++s) {
         if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) break;
