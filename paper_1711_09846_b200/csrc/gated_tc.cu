@@ -53,6 +53,8 @@ struct Tile {
   static constexpr uint32_t kCols = 4 * HN;    // two accumulators of g and u
 };
 
+// brings a tensor map into the cache of descriptors, ahead of the first load
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 // a bounded wait of a whole warp: every lane gives up if one does
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
   return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag));
@@ -175,6 +177,7 @@ __device__ __forceinline__ void gated_tiles(const TileMaps& maps, const TilePara
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = PAIR ? cluster_ctarank() : 0;
   const int first = PAIR ? blockIdx.x >> 1 : blockIdx.x, step = PAIR ? gridDim.x >> 1 : gridDim.x;
+  if (threadIdx.x == 64) { prefetch_map(&maps.x); prefetch_map(&maps.w); }
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
     for (int a = 0; a < 2; ++a) { mbar_init(&tfull[a], 1); mbar_init(&tempty[a], (PAIR ? 2 : 1) * kEpiW); }
@@ -337,6 +340,7 @@ constexpr int kRowsForward = 32;
 constexpr int kRowsLanes = 128, kRowsPitch = kRowsLanes + 4;      // floats of a row's partial sums
 constexpr int kRowsThreads = 192;
 constexpr int kRowsSplits = 8;
+constexpr int kSms = 148;              // (what tiles and splits are counted against)
 
 struct RowsParams {
   int rows, blocks;               // blocks of N rows of a member
@@ -348,11 +352,12 @@ struct RowsParams {
   pbt_drop_rule rule;
   Counters* counters;
 };
-template <int N>
+// DEEP: for two CTAs an SM at most, with more of the weight under way; else more CTAs share it, one's set-up and end beside another's loads
+template <int N, bool DEEP>
 struct RowsTile {
   static constexpr int kStage = (128 + N) * kBK * 2;
-  static constexpr int kStages = 3;
-  static constexpr int kPerSm = N == 16 ? 4 : N <= 64 ? 3 : 2;          // CTAs that share an SM: one's set-up and end beside another's loads
+  static constexpr int kStages = DEEP ? 5 : 3;
+  static constexpr int kPerSm = DEEP ? 2 : N == 16 ? 4 : N <= 64 ? 3 : 2;
   static constexpr int kSums = N * kRowsPitch * 4;
   static constexpr int kBars = kStages * kStage > kSums ? kStages * kStage : (kSums + 255) / 256 * 256;
   static constexpr int kTotal = kBars + 256 + 1024;
@@ -366,9 +371,9 @@ __device__ __forceinline__ float4 ld_cluster(uint32_t addr) {
   return v;
 }
 
-template <int N, bool DX, int THREADS>
+template <int N, bool DX, bool DEEP, int THREADS>
 __device__ __forceinline__ void rows_product(const CUtensorMap& tmA, const CUtensorMap& tmB, const RowsParams& p, uint8_t* smem_raw, int tile, int m, int t0) {
-  typedef RowsTile<N> L;
+  typedef RowsTile<N, DEEP> L;
   constexpr int kUnits = DX ? kRowsLanes : kRowsLanes / 2;       // hidden units, or columns of dx
   uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBars);
@@ -379,6 +384,7 @@ __device__ __forceinline__ void rows_product(const CUtensorMap& tmA, const CUten
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int splits = (int)cluster_size(), rank = (int)cluster_ctarank(), n0 = tile * kUnits;
   const int kb0 = (int)((long long)p.k_blocks * rank / splits), kb1 = (int)((long long)p.k_blocks * (rank + 1) / splits);
+  if (threadIdx.x == 32) { prefetch_map(&tmA); prefetch_map(&tmB); }
   if (threadIdx.x == 0) {
     for (int s = 0; s < L::kStages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
     mbar_init(done, 1);
@@ -515,11 +521,11 @@ __device__ __forceinline__ void rows_product(const CUtensorMap& tmA, const CUten
   if (warp == 1) tmem_dealloc(tmem, L::kCols);
 }
 // DX: launched while the kernel that makes dg and du runs
-template <int N, bool DX>
-__global__ void __launch_bounds__(kRowsThreads, RowsTile<N>::kPerSm) k_gated_rows(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const RowsParams p) {
+template <int N, bool DX, bool DEEP>
+__global__ void __launch_bounds__(kRowsThreads, RowsTile<N, DEEP>::kPerSm) k_gated_rows(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const RowsParams p) {
   if (!DX) pdl_prologue();
   extern __shared__ uint8_t smem_raw[];
-  rows_product<N, DX, kRowsThreads>(tmA, tmB, p, smem_raw, (int)(blockIdx.x / cluster_size()), blockIdx.y / p.blocks, (int)(blockIdx.y % p.blocks) * N);
+  rows_product<N, DX, DEEP, kRowsThreads>(tmA, tmB, p, smem_raw, (int)(blockIdx.x / cluster_size()), blockIdx.y / p.blocks, (int)(blockIdx.y % p.blocks) * N);
 }
 
 // the parts of a contraction: as many as there are places for CTAs, four blocks each at least
@@ -528,15 +534,26 @@ int rows_splits(long long tiles, int k_blocks, long long places) {
   while (splits < kRowsSplits && tiles * splits * 2 <= places && k_blocks >= splits * 2 * 4) splits *= 2;
   return splits;
 }
-template <int N, bool DX>
-cudaError_t launch_rows(const pbt_gated_desc* d, const RowsParams& p, const CUtensorMap& tmA, const CUtensorMap& tmB, cudaStream_t s) {
+template <int N, bool DX, bool DEEP>
+cudaError_t launch_rows(const pbt_gated_desc* d, const RowsParams& p, const CUtensorMap& tmA, const CUtensorMap& tmB, unsigned units, unsigned blocks, int splits,
+                        cudaStream_t s) {
+  typedef RowsTile<N, DEEP> L;
   static DeviceSetup setup;
   int sms = 0;
-  const cudaError_t e = device_setup(&setup, k_gated_rows<N, DX>, RowsTile<N>::kTotal, &sms);
+  const cudaError_t e = device_setup(&setup, k_gated_rows<N, DX, DEEP>, L::kTotal, &sms);
   if (e != cudaSuccess) return e;
+  return launch_clusters(dim3(units * splits, blocks), kRowsThreads, L::kTotal, splits, DX, s, k_gated_rows<N, DX, DEEP>, tmA, tmB, p);
+}
+// (32 rows, 2048 -> 4096, 256 CTAs: 10.8 us deep, 12.0 else; 40 members x 20 rows, 512 -> 1024, 640: 26 and 22)
+template <int N, bool DX>
+cudaError_t launch_rows(const pbt_gated_desc* d, const RowsParams& p, const CUtensorMap& tmA, const CUtensorMap& tmB, cudaStream_t s) {
   const unsigned units = DX ? (d->width + 127) / 128 : (d->hidden + 63) / 64, blocks = (unsigned)p.blocks * d->members;
-  const int splits = rows_splits((long long)units * blocks, p.k_blocks, (long long)sms * RowsTile<N>::kPerSm);
-  return launch_clusters(dim3(units * splits, blocks), kRowsThreads, RowsTile<N>::kTotal, splits, DX, s, k_gated_rows<N, DX>, tmA, tmB, p);
+  const long long tiles = (long long)units * blocks;
+  if constexpr (N <= 32) {
+    const int splits = rows_splits(tiles, p.k_blocks, 2 * kSms);
+    if (tiles * splits <= 2 * kSms) return launch_rows<N, DX, true>(d, p, tmA, tmB, units, blocks, splits, s);
+  }
+  return launch_rows<N, DX, false>(d, p, tmA, tmB, units, blocks, rows_splits(tiles, p.k_blocks, kSms * RowsTile<N, false>::kPerSm), s);
 }
 int rows_columns(const pbt_gated_desc* d) { return d->rows <= 16 ? 16 : d->rows <= 32 ? 32 : d->rows <= 64 ? 64 : 128; }
 // what the two products of this form have in common; k: their contraction
@@ -658,7 +675,7 @@ struct FewParams {
 template <int N>
 struct FewShared {
   static constexpr int kOuter = (int)sizeof(OuterShared<N / 16>) + 16;
-  static constexpr int kTotal = RowsTile<N>::kTotal > kOuter ? RowsTile<N>::kTotal : kOuter;
+  static constexpr int kTotal = RowsTile<N, false>::kTotal > kOuter ? RowsTile<N, false>::kTotal : kOuter;
 };
 // Clusters of CTAs for dx first, then a CTA for every tile of dW; launched while the kernel that makes dg and du runs.
 template <int N>
@@ -666,7 +683,7 @@ __global__ void __launch_bounds__(256, N == 16 ? 4 : 3) k_gated_few_gradients(co
   extern __shared__ uint8_t smem_raw[];
   if ((int)blockIdx.x < p.dx_blocks) {
     const int cluster = (int)(blockIdx.x / cluster_size());
-    rows_product<N, true, 256>(tmA, tmB, p.dx, smem_raw, cluster % p.dx_tiles, cluster / p.dx_tiles, 0);
+    rows_product<N, true, false, 256>(tmA, tmB, p.dx, smem_raw, cluster % p.dx_tiles, cluster / p.dx_tiles, 0);
     return;
   }
   if (blockIdx.x < p.blocks) {
