@@ -39,6 +39,23 @@ struct CellArgs {
   pbt_drop_rule rule;
 };
 
+__device__ __forceinline__ void store_pairs(float* p, const Eight& e) {
+#pragma unroll
+  for (int c = 0; c < kGroup; ++c) p[c] = e.v[c];
+}
+// pairs from the first 4-byte boundary on
+__device__ __forceinline__ void store_pairs(bf16* p, const Eight& e) {
+  auto pair = [&](int c) { *reinterpret_cast<__nv_bfloat162*>(p + c) = __floats2bfloat162_rn(e.v[c], e.v[c + 1]); };
+  if (((uintptr_t)p & 3) == 0) {
+#pragma unroll
+    for (int c = 0; c < kGroup; c += 2) pair(c);
+  } else {
+    store(p, e.v[0]);
+#pragma unroll
+    for (int c = 1; c < kGroup - 1; c += 2) pair(c);
+    store(p + kGroup - 1, e.v[kGroup - 1]);
+  }
+}
 // VEC: 16-byte loads and stores everywhere.  Bound by its bytes, 14 a hidden unit in bf16 (80 x 512 x 2048: 189 us, 6.2 TB/s).
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) k_gated_cells(const CellArgs<T> a) {
@@ -54,13 +71,13 @@ __global__ void __launch_bounds__(256) k_gated_cells(const CellArgs<T> a) {
   const T* from = a.dh + m * a.dh_member + row * a.dh_row + c0;
   const uint4 z0 = load16(z), z1 = load16(z + 4), z2 = load16(z + a.pitch), z3 = load16(z + a.pitch + 4);
   Eight dh;
-  if (!VEC) {
+  if constexpr (sizeof(T) == 2) {
+    dh = unpack(VEC ? load16(from) : joined(pieces_of(from, (int)n)));
+  } else if constexpr (VEC) {
+    dh = unpack(load16(from), load16(from + 4));
+  } else {
 #pragma unroll
     for (int c = 0; c < kGroup; ++c) dh.v[c] = c < n ? as_float(from[c]) : 0.f;
-  } else if constexpr (sizeof(T) == 2) {
-    dh = unpack(load16(from));
-  } else {
-    dh = unpack(load16(from), load16(from + 4));
   }
   const Eight g = unpack(z0, z1), u = unpack(z2, z3);
   uint32_t in = 0xFFu;
@@ -82,6 +99,9 @@ __global__ void __launch_bounds__(256) k_gated_cells(const CellArgs<T> a) {
   if constexpr (VEC) {
     store8(out, dg);
     store8(out + a.hidden, du);
+  } else if (n == kGroup) {
+    store8(out, dg);              // (a row of dg and du begins on 16 bytes, du within it anywhere)
+    store_pairs(out + a.hidden, du);
   } else {
 #pragma unroll
     for (int c = 0; c < kGroup; ++c) {

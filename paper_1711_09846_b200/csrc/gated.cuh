@@ -32,6 +32,40 @@ cudaError_t f32_forward(const pbt_gated_desc* d, float* h, float* z, int pitch, 
 cudaError_t f32_backward(const pbt_gated_desc* d, const float* dz, int dz_pitch, cudaStream_t s);
 
 #ifdef __CUDACC__
+// Eight bf16 elements from any place, of which the first n (1 to 8) exist and the others come as zeros: the 16-byte pieces that hold them, the second one
+// only if one of the n lies in it (nothing is read beyond the piece that holds the last of them), shifted together.
+struct Pieces {
+  uint4 a, b;
+  int off, n;
+};
+__device__ __forceinline__ Pieces pieces_of(const bf16* from, int n) {
+  Pieces p;
+  const uintptr_t addr = (uintptr_t)from;
+  const uint4* piece = reinterpret_cast<const uint4*>(addr & ~(uintptr_t)15);
+  p.off = (int)(addr & 15) / 2;
+  p.n = n;
+  p.a = __ldg(piece);
+  p.b = p.off + n > 8 ? __ldg(piece + 1) : make_uint4(0u, 0u, 0u, 0u);
+  return p;
+}
+__device__ __forceinline__ uint4 joined(const Pieces& p) {
+  uint32_t w[8] = {p.a.x, p.a.y, p.a.z, p.a.w, p.b.x, p.b.y, p.b.z, p.b.w};      // (off + 7 < 16)
+  if (p.off & 4)
+#pragma unroll
+    for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+  if (p.off & 2)
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+  const uint32_t bits = (p.off & 1) * 16;
+  uint32_t o[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = __funnelshift_r(w[i], w[i + 1], bits);
+  if (p.n < 8)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = 2 * i >= p.n ? 0u : 2 * i + 1 >= p.n ? o[i] & 0xFFFFu : o[i];
+  return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
 // Launches clusters of `cluster` CTAs; `after`: they may begin while the predecessor in the stream still runs (see launch_after).
 template <typename... KArgs, typename... Args>
 cudaError_t launch_clusters(dim3 grid, unsigned threads, size_t smem, unsigned cluster, bool after, cudaStream_t s, void (*kernel)(KArgs...), Args&&... args) {

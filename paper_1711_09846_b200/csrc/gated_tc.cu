@@ -748,47 +748,25 @@ struct PackJobs {
   PackJob job[2];
   int n;
 };
-// Eight elements from any place as a vector: the 16-byte pieces that hold them, the second one only if an element of the row lies in it, shifted together.
 // Bound by issue as much as by the transfers.
 __global__ void __launch_bounds__(256) k_gated_pack(const PackJobs a) {
   pdl_prologue();
   const bool second = a.n > 1 && blockIdx.x >= a.job[1].block0;
   const PackJob j = second ? a.job[1] : a.job[0];
   const uint32_t first = (blockIdx.x - j.block0) * (256 * kPackEach) + threadIdx.x;
-  uint4 a0[kPackEach], a1[kPackEach];
-  int off[kPackEach], n[kPackEach];
+  Pieces pieces[kPackEach];
 #pragma unroll
   for (int u = 0; u < kPackEach; ++u) {
     const uint32_t i = first + u * 256;
-    n[u] = 0;
     if (i >= j.vectors) continue;
     const uint32_t at = quotient(i, j.by_row), m = quotient(at, j.by_member);
     const int c = (int)(i - at * j.per_row) * 8;
-    const uintptr_t addr = (uintptr_t)(j.src + m * j.member + (long long)(at - m * j.rows) * j.row + c);
-    const uint4* piece = reinterpret_cast<const uint4*>(addr & ~(uintptr_t)15);
-    off[u] = (int)(addr & 15) / 2;
-    n[u] = min(8, j.cols - c);
-    a0[u] = __ldg(piece);
-    a1[u] = off[u] + n[u] > 8 ? __ldg(piece + 1) : make_uint4(0u, 0u, 0u, 0u);
+    pieces[u] = pieces_of(j.src + m * j.member + (long long)(at - m * j.rows) * j.row + c, min(8, j.cols - c));
   }
 #pragma unroll
   for (int u = 0; u < kPackEach; ++u) {
-    if (!n[u]) continue;
-    uint32_t w[8] = {a0[u].x, a0[u].y, a0[u].z, a0[u].w, a1[u].x, a1[u].y, a1[u].z, a1[u].w};      // (off + 7 < 16)
-    if (off[u] & 4)
-#pragma unroll
-      for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
-    if (off[u] & 2)
-#pragma unroll
-      for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
-    const uint32_t bits = (off[u] & 1) * 16;
-    uint32_t o[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = __funnelshift_r(w[i], w[i + 1], bits);
-    if (n[u] < 8)                 // a row's last vector: zeros behind its last element
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] = 2 * i >= n[u] ? 0u : 2 * i + 1 >= n[u] ? o[i] & 0xFFFFu : o[i];
-    *reinterpret_cast<uint4*>(j.dst + (long long)(first + u * 256) * 8) = make_uint4(o[0], o[1], o[2], o[3]);
+    const uint32_t i = first + u * 256;
+    if (i < j.vectors) *reinterpret_cast<uint4*>(j.dst + (long long)i * 8) = joined(pieces[u]);
   }
 }
 
