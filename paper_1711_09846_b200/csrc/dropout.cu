@@ -2,6 +2,8 @@
 //
 // One pass over x (and residual): 4 or 6 bytes an element in bf16, 8 or 12 in fp32.  A group of eight neighbouring columns shares one
 // block of the generator (20 32-bit multiplications with a 64-bit product), so that the draws cost less than the transfers.
+#include <type_traits>
+
 #include "dropout.cuh"
 
 namespace pbt {
@@ -175,10 +177,18 @@ cudaError_t launch(const pbt_dropout_desc* d, cudaStream_t s) {
   auto grid = [&](int per_block) { return dim3((unsigned)((per_member + per_block - 1) / per_block), (unsigned)d->members); };
   if (vectors) {
     const bool flat = d->rows == 1 || (d->x_row == d->width && (!RESIDUAL || d->residual_row == d->width));
-    // two groups a thread once every SM has its fill of threads
-    const bool large = per_member * d->members >= 148ull * 2048 * 2;
-    if (flat) return large ? launch_with(grid(512), 256, 0, s)(k_dropout<T, RESIDUAL, true, 2>, a) : launch_with(grid(256), 256, 0, s)(k_dropout<T, RESIDUAL, true, 1>, a);
-    return large ? launch_with(grid(512), 256, 0, s)(k_dropout<T, RESIDUAL, false, 2>, a) : launch_with(grid(256), 256, 0, s)(k_dropout<T, RESIDUAL, false, 1>, a);
+    // Groups of a thread: bf16 takes two or three, which share the generator's first rounds (they go by the member and the step alone) and keep more
+    // bytes under way; fp32, twice the bytes a group, one.  80 x 512 x 2048 bf16 with residual (without): one 90.7 us (77.8), two 87.4 (66.2), three 79.3
+    // (61.9), four 79.2 (63.7), and a plain copy of 4 bytes an element 52.5; 16 x 256 x 1024: 5.9, 5.5, 5.9; 80 x 512 x 2048 fp32 146.1 (98.6), 146.0 (101.4).
+    const uint64_t all = per_member * d->members, fill = 148ull * 2048;       // the GPU's threads
+    const int each = sizeof(T) == 4 || all < fill ? 1 : all < 4 * fill ? 2 : 3;
+    auto go = [&](auto is_flat) {
+      constexpr bool F = decltype(is_flat)::value;
+      if (each == 3) return launch_with(grid(768), 256, 0, s)(k_dropout<T, RESIDUAL, F, 3>, a);
+      if (each == 2) return launch_with(grid(512), 256, 0, s)(k_dropout<T, RESIDUAL, F, 2>, a);
+      return launch_with(grid(256), 256, 0, s)(k_dropout<T, RESIDUAL, F, 1>, a);
+    };
+    return flat ? go(std::true_type()) : go(std::false_type());
   }
   const long long total = cells * d->members, blocks = (total + 256 * kGroup - 1) / (256 * kGroup);
   const uintptr_t bases = (uintptr_t)d->x | (uintptr_t)d->y | (RESIDUAL ? (uintptr_t)d->residual : 0);
