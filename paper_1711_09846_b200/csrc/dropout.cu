@@ -87,53 +87,92 @@ __global__ void __launch_bounds__(256) k_dropout(const Args<T> a) {
   }
 }
 
-// Any width from 8 on, all activations without gaps: a thread has eight elements that follow one another from a 16-byte boundary, which belong to
-// two or three groups and one or two rows (the second one perhaps of the next member).  I: 32 bits as far as they hold every place (a 64-bit
-// division costs as much as the draws).
-template <typename T, bool RESIDUAL, typename I>
-__global__ void __launch_bounds__(256) k_dropout_odd(const Args<T> a, I total) {
+// Any width from 8 on, all activations without gaps (less than 2^31 elements of them): a thread has U vectors of eight elements from a 16-byte boundary, 32
+// apart, which belong to two or three groups and one or two rows (the second one perhaps of the next member).  Every lane draws the group that its vector begins
+// in; the next vector, the next lane's, begins in the group that follows it, or in the first one of the next row, so that its bits come from there, the last
+// lane's from one more draw of the warp.  Only a row's last vector, where it begins inside
+// the last group but one, takes a draw of its own.  Bound by issue (80 x 512 x 2047 bf16 68 % of the cycles; 2048 columns take 62 us, these 114).
+template <typename T, bool RESIDUAL, int U>
+__global__ void __launch_bounds__(256) k_dropout_odd(const Args<T> a, const uint32_t total, const Divisor by_width, const Divisor by_rows) {
   pdl_prologue();
-  const I at = ((I)blockIdx.x * 256 + threadIdx.x) * kGroup;
-  if (at >= total) return;
-  const bool whole = total - at >= kGroup;
-  const I line = at / a.width;                               // row of all members' rows
-  const uint32_t col = (uint32_t)(at - line * a.width), m = (uint32_t)(line / a.rows), row = (uint32_t)(line - (I)m * a.rows), left = a.width - col;
-  Eight e, q;
-  if (whole) {
-    e = values(load8(a.x + at));
-    if (RESIDUAL) q = values(load8(a.residual + at));
-  } else {
+  const int lane = threadIdx.x & 31;
+  const uint32_t v0 = (blockIdx.x * 8 + (threadIdx.x >> 5)) * (32 * U) + lane;
+  if ((v0 - lane) * kGroup >= total) return;
+  Raw<T> vx[U], vr[U];
 #pragma unroll
-    for (int c = 0; c < kGroup; ++c) {
-      e.v[c] = c < total - at ? as_float(a.x[at + c]) : 0.f;
-      if (RESIDUAL) q.v[c] = c < total - at ? as_float(a.residual[at + c]) : 0.f;
+  for (int u = 0; u < U; ++u) {
+    const uint32_t at = (v0 + u * 32) * kGroup;
+    if (at + kGroup > total) continue;
+    vx[u] = load8(a.x + at);
+    if (RESIDUAL) vr[u] = load8(a.residual + at);
+  }
+  struct Place {
+    uint32_t at, row, col, member;
+  };
+  auto place = [&](int u) {
+    Place q;
+    q.at = (v0 + u * 32) * kGroup;
+    const uint32_t line = quotient(q.at, by_width);
+    q.member = quotient(line, by_rows);
+    q.row = line - q.member * a.rows;
+    q.col = q.at - line * a.width;
+    return q;
+  };
+  uint32_t bits[U + 1], last = 0xFFFFFFFFu;
+  float scale[U + 1];
+  Draw d = {};
+#pragma unroll
+  for (int u = 0; u <= U; ++u) {
+    const Place q = place(u);
+    bits[u] = 0;
+    if (q.at >= total) continue;
+    if (q.member != last) d = draw_of(a.rule, q.member);
+    last = q.member;
+    bits[u] = kept_bits(d, q.row * a.groups + q.col / kGroup);
+    scale[u] = d.on ? d.scale : 1.f;
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const uint32_t across = __shfl_down_sync(0xFFFFFFFFu, bits[u], 1), around = __shfl_sync(0xFFFFFFFFu, bits[u + 1], 0), next = lane == 31 ? around : across;
+    const Place q = place(u);
+    const uint32_t at = q.at, shift = q.col % kGroup, left = a.width - q.col;
+    if (at >= total) continue;
+    uint32_t in = bits[u] >> shift;
+    float next_scale = scale[u];
+    if (left > kGroup) {
+      in |= next << (kGroup - shift);               // (without a shift nothing of it is looked at)
+    } else {
+      if (shift && left > kGroup - shift) in |= kept_bits(draw_of(a.rule, q.member), q.row * a.groups + q.col / kGroup + 1) << (kGroup - shift);
+      if (left < kGroup) {
+        in = (in & ((1u << left) - 1u)) | next << left;
+        if (q.row + 1 == a.rows && at + left < total) {
+          const Draw other = draw_of(a.rule, q.member + 1);
+          next_scale = other.on ? other.scale : 1.f;
+        }
+      }
     }
-  }
-  const Draw d = draw_of(a.rule, m);
-  const uint32_t block = row * a.groups + col / kGroup, shift = col % kGroup;
-  uint32_t bits = kept_bits(d, block) >> shift;
-  float scale = d.on ? d.scale : 1.f, next_scale = scale;
-  if (shift && left > kGroup - shift) bits |= kept_bits(d, block + 1) << (kGroup - shift);
-  if (left < kGroup && left < total - at) {
-    Draw next = d;
-    const bool same = row + 1 < a.rows;
-    if (!same) {
-      next = draw_of(a.rule, m + 1);
-      next_scale = next.on ? next.scale : 1.f;
+    if (at + kGroup <= total) {
+      Eight e = values(vx[u]);
+      if (next_scale == scale[u]) {
+#pragma unroll
+        for (int c = 0; c < kGroup; ++c) e.v[c] = drop(e.v[c], in >> c & 1u, scale[u]);
+      } else {
+#pragma unroll
+        for (int c = 0; c < kGroup; ++c) e.v[c] = drop(e.v[c], in >> c & 1u, c < left ? scale[u] : next_scale);
+      }
+      if (RESIDUAL) {
+        const Eight r = values(vr[u]);
+#pragma unroll
+        for (int c = 0; c < kGroup; ++c) e.v[c] += r.v[c];
+      }
+      store8(a.y + at, e);
+    } else {
+      for (uint32_t c = 0; at + c < total; ++c) {
+        float v = drop(as_float(a.x[at + c]), in >> c & 1u, c < left ? scale[u] : next_scale);
+        if (RESIDUAL) v += as_float(a.residual[at + c]);
+        store(a.y + at + c, v);
+      }
     }
-    bits = (bits & ((1u << left) - 1u)) | kept_bits(next, same ? (row + 1) * a.groups : 0u) << left;
-  }
-#pragma unroll
-  for (int c = 0; c < kGroup; ++c) {
-    e.v[c] = drop(e.v[c], bits >> c & 1u, c < left ? scale : next_scale);
-    if (RESIDUAL) e.v[c] += q.v[c];
-  }
-  if (whole) {
-    store8(a.y + at, e);
-  } else {
-#pragma unroll
-    for (int c = 0; c < kGroup; ++c)
-      if (c < total - at) store(a.y + at + c, e.v[c]);
   }
 }
 
@@ -190,11 +229,17 @@ cudaError_t launch(const pbt_dropout_desc* d, cudaStream_t s) {
     };
     return flat ? go(std::true_type()) : go(std::false_type());
   }
-  const long long total = cells * d->members, blocks = (total + 256 * kGroup - 1) / (256 * kGroup);
+  const long long total = cells * d->members;
   const uintptr_t bases = (uintptr_t)d->x | (uintptr_t)d->y | (RESIDUAL ? (uintptr_t)d->residual : 0);
-  if (d->width >= kGroup && (bases & 15) == 0 && blocks <= 0x7FFFFFFF && gapless(d->x_member, d->x_row) && (!RESIDUAL || gapless(d->residual_member, d->residual_row))) {
-    if (total < 0xFFFFF000ll) return launch_with((unsigned)blocks, 256, 0, s)(k_dropout_odd<T, RESIDUAL, uint32_t>, a, (uint32_t)total);
-    return launch_with((unsigned)blocks, 256, 0, s)(k_dropout_odd<T, RESIDUAL, unsigned long long>, a, (unsigned long long)total);
+  if (d->width >= kGroup && (bases & 15) == 0 && total < 0x7FFF0000ll && gapless(d->x_member, d->x_row) &&
+      (!RESIDUAL || gapless(d->residual_member, d->residual_row))) {
+    // Vectors of a thread, once the GPU has its fill of threads with them: 80 x 512 x 2047 bf16 with residual (without) two 133 us (126), three 127 (114), four
+    // 142 (113); fp32 162 (129), 179 (127), 167 (147).
+    constexpr int U = sizeof(T) == 4 && RESIDUAL ? 2 : 3;
+    const Divisor by_width = divisor((uint32_t)d->width), by_rows = divisor((uint32_t)d->rows);
+    auto blocks = [&](int each) { return (unsigned)((total + 256 * kGroup * each - 1) / (256 * kGroup * each)); };
+    if (total >= 148ll * 2048 * kGroup * 2) return launch_with(blocks(U), 256, 0, s)(k_dropout_odd<T, RESIDUAL, U>, a, (uint32_t)total, by_width, by_rows);
+    return launch_with(blocks(1), 256, 0, s)(k_dropout_odd<T, RESIDUAL, 1>, a, (uint32_t)total, by_width, by_rows);
   }
   return launch_with(grid(256), 256, 0, s)(k_dropout_strided<T, RESIDUAL>, a);
 }

@@ -11,7 +11,18 @@ int check_rule(const pbt_drop_rule* r, long long members, long long rows, long l
 // columns that one block of the generator serves
 constexpr int kGroup = 8;
 
+// n / d for n < 2^31 in two instructions (the quotient of a product with a rounded reciprocal of 32 bits; the error stays below 1 / d there)
+struct Divisor {
+  uint32_t factor, shift;
+};
+inline Divisor divisor(uint32_t d) {
+  uint32_t s = 0;
+  while (s < 31 && (1u << s) < d) ++s;                          // 2^(s - 1) < d <= 2^s
+  return {(uint32_t)(((1ull << (31 + s)) + d - 1) / d), s};     // (d = 1: 2^31)
+}
 #ifdef __CUDACC__
+__device__ __forceinline__ uint32_t quotient(uint32_t n, Divisor d) { return (uint32_t)(((uint64_t)n * d.factor) >> 31) >> d.shift; }
+
 // What a thread has to know to draw for one member.
 struct Draw {
   uint32_t member, step, stream;

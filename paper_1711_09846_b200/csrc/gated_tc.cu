@@ -17,7 +17,10 @@ namespace gated {
 namespace {
 
 using namespace tc;
+using dropout::Divisor;
+using dropout::divisor;
 using dropout::Eight;
+using dropout::quotient;
 using dropout::store8;
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -724,17 +727,6 @@ cudaError_t launch_few(const pbt_gated_desc* d, FewParams& p, const CUtensorMap&
 // ------------------------------------------------------------------------------------------------------------------
 // Operands whose rows are not multiples of 16 bytes are copied once into rows that are, both in one launch.
 // ------------------------------------------------------------------------------------------------------------------
-// n / d for n < 2^31 in two instructions (the quotient of a product with a rounded reciprocal of 32 bits; the error stays below 1 / d there)
-struct Divisor {
-  uint32_t factor, shift;
-};
-Divisor divisor(uint32_t d) {
-  uint32_t s = 0;
-  while (s < 31 && (1u << s) < d) ++s;                          // 2^(s - 1) < d <= 2^s
-  return {(uint32_t)(((1ull << (31 + s)) + d - 1) / d), s};     // (d = 1: 2^31)
-}
-__device__ __forceinline__ uint32_t quotient(uint32_t n, Divisor d) { return (uint32_t)(((uint64_t)n * d.factor) >> 31) >> d.shift; }
-
 struct PackJob {
   const bf16* src; long long row, member;
   bf16* dst;

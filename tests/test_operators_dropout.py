@@ -67,8 +67,10 @@ def test_the_oracle_of_the_masks_is_the_generator():
     assert s == [65536 / (65536 - bits), 0.0]
 
 
+# (the last ones: vectors that reach over rows and members, in small calls and in those that fill the GPU)
 SHAPES = [(1, 1, 1), (1, 1, 8), (2, 3, 7), (1, 5, 64), (3, 17, 100), (2, 33, 256), (1, 4, 1001), (5, 9, 1000), (2, 40, 2048), (1, 3, 2052),
-          (1, 2, 8191), (70, 3, 48), (1, 6000, 24), (300, 1, 9)]
+          (1, 2, 8191), (70, 3, 48), (1, 6000, 24), (300, 1, 9), (400, 1, 13), (7, 1, 8), (9, 3, 11),
+          (600, 9, 1003), (5000, 1, 1001), (2, 20000, 139)]
 
 
 @pytest.mark.gpu
@@ -170,19 +172,20 @@ def test_draws_follow_member_step_site_and_seed():
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
-def test_activations_beyond_32_bit_offsets(dtype):
+@pytest.mark.parametrize("width", [2047, 2048])
+def test_activations_beyond_32_bit_offsets(width, dtype):
     """The last rows of more than 2^31 elements, in one member and as members that lie far apart."""
     import torch
     import paper_1711_09846_b200 as pbt
-    rows, width = 1_100_000, 2048
+    rows = 1_100_000
     x = torch.empty(1, rows, width, device="cuda", dtype=getattr(torch, dtype)).fill_(1.5)
     y = pbt.dropout_forward(x, pbt.Dropout(0.25, 7, 8), residual=x)[0, -2:].clone()
     block = (np.arange(2, dtype=np.uint64)[:, None] + np.uint64(rows - 2)) * np.uint64(256) + np.arange(256, dtype=np.uint64)
     words = philox4x32_10_np(np.uint64(0), np.uint64(8), np.uint64(5), block, 7)
-    bits = np.stack([w >> s & np.uint32(0xFFFF) for w in words for s in (np.uint32(0), np.uint32(16))], -1).reshape(2, width)
+    bits = np.stack([w >> s & np.uint32(0xFFFF) for w in words for s in (np.uint32(0), np.uint32(16))], -1).reshape(2, 2048)[:, :width]
     assert torch.equal(y.cpu().double(), torch.from_numpy(np.where(bits >= 16384, 1.5 / 0.75, 0.0) + 1.5))
-    far = x.view(-1)[:2 * rows * 1024].view(2, rows, 1024)[:, :3]       # (the second member 2^30 elements on)
-    _verify(pbt.dropout_forward(far, pbt.Dropout(0.25, 7, 8)), far, None, scales(2, 3, 1024, [0.25] * 2, 7, [8] * 2))
+    far = x.view(-1)[:2 * rows * 1000].view(2, rows, 1000)[:, :3]       # (the second member 1.1e9 elements on)
+    _verify(pbt.dropout_forward(far, pbt.Dropout(0.25, 7, 8)), far, None, scales(2, 3, 1000, [0.25] * 2, 7, [8] * 2))
 
 
 @pytest.mark.gpu
