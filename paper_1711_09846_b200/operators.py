@@ -435,7 +435,7 @@ class Dropout:
     the same); first_member: index of the first member in the whole population, for a shard of it.
 
     The tensors are used where they lie: update them in place between calls.  Both passes of a step take the same object (or an equal one)."""
-    __slots__ = ("rate", "seed", "step", "site", "first_member", "tensors", "members", "device", "rule")
+    __slots__ = ("rate", "seed", "step", "site", "first_member", "tensors", "members", "device", "rule", "_known")
 
     def __init__(self, rate: Union[float, torch.Tensor], seed: int, step: Union[int, torch.Tensor], site: int = 0, first_member: int = 0):
         self.rate, self.seed, self.step, self.site, self.first_member = rate, seed, step, site, first_member
@@ -454,6 +454,7 @@ class Dropout:
         self.members, self.device = (self.tensors[0].shape[0], self.tensors[0].device) if self.tensors else (None, None)
         _require(all(t.shape[0] == self.members and t.device == self.device for t in self.tensors), "a dropout's rate and step differ in members or device")
         self.rule = PbtDropRule(rates, steps, seed, step, rate, site, first_member)
+        self._known = (None, None, b"")                  # geometry of the last dropout_forward's activations, and what the library is told of it
 
     def _for(self, members, device) -> PbtDropRule:
         if self.members is not None and (self.members != members or self.device != device):
@@ -463,18 +464,30 @@ class Dropout:
 
 def dropout_forward(x, dropout: Dropout, residual=None, stream=None):
     """residual + keep x / (1 - rate) (pbt_dropout); x and residual: [members, rows, width], float32 or bfloat16, with contiguous columns."""
-    shape, dtype, device = x.shape, x.dtype, x.device
+    kind = (x.shape, x.stride(), x.dtype, x.device)
+    other = None if residual is None else (residual.shape, residual.stride(), residual.dtype, residual.device)
+    known, known_other, told = dropout._known
+    if known != kind or known_other != other:            # (checks and description cost a small call as much as its launch)
+        told = _describe_dropout(x, dropout, residual)
+        dropout._known = (kind, other, told)
+    d = PbtDropoutDesc.from_buffer_copy(told)
+    d.x = x.data_ptr()
+    if residual is not None:
+        d.residual = residual.data_ptr()
+    return _on(kind[3], stream, () if stream is None else (x, residual, *dropout.tensors), _dropout, d, x)
+
+
+def _describe_dropout(x, dropout, residual) -> bytes:
+    """What pbt_dropout is told of activations like these, their addresses apart."""
+    shape, dtype, device = kind = x.shape, x.dtype, x.device
     if not (x.is_cuda and len(shape) == 3 and dtype in _TYPES):
         raise ValueError("activations are CUDA tensors [members, rows, width], float32 or bfloat16")
     m, rows, width = shape
     if m > _MOST or rows > _MOST or width > _MOST:
         raise ValueError("activations have at most 2^31 - 1 members, rows and columns")
-    member, row, column = x.stride()
-    if column != 1 and width != 1:
-        raise ValueError("x has to have contiguous columns")
-    other, other_member, other_row = (None, 0, 0) if residual is None else _activation(residual, (shape, dtype, device), "residual")
-    d = PbtDropoutDesc(m, rows, width, _TYPES[dtype], x.data_ptr(), member, row, other, other_member, other_row, None, dropout._for(m, device))
-    return _on(device, stream, () if stream is None else (x, residual, *dropout.tensors), _dropout, d, x)
+    _, member, row = _activation(x, kind, "x")
+    _, other_member, other_row = (None, 0, 0) if residual is None else _activation(residual, kind, "residual")
+    return bytes(PbtDropoutDesc(m, rows, width, _TYPES[dtype], None, member, row, None, other_member, other_row, None, dropout._for(m, device)))
 
 
 def _dropout(s, d, x):
