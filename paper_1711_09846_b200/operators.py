@@ -537,38 +537,50 @@ class GatedUnit:
         d.weight, d.weight_member, d.weight_row = weight.data_ptr(), weight.stride(0), weight.stride(1)
         self._status = torch.zeros(8, dtype=torch.int32, device=weight.device)
         self._floats = torch.empty(0, device=weight.device)         # (new_empty of a tensor costs less than torch.empty with a type and a device)
+        self._known, self._known_backward = (None, b""), (None, b"", 0)      # geometry of the last calls, and what the library is told of it
         self._home = _current_stream(weight.device.index)
         torch.cuda.current_stream(weight.device).synchronize()      # the calls may be on any stream
         d.status_device = self._status.data_ptr()
         _check(self.lib.pbt_gated_query_workspace(C.byref(d), 0, C.byref(C.c_size_t(0))))
 
-    def _call(self, x, dropout, kept):
-        """The description of a call on these rows (a copy: calls from several threads do not share it)."""
+    def _describe(self, x, dh=None, kept=None) -> bytes:
+        """What the library is told of a call on rows like these, their addresses apart."""
         shape, width = x.shape, self._width
         if not (len(shape) == 3 and shape[0] == self._members and shape[2] == width and x.dtype is self._dtype and x.device == self._device):
             raise ValueError("x is [members, rows, width] of the weight's members, width, type and device")
         rows = shape[1]
         if rows > _MOST:
             raise ValueError("a call has at most 2^31 - 1 rows")
-        member, row, column = x.stride()
-        if column != 1 and width != 1:
-            raise ValueError("x has to have contiguous columns")
         d = PbtGatedDesc.from_buffer_copy(self._desc)
-        d.rows, d.x, d.x_member, d.x_row = rows, x.data_ptr(), member, row if rows > 1 else max(row, width)      # (a single row may carry any stride)
+        d.rows = rows
+        d.x_member, d.x_row = _rows_of(x, "x")
+        if dh is not None:
+            if not (dh.shape == (self._members, rows, self.hidden) and dh.dtype is self._dtype and dh.device == self._device):
+                raise ValueError("dh is [members, rows, hidden] of the weight's type and device")
+            d.dh_member, d.dh_row = _rows_of(dh, "dh")
+        if kept is not None and not (kept.shape == (self._members, rows, 2, self._pitch) and kept.dtype is torch.float32 and kept.device == self._device
+                                     and kept.is_contiguous()):
+            raise ValueError("kept is what forward(keep=True) returned")
+        return bytes(d)
+
+    def _call(self, told, x, dropout):
+        """The description of a call (its own: calls from several threads share none)."""
+        d = PbtGatedDesc.from_buffer_copy(told)
+        d.x = x.data_ptr()
         if dropout is not None:
             d.drop = C.addressof(dropout._for(self._members, self._device))
-        if kept is not None:
-            if not (kept.shape == (self._members, rows, 2, self._pitch) and kept.dtype is torch.float32 and kept.device == self._device and kept.is_contiguous()):
-                raise ValueError("kept is what forward(keep=True) returned")
-            d.kept = kept.data_ptr()
-        return d, rows
+        return d
 
     def forward(self, x, dropout: Optional[Dropout] = None, keep: bool = False, stream=None):
         """h [members, rows, hidden]; with keep, also g and u in float32 for the backward pass (8 bytes a hidden unit; without
         them it works them out anew, which costs two thirds of a forward pass more)."""
-        d, rows = self._call(x, dropout, None)
+        kind = (x.shape, x.stride(), x.dtype, x.device)
+        known, told = self._known
+        if known != kind:                                # (checks and description cost a small call as much as its launch)
+            told = self._describe(x)
+            self._known = (kind, told)
         inputs = () if stream is None else (x, self.weight, *(dropout.tensors if dropout else ()))
-        return _on(self._device, stream, inputs, self._forward, d, rows, keep)
+        return _on(self._device, stream, inputs, self._forward, self._call(told, x, dropout), kind[0][1], keep)
 
     def _forward(self, s, d, rows, keep):
         h = self.weight.new_empty((self._members, rows, self.hidden))
@@ -578,29 +590,48 @@ class GatedUnit:
             kept = self._floats.new_empty((self._members, rows, 2, self._pitch))
             d.kept = kept.data_ptr()
         if rows:
-            # a forward pass needs a workspace for bfloat16 rows of odd sizes only: asking for its size costs a small call as much as its checks
-            rc = self.lib.pbt_gated_forward(d, None, 0, s)
-            if rc:
-                self._run(d, 0, self.lib.pbt_gated_forward, s, rc)
-            elif s != self._home:
-                self._keep_status()
+            # a forward pass needs a workspace for bfloat16 rows of odd sizes only
+            self._run(d, 0, self.lib.pbt_gated_forward, s, 0)
         return (h, kept) if keep else h
 
     def backward(self, dh, x, kept=None, dropout: Optional[Dropout] = None, stream=None):
         """(dx, dweight) from dh [members, rows, hidden], the forward pass's x, what it kept (or None) and its dropout.  dweight is
         [members, 2 hidden, width] of the weight's type, every member's own even where the weight is one for all."""
-        d, rows = self._call(x, dropout, kept)
-        if not (dh.shape == (self._members, rows, self.hidden) and dh.dtype is self._dtype and dh.device == self._device):
-            raise ValueError("dh is [members, rows, hidden] of the weight's type and device")
-        d.dh, d.dh_member, d.dh_row = _rows_of(dh, "dh")
+        kind = (x.shape, x.stride(), x.dtype, x.device, dh.shape, dh.stride(), dh.dtype, dh.device,
+                None if kept is None else (kept.shape, kept.stride(), kept.dtype, kept.device))
+        known, told, nbytes = self._known_backward
+        if known != kind:
+            told = self._describe(x, dh, kept)
+            nbytes = 0
+        d = self._call(told, x, dropout)
+        d.dh = dh.data_ptr()
+        if kept is not None:
+            d.kept = kept.data_ptr()
         inputs = () if stream is None else (dh, x, kept, self.weight, *(dropout.tensors if dropout else ()))
-        return _on(self._device, stream, inputs, self._backward, d, x)
+        result, need = _on(self._device, stream, inputs, self._backward, d, x, nbytes)
+        if known != kind or need != nbytes:
+            self._known_backward = (kind, told, need)
+        return result
 
-    def _backward(self, s, d, x):
+    def _backward(self, s, d, x, nbytes):
         dx, dweight = _like(x), _like(self.weight)
         d.dx, d.dweight = dx.data_ptr(), dweight.data_ptr()
-        self._run(d, 1, self.lib.pbt_gated_backward, s, _NO_WORKSPACE)
-        return dx, dweight
+        return (dx, dweight), self._run(d, 1, self.lib.pbt_gated_backward, s, nbytes)
+
+    def _run(self, d, backward, call, s, nbytes):
+        """The call with a workspace of `nbytes`, which the last one like it took, or of what the library asks for; returns the bytes."""
+        if s != self._home:      # keeps the status words until the call is done, should the object go first
+            self._status.record_stream(torch.cuda.current_stream(self._device))
+        rc = _with_workspace(call, d, nbytes, s) if nbytes else call(d, None, 0, s)
+        if rc == _NO_WORKSPACE:
+            need = C.c_size_t(0)
+            rc = self.lib.pbt_gated_query_workspace(d, backward, C.byref(need))
+            nbytes = need.value
+            if not rc:
+                rc = _with_workspace(call, d, nbytes, s)
+        if rc:
+            _check(rc)
+        return nbytes
 
     def check(self):
         """Waits for the enqueued calls and raises if one of the kernels' bounded waits ran out (PBT_ERR_TIMEOUT)."""
@@ -609,26 +640,10 @@ class GatedUnit:
         if code:
             raise PbtError(code, "a bounded wait inside a kernel ran out")
 
-    def _keep_status(self):
-        """Keeps the status words until the current stream's calls are done, should the object go first."""
-        self._status.record_stream(torch.cuda.current_stream(self._device))
-
-    def _run(self, d, backward, call, s, rc):
-        """The call with a workspace, after an answer `rc` to one without."""
-        if s != self._home:
-            self._keep_status()
-        if rc == _NO_WORKSPACE:
-            nbytes = C.c_size_t(0)
-            rc = self.lib.pbt_gated_query_workspace(d, backward, C.byref(nbytes))
-            if not rc:
-                rc = _with_workspace(call, d, nbytes.value, s)
-        if rc:
-            _check(rc)
-
 
 def _rows_of(t, name):
     member, row, column = t.stride()
     rows, columns = t.shape[1], t.shape[2]
     if column != 1 and columns != 1:
         raise ValueError(f"{name} has to have contiguous columns")
-    return t.data_ptr(), member, row if rows > 1 else max(row, columns)      # (a single row may carry any stride)
+    return member, row if rows > 1 else max(row, columns)      # (a single row may carry any stride)

@@ -356,8 +356,8 @@ def test_nothing_is_written_beside_the_results(shape, dtype):
         return t, t[guard:guard + n]
     sizes = dict(h=m * rows * hidden * size, kept=m * rows * 2 * ((hidden + 7) // 8 * 8) * 4, dx=m * rows * width * size, dweight=m * 2 * hidden * width * size)
     places = {k: between(n) for k, n in sizes.items()}
-    d, _ = layer._call(c["x"], c["dropout"], None)
-    d.dh, d.dh_member, d.dh_row = c["dh"].data_ptr(), c["dh"].stride(0), c["dh"].stride(1)
+    d = layer._call(layer._describe(c["x"], c["dh"]), c["x"], c["dropout"])
+    d.dh = c["dh"].data_ptr()
     for k, (_, t) in places.items():
         setattr(d, k, t.data_ptr())
     n = C.c_size_t(0)
