@@ -632,10 +632,13 @@ int pbt_dropout(const pbt_dropout_desc* desc, void* stream);
  * keep, rate: `drop` (its width is `hidden`), or NULL: nothing is dropped.  activation: 0 silu, 1 gelu (with the error function), 2 relu, 3 sigmoid.
  * Activations [members][rows][...]; x, dh and weight have any member stride (0: one weight for all members; dweight is each
  * member's own all the same) and any row stride of at least a row, in elements; columns are contiguous, results, too.  All of one type (0 float,
- * 1 bfloat16), products are summed in fp32.  g and u stay fp32: `kept` float [members][rows][2][hidden rounded up to 8] is written by the forward
- * pass unless NULL and read by the backward pass, which works them out anew where it is NULL.  For bfloat16, dg and du are rounded once, as operands of dx and dW.
- * members <= 65535; rows, width and 2 hidden < 2^22.  rows = 0: dweight is zero.  The calls only enqueue; results are reproducible bit for bit.
- * status_device: 32 zeroed bytes of device memory, as for pbt_grouped_gemm (bfloat16).
+ * 1 bfloat16), products are summed in fp32.  g and u stay fp32: `kept` float [members][rows][2][hidden rounded up to 8], 16-byte aligned, is written by the
+ * forward pass unless NULL and read by the backward pass, which works them out anew where it is NULL.  For bfloat16, dg and du are rounded once, as operands of
+ * dx and dW.  Elements have to be aligned to their size only; bfloat16 rows that are no multiples of 16 bytes are fetched in the aligned 16-byte pieces that hold them
+ * (up to 15 bytes on either side of an input are read, never used, and never beyond the piece), x and weight up to 2^34 elements of them.
+ * A dropped unit is zero, and so are its gradients, whatever g, u and dh are.  A row depends on its own row of x and its member's weight alone.
+ * members <= 65535; rows, width and 2 hidden < 2^22.  rows = 0: dweight is zero.  The calls only enqueue; results are reproducible bit for bit.  Should a bounded
+ * wait of a bfloat16 kernel run out, the fifth 32-bit word of status_device becomes PBT_ERR_TIMEOUT and the results are void.
  */
 typedef struct pbt_gated_desc {
   int32_t members, rows, width, hidden;
@@ -647,7 +650,7 @@ typedef struct pbt_gated_desc {
   float* kept;
   const void* dh; int64_t dh_member, dh_row;
   void* dx; void* dweight;
-  void* status_device;
+  void* status_device;          /* bfloat16: 32 zeroed bytes of device memory, as for pbt_grouped_gemm */
 } pbt_gated_desc;
 /* Bytes of device workspace (256-byte aligned base) of one forward (backward == 0) or backward call of this description, its pointers
  * (kept or not, alignment) and strides included; 0: workspace may be NULL. */

@@ -262,6 +262,13 @@ int check(const pbt_gated_desc* d) {
   if (d->dtype == 1 && !d->status_device) return fail(PBT_ERR_INVALID_ARG, "status_device is required by the tensor-core kernels");
   if (d->weight_row < d->width || d->weight_member < 0) return fail(PBT_ERR_INVALID_ARG, "weight_row is smaller than a row, or weight_member negative");
   if (d->rows && (!d->x || d->x_row < d->width || d->x_member < 0)) return fail(PBT_ERR_INVALID_ARG, "x is NULL, its row stride smaller than a row or its member stride negative");
+  if ((uintptr_t)d->kept & 15) return fail(PBT_ERR_INVALID_ARG, "kept has to begin on 16 bytes");
+  if (d->dtype) {
+    const Plan p = plan_of(d, false);
+    const unsigned long long per_row = (d->width + 7) / 8, most = 0x7FFFF000ull;      // (32 GB)
+    if ((p.pack_x && (unsigned long long)d->members * d->rows * per_row > most) || (p.pack_w && (unsigned long long)d->members * 2 * d->hidden * per_row > most))
+      return fail(PBT_ERR_UNSUPPORTED, "rows of x or weight that are not multiples of 16 bytes are laid out anew, 2^34 elements at most");
+  }
   return d->drop ? dropout::check_rule(d->drop, d->members, d->rows, d->hidden) : PBT_OK;
 }
 

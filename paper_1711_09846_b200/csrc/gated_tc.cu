@@ -776,7 +776,7 @@ cudaError_t tc_pack(const PackSource* src, int n, cudaStream_t s) {
     const PackSource& q = src[i];
     const int per_row = (q.cols + 7) / 8;
     const unsigned long long vectors = (unsigned long long)q.members * q.rows * per_row;
-    if (vectors > 0x7FFFF000ull) return cudaErrorInvalidConfiguration;      // (a 32 GB operand)
+    if (vectors > 0x7FFFF000ull) return cudaErrorInvalidConfiguration;      // (refused before)
     a.job[i] = {q.from.p, q.from.row, q.from.member, q.to, q.rows, q.cols, per_row, (uint32_t)vectors, divisor(per_row), divisor(q.rows), blocks};
     blocks += (unsigned)((vectors + 256 * kPackEach - 1) / (256 * kPackEach));
   }

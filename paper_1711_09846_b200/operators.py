@@ -440,6 +440,7 @@ class Dropout:
     def __init__(self, rate: Union[float, torch.Tensor], seed: int, step: Union[int, torch.Tensor], site: int = 0, first_member: int = 0):
         self.rate, self.seed, self.step, self.site, self.first_member = rate, seed, step, site, first_member
         self.tensors, rates, steps = (), None, None
+        seed, site, first_member = int(seed), int(site), int(first_member)
         if isinstance(rate, torch.Tensor):
             _require(rate.is_cuda and rate.dtype is torch.float32 and rate.dim() == 1 and rate.is_contiguous(),
                      "a dropout's rate is a number or a contiguous float32 tensor [members] on the device")
@@ -448,6 +449,7 @@ class Dropout:
             _require(step.is_cuda and step.dtype is torch.int64 and step.dim() == 1 and step.is_contiguous(),
                      "a dropout's step is a number or a contiguous int64 tensor [members] on the device")
             self.tensors, steps, step = (*self.tensors, step), step.data_ptr(), 0
+        rate, step = float(rate), int(step)
         _require(0 <= seed < 1 << 64 and 0 <= step < 1 << 63 and 0 <= site <= 1 << 30 and 0 <= first_member <= _MOST,
                  "a dropout's seed is a number of 64 bits; step, site (at most 2^30) and first_member are not negative")
         _require(0 <= rate <= 1, "a dropout's rate lies in [0, 1]")

@@ -398,7 +398,8 @@ def test_the_c_calls_refuse_what_they_cannot_do():
     common = [(1, dict(members=0)), (1, dict(rows=-1)), (1, dict(width=0)), (1, dict(hidden=0)), (2, dict(members=65536)), (2, dict(rows=1 << 22)),
               (2, dict(width=1 << 22)), (2, dict(hidden=1 << 21)), (2, dict(members=65535, rows=1 << 20, hidden=1 << 20, width=1 << 20, x_row=1 << 20, weight_row=1 << 20)),
               (2, dict(dtype=2)), (2, dict(activation=4)), (2, dict(activation=-1)), (1, dict(weight=None)), (1, dict(weight_row=7)), (1, dict(weight_member=-8)),
-              (1, dict(x=None)), (1, dict(x_row=7)), (1, dict(x_member=-1)), (1, dict(status_device=None)), (1, dict(drop=C.addressof(rule)))]
+              (1, dict(x=None)), (1, dict(x_row=7)), (1, dict(x_member=-1)), (1, dict(status_device=None)), (1, dict(drop=C.addressof(rule))), (1, dict(kept=4100)), (2, dict(rows=1 << 21, members=1 << 10, width=33, x_row=33, weight_row=40)),
+              (2, dict(rows=40, hidden=1 << 20, members=1 << 10, width=65, x_row=72, weight_row=65, x_member=72, weight_member=1))]
     for code, kw in common:
         for backward in (0, 1):
             assert lib.pbt_gated_query_workspace(C.byref(desc(**kw)), backward, C.byref(n)) == code, kw
