@@ -23,7 +23,7 @@ struct Args {
   const T* residual; long long residual_member, residual_row;
   T* y;
   uint32_t rows, width, groups;     // groups of a row
-  pbt_drop_rule rule;
+  Rule rule;
 };
 
 template <typename T>
@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(256) k_dropout(const Args<T> a) {
     if (i >= total || i < first) continue;
     Eight e = values(vx[u]);
     if (d.on) {
-      const U4 w = draw_group(d, i);
+      const U4 w = draw_group(a.rule, d, i);
 #pragma unroll
       for (int c = 0; c < kGroup; ++c) e.v[c] = drop(e.v[c], kept(w, c, d.limit), d.scale);
     }
@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(256) k_dropout_odd(const Args<T> a, const uint
     if (q.at >= total) continue;
     if (q.member != last) d = draw_of(a.rule, q.member);
     last = q.member;
-    bits[u] = kept_bits(d, q.row * a.groups + q.col / kGroup);
+    bits[u] = kept_bits(a.rule, d, q.row * a.groups + q.col / kGroup);
     scale[u] = d.on ? d.scale : 1.f;
   }
 #pragma unroll
@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(256) k_dropout_odd(const Args<T> a, const uint
     if (left > kGroup) {
       in |= next << (kGroup - shift);               // (without a shift nothing of it is looked at)
     } else {
-      if (shift && left > kGroup - shift) in |= kept_bits(draw_of(a.rule, q.member), q.row * a.groups + q.col / kGroup + 1) << (kGroup - shift);
+      if (shift && left > kGroup - shift) in |= kept_bits(a.rule, draw_of(a.rule, q.member), q.row * a.groups + q.col / kGroup + 1) << (kGroup - shift);
       if (left < kGroup) {
         in = (in & ((1u << left) - 1u)) | next << left;
         if (q.row + 1 == a.rows && at + left < total) {
@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(256) k_dropout_strided(const Args<T> a) {
   const T* r = RESIDUAL ? a.residual + m * a.residual_member + row * a.residual_row + c0 : nullptr;
   T* y = a.y + ((long long)m * a.rows + row) * a.width + c0;
   const Draw d = draw_of(a.rule, m);
-  const uint32_t bits = kept_bits(d, (uint32_t)i);
+  const uint32_t bits = kept_bits(a.rule, d, (uint32_t)i);
   const float scale = d.on ? d.scale : 1.f;
 #pragma unroll
   for (int c = 0; c < kGroup; ++c) {
@@ -203,7 +203,7 @@ template <typename T, bool RESIDUAL>
 cudaError_t launch(const pbt_dropout_desc* d, cudaStream_t s) {
   const uint32_t groups = (uint32_t)((d->width + kGroup - 1) / kGroup);
   const Args<T> a = {(const T*)d->x, d->x_member, d->x_row, (const T*)d->residual, d->residual_member, d->residual_row, (T*)d->y,
-                     (uint32_t)d->rows, (uint32_t)d->width, groups, d->rule};
+                     (uint32_t)d->rows, (uint32_t)d->width, groups, rule_of(d->rule)};
   const uint64_t per_member = (uint64_t)d->rows * groups;
   const long long cells = (long long)d->rows * d->width, step = 16 / sizeof(T);
   const bool many = d->members > 1;

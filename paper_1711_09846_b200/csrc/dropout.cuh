@@ -20,23 +20,36 @@ inline Divisor divisor(uint32_t d) {
   while (s < 31 && (1u << s) < d) ++s;                          // 2^(s - 1) < d <= 2^s
   return {(uint32_t)(((1ull << (31 + s)) + d - 1) / d), s};     // (d = 1: 2^31)
 }
+// A rule as the kernels take it, with the keys of the generator's rounds: operands from constant memory instead of two additions a round.
+struct Rule {
+  pbt_drop_rule rule;
+  uint32_t keys[20];
+};
+inline Rule rule_of(const pbt_drop_rule& r) {
+  Rule k = {r, {}};
+  for (int i = 0; i < 10; ++i) {
+    k.keys[2 * i] = (uint32_t)r.seed + 0x9E3779B9u * i;
+    k.keys[2 * i + 1] = (uint32_t)(r.seed >> 32) + 0xBB67AE85u * i;
+  }
+  return k;
+}
+
 #ifdef __CUDACC__
 __device__ __forceinline__ uint32_t quotient(uint32_t n, Divisor d) { return (uint32_t)(((uint64_t)n * d.factor) >> 31) >> d.shift; }
 
 // What a thread has to know to draw for one member.
 struct Draw {
   uint32_t member, step, stream;
-  uint64_t seed;
   uint32_t limit;     // a 16-bit draw d is kept where d << 16 > limit; only for `on`
   float scale;        // of what is kept
   bool on;            // false: a rate that rounds to 0, nothing is drawn
 };
-__device__ __forceinline__ Draw draw_of(const pbt_drop_rule& r, int m) {
+__device__ __forceinline__ Draw draw_of(const Rule& rule, int m) {
+  const pbt_drop_rule& r = rule.rule;
   Draw d;
   d.member = (uint32_t)(r.first_member + m);
   d.step = (uint32_t)(r.steps ? __ldg(reinterpret_cast<const long long*>(r.steps) + m) : (long long)r.step);
   d.stream = kStreamDropout + (uint32_t)r.site;
-  d.seed = r.seed;
   const float rate = r.rate ? __ldg(r.rate + m) : r.rate_all;
   const uint32_t t = (uint32_t)rintf(fminf(fmaxf(rate, 0.f), 1.f) * 65536.f);
   d.on = t != 0;
@@ -46,12 +59,23 @@ __device__ __forceinline__ Draw draw_of(const pbt_drop_rule& r, int m) {
 }
 // The draws of eight neighbouring columns, and whether column c of them is kept (an odd column has the upper half of its word; what the
 // lower half adds below it changes no comparison with limit, whose lower half is all ones).
-__device__ __forceinline__ U4 draw_group(const Draw& d, uint32_t block) { return philox4x32_10(d.member, d.step, d.stream, block, d.seed); }
+__device__ __forceinline__ U4 draw_group(const Rule& rule, const Draw& d, uint32_t block) {
+  uint32_t c0 = d.member, c1 = d.step, c2 = d.stream, c3 = block;      // philox4x32_10
+#pragma unroll
+  for (int i = 0; i < 10; ++i) {
+    const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;
+    c0 = (uint32_t)(p1 >> 32) ^ c1 ^ rule.keys[2 * i];
+    c1 = (uint32_t)p1;
+    c2 = (uint32_t)(p0 >> 32) ^ c3 ^ rule.keys[2 * i + 1];
+    c3 = (uint32_t)p0;
+  }
+  return {{c0, c1, c2, c3}};
+}
 __device__ __forceinline__ bool kept(const U4& w, int c, uint32_t limit) { return ((c & 1) ? w.x[c >> 1] : w.x[c >> 1] << 16) > limit; }
 // bit c: column c is kept
-__device__ __forceinline__ uint32_t kept_bits(const Draw& d, uint32_t block) {
+__device__ __forceinline__ uint32_t kept_bits(const Rule& rule, const Draw& d, uint32_t block) {
   if (!d.on) return 0xFFu;
-  const U4 w = draw_group(d, block);
+  const U4 w = draw_group(rule, d, block);
   uint32_t bits = 0;
 #pragma unroll
   for (int c = 0; c < kGroup; ++c) bits |= kept(w, c, d.limit) ? 1u << c : 0u;

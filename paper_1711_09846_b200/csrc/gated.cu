@@ -36,7 +36,7 @@ struct CellArgs {
   T* out; long long out_pitch;                    // [dg du] [members][rows][out_pitch]
   uint32_t rows, hidden, groups;
   int activation, drop;
-  pbt_drop_rule rule;
+  dropout::Rule rule;
 };
 
 __device__ __forceinline__ void store_pairs(float* p, const Eight& e) {
@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(256) k_gated_cells(const CellArgs<T> a) {
   float f = 1.f;
   if (a.drop) {
     const dropout::Draw d = dropout::draw_of(a.rule, m);
-    in = dropout::kept_bits(d, (uint32_t)i);
+    in = dropout::kept_bits(a.rule, d, (uint32_t)i);
     if (d.on) f = d.scale;
   }
   Eight dg, du;
@@ -165,7 +165,7 @@ CellArgs<T> cells_of(const pbt_gated_desc* d, const Plan& p, const float* z) {
   a.z = z; a.pitch = p.pitch;
   a.rows = (uint32_t)d->rows; a.hidden = (uint32_t)d->hidden; a.groups = (uint32_t)(p.pitch / kGroup);
   a.activation = d->activation; a.drop = d->drop != nullptr;
-  if (d->drop) a.rule = *d->drop;
+  if (d->drop) a.rule = dropout::rule_of(*d->drop);
   return a;
 }
 template <typename T>

@@ -57,7 +57,7 @@ struct ProductParams {
   // forward
   float* z; int pitch;
   int activation, drop;
-  pbt_drop_rule rule;
+  dropout::Rule rule;
 };
 
 // a box of kK rows and COLS floats into staged rows of PITCH, `rows` x `cols` of which exist (the others are zero)
@@ -224,7 +224,7 @@ __device__ __forceinline__ void product_tile(const ProductParams& p, float* f32_
       for (int e = 0; e < 8; ++e) g.v[e] = activation(p.activation, g.v[e]) * u.v[e];
       if (p.drop) {
         const dropout::Draw d = dropout::draw_of(p.rule, m);
-        const uint32_t in = dropout::kept_bits(d, (uint32_t)(m0 + r) * (uint32_t)((p.N + 7) / 8) + (uint32_t)(col / 8));
+        const uint32_t in = dropout::kept_bits(p.rule, d, (uint32_t)(m0 + r) * (uint32_t)((p.N + 7) / 8) + (uint32_t)(col / 8));
         const float f = d.on ? d.scale : 1.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) g.v[e] = (in >> e & 1u) ? f * g.v[e] : 0.f;
@@ -349,7 +349,7 @@ cudaError_t f32_forward(const pbt_gated_desc* d, float* h, float* z, int pitch, 
   p.M = d->rows; p.N = d->hidden; p.K = d->width;
   p.z = z; p.pitch = pitch;
   p.activation = d->activation; p.drop = d->drop != nullptr;
-  if (d->drop) p.rule = *d->drop;
+  if (d->drop) p.rule = dropout::rule_of(*d->drop);
   fill(d, &p, true);
   if (p.M <= Few::BM) return launch_forward<Few>(d, p, s);
   if (p.M <= Half::BM) return launch_forward<Half>(d, p, s);

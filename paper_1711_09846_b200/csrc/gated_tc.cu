@@ -36,7 +36,7 @@ struct TileParams {
   int activation, drop, h_tma;
   bf16* h;                                     // or null: only g and u
   int want_z;
-  pbt_drop_rule rule;
+  dropout::Rule rule;
   Counters* counters;
 };
 struct TileMaps {
@@ -132,7 +132,7 @@ __device__ __forceinline__ void drain(const TileParams& p, const TileMaps& maps,
     if (d.on) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const U4 w = dropout::draw_group(d, (uint32_t)row * groups + (uint32_t)(col / dropout::kGroup + j));
+        const U4 w = dropout::draw_group(p.rule, d, (uint32_t)row * groups + (uint32_t)(col / dropout::kGroup + j));
 #pragma unroll
         for (int c = 0; c < 8; ++c) u[8 * j + c] = dropout::kept(w, c, d.limit) ? __float_as_uint(__uint_as_float(u[8 * j + c]) * d.scale) : 0u;
       }
@@ -352,7 +352,7 @@ struct RowsParams {
   int activation, drop, vec;
   bf16* out;                      // h (or null), dx
   float* z; int pitch;            // or null
-  pbt_drop_rule rule;
+  dropout::Rule rule;
   Counters* counters;
 };
 // DEEP: for two CTAs an SM at most, with more of the weight under way; else more CTAs share it, one's set-up and end beside another's loads
@@ -505,7 +505,7 @@ __device__ __forceinline__ void rows_product(const CUtensorMap& tmA, const CUten
       for (int e = 0; e < 8; ++e) g.v[e] = activation_bf16(p.activation, g.v[e]) * u.v[e];
       if (p.drop) {
         const dropout::Draw d = dropout::draw_of(p.rule, m);
-        const uint32_t in = dropout::kept_bits(d, (uint32_t)t * (uint32_t)((p.hidden + 7) / 8) + (uint32_t)(col / 8));
+        const uint32_t in = dropout::kept_bits(p.rule, d, (uint32_t)t * (uint32_t)((p.hidden + 7) / 8) + (uint32_t)(col / 8));
         const float f = d.on ? d.scale : 1.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) g.v[e] = (in >> e & 1u) ? g.v[e] * f : 0.f;
@@ -789,7 +789,7 @@ static cudaError_t rows_forward(const pbt_gated_desc* d, const Operand& x, const
   p.a_batched = d->members > 1 && w.member != 0;
   p.activation = d->activation;
   p.drop = d->drop != nullptr;
-  if (d->drop) p.rule = *d->drop;
+  if (d->drop) p.rule = dropout::rule_of(*d->drop);
   p.out = (bf16*)h; p.z = z; p.pitch = pitch;
   CUtensorMap tmA, tmB;
   if (!make_map(&tmA, w.p, d->width, 2ll * d->hidden, w.row, p.a_batched ? d->members : 1, w.member, 64) || !rows_params(d, false, x, d->width, &p, &tmB))
@@ -830,7 +830,7 @@ cudaError_t tc_forward(const pbt_gated_desc* d, const Operand& x, const Operand&
   p.h = (bf16*)h;
   p.want_z = z != nullptr;
   p.drop = d->drop != nullptr;
-  if (d->drop) p.rule = *d->drop;
+  if (d->drop) p.rule = dropout::rule_of(*d->drop);
   p.counters = (Counters*)d->status_device;
 
   static DeviceSetup setup_pair, setup_wide, setup_narrow;
