@@ -40,8 +40,8 @@ __device__ __forceinline__ Raw<T> load8(const T* p) {
 __device__ __forceinline__ Eight values(const Raw<bf16>& r) { return unpack(r.a); }
 __device__ __forceinline__ Eight values(const Raw<float>& r) { return unpack(r.a, r.b); }
 
-// element by element: the kept ones scaled, the others zero
-__device__ __forceinline__ float drop(float x, bool in, float scale) { return in ? x * scale : 0.f; }
+// the residual (or 0) and the element scaled, if it is kept; one rounding
+__device__ __forceinline__ float drop(float x, bool in, float scale, float residual) { return fmaf(in ? x : 0.f, scale, residual); }
 
 // Whole groups in 16-byte vectors, U of them a thread, 256 apart, so that all their loads are under way before the first draw.
 // FLAT: rows follow one another without gaps, and a group's number in the member is its place, too.
@@ -72,14 +72,13 @@ __global__ void __launch_bounds__(256) k_dropout(const Args<T> a) {
   for (int u = 0; u < U; ++u) {
     const uint32_t i = first + u * 256;
     if (i >= total || i < first) continue;
-    Eight e = values(vx[u]);
+    Eight e = values(vx[u]), q = {};
+    if (RESIDUAL) q = values(vr[u]);
     if (d.on) {
       const U4 w = draw_group(a.rule, d, i);
 #pragma unroll
-      for (int c = 0; c < kGroup; ++c) e.v[c] = drop(e.v[c], kept(w, c, d.limit), d.scale);
-    }
-    if (RESIDUAL) {
-      const Eight q = values(vr[u]);
+      for (int c = 0; c < kGroup; ++c) e.v[c] = drop(e.v[c], kept(w, c, d.limit), d.scale, q.v[c]);
+    } else if (RESIDUAL) {
 #pragma unroll
       for (int c = 0; c < kGroup; ++c) e.v[c] += q.v[c];
     }
@@ -152,25 +151,19 @@ __global__ void __launch_bounds__(256) k_dropout_odd(const Args<T> a, const uint
       }
     }
     if (at + kGroup <= total) {
-      Eight e = values(vx[u]);
+      Eight e = values(vx[u]), r = {};
+      if (RESIDUAL) r = values(vr[u]);
       if (next_scale == scale[u]) {
 #pragma unroll
-        for (int c = 0; c < kGroup; ++c) e.v[c] = drop(e.v[c], in >> c & 1u, scale[u]);
+        for (int c = 0; c < kGroup; ++c) e.v[c] = drop(e.v[c], in >> c & 1u, scale[u], r.v[c]);
       } else {
 #pragma unroll
-        for (int c = 0; c < kGroup; ++c) e.v[c] = drop(e.v[c], in >> c & 1u, c < left ? scale[u] : next_scale);
-      }
-      if (RESIDUAL) {
-        const Eight r = values(vr[u]);
-#pragma unroll
-        for (int c = 0; c < kGroup; ++c) e.v[c] += r.v[c];
+        for (int c = 0; c < kGroup; ++c) e.v[c] = drop(e.v[c], in >> c & 1u, c < left ? scale[u] : next_scale, r.v[c]);
       }
       store8(a.y + at, e);
     } else {
       for (uint32_t c = 0; at + c < total; ++c) {
-        float v = drop(as_float(a.x[at + c]), in >> c & 1u, c < left ? scale[u] : next_scale);
-        if (RESIDUAL) v += as_float(a.residual[at + c]);
-        store(a.y + at + c, v);
+        store(a.y + at + c, drop(as_float(a.x[at + c]), in >> c & 1u, c < left ? scale[u] : next_scale, RESIDUAL ? as_float(a.residual[at + c]) : 0.f));
       }
     }
   }
@@ -193,9 +186,7 @@ __global__ void __launch_bounds__(256) k_dropout_strided(const Args<T> a) {
 #pragma unroll
   for (int c = 0; c < kGroup; ++c) {
     if (c >= n) break;
-    float v = drop(as_float(x[c]), bits >> c & 1u, scale);
-    if (RESIDUAL) v += as_float(r[c]);
-    store(y + c, v);
+    store(y + c, drop(as_float(x[c]), bits >> c & 1u, scale, RESIDUAL ? as_float(r[c]) : 0.f));
   }
 }
 
