@@ -1,7 +1,8 @@
 // Dropout of activations, with masks that are drawn where they are needed: y = residual + keep x / (1 - rate).
 //
 // One pass over x (and residual): 4 or 6 bytes an element in bf16, 8 or 12 in fp32.  A group of eight neighbouring columns shares one
-// block of the generator (20 32-bit multiplications with a 64-bit product), so that the draws cost less than the transfers.
+// block of the generator (20 32-bit multiplications with a 64-bit product), so that the draws cost less than the transfers.  80 x 512 x 2048 bf16: 78 us with a residual
+// (6.5 TB/s, the measured copy rate), 58 without (5.8 TB/s); 24 x 1024 x 512 fp32 with a residual 25 (6.1).
 #include <type_traits>
 
 #include "dropout.cuh"
@@ -90,7 +91,8 @@ __global__ void __launch_bounds__(256) k_dropout(const Args<T> a) {
 // apart, which belong to two or three groups and one or two rows (the second one perhaps of the next member).  Every lane draws the group that its vector begins
 // in; the next vector, the next lane's, begins in the group that follows it, or in the first one of the next row, so that its bits come from there, the last
 // lane's from one more draw of the warp.  Only a row's last vector, where it begins inside
-// the last group but one, takes a draw of its own.  Bound by issue (80 x 512 x 2047 bf16 68 % of the cycles; 2048 columns take 62 us, these 114).
+// the last group but one, takes a draw of its own.  Bound by issue (80 x 512 x 2047 bf16 98 us; 2048
+// columns take 58).
 template <typename T, bool RESIDUAL, int U>
 __global__ void __launch_bounds__(256) k_dropout_odd(const Args<T> a, const uint32_t total, const Divisor by_width, const Divisor by_rows) {
   pdl_prologue();
@@ -207,14 +209,14 @@ cudaError_t launch(const pbt_dropout_desc* d, cudaStream_t s) {
   auto grid = [&](int per_block) { return dim3((unsigned)((per_member + per_block - 1) / per_block), (unsigned)d->members); };
   if (vectors) {
     const bool flat = d->rows == 1 || (d->x_row == d->width && (!RESIDUAL || d->residual_row == d->width));
-    // Groups of a thread: bf16 takes two or three, which share the generator's first rounds (they go by the member and the step alone) and keep more
-    // bytes under way; fp32, twice the bytes a group, one.  80 x 512 x 2048 bf16 with residual (without): one 90.7 us (77.8), two 87.4 (66.2), three 79.3
-    // (61.9), four 79.2 (63.7), and a plain copy of 4 bytes an element 52.5; 16 x 256 x 1024: 5.9, 5.5, 5.9; 80 x 512 x 2048 fp32 146.1 (98.6), 146.0 (101.4).
+    // Groups of a thread: bf16 takes two or four, which share the generator's first rounds (they go by the member and the step alone) and keep more
+    // bytes under way; fp32, twice the bytes a group, one.  80 x 512 x 2048 bf16 with residual (without): one 92.1 us (70.8), two 83.1 (65.0), three 81.3
+    // (62.4), four 77.7 (58.1), and a plain copy of 4 bytes an element 52.4; 16 x 256 x 1024: 5.4, 5.1, 5.5, 5.5; 80 x 512 x 2048 fp32 146.3 (100.1) to 146.6 (101.0).
     const uint64_t all = per_member * d->members, fill = 148ull * 2048;       // the GPU's threads
-    const int each = sizeof(T) == 4 || all < fill ? 1 : all < 4 * fill ? 2 : 3;
+    const int each = sizeof(T) == 4 || all < fill ? 1 : all < 4 * fill ? 2 : 4;
     auto go = [&](auto is_flat) {
       constexpr bool F = decltype(is_flat)::value;
-      if (each == 3) return launch_with(grid(768), 256, 0, s)(k_dropout<T, RESIDUAL, F, 3>, a);
+      if (each == 4) return launch_with(grid(1024), 256, 0, s)(k_dropout<T, RESIDUAL, F, 4>, a);
       if (each == 2) return launch_with(grid(512), 256, 0, s)(k_dropout<T, RESIDUAL, F, 2>, a);
       return launch_with(grid(256), 256, 0, s)(k_dropout<T, RESIDUAL, F, 1>, a);
     };
@@ -224,8 +226,8 @@ cudaError_t launch(const pbt_dropout_desc* d, cudaStream_t s) {
   const uintptr_t bases = (uintptr_t)d->x | (uintptr_t)d->y | (RESIDUAL ? (uintptr_t)d->residual : 0);
   if (d->width >= kGroup && (bases & 15) == 0 && total < 0x7FFF0000ll && gapless(d->x_member, d->x_row) &&
       (!RESIDUAL || gapless(d->residual_member, d->residual_row))) {
-    // Vectors of a thread, once the GPU has its fill of threads with them: 80 x 512 x 2047 bf16 with residual (without) two 133 us (126), three 127 (114), four
-    // 142 (113); fp32 162 (129), 179 (127), 167 (147).
+    // Vectors of a thread, once the GPU has its fill of threads with them: 80 x 512 x 2047 bf16 with residual (without) one 141 us (138), two 114 (109), three
+    // 104 (98), four 105 (95); fp32 151 (135), 147 (112), 150 (105), 165 (111).
     constexpr int U = sizeof(T) == 4 && RESIDUAL ? 2 : 3;
     const Divisor by_width = divisor((uint32_t)d->width), by_rows = divisor((uint32_t)d->rows);
     auto blocks = [&](int each) { return (unsigned)((total + 256 * kGroup * each - 1) / (256 * kGroup * each)); };
