@@ -90,9 +90,8 @@ __global__ void __launch_bounds__(256) k_dropout(const Args<T> a) {
 // Any width from 8 on, all activations without gaps (less than 2^31 elements of them): a thread has U vectors of eight elements from a 16-byte boundary, 32
 // apart, which belong to two or three groups and one or two rows (the second one perhaps of the next member).  Every lane draws the group that its vector begins
 // in; the next vector, the next lane's, begins in the group that follows it, or in the first one of the next row, so that its bits come from there, the last
-// lane's from one more draw of the warp.  Only a row's last vector, where it begins inside
-// the last group but one, takes a draw of its own.  Bound by issue (80 x 512 x 2047 bf16 98 us; 2048
-// columns take 58).
+// lane's from one more draw of the warp.  Only a row's last vector, where it begins inside the last group but one, takes a draw of its own.
+// Bound by issue (80 x 512 x 2047 bf16 with a residual 104 us, without 98; 2048 columns take 78 and 58).
 template <typename T, bool RESIDUAL, int U>
 __global__ void __launch_bounds__(256) k_dropout_odd(const Args<T> a, const uint32_t total, const Divisor by_width, const Divisor by_rows) {
   pdl_prologue();
