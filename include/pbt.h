@@ -631,7 +631,8 @@ int pbt_dropout(const pbt_dropout_desc* desc, void* stream);
  *   dg = keep / (1 - rate) dh u act'(g),  du = keep / (1 - rate) dh act(g),  dx = [dg du] W,  dW = [dg du]^T x
  * keep, rate: `drop` (its width is `hidden`), or NULL: nothing is dropped.  activation: 0 silu, 1 gelu (with the error function), 2 relu, 3 sigmoid.
  * Activations [members][rows][...]; x, dh and weight have any member stride (0: one weight for all members; dweight is each
- * member's own all the same) and any row stride of at least a row, in elements; columns are contiguous, results, too.  All of one type (0 float,
+ * member's own all the same) and any row stride of at least a row, in elements; columns are contiguous, results, too,
+ * which overlap nothing else.  All of one type (0 float,
  * 1 bfloat16), products are summed in fp32.  g and u stay fp32: `kept` float [members][rows][2][hidden rounded up to 8], 16-byte aligned, is written by the
  * forward pass unless NULL and read by the backward pass, which works them out anew where it is NULL.  For bfloat16, dg and du are rounded once, as operands of
  * dx and dW.  Elements have to be aligned to their size only; bfloat16 rows that are no multiples of 16 bytes are fetched in the aligned 16-byte pieces that hold them

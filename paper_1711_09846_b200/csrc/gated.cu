@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(256) k_gated_cells(const CellArgs<T> a) {
   for (int c = 0; c < kGroup; ++c) {
     const bool keep = in >> c & 1u;
     float slope;
-    const float act = activation(a.activation, g.v[c], &slope), v = f * dh.v[c];
+    const float act = activation<T>(a.activation, g.v[c], &slope), v = f * dh.v[c];
     dg.v[c] = keep ? v * u.v[c] * slope : 0.f;
     du.v[c] = keep ? v * act : 0.f;
   }

@@ -221,7 +221,7 @@ __device__ __forceinline__ void product_tile(const ProductParams& p, float* f32_
       }
       if (!p.c) continue;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) g.v[e] = activation(p.activation, g.v[e]) * u.v[e];
+      for (int e = 0; e < 8; ++e) g.v[e] = activation<float>(p.activation, g.v[e]) * u.v[e];
       if (p.drop) {
         const dropout::Draw d = dropout::draw_of(p.rule, m);
         const uint32_t in = dropout::kept_bits(p.rule, d, (uint32_t)(m0 + r) * (uint32_t)((p.N + 7) / 8) + (uint32_t)(col / 8));
