@@ -35,7 +35,7 @@ struct CellArgs {
   const T* dh; long long dh_member, dh_row;
   T* out; long long out_pitch;                    // [dg du] [members][rows][out_pitch]
   uint32_t rows, hidden, groups;
-  int activation, drop;
+  int activation, drop, beside;
   dropout::Rule rule;
 };
 
@@ -56,11 +56,24 @@ __device__ __forceinline__ void store_pairs(bf16* p, const Eight& e) {
     store(p + kGroup - 1, e.v[kGroup - 1]);
   }
 }
+// Beside the kernel that packs operands, which it needs nothing of: the products, which do, may begin when both are done.
+struct Turn {
+  bool beside;
+  __device__ __forceinline__ Turn(bool b) : beside(b) {
+    if (beside) return;
+    pdl_prologue();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the products may begin with their other operands
+  }
+  __device__ __forceinline__ ~Turn() {
+    if (!beside) return;
+    pdl_prologue();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  }
+};
 // VEC: 16-byte loads and stores everywhere.  Bound by its bytes, 14 a hidden unit in bf16 (80 x 512 x 2048: 189 us, 6.2 TB/s).
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) k_gated_cells(const CellArgs<T> a) {
-  pdl_prologue();
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the products may begin with their other operands
+  const Turn turn(a.beside);
   const int m = blockIdx.y;
   const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= (uint64_t)a.rows * a.groups) return;
@@ -175,7 +188,8 @@ cudaError_t launch_cells(const pbt_gated_desc* d, const CellArgs<T>& a, cudaStre
   constexpr int kStep = 16 / sizeof(T);
   const bool vec = d->hidden % kGroup == 0 && ((uintptr_t)a.out & 15) == 0 && a.out_pitch % kStep == 0 &&
                    ((uintptr_t)a.dh & 15) == 0 && (d->rows == 1 || a.dh_row % kStep == 0) && (d->members == 1 || a.dh_member % kStep == 0);
-  return vec ? launch_with(grid, 256, 0, s)(k_gated_cells<T, true>, a) : launch_with(grid, 256, 0, s)(k_gated_cells<T, false>, a);
+  const int order = a.beside ? kBeside : 0;
+  return vec ? launch_ordered(order, grid, 256, 0, s, k_gated_cells<T, true>, a) : launch_ordered(order, grid, 256, 0, s, k_gated_cells<T, false>, a);
 }
 
 GemmArgs product(const pbt_gated_desc* d) {
@@ -191,7 +205,7 @@ cudaError_t forward(const pbt_gated_desc* d, char* ws, cudaStream_t s) {
   if (d->dtype) {
     Operands o;
     const cudaError_t e = operands_of(d, p, ws, &o, s);
-    return e == cudaSuccess ? tc_forward(d, o.x, o.w, d->h, d->kept, p.pitch, s) : e;
+    return e == cudaSuccess ? tc_forward(d, o.x, o.w, d->h, d->kept, p.pitch, p.pack_x || p.pack_w, s) : e;
   }
   return f32_forward(d, (float*)d->h, d->kept, p.pitch, s);
 }
@@ -218,7 +232,7 @@ cudaError_t backward(const pbt_gated_desc* d, char* ws, cudaStream_t s) {
   if (d->dtype) e = operands_of(d, p, ws, &o, s);
   if (e == cudaSuccess && !z) {
     float* made = (float*)(ws + p.z);
-    e = d->dtype ? tc_forward(d, o.x, o.w, nullptr, made, p.pitch, s) : f32_forward(d, nullptr, made, p.pitch, s);
+    e = d->dtype ? tc_forward(d, o.x, o.w, nullptr, made, p.pitch, p.pack_x || p.pack_w, s) : f32_forward(d, nullptr, made, p.pitch, s);
     z = made;
   }
   if (e != cudaSuccess) return e;
@@ -226,6 +240,7 @@ cudaError_t backward(const pbt_gated_desc* d, char* ws, cudaStream_t s) {
   CellArgs<T> a = cells_of<T>(d, p, z);
   a.dh = (const T*)d->dh; a.dh_member = d->dh_member; a.dh_row = d->dh_row;
   a.out = dz; a.out_pitch = p.dz_pitch;
+  a.beside = d->kept && (p.pack_x || p.pack_w);
   e = launch_cells<T>(d, a, s);
   if (e != cudaSuccess) return e;
   if (!d->dtype) return f32_backward(d, (const float*)dz, p.dz_pitch, s);
@@ -237,9 +252,11 @@ cudaError_t backward(const pbt_gated_desc* d, char* ws, cudaStream_t s) {
   g.b_mn = 1;
   g.B = o.w.p; g.ldb = o.w.row; g.strideB = o.w.member;
   g.C = d->dx; g.ldc = d->width; g.strideC = (long long)d->rows * d->width;
+  g.order = kAfter | kLeads;
   if (tc_dx_few(d)) e = tc_dx(d, left, o.w, s);
   else e = run_product(d, g, s);
   if (e != cudaSuccess) return e;
+  g.order = kBeside;      // dW takes the SMs that dx leaves in its last wave
   g.a_mn = 1;
   g.M = 2 * d->hidden; g.K = d->rows;
   g.B = o.x.p; g.ldb = o.x.row; g.strideB = o.x.member;

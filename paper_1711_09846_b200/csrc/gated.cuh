@@ -20,7 +20,7 @@ struct PackSource {
   int members, rows, cols;
 };
 cudaError_t tc_pack(const PackSource* src, int n, cudaStream_t s);      // one or two
-cudaError_t tc_forward(const pbt_gated_desc* d, const Operand& x, const Operand& w, void* h, float* z, int pitch, cudaStream_t s);
+cudaError_t tc_forward(const pbt_gated_desc* d, const Operand& x, const Operand& w, void* h, float* z, int pitch, bool packed, cudaStream_t s);      // packed: tc_pack is its predecessor
 // dx = [dg du] W by CTAs that share a contraction, for few rows; launched right behind the kernel that makes dg and du
 bool tc_dx_few(const pbt_gated_desc* d);
 cudaError_t tc_dx(const pbt_gated_desc* d, const Operand& dz, const Operand& w, cudaStream_t s);

@@ -539,24 +539,24 @@ int rows_splits(long long tiles, int k_blocks, long long places) {
 }
 template <int N, bool DX, bool DEEP>
 cudaError_t launch_rows(const pbt_gated_desc* d, const RowsParams& p, const CUtensorMap& tmA, const CUtensorMap& tmB, unsigned units, unsigned blocks, int splits,
-                        cudaStream_t s) {
+                        bool after, cudaStream_t s) {
   typedef RowsTile<N, DEEP> L;
   static DeviceSetup setup;
   int sms = 0;
   const cudaError_t e = device_setup(&setup, k_gated_rows<N, DX, DEEP>, L::kTotal, &sms);
   if (e != cudaSuccess) return e;
-  return launch_clusters(dim3(units * splits, blocks), kRowsThreads, L::kTotal, splits, DX, s, k_gated_rows<N, DX, DEEP>, tmA, tmB, p);
+  return launch_clusters(dim3(units * splits, blocks), kRowsThreads, L::kTotal, splits, after, s, k_gated_rows<N, DX, DEEP>, tmA, tmB, p);
 }
 // (32 rows, 2048 -> 4096, 256 CTAs: 10.8 us deep, 12.0 else; 40 members x 20 rows, 512 -> 1024, 640: 26 and 22)
 template <int N, bool DX>
-cudaError_t launch_rows(const pbt_gated_desc* d, const RowsParams& p, const CUtensorMap& tmA, const CUtensorMap& tmB, cudaStream_t s) {
+cudaError_t launch_rows(const pbt_gated_desc* d, const RowsParams& p, const CUtensorMap& tmA, const CUtensorMap& tmB, bool after, cudaStream_t s) {
   const unsigned units = DX ? (d->width + 127) / 128 : (d->hidden + 63) / 64, blocks = (unsigned)p.blocks * d->members;
   const long long tiles = (long long)units * blocks;
   if constexpr (N <= 32) {
     const int splits = rows_splits(tiles, p.k_blocks, 2 * kSms);
-    if (tiles * splits <= 2 * kSms) return launch_rows<N, DX, true>(d, p, tmA, tmB, units, blocks, splits, s);
+    if (tiles * splits <= 2 * kSms) return launch_rows<N, DX, true>(d, p, tmA, tmB, units, blocks, splits, after, s);
   }
-  return launch_rows<N, DX, false>(d, p, tmA, tmB, units, blocks, rows_splits(tiles, p.k_blocks, kSms * RowsTile<N, false>::kPerSm), s);
+  return launch_rows<N, DX, false>(d, p, tmA, tmB, units, blocks, rows_splits(tiles, p.k_blocks, kSms * RowsTile<N, false>::kPerSm), after, s);
 }
 int rows_columns(const pbt_gated_desc* d) { return d->rows <= 16 ? 16 : d->rows <= 32 ? 32 : d->rows <= 64 ? 64 : 128; }
 // what the two products of this form have in common; k: their contraction
@@ -716,7 +716,7 @@ cudaError_t launch_few(const pbt_gated_desc* d, FewParams& p, const CUtensorMap&
   // Together while there is a place for every CTA (one token, 1024 -> 2048: a backward pass 8.7 us, one after the other 11.9); beyond that tiles of dW that
   // take the place of CTAs of dx hold them up (16 members x 5 rows, 1024 -> 1024: 55 and 35).
   if (dx + dw > (long long)sms * (N == 16 ? 4 : 3)) {
-    const cudaError_t first = launch_rows<N, true>(d, p.dx, tmA, tmB, s);
+    const cudaError_t first = launch_rows<N, true>(d, p.dx, tmA, tmB, true, s);
     return first != cudaSuccess ? first : launch_after(dim3((unsigned)p.dw_columns, (unsigned)p.dw_rows, (unsigned)d->members), 256, 0, s, k_gated_outer<N / 16>, p.dw);
   }
   p.dx_blocks = (int)dx;
@@ -742,7 +742,7 @@ struct PackJobs {
 };
 // Bound by issue as much as by the transfers.
 __global__ void __launch_bounds__(256) k_gated_pack(const PackJobs a) {
-  pdl_prologue();
+  order_begin(kLeads);
   const bool second = a.n > 1 && blockIdx.x >= a.job[1].block0;
   const PackJob j = second ? a.job[1] : a.job[0];
   const uint32_t first = (blockIdx.x - j.block0) * (256 * kPackEach) + threadIdx.x;
@@ -784,7 +784,7 @@ cudaError_t tc_pack(const PackSource* src, int n, cudaStream_t s) {
   return launch_with(blocks, 256, 0, s)(k_gated_pack, a);
 }
 
-static cudaError_t rows_forward(const pbt_gated_desc* d, const Operand& x, const Operand& w, void* h, float* z, int pitch, cudaStream_t s) {
+static cudaError_t rows_forward(const pbt_gated_desc* d, const Operand& x, const Operand& w, void* h, float* z, int pitch, bool packed, cudaStream_t s) {
   RowsParams p = {};
   p.a_batched = d->members > 1 && w.member != 0;
   p.activation = d->activation;
@@ -794,7 +794,7 @@ static cudaError_t rows_forward(const pbt_gated_desc* d, const Operand& x, const
   CUtensorMap tmA, tmB;
   if (!make_map(&tmA, w.p, d->width, 2ll * d->hidden, w.row, p.a_batched ? d->members : 1, w.member, 64) || !rows_params(d, false, x, d->width, &p, &tmB))
     return cudaErrorInvalidValue;
-  return rows_columns(d) == 16 ? launch_rows<16, false>(d, p, tmA, tmB, s) : launch_rows<32, false>(d, p, tmA, tmB, s);
+  return rows_columns(d) == 16 ? launch_rows<16, false>(d, p, tmA, tmB, packed, s) : launch_rows<32, false>(d, p, tmA, tmB, packed, s);
 }
 
 // dx beyond the rows of tc_gradients: where larger tiles would leave a third of the SMs without one (one member's 500 rows, 2048 -> 2048: a whole backward pass
@@ -806,7 +806,7 @@ cudaError_t tc_dx(const pbt_gated_desc* d, const Operand& dz, const Operand& w, 
   RowsParams p = {};
   CUtensorMap tmA, tmB;
   if (!dx_params(d, dz, w, &p, &tmA, &tmB)) return cudaErrorInvalidValue;
-  return rows_columns(d) == 64 ? launch_rows<64, true>(d, p, tmA, tmB, s) : launch_rows<128, true>(d, p, tmA, tmB, s);
+  return rows_columns(d) == 64 ? launch_rows<64, true>(d, p, tmA, tmB, true, s) : launch_rows<128, true>(d, p, tmA, tmB, true, s);
 }
 
 bool tc_gradients_few(const pbt_gated_desc* d) { return d->rows <= kOuterMost; }
@@ -818,8 +818,8 @@ cudaError_t tc_gradients(const pbt_gated_desc* d, const Operand& dz, const Opera
   return rows_columns(d) == 16 ? launch_few<16>(d, p, tmA, tmB, s) : launch_few<32>(d, p, tmA, tmB, s);
 }
 
-cudaError_t tc_forward(const pbt_gated_desc* d, const Operand& x, const Operand& w, void* h, float* z, int pitch, cudaStream_t s) {
-  if (d->rows <= kRowsForward) return rows_forward(d, x, w, h, z, pitch, s);
+cudaError_t tc_forward(const pbt_gated_desc* d, const Operand& x, const Operand& w, void* h, float* z, int pitch, bool packed, cudaStream_t s) {
+  if (d->rows <= kRowsForward) return rows_forward(d, x, w, h, z, pitch, packed, s);
   TileParams p;
   memset(&p, 0, sizeof(p));
   p.rows = d->rows; p.hidden = d->hidden;
@@ -868,7 +868,7 @@ cudaError_t tc_forward(const pbt_gated_desc* d, const Operand& x, const Operand&
   if (!ok) return cudaErrorInvalidValue;
 
   auto launch = [&](auto kernel, int bytes, int at_once, int ctas) {
-    return launch_with((unsigned)(ctas * std::min(p.num_tiles, at_once)), kTcThreads, bytes, s)(kernel, maps, p);
+    return launch_ordered(packed ? kAfter : 0, (unsigned)(ctas * std::min(p.num_tiles, at_once)), kTcThreads, bytes, s, kernel, maps, p);
   };
   if (use_pair) return launch(k_gated_tc_pair, Tile<true, 128, kPairStages>::kTotal, sms / 2, 2);
   if (hn == 128) return launch(k_gated_tc<128, 3>, Tile<false, 128, 3>::kTotal, sms, 1);

@@ -38,7 +38,7 @@ struct Smem {
 template <int BN, int STAGES, int EPI, int NEPIW>
 __global__ void __launch_bounds__(64 + 32 * NEPIW, 1)
 k_gemm_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const TcParams p) {
-  pdl_prologue();
+  order_begin(p.order);
   using L = Smem<BN, STAGES, NEPIW>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -183,6 +183,7 @@ k_gemm_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
   tc_fence_before();
   __syncthreads();
   if (warp == 1) tmem_dealloc(tmem_base, kTmemCols);
+  order_end(p.order);
 }
 
 template <int BN, int STAGES, int EPI, int NEPIW>
@@ -195,7 +196,7 @@ cudaError_t launch_cfg(const CUtensorMap& tmA, const CUtensorMap& tmB, TcParams&
   p.tiles_n = (p.N + BN - 1) / BN;
   p.num_tiles = p.tiles_m * p.tiles_n * p.batch;
   const int grid = p.num_tiles < sms ? p.num_tiles : sms;
-  launch_with(grid, 64 + 32 * NEPIW, L::kTotal, s)(k_gemm_tc<BN, STAGES, EPI, NEPIW>, tmA, tmB, p);
+  launch_ordered(p.order, grid, 64 + 32 * NEPIW, L::kTotal, s, k_gemm_tc<BN, STAGES, EPI, NEPIW>, tmA, tmB, p);
   return cudaGetLastError();
 }
 
@@ -252,6 +253,7 @@ cudaError_t launch_gemm_tc(const GemmArgs& g, Counters* counters, cudaStream_t s
   p.bias = g.bias; p.strideBias = g.strideBias; p.relu = g.relu;
   p.mask = reinterpret_cast<const bf16*>(g.mask); p.ldmask = g.ldmask; p.strideMask = g.strideMask;
   p.counters = counters;
+  p.order = g.order;
   int BN = g.N >= 256 ? 256 : 128;
   if (BN == 256) {
     // Few tiles: 128-wide tiles when the 256-wide ones would leave most of the last wave idle (a wave of half tiles

@@ -37,7 +37,7 @@ static_assert(kPSmemTotal <= 232448, "shared memory budget of one CTA");
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPThreads, 1)
 k_gemm_tc_pair(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                const __grid_constant__ CUtensorMap tmC, const TcParams p) {
-  pdl_prologue();
+  order_begin(p.order);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + kPBarOffset);   // used in the leader only
@@ -194,6 +194,7 @@ k_gemm_tc_pair(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   __syncthreads();
   cluster_sync_all();   // neither CTA leaves while its partner may still signal its barriers or read its operands
   if (warp == 1) tmem_dealloc_pair(tmem_base, kTmemCols);
+  order_end(p.order);
 }
 
 }  // namespace
@@ -229,6 +230,7 @@ cudaError_t launch_gemm_tc_pair(const GemmArgs& g, Counters* counters, cudaStrea
   p.bias = g.bias; p.strideBias = g.strideBias; p.relu = g.relu;
   p.mask = reinterpret_cast<const bf16*>(g.mask); p.ldmask = g.ldmask; p.strideMask = g.strideMask;
   p.counters = counters;
+  p.order = g.order;
   CUtensorMap tmA, tmB;
   bool ok;
   const long long a_rows = g.a_rowoff ? g.a_rows_total : (g.a_mn ? g.K : g.M);   // a windowed operand: the whole pool
@@ -256,7 +258,7 @@ cudaError_t launch_gemm_tc_pair(const GemmArgs& g, Counters* counters, cudaStrea
   if (e != cudaSuccess) return e;
   int pairs = sms / 2;
   if (pairs > p.num_tiles) pairs = p.num_tiles;
-  launch_with(2 * pairs, kPThreads, kPSmemTotal, s)(k_gemm_tc_pair, tmA, tmB, tmC, p);
+  launch_ordered(p.order, 2 * pairs, kPThreads, kPSmemTotal, s, k_gemm_tc_pair, tmA, tmB, tmC, p);
   return cudaGetLastError();
 }
 

@@ -89,6 +89,19 @@ inline LaunchCfg launch_with(dim3 grid, dim3 block, size_t smem, cudaStream_t st
 // leaves or write what it reads, before they do.  What the predecessor writes is read past the read-only path (__ldcg, cp.async, TMA), since it
 // changes while the kernel runs.  Every grid waits in some thread before it ends, so that whatever follows in the stream, waiting or not, follows
 // the predecessor, too.
+// How a kernel that takes an Order stands to its neighbours in the stream.
+enum Order : int {
+  kAfter = 1,       // launched while its predecessor, which allows it, runs; waits for it before anything else
+  kBeside = 2,      // the same, but it needs nothing of that predecessor (all before it is complete), and waits for it at its end
+  kLeads = 4,       // allows the same to its successor, once all its CTAs run
+};
+__device__ __forceinline__ void order_begin(int order) {
+  if (!(order & kBeside)) pdl_prologue();
+  if (order & kLeads) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+__device__ __forceinline__ void order_end(int order) {
+  if (order & kBeside) pdl_prologue();
+}
 template <typename... KArgs, typename... Args>
 cudaError_t launch_after(dim3 grid, unsigned threads, size_t smem, cudaStream_t s, void (*kernel)(KArgs...), Args&&... args) {
   cudaLaunchConfig_t cfg;
@@ -103,6 +116,11 @@ cudaError_t launch_after(dim3 grid, unsigned threads, size_t smem, cudaStream_t 
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, KArgs(static_cast<Args&&>(args))...);
+}
+template <typename... KArgs, typename... Args>
+cudaError_t launch_ordered(int order, dim3 grid, unsigned threads, size_t smem, cudaStream_t s, void (*kernel)(KArgs...), Args&&... args) {
+  if (order & (kAfter | kBeside)) return launch_after(grid, threads, smem, s, kernel, static_cast<Args&&>(args)...);
+  return launch_with(grid, threads, smem, s)(kernel, static_cast<Args&&>(args)...);
 }
 #endif
 
@@ -158,6 +176,7 @@ struct GemmArgs {
   // k for an MN-major one.
   const int* a_rowoff; long long a_rows_total;
   const int* b_rowoff; long long b_rows_total;
+  int order;      // Order below (tensor-core kernels only); 0: plain stream order
 };
 
 // launchers (each enqueues on `s` and returns the CUDA error of the launch)

@@ -22,6 +22,7 @@ struct TcParams {
   Counters* counters;
   const int* a_rowoff;   // per-problem first row of the A / B operand inside a shared matrix (null: batched operand)
   const int* b_rowoff;
+  int order;             // Order
 };
 
 
