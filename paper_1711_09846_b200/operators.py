@@ -538,7 +538,8 @@ class GatedUnit:
         d.members, d.width, d.hidden, d.dtype, d.activation = m, k, n // 2, _TYPES[weight.dtype], _ACTIVATIONS[activation]
         d.weight, d.weight_member, d.weight_row = weight.data_ptr(), weight.stride(0), weight.stride(1)
         self._status = torch.zeros(8, dtype=torch.int32, device=weight.device)
-        self._floats = torch.empty(0, device=weight.device)         # (new_empty of a tensor costs less than torch.empty with a type and a device)
+        # (new_empty of a tensor costs less than torch.empty with a type and a device; the type is named here, or it would be torch's default one)
+        self._floats = torch.empty(0, dtype=torch.float32, device=weight.device)
         self._known, self._known_backward = (None, b""), (None, b"", 0)      # geometry of the last calls, and what the library is told of it
         self._home = _current_stream(weight.device.index)
         torch.cuda.current_stream(weight.device).synchronize()      # the calls may be on any stream
