@@ -425,6 +425,14 @@ class AdapterProjection:
 # --- dropout -----------------------------------------------------------------------------------------------------------------
 
 
+class _Rule(NamedTuple):
+    """A dropout as the library is told of it, and the tensors that it points to."""
+    rule: PbtDropRule
+    tensors: tuple
+    members: Optional[int]
+    device: Optional[torch.device]
+
+
 class Dropout:
     """Which elements of which member are dropped (pbt_drop_rule).  No mask is stored: both directions draw it from
     (seed; member, the member's step, site, place of the element).
@@ -434,52 +442,66 @@ class Dropout:
     replayed has to take, or it draws the same masks again); site: which dropout of the network (two with the same site and width draw
     the same); first_member: index of the first member in the whole population, for a shard of it.
 
-    The tensors are used where they lie: update them in place between calls.  Both passes of a step take the same object (or an equal one)."""
-    __slots__ = ("rate", "seed", "step", "site", "first_member", "tensors", "members", "device", "rule", "_known")
+    The tensors are used where they lie: update them in place between steps.  What is assigned to one of the five is checked like the constructor's
+    arguments and holds from the next call on (a captured graph keeps the numbers that it was captured with).  Both passes of a step take
+    the same dropout, or one of the same values."""
+    __slots__ = ("_values", "_laid", "_known")
 
     def __init__(self, rate: Union[float, torch.Tensor], seed: int, step: Union[int, torch.Tensor], site: int = 0, first_member: int = 0):
-        self.rate, self.seed, self.step, self.site, self.first_member = rate, seed, step, site, first_member
-        self.tensors, rates, steps = (), None, None
+        self._known = (None, None, None, b"")            # geometry of the last dropout_forward's activations and its rule, and what the library is told of them
+        self._lay_out(rate, seed, step, site, first_member)
+
+    def _lay_out(self, *values) -> _Rule:
+        rate, seed, step, site, first_member = values
+        tensors, rates, steps = (), None, None
         seed, site, first_member = int(seed), int(site), int(first_member)
         if isinstance(rate, torch.Tensor):
             _require(rate.is_cuda and rate.dtype is torch.float32 and rate.dim() == 1 and rate.is_contiguous(),
                      "a dropout's rate is a number or a contiguous float32 tensor [members] on the device")
-            self.tensors, rates, rate = (rate,), rate.data_ptr(), 0.0
+            tensors, rates, rate = (rate,), rate.data_ptr(), 0.0
         if isinstance(step, torch.Tensor):
             _require(step.is_cuda and step.dtype is torch.int64 and step.dim() == 1 and step.is_contiguous(),
                      "a dropout's step is a number or a contiguous int64 tensor [members] on the device")
-            self.tensors, steps, step = (*self.tensors, step), step.data_ptr(), 0
+            tensors, steps, step = (*tensors, step), step.data_ptr(), 0
         rate, step = float(rate), int(step)
         _require(0 <= seed < 1 << 64 and 0 <= step < 1 << 63 and 0 <= site <= 1 << 30 and 0 <= first_member <= _MOST,
                  "a dropout's seed is a number of 64 bits; step, site (at most 2^30) and first_member are not negative")
         _require(0 <= rate <= 1, "a dropout's rate lies in [0, 1]")
-        self.members, self.device = (self.tensors[0].shape[0], self.tensors[0].device) if self.tensors else (None, None)
-        _require(all(t.shape[0] == self.members and t.device == self.device for t in self.tensors), "a dropout's rate and step differ in members or device")
-        self.rule = PbtDropRule(rates, steps, seed, step, rate, site, first_member)
-        self._known = (None, None, b"")                  # geometry of the last dropout_forward's activations, and what the library is told of it
+        members, device = (tensors[0].shape[0], tensors[0].device) if tensors else (None, None)
+        _require(all(t.shape[0] == members and t.device == device for t in tensors), "a dropout's rate and step differ in members or device")
+        self._laid = _Rule(PbtDropRule(rates, steps, seed, step, rate, site, first_member), tensors, members, device)
+        self._values = values
+        return self._laid
 
-    def _for(self, members, device) -> PbtDropRule:
-        if self.members is not None and (self.members != members or self.device != device):
-            raise ValueError("a dropout's rate and step are [members] of the activations, on their device")
-        return self.rule
+    def _change(self, k, value):
+        self._lay_out(*self._values[:k], value, *self._values[k + 1:])
+
+    rate, seed, step, site, first_member = (property(lambda self, k=k: self._values[k], lambda self, value, k=k: self._change(k, value)) for k in range(5))
+
+
+def _rule_for(laid: _Rule, members, device) -> PbtDropRule:
+    if laid.members is not None and (laid.members != members or laid.device != device):
+        raise ValueError("a dropout's rate and step are [members] of the activations, on their device")
+    return laid.rule
 
 
 def dropout_forward(x, dropout: Dropout, residual=None, stream=None):
     """residual + keep x / (1 - rate) (pbt_dropout); x and residual: [members, rows, width], float32 or bfloat16, with contiguous columns."""
     kind = (x.shape, x.stride(), x.dtype, x.device)
     other = None if residual is None else (residual.shape, residual.stride(), residual.dtype, residual.device)
-    known, known_other, told = dropout._known
-    if known != kind or known_other != other:            # (checks and description cost a small call as much as its launch)
-        told = _describe_dropout(x, dropout, residual)
-        dropout._known = (kind, other, told)
+    laid = dropout._laid
+    known, known_other, known_laid, told = dropout._known
+    if known != kind or known_other != other or known_laid is not laid:      # (checks and description cost a small call as much as its launch)
+        told = _describe_dropout(x, laid, residual)
+        dropout._known = (kind, other, laid, told)
     d = PbtDropoutDesc.from_buffer_copy(told)
     d.x = x.data_ptr()
     if residual is not None:
         d.residual = residual.data_ptr()
-    return _on(kind[3], stream, () if stream is None else (x, residual, *dropout.tensors), _dropout, d, x)
+    return _on(kind[3], stream, () if stream is None else (x, residual, *laid.tensors), _dropout, d, x)
 
 
-def _describe_dropout(x, dropout, residual) -> bytes:
+def _describe_dropout(x, laid, residual) -> bytes:
     """What pbt_dropout is told of activations like these, their addresses apart."""
     shape, dtype, device = kind = x.shape, x.dtype, x.device
     if not (x.is_cuda and len(shape) == 3 and dtype in _TYPES):
@@ -489,7 +511,7 @@ def _describe_dropout(x, dropout, residual) -> bytes:
         raise ValueError("activations have at most 2^31 - 1 members, rows and columns")
     _, member, row = _activation(x, kind, "x")
     _, other_member, other_row = (None, 0, 0) if residual is None else _activation(residual, kind, "residual")
-    return bytes(PbtDropoutDesc(m, rows, width, _TYPES[dtype], None, member, row, None, other_member, other_row, None, dropout._for(m, device)))
+    return bytes(PbtDropoutDesc(m, rows, width, _TYPES[dtype], None, member, row, None, other_member, other_row, None, _rule_for(laid, m, device)))
 
 
 def _dropout(s, d, x):
@@ -571,7 +593,9 @@ class GatedUnit:
         d = PbtGatedDesc.from_buffer_copy(told)
         d.x = x.data_ptr()
         if dropout is not None:
-            d.drop = C.addressof(dropout._for(self._members, self._device))
+            laid = dropout._laid
+            d.drop = C.addressof(_rule_for(laid, self._members, self._device))
+            d.laid = laid                                # (lives as long as the description, whatever becomes of the dropout meanwhile)
         return d
 
     def forward(self, x, dropout: Optional[Dropout] = None, keep: bool = False, stream=None):
@@ -582,8 +606,9 @@ class GatedUnit:
         if known != kind:                                # (checks and description cost a small call as much as its launch)
             told = self._describe(x)
             self._known = (kind, told)
-        inputs = () if stream is None else (x, self.weight, *(dropout.tensors if dropout else ()))
-        return _on(self._device, stream, inputs, self._forward, self._call(told, x, dropout), kind[0][1], keep)
+        d = self._call(told, x, dropout)
+        inputs = () if stream is None else (x, self.weight, *(() if dropout is None else d.laid.tensors))
+        return _on(self._device, stream, inputs, self._forward, d, kind[0][1], keep)
 
     def _forward(self, s, d, rows, keep):
         h = self.weight.new_empty((self._members, rows, self.hidden))
@@ -610,7 +635,7 @@ class GatedUnit:
         d.dh = dh.data_ptr()
         if kept is not None:
             d.kept = kept.data_ptr()
-        inputs = () if stream is None else (dh, x, kept, self.weight, *(dropout.tensors if dropout else ()))
+        inputs = () if stream is None else (dh, x, kept, self.weight, *(() if dropout is None else d.laid.tensors))
         result, need = _on(self._device, stream, inputs, self._backward, d, x, nbytes)
         if known != kind or need != nbytes:
             self._known_backward = (kind, told, need)

@@ -1,0 +1,94 @@
+"""What a caller changes between two calls of the same sizes: the next call goes by it, or is refused."""
+import pytest
+
+from recording_library import install, on_device
+
+CHANGES = [("rate", 0.25), ("seed", 99), ("step", 12), ("site", 3), ("first_member", 5)]
+
+
+def _told(rule):
+    return dict(rate=rule.rate_all, seed=rule.seed, step=rule.step, site=rule.site, first_member=rule.first_member)
+
+
+@pytest.mark.parametrize("name, value", CHANGES)
+@pytest.mark.parametrize("gated", [False, True])
+def test_a_dropout_that_is_changed_is_what_the_next_call_is_told(monkeypatch, name, value, gated):
+    import torch
+    import paper_1711_09846_b200 as pbt
+    lib = install(monkeypatch)
+    x, dh = (on_device(torch.zeros(2, 3, n)) for n in (16, 8))
+    unit = pbt.GatedUnit(on_device(torch.zeros(2, 16, 16)))
+    drop = pbt.Dropout(0.5, 7, 11, 1, 2)
+
+    def call():
+        if gated:
+            unit.forward(x, dropout=drop)
+            unit.backward(dh, x, dropout=drop)
+        else:
+            pbt.dropout_forward(x, drop, residual=x)
+            pbt.dropout_backward(x, drop)
+        return [_told(r) for r in lib.rules[-2:]]
+    before = dict(rate=0.5, seed=7, step=11, site=1, first_member=2)
+    assert call() == [before, before]
+    setattr(drop, name, value)
+    assert getattr(drop, name) == value and call() == [{**before, name: value}] * 2
+    drop.step += 1
+    assert call() == [{**before, name: value, "step": (value if name == "step" else 11) + 1}] * 2
+
+
+def test_a_dropout_takes_tensors_in_the_place_of_numbers_and_the_other_way_round(monkeypatch):
+    import torch
+    import paper_1711_09846_b200 as pbt
+    lib = install(monkeypatch)
+    x = on_device(torch.zeros(2, 3, 16))
+    rate, step = on_device(torch.zeros(2)), on_device(torch.zeros(2, dtype=torch.int64))
+    drop = pbt.Dropout(0.5, 7, 11)
+    pbt.dropout_forward(x, drop)
+    drop.rate, drop.step = rate, step
+    drop.step += 1                                     # in place, and the same tensor again
+    pbt.dropout_forward(x, drop)
+    assert (lib.rules[-1].rate, lib.rules[-1].steps) == (rate.data_ptr(), step.data_ptr()) and step.tolist() == [1, 1]
+    drop.rate = 0.25
+    pbt.dropout_forward(x, drop)
+    assert (lib.rules[-1].rate, lib.rules[-1].rate_all, lib.rules[-1].steps) == (None, 0.25, step.data_ptr())
+
+
+def test_what_a_dropout_cannot_be_changed_to_leaves_it_as_it_was(monkeypatch):
+    import torch
+    import paper_1711_09846_b200 as pbt
+    lib = install(monkeypatch)
+    x = on_device(torch.zeros(2, 3, 16))
+    drop = pbt.Dropout(0.5, 7, 11, 1, 2)
+    pbt.dropout_forward(x, drop)
+    three = on_device(torch.zeros(3))
+    for name, bad in (("rate", 1.5), ("rate", float("nan")), ("rate", three.double()), ("seed", -1), ("step", -1), ("step", three), ("site", (1 << 30) + 1),
+                      ("first_member", -1)):
+        with pytest.raises(ValueError):
+            setattr(drop, name, bad)
+    pbt.dropout_forward(x, drop)
+    assert _told(lib.rules[-1]) == _told(lib.rules[0])
+    drop.rate = three                                  # one rate too many for these activations, in whatever order they meet
+    with pytest.raises(ValueError):
+        pbt.dropout_forward(x, drop)
+    with pytest.raises(ValueError):
+        drop.step = on_device(torch.zeros(2, dtype=torch.int64))
+    with pytest.raises(AttributeError):
+        drop.stage = 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name, value", CHANGES)
+def test_the_masks_of_a_changed_dropout_are_those_of_a_new_one(name, value):
+    import torch
+    import paper_1711_09846_b200 as pbt
+    args = dict(rate=0.5, seed=7, step=11, site=1, first_member=2)
+    x = torch.ones(2, 40, 200, device="cuda")
+    unit = pbt.GatedUnit(torch.randn(2, 64, 200, device="cuda"), "sigmoid")
+    drop = pbt.Dropout(**args)
+
+    def masks(d):
+        return pbt.dropout_forward(x, d), unit.forward(x, dropout=d)
+    first = masks(drop)
+    setattr(drop, name, value)
+    for was, got, want in zip(first, masks(drop), masks(pbt.Dropout(**{**args, name: value}))):
+        assert torch.equal(got, want) and not torch.equal(got, was)
