@@ -429,6 +429,7 @@ class _Rule(NamedTuple):
     """A dropout as the library is told of it, and the tensors that it points to."""
     rule: PbtDropRule
     tensors: tuple
+    places: tuple                # (tensor, its address)
     members: Optional[int]
     device: Optional[torch.device]
 
@@ -442,7 +443,7 @@ class Dropout:
     replayed has to take, or it draws the same masks again); site: which dropout of the network (two with the same site and width draw
     the same); first_member: index of the first member in the whole population, for a shard of it.
 
-    The tensors are used where they lie: update them in place between steps.  What is assigned to one of the five is checked like the constructor's
+    The tensors are used where they lie at the call: update them in place between steps.  What is assigned to one of the five is checked like the constructor's
     arguments and holds from the next call on (a captured graph keeps the numbers that it was captured with).  Both passes of a step take
     the same dropout, or one of the same values."""
     __slots__ = ("_values", "_laid", "_known")
@@ -469,9 +470,19 @@ class Dropout:
         _require(0 <= rate <= 1, "a dropout's rate lies in [0, 1]")
         members, device = (tensors[0].shape[0], tensors[0].device) if tensors else (None, None)
         _require(all(t.shape[0] == members and t.device == device for t in tensors), "a dropout's rate and step differ in members or device")
-        self._laid = _Rule(PbtDropRule(rates, steps, seed, step, rate, site, first_member), tensors, members, device)
+        places = tuple((t, t.data_ptr()) for t in tensors)
+        _require(members == 0 or all(at for _, at in places), "a dropout's rate or step has no memory")
+        self._laid = _Rule(PbtDropRule(rates, steps, seed, step, rate, site, first_member), tensors, places, members, device)
         self._values = values
         return self._laid
+
+    def _now(self) -> _Rule:
+        """The rule for a call, laid out anew if a tensor's storage was replaced."""
+        laid = self._laid
+        for t, at in laid.places:
+            if t.data_ptr() != at or t.numel() != laid.members:
+                return self._lay_out(*self._values)
+        return laid
 
     def _change(self, k, value):
         self._lay_out(*self._values[:k], value, *self._values[k + 1:])
@@ -489,7 +500,7 @@ def dropout_forward(x, dropout: Dropout, residual=None, stream=None):
     """residual + keep x / (1 - rate) (pbt_dropout); x and residual: [members, rows, width], float32 or bfloat16, with contiguous columns."""
     kind = (x.shape, x.stride(), x.dtype, x.device)
     other = None if residual is None else (residual.shape, residual.stride(), residual.dtype, residual.device)
-    laid = dropout._laid
+    laid = dropout._now()
     known, known_other, known_laid, told = dropout._known
     if known != kind or known_other != other or known_laid is not laid:      # (checks and description cost a small call as much as its launch)
         told = _describe_dropout(x, laid, residual)
@@ -593,7 +604,7 @@ class GatedUnit:
         d = PbtGatedDesc.from_buffer_copy(told)
         d.x = x.data_ptr()
         if dropout is not None:
-            laid = dropout._laid
+            laid = dropout._now()
             d.drop = C.addressof(_rule_for(laid, self._members, self._device))
             d.laid = laid                                # (lives as long as the description, whatever becomes of the dropout meanwhile)
         return d

@@ -92,3 +92,42 @@ def test_the_masks_of_a_changed_dropout_are_those_of_a_new_one(name, value):
     setattr(drop, name, value)
     for was, got, want in zip(first, masks(drop), masks(pbt.Dropout(**{**args, name: value}))):
         assert torch.equal(got, want) and not torch.equal(got, was)
+
+
+def test_a_dropout_follows_its_tensors_to_other_memory(monkeypatch):
+    """A tensor whose storage is replaced (p.data = ..., which flattening optimizers and module moves do) is read where it lies now."""
+    import torch
+    import paper_1711_09846_b200 as pbt
+    lib = install(monkeypatch)
+    x = on_device(torch.zeros(2, 3, 16))
+    unit = pbt.GatedUnit(on_device(torch.zeros(2, 16, 16)))
+    rate, step = on_device(torch.zeros(2)), on_device(torch.zeros(2, dtype=torch.int64))
+    drop = pbt.Dropout(rate, 7, step)
+
+    def told():
+        pbt.dropout_forward(x, drop)
+        unit.forward(x, dropout=drop)
+        assert _places(lib.rules[-1]) == _places(lib.rules[-2])
+        return _places(lib.rules[-1])
+    old = told()
+    assert old == (rate.data_ptr(), step.data_ptr())
+    other = on_device(torch.ones(2)), on_device(torch.ones(2, dtype=torch.int64))
+    rate.data = other[0]
+    assert told() == (other[0].data_ptr(), old[1])
+    step.data = other[1]
+    assert told() == (other[0].data_ptr(), other[1].data_ptr())
+    for bad in (torch.zeros(3), torch.zeros(2, dtype=torch.float64), torch.zeros(4)[::2]):
+        rate.data = on_device(bad)
+        with pytest.raises(ValueError):
+            pbt.dropout_forward(x, drop)
+        with pytest.raises(ValueError):
+            unit.forward(x, dropout=drop)
+    rate.data = other[0][:1]                           # the same place, one rate too few
+    with pytest.raises(ValueError):
+        pbt.dropout_forward(x, drop)
+    rate.data = other[0]
+    assert told() == (other[0].data_ptr(), other[1].data_ptr())
+
+
+def _places(rule):
+    return rule.rate, rule.steps
