@@ -550,7 +550,8 @@ class GatedUnit:
     h = keep / (1 - rate) act(x Wg^T) (x Wu^T).
 
     weight: [members, 2 hidden, width], the gate's rows first, then the up-projection's; float32 or bfloat16, contiguous columns, any
-    member and row stride (weight.expand(...): one for all members).  It is used where it lies: update it in place between calls.
+    member and row stride (weight.expand(...): one for all members).  It is used where it lies at the call: update it in place between calls.  Its
+    storage may be replaced by one of the same shape and strides.
     activation: "silu", "gelu" (with the error function), "relu" or "sigmoid".  The projection behind it is a plain product: grouped_gemm, or
     AdapterProjection where it is shared.
 
@@ -563,9 +564,10 @@ class GatedUnit:
         _require(n > 0 and n % 2 == 0, "weight has the gate's rows and as many of the up-projection")
         _require(activation in _ACTIVATIONS, "activation is " + ", ".join(_ACTIVATIONS))
         _require(max(m, n, k) <= _MOST, "members, hidden and width are at most 2^31 - 1")
-        self.weight, self.hidden = weight, n // 2
+        self._weight, self._hidden = weight, n // 2
         self._members, self._width, self._dtype, self._device = m, k, weight.dtype, weight.device
-        self._pitch = (self.hidden + 7) // 8 * 8                    # of g and u
+        self._shape, self._strides = weight.shape, weight.stride()
+        self._pitch = (self._hidden + 7) // 8 * 8                   # of g and u
         self.lib = load_library()
         d = self._desc = PbtGatedDesc()
         d.members, d.width, d.hidden, d.dtype, d.activation = m, k, n // 2, _TYPES[weight.dtype], _ACTIVATIONS[activation]
@@ -579,6 +581,9 @@ class GatedUnit:
         d.status_device = self._status.data_ptr()
         _check(self.lib.pbt_gated_query_workspace(C.byref(d), 0, C.byref(C.c_size_t(0))))
 
+    weight = property(lambda self: self._weight)
+    hidden = property(lambda self: self._hidden)
+
     def _describe(self, x, dh=None, kept=None) -> bytes:
         """What the library is told of a call on rows like these, their addresses apart."""
         shape, width = x.shape, self._width
@@ -591,7 +596,7 @@ class GatedUnit:
         d.rows = rows
         d.x_member, d.x_row = _rows_of(x, "x")
         if dh is not None:
-            if not (dh.shape == (self._members, rows, self.hidden) and dh.dtype is self._dtype and dh.device == self._device):
+            if not (dh.shape == (self._members, rows, self._hidden) and dh.dtype is self._dtype and dh.device == self._device):
                 raise ValueError("dh is [members, rows, hidden] of the weight's type and device")
             d.dh_member, d.dh_row = _rows_of(dh, "dh")
         if kept is not None and not (kept.shape == (self._members, rows, 2, self._pitch) and kept.dtype is torch.float32 and kept.device == self._device
@@ -601,8 +606,11 @@ class GatedUnit:
 
     def _call(self, told, x, dropout):
         """The description of a call (its own: calls from several threads share none)."""
+        w = self._weight
+        if w.shape != self._shape or w.stride() != self._strides or w.dtype is not self._dtype or w.device != self._device:
+            raise ValueError("the weight's shape, strides, type or device changed: it takes another GatedUnit")
         d = PbtGatedDesc.from_buffer_copy(told)
-        d.x = x.data_ptr()
+        d.x, d.weight = x.data_ptr(), w.data_ptr()
         if dropout is not None:
             laid = dropout._now()
             d.drop = C.addressof(_rule_for(laid, self._members, self._device))
@@ -618,11 +626,11 @@ class GatedUnit:
             told = self._describe(x)
             self._known = (kind, told)
         d = self._call(told, x, dropout)
-        inputs = () if stream is None else (x, self.weight, *(() if dropout is None else d.laid.tensors))
+        inputs = () if stream is None else (x, self._weight, *(() if dropout is None else d.laid.tensors))
         return _on(self._device, stream, inputs, self._forward, d, kind[0][1], keep)
 
     def _forward(self, s, d, rows, keep):
-        h = self.weight.new_empty((self._members, rows, self.hidden))
+        h = self._weight.new_empty((self._members, rows, self._hidden))
         d.h = h.data_ptr()
         kept = None
         if keep:
@@ -646,14 +654,14 @@ class GatedUnit:
         d.dh = dh.data_ptr()
         if kept is not None:
             d.kept = kept.data_ptr()
-        inputs = () if stream is None else (dh, x, kept, self.weight, *(() if dropout is None else d.laid.tensors))
+        inputs = () if stream is None else (dh, x, kept, self._weight, *(() if dropout is None else d.laid.tensors))
         result, need = _on(self._device, stream, inputs, self._backward, d, x, nbytes)
         if known != kind or need != nbytes:
             self._known_backward = (kind, told, need)
         return result
 
     def _backward(self, s, d, x, nbytes):
-        dx, dweight = _like(x), _like(self.weight)
+        dx, dweight = _like(x), _like(self._weight)
         d.dx, d.dweight = dx.data_ptr(), dweight.data_ptr()
         return (dx, dweight), self._run(d, 1, self.lib.pbt_gated_backward, s, nbytes)
 
@@ -674,7 +682,7 @@ class GatedUnit:
 
     def check(self):
         """Waits for the enqueued calls and raises if one of the kernels' bounded waits ran out (PBT_ERR_TIMEOUT)."""
-        torch.cuda.synchronize(self.weight.device)
+        torch.cuda.synchronize(self._weight.device)
         code = int(self._status[4].item())
         if code:
             raise PbtError(code, "a bounded wait inside a kernel ran out")

@@ -131,3 +131,66 @@ def test_a_dropout_follows_its_tensors_to_other_memory(monkeypatch):
 
 def _places(rule):
     return rule.rate, rule.steps
+
+
+def test_a_unit_follows_its_weight_to_other_memory(monkeypatch):
+    """The same for a weight, in calls of sizes that were seen before; another geometry is refused."""
+    import torch
+    import paper_1711_09846_b200 as pbt
+    lib = install(monkeypatch)
+    x, dh = (on_device(torch.zeros(2, 3, n)) for n in (16, 8))
+    w = on_device(torch.zeros(2, 16, 16))
+    unit = pbt.GatedUnit(w)
+
+    def told():
+        _, kept = unit.forward(x, keep=True)
+        unit.backward(dh, x, kept)
+        places = {d.weight for _, d in lib.calls[-2:]}
+        assert len(places) == 1 and all((d.weight_member, d.weight_row) == (256, 16) for _, d in lib.calls[-2:])
+        return places.pop()
+    assert told() == w.data_ptr()
+    other = on_device(torch.ones(2, 16, 16))
+    old, w.data = w.data_ptr(), other
+    assert told() == other.data_ptr() != old
+    assert unit.weight is w
+    seen = len(lib.calls)
+    for bad in (torch.zeros(2, 16, 18)[..., :16], torch.zeros(2, 16, 16).transpose(1, 2), torch.zeros(2, 18, 16), torch.zeros(1, 16, 16).expand(2, 16, 16),
+                torch.zeros(2, 16, 16, dtype=torch.bfloat16)):
+        w.data = on_device(bad)
+        for call in (lambda: unit.forward(x), lambda: unit.backward(dh, x)):
+            with pytest.raises(ValueError):
+                call()
+    assert len(lib.calls) == seen
+    w.data = other
+    assert told() == other.data_ptr()
+    for name, value in (("weight", other), ("hidden", 4)):
+        with pytest.raises(AttributeError):
+            setattr(unit, name, value)
+    assert unit.hidden == 8
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows", [3, 100, 400])
+def test_results_of_tensors_that_were_moved(rows, dtype):
+    """Weight, rates and steps in other memory (the weight's at another alignment, too), the old memory overwritten: the bits of new objects."""
+    import torch
+    import paper_1711_09846_b200 as pbt
+    gen = torch.Generator().manual_seed(rows)
+    x, w, dh = (torch.randn(*shape, generator=gen).to(getattr(torch, dtype)).cuda() for shape in ((2, rows, 72), (2, 80, 72), (2, rows, 40)))
+    rate, step = torch.full((2,), 0.3, device="cuda"), torch.tensor([4, 5], device="cuda")
+    unit, drop = pbt.GatedUnit(w), pbt.Dropout(rate, 7, step)
+
+    def run(unit, drop):
+        h, kept = unit.forward(x, dropout=drop, keep=True)
+        return (h, *unit.backward(dh, x, kept, dropout=drop), pbt.dropout_forward(x, drop))
+    run(unit, drop)
+    for by in (0, 1, 8):
+        olds = [t.data for t in (w, rate, step)]
+        place = torch.empty(w.numel() + 8, dtype=w.dtype, device="cuda")[by:by + w.numel()].view(w.shape)
+        w.data, rate.data, step.data = place.copy_(w).mul_(1 + by), torch.full((2,), 0.2 + by / 32, device="cuda"), step + 1 + by
+        for old in olds:
+            old.fill_(float("nan") if old.is_floating_point() else 1 << 20)
+        for a, b in zip(run(unit, drop), run(pbt.GatedUnit(w), pbt.Dropout(rate, 7, step))):
+            assert torch.equal(a, b) and bool(torch.isfinite(a).all())
+    unit.check()
