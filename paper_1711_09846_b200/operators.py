@@ -681,10 +681,12 @@ class GatedUnit:
         return nbytes
 
     def check(self):
-        """Waits for the enqueued calls and raises if one of the kernels' bounded waits ran out (PBT_ERR_TIMEOUT)."""
-        torch.cuda.synchronize(self._weight.device)
+        """Waits for the enqueued calls and raises if one of the kernels' bounded waits ran out since the last check (PBT_ERR_TIMEOUT)."""
+        torch.cuda.synchronize(self._device)
         code = int(self._status[4].item())
         if code:
+            self._status.zero_()
+            torch.cuda.synchronize(self._device)         # the next calls may be on any stream
             raise PbtError(code, "a bounded wait inside a kernel ran out")
 
 
