@@ -426,10 +426,10 @@ class AdapterProjection:
 
 
 class _Rule(NamedTuple):
-    """A dropout as the library is told of it, and the tensors that it points to."""
+    """A dropout as the library is told of it, and the tensors that it points to; places: of each, with its address and bytes."""
     rule: PbtDropRule
     tensors: tuple
-    places: tuple                # (tensor, its address)
+    places: tuple
     members: Optional[int]
     device: Optional[torch.device]
 
@@ -470,8 +470,8 @@ class Dropout:
         _require(0 <= rate <= 1, "a dropout's rate lies in [0, 1]")
         members, device = (tensors[0].shape[0], tensors[0].device) if tensors else (None, None)
         _require(all(t.shape[0] == members and t.device == device for t in tensors), "a dropout's rate and step differ in members or device")
-        places = tuple((t, t.data_ptr()) for t in tensors)
-        _require(members == 0 or all(at for _, at in places), "a dropout's rate or step has no memory")
+        places = tuple((t, t.data_ptr(), t.nbytes) for t in tensors)
+        _require(members == 0 or all(at for _, at, _ in places), "a dropout's rate or step has no memory")
         self._laid = _Rule(PbtDropRule(rates, steps, seed, step, rate, site, first_member), tensors, places, members, device)
         self._values = values
         return self._laid
@@ -479,8 +479,8 @@ class Dropout:
     def _now(self) -> _Rule:
         """The rule for a call, laid out anew if a tensor's storage was replaced."""
         laid = self._laid
-        for t, at in laid.places:
-            if t.data_ptr() != at or t.numel() != laid.members:
+        for t, at, nbytes in laid.places:
+            if t.data_ptr() != at or t.nbytes != nbytes:
                 return self._lay_out(*self._values)
         return laid
 
@@ -566,7 +566,7 @@ class GatedUnit:
         _require(max(m, n, k) <= _MOST, "members, hidden and width are at most 2^31 - 1")
         self._weight, self._hidden = weight, n // 2
         self._members, self._width, self._dtype, self._device = m, k, weight.dtype, weight.device
-        self._shape, self._strides = weight.shape, weight.stride()
+        self._geometry = (weight.shape, weight.stride(), weight.dtype, weight.device)
         self._pitch = (self._hidden + 7) // 8 * 8                   # of g and u
         self.lib = load_library()
         d = self._desc = PbtGatedDesc()
@@ -604,17 +604,16 @@ class GatedUnit:
             raise ValueError("kept is what forward(keep=True) returned")
         return bytes(d)
 
-    def _call(self, told, x, dropout):
-        """The description of a call (its own: calls from several threads share none)."""
+    def _call(self, told, x, dropout, laid=None):
+        """The description of a call (its own: calls from several threads share none).  `laid` is what the dropout is laid out like; the caller holds
+        it until the call is done, whatever becomes of the dropout meanwhile."""
         w = self._weight
-        if w.shape != self._shape or w.stride() != self._strides or w.dtype is not self._dtype or w.device != self._device:
+        if (w.shape, w.stride(), w.dtype, w.device) != self._geometry:
             raise ValueError("the weight's shape, strides, type or device changed: it takes another GatedUnit")
         d = PbtGatedDesc.from_buffer_copy(told)
         d.x, d.weight = x.data_ptr(), w.data_ptr()
         if dropout is not None:
-            laid = dropout._now()
-            d.drop = C.addressof(_rule_for(laid, self._members, self._device))
-            d.laid = laid                                # (lives as long as the description, whatever becomes of the dropout meanwhile)
+            d.drop = C.addressof(_rule_for(laid or dropout._laid, self._members, self._device))
         return d
 
     def forward(self, x, dropout: Optional[Dropout] = None, keep: bool = False, stream=None):
@@ -625,8 +624,9 @@ class GatedUnit:
         if known != kind:                                # (checks and description cost a small call as much as its launch)
             told = self._describe(x)
             self._known = (kind, told)
-        d = self._call(told, x, dropout)
-        inputs = () if stream is None else (x, self._weight, *(() if dropout is None else d.laid.tensors))
+        laid = None if dropout is None else dropout._now()
+        d = self._call(told, x, dropout, laid)
+        inputs = () if stream is None else (x, self._weight, *(laid.tensors if laid else ()))
         return _on(self._device, stream, inputs, self._forward, d, kind[0][1], keep)
 
     def _forward(self, s, d, rows, keep):
@@ -650,11 +650,12 @@ class GatedUnit:
         if known != kind:
             told = self._describe(x, dh, kept)
             nbytes = 0
-        d = self._call(told, x, dropout)
+        laid = None if dropout is None else dropout._now()
+        d = self._call(told, x, dropout, laid)
         d.dh = dh.data_ptr()
         if kept is not None:
             d.kept = kept.data_ptr()
-        inputs = () if stream is None else (dh, x, kept, self._weight, *(() if dropout is None else d.laid.tensors))
+        inputs = () if stream is None else (dh, x, kept, self._weight, *(laid.tensors if laid else ()))
         result, need = _on(self._device, stream, inputs, self._backward, d, x, nbytes)
         if known != kind or need != nbytes:
             self._known_backward = (kind, told, need)
