@@ -163,6 +163,19 @@ __device__ __forceinline__ void drain(const TileParams& p, const TileMaps& maps,
   }
 }
 
+// A pair in which a wait ran out: the leader's barriers count what both CTAs load, and one of the two may be up to a ring of loads ahead.  Of these,
+// the leader's were announced for both, and the partner's part never comes; the partner's are under way and were not announced.  With both put right, every
+// load's phase ends when its copies have landed.
+template <int STAGES, int BYTES>
+__device__ __forceinline__ void settle(uint64_t* full, uint32_t leader, uint32_t partner) {
+  const uint32_t less = min(leader, partner), more = max(leader, partner);
+  for (uint32_t i = less; i < more; ++i) {
+    if (i >= partner) mbar_complete_tx(&full[i % STAGES], BYTES);
+    else mbar_expect_tx(&full[i % STAGES], BYTES);
+  }
+  for (uint32_t i = more - min(more, (uint32_t)STAGES); i < more; ++i) mbar_wait_out(&full[i % STAGES], i / STAGES & 1);
+}
+
 template <bool PAIR, int HN, int STAGES>
 __device__ __forceinline__ void gated_tiles(const TileMaps& maps, const TileParams& p) {
   pdl_prologue();
@@ -176,6 +189,8 @@ __device__ __forceinline__ void gated_tiles(const TileMaps& maps, const TilePara
   uint64_t* idle = tempty + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(idle + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  volatile uint32_t* told = tmem_slot + 2;                               // of a pair: the partner's loads, and whether it gave up
+  uint32_t issued = 0;                                                   // loads of this CTA (thread 0)
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = PAIR ? cluster_ctarank() : 0;
@@ -232,14 +247,12 @@ __device__ __forceinline__ void gated_tiles(const TileMaps& maps, const TilePara
             tma_load_3d(sb + HN * kBK * 2, &maps.w, &full[stage], k0, p.hidden + n0, cw);
           }
           if (++stage == STAGES) { stage = 0; phase ^= 1; }
+          ++issued;
         }
       }
       if (!ok) give_up(31);
-      // Every stage that was armed has landed before the CTA ends, and been read unless a wait ran out.  What a pair's second CTA loads is
-      // counted by the leader alone; when one of them gave up, a stage may never be complete or not be counted, and what is under way has a millisecond to land.
-      if (rank == 0)
-        for (int s = 0; s < STAGES; ++s) mbar_wait_out(&full[s], s < (int)stage ? phase : phase ^ 1, PAIR && *abort_flag ? 1u << 14 : 1u << 22);
-      for (int i = 0; PAIR && !ok && i < 16384; ++i) __nanosleep(64);
+      // every stage that was armed has landed before the CTA ends (of a pair: below, if a wait ran out; else the products have read them)
+      for (int s = 0; s < STAGES && !PAIR; ++s) mbar_wait_out(&full[s], s < (int)stage ? phase : phase ^ 1);
       for (int s = 0; s < STAGES && ok; ++s) {
         if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) break;
         if (++stage == STAGES) { stage = 0; phase ^= 1; }
@@ -312,7 +325,17 @@ __device__ __forceinline__ void gated_tiles(const TileMaps& maps, const TilePara
   }
   tc_fence_before();
   __syncthreads();
-  if (PAIR) cluster_sync_all();   // neither CTA leaves while its partner may still signal its barriers or read its operands
+  if (PAIR) {
+    if (threadIdx.x == 0) {
+      st_cluster(map_to_cta(smem_u32(tmem_slot + 2), rank ^ 1), issued);
+      st_cluster(map_to_cta(smem_u32(tmem_slot + 3), rank ^ 1), (uint32_t)*abort_flag);
+    }
+    cluster_sync_all();   // neither CTA leaves while its partner may still signal its barriers or read its operands
+    if (*abort_flag || told[1]) {                // (both CTAs see the same)
+      if (threadIdx.x == 0 && rank == 0) settle<STAGES, L::kStage>(full, issued, told[0]);
+      cluster_sync_all();                        // nothing is in flight to either
+    }
+  }
   if (warp == 1) {
     if (PAIR) tmem_dealloc_pair(tmem_base, L::kCols);
     else tmem_dealloc(tmem_base, L::kCols);
