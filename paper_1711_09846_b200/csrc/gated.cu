@@ -3,6 +3,10 @@
 //
 // g and u stay in fp32 for the backward pass: as bf16 numbers they would add their own rounding to that of every gradient (dg and du have it once, as operands),
 // and a kept fp32 pair costs 0.2 ms of 2 for 80 members x 512 rows x 2048 hidden units, working it out anew 0.5.
+//
+// dg and du of a bf16 pass are rounded to bf16 before dx and dW, which then are off by 0.0023 of their 2-norm, 1.4 times what the rounding of the results alone leaves (0.0017).
+// A tensor-core product takes both operands in one 16-bit type; dg and du of 32 bits would go through it as two bf16 numbers each and double both products (another
+// 1.1 ms of 2 at that size).  Whoever needs gradients without that rounding has the fp32 unit.
 #include <algorithm>
 
 #include "gated.cuh"

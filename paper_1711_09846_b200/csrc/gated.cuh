@@ -85,7 +85,8 @@ cudaError_t launch_clusters(dim3 grid, unsigned threads, size_t smem, unsigned c
   return cudaLaunchKernelEx(&cfg, kernel, KArgs(static_cast<Args&&>(args))...);
 }
 
-// What goes into a bf16 number takes the short exponential and quotient (off by 2 + 1.2 |v| units of 2^-24 of the value), fp32 results the exact ones.
+// What goes into a bf16 number takes the short exponential, off by 2 + 1.2 |v| ulp at most, and the short quotient, by 2 ulp more (an ulp is at most 2^-23 of the
+// value; a bf16 result's rounding is 2^-8, 2^15 of them); fp32 results take expf and the rounded quotient.
 template <typename T>
 __device__ __forceinline__ float exponential(float v) {
   if constexpr (sizeof(T) == 4) return expf(v);

@@ -83,12 +83,6 @@ struct LaunchCfg {
 };
 inline LaunchCfg launch_with(dim3 grid, dim3 block, size_t smem, cudaStream_t stream) { return LaunchCfg{grid, block, smem, stream}; }
 
-// Launches a kernel that may begin while its predecessor in the stream still runs, whatever pbt_spec.programmatic_launches
-// says.  The predecessor allows it (griddepcontrol.launch_dependents, which takes effect once all its blocks are running, so
-// that everything before it is complete), and the kernel waits for its end (griddepcontrol.wait) in the threads that read what it
-// leaves or write what it reads, before they do.  What the predecessor writes is read past the read-only path (__ldcg, cp.async, TMA), since it
-// changes while the kernel runs.  Every grid waits in some thread before it ends, so that whatever follows in the stream, waiting or not, follows
-// the predecessor, too.
 // How a kernel that takes an Order stands to its neighbours in the stream.
 enum Order : int {
   kAfter = 1,       // launched while its predecessor, which allows it, runs; waits for it before anything else
@@ -102,6 +96,13 @@ __device__ __forceinline__ void order_begin(int order) {
 __device__ __forceinline__ void order_end(int order) {
   if (order & kBeside) pdl_prologue();
 }
+
+// Launches a kernel that may begin while its predecessor in the stream still runs, whatever pbt_spec.programmatic_launches
+// says.  The predecessor allows it (griddepcontrol.launch_dependents, which takes effect once all its blocks are running, so
+// that everything before it is complete), and the kernel waits for its end (griddepcontrol.wait) in the threads that read what it
+// leaves or write what it reads, before they do.  What the predecessor writes is read past the read-only path (__ldcg, cp.async, TMA), since it
+// changes while the kernel runs.  Every grid waits in some thread before it ends, so that whatever follows in the stream, waiting or not, follows
+// the predecessor, too.
 template <typename... KArgs, typename... Args>
 cudaError_t launch_after(dim3 grid, unsigned threads, size_t smem, cudaStream_t s, void (*kernel)(KArgs...), Args&&... args) {
   cudaLaunchConfig_t cfg;
@@ -176,7 +177,7 @@ struct GemmArgs {
   // k for an MN-major one.
   const int* a_rowoff; long long a_rows_total;
   const int* b_rowoff; long long b_rows_total;
-  int order;      // Order below (tensor-core kernels only); 0: plain stream order
+  int order;      // Order above (tensor-core kernels only); 0: plain stream order
 };
 
 // launchers (each enqueues on `s` and returns the CUDA error of the launch)
