@@ -363,12 +363,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_gated_tc(const __grid_constan
 //   dx        128 lanes: columns of the weight, read as it lies (its rows are the contraction: MN-major); N columns: rows of [dg du]
 // The partial sums of a cluster meet in shared memory, where every CTA adds up its own share of the rows over all CTAs' partial sums (in their
 // order); there g and u of a hidden unit meet, too.
-// Rows up to which the forward pass takes this form (32 rows, 2048 -> 4096: 12 us, in tiles 15; 50 rows of 8 members, 1024 -> 1024: 12.3 and 10.8).
+// Rows up to which the forward pass takes this form.  In it and in tiles, us: one member 1024 -> 2048, 32 rows 6.9 and 8.4; 2048 -> 4096, 32 rows 11.2 and 13.9, 40 rows
+// 13.1 and 14.0, 64 rows 14.7 and 13.9; 4096 -> 4096, 32 rows 17.7 and 23.3, 64 rows 21.0 and 23.2, 128 rows 25.7 and 23.5.  More members, 32 rows: 4 x 1024 -> 1024 8.8
+// and 8.6, 16 x 16.9 and 16.7, 40 x 512 -> 1024 22.8 and 20.9 (16 rows 7.5 and 8.7, 15.6 and 16.5, 22.0 and 20.8); 8 x 50 rows, 1024 -> 1024, 12.2 and 10.7.
 constexpr int kRowsForward = 32;
 constexpr int kRowsLanes = 128, kRowsPitch = kRowsLanes + 4;      // floats of a row's partial sums
 constexpr int kRowsThreads = 192;
 constexpr int kRowsSplits = 8;
-constexpr int kSms = 148;              // (what tiles and splits are counted against)
+constexpr int kSms = 148;              // a B200's, against which rules count tiles and splits (no result goes by it)
 
 struct RowsParams {
   int rows, blocks;               // blocks of N rows of a member
