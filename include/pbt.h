@@ -636,7 +636,8 @@ int pbt_dropout(const pbt_dropout_desc* desc, void* stream);
  * 1 bfloat16), products are summed in fp32.  g and u stay fp32: `kept` float [members][rows][2][hidden rounded up to 8], 16-byte aligned, is written by the
  * forward pass unless NULL and read by the backward pass, which works them out anew where it is NULL.  For bfloat16, dg and du are rounded once, as operands of
  * dx and dW.  Elements have to be aligned to their size only; bfloat16 rows that are no multiples of 16 bytes are fetched in the aligned 16-byte pieces that hold them
- * (up to 15 bytes on either side of an input are read, never used, and never beyond the piece), x and weight up to 2^34 elements of them.
+ * (up to 15 bytes on either side of an input are read, never used, and never beyond the piece), x and weight up to 2^34 elements of them; where bases and strides are multiples of
+ * 16 bytes, whatever the width, x and weight are read where they lie.
  * A dropped unit is zero, and so are its gradients, whatever g, u and dh are.  A row depends on its own row of x and its member's weight alone.
  * members <= 65535; rows, width and 2 hidden < 2^22.  rows = 0: dweight is zero.  The calls only enqueue; results are reproducible bit for bit.  Should a bounded
  * wait of a bfloat16 kernel run out, the fifth 32-bit word of status_device becomes PBT_ERR_TIMEOUT and the results are void.

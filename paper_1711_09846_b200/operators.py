@@ -551,7 +551,8 @@ class GatedUnit:
 
     weight: [members, 2 hidden, width], the gate's rows first, then the up-projection's; float32 or bfloat16, contiguous columns, any
     member and row stride (weight.expand(...): one for all members).  It is used where it lies at the call: update it in place between calls.  Its
-    storage may be replaced by one of the same shape and strides.
+    storage may be replaced by one of the same shape and strides.  A bfloat16 weight (or x) of an odd width is best held with rows padded to a multiple of
+    eight elements: others are laid out anew in every call.
     activation: "silu", "gelu" (with the error function), "relu" or "sigmoid".  The projection behind it is a plain product: grouped_gemm, or
     AdapterProjection where it is shared.
 
