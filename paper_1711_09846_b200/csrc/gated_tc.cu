@@ -165,7 +165,7 @@ __device__ __forceinline__ void drain(const TileParams& p, const TileMaps& maps,
 
 // A pair in which a wait ran out: the leader's barriers count what both CTAs load, and one of the two may be up to a ring of loads ahead.  Of these,
 // the leader's were announced for both, and the partner's part never comes; the partner's are under way and were not announced.  With both put right, every
-// load's phase ends when its copies have landed.
+// load's phase ends when its copies have landed.  (The counts are far from wrapping: 2^32 loads are 140 TB through one pair.)
 template <int STAGES, int BYTES>
 __device__ __forceinline__ void settle(uint64_t* full, uint32_t leader, uint32_t partner) {
   const uint32_t less = min(leader, partner), more = max(leader, partner);

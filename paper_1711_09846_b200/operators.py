@@ -472,9 +472,9 @@ class Dropout:
         _require(all(t.shape[0] == members and t.device == device for t in tensors), "a dropout's rate and step differ in members or device")
         places = tuple((t, t.data_ptr(), t.nbytes) for t in tensors)
         _require(members == 0 or all(at for _, at, _ in places), "a dropout's rate or step has no memory")
-        self._laid = _Rule(PbtDropRule(rates, steps, seed, step, rate, site, first_member), tensors, places, members, device)
-        self._values = values
-        return self._laid
+        laid = _Rule(PbtDropRule(rates, steps, seed, step, rate, site, first_member), tensors, places, members, device)
+        self._values, self._laid = values, laid          # (a value that is refused changes nothing)
+        return laid
 
     def _now(self) -> _Rule:
         """The rule for a call, laid out anew if a tensor's storage was replaced."""
